@@ -330,6 +330,126 @@ int prima_gemv_q4k_noalloc(const void* dev_w, int64_t rows, int64_t cols, const 
                            float* dev_y, void* stream);
 const char* prima_gemv_q4k_noalloc_error(void);
 
+/* ---- several candidate continuations over one paged cache --------------------------------------------------------
+ * Speculative decoding verifies drafted tokens (Appendix A.9, A.12); with a draft that proposes a TREE of tokens
+ * instead of a chain, one step scores all of its branches.  Beam search keeps several continuations alive.  Both need
+ * caches whose sequences share, fork and drop positions, so the cache is cut into pages.
+ *
+ * Cache: two arrays (keys, values) of the caller, [n_layers][n_pages][n_kv_heads][page_size][head_dim] in binary16 or
+ * bfloat16.  Position ("slot") j of a sequence is row j % page_size of page table[j / page_size], table being the
+ * sequence's row of a page table, and the same page serves all layers.  A cache of prima_ctx is the special case of
+ * one page of kv_capacity positions.
+ *
+ * Batch: n_seq sequences; the rows (tokens) row_begin[s] .. row_begin[s+1]-1 of the step belong to sequence s, which
+ * already holds ctx_len[s] positions, and row i of the sequence occupies slot ctx_len[s] + i.  All arrays are device
+ * memory and are read when the kernels run, so that a captured graph may be replayed with new contents (n_seq, n_tok,
+ * strides and pointers are fixed in it).  Rows from row_begin[n_seq] on are padding: nothing is written for
+ * them.  row_begin must ascend from 0 to at most n_tok.
+ *
+ * What the kernels find in device memory cannot be checked when a call is made.  A page id outside 0..n_pages-1, a
+ * slot beyond the table, a decreasing row_begin or a path entry outside the step never leads to an access outside the
+ * arrays: the kernel skips the entry (attention: treats the position as not visible) and raises a bit of the pool's
+ * status word, which prima_paged_sync reports.
+ *
+ * All calls queue their kernels on `stream` and return; none allocates, waits or keeps anything of a call for the
+ * next.  Calls on different streams are independent as far as their arrays and workspaces are.  Calls may be
+ * captured.  The pool's device is made current for the duration of a call.  Errors: PRIMA_ERR_ARG with nothing
+ * queued, the message in prima_last_error(NULL); PRIMA_ERR_CUDA. */
+#define PRIMA_DT_F32 0
+#define PRIMA_DT_F16 1
+#define PRIMA_DT_BF16 2
+
+typedef struct {
+  int32_t n_layers;
+  int32_t n_pages;
+  int32_t page_size;    /* positions per page: a power of two, 8..32768                              */
+  int32_t n_kv_heads;   /* 1..1024                                                                    */
+  int32_t head_dim;     /* 64 or 128                                                                  */
+  int32_t dtype;        /* PRIMA_DT_F16 or PRIMA_DT_BF16                                              */
+  float rope_theta;     /* > 0                                                                        */
+  int32_t rope_mode;    /* 0: rotate pairs (i, i + head_dim/2); 1: pairs (2i, 2i+1)                   */
+  int32_t device;       /* CUDA ordinal                                                               */
+} prima_paged_config;
+
+typedef struct prima_paged prima_paged; /* opaque, owned by the library */
+
+typedef struct {
+  int32_t n_seq;               /* >= 1                                                                */
+  int32_t n_tok;               /* rows of the step, padding included; >= 1                            */
+  const int32_t* row_begin;    /* dev [n_seq + 1]                                                     */
+  const int32_t* ctx_len;      /* dev [n_seq]                                                         */
+  const int32_t* table;        /* dev [n_seq][table_stride]: page ids                                 */
+  int64_t table_stride;        /* pages per row of the table, >= 1                                    */
+  const int32_t* pos;          /* dev [n_tok], or NULL: the slot.  Position that the rotation of a row uses (in a
+                                  tree: context + depth of the node)                                  */
+  const uint64_t* mask;        /* dev [n_tok][mask_words], or NULL.  Bit a (word a / 64, bit a % 64) of a row: the row
+                                  sees row a of its own sequence.  NULL: rows 0..i are visible to row i */
+  int32_t mask_words;          /* 1..16 with a mask (rows a >= 64 * mask_words of a sequence are visible to none) */
+} prima_paged_batch;
+
+/* A pool over the caller's two arrays (16-byte aligned, of the shape above), which
+ * must outlive it.  Copies a small table to the device (this call waits). */
+int prima_paged_create(const prima_paged_config* cfg, void* dev_k, void* dev_v, prima_paged** out);
+/* Waits for the device, then frees what create allocated (not the caller's arrays). */
+int prima_paged_destroy(prima_paged* pool);
+/* Waits for `stream`; PRIMA_ERR_DEVICE, once, if a kernel of this pool met a bad entry since the last call. */
+int prima_paged_sync(prima_paged* pool, void* stream);
+
+/* Rotate queries and keys and append keys and values of all rows to `layer`.  q [n_tok][n_q_heads][head_dim] (may be
+ * NULL), k, v [n_tok][n_kv_heads][head_dim]: dev, of type in_dtype (PRIMA_DT_F32 or the cache's), heads contiguous,
+ * q_stride / k_stride / v_stride elements from token to token (the three may be slices of one fused array).  Row t is
+ * turned by the angles pos_t * theta^(-2i/head_dim), evaluated as an exact fraction of a turn in 64 bits; products in
+ * 32 bits, rounded once to the cache's type.  q_out: dev [n_tok][n_q_heads][head_dim] of the cache's type, contiguous,
+ * 16-byte aligned. */
+int prima_paged_append(prima_paged* pool, int layer, const prima_paged_batch* batch, const void* q, const void* k, const void* v,
+                       int in_dtype, int n_q_heads, int64_t q_stride, int64_t k_stride, int64_t v_stride, void* q_out, void* stream);
+
+/* Attention of every row over the positions 0 .. ctx_len-1 of its sequence and over the rows of its own sequence that
+ * it sees (mask), all of which must be in the cache: out[t][h] = sum_j p_j v_j, p = softmax(scale * q . k_j), query
+ * head h reading KV head h / (n_q_heads / n_kv_heads).  q, out: dev [n_tok][n_q_heads][head_dim], contiguous, 16-byte
+ * aligned; q of the cache's type, out of type out_dtype (the cache's, or PRIMA_DT_F32).  lse: dev fp32
+ * [n_tok][n_q_heads] or NULL: log(sum_j exp(scale * q . k_j)).  A row that sees nothing yields zeros and -infinity.
+ * Positions that no row of the sequence sees are not used, whatever their bytes; keys may hold any bytes where a row
+ * does not see them.  The value of a position that some row of the sequence sees must be finite.
+ * scale > 0, finite.  n_q_heads: a multiple of n_kv_heads, at most 64 times it.  Scores, maxima and sums in 32 bits; the probabilities enter
+ * the second product in the cache's type (rounding of half a step, relative 2^-11 resp. 2^-8 of each).
+ * workspace: dev, 256-byte aligned, of at least the bytes that prima_tree_attention_workspace names for the same
+ * (n_seq, n_tok, n_q_heads); its contents before and after mean nothing; calls that may overlap need one each. */
+int64_t prima_tree_attention_workspace(const prima_paged* pool, int n_seq, int n_tok, int n_q_heads);
+int prima_tree_attention(prima_paged* pool, int layer, const prima_paged_batch* batch, const void* q, int n_q_heads, float scale,
+                         void* out, int out_dtype, float* lse, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* After a verification: the rows path[s][0 .. path_len[s]-1] of sequence s (indices into its rows of the step,
+ * strictly ascending) were accepted; their keys and values move to the slots ctx_len[s], ctx_len[s] + 1, ... in all
+ * layers.  path: dev int32 [n_seq][path_stride]; path_len: dev int32 [n_seq], 0..path_stride.  batch: row_begin,
+ * ctx_len and table are used. */
+int prima_paged_accept(prima_paged* pool, const prima_paged_batch* batch, const int32_t* path, const int32_t* path_len, int path_stride,
+                       void* stream);
+
+/* The `keep` best continuations of n_beams beams of each of n_req requests.  logits: dev [n_req][n_beams] rows of
+ * `vocab` values of type dtype (fp32, fp16, bf16), row_stride elements apart.  Candidate (b, w) of a request has the
+ * score cum[b] + log softmax(logits[b])[w], evaluated in 64 bits; a beam with finished[b] != 0 has one candidate,
+ * (b, end_token) with score cum[b].  Candidates are ordered by score, equal ones by b * vocab + w; outputs: dev
+ * score fp32, parent int32 (b), token int32 (w), each [n_req][keep], best first.  A logit of -infinity or NaN is no
+ * candidate and has no weight, +infinity counts as the largest finite fp32; a cum of -infinity or NaN leaves a beam
+ * without candidates; places for which no candidate is left get score -infinity, parent 0, token -1.  finished: dev
+ * uint8 [n_req][n_beams] or NULL (end_token is then ignored).  n_beams, keep: 1..64; n_beams * vocab < 2^31.
+ * workspace as above. */
+int64_t prima_beam_select_workspace(int n_req, int n_beams, int vocab, int keep);
+int prima_beam_select(const void* logits, int dtype, int n_req, int n_beams, int vocab, int64_t row_stride, const float* cum,
+                      const uint8_t* finished, int end_token, int keep, float* score, int32_t* parent, int32_t* token, void* workspace,
+                      int64_t workspace_bytes, void* stream);
+
+/* The reordering that follows: new row r = (request, j) of the page tables continues old row request * n_beams +
+ * parent[request][j].  table_out[r] holds its pages up to its length_in positions and -1 behind them, length_out[r]
+ * its length.  Full pages are shared.  Of the rows that continue the same old row, the first keeps the last, partly
+ * filled page; every other one gets page fresh[r] (a page that no row uses, all different), into which the length %
+ * page_size entries are copied in all layers.  table_in dev int32 [n_req * n_beams][table_stride]; table_out dev int32
+ * [n_req * keep][table_stride], not overlapping table_in; length_in / length_out likewise. */
+int prima_paged_reorder(prima_paged* pool, int n_req, int n_beams, int keep, const int32_t* table_in, int64_t table_stride,
+                        const int32_t* length_in, const int32_t* parent, const int32_t* fresh, int32_t* table_out, int32_t* length_out,
+                        void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -35,6 +35,8 @@ EXPORTS = [
     "prima_gemv_plan_destroy", "prima_gemv_q4k_noalloc", "prima_gemv_q4k_noalloc_error",
     "prima_forward_window_seqs", "prima_kv_load_seq", "prima_kv_read_seq", "prima_ctx_set_option", "prima_stream_stats",
     "prima_fmt_block_weights", "prima_fmt_block_bytes", "prima_dequant_fmt", "prima_gemv_fmt", "prima_fmt_last_error",
+    "prima_paged_create", "prima_paged_destroy", "prima_paged_sync", "prima_paged_append", "prima_paged_accept", "prima_paged_reorder",
+    "prima_tree_attention", "prima_tree_attention_workspace", "prima_beam_select", "prima_beam_select_workspace",
 ]
 
 
@@ -42,6 +44,16 @@ class ModelConfig(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("n_layers", "hidden", "n_q_heads", "n_kv_heads", "head_dim", "ffn", "vocab",
                                          "kv_capacity", "max_n_tok")] + \
                [("rms_eps", C.c_float), ("rope_theta", C.c_float), ("rope_mode", C.c_int32), ("device", C.c_int32)]
+
+
+class PagedConfig(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_layers", "n_pages", "page_size", "n_kv_heads", "head_dim", "dtype")] + \
+               [("rope_theta", C.c_float), ("rope_mode", C.c_int32), ("device", C.c_int32)]
+
+
+class PagedBatchDesc(C.Structure):
+    _fields_ = [("n_seq", C.c_int32), ("n_tok", C.c_int32), ("row_begin", C.c_void_p), ("ctx_len", C.c_void_p), ("table", C.c_void_p),
+                ("table_stride", C.c_int64), ("pos", C.c_void_p), ("mask", C.c_void_p), ("mask_words", C.c_int32)]
 
 
 class PrimaError(RuntimeError):
@@ -97,8 +109,21 @@ def lib():
         L.prima_gemv_q4k_noalloc.argtypes = [vp, i64, i64, vp, i32, vp, vp]
         L.prima_gemv_q4k_noalloc_error.argtypes = []
         L.prima_gemv_q4k_noalloc_error.restype = C.c_char_p
+        L.prima_paged_create.argtypes = [C.POINTER(PagedConfig), vp, vp, C.POINTER(vp)]
+        L.prima_paged_destroy.argtypes = [vp]
+        L.prima_paged_sync.argtypes = [vp, vp]
+        L.prima_paged_append.argtypes = [vp, i32, vp, vp, vp, vp, i32, i32, i64, i64, i64, vp, vp]
+        L.prima_paged_accept.argtypes = [vp, vp, vp, vp, i32, vp]
+        L.prima_paged_reorder.argtypes = [vp, i32, i32, i32, vp, i64, vp, vp, vp, vp, vp, vp]
+        L.prima_tree_attention.argtypes = [vp, i32, vp, vp, i32, C.c_float, vp, i32, vp, vp, i64, vp]
+        L.prima_tree_attention_workspace.argtypes = [vp, i32, i32, i32]
+        L.prima_tree_attention_workspace.restype = i64
+        L.prima_beam_select.argtypes = [vp, i32, i32, i32, i32, i64, vp, vp, i32, i32, vp, vp, vp, vp, i64, vp]
+        L.prima_beam_select_workspace.argtypes = [i32, i32, i32, i32]
+        L.prima_beam_select_workspace.restype = i64
         for name in EXPORTS:
-            if name not in ("prima_last_error", "prima_launch_count", "prima_gemv_q4k_noalloc_error", "prima_fmt_last_error"):
+            if name not in ("prima_last_error", "prima_launch_count", "prima_gemv_q4k_noalloc_error", "prima_fmt_last_error",
+                            "prima_tree_attention_workspace", "prima_beam_select_workspace"):
                 getattr(L, name).restype = C.c_int
         _lib = L
     return _lib
@@ -281,3 +306,188 @@ class Context:
 
     def last_error(self) -> str:
         return lib().prima_last_error(self._h).decode()
+
+
+# ---- several candidate continuations over one paged cache ------------------------------------------------
+DT_F32, DT_F16, DT_BF16 = 0, 1, 2
+
+
+def _dtype_code(t) -> int:
+    import torch
+    code = {torch.float32: DT_F32, torch.float16: DT_F16, torch.bfloat16: DT_BF16}.get(t.dtype)
+    if code is None:
+        raise ValueError(f"expected float32, float16 or bfloat16, got {t.dtype}")
+    return code
+
+
+def _need(t, name: str, dtype: str, shape, device):
+    """Checks a contiguous CUDA tensor of a plain argument; returns its address."""
+    if str(t.dtype) != "torch." + dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _stream_of(stream, device):
+    import torch
+    s = stream if stream is not None else torch.cuda.current_stream(device)
+    return s.cuda_stream
+
+
+def _scratch(n_bytes: int, device, stream):
+    """A workspace for one call.  It comes from torch's allocator on the stream that the call runs on, so that it is
+    reused only behind the call (and lies in the graph's own pool under capture)."""
+    import torch
+    if stream is None:
+        return torch.empty(n_bytes, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(n_bytes, dtype=torch.uint8, device=device)
+
+
+class PagedBatch:
+    """prima_paged_batch: the sequences of a step, their page tables and the rows that belong to them.
+
+    ``table`` int32 [n_seq, pages], ``row_begin`` int32 [n_seq + 1], ``ctx_len`` int32 [n_seq], ``pos`` int32 [n_tok]
+    or None, ``mask`` int64 [n_tok, words] (bits) or None: contiguous CUDA tensors, read when the kernels run.  One
+    batch serves every layer of a step."""
+
+    def __init__(self, table, row_begin, ctx_len, n_tok: int, pos=None, mask=None):
+        n_seq, dev = ctx_len.numel(), ctx_len.device
+        if table.dim() != 2 or not table.is_cuda:
+            raise ValueError("table: expected a CUDA tensor [n_seq, pages]")
+        self.device, self.n_seq, self.n_tok = dev, n_seq, int(n_tok)
+        self._keep = (table, row_begin, ctx_len, pos, mask)
+        words = 0
+        if mask is not None:
+            if mask.dim() != 2:
+                raise ValueError("mask: expected [n_tok, words]")
+            words = mask.shape[1]
+        self.desc = PagedBatchDesc(n_seq, self.n_tok, _need(row_begin, "row_begin", "int32", (n_seq + 1,), dev), _need(ctx_len, "ctx_len", "int32", (n_seq,), dev),
+                                   _need(table, "table", "int32", (n_seq, table.shape[1]), dev), table.shape[1],
+                                   _need(pos, "pos", "int32", (self.n_tok,), dev) if pos is not None else None,
+                                   _need(mask, "mask", "int64", (self.n_tok, words), dev) if mask is not None else None, words)
+        self._ref = C.byref(self.desc)
+
+
+class PagedCache:
+    """prima_paged_*: a paged cache over two caller-owned tensors [n_layers, n_pages, n_kv_heads, page_size, head_dim]."""
+
+    def __init__(self, k_pages, v_pages, rope_theta: float = 1e4, rope_mode: int = 0):
+        if k_pages.dim() != 5 or k_pages.shape != v_pages.shape or k_pages.dtype != v_pages.dtype or k_pages.device != v_pages.device:
+            raise ValueError("k_pages and v_pages: two tensors [n_layers, n_pages, n_kv_heads, page_size, head_dim] of one type on one device")
+        kp, vp = _dev_ptr(k_pages), _dev_ptr(v_pages)
+        self.n_layers, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k_pages.shape
+        self.dtype, self.device = k_pages.dtype, k_pages.device
+        self._keep = (k_pages, v_pages)
+        self._h = C.c_void_p()
+        cfg = PagedConfig(*k_pages.shape[:2], self.page_size, self.n_kv_heads, self.head_dim, _dtype_code(k_pages), rope_theta, rope_mode, self.device.index)
+        _check(lib().prima_paged_create(C.byref(cfg), kp, vp, C.byref(self._h)))
+
+    def close(self):
+        if self._h:
+            lib().prima_paged_destroy(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _rows(self, t, name: str, batch: PagedBatch):
+        """(address, elements from token to token) of [n_tok, heads, head_dim] with adjacent heads."""
+        if t.dim() != 3 or t.shape[0] != batch.n_tok or t.shape[2] != self.head_dim or t.device != self.device or \
+                t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != self.head_dim):
+            raise ValueError(f"{name}: expected [{batch.n_tok}, heads, {self.head_dim}] on {self.device} with adjacent heads, got {tuple(t.shape)} on {t.device}, strides {t.stride()}")
+        return t.data_ptr(), (t.stride(0) if batch.n_tok > 1 else t.shape[1] * self.head_dim)
+
+    def _batch(self, batch: PagedBatch):
+        if batch.device != self.device:
+            raise ValueError("the batch is on another device than the cache")
+        return batch._ref
+
+    def append(self, layer: int, batch: PagedBatch, q, k, v, q_out=None, stream=None):
+        """prima_paged_append: rotate q (or None) and k, write q_out, append k and v to ``layer``."""
+        if k.shape[1:2] != (self.n_kv_heads,) or v.shape[1:2] != (self.n_kv_heads,) or k.dtype != v.dtype or (q is not None and q.dtype != k.dtype):
+            raise ValueError(f"k and v: expected {self.n_kv_heads} heads; q, k and v of one type")
+        kp, ks = self._rows(k, "k", batch)
+        vp, vs = self._rows(v, "v", batch)
+        qp = qo = None
+        qs = heads = 0
+        if q is not None:
+            heads = q.shape[1]
+            qp, qs = self._rows(q, "q", batch)
+            if q_out is None or q_out.dtype != self.dtype:
+                raise ValueError("q_out: expected a tensor of the cache's type")
+            qo = _need(q_out, "q_out", str(self.dtype)[6:], (batch.n_tok, heads, self.head_dim), self.device)
+        _check(lib().prima_paged_append(self._h, layer, self._batch(batch), qp, kp, vp, _dtype_code(k), heads, qs, ks, vs, qo, _stream_of(stream, self.device)))
+
+    def tree_attention_workspace(self, batch: PagedBatch, n_q_heads: int = 0, stream=None):
+        """A workspace for ``tree_attention`` (for any number of query heads if none is named); calls that may overlap need one each."""
+        n = lib().prima_tree_attention_workspace(self._h, batch.n_seq, batch.n_tok, n_q_heads or 64 * self.n_kv_heads)
+        if n < 0:
+            raise PrimaError(n, "prima_tree_attention_workspace")
+        return _scratch(n, self.device, stream)
+
+    def tree_attention(self, layer: int, batch: PagedBatch, q, out, scale=None, lse=None, workspace=None, stream=None):
+        """prima_tree_attention; ``scale`` defaults to head_dim ** -0.5."""
+        if q.dim() != 3 or q.dtype != self.dtype:
+            raise ValueError("q: expected [n_tok, n_q_heads, head_dim] of the cache's type")
+        heads = q.shape[1]
+        shape = (batch.n_tok, heads, self.head_dim)
+        qp = _need(q, "q", str(self.dtype)[6:], shape, self.device)
+        op = _need(out, "out", str(out.dtype)[6:], shape, self.device)
+        lp = _need(lse, "lse", "float32", shape[:2], self.device) if lse is not None else None
+        if workspace is None:
+            workspace = self.tree_attention_workspace(batch, heads, stream)
+        _check(lib().prima_tree_attention(self._h, layer, self._batch(batch), qp, heads, scale if scale is not None else self.head_dim ** -0.5, op, _dtype_code(out), lp,
+                                          workspace.data_ptr(), workspace.numel(), _stream_of(stream, self.device)))
+
+    def accept(self, batch: PagedBatch, path, path_len, stream=None):
+        """prima_paged_accept: ``path`` int32 [n_seq, longest], ``path_len`` int32 [n_seq]."""
+        if path.dim() != 2:
+            raise ValueError("path: expected [n_seq, longest path]")
+        pp = _need(path, "path", "int32", (batch.n_seq, path.shape[1]), self.device)
+        pl = _need(path_len, "path_len", "int32", (batch.n_seq,), self.device)
+        _check(lib().prima_paged_accept(self._h, self._batch(batch), pp, pl, path.shape[1], _stream_of(stream, self.device)))
+
+    def reorder(self, table, length, parent, fresh, table_out, length_out, stream=None):
+        """prima_paged_reorder: ``parent`` int32 [n_req, keep]; ``table`` int32 [n_req * n_beams, pages]; ``fresh`` int32 [n_req * keep]."""
+        n_req, keep = parent.shape
+        rows, pages = table.shape
+        if rows % n_req:
+            raise ValueError("table: expected a row for every beam of every request")
+        dev = self.device
+        _check(lib().prima_paged_reorder(self._h, n_req, rows // n_req, keep, _need(table, "table", "int32", (rows, pages), dev), pages,
+                                         _need(length, "length", "int32", (rows,), dev), _need(parent, "parent", "int32", (n_req, keep), dev),
+                                         _need(fresh, "fresh", "int32", (n_req * keep,), dev), _need(table_out, "table_out", "int32", (n_req * keep, pages), dev),
+                                         _need(length_out, "length_out", "int32", (n_req * keep,), dev), _stream_of(stream, dev)))
+
+    def sync(self, stream=None):
+        """Waits; raises if a kernel met a bad page, slot, row or path since the last call."""
+        _check(lib().prima_paged_sync(self._h, _stream_of(stream, self.device)))
+
+
+def prima_beam_select_workspace(n_req: int, n_beams: int, vocab: int, keep: int, device=None, stream=None):
+    """A workspace for ``prima_beam_select``; calls that may overlap need one each."""
+    n = lib().prima_beam_select_workspace(n_req, n_beams, vocab, keep)
+    if n < 0:
+        raise PrimaError(n, "prima_beam_select_workspace: sizes out of range")
+    return _scratch(n, device if device is not None else "cuda", stream)
+
+
+def prima_beam_select(logits, cum, score, parent, token, finished=None, end_token: int = -1, workspace=None, stream=None):
+    """prima_beam_select: ``logits`` [n_req, n_beams, vocab] (rows may be padded), ``cum`` fp32 [n_req, n_beams],
+    outputs ``score`` fp32, ``parent`` and ``token`` int32 [n_req, keep]."""
+    if logits.dim() != 3 or not logits.is_cuda or logits.stride(2) != 1 or (logits.shape[0] > 1 and logits.stride(0) != logits.shape[1] * logits.stride(1)):
+        raise ValueError("logits: expected a CUDA tensor [n_req, n_beams, vocab] with evenly spaced rows")
+    n_req, n_beams, vocab = logits.shape
+    dev, keep = logits.device, score.shape[-1]
+    if workspace is None:
+        workspace = prima_beam_select_workspace(n_req, n_beams, vocab, keep, dev, stream)
+    stride = logits.stride(1) if n_beams > 1 else logits.stride(0) if n_req > 1 else vocab
+    import torch
+    with torch.cuda.device(dev):
+        _check(lib().prima_beam_select(logits.data_ptr(), _dtype_code(logits), n_req, n_beams, vocab, stride, _need(cum, "cum", "float32", (n_req, n_beams), dev),
+                                       _need(finished, "finished", "uint8", (n_req, n_beams), dev) if finished is not None else None, end_token, keep,
+                                       _need(score, "score", "float32", (n_req, keep), dev), _need(parent, "parent", "int32", (n_req, keep), dev),
+                                       _need(token, "token", "int32", (n_req, keep), dev), workspace.data_ptr(), workspace.numel(), _stream_of(stream, dev)))

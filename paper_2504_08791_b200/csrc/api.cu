@@ -8,6 +8,7 @@
 
 #include "../../include/prima.h"
 #include "common.cuh"
+#include "paged.cuh"
 
 using namespace prima;
 
@@ -466,6 +467,11 @@ void queue_reset(prima_ctx* c) {
 }
 
 }  // namespace
+
+namespace prima {
+int call_fail(int code, const char* what) { return fail(nullptr, code, what); }
+int call_cuda_fail(cudaError_t e, const char* what) { return cuda_fail(nullptr, e, what); }
+}  // namespace prima
 
 // =============================================================================================
 extern "C" {

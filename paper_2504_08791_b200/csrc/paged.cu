@@ -1,0 +1,397 @@
+// The paged cache: pool, rotation and append of a step's rows, accepted paths of drafted trees, reordering of beams.
+//
+// All three kernels move bytes and compute next to nothing; what bounds them is HBM for large steps and, for the small
+// ones that decoding makes, the chain of dependent reads (row_begin -> ctx_len -> table -> entry), so each keeps that
+// chain short and has everything else in flight beside it.
+#include <cmath>
+#include <cstdio>
+#include <new>
+
+#include "paged.cuh"
+
+namespace prima {
+namespace {
+
+// ---- rotation and append ----------------------------------------------------------------------------------------
+// Row t at position p: pair i of every query and key head is turned by 2 pi frac(p f_i), f_i = theta^(-2i/D) / (2 pi).
+// p f_i is formed in 64 bits (error p f_i 2^-53 turns, below 2^-24 up to p = 2^29), its whole turns are dropped and the
+// rest goes to sincospif in 32 bits.  A CTA takes kTok rows: the sines of a row are computed once, by head_dim / 2
+// threads, and serve all of its heads.  An item is 16 elements of a head: 8 pairs (two 16-byte pieces of the result).
+template <typename T, typename In, int D, int kTok>
+__global__ void __launch_bounds__(256) append_kernel(PoolView pool, BatchView b, int layer, const In* __restrict__ q, const In* __restrict__ k,
+                                                     const In* __restrict__ v, int n_q_heads, int64_t q_stride, int64_t k_stride,
+                                                     int64_t v_stride, bool wide, const double* __restrict__ freq, int mode,
+                                                     T* __restrict__ q_out) {
+  constexpr int kPairs = D / 2, kItems = D / 16;
+  __shared__ float2 s_cs[kTok][kPairs];
+  __shared__ int64_t s_row[kTok];        // row of the arrays, -1: not to be written; -2: padding
+  const int t0 = blockIdx.x * kTok;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int G = pool.n_kv_heads, heads = n_q_heads + 2 * G;
+  const int per_tok = heads * kItems;
+  const int n_items = min(kTok, b.n_tok - t0) * per_tok;
+
+  float x[2][8];
+  auto load = [&](int item) {
+    const int tk = item / per_tok, r = item - tk * per_tok;
+    const int head = r / kItems, c = r % kItems;
+    const int64_t t = t0 + tk;
+    const In* src = head < n_q_heads ? (q ? q + t * q_stride + head * D : nullptr)
+                                     : head < n_q_heads + G ? k + t * k_stride + (head - n_q_heads) * D : v + t * v_stride + (head - n_q_heads - G) * D;
+    if (!src) return;
+    if (mode == 0 && head < n_q_heads + G) {
+      load8(src + 8 * c, wide, x[0]);
+      load8(src + kPairs + 8 * c, wide, x[1]);
+    } else {
+      load8(src + 16 * c, wide, x[0]);
+      load8(src + 16 * c + 8, wide, x[1]);
+    }
+  };
+  int item = threadIdx.x;
+  if (item < n_items) load(item);        // in flight while the places are looked up
+
+  for (int tk = warp; tk < kTok; tk += 8) {
+    const int t = t0 + tk;
+    int64_t row = -2;
+    int p = 0;
+    if (t < b.n_tok) {
+      if (b.pos) p = __ldg(b.pos + t);
+      const int s = seq_of_row(b, t, lane);
+      if (s < b.n_seq) {
+        const int first = __ldg(b.row_begin + s), ctx = __ldg(b.ctx_len + s);
+        if (t < first || first < 0 || ctx < 0) {
+          if (lane == 0) raise(pool.status, kBadRows);
+          row = -2;
+        } else {
+          const int64_t slot = static_cast<int64_t>(ctx) + (t - first);
+          if (lane == 0) row = slot_row(pool, b.table + s * b.table_stride, b.table_stride, layer, slot);
+          if (!b.pos) p = static_cast<int>(slot);
+        }
+      }
+    }
+    row = __shfl_sync(0xffffffffu, row, 0);
+    if (lane == 0) s_row[tk] = row;
+    for (int i = lane; i < kPairs; i += 32) {
+      const double turns = p * __ldg(freq + i);
+      float sn, cs;
+      sincospif(static_cast<float>(2.0 * (turns - rint(turns))), &sn, &cs);
+      s_cs[tk][i] = make_float2(cs, sn);
+    }
+  }
+  __syncthreads();
+
+  for (; item < n_items; item += 256) {
+    if (item != static_cast<int>(threadIdx.x)) load(item);
+    const int tk = item / per_tok, r = item - tk * per_tok;
+    const int head = r / kItems, c = r % kItems;
+    const int64_t row = s_row[tk];
+    if (row == -2) continue;
+    const bool is_q = head < n_q_heads, is_v = head >= n_q_heads + G;
+    if (is_q && !q) continue;
+    if (!is_q && row < 0) continue;
+    T* dst = is_q ? q_out + (static_cast<int64_t>(t0 + tk) * n_q_heads + head) * D
+                  : static_cast<T*>(is_v ? pool.v : pool.k) + (row + (static_cast<int64_t>(head - n_q_heads - (is_v ? G : 0)) << pool.page_shift)) * D;
+    if (is_v) {
+      store8(dst + 16 * c, x[0]);
+      store8(dst + 16 * c + 8, x[1]);
+    } else if (mode == 0) {
+      float u[8], w[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float2 cs = s_cs[tk][8 * c + i];
+        u[i] = x[0][i] * cs.x - x[1][i] * cs.y;
+        w[i] = x[0][i] * cs.y + x[1][i] * cs.x;
+      }
+      store8(dst + 8 * c, u);
+      store8(dst + kPairs + 8 * c, w);
+    } else {
+      float u[2][8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float2 cs = s_cs[tk][8 * c + i];
+        const float a = x[i / 4][2 * (i % 4)], d = x[i / 4][2 * (i % 4) + 1];
+        u[i / 4][2 * (i % 4)] = a * cs.x - d * cs.y;
+        u[i / 4][2 * (i % 4) + 1] = a * cs.y + d * cs.x;
+      }
+      store8(dst + 16 * c, u[0]);
+      store8(dst + 16 * c + 8, u[1]);
+    }
+  }
+}
+
+// ---- accepted paths ---------------------------------------------------------------------------------------------
+// One warp per (sequence, layer, keys or values, KV head): rows path[0..n-1] of the step move to rows 0..n-1.  path
+// ascends, so path[j] >= j: a batch of up to 32 rows that is read whole before any of it is written never overwrites
+// a row that a later batch reads.
+template <int D>
+__global__ void __launch_bounds__(128) accept_kernel(PoolView pool, BatchView b, const int32_t* __restrict__ path, const int32_t* __restrict__ path_len,
+                                                     int path_stride) {
+  constexpr int kPieces = D * 2 / 16, kRows = 32 / kPieces;      // 16-byte pieces of a row, rows per warp instruction
+  const int lane = threadIdx.x & 31;
+  const int s = blockIdx.x;
+  const int G = pool.n_kv_heads;
+  const int64_t w = static_cast<int64_t>(blockIdx.y) * 4 + (threadIdx.x >> 5);
+  if (w >= static_cast<int64_t>(pool.n_layers) * 2 * G) return;
+  const int g = static_cast<int>(w % G), layer = static_cast<int>(w / G / 2);
+  uint4* const base = static_cast<uint4*>(w / G % 2 ? pool.v : pool.k);
+  const int first = __ldg(b.row_begin + s), end = __ldg(b.row_begin + s + 1), ctx = __ldg(b.ctx_len + s);
+  int n = __ldg(path_len + s);
+  if (first < 0 || end < first || end > b.n_tok || ctx < 0 || n < 0 || n > path_stride) {
+    if (lane == 0) raise(pool.status, n < 0 || n > path_stride ? kBadPath : kBadRows);
+    return;
+  }
+  for (int j0 = 0; j0 < n; j0 += 32) {
+    int64_t from = -1, to = -1;
+    if (j0 + lane < n) {
+      const int a = __ldg(path + static_cast<int64_t>(s) * path_stride + j0 + lane);
+      if (a < 0 || a >= end - first) {
+        raise(pool.status, kBadPath);
+      } else if (a != j0 + lane) {
+        const int32_t* row = b.table + s * b.table_stride;
+        from = slot_row(pool, row, b.table_stride, layer, static_cast<int64_t>(ctx) + a);
+        to = slot_row(pool, row, b.table_stride, layer, static_cast<int64_t>(ctx) + j0 + lane);
+      }
+    }
+    const int64_t shift = static_cast<int64_t>(g) << pool.page_shift;
+    uint4 x[kPieces];
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int64_t f = __shfl_sync(0xffffffffu, from, i * kRows + lane / kPieces), o = __shfl_sync(0xffffffffu, to, i * kRows + lane / kPieces);
+      if (f >= 0 && o >= 0) x[i] = __ldcg(base + (f + shift) * kPieces + lane % kPieces);
+    }
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int64_t f = __shfl_sync(0xffffffffu, from, i * kRows + lane / kPieces), o = __shfl_sync(0xffffffffu, to, i * kRows + lane / kPieces);
+      if (f >= 0 && o >= 0) base[(o + shift) * kPieces + lane % kPieces] = x[i];
+    }
+    __syncwarp();
+  }
+}
+
+// ---- reordering of beams ----------------------------------------------------------------------------------------
+// blockIdx.x = new row; the first CTA of a row writes its table and length, and one warp per (layer, keys or values,
+// KV head) copies the entries of the last page when an earlier row of the request has the same parent.  The entries
+// of one head are consecutive, (length % page_size) * head_dim * 2 bytes.
+__global__ void __launch_bounds__(128) reorder_kernel(PoolView pool, int D, int n_beams, int keep, const int32_t* __restrict__ table_in, int64_t stride,
+                                                      const int32_t* __restrict__ length_in, const int32_t* __restrict__ parent,
+                                                      const int32_t* __restrict__ fresh, int32_t* __restrict__ table_out, int32_t* __restrict__ length_out) {
+  const int r = blockIdx.x, req = r / keep, j = r - req * keep;
+  const int lane = threadIdx.x & 31;
+  const int G = pool.n_kv_heads;
+  int p = __ldg(parent + r);
+  const int f = __ldg(fresh + r);
+  bool shared_parent = false;
+  for (int i = lane; i < j; i += 32) shared_parent |= __ldg(parent + r - j + i) == p;
+  shared_parent = __any_sync(0xffffffffu, shared_parent);
+  const bool bad = p < 0 || p >= n_beams;
+  if (bad) p = 0;
+  const int64_t src = static_cast<int64_t>(req) * n_beams + p;
+  const int len = __ldg(length_in + src);
+  const int64_t pages = (static_cast<int64_t>(max(len, 0)) + (1 << pool.page_shift) - 1) >> pool.page_shift;
+  const int tail = len & ((1 << pool.page_shift) - 1);
+  const bool bad_len = len < 0 || pages > stride;
+  const int last = !bad_len && pages > 0 ? __ldg(table_in + src * stride + pages - 1) : 0;
+  const bool copies = shared_parent && tail != 0 && !bad_len;
+  const bool bad_page = copies && (static_cast<unsigned>(last) >= static_cast<unsigned>(pool.n_pages) || static_cast<unsigned>(f) >= static_cast<unsigned>(pool.n_pages));
+  if (blockIdx.y == 0) {
+    if (threadIdx.x == 0) {
+      if (bad) raise(pool.status, kBadPath);
+      if (bad_len) raise(pool.status, kBadRows);
+      if (bad_page) raise(pool.status, kBadPage);
+      length_out[r] = bad_len ? 0 : len;
+    }
+    for (int64_t i = threadIdx.x; i < stride; i += blockDim.x)
+      table_out[r * stride + i] = bad_len || i >= pages ? -1 : copies && i == pages - 1 ? f : __ldg(table_in + src * stride + i);
+  }
+  if (!copies || bad_page) return;
+  const int64_t w = static_cast<int64_t>(blockIdx.y) * 4 + (threadIdx.x >> 5);
+  if (w >= static_cast<int64_t>(pool.n_layers) * 2 * G) return;
+  const int g = static_cast<int>(w % G);
+  const int64_t layer = w / G / 2;
+  const int pieces_row = D / 8;
+  uint4* const base = static_cast<uint4*>(w / G % 2 ? pool.v : pool.k);
+  const uint4* from = base + ((((layer * pool.n_pages + last) * G + g) << pool.page_shift)) * pieces_row;
+  uint4* to = base + ((((layer * pool.n_pages + f) * G + g) << pool.page_shift)) * pieces_row;
+  const int n = tail * pieces_row;
+  int i = lane;
+  for (; i + 96 < n; i += 128) {
+    const uint4 a = __ldcg(from + i), c = __ldcg(from + i + 32), d = __ldcg(from + i + 64), e = __ldcg(from + i + 96);
+    to[i] = a;
+    to[i + 32] = c;
+    to[i + 64] = d;
+    to[i + 96] = e;
+  }
+  for (; i < n; i += 32) to[i] = __ldcg(from + i);
+}
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+template <typename T, typename In, int D>
+cudaError_t launch_append(const prima_paged& pool, const BatchView& b, int layer, const void* q, const void* k, const void* v, int n_q_heads,
+                          int64_t qs, int64_t ks, int64_t vs, void* q_out, cudaStream_t st) {
+  const int64_t per16 = 16 / static_cast<int64_t>(sizeof(In));
+  const bool wide = (!q || (aligned16(q) && qs % per16 == 0)) && aligned16(k) && aligned16(v) && ks % per16 == 0 && vs % per16 == 0;
+  // Few rows: one per CTA, for the shortest path; many: four, which share the look-up's latency.
+  const bool few = b.n_tok <= 4 * pool.sm_count;
+  auto kernel = few ? append_kernel<T, In, D, 1> : append_kernel<T, In, D, 4>;
+  const int tok = few ? 1 : 4;
+  kernel<<<(b.n_tok + tok - 1) / tok, 256, 0, st>>>(view_of(pool), b, layer, static_cast<const In*>(q), static_cast<const In*>(k),
+                                                    static_cast<const In*>(v), n_q_heads, qs, ks, vs, wide, pool.freq, pool.cfg.rope_mode,
+                                                    static_cast<T*>(q_out));
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+int check_batch(const prima_paged* pool, const prima_paged_batch* b, const char* who) {
+  char msg[160];
+  const char* bad = nullptr;
+  if (!pool || !b) bad = "null pool or batch";
+  else if (b->n_seq < 1 || b->n_tok < 1) bad = "n_seq and n_tok must be positive";
+  else if (!b->row_begin || !b->ctx_len || !b->table || b->table_stride < 1) bad = "row_begin, ctx_len and table are needed";
+  else if (b->mask && (b->mask_words < 1 || b->mask_words > 16)) bad = "mask_words outside 1..16";
+  if (!bad) return PRIMA_OK;
+  snprintf(msg, sizeof msg, "%s: %s", who, bad);
+  return call_fail(PRIMA_ERR_ARG, msg);
+}
+
+}  // namespace prima
+
+using namespace prima;
+
+extern "C" {
+
+int prima_paged_create(const prima_paged_config* cfg, void* dev_k, void* dev_v, prima_paged** out) {
+  if (out) *out = nullptr;
+  if (!cfg || !out || !dev_k || !dev_v) return call_fail(PRIMA_ERR_ARG, "prima_paged_create: null argument");
+  const prima_paged_config& c = *cfg;
+  if (c.n_layers < 1 || c.n_pages < 1 || c.page_size < 8 || c.page_size > 32768 || (c.page_size & (c.page_size - 1)) || c.n_kv_heads < 1 ||
+      c.n_kv_heads > 1024 || (c.head_dim != 64 && c.head_dim != 128) || (c.dtype != PRIMA_DT_F16 && c.dtype != PRIMA_DT_BF16) ||
+      !(c.rope_theta > 0.f) || std::isinf(c.rope_theta) || (c.rope_mode != 0 && c.rope_mode != 1) || c.device < 0)
+    return call_fail(PRIMA_ERR_ARG, "prima_paged_create: inconsistent shape");
+  if (static_cast<double>(c.n_layers) * c.n_pages * c.n_kv_heads * c.page_size >= 2147483648.0)
+    return call_fail(PRIMA_ERR_ARG, "prima_paged_create: layers * pages * heads * page_size must stay below 2^31");
+  if (!aligned16(dev_k) || !aligned16(dev_v)) return call_fail(PRIMA_ERR_ARG, "prima_paged_create: the arrays must be 16-byte aligned");
+  int n_dev = 0;
+  cudaError_t e = cudaGetDeviceCount(&n_dev);
+  if (e != cudaSuccess) return call_cuda_fail(e, "cudaGetDeviceCount");
+  if (c.device >= n_dev) return call_fail(PRIMA_ERR_ARG, "prima_paged_create: no such device");
+  CallDevice dev(c.device);
+  if (!dev.ok) return call_fail(PRIMA_ERR_CUDA, "cudaSetDevice failed");
+  prima_paged* p = new (std::nothrow) prima_paged();
+  if (!p) return call_fail(PRIMA_ERR_NOMEM, "out of host memory");
+  p->cfg = c;
+  p->k = dev_k;
+  p->v = dev_v;
+  while ((1 << p->page_shift) < c.page_size) ++p->page_shift;
+  double freq[64];
+  for (int i = 0; i < c.head_dim / 2; ++i)
+    freq[i] = std::pow(static_cast<double>(c.rope_theta), -2.0 * i / c.head_dim) / 6.283185307179586476925286766559;
+  e = cudaDeviceGetAttribute(&p->sm_count, cudaDevAttrMultiProcessorCount, c.device);
+  if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&p->freq), sizeof freq);
+  if (e == cudaSuccess) e = cudaMemcpy(p->freq, freq, sizeof(double) * c.head_dim / 2, cudaMemcpyHostToDevice);
+  if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&p->status), sizeof(int));
+  if (e == cudaSuccess) e = cudaMemset(p->status, 0, sizeof(int));
+  if (e == cudaSuccess) e = cudaDeviceSynchronize();
+  if (e != cudaSuccess) {
+    prima_paged_destroy(p);
+    return call_cuda_fail(e, "prima_paged_create");
+  }
+  *out = p;
+  return PRIMA_OK;
+}
+
+int prima_paged_destroy(prima_paged* p) {
+  if (!p) return PRIMA_OK;
+  CallDevice dev(p->cfg.device);
+  cudaDeviceSynchronize();
+  cudaFree(p->freq);
+  cudaFree(p->status);
+  delete p;
+  return PRIMA_OK;
+}
+
+int prima_paged_sync(prima_paged* p, void* stream) {
+  if (!p) return call_fail(PRIMA_ERR_ARG, "prima_paged_sync: null pool");
+  CallDevice dev(p->cfg.device);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  int status = 0;
+  cudaError_t e = cudaMemcpyAsync(&status, p->status, sizeof(int), cudaMemcpyDeviceToHost, st);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+  if (e == cudaSuccess && status) {
+    e = cudaMemsetAsync(p->status, 0, sizeof(int), st);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+  }
+  if (e != cudaSuccess) return call_cuda_fail(e, "prima_paged_sync");
+  if (!status) return PRIMA_OK;
+  char msg[200];
+  snprintf(msg, sizeof msg, "entries were skipped:%s%s%s%s%s", status & kBadPage ? " a page id outside the pool;" : "",
+           status & kBadSlot ? " a slot beyond the page table;" : "", status & kBadRows ? " bad row_begin or length;" : "",
+           status & kBadPath ? " a path entry or parent out of range;" : "", status & kGaveUp ? " a bounded wait inside a kernel gave up;" : "");
+  return call_fail(PRIMA_ERR_DEVICE, msg);
+}
+
+int prima_paged_append(prima_paged* p, int layer, const prima_paged_batch* batch, const void* q, const void* k, const void* v, int in_dtype,
+                       int n_q_heads, int64_t q_stride, int64_t k_stride, int64_t v_stride, void* q_out, void* stream) {
+  const int rc = check_batch(p, batch, "prima_paged_append");
+  if (rc != PRIMA_OK) return rc;
+  const prima_paged_config& c = p->cfg;
+  if (layer < 0 || layer >= c.n_layers) return call_fail(PRIMA_ERR_ARG, "prima_paged_append: layer out of range");
+  if (!k || !v || (q != nullptr) != (q_out != nullptr)) return call_fail(PRIMA_ERR_ARG, "prima_paged_append: null k or v, or only one of q and q_out");
+  if (in_dtype != PRIMA_DT_F32 && in_dtype != c.dtype) return call_fail(PRIMA_ERR_ARG, "prima_paged_append: in_dtype is neither fp32 nor the cache's type");
+  if (q ? n_q_heads < 1 || n_q_heads > (1 << 16) : n_q_heads != 0) return call_fail(PRIMA_ERR_ARG, "prima_paged_append: n_q_heads");
+  if (!aligned16(q_out)) return call_fail(PRIMA_ERR_ARG, "prima_paged_append: q_out must be 16-byte aligned");
+  const int64_t need_q = static_cast<int64_t>(n_q_heads) * c.head_dim, need_kv = static_cast<int64_t>(c.n_kv_heads) * c.head_dim;
+  if ((q && q_stride < need_q) || k_stride < need_kv || v_stride < need_kv) return call_fail(PRIMA_ERR_ARG, "prima_paged_append: a stride is shorter than a row");
+  CallDevice dev(c.device);
+  if (!dev.ok) return call_fail(PRIMA_ERR_CUDA, "cudaSetDevice failed");
+  const BatchView b = view_of(*batch);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  using launcher = cudaError_t (*)(const prima_paged&, const BatchView&, int, const void*, const void*, const void*, int, int64_t, int64_t, int64_t, void*, cudaStream_t);
+  static const launcher table[2][2][2] = {
+      {{launch_append<__half, float, 64>, launch_append<__half, float, 128>}, {launch_append<__half, __half, 64>, launch_append<__half, __half, 128>}},
+      {{launch_append<__nv_bfloat16, float, 64>, launch_append<__nv_bfloat16, float, 128>},
+       {launch_append<__nv_bfloat16, __nv_bfloat16, 64>, launch_append<__nv_bfloat16, __nv_bfloat16, 128>}}};
+  const cudaError_t e = table[c.dtype == PRIMA_DT_BF16][in_dtype != PRIMA_DT_F32][c.head_dim == 128](*p, b, layer, q, k, v, n_q_heads, q_stride, k_stride,
+                                                                                                  v_stride, q_out, st);
+  return e == cudaSuccess ? PRIMA_OK : call_cuda_fail(e, "prima_paged_append");
+}
+
+int prima_paged_accept(prima_paged* p, const prima_paged_batch* batch, const int32_t* path, const int32_t* path_len, int path_stride, void* stream) {
+  const int rc = check_batch(p, batch, "prima_paged_accept");
+  if (rc != PRIMA_OK) return rc;
+  if (!path || !path_len || path_stride < 1) return call_fail(PRIMA_ERR_ARG, "prima_paged_accept: path, path_len and a positive path_stride are needed");
+  CallDevice dev(p->cfg.device);
+  if (!dev.ok) return call_fail(PRIMA_ERR_CUDA, "cudaSetDevice failed");
+  const int64_t warps = static_cast<int64_t>(p->cfg.n_layers) * 2 * p->cfg.n_kv_heads;
+  if ((warps + 3) / 4 > 65535) return call_fail(PRIMA_ERR_ARG, "prima_paged_accept: layers * KV heads above 131070");
+  const dim3 grid(static_cast<unsigned>(batch->n_seq), static_cast<unsigned>((warps + 3) / 4));
+  auto kernel = p->cfg.head_dim == 128 ? accept_kernel<128> : accept_kernel<64>;
+  kernel<<<grid, 128, 0, static_cast<cudaStream_t>(stream)>>>(view_of(*p), view_of(*batch), path, path_len, path_stride);
+  const cudaError_t e = cudaGetLastError();
+  return e == cudaSuccess ? PRIMA_OK : call_cuda_fail(e, "prima_paged_accept");
+}
+
+int prima_paged_reorder(prima_paged* p, int n_req, int n_beams, int keep, const int32_t* table_in, int64_t table_stride, const int32_t* length_in,
+                        const int32_t* parent, const int32_t* fresh, int32_t* table_out, int32_t* length_out, void* stream) {
+  if (!p || !table_in || !length_in || !parent || !fresh || !table_out || !length_out)
+    return call_fail(PRIMA_ERR_ARG, "prima_paged_reorder: null argument");
+  if (n_req < 1 || n_beams < 1 || keep < 1 || n_beams > 65536 || keep > 65536 || table_stride < 1 ||
+      static_cast<int64_t>(n_req) * std::max(n_beams, keep) > 2147483647)
+    return call_fail(PRIMA_ERR_ARG, "prima_paged_reorder: bad size");
+  const int64_t rows_in = static_cast<int64_t>(n_req) * n_beams, rows_out = static_cast<int64_t>(n_req) * keep;
+  auto overlap = [](const int32_t* a, int64_t na, const int32_t* b, int64_t nb) { return a < b + nb && b < a + na; };
+  if (overlap(table_in, rows_in * table_stride, table_out, rows_out * table_stride) || overlap(length_in, rows_in, length_out, rows_out))
+    return call_fail(PRIMA_ERR_ARG, "prima_paged_reorder: the new tables overlap the old ones");
+  CallDevice dev(p->cfg.device);
+  if (!dev.ok) return call_fail(PRIMA_ERR_CUDA, "cudaSetDevice failed");
+  const int64_t warps = static_cast<int64_t>(p->cfg.n_layers) * 2 * p->cfg.n_kv_heads;
+  if ((warps + 3) / 4 > 65535) return call_fail(PRIMA_ERR_ARG, "prima_paged_reorder: layers * KV heads above 131070");
+  const dim3 grid(static_cast<unsigned>(rows_out), static_cast<unsigned>((warps + 3) / 4));
+  reorder_kernel<<<grid, 128, 0, static_cast<cudaStream_t>(stream)>>>(view_of(*p), p->cfg.head_dim, n_beams, keep, table_in, table_stride, length_in, parent,
+                                                                    fresh, table_out, length_out);
+  const cudaError_t e = cudaGetLastError();
+  return e == cudaSuccess ? PRIMA_OK : call_cuda_fail(e, "prima_paged_reorder");
+}
+
+}  // extern "C"

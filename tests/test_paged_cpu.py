@@ -1,0 +1,93 @@
+"""The paged cache without a GPU: refusals of the C entry points, and the index arithmetic compiled for the host."""
+import ctypes
+import os
+import subprocess
+
+import numpy as np
+import pytest
+
+from paper_2504_08791_b200 import binding, build
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def index(tmp_path_factory):
+    d = tmp_path_factory.mktemp("index")
+    src = d / "index.cpp"
+    src.write_text('''
+#include "%s/paper_2504_08791_b200/csrc/paged_index.h"
+extern "C" int64_t find(int layers, int pages, int shift, int heads, const int32_t* row, int64_t stride, int layer, int64_t slot) {
+  return prima::find_slot({layers, pages, shift, heads}, row, stride, layer, slot);
+}
+''' % ROOT)
+    lib = d / "index.so"
+    subprocess.run(["g++", "-O1", "-std=c++17", "-Wall", "-Werror", "-fsanitize=undefined", "-fno-sanitize-recover", "-shared", "-fPIC", str(src), "-o", str(lib)], check=True)
+    L = ctypes.CDLL(str(lib))
+    L.find.restype = ctypes.c_int64
+    L.find.argtypes = [ctypes.c_int] * 4 + [ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_int64]
+    return L
+
+
+def test_slots_of_good_and_bad_tables(index):
+    layers, pages, shift, heads = 3, 50, 4, 8
+    row = np.array([7, 49, 0, -1, 50, -2 ** 31, 2 ** 31 - 1], np.int32)
+    at = row.ctypes.data
+    for layer in range(layers):
+        for slot in range(-5, 16 * 7 + 40):
+            got = index.find(layers, pages, shift, heads, at, 7, layer, slot)
+            page = int(row[slot // 16]) if 0 <= slot < 112 else None
+            if page is None:
+                assert got == -2
+            elif not 0 <= page < pages:
+                assert got == -1
+            else:
+                assert got == ((layer * pages + page) * heads) * 16 + slot % 16
+                assert got + (heads - 1) * 16 < layers * pages * heads * 16
+    for slot in (2 ** 31, 2 ** 40, -2 ** 40, 2 ** 63 - 1, -2 ** 63):
+        assert index.find(layers, pages, shift, heads, at, 7, 0, slot) == -2
+
+
+def test_rows_of_a_large_cache_pass_32_bits_of_bytes(index):
+    # 80 layers x 3000 pages x 8 heads x 64 positions: 1.2e8 rows of 256 bytes
+    row = np.array([2999], np.int32)
+    assert index.find(80, 3000, 6, 8, row.ctypes.data, 1, 79, 63) == ((79 * 3000 + 2999) * 8) * 64 + 63
+    assert (((79 * 3000 + 2999) * 8) * 64 + 63) * 256 > 2 ** 32
+
+
+def test_refusals_need_no_gpu():
+    build.build()
+    L = binding.lib()
+    h = ctypes.c_void_p()
+    good = dict(n_layers=1, n_pages=4, page_size=16, n_kv_heads=2, head_dim=128, dtype=binding.DT_F16, rope_theta=1e4, rope_mode=0, device=0)
+
+    def create(**change):
+        c = binding.PagedConfig(*[{**good, **change}[n] for n, _ in binding.PagedConfig._fields_])
+        return L.prima_paged_create(ctypes.byref(c), 4096, 8192, ctypes.byref(h))
+    for change in (dict(n_layers=0), dict(n_pages=0), dict(page_size=4), dict(page_size=24), dict(page_size=65536), dict(n_kv_heads=0), dict(n_kv_heads=1025), dict(head_dim=96), dict(head_dim=256),
+                   dict(dtype=binding.DT_F32), dict(dtype=7), dict(rope_theta=0.0), dict(rope_theta=float("inf")), dict(rope_theta=float("nan")), dict(rope_mode=2), dict(device=-1),
+                   dict(n_pages=1 << 30), dict(n_layers=1 << 20, n_pages=1 << 20)):
+        assert create(**change) == binding.ERR_ARG, change
+        assert b"prima_paged_create" in L.prima_last_error(None)
+    c = binding.PagedConfig(*[good[n] for n, _ in binding.PagedConfig._fields_])
+    assert L.prima_paged_create(ctypes.byref(c), None, 8192, ctypes.byref(h)) == binding.ERR_ARG
+    assert L.prima_paged_create(ctypes.byref(c), 4100, 8192, ctypes.byref(h)) == binding.ERR_ARG
+    assert L.prima_paged_create(None, 4096, 8192, ctypes.byref(h)) == binding.ERR_ARG and not h.value
+    b = binding.PagedBatchDesc(1, 1, 4096, 4096, 4096, 1, None, None, 0)
+    ref = ctypes.byref(b)
+    assert L.prima_paged_append(None, 0, ref, None, 4096, 4096, 0, 0, 0, 256, 256, None, None) == binding.ERR_ARG
+    assert L.prima_paged_accept(None, ref, 4096, 4096, 1, None) == binding.ERR_ARG
+    assert L.prima_paged_reorder(None, 1, 1, 1, 4096, 1, 4096, 4096, 4096, 4096, 4096, None) == binding.ERR_ARG
+    assert L.prima_tree_attention(None, 0, ref, 4096, 2, 1.0, 4096, 1, None, 4096, 1 << 40, None) == binding.ERR_ARG
+    assert L.prima_tree_attention_workspace(None, 1, 1, 1) == binding.ERR_ARG
+    assert L.prima_paged_sync(None, None) == binding.ERR_ARG and L.prima_paged_destroy(None) == binding.OK
+    select = [4096, 0, 1, 4, 100, 100, 4096, None, 0, 4, 4096, 4096, 4096, 4096, 1 << 40, None]
+    for i, bad in ((0, None), (1, 3), (2, 0), (3, 0), (3, 65), (4, 0), (5, 99), (6, None), (9, 0), (9, 65), (10, None), (11, None), (12, None), (13, None), (13, 4224), (14, 8)):
+        args = list(select)
+        args[i] = bad
+        assert L.prima_beam_select(*args) == binding.ERR_ARG, (i, bad)
+    args = list(select)
+    args[7], args[8] = 4096, 100      # an end token outside the vocabulary
+    assert L.prima_beam_select(*args) == binding.ERR_ARG
+    assert L.prima_beam_select_workspace(1, 64, 1 << 26, 4) == binding.ERR_ARG
+    assert L.prima_beam_select_workspace(16, 8, 152064, 8) > 0
