@@ -292,6 +292,7 @@ int prima_paged_create(const prima_paged_config* cfg, void* dev_k, void* dev_v, 
   if (e == cudaSuccess) e = cudaMemcpy(p->freq, freq, sizeof(double) * c.head_dim / 2, cudaMemcpyHostToDevice);
   if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&p->status), sizeof(int));
   if (e == cudaSuccess) e = cudaMemset(p->status, 0, sizeof(int));
+  if (e == cudaSuccess) e = make_tree_maps(p);
   if (e == cudaSuccess) e = cudaDeviceSynchronize();
   if (e != cudaSuccess) {
     prima_paged_destroy(p);
@@ -307,6 +308,7 @@ int prima_paged_destroy(prima_paged* p) {
   cudaDeviceSynchronize();
   cudaFree(p->freq);
   cudaFree(p->status);
+  free_tree_maps(p);
   delete p;
   return PRIMA_OK;
 }

@@ -40,6 +40,10 @@ struct CallDevice {              // makes a device current for the duration of a
 // The checks of a batch that need no device memory; PRIMA_OK or an error that is already recorded.
 int check_batch(const prima_paged* pool, const prima_paged_batch* b, const char* who);
 
+// The tensor maps that the attention kernel's copies use (tree_attention.cu).
+cudaError_t make_tree_maps(prima_paged* pool);
+void free_tree_maps(prima_paged* pool);
+
 struct BatchView {
   int n_seq, n_tok;
   const int32_t* row_begin;

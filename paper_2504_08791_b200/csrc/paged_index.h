@@ -31,4 +31,76 @@ PRIMA_HD int64_t find_slot(const PageShape& p, const int32_t* table_row, int64_t
   return (((static_cast<int64_t>(layer) * p.n_pages + page) * p.n_kv_heads) << p.page_shift) + (slot & ((1 << p.page_shift) - 1));
 }
 
+// ---- how the work of tree attention is dealt out -------------------------------------------------------------------
+// The rows of a sequence that read one KV head (node-major: row = node * group + query head in the group) are cut into
+// tiles of kTileRows, the positions that a tile may see into units of kTilePos.  The units of all sequences, KV heads
+// and row tiles, in this order, form one line that is cut into equal shares, one per CTA, so that long and short
+// sequences balance.  A stretch of units of one (sequence, KV head, row tile) inside a share is a segment.
+constexpr int kTileRows = 256;
+constexpr int kTilePos = 128;
+
+struct TreeShape {
+  int n_kv_heads, group;     // query heads that share a KV head
+  int causal;                // no mask: row i of a sequence sees rows 0 .. i
+  int64_t capacity;          // positions that a page table row can name
+};
+
+PRIMA_HD int tree_row_tiles(const TreeShape& t, int nodes) {
+  return static_cast<int>((static_cast<int64_t>(nodes) * t.group + kTileRows - 1) / kTileRows);
+}
+// Positions 0 .. result-1 are all that the rows of tile rt may see.
+PRIMA_HD int64_t tree_kv_end(const TreeShape& t, int ctx, int nodes, int rt) {
+  int64_t seen = nodes;
+  if (t.causal) {
+    const int64_t last = (static_cast<int64_t>(rt + 1) * kTileRows + t.group - 1) / t.group;
+    if (last < seen) seen = last;
+  }
+  const int64_t end = ctx + seen;
+  return end < t.capacity ? end : t.capacity;
+}
+PRIMA_HD int64_t tree_chunks(const TreeShape& t, int ctx, int nodes, int rt) { return (tree_kv_end(t, ctx, nodes, rt) + kTilePos - 1) / kTilePos; }
+PRIMA_HD int64_t tree_units(const TreeShape& t, int ctx, int nodes) {
+  int64_t n = 0;
+  const int tiles = tree_row_tiles(t, nodes);
+  if (!t.causal || tiles <= 1) return tiles ? t.n_kv_heads * tiles * tree_chunks(t, ctx, nodes, 0) : 0;
+  for (int rt = 0; rt < tiles; ++rt) n += tree_chunks(t, ctx, nodes, rt);
+  return n * t.n_kv_heads;
+}
+// Share of CTA c of n_cta: units tree_share(c) .. tree_share(c + 1) - 1.  The CTA of unit u is the last one whose
+// share begins at or before u.
+PRIMA_HD int64_t tree_share(int64_t units, int n_cta, int c) { return units * c / n_cta; }
+PRIMA_HD int tree_cta_of(int64_t units, int n_cta, int64_t u) { return static_cast<int>(((u + 1) * n_cta - 1) / units); }
+
+struct TreeSegment {
+  int seq, head, row_tile;   // head: KV head
+  int chunk0, chunk1;        // units of this share
+  int chunks;                // units of the whole (sequence, KV head, row tile)
+};
+// The segment that starts at unit u (counted from the first unit of its sequence) and ends at or before unit u_end.
+PRIMA_HD TreeSegment tree_segment(const TreeShape& t, int seq, int ctx, int nodes, int64_t u, int64_t u_end) {
+  TreeSegment s;
+  s.seq = seq;
+  const int tiles = tree_row_tiles(t, nodes);
+  const int64_t per_head = tree_units(t, ctx, nodes) / t.n_kv_heads;
+  s.head = static_cast<int>(u / per_head);
+  int64_t r = u - s.head * per_head;
+  int64_t chunks = tree_chunks(t, ctx, nodes, 0);
+  int rt = 0;
+  if (!t.causal) {
+    rt = static_cast<int>(r / chunks);
+    r -= rt * chunks;
+  } else {
+    while (rt + 1 < tiles && r >= chunks) {
+      r -= chunks;
+      chunks = tree_chunks(t, ctx, nodes, ++rt);
+    }
+  }
+  s.row_tile = rt;
+  s.chunk0 = static_cast<int>(r);
+  s.chunks = static_cast<int>(chunks);
+  const int64_t end = r + (u_end - u);
+  s.chunk1 = static_cast<int>(end < chunks ? end : chunks);
+  return s;
+}
+
 }  // namespace prima

@@ -20,12 +20,28 @@ def index(tmp_path_factory):
 extern "C" int64_t find(int layers, int pages, int shift, int heads, const int32_t* row, int64_t stride, int layer, int64_t slot) {
   return prima::find_slot({layers, pages, shift, heads}, row, stride, layer, slot);
 }
+using namespace prima;
+extern "C" int64_t units(int heads, int group, int causal, int64_t capacity, int ctx, int nodes) { return tree_units({heads, group, causal, capacity}, ctx, nodes); }
+extern "C" int64_t kv_end(int heads, int group, int causal, int64_t capacity, int ctx, int nodes, int rt) { return tree_kv_end({heads, group, causal, capacity}, ctx, nodes, rt); }
+extern "C" int64_t share(int64_t units, int n, int c) { return tree_share(units, n, c); }
+extern "C" int cta_of(int64_t units, int n, int64_t u) { return tree_cta_of(units, n, u); }
+extern "C" void segment(int heads, int group, int causal, int64_t capacity, int seq, int ctx, int nodes, int64_t u, int64_t end, int* out) {
+  const TreeSegment s = tree_segment({heads, group, causal, capacity}, seq, ctx, nodes, u, end);
+  out[0] = s.seq; out[1] = s.head; out[2] = s.row_tile; out[3] = s.chunk0; out[4] = s.chunk1; out[5] = s.chunks;
+}
 ''' % ROOT)
     lib = d / "index.so"
     subprocess.run(["g++", "-O1", "-std=c++17", "-Wall", "-Werror", "-fsanitize=undefined", "-fno-sanitize-recover", "-shared", "-fPIC", str(src), "-o", str(lib)], check=True)
     L = ctypes.CDLL(str(lib))
     L.find.restype = ctypes.c_int64
     L.find.argtypes = [ctypes.c_int] * 4 + [ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_int64]
+    i32, i64 = ctypes.c_int, ctypes.c_int64
+    L.units.restype = L.kv_end.restype = L.share.restype = i64
+    L.units.argtypes = [i32, i32, i32, i64, i32, i32]
+    L.kv_end.argtypes = [i32, i32, i32, i64, i32, i32, i32]
+    L.share.argtypes = [i64, i32, i32]
+    L.cta_of.argtypes = [i64, i32, i64]
+    L.segment.argtypes = [i32, i32, i32, i64, i32, i32, i32, i64, i64, ctypes.c_void_p]
     return L
 
 
@@ -53,6 +69,45 @@ def test_rows_of_a_large_cache_pass_32_bits_of_bytes(index):
     row = np.array([2999], np.int32)
     assert index.find(80, 3000, 6, 8, row.ctypes.data, 1, 79, 63) == ((79 * 3000 + 2999) * 8) * 64 + 63
     assert (((79 * 3000 + 2999) * 8) * 64 + 63) * 256 > 2 ** 32
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_shares_of_tree_attention_cover_every_position_once(index, seed):
+    """The segments of all CTAs, put together, are every unit of every (sequence, KV head, row tile), once, in order."""
+    rs = np.random.RandomState(seed)
+    n_seq, heads, group, causal, n_cta = int(rs.randint(1, 30)), int(rs.choice([1, 2, 8])), int(rs.choice([1, 3, 5, 8, 64])), int(seed % 2), int(rs.choice([1, 3, 148]))
+    capacity = int(rs.choice([512, 1 << 20]))
+    ctx, nodes = rs.randint(0, 3000, n_seq), rs.choice([0, 1, 2, 16, 33, 64, 300], n_seq)
+    want = []
+    for s in range(n_seq):
+        for g in range(heads):
+            for rt in range(-(-int(nodes[s]) * group // 256)):
+                last_row = min(int(nodes[s]) * group, 256 * (rt + 1)) - 1
+                end = min(capacity, int(ctx[s]) + (last_row // group + 1 if causal else int(nodes[s])))
+                got_end = index.kv_end(heads, group, causal, capacity, int(ctx[s]), int(nodes[s]), rt)
+                assert got_end == end
+                want += [(s, g, rt, c, -(-end // 128)) for c in range(-(-end // 128))]
+    per_seq = [index.units(heads, group, causal, capacity, int(c), int(n)) for c, n in zip(ctx, nodes)]
+    total = sum(per_seq)
+    assert total == len(want)
+    if not total:
+        return
+    got = []
+    out = (ctypes.c_int * 6)()
+    for cta in range(n_cta):
+        u, end = index.share(total, n_cta, cta), index.share(total, n_cta, cta + 1)
+        assert end - u in (total // n_cta, total // n_cta + 1)
+        while u < end:
+            assert index.cta_of(total, n_cta, u) == cta
+            first, s = 0, 0
+            while u >= first + per_seq[s]:
+                first += per_seq[s]
+                s += 1
+            index.segment(heads, group, causal, capacity, s, int(ctx[s]), int(nodes[s]), u - first, end - first, out)
+            assert out[0] == s and out[4] > out[3]
+            got += [(s, out[1], out[2], c, out[5]) for c in range(out[3], out[4])]
+            u += out[4] - out[3]
+    assert got == want
 
 
 def test_refusals_need_no_gpu():
