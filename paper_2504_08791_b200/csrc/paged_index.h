@@ -66,10 +66,29 @@ PRIMA_HD int64_t tree_units(const TreeShape& t, int ctx, int nodes) {
   for (int rt = 0; rt < tiles; ++rt) n += tree_chunks(t, ctx, nodes, rt);
   return n * t.n_kv_heads;
 }
-// Share of CTA c of n_cta: units tree_share(c) .. tree_share(c + 1) - 1.  The CTA of unit u is the last one whose
-// share begins at or before u.
-PRIMA_HD int64_t tree_share(int64_t units, int n_cta, int c) { return units * c / n_cta; }
-PRIMA_HD int tree_cta_of(int64_t units, int n_cta, int64_t u) { return static_cast<int>(((u + 1) * n_cta - 1) / units); }
+// Division of non-negative numbers that are nearly always small: 64-bit division is a long subroutine on the GPU.
+PRIMA_HD int64_t div_small(int64_t a, int64_t b) {
+  return (a | b) >> 31 ? a / b : static_cast<int64_t>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b));
+}
+// Shares: CTA c of n_cta has base units, the first `more` CTAs one more.
+struct TreeShares {
+  int64_t base;
+  int more;
+};
+PRIMA_HD TreeShares tree_shares(int64_t units, int n_cta) {
+  const int64_t q = div_small(units, n_cta);
+  return {q, static_cast<int>(units - q * n_cta)};
+}
+PRIMA_HD int64_t tree_share_begin(const TreeShares& s, int c) { return s.base * c + (c < s.more ? c : s.more); }
+// The CTA whose share holds unit u.
+PRIMA_HD int tree_cta_of(const TreeShares& s, int64_t u) {
+  const int64_t long_ones = (s.base + 1) * s.more;
+  return static_cast<int>(u < long_ones ? div_small(u, s.base + 1) : s.more + div_small(u - long_ones, s.base));
+}
+
+// x / d for 0 <= x < kTileRows + 64, 1 <= d <= 64, by a multiplication with m = small_inverse(d).
+PRIMA_HD uint32_t small_inverse(int d) { return 65536u / static_cast<uint32_t>(d) + 1u; }
+PRIMA_HD int small_div(int x, uint32_t m) { return static_cast<int>(static_cast<uint32_t>(x) * m >> 16); }
 
 struct TreeSegment {
   int seq, head, row_tile;   // head: KV head
@@ -81,13 +100,13 @@ PRIMA_HD TreeSegment tree_segment(const TreeShape& t, int seq, int ctx, int node
   TreeSegment s;
   s.seq = seq;
   const int tiles = tree_row_tiles(t, nodes);
-  const int64_t per_head = tree_units(t, ctx, nodes) / t.n_kv_heads;
-  s.head = static_cast<int>(u / per_head);
+  const int64_t per_head = div_small(tree_units(t, ctx, nodes), t.n_kv_heads);
+  s.head = static_cast<int>(div_small(u, per_head));
   int64_t r = u - s.head * per_head;
   int64_t chunks = tree_chunks(t, ctx, nodes, 0);
   int rt = 0;
   if (!t.causal) {
-    rt = static_cast<int>(r / chunks);
+    rt = static_cast<int>(div_small(r, chunks));
     r -= rt * chunks;
   } else {
     while (rt + 1 < tiles && r >= chunks) {

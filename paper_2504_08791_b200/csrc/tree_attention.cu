@@ -30,11 +30,7 @@ namespace prima {
 namespace {
 
 constexpr int kSoftmaxThreads = 256;
-constexpr int kThreads = kSoftmaxThreads + 128;      // two warpgroups of softmax, one whose first two warps copy and multiply
-// Registers: 384 threads may have 168 each; the softmax threads hold a row of 128 scores and take what the others do
-// not need (256 x 208 + 128 x 80 <= 384 x 168).
-constexpr int kSoftmaxRegs = 208, kOtherRegs = 80;
-static_assert(kSoftmaxThreads * kSoftmaxRegs + (kThreads - kSoftmaxThreads) * kOtherRegs <= kThreads * 168, "the split may not exceed the launch");
+constexpr int kThreads = kSoftmaxThreads + 64;
 constexpr int kMaxSegments = 24;       // planned at a time
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
 constexpr float kSlack = 8.f;          // binary exponent by which a score may exceed the reference
@@ -65,8 +61,7 @@ struct Control {
 
 // What a CTA leaves about the segment that begins in it and goes on in later ones.
 struct TailNote {
-  int rows, row0, first, nodes, head, last_cta;
-  long long units;
+  int rows, row0, first, head, last_cta, unused[3];
 };
 
 struct TreeArgs {
@@ -75,6 +70,7 @@ struct TreeArgs {
   TreeShape shape;
   int layer, n_q_heads;
   float scale_log2;
+  uint32_t group_inverse;      // small_inverse(shape.group)
   const void* q;
   void* out;
   float* lse;
@@ -160,8 +156,9 @@ __device__ void plan(const TreeArgs& a, Control* ctl, void* scratch, long long* 
     }
     loaded = b.n_seq <= kThreads;      // the only window is in the registers
     *units = sum;
-    *u = tree_share(sum, gridDim.x, blockIdx.x);
-    *u_end = tree_share(sum, gridDim.x, blockIdx.x + 1);
+    const TreeShares shares = tree_shares(sum, gridDim.x);
+    *u = tree_share_begin(shares, blockIdx.x);
+    *u_end = tree_share_begin(shares, blockIdx.x + 1);
     if (tid == 0 && *u == *u_end) a.notes[blockIdx.x].rows = 0;
   }
   if (*u >= *u_end) {
@@ -212,10 +209,8 @@ __device__ void plan(const TreeArgs& a, Control* ctl, void* scratch, long long* 
         note.rows = s.kind == 2 ? s.rows : 0;
         note.row0 = s.row0;
         note.first = s.first;
-        note.nodes = s.nodes;
         note.head = s.head;
-        note.last_cta = tree_cta_of(*units, gridDim.x, at + (t.chunks - t.chunk0) - 1);
-        note.units = *units;
+        note.last_cta = s.kind == 2 ? tree_cta_of(tree_shares(*units, gridDim.x), at + t.chunks - 1) : 0;
       }
       at = next;
     }
@@ -285,6 +280,29 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
+// Two 32-bit operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 x, float2 y, float2 z) {
+  unsigned long long d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(*reinterpret_cast<unsigned long long*>(&x)), "l"(*reinterpret_cast<unsigned long long*>(&y)),
+      "l"(*reinterpret_cast<unsigned long long*>(&z)));
+  return *reinterpret_cast<float2*>(&d);
+}
+__device__ __forceinline__ float2 add2(float2 x, float2 y) {
+  unsigned long long d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*reinterpret_cast<unsigned long long*>(&x)), "l"(*reinterpret_cast<unsigned long long*>(&y)));
+  return *reinterpret_cast<float2*>(&d);
+}
+__device__ __forceinline__ float max_of(const uint32_t (&x)[32]) {
+  float t[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    t[c] = __uint_as_float(x[8 * c]);
+#pragma unroll
+    for (int j = 1; j < 8; ++j) t[c] = fmaxf(t[c], __uint_as_float(x[8 * c + j]));
+  }
+  return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+}
+
 // 32 columns of a row of the result, scaled.
 template <typename T>
 __device__ __forceinline__ void store_row(T* dst, const float (&x)[32]) {
@@ -302,14 +320,27 @@ __device__ __forceinline__ void store_row<float>(float* dst, const float (&x)[32
 
 // The ring holds keys and values in the order in which they are used.  In a tile of two halves both use unit t:
 // K0 V0 K1 V1 ...; where the groups take every other unit: K0 K1 V0 K2 V1 ... V(n-1).
-__device__ __forceinline__ int place_of_k(bool halves, int t, int) { return halves ? 2 * t : t == 0 ? 0 : 2 * t - 1; }
 __device__ __forceinline__ int place_of_v(bool halves, int t, int n) { return halves ? 2 * t + 1 : t == n - 1 ? 2 * n - 1 : 2 * t + 2; }
 
+// A place of the ring, stepped without divisions.
+template <int kSlots>
+struct RingPlace {
+  uint32_t slot = 0, phase = 0;
+  __device__ __forceinline__ void step(uint32_t n) {      // n <= kSlots
+    slot += n;
+    if (slot >= kSlots) {
+      slot -= kSlots;
+      phase ^= 1;
+    }
+  }
+};
+
 template <typename T, typename Out, int D>
-__global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, TreeArgs a) {
+__global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
+                                                           const __grid_constant__ TreeArgs a) {
   using Geo = Geometry<D>;
   constexpr int kSlots = Geo::kSlots;
-  constexpr bool kBf16 = sizeof(T) == 2 && !__is_same(T, __half);
+  constexpr bool kBf16 = !__is_same(T, __half);
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   uint8_t* s_q = smem;
@@ -347,177 +378,196 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
   pdl_wait();
 
   long long u = 0, u_end = -1, units = 0;
-  // running counts of this role
-  uint32_t n_places = 0;        // places of the ring used up by earlier segments
-  uint32_t n_q = 0;             // segments
+  // running state of this role
+  RingPlace<kSlots> ring;       // copies and products: the place that the segment begins with
+  uint32_t copies_before = 0;   // copies: places used so far, up to kSlots (the ring is empty at first)
+  uint32_t n_q = 0;             // products: segments
   uint32_t n_tiles[2] = {0, 0}; // units that group w has taken
 
-  if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-    do {
+  do {
     plan(a, ctl, s_q, &u, &u_end, &units);
     const int n_segments = ctl->n_segments;
+
     if (warp == 8) {
       // ---- copies ----
       const int shift = a.pool.page_shift;
       const int box_rows = min(1 << shift, kTilePos);
       const int boxes = kTilePos / box_rows;           // per 64 columns of a unit
+      const int box = lane % boxes, panel = lane / boxes;
+      const uint32_t dst = smem_u32(s_ring) + panel * Geo::kPanel + box * box_rows * 128;
       for (int si = 0; si < n_segments; ++si) {
         const Segment s = ctl->seg[si];
-        const long long limit = s.limit;
         const bool halves = s.rows > 128;
         const int n = s.chunk1 - s.chunk0;
         const int32_t* table = a.b.table + s.seq * a.b.table_stride;
-        const int box = lane % boxes, panel = lane / boxes;
-        const bool copies = panel < D / 64;
+        // A lane's row of the arrays for unit t, or -1; read one step ahead.
+        auto row_of = [&](int t) -> int64_t {
+          const long long pos = static_cast<long long>(s.chunk0 + t) * kTilePos + box * box_rows;
+          if (panel >= D / 64 || pos >= s.limit) return -1;
+          const int64_t r = find_slot(a.pool, table, a.b.table_stride, a.layer, pos);
+          if (r >= 0) return r + (static_cast<int64_t>(s.head) << shift);
+          raise(status, static_cast<int>(-r));
+          return -1;
+        };
+        int64_t row_k = row_of(0), row_v = row_k;      // of the next unit whose keys, whose values are due
+        int64_t row_mid = -1;                          // every other unit each: the unit between the two
+        int tk = 0;
         for (int p = 0; p < 2 * n; ++p) {
           const bool is_v = halves ? p & 1 : p == 2 * n - 1 || (p > 0 && !(p & 1));
-          const int t = halves ? p >> 1 : p == 0 ? 0 : p == 2 * n - 1 ? n - 1 : is_v ? p / 2 - 1 : (p + 1) / 2;
-          const long long pos = static_cast<long long>(s.chunk0 + t) * kTilePos + box * box_rows;
-          int64_t row = -1;
-          if (copies && pos < limit) {
-            const int64_t r = find_slot(a.pool, table, a.b.table_stride, a.layer, pos);
-            if (r >= 0) row = r + (static_cast<int64_t>(s.head) << shift);
-            else raise(status, static_cast<int>(-r));
-          }
-          const uint32_t place = n_places + p, slot = place % kSlots, round = place / kSlots;
+          const int64_t row = is_v ? row_v : row_k;
           const int n_copies = __popc(__ballot_sync(0xffffffffu, row >= 0));
           bool ok = true;
-          if (round > 0) ok = wait_for(bar_empty + 8 * slot, (round - 1) & 1, give_up, status);
+          if (copies_before >= kSlots) ok = wait_for(bar_empty + 8 * ring.slot, ring.phase ^ 1, give_up, status);
           ok = __all_sync(0xffffffffu, ok);
           if (ok) {
-            if (lane == 0) mbar_expect(bar_full + 8 * slot, static_cast<uint32_t>(n_copies) * box_rows * 128);
+            if (lane == 0) mbar_expect(bar_full + 8 * ring.slot, static_cast<uint32_t>(n_copies) * box_rows * 128);
             __syncwarp();
-            if (row >= 0)
-              tma_load_2d(smem_u32(s_ring) + slot * Geo::kSlotBytes + panel * Geo::kPanel + box * box_rows * 128, is_v ? &v_map : &k_map, panel * 64,
-                          static_cast<int>(row), bar_full + 8 * slot);
+            if (row >= 0) tma_load_2d(dst + ring.slot * Geo::kSlotBytes, is_v ? &v_map : &k_map, panel * 64, static_cast<int>(row), bar_full + 8 * ring.slot);
+          }
+          ring.step(1);
+          if (copies_before < kSlots) ++copies_before;
+          if (!is_v) {
+            ++tk;
+            const int64_t next = tk < n ? row_of(tk) : -1;
+            if (halves) {
+              row_mid = next;
+            } else if (tk == 1) {
+              row_mid = next;            // unit 1; row_v stays at unit 0
+            }
+            row_k = next;
+          } else if (halves) {
+            row_v = row_mid;
+          } else {
+            // the values of unit t have gone out; those of t + 1 follow, whose row was read for its keys
+            row_v = row_mid;
+            row_mid = row_k;
           }
         }
-        n_places += 2 * n;
       }
     } else if (warp == 9) {
       // ---- products ----
       if (lane == 0) {
         constexpr uint32_t kDescS = mma_f16_desc(kBf16, false, 128, kTilePos), kDescO = mma_f16_desc(kBf16, true, 128, D);
+        const uint64_t q_desc = smem_operand(smem_u32(s_q), 16), k_desc = smem_operand(smem_u32(s_ring), 16), v_desc = smem_operand(smem_u32(s_ring), Geo::kPanel);
         for (int si = 0; si < n_segments; ++si) {
-          const Segment s = ctl->seg[si];
-          const bool halves = s.rows > 128;
-          const int n = s.chunk1 - s.chunk0;
+          const bool halves = ctl->seg[si].rows > 128;
+          const int n = ctl->seg[si].chunk1 - ctl->seg[si].chunk0;
           bool ok = wait_for(bar_q, n_q & 1, give_up, status);
           ++n_q;
           tc_fence_after();
-          auto wait_place = [&](uint32_t place) { ok = wait_for(bar_full + 8 * (place % kSlots), (place / kSlots) & 1, give_up, status) && ok; };
-          auto scores = [&](int w, int t) {            // S_w = Q K_t^T
-            const uint32_t place = n_places + place_of_k(halves, t, n);
-            wait_place(place);
+          RingPlace<kSlots> pk = ring, pv = ring;      // of the next keys, the next values
+          pv.step(halves || n == 1 ? 1 : 2);
+          int tk = 0, tv = 0;
+          auto scores = [&](int w) {                   // S_w = Q K^T
+            ok = wait_for(bar_full + 8 * pk.slot, pk.phase, give_up, status) && ok;
             if (!ok) return;
-            const uint32_t kk = smem_u32(s_ring) + (place % kSlots) * Geo::kSlotBytes, qq = smem_u32(s_q) + (halves ? w : 0) * Geo::kQBytes;
+            const uint64_t kk = k_desc + pk.slot * (Geo::kSlotBytes >> 4), qq = q_desc + (halves && w ? Geo::kQBytes >> 4 : 0);
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) {
-              const uint32_t at = i / 4 * Geo::kPanel + i % 4 * 32;
-              mma_ss(tmem + w * kTilePos, smem_operand(qq + at, 16), smem_operand(kk + at, 16), kDescS, i > 0);
+              constexpr int kStep = 32 >> 4;
+              const int at = i / 4 * (Geo::kPanel >> 4) + i % 4 * kStep;
+              mma_ss(tmem + w * kTilePos, qq + at, kk + at, kDescS, i > 0);
             }
             tc_commit(bar_s + 8 * w);
-            if (!halves || w == 1) tc_commit(bar_empty + 8 * (place % kSlots));
+            if (!halves || w == 1) {
+              tc_commit(bar_empty + 8 * pk.slot);
+              pk.step(!halves && tk == 0 ? 1 : 2);
+              ++tk;
+            }
           };
-          auto outputs = [&](int w, int t, bool add) {      // O_w += P_w V_t
-            const uint32_t place = n_places + place_of_v(halves, t, n);
-            wait_place(place);
+          auto outputs = [&](int w, bool add) {        // O_w += P_w V
+            ok = wait_for(bar_full + 8 * pv.slot, pv.phase, give_up, status) && ok;
             if (!ok) return;
-            const uint32_t vv = smem_u32(s_ring) + (place % kSlots) * Geo::kSlotBytes;
+            const uint64_t vv = v_desc + pv.slot * (Geo::kSlotBytes >> 4);
 #pragma unroll
-            for (int i = 0; i < kTilePos / 16; ++i)
-              mma_ts(tmem + 256 + w * D, tmem + w * kTilePos + i * 8, smem_operand(vv + i * 16 * 128, Geo::kPanel), kDescO, add || i > 0);
+            for (int i = 0; i < kTilePos / 16; ++i) mma_ts(tmem + 256 + w * D, tmem + w * kTilePos + i * 8, vv + i * (16 * 128 >> 4), kDescO, add || i > 0);
             tc_commit(bar_pv + 8 * w);
-            if (!halves || w == 1) tc_commit(bar_empty + 8 * (place % kSlots));
+            if (!halves || w == 1) {
+              tc_commit(bar_empty + 8 * pv.slot);
+              ++tv;
+              pv.step(!halves && tv == n - 1 ? 1 : 2);
+            }
           };
-          const int n0 = halves ? n : (n + 1) / 2;
-          auto count = [&](int w) { return halves ? n : (n + 1 - w) / 2; };
-          auto unit = [&](int w, int i) { return halves ? i : 2 * i + w; };
-#pragma unroll
-          for (int w = 0; w < 2; ++w)
-            if (count(w) > 0) scores(w, unit(w, 0));
+          const int n0 = halves ? n : (n + 1) / 2, n1 = halves ? n : n / 2;
+          scores(0);
+          if (n1 > 0) scores(1);
           for (int i = 0; i < n0; ++i) {
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
-              if (i >= count(w)) continue;
+              const int count = w ? n1 : n0;
+              if (i >= count) continue;
               ok = wait_for(bar_p + 8 * w, n_tiles[w] & 1, give_up, status) && ok;
               tc_fence_after();
-              outputs(w, unit(w, i), i > 0);
-              if (i + 1 < count(w)) {
+              outputs(w, i > 0);
+              if (i + 1 < count) {
                 // P lies over S: the next scores may not be written before the product has read it
                 ok = wait_for(bar_pv + 8 * w, n_tiles[w] & 1, give_up, status) && ok;
-                scores(w, unit(w, i + 1));
+                scores(w);
               }
               ++n_tiles[w];
             }
           }
-          n_places += 2 * n;
+          for (int i = 0; i < 2 * n; i += kSlots) ring.step(min(2 * n - i, kSlots));
         }
       }
       __syncwarp();
-    }
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
-    } while (u < u_end);
-  } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
-    do {
-    plan(a, ctl, s_q, &u, &u_end, &units);
-    const int n_segments = ctl->n_segments;
-    {
+    } else {
       // ---- softmax ----
       const int w = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
       const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
       const uint32_t t_s = tmem + lanes + w * kTilePos, t_o = tmem + lanes + 256 + w * D;
-      const T* q = static_cast<const T*>(a.q);
       const int group = a.shape.group;
       for (int si = 0; si < n_segments; ++si) {
-        const Segment& s = ctl->seg[si];      // read again where it is needed: registers are short
+        const Segment& s = ctl->seg[si];      // read again where it is needed
         const bool halves = s.rows > 128;
         const int n = s.chunk1 - s.chunk0;
-        // Queries: this group's rows of the tile, or half of the only 128
-        constexpr int kPieces = D / 8;
-        const int q_rows = halves ? 128 : 64, q_tile = halves ? w : 0, q_row0 = halves ? 0 : 64 * w;
-        uint4 x[kPieces];
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-          const int idx = (tid & 127) + 128 * i, row = q_row0 + idx / kPieces, piece = idx % kPieces;
-          const int in_tile = q_tile * 128 + row;
-          x[i] = make_uint4(0, 0, 0, 0);
-          if (idx < q_rows * kPieces && in_tile < s.rows) {
-            const int gr = s.row0 + in_tile;
-            x[i] = __ldg(reinterpret_cast<const uint4*>(q + (static_cast<int64_t>(s.first + gr / group) * a.n_q_heads + s.head * group + gr % group) * D) + piece);
-          }
-        }
         auto view_of_segment = [&](bool bad_pages) {
           return SegmentView{a.b, a.pool, s.first, s.nodes, s.ctx, s.limit, a.b.table + s.seq * a.b.table_stride, bad_pages};
         };
+        // Row x of the tile: element 0 of its head in an array [n_tok][n_q_heads]
+        const int t0 = s.row0 / group, rem0 = s.row0 - t0 * group;
+        auto out_row = [&](int x) {
+          const int y = rem0 + x, t = small_div(y, a.group_inverse);
+          return static_cast<int64_t>(s.first + t0 + t) * a.n_q_heads + s.head * group + (y - t * group);
+        };
+        // Queries: this group's rows of the tile, or half of the only 128
+        constexpr int kPieces = D / 8;
+        const int q_first = 64 * w * (halves ? 2 : 1), q_rows = halves ? 128 : 64;      // rows q_first .. + q_rows of the tile
+        const T* q = static_cast<const T*>(a.q);
+        uint4 x[kPieces];
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+          const int idx = (tid & 127) + 128 * i, row = idx / kPieces, piece = idx % kPieces;
+          x[i] = make_uint4(0, 0, 0, 0);
+          if (row < q_rows && q_first + row < s.rows) x[i] = __ldg(reinterpret_cast<const uint4*>(q + out_row(q_first + row) * D) + piece);
+        }
         uint32_t bad = 0;
-        const SegmentView view = view_of_segment(false);
-        const long long pos_end = min(static_cast<long long>(s.chunk1) * kTilePos, s.limit);
-        for (long long pg = (static_cast<long long>(s.chunk0) * kTilePos >> a.pool.page_shift) + tid; (pg << a.pool.page_shift) < pos_end; pg += kSoftmaxThreads)
-          bad |= !view.page_ok(pg << a.pool.page_shift);
+        {
+          const SegmentView view = view_of_segment(false);
+          const long long pos_end = min(static_cast<long long>(s.chunk1) * kTilePos, s.limit);
+          for (long long pg = (static_cast<long long>(s.chunk0) * kTilePos >> a.pool.page_shift) + tid; (pg << a.pool.page_shift) < pos_end; pg += kSoftmaxThreads)
+            bad |= !view.page_ok(pg << a.pool.page_shift);
+        }
         // also: both groups are done with the previous segment
         asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 q, %1, 0;\nbar.red.or.pred p, 1, %2, q;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(bad) : "r"(bad), "n"(kSoftmaxThreads) : "memory");
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
-          const int idx = (tid & 127) + 128 * i, row = q_row0 + idx / kPieces, piece = idx % kPieces;
-          if (idx < q_rows * kPieces)
-            *reinterpret_cast<uint4*>(s_q + q_tile * Geo::kQBytes + piece / 8 * Geo::kPanel + row * 128 + ((piece % 8) ^ (row & 7)) * 16) = x[i];
+          const int idx = (tid & 127) + 128 * i, row = idx / kPieces, piece = idx % kPieces, in_acc = (q_first + row) & 127;
+          if (row < q_rows)
+            *reinterpret_cast<uint4*>(s_q + (halves && w ? Geo::kQBytes : 0) + piece / 8 * Geo::kPanel + in_acc * 128 + ((piece % 8) ^ (in_acc & 7)) * 16) = x[i];
         }
         fence_async_smem();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar_q);
 
-        const int my_rows = halves ? (w == 0 ? 128 : s.rows - 128) : s.rows;
+        const int in_tile = (halves ? w * 128 : 0) + r;            // this thread's row
+        const int my_rows = s.rows - (halves ? w * 128 : 0);
         const bool live = quarter * 32 < my_rows;
-        const int gr = s.row0 + (halves ? w * 128 : 0) + r;
-        const int node = r < my_rows ? gr / group : 0;
+        const int node = in_tile < s.rows ? t0 + small_div(rem0 + in_tile, a.group_inverse) : 0;
         const int count = halves ? n : (n + 1 - w) / 2;
-        float m = -INFINITY, sum = 0.f;
+        float m = -INFINITY;
+        float2 sum = make_float2(0.f, 0.f);
         for (int i = 0; i < count; ++i) {
           const int t = halves ? i : 2 * i + w;
           const long long pos0 = static_cast<long long>(s.chunk0 + t) * kTilePos;
@@ -525,75 +575,99 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
           wait_for(bar_s + 8 * w, n_tiles[w] & 1, give_up, status);
           tc_fence_after();
           if (live) {
-            uint32_t sc[4][32];
-            auto load_scores = [&]() {
-#pragma unroll
-              for (int c = 0; c < 4; ++c) tmem_load(sc[c], t_s + 32 * c);
-              tmem_wait_load();
-#pragma unroll
-              for (int c = 0; c < 4; ++c) tmem_use(sc[c]);
-              if (edge) {
-                const SegmentView view = view_of_segment(bad);
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                  const uint32_t seen = view.seen_by(node, pos0 + 32 * c);
+            uint32_t sa[32], sb[32];
+            if (i == 0 || edge) {
+              // The first reference, and -infinity where the row does not see.
+              float top = -INFINITY;
+#pragma unroll 1
+              for (int c = 0; c < 4; ++c) {
+                tmem_load(sa, t_s + 32 * c);
+                const uint32_t seen = edge ? view_of_segment(bad).seen_by(node, pos0 + 32 * c) : 0xffffffffu;
+                tmem_wait_load();
+                tmem_use(sa);
+                if (edge) {
 #pragma unroll
                   for (int j = 0; j < 32; ++j)
-                    if (!(seen >> j & 1)) sc[c][j] = 0xff800000u;
+                    if (!(seen >> j & 1)) sa[j] = 0xff800000u;
+                  tmem_store(t_s + 32 * c, sa);
                 }
+                top = fmaxf(top, max_of(sa));
               }
-            };
-            load_scores();
-            float top[4];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              top[c] = __uint_as_float(sc[c][0]);
-#pragma unroll
-              for (int j = 1; j < 32; ++j) top[c] = fmaxf(top[c], __uint_as_float(sc[c][j]));
+              if (edge) tmem_wait_store();
+              if (i == 0) m = top * a.scale_log2;
             }
-            const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale_log2;
-            if (i == 0) {
-              m = mx;
-            } else if (__any_sync(0xffffffffu, mx > m + kSlack)) {
-              const float m_new = mx > m + kSlack ? mx : m;
+            float2 shift = make_float2(m == -INFINITY ? 0.f : -m, 0.f);
+            shift.y = shift.x;
+            const float2 scale = make_float2(a.scale_log2, a.scale_log2);
+            auto rescale = [&](float top, int c) {      // a score of chunk c exceeds the reference by more than the slack
+              // A whole exponent, so that P and O are scaled without rounding.
+              const float m_new = top > m + kSlack ? (m == -INFINITY ? top : m + ceilf(top - m)) : m;
               const float f = m == m_new ? 1.f : ex2(m - m_new);
               m = m_new;
-              sum *= f;
+              shift.x = shift.y = m == -INFINITY ? 0.f : -m;
+              sum.x *= f;
+              sum.y *= f;
+              uint32_t y[16];
+              if (i > 0) {
+#pragma unroll 1
+                for (int k = 0; k < D / 16; ++k) {
+                  tmem_load(y, t_o + 16 * k);
+                  tmem_wait_load();
+                  tmem_use(y);
 #pragma unroll
-              for (int c = 0; c < D / 32; ++c) {
-                uint32_t o[32];
-                tmem_load(o, t_o + 32 * c);
-                tmem_wait_load();
-                tmem_use(o);
-#pragma unroll
-                for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-                tmem_store(t_o + 32 * c, o);
+                  for (int j = 0; j < 16; ++j) y[j] = __float_as_uint(__uint_as_float(y[j]) * f);
+                  tmem_store(t_o + 16 * k, y);
+                }
               }
-              load_scores();      // rare: cheaper than the registers that would hold them meanwhile
-            }
-            const float shift = m == -INFINITY ? 0.f : -m;
-            float part[4] = {0.f, 0.f, 0.f, 0.f};
+              tmem_wait_store();
+#pragma unroll 1
+              for (int k = 0; k < c; ++k) {
+                tmem_load(y, t_s + 16 * k);
+                tmem_wait_load();
+                tmem_use(y);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
+                for (int j = 0; j < 16; ++j) {
+                  const float2 p = Half2Of<T>::unpack(y[j]);
+                  y[j] = Half2Of<T>::pack(p.x * f, p.y * f);
+                }
+                tmem_store(t_s + 16 * k, y);
+              }
+            };
+            auto chunk = [&](const uint32_t (&sc)[32], int c) {
+              const float top = max_of(sc) * a.scale_log2;
+              if (__any_sync(0xffffffffu, top > m + kSlack)) rescale(top, c);
               uint32_t packed[16];
 #pragma unroll
               for (int j = 0; j < 16; ++j) {
-                const float p0 = ex2(fmaf(__uint_as_float(sc[c][2 * j]), a.scale_log2, shift)), p1 = ex2(fmaf(__uint_as_float(sc[c][2 * j + 1]), a.scale_log2, shift));
-                part[j & 3] += p0 + p1;
-                packed[j] = Half2Of<T>::pack(p0, p1);
+                float2 p = fma2(make_float2(__uint_as_float(sc[2 * j]), __uint_as_float(sc[2 * j + 1])), scale, shift);
+                p = make_float2(ex2(p.x), ex2(p.y));
+                sum = add2(sum, p);
+                packed[j] = Half2Of<T>::pack(p.x, p.y);
               }
               tmem_store(t_s + 16 * c, packed);
+            };
+            tmem_load(sa, t_s);
+#pragma unroll 1
+            for (int c = 0; c < 4; c += 2) {
+              tmem_wait_load();
+              tmem_use(sa);
+              tmem_load(sb, t_s + 32 * c + 32);
+              chunk(sa, c);
+              tmem_wait_load();
+              tmem_use(sb);
+              if (c == 0) tmem_load(sa, t_s + 64);
+              chunk(sb, c + 1);
             }
-            sum += (part[0] + part[1]) + (part[2] + part[3]);
             tmem_wait_store();
           }
           if (edge) {
             // Values at positions that no row sees may be anything, and 0 x NaN is NaN: clear them.
             const uint32_t seen = view_of_segment(bad).seen_by_any(pos0 + 32 * quarter, lane);
-            const uint32_t place = n_places + place_of_v(halves, t, n);
-            wait_for(bar_full + 8 * (place % kSlots), (place / kSlots) & 1, give_up, status);
+            RingPlace<kSlots> pv = ring;
+            for (int k = place_of_v(halves, t, n); k > 0; k -= kSlots) pv.step(min(k, kSlots));
+            wait_for(bar_full + 8 * pv.slot, pv.phase, give_up, status);
             if (!(seen >> lane & 1)) {
-              uint8_t* row = s_ring + (place % kSlots) * Geo::kSlotBytes + r * 128;
+              uint8_t* row = s_ring + pv.slot * Geo::kSlotBytes + r * 128;
 #pragma unroll
               for (int c = 0; c < D / 8; ++c) *reinterpret_cast<uint4*>(row + c / 8 * Geo::kPanel + c % 8 * 16) = make_uint4(0, 0, 0, 0);
             }
@@ -604,17 +678,17 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
           if (lane == 0) mbar_arrive(bar_p + 8 * w);
           ++n_tiles[w];
         }
-        n_places += 2 * n;
+        for (int k = 2 * n; k > 0; k -= kSlots) ring.step(min(k, kSlots));
         if (count > 0) {
           wait_for(bar_pv + 8 * w, (n_tiles[w] - 1) & 1, give_up, status);
           tc_fence_after();
         }
         // ---- the segment's result ----
         const bool join = !halves && n > 1;
-        float other_m = -INFINITY, other_sum = 0.f;
+        float total = sum.x + sum.y, other_m = -INFINITY, other_sum = 0.f;
         if (join) {      // group 1 hands its state to group 0 through tensor memory: the same lanes hold the same rows
           if (w == 1 && live) {
-            const uint32_t ml[2] = {__float_as_uint(m), __float_as_uint(sum)};
+            const uint32_t ml[2] = {__float_as_uint(m), __float_as_uint(total)};
             tmem_store(t_s, ml);
             tmem_wait_store();
           }
@@ -632,32 +706,38 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
         }
         if (live && (halves || w == 0)) {
           const float m_all = fmaxf(m, other_m);
-          const float f0 = m == -INFINITY ? 0.f : ex2(m - m_all), f1 = other_m == -INFINITY ? 0.f : ex2(other_m - m_all);
-          const float total = sum * f0 + other_sum * f1;
-          const float inv = total > 0.f ? 1.f / total : 0.f;
-          const int in_tile = (halves ? w * 128 : 0) + r;
-          const int64_t out_row = static_cast<int64_t>(s.first + gr / group) * a.n_q_heads + s.head * group + gr % group;
+          float f0 = m == -INFINITY ? 0.f : ex2(m - m_all), f1 = other_m == -INFINITY ? 0.f : ex2(other_m - m_all);
+          total = total * f0 + other_sum * f1;
+          if (s.kind == 0) {
+            const float inv = total > 0.f ? 1.f / total : 0.f;
+            f0 *= inv;
+            f1 *= inv;
+          }
+          const bool mine = in_tile < s.rows;
+          const int64_t at = mine ? out_row(in_tile) : 0;
           const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) + (s.kind == 2);
-#pragma unroll
+#pragma unroll 1
           for (int c = 0; c < D / 32; ++c) {
-            uint32_t o[32], o1[32];
-            tmem_load(o, t_o + 32 * c);
-            if (join) tmem_load(o1, t_o + D + 32 * c);
-            tmem_wait_load();
-            tmem_use(o);
+            uint32_t o[32];
             float y[32];
-            const float g0 = s.kind == 0 ? f0 * inv : f0, g1 = s.kind == 0 ? f1 * inv : f1;
+            tmem_load(o, t_o + 32 * c);
             if (join) {
+              uint32_t o1[32];
+              tmem_load(o1, t_o + D + 32 * c);
+              tmem_wait_load();
+              tmem_use(o);
               tmem_use(o1);
 #pragma unroll
-              for (int j = 0; j < 32; ++j) y[j] = __uint_as_float(o[j]) * g0 + __uint_as_float(o1[j]) * g1;
+              for (int j = 0; j < 32; ++j) y[j] = __uint_as_float(o[j]) * f0 + __uint_as_float(o1[j]) * f1;
             } else {
+              tmem_wait_load();
+              tmem_use(o);
 #pragma unroll
-              for (int j = 0; j < 32; ++j) y[j] = __uint_as_float(o[j]) * g0;
+              for (int j = 0; j < 32; ++j) y[j] = __uint_as_float(o[j]) * f0;
             }
-            if (r < my_rows) {
+            if (mine) {
               if (s.kind == 0) {
-                store_row(static_cast<Out*>(a.out) + out_row * D + 32 * c, y);
+                store_row(static_cast<Out*>(a.out) + at * D + 32 * c, y);
               } else {
                 float4* dst = reinterpret_cast<float4*>(a.part_o) + (slot * (D / 4) + 8 * c) * kTileRows + in_tile;
 #pragma unroll
@@ -665,9 +745,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
               }
             }
           }
-          if (r < my_rows) {
+          if (mine) {
             if (s.kind != 0) a.part_ml[slot * kTileRows + in_tile] = make_float2(m_all, total);
-            else if (a.lse) a.lse[out_row] = total > 0.f ? (m_all + log2f(total)) * kLn2 : -INFINITY;
+            else if (a.lse) a.lse[at] = total > 0.f ? (m_all + log2f(total)) * kLn2 : -INFINITY;
           }
           tc_fence_before();
         }
@@ -676,8 +756,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    } while (u < u_end);
-  }
+  } while (u < u_end);
 
   // A wait that gave up may have left products or copies under way: they end before the memory is given back.
   if (ctl->give_up) {
@@ -686,8 +765,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
       for (int i = 0; i < (1 << 22) && !mbar_test(bar_drain, 0); ++i) {}
     }
     if (tid == 8 * 32)
-      for (uint32_t p = n_places > kSlots ? n_places - kSlots : 0; p < n_places; ++p)
-        for (int i = 0; i < (1 << 16) && !mbar_test(bar_full + 8 * (p % kSlots), (p / kSlots) & 1); ++i) {}
+      for (uint32_t p = 0; p < copies_before; ++p) {      // the last places
+        ring.phase ^= ring.slot == 0;
+        ring.slot = ring.slot == 0 ? kSlots - 1 : ring.slot - 1;
+        for (int i = 0; i < (1 << 16) && !mbar_test(bar_full + 8 * ring.slot, ring.phase); ++i) {}
+      }
     __syncthreads();
   }
   if (warp == 9) tmem_free(tmem, 512);
@@ -697,24 +779,22 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
 // blockIdx.x = the CTA in which a cut segment begins, blockIdx.y = 32 of its rows; a thread owns one row and D / 8
 // columns, so that reads of the parts are contiguous across the warp.
 template <typename Out, int D>
-__global__ void __launch_bounds__(256) tree_merge_kernel(TreeArgs a, int n_cta) {
+__global__ void __launch_bounds__(256) tree_merge_kernel(const __grid_constant__ TreeArgs a) {
   pdl_trigger();
   pdl_wait();
   const TailNote note = a.notes[blockIdx.x];
   const int row = blockIdx.y * 32 + (threadIdx.x & 31), part = threadIdx.x >> 5;
   if (row >= note.rows) return;
   auto slot_of = [&](int c) { return c == static_cast<int>(blockIdx.x) ? 2 * static_cast<int64_t>(c) + 1 : 2 * static_cast<int64_t>(c); };
-  auto empty = [&](int c) { return tree_share(note.units, n_cta, c) == tree_share(note.units, n_cta, c + 1); };
   float m = -INFINITY;
   for (int c = blockIdx.x; c <= note.last_cta; ++c)
-    if (!empty(c)) m = fmaxf(m, __ldcg(&a.part_ml[slot_of(c) * kTileRows + row].x));
+    m = fmaxf(m, __ldcg(&a.part_ml[slot_of(c) * kTileRows + row].x));
   float total = 0.f;
   constexpr int kQuads = D / 32;
   float4 o[kQuads];
 #pragma unroll
   for (int i = 0; i < kQuads; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int c = blockIdx.x; c <= note.last_cta; ++c) {
-    if (empty(c)) continue;
     const float2 ml = __ldcg(&a.part_ml[slot_of(c) * kTileRows + row]);
     const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - m);
     total += ml.y * f;
@@ -764,7 +844,7 @@ cudaError_t launch_tree(const prima_paged& pool, TreeArgs a, cudaStream_t st) {
   const Maps* maps = static_cast<const Maps*>(pool.maps);
   cudaError_t e = launch_pdl(kernel, dim3(pool.sm_count), dim3(kThreads), kSmem, st, maps->k, maps->v, a);
   if (e != cudaSuccess) return e;
-  return launch_pdl(tree_merge_kernel<Out, D>, dim3(pool.sm_count, kTileRows / 32), dim3(256), 0, st, a, pool.sm_count);
+  return launch_pdl(tree_merge_kernel<Out, D>, dim3(pool.sm_count, kTileRows / 32), dim3(256), 0, st, a);
 }
 
 }  // namespace
@@ -833,6 +913,7 @@ int prima_tree_attention(prima_paged* p, int layer, const prima_paged_batch* bat
   a.layer = layer;
   a.n_q_heads = n_q_heads;
   a.scale_log2 = scale * kLog2e;
+  a.group_inverse = small_inverse(a.shape.group);
   a.q = q;
   a.out = out;
   a.lse = lse;

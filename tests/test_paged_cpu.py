@@ -23,8 +23,9 @@ extern "C" int64_t find(int layers, int pages, int shift, int heads, const int32
 using namespace prima;
 extern "C" int64_t units(int heads, int group, int causal, int64_t capacity, int ctx, int nodes) { return tree_units({heads, group, causal, capacity}, ctx, nodes); }
 extern "C" int64_t kv_end(int heads, int group, int causal, int64_t capacity, int ctx, int nodes, int rt) { return tree_kv_end({heads, group, causal, capacity}, ctx, nodes, rt); }
-extern "C" int64_t share(int64_t units, int n, int c) { return tree_share(units, n, c); }
-extern "C" int cta_of(int64_t units, int n, int64_t u) { return tree_cta_of(units, n, u); }
+extern "C" int64_t share(int64_t units, int n, int c) { return tree_share_begin(tree_shares(units, n), c); }
+extern "C" int cta_of(int64_t units, int n, int64_t u) { return tree_cta_of(tree_shares(units, n), u); }
+extern "C" int small(int x, int d) { return small_div(x, small_inverse(d)); }
 extern "C" void segment(int heads, int group, int causal, int64_t capacity, int seq, int ctx, int nodes, int64_t u, int64_t end, int* out) {
   const TreeSegment s = tree_segment({heads, group, causal, capacity}, seq, ctx, nodes, u, end);
   out[0] = s.seq; out[1] = s.head; out[2] = s.row_tile; out[3] = s.chunk0; out[4] = s.chunk1; out[5] = s.chunks;
@@ -69,6 +70,23 @@ def test_rows_of_a_large_cache_pass_32_bits_of_bytes(index):
     row = np.array([2999], np.int32)
     assert index.find(80, 3000, 6, 8, row.ctypes.data, 1, 79, 63) == ((79 * 3000 + 2999) * 8) * 64 + 63
     assert (((79 * 3000 + 2999) * 8) * 64 + 63) * 256 > 2 ** 32
+
+
+def test_division_by_the_group(index):
+    for d in range(1, 65):
+        for x in range(256 + 64):
+            assert index.small(x, d) == x // d
+
+
+def test_shares_of_many_units(index):
+    for total in (1, 147, 148, 149, 2 ** 31 - 1, 2 ** 31, 2 ** 40 + 12345):
+        for cta in (0, 1, 77, 147):
+            a, b = index.share(total, 148, cta), index.share(total, 148, cta + 1)
+            assert b - a in (total // 148, total // 148 + 1)
+            for u in {a, b - 1}:
+                if a <= u < b:
+                    assert index.cta_of(total, 148, u) == cta
+        assert index.share(total, 148, 0) == 0 and index.share(total, 148, 148) == total
 
 
 @pytest.mark.parametrize("seed", range(12))
