@@ -30,7 +30,8 @@ namespace prima {
 namespace {
 
 constexpr int kSoftmaxThreads = 256;
-constexpr int kThreads = kSoftmaxThreads + 64;
+constexpr int kThreads = kSoftmaxThreads + 96;
+constexpr int kSub = 64;               // positions whose scores are in tensor memory at a time, per group and buffer
 constexpr int kMaxSegments = 24;       // planned at a time
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
 constexpr float kSlack = 8.f;          // binary exponent by which a score may exceed the reference
@@ -51,7 +52,7 @@ struct Segment {
 };
 
 struct Control {
-  unsigned long long full[12], empty[12], s_ready[2], p_ready[2], pv_done[2], q_ready, drained;
+  unsigned long long full[12], empty[12], s_ready[4], p_ready[4], pv_done[4], q_ready, drained[2];      // [group][buffer]
   uint32_t tmem;
   int give_up;
   int n_segments, found;
@@ -318,10 +319,6 @@ __device__ __forceinline__ void store_row<float>(float* dst, const float (&x)[32
   for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(dst + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
 }
 
-// The ring holds keys and values in the order in which they are used.  In a tile of two halves both use unit t:
-// K0 V0 K1 V1 ...; where the groups take every other unit: K0 K1 V0 K2 V1 ... V(n-1).
-__device__ __forceinline__ int place_of_v(bool halves, int t, int n) { return halves ? 2 * t + 1 : t == n - 1 ? 2 * n - 1 : 2 * t + 2; }
-
 // A place of the ring, stepped without divisions.
 template <int kSlots>
 struct RingPlace {
@@ -348,7 +345,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
   Control* ctl = reinterpret_cast<Control*>(s_ring + kSlots * Geo::kSlotBytes);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t bar_full = smem_u32(ctl->full), bar_empty = smem_u32(ctl->empty), bar_s = smem_u32(ctl->s_ready), bar_p = smem_u32(ctl->p_ready),
-                 bar_pv = smem_u32(ctl->pv_done), bar_q = smem_u32(&ctl->q_ready), bar_drain = smem_u32(&ctl->drained);
+                 bar_pv = smem_u32(ctl->pv_done), bar_q = smem_u32(&ctl->q_ready), bar_drain = smem_u32(ctl->drained);
   int* const give_up = &ctl->give_up;
   int* const status = a.pool.status;
 
@@ -356,15 +353,16 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
   if (tid == 0) {
     for (int i = 0; i < kSlots; ++i) {
       mbar_init(bar_full + 8 * i, 1);
-      mbar_init(bar_empty + 8 * i, 1);
+      mbar_init(bar_empty + 8 * i, 2);
     }
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < 4; ++i) {
       mbar_init(bar_s + 8 * i, 1);
       mbar_init(bar_p + 8 * i, 4);
       mbar_init(bar_pv + 8 * i, 1);
     }
     mbar_init(bar_q, 8);
     mbar_init(bar_drain, 1);
+    mbar_init(bar_drain + 8, 1);
     ctl->give_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     tma_prefetch_map(&k_map);
@@ -382,7 +380,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
   RingPlace<kSlots> ring;       // copies and products: the place that the segment begins with
   uint32_t copies_before = 0;   // copies: places used so far, up to kSlots (the ring is empty at first)
   uint32_t n_q = 0;             // products: segments
-  uint32_t n_tiles[2] = {0, 0}; // units that group w has taken
+  uint32_t n_sub = 0;           // sub-tiles of this thread's group; sub-tile i uses buffer i % 2
 
   do {
     plan(a, ctl, s_q, &u, &u_end, &units);
@@ -400,7 +398,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
         const bool halves = s.rows > 128;
         const int n = s.chunk1 - s.chunk0;
         const int32_t* table = a.b.table + s.seq * a.b.table_stride;
-        // A lane's row of the arrays for unit t, or -1; read one step ahead.
+        // A lane's row of the arrays for unit t, or -1
         auto row_of = [&](int t) -> int64_t {
           const long long pos = static_cast<long long>(s.chunk0 + t) * kTilePos + box * box_rows;
           if (panel >= D / 64 || pos >= s.limit) return -1;
@@ -409,105 +407,87 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
           raise(status, static_cast<int>(-r));
           return -1;
         };
-        int64_t row_k = row_of(0), row_v = row_k;      // of the next unit whose keys, whose values are due
-        int64_t row_mid = -1;                          // every other unit each: the unit between the two
-        int tk = 0;
-        for (int p = 0; p < 2 * n; ++p) {
-          const bool is_v = halves ? p & 1 : p == 2 * n - 1 || (p > 0 && !(p & 1));
-          const int64_t row = is_v ? row_v : row_k;
+        int64_t row = row_of(0);
+        for (int t = 0; t < n; ++t) {
           const int n_copies = __popc(__ballot_sync(0xffffffffu, row >= 0));
-          bool ok = true;
-          if (copies_before >= kSlots) ok = wait_for(bar_empty + 8 * ring.slot, ring.phase ^ 1, give_up, status);
-          ok = __all_sync(0xffffffffu, ok);
-          if (ok) {
-            if (lane == 0) mbar_expect(bar_full + 8 * ring.slot, static_cast<uint32_t>(n_copies) * box_rows * 128);
-            __syncwarp();
-            if (row >= 0) tma_load_2d(dst + ring.slot * Geo::kSlotBytes, is_v ? &v_map : &k_map, panel * 64, static_cast<int>(row), bar_full + 8 * ring.slot);
-          }
-          ring.step(1);
-          if (copies_before < kSlots) ++copies_before;
-          if (!is_v) {
-            ++tk;
-            const int64_t next = tk < n ? row_of(tk) : -1;
-            if (halves) {
-              row_mid = next;
-            } else if (tk == 1) {
-              row_mid = next;            // unit 1; row_v stays at unit 0
+#pragma unroll
+          for (int is_v = 0; is_v < 2; ++is_v) {
+            bool ok = true;
+            if (copies_before >= kSlots) ok = wait_for(bar_empty + 8 * ring.slot, ring.phase ^ 1, give_up, status);
+            ok = __all_sync(0xffffffffu, ok);
+            if (ok) {
+              if (lane == 0) mbar_expect(bar_full + 8 * ring.slot, static_cast<uint32_t>(n_copies) * box_rows * 128);
+              __syncwarp();
+              if (row >= 0) tma_load_2d(dst + ring.slot * Geo::kSlotBytes, is_v ? &v_map : &k_map, panel * 64, static_cast<int>(row), bar_full + 8 * ring.slot);
             }
-            row_k = next;
-          } else if (halves) {
-            row_v = row_mid;
-          } else {
-            // the values of unit t have gone out; those of t + 1 follow, whose row was read for its keys
-            row_v = row_mid;
-            row_mid = row_k;
+            ring.step(1);
+            if (copies_before < kSlots) ++copies_before;
           }
+          if (t + 1 < n) row = row_of(t + 1);
         }
       }
-    } else if (warp == 9) {
-      // ---- products ----
+    } else if (warp >= 9) {
+      // ---- products: one thread per group, so that neither waits for the other's softmax ----
       if (lane == 0) {
-        constexpr uint32_t kDescS = mma_f16_desc(kBf16, false, 128, kTilePos), kDescO = mma_f16_desc(kBf16, true, 128, D);
-        const uint64_t q_desc = smem_operand(smem_u32(s_q), 16), k_desc = smem_operand(smem_u32(s_ring), 16), v_desc = smem_operand(smem_u32(s_ring), Geo::kPanel);
+        const int w = warp - 9;
+        constexpr uint32_t kDescS = mma_f16_desc(kBf16, false, 128, kSub), kDescO = mma_f16_desc(kBf16, true, 128, D);
+        const uint32_t t_s = tmem + w * 2 * kSub, t_o = tmem + 256 + w * D;
+        const uint64_t k_desc = smem_operand(smem_u32(s_ring), 16), v_desc = smem_operand(smem_u32(s_ring), Geo::kPanel);
         for (int si = 0; si < n_segments; ++si) {
           const bool halves = ctl->seg[si].rows > 128;
-          const int n = ctl->seg[si].chunk1 - ctl->seg[si].chunk0;
+          const int n = ctl->seg[si].chunk1 - ctl->seg[si].chunk0, count = halves ? 2 * n : n;
+          const uint64_t q_desc = smem_operand(smem_u32(s_q) + (halves && w ? Geo::kQBytes : 0), 16);
           bool ok = wait_for(bar_q, n_q & 1, give_up, status);
           ++n_q;
           tc_fence_after();
-          RingPlace<kSlots> pk = ring, pv = ring;      // of the next keys, the next values
-          pv.step(halves || n == 1 ? 1 : 2);
-          int tk = 0, tv = 0;
-          auto scores = [&](int w) {                   // S_w = Q K^T
-            ok = wait_for(bar_full + 8 * pk.slot, pk.phase, give_up, status) && ok;
+          RingPlace<kSlots> pk = ring, pv = ring;      // of the unit whose keys, whose values are due
+          pv.step(1);
+          // Sub-tile j: half w of unit j, or half j % 2 of unit j / 2
+          auto scores = [&](int j) {                   // S = Q K^T
+            const int half = halves ? j & 1 : w;
+            if (!halves || half == 0) ok = wait_for(bar_full + 8 * pk.slot, pk.phase, give_up, status) && ok;
             if (!ok) return;
-            const uint64_t kk = k_desc + pk.slot * (Geo::kSlotBytes >> 4), qq = q_desc + (halves && w ? Geo::kQBytes >> 4 : 0);
+            const uint32_t buffer = (n_sub + j) & 1;
+            const uint64_t kk = k_desc + pk.slot * (Geo::kSlotBytes >> 4) + half * (kSub * 128 >> 4);
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) {
-              constexpr int kStep = 32 >> 4;
-              const int at = i / 4 * (Geo::kPanel >> 4) + i % 4 * kStep;
-              mma_ss(tmem + w * kTilePos, qq + at, kk + at, kDescS, i > 0);
+              const int at = i / 4 * (Geo::kPanel >> 4) + i % 4 * (32 >> 4);
+              mma_ss(t_s + buffer * kSub, q_desc + at, kk + at, kDescS, i > 0);
             }
-            tc_commit(bar_s + 8 * w);
-            if (!halves || w == 1) {
+            tc_commit(bar_s + 8 * (2 * w + buffer));
+            if (!halves || half == 1) {
               tc_commit(bar_empty + 8 * pk.slot);
-              pk.step(!halves && tk == 0 ? 1 : 2);
-              ++tk;
+              pk.step(2);
             }
           };
-          auto outputs = [&](int w, bool add) {        // O_w += P_w V
-            ok = wait_for(bar_full + 8 * pv.slot, pv.phase, give_up, status) && ok;
+          auto outputs = [&](int j) {                  // O += P V
+            const int half = halves ? j & 1 : w;
+            if (!halves || half == 0) ok = wait_for(bar_full + 8 * pv.slot, pv.phase, give_up, status) && ok;
+            const uint32_t buffer = (n_sub + j) & 1;
+            ok = wait_for(bar_p + 8 * (2 * w + buffer), (n_sub + j) >> 1 & 1, give_up, status) && ok;
             if (!ok) return;
-            const uint64_t vv = v_desc + pv.slot * (Geo::kSlotBytes >> 4);
+            tc_fence_after();
+            const uint64_t vv = v_desc + pv.slot * (Geo::kSlotBytes >> 4) + half * (kSub * 128 >> 4);
 #pragma unroll
-            for (int i = 0; i < kTilePos / 16; ++i) mma_ts(tmem + 256 + w * D, tmem + w * kTilePos + i * 8, vv + i * (16 * 128 >> 4), kDescO, add || i > 0);
-            tc_commit(bar_pv + 8 * w);
-            if (!halves || w == 1) {
+            for (int i = 0; i < kSub / 16; ++i) mma_ts(t_o, t_s + buffer * kSub + i * 8, vv + i * (16 * 128 >> 4), kDescO, j > 0 || i > 0);
+            tc_commit(bar_pv + 8 * (2 * w + buffer));
+            if (!halves || half == 1) {
               tc_commit(bar_empty + 8 * pv.slot);
-              ++tv;
-              pv.step(!halves && tv == n - 1 ? 1 : 2);
+              pv.step(2);
             }
           };
-          const int n0 = halves ? n : (n + 1) / 2, n1 = halves ? n : n / 2;
           scores(0);
-          if (n1 > 0) scores(1);
-          for (int i = 0; i < n0; ++i) {
-#pragma unroll
-            for (int w = 0; w < 2; ++w) {
-              const int count = w ? n1 : n0;
-              if (i >= count) continue;
-              ok = wait_for(bar_p + 8 * w, n_tiles[w] & 1, give_up, status) && ok;
-              tc_fence_after();
-              outputs(w, i > 0);
-              if (i + 1 < count) {
-                // P lies over S: the next scores may not be written before the product has read it
-                ok = wait_for(bar_pv + 8 * w, n_tiles[w] & 1, give_up, status) && ok;
-                scores(w);
-              }
-              ++n_tiles[w];
+          if (count > 1) scores(1);
+          for (int j = 0; j < count; ++j) {
+            outputs(j);
+            if (j + 2 < count) {
+              // P lies over S: the next scores of this buffer may not be written before the product has read it
+              ok = wait_for(bar_pv + 8 * (2 * w + ((n_sub + j) & 1)), (n_sub + j) >> 1 & 1, give_up, status) && ok;
+              scores(j + 2);
             }
           }
-          for (int i = 0; i < 2 * n; i += kSlots) ring.step(min(2 * n - i, kSlots));
+          n_sub += count;
+          for (int k = 2 * n; k > 0; k -= kSlots) ring.step(min(k, kSlots));
         }
       }
       __syncwarp();
@@ -515,7 +495,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
       // ---- softmax ----
       const int w = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
       const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
-      const uint32_t t_s = tmem + lanes + w * kTilePos, t_o = tmem + lanes + 256 + w * D;
+      const uint32_t t_s = tmem + lanes + w * 2 * kSub, t_o = tmem + lanes + 256 + w * D;
       const int group = a.shape.group;
       for (int si = 0; si < n_segments; ++si) {
         const Segment& s = ctl->seg[si];      // read again where it is needed
@@ -565,126 +545,99 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
         const int my_rows = s.rows - (halves ? w * 128 : 0);
         const bool live = quarter * 32 < my_rows;
         const int node = in_tile < s.rows ? t0 + small_div(rem0 + in_tile, a.group_inverse) : 0;
-        const int count = halves ? n : (n + 1 - w) / 2;
+        const int count = halves ? 2 * n : n;
         float m = -INFINITY;
         float2 sum = make_float2(0.f, 0.f);
-        for (int i = 0; i < count; ++i) {
-          const int t = halves ? i : 2 * i + w;
-          const long long pos0 = static_cast<long long>(s.chunk0 + t) * kTilePos;
-          const bool edge = pos0 + kTilePos > s.ctx || bad;
-          wait_for(bar_s + 8 * w, n_tiles[w] & 1, give_up, status);
+        for (int j = 0; j < count; ++j, ++n_sub) {
+          const int t = halves ? j >> 1 : j, half = halves ? j & 1 : w;
+          const long long pos0 = static_cast<long long>(s.chunk0 + t) * kTilePos + half * kSub;
+          const bool edge = pos0 + kSub > s.ctx || bad;
+          const uint32_t buffer = n_sub & 1, phase = n_sub >> 1 & 1;
+          wait_for(bar_s + 8 * (2 * w + buffer), phase, give_up, status);
           tc_fence_after();
           if (live) {
-            uint32_t sa[32], sb[32];
-            if (i == 0 || edge) {
-              // The first reference, and -infinity where the row does not see.
-              float top = -INFINITY;
-#pragma unroll 1
-              for (int c = 0; c < 4; ++c) {
-                tmem_load(sa, t_s + 32 * c);
-                const uint32_t seen = edge ? view_of_segment(bad).seen_by(node, pos0 + 32 * c) : 0xffffffffu;
-                tmem_wait_load();
-                tmem_use(sa);
-                if (edge) {
+            uint32_t sc[2][32];
 #pragma unroll
-                  for (int j = 0; j < 32; ++j)
-                    if (!(seen >> j & 1)) sa[j] = 0xff800000u;
-                  tmem_store(t_s + 32 * c, sa);
-                }
-                top = fmaxf(top, max_of(sa));
-              }
-              if (edge) tmem_wait_store();
-              if (i == 0) m = top * a.scale_log2;
+            for (int c = 0; c < 2; ++c) tmem_load(sc[c], t_s + buffer * kSub + 32 * c);
+            uint32_t seen[2] = {0xffffffffu, 0xffffffffu};
+            if (edge) {
+              const SegmentView view = view_of_segment(bad);
+              seen[0] = view.seen_by(node, pos0);
+              seen[1] = view.seen_by(node, pos0 + 32);
             }
-            float2 shift = make_float2(m == -INFINITY ? 0.f : -m, 0.f);
-            shift.y = shift.x;
-            const float2 scale = make_float2(a.scale_log2, a.scale_log2);
-            auto rescale = [&](float top, int c) {      // a score of chunk c exceeds the reference by more than the slack
-              // A whole exponent, so that P and O are scaled without rounding.
-              const float m_new = top > m + kSlack ? (m == -INFINITY ? top : m + ceilf(top - m)) : m;
+            tmem_wait_load();
+#pragma unroll
+            for (int c = 0; c < 2; ++c) tmem_use(sc[c]);
+            if (edge) {
+#pragma unroll
+              for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int k = 0; k < 32; ++k)
+                  if (!(seen[c] >> k & 1)) sc[c][k] = 0xff800000u;
+            }
+            const float top = fmaxf(max_of(sc[0]), max_of(sc[1])) * a.scale_log2;
+            if (j == 0) {
+              m = top;
+            } else if (__any_sync(0xffffffffu, top > m + kSlack)) {
+              const float m_new = top > m + kSlack ? top : m;
               const float f = m == m_new ? 1.f : ex2(m - m_new);
               m = m_new;
-              shift.x = shift.y = m == -INFINITY ? 0.f : -m;
               sum.x *= f;
               sum.y *= f;
-              uint32_t y[16];
-              if (i > 0) {
+              // the product of the sub-tile before, which may still be adding to O
+              wait_for(bar_pv + 8 * (2 * w + (buffer ^ 1)), (n_sub - 1) >> 1 & 1, give_up, status);
+              tc_fence_after();
 #pragma unroll 1
-                for (int k = 0; k < D / 16; ++k) {
-                  tmem_load(y, t_o + 16 * k);
-                  tmem_wait_load();
-                  tmem_use(y);
-#pragma unroll
-                  for (int j = 0; j < 16; ++j) y[j] = __float_as_uint(__uint_as_float(y[j]) * f);
-                  tmem_store(t_o + 16 * k, y);
-                }
-              }
-              tmem_wait_store();
-#pragma unroll 1
-              for (int k = 0; k < c; ++k) {
-                tmem_load(y, t_s + 16 * k);
+              for (int k = 0; k < D / 16; ++k) {
+                uint32_t y[16];
+                tmem_load(y, t_o + 16 * k);
                 tmem_wait_load();
                 tmem_use(y);
 #pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                  const float2 p = Half2Of<T>::unpack(y[j]);
-                  y[j] = Half2Of<T>::pack(p.x * f, p.y * f);
-                }
-                tmem_store(t_s + 16 * k, y);
+                for (int i = 0; i < 16; ++i) y[i] = __float_as_uint(__uint_as_float(y[i]) * f);
+                tmem_store(t_o + 16 * k, y);
               }
-            };
-            auto chunk = [&](const uint32_t (&sc)[32], int c) {
-              const float top = max_of(sc) * a.scale_log2;
-              if (__any_sync(0xffffffffu, top > m + kSlack)) rescale(top, c);
-              uint32_t packed[16];
+            }
+            const float2 scale = make_float2(a.scale_log2, a.scale_log2), shift = m == -INFINITY ? make_float2(0.f, 0.f) : make_float2(-m, -m);
+            uint32_t packed[32];
 #pragma unroll
-              for (int j = 0; j < 16; ++j) {
-                float2 p = fma2(make_float2(__uint_as_float(sc[2 * j]), __uint_as_float(sc[2 * j + 1])), scale, shift);
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+              for (int k = 0; k < 16; ++k) {
+                float2 p = fma2(make_float2(__uint_as_float(sc[c][2 * k]), __uint_as_float(sc[c][2 * k + 1])), scale, shift);
                 p = make_float2(ex2(p.x), ex2(p.y));
                 sum = add2(sum, p);
-                packed[j] = Half2Of<T>::pack(p.x, p.y);
+                packed[16 * c + k] = Half2Of<T>::pack(p.x, p.y);
               }
-              tmem_store(t_s + 16 * c, packed);
-            };
-            tmem_load(sa, t_s);
-#pragma unroll 1
-            for (int c = 0; c < 4; c += 2) {
-              tmem_wait_load();
-              tmem_use(sa);
-              tmem_load(sb, t_s + 32 * c + 32);
-              chunk(sa, c);
-              tmem_wait_load();
-              tmem_use(sb);
-              if (c == 0) tmem_load(sa, t_s + 64);
-              chunk(sb, c + 1);
-            }
+            tmem_store(t_s + buffer * kSub, packed);
             tmem_wait_store();
           }
           if (edge) {
             // Values at positions that no row sees may be anything, and 0 x NaN is NaN: clear them.
-            const uint32_t seen = view_of_segment(bad).seen_by_any(pos0 + 32 * quarter, lane);
+            const uint32_t seen = view_of_segment(bad).seen_by_any(pos0 + (r & 32), lane);
             RingPlace<kSlots> pv = ring;
-            for (int k = place_of_v(halves, t, n); k > 0; k -= kSlots) pv.step(min(k, kSlots));
+            for (int k = 2 * t + 1; k > 0; k -= kSlots) pv.step(min(k, kSlots));
             wait_for(bar_full + 8 * pv.slot, pv.phase, give_up, status);
             if (!(seen >> lane & 1)) {
-              uint8_t* row = s_ring + pv.slot * Geo::kSlotBytes + r * 128;
+              uint8_t* row = s_ring + pv.slot * Geo::kSlotBytes + (half * kSub + (r & 63)) * 128;
+              constexpr int kHalfRow = D / 16;      // 16-byte pieces
 #pragma unroll
-              for (int c = 0; c < D / 8; ++c) *reinterpret_cast<uint4*>(row + c / 8 * Geo::kPanel + c % 8 * 16) = make_uint4(0, 0, 0, 0);
+              for (int c = 0; c < kHalfRow; ++c) {
+                const int piece = (r >> 6) * kHalfRow + c;
+                *reinterpret_cast<uint4*>(row + piece / 8 * Geo::kPanel + piece % 8 * 16) = make_uint4(0, 0, 0, 0);
+              }
             }
             fence_async_smem();
           }
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(bar_p + 8 * w);
-          ++n_tiles[w];
+          if (lane == 0) mbar_arrive(bar_p + 8 * (2 * w + buffer));
         }
         for (int k = 2 * n; k > 0; k -= kSlots) ring.step(min(k, kSlots));
-        if (count > 0) {
-          wait_for(bar_pv + 8 * w, (n_tiles[w] - 1) & 1, give_up, status);
-          tc_fence_after();
-        }
+        wait_for(bar_pv + 8 * (2 * w + ((n_sub - 1) & 1)), (n_sub - 1) >> 1 & 1, give_up, status);
+        tc_fence_after();
         // ---- the segment's result ----
-        const bool join = !halves && n > 1;
+        const bool join = !halves;
         float total = sum.x + sum.y, other_m = -INFINITY, other_sum = 0.f;
         if (join) {      // group 1 hands its state to group 0 through tensor memory: the same lanes hold the same rows
           if (w == 1 && live) {
@@ -697,7 +650,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
           tc_fence_after();
           if (w == 0 && live) {
             uint32_t ml[2];
-            tmem_load(ml, t_s + kTilePos);
+            tmem_load(ml, t_s + 2 * kSub);
             tmem_wait_load();
             tmem_use(ml);
             other_m = __uint_as_float(ml[0]);
@@ -760,9 +713,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
 
   // A wait that gave up may have left products or copies under way: they end before the memory is given back.
   if (ctl->give_up) {
-    if (tid == 9 * 32) {
-      tc_commit(bar_drain);
-      for (int i = 0; i < (1 << 22) && !mbar_test(bar_drain, 0); ++i) {}
+    if (warp >= 9 && lane == 0) {
+      tc_commit(bar_drain + 8 * (warp - 9));
+      for (int i = 0; i < (1 << 22) && !mbar_test(bar_drain + 8 * (warp - 9), 0); ++i) {}
     }
     if (tid == 8 * 32)
       for (uint32_t p = 0; p < copies_before; ++p) {      // the last places
