@@ -45,21 +45,36 @@ __device__ __forceinline__ void tmem_wait_store() { asm volatile("tcgen05.wait::
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
+// One lane of a converged warp, the same one every time; what it guards is known to be uniform.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t ok;
+  asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(ok));
+  return ok != 0;
+}
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(0xffffffffu, x, 0); }
+
+// An operand in shared memory: its descriptor, whose upper half is the same for all of them.  The MMA takes its
+// descriptors from uniform registers: with per-thread arithmetic in between, an instruction costs the issuing thread
+// over 70 cycles instead of a few.
+struct SmemOperand {
+  uint32_t lo, hi;
+  __device__ __forceinline__ SmemOperand operator+(uint32_t bytes) const { return {lo + (bytes >> 4), hi}; }
+};
 // D (tensor memory, fp32) (+)= A (shared memory) x B (shared memory).
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
-  asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a), "l"(b), "r"(idesc),
+__device__ __forceinline__ void mma_ss(uint32_t d, SmemOperand a, SmemOperand b, uint32_t idesc, bool add) {
+  asm volatile("{\n.reg .pred p;\n.reg .b64 a, b;\nsetp.ne.b32 p, %6, 0;\nmov.b64 a, {%1, %2};\nmov.b64 b, {%3, %4};\n"
+               "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %5, p;\n}" ::"r"(d), "r"(a.lo), "r"(a.hi), "r"(b.lo), "r"(b.hi), "r"(idesc),
                "r"(static_cast<uint32_t>(add)) : "memory");
 }
 // D (+)= A (tensor memory, two 16-bit values per column) x B (shared memory).
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
-  asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a), "l"(b), "r"(idesc),
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, SmemOperand b, uint32_t idesc, bool add) {
+  asm volatile("{\n.reg .pred p;\n.reg .b64 b;\nsetp.ne.b32 p, %5, 0;\nmov.b64 b, {%2, %3};\n"
+               "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n}" ::"r"(d), "r"(a), "r"(b.lo), "r"(b.hi), "r"(idesc),
                "r"(static_cast<uint32_t>(add)) : "memory");
 }
 // Descriptor of an operand in shared memory: rows of 128 bytes in the 128-byte swizzle, groups of 8 rows 1024 bytes
 // apart; lead: bytes from one block of 64 columns to the next (used where the columns are the M or N axis).
-__device__ __forceinline__ uint64_t smem_operand(uint32_t addr, uint32_t lead) {
-  return static_cast<uint64_t>((addr & 0x3ffff) >> 4) | static_cast<uint64_t>(lead >> 4) << 16 | static_cast<uint64_t>(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
-}
+__device__ __forceinline__ SmemOperand smem_operand(uint32_t addr, uint32_t lead) { return {addr >> 4 | (lead >> 4) << 16, (1024 >> 4) | 1u << 14 | 2u << 29}; }
 // kind::f16 instruction descriptor: fp32 accumulator, A with K innermost; `bf16` or binary16; B with K (b_mn = false)
 // or N innermost.
 __host__ __device__ constexpr uint32_t mma_f16_desc(bool bf16, bool b_mn, int m, int n) {

@@ -395,7 +395,6 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
       const uint32_t dst = smem_u32(s_ring) + panel * Geo::kPanel + box * box_rows * 128;
       for (int si = 0; si < n_segments; ++si) {
         const Segment s = ctl->seg[si];
-        const bool halves = s.rows > 128;
         const int n = s.chunk1 - s.chunk0;
         const int32_t* table = a.b.table + s.seq * a.b.table_stride;
         // A lane's row of the arrays for unit t, or -1
@@ -427,70 +426,67 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
         }
       }
     } else if (warp >= 9) {
-      // ---- products: one thread per group, so that neither waits for the other's softmax ----
-      if (lane == 0) {
-        const int w = warp - 9;
-        constexpr uint32_t kDescS = mma_f16_desc(kBf16, false, 128, kSub), kDescO = mma_f16_desc(kBf16, true, 128, D);
-        const uint32_t t_s = tmem + w * 2 * kSub, t_o = tmem + 256 + w * D;
-        const uint64_t k_desc = smem_operand(smem_u32(s_ring), 16), v_desc = smem_operand(smem_u32(s_ring), Geo::kPanel);
-        for (int si = 0; si < n_segments; ++si) {
-          const bool halves = ctl->seg[si].rows > 128;
-          const int n = ctl->seg[si].chunk1 - ctl->seg[si].chunk0, count = halves ? 2 * n : n;
-          const uint64_t q_desc = smem_operand(smem_u32(s_q) + (halves && w ? Geo::kQBytes : 0), 16);
-          bool ok = wait_for(bar_q, n_q & 1, give_up, status);
-          ++n_q;
+      // ---- products: one warp per group, so that neither waits for the other's softmax ----
+      const uint32_t w = uniform(warp) - 9;
+      constexpr uint32_t kDescS = mma_f16_desc(kBf16, false, 128, kSub), kDescO = mma_f16_desc(kBf16, true, 128, D);
+      const uint32_t u_tmem = uniform(tmem), t_s = u_tmem + w * 2 * kSub, t_o = u_tmem + 256 + w * D;
+      const uint32_t ring_addr = uniform(smem_u32(s_ring)), q_addr = uniform(smem_u32(s_q));
+      const SmemOperand k_all = smem_operand(ring_addr, 16), v_all = smem_operand(ring_addr, Geo::kPanel);
+      for (int si = 0; si < n_segments; ++si) {
+        const bool halves = uniform(ctl->seg[si].rows) > 128;
+        const int n = uniform(ctl->seg[si].chunk1 - ctl->seg[si].chunk0), count = halves ? 2 * n : n;
+        const SmemOperand qq = smem_operand(q_addr + (halves ? w * Geo::kQBytes : 0), 16);
+        bool ok = wait_for(bar_q, n_q & 1, give_up, status);
+        ++n_q;
+        RingPlace<kSlots> pk = ring, pv = ring;      // of the unit whose keys, whose values are due
+        pv.step(1);
+        // Sub-tile j: half w of unit j, or half j % 2 of unit j / 2
+        auto scores = [&](int j) {                   // S = Q K^T
+          const uint32_t half = halves ? j & 1 : w;
+          if (!halves || half == 0) ok = wait_for(bar_full + 8 * pk.slot, pk.phase, give_up, status) && ok;
+          const bool last = !halves || half == 1;
           tc_fence_after();
-          RingPlace<kSlots> pk = ring, pv = ring;      // of the unit whose keys, whose values are due
-          pv.step(1);
-          // Sub-tile j: half w of unit j, or half j % 2 of unit j / 2
-          auto scores = [&](int j) {                   // S = Q K^T
-            const int half = halves ? j & 1 : w;
-            if (!halves || half == 0) ok = wait_for(bar_full + 8 * pk.slot, pk.phase, give_up, status) && ok;
-            if (!ok) return;
+          if (__all_sync(0xffffffffu, ok) && elect_one()) {
             const uint32_t buffer = (n_sub + j) & 1;
-            const uint64_t kk = k_desc + pk.slot * (Geo::kSlotBytes >> 4) + half * (kSub * 128 >> 4);
+            const SmemOperand kk = k_all + (pk.slot * Geo::kSlotBytes + half * (kSub * 128));
 #pragma unroll
-            for (int i = 0; i < D / 16; ++i) {
-              const int at = i / 4 * (Geo::kPanel >> 4) + i % 4 * (32 >> 4);
-              mma_ss(t_s + buffer * kSub, q_desc + at, kk + at, kDescS, i > 0);
-            }
+            for (int i = 0; i < D / 16; ++i) mma_ss(t_s + buffer * kSub, qq + (i / 4 * Geo::kPanel + i % 4 * 32), kk + (i / 4 * Geo::kPanel + i % 4 * 32), kDescS, i > 0);
             tc_commit(bar_s + 8 * (2 * w + buffer));
-            if (!halves || half == 1) {
-              tc_commit(bar_empty + 8 * pk.slot);
-              pk.step(2);
-            }
-          };
-          auto outputs = [&](int j) {                  // O += P V
-            const int half = halves ? j & 1 : w;
-            if (!halves || half == 0) ok = wait_for(bar_full + 8 * pv.slot, pv.phase, give_up, status) && ok;
-            const uint32_t buffer = (n_sub + j) & 1;
-            ok = wait_for(bar_p + 8 * (2 * w + buffer), (n_sub + j) >> 1 & 1, give_up, status) && ok;
-            if (!ok) return;
-            tc_fence_after();
-            const uint64_t vv = v_desc + pv.slot * (Geo::kSlotBytes >> 4) + half * (kSub * 128 >> 4);
-#pragma unroll
-            for (int i = 0; i < kSub / 16; ++i) mma_ts(t_o, t_s + buffer * kSub + i * 8, vv + i * (16 * 128 >> 4), kDescO, j > 0 || i > 0);
-            tc_commit(bar_pv + 8 * (2 * w + buffer));
-            if (!halves || half == 1) {
-              tc_commit(bar_empty + 8 * pv.slot);
-              pv.step(2);
-            }
-          };
-          scores(0);
-          if (count > 1) scores(1);
-          for (int j = 0; j < count; ++j) {
-            outputs(j);
-            if (j + 2 < count) {
-              // P lies over S: the next scores of this buffer may not be written before the product has read it
-              ok = wait_for(bar_pv + 8 * (2 * w + ((n_sub + j) & 1)), (n_sub + j) >> 1 & 1, give_up, status) && ok;
-              scores(j + 2);
-            }
+            if (last) tc_commit(bar_empty + 8 * pk.slot);
           }
-          n_sub += count;
-          for (int k = 2 * n; k > 0; k -= kSlots) ring.step(min(k, kSlots));
+          __syncwarp();
+          if (last) pk.step(2);
+        };
+        auto outputs = [&](int j) {                  // O += P V
+          const uint32_t half = halves ? j & 1 : w;
+          if (!halves || half == 0) ok = wait_for(bar_full + 8 * pv.slot, pv.phase, give_up, status) && ok;
+          const bool last = !halves || half == 1;
+          const uint32_t buffer = (n_sub + j) & 1;
+          ok = wait_for(bar_p + 8 * (2 * w + buffer), (n_sub + j) >> 1 & 1, give_up, status) && ok;
+          tc_fence_after();
+          if (__all_sync(0xffffffffu, ok) && elect_one()) {
+            const SmemOperand vv = v_all + (pv.slot * Geo::kSlotBytes + half * (kSub * 128));
+#pragma unroll
+            for (int i = 0; i < kSub / 16; ++i) mma_ts(t_o, t_s + buffer * kSub + i * 8, vv + i * (16 * 128), kDescO, j > 0 || i > 0);
+            tc_commit(bar_pv + 8 * (2 * w + buffer));
+            if (last) tc_commit(bar_empty + 8 * pv.slot);
+          }
+          __syncwarp();
+          if (last) pv.step(2);
+        };
+        scores(0);
+        if (count > 1) scores(1);
+        for (int j = 0; j < count; ++j) {
+          outputs(j);
+          if (j + 2 < count) {
+            // P lies over S: the next scores of this buffer may not be written before the product has read it
+            ok = wait_for(bar_pv + 8 * (2 * w + ((n_sub + j) & 1)), (n_sub + j) >> 1 & 1, give_up, status) && ok;
+            scores(j + 2);
+          }
         }
+        n_sub += count;
+        for (int k = 2 * n; k > 0; k -= kSlots) ring.step(min(k, kSlots));
       }
-      __syncwarp();
     } else {
       // ---- softmax ----
       const int w = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
