@@ -30,9 +30,12 @@ namespace prima {
 namespace {
 
 constexpr int kSoftmaxThreads = 256;
-constexpr int kThreads = kSoftmaxThreads + 96;
-constexpr int kSub = 64;               // positions whose scores are in tensor memory at a time, per group and buffer
-constexpr int kMaxSegments = 24;       // planned at a time
+constexpr int kThreads = kSoftmaxThreads + 128;      // two warpgroups of softmax; one of copies, products (two warps) and an idle warp
+// Registers: 384 threads may have 168 each; the softmax threads hold a row of 128 scores and take what the others do
+// not need.
+constexpr int kSoftmaxRegs = 208, kOtherRegs = 80;
+static_assert(kSoftmaxThreads * kSoftmaxRegs + (kThreads - kSoftmaxThreads) * kOtherRegs <= kThreads * 168, "the split may not exceed the launch");
+constexpr int kSegments = 4;           // planned ahead
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
 constexpr float kSlack = 8.f;          // binary exponent by which a score may exceed the reference
 
@@ -46,18 +49,23 @@ template <int D> struct Geometry {
 struct Segment {
   int seq, head, row0, rows;           // rows row0 .. row0 + rows - 1 of the (sequence, KV head)
   int first, nodes, ctx;               // the sequence: first row of the step, rows, cached positions
-  int chunk0, chunk1;
+  int chunk0, n;                       // first unit and their number
   int kind;                            // 0: whole; 1: continues; 2: begins here and goes on
   long long limit;                     // positions that the tile may see
+  __device__ __forceinline__ bool halves() const { return rows > 128; }
+  // Units of group w, and the i-th of them
+  __device__ __forceinline__ int count(int w) const { return halves() ? n : (n + 1 - w) >> 1; }
+  __device__ __forceinline__ int unit(int w, int i) const { return halves() ? i : 2 * i + w; }
 };
 
 struct Control {
-  unsigned long long full[12], empty[12], s_ready[4], p_ready[4], pv_done[4], q_ready, drained[2];      // [group][buffer]
+  unsigned long long full[12], empty[12], s_ready[2], p_ready[4], pv_done[2], q_ready, drained[2];      // of each group; p_ready: of each half of its unit
+  unsigned long long seg_full[kSegments], seg_empty[kSegments];
+  Segment seg[kSegments];              // n = 0: no more
   uint32_t tmem;
   int give_up;
-  int n_segments, found;
-  long long unit;
-  Segment seg[kMaxSegments];
+  int bad[16];                         // of the last units: some page is none (the ring holds at most six)
+  float2 ml[128];                      // reference and sum of group 1's rows
 };
 
 // What a CTA leaves about the segment that begins in it and goes on in later ones.
@@ -90,137 +98,87 @@ __device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, int* giv
   return false;
 }
 
-// ---- planning -------------------------------------------------------------------------------------------------------
-// Lengths of a sequence; nodes = 0 for one whose entries make no sense.
-__device__ __forceinline__ bool sequence(const BatchView& b, int i, int* first, int* nodes, int* ctx) {
-  const int f = __ldg(b.row_begin + i), e = __ldg(b.row_begin + i + 1), c = __ldg(b.ctx_len + i);
-  const bool ok = f >= 0 && e >= f && e <= b.n_tok && c >= 0;
-  *first = f;
-  *nodes = ok ? e - f : 0;
-  *ctx = c;
-  return ok;
+// The hand-over of segments, which goes on after a wait has given up elsewhere (nothing else may be left waiting).
+__device__ __forceinline__ bool wait_segment(uint32_t bar, uint32_t parity) {
+  for (int i = 0; i < (1 << 24); ++i)
+    if (mbar_test(bar, parity)) return true;
+  return false;
 }
 
-// Exclusive prefix sum of v over the CTA and the total; s_warp: one word per warp and one more.
-__device__ __forceinline__ long long block_scan(long long v, long long* s_warp, long long* total) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  long long x = v;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const long long y = __shfl_up_sync(0xffffffffu, x, o);
-    if (lane >= o) x += y;
-  }
-  if (lane == 31) s_warp[warp] = x;
-  __syncthreads();
-  long long before = 0, all = 0;
-#pragma unroll
-  for (int w = 0; w < kThreads / 32; ++w) {
-    const long long y = s_warp[w];
-    if (w < warp) before += y;
-    all += y;
-  }
-  __syncthreads();
-  *total = all;
-  return before + x - v;
-}
-
-// Fills ctl->seg with the next segments of this CTA's share; the whole CTA calls it.  `scratch` is shared memory that
-// nothing else uses meanwhile.  On the first call *u_end < 0: the share is worked out too.
-__device__ void plan(const TreeArgs& a, Control* ctl, void* scratch, long long* u, long long* u_end, long long* units) {
-  struct Window { long long prefix[kThreads + 1]; int first[kThreads], nodes[kThreads], ctx[kThreads]; };
-  long long* s_warp = static_cast<long long*>(scratch);
-  Window* w = reinterpret_cast<Window*>(s_warp + 16);
-  const int tid = threadIdx.x;
-  const BatchView& b = a.b;
+// ---- this CTA's share, segment by segment -----------------------------------------------------------------------------
+// One warp walks the share, 32 sequences at a time, one per lane, and hands the segments to the others ahead of time.
+struct Cursor {
+  const TreeArgs& a;
+  const int lane;
+  long long total = 0, u = 0, u_end = 0;
+  int w0 = 0;                                  // first sequence of the window
+  long long window = 0, before = 0, units = 0; // of the window; of the lane's sequence: units in front of it, its own
   int first = 0, nodes = 0, ctx = 0;
-  long long mine = 0, before = 0, total = 0;
-  auto load = [&](int w0) {
-    const int i = w0 + tid;
-    mine = 0;
-    nodes = 0;
-    if (i < b.n_seq) {
-      const bool ok = sequence(b, i, &first, &nodes, &ctx);
-      mine = tree_units(a.shape, ctx, nodes);
-      if (*u_end < 0 && blockIdx.x == 0) {
+
+  __device__ __forceinline__ bool read(int i) {
+    const int f = __ldg(a.b.row_begin + i), e = __ldg(a.b.row_begin + i + 1), c = __ldg(a.b.ctx_len + i);
+    const bool ok = f >= 0 && e >= f && e <= a.b.n_tok && c >= 0;
+    first = f;
+    nodes = ok ? e - f : 0;
+    ctx = c;
+    units = ok ? tree_units(a.shape, ctx, nodes) : 0;
+    return ok;
+  }
+  __device__ void load(long long in_front) {
+    units = 0;
+    if (w0 + lane < a.b.n_seq) read(w0 + lane);
+    long long x = units;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    before = in_front + x - units;
+    window = in_front + __shfl_sync(0xffffffffu, x, 31);
+  }
+  __device__ Cursor(const TreeArgs& args, int lane_, bool reports) : a(args), lane(lane_) {
+    for (int i = lane; i < a.b.n_seq; i += 32) {
+      const bool ok = read(i);
+      total += units;
+      if (reports) {
         if (!ok) raise(a.pool.status, kBadRows);
         else if (nodes && static_cast<long long>(ctx) + nodes > a.shape.capacity) raise(a.pool.status, kBadSlot);
       }
     }
-    before = block_scan(mine, s_warp, &total);
-  };
-  bool loaded = false;
-  if (*u_end < 0) {
-    long long sum = 0;
-    for (int w0 = 0; w0 < b.n_seq; w0 += kThreads) {
-      load(w0);
-      sum += total;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+    const TreeShares shares = tree_shares(total, gridDim.x);
+    u = tree_share_begin(shares, blockIdx.x);
+    u_end = tree_share_begin(shares, blockIdx.x + 1);
+    load(0);
+  }
+  __device__ bool next(Segment* s) {
+    if (u >= u_end) return false;
+    unsigned hit;
+    while (!(hit = __ballot_sync(0xffffffffu, u >= before && u < before + units))) {      // ends: u is below the total
+      w0 += 32;
+      load(window);
     }
-    loaded = b.n_seq <= kThreads;      // the only window is in the registers
-    *units = sum;
-    const TreeShares shares = tree_shares(sum, gridDim.x);
-    *u = tree_share_begin(shares, blockIdx.x);
-    *u_end = tree_share_begin(shares, blockIdx.x + 1);
-    if (tid == 0 && *u == *u_end) a.notes[blockIdx.x].rows = 0;
+    const int src = __ffs(hit) - 1;
+    const long long in_front = __shfl_sync(0xffffffffu, before, src);
+    s->first = __shfl_sync(0xffffffffu, first, src);
+    s->nodes = __shfl_sync(0xffffffffu, nodes, src);
+    s->ctx = __shfl_sync(0xffffffffu, ctx, src);
+    const TreeSegment t = tree_segment(a.shape, w0 + src, s->ctx, s->nodes, u - in_front, u_end - in_front);
+    s->seq = t.seq;
+    s->head = t.head;
+    s->row0 = t.row_tile * kTileRows;
+    s->rows = static_cast<int>(min(static_cast<long long>(s->nodes) * a.shape.group - s->row0, static_cast<long long>(kTileRows)));
+    s->chunk0 = t.chunk0;
+    s->n = t.chunk1 - t.chunk0;
+    s->kind = t.chunk0 ? 1 : t.chunk1 < t.chunks ? 2 : 0;
+    s->limit = tree_kv_end(a.shape, s->ctx, s->nodes, t.row_tile);
+    last_unit = u + t.chunks - t.chunk0 - 1;
+    u += s->n;
+    return true;
   }
-  if (*u >= *u_end) {
-    if (tid == 0) ctl->n_segments = 0;
-    __syncthreads();
-    return;
-  }
-  long long running = 0;
-  int w0 = 0;
-  for (;; w0 += kThreads) {
-    if (!loaded) load(w0);
-    if (*u < running + total || w0 + kThreads >= b.n_seq) break;
-    running += total;
-  }
-  w->prefix[tid] = running + before;
-  if (tid == kThreads - 1) w->prefix[kThreads] = running + before + mine;
-  w->first[tid] = first;
-  w->nodes[tid] = nodes;
-  w->ctx[tid] = ctx;
-  if (*u >= running + before && *u < running + before + mine) ctl->found = tid;
-  __syncthreads();
-  if (tid == 0) {
-    long long at = *u;
-    int j = ctl->found, n = 0;
-    while (n < kMaxSegments && at < *u_end && j < kThreads) {
-      if (at >= w->prefix[j + 1]) {
-        ++j;
-        continue;
-      }
-      const TreeSegment t = tree_segment(a.shape, w0 + j, w->ctx[j], w->nodes[j], at - w->prefix[j], *u_end - w->prefix[j]);
-      const long long rows_all = static_cast<long long>(w->nodes[j]) * a.shape.group;
-      const long long limit = tree_kv_end(a.shape, w->ctx[j], w->nodes[j], t.row_tile);
-      Segment& s = ctl->seg[n++];
-      s.seq = t.seq;
-      s.head = t.head;
-      s.row0 = t.row_tile * kTileRows;
-      s.rows = static_cast<int>(min(rows_all - s.row0, static_cast<long long>(kTileRows)));
-      s.first = w->first[j];
-      s.nodes = w->nodes[j];
-      s.ctx = w->ctx[j];
-      s.chunk0 = t.chunk0;
-      s.chunk1 = t.chunk1;
-      s.kind = t.chunk0 ? 1 : t.chunk1 < t.chunks ? 2 : 0;
-      s.limit = limit;
-      const long long next = at + (t.chunk1 - t.chunk0);
-      if (next >= *u_end) {
-        TailNote& note = a.notes[blockIdx.x];
-        note.rows = s.kind == 2 ? s.rows : 0;
-        note.row0 = s.row0;
-        note.first = s.first;
-        note.head = s.head;
-        note.last_cta = s.kind == 2 ? tree_cta_of(tree_shares(*units, gridDim.x), at + t.chunks - 1) : 0;
-      }
-      at = next;
-    }
-    ctl->n_segments = n;
-    ctl->unit = at;
-  }
-  __syncthreads();
-  *u = ctl->unit;
-}
+  long long last_unit = 0;      // of the whole (sequence, KV head, row tile) of the segment that next() gave
+};
 
 // ---- what a row sees ------------------------------------------------------------------------------------------------
 // Bits for 32 positions from `pos` on.  a = index of the position among the rows of the step, negative in the context.
@@ -293,15 +251,16 @@ __device__ __forceinline__ float2 add2(float2 x, float2 y) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*reinterpret_cast<unsigned long long*>(&x)), "l"(*reinterpret_cast<unsigned long long*>(&y)));
   return *reinterpret_cast<float2*>(&d);
 }
-__device__ __forceinline__ float max_of(const uint32_t (&x)[32]) {
-  float t[4];
+__device__ __forceinline__ float max3(float x, float y, float z) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(x), "f"(y), "f"(z));
+  return d;
+}
+__device__ __forceinline__ float max_of(const uint32_t (&x)[32], float top) {
+  float t[4] = {top, __uint_as_float(x[0]), __uint_as_float(x[1]), __uint_as_float(x[2])};
 #pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    t[c] = __uint_as_float(x[8 * c]);
-#pragma unroll
-    for (int j = 1; j < 8; ++j) t[c] = fmaxf(t[c], __uint_as_float(x[8 * c + j]));
-  }
-  return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+  for (int j = 3; j + 1 < 32; j += 2) t[j / 2 & 3] = max3(t[j / 2 & 3], __uint_as_float(x[j]), __uint_as_float(x[j + 1]));
+  return fmaxf(max3(t[0], t[1], t[2]), fmaxf(t[3], __uint_as_float(x[31])));
 }
 
 // 32 columns of a row of the result, scaled.
@@ -330,7 +289,15 @@ struct RingPlace {
       phase ^= 1;
     }
   }
+  __device__ __forceinline__ void skip(int n) {
+    for (; n > 0; n -= kSlots) step(min(n, kSlots));
+  }
 };
+
+// 16 bytes to shared memory in the background; zeros where there is nothing to copy.
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
 
 template <typename T, typename Out, int D>
 __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
@@ -345,7 +312,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
   Control* ctl = reinterpret_cast<Control*>(s_ring + kSlots * Geo::kSlotBytes);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t bar_full = smem_u32(ctl->full), bar_empty = smem_u32(ctl->empty), bar_s = smem_u32(ctl->s_ready), bar_p = smem_u32(ctl->p_ready),
-                 bar_pv = smem_u32(ctl->pv_done), bar_q = smem_u32(&ctl->q_ready), bar_drain = smem_u32(ctl->drained);
+                 bar_pv = smem_u32(ctl->pv_done), bar_seg = smem_u32(ctl->seg_full), bar_seg_empty = smem_u32(ctl->seg_empty), bar_q = smem_u32(&ctl->q_ready), bar_drain = smem_u32(ctl->drained);
   int* const give_up = &ctl->give_up;
   int* const status = a.pool.status;
 
@@ -355,10 +322,15 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
       mbar_init(bar_full + 8 * i, 1);
       mbar_init(bar_empty + 8 * i, 2);
     }
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 2; ++i) {
       mbar_init(bar_s + 8 * i, 1);
-      mbar_init(bar_p + 8 * i, 4);
+      mbar_init(bar_p + 16 * i, 4);
+      mbar_init(bar_p + 16 * i + 8, 4);
       mbar_init(bar_pv + 8 * i, 1);
+    }
+    for (int i = 0; i < kSegments; ++i) {
+      mbar_init(bar_seg + 8 * i, 1);
+      mbar_init(bar_seg_empty + 8 * i, 11);
     }
     mbar_init(bar_q, 8);
     mbar_init(bar_drain, 1);
@@ -375,341 +347,417 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
   const uint32_t tmem = ctl->tmem;
   pdl_wait();
 
-  long long u = 0, u_end = -1, units = 0;
-  // running state of this role
-  RingPlace<kSlots> ring;       // copies and products: the place that the segment begins with
+  // Segment i of this CTA, or nothing when there are no more; the caller's warp gives it back with done_with(i).
+  auto segment = [&](uint32_t i) -> const Segment* {
+    const Segment* s = &ctl->seg[i % kSegments];
+    if (!wait_segment(bar_seg + 8 * (i % kSegments), i / kSegments & 1)) {
+      if (lane == 0) raise(status, kGaveUp);
+      return nullptr;
+    }
+    return s->n ? s : nullptr;
+  };
+  auto done_with = [&](uint32_t i) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar_seg_empty + 8 * (i % kSegments));
+  };
+  RingPlace<kSlots> ring;       // the place that the segment begins with
   uint32_t copies_before = 0;   // copies: places used so far, up to kSlots (the ring is empty at first)
-  uint32_t n_q = 0;             // products: segments
-  uint32_t n_sub = 0;           // sub-tiles of this thread's group; sub-tile i uses buffer i % 2
 
-  do {
-    plan(a, ctl, s_q, &u, &u_end, &units);
-    const int n_segments = ctl->n_segments;
-
-    if (warp == 8) {
-      // ---- copies ----
-      const int shift = a.pool.page_shift;
-      const int box_rows = min(1 << shift, kTilePos);
-      const int boxes = kTilePos / box_rows;           // per 64 columns of a unit
-      const int box = lane % boxes, panel = lane / boxes;
-      const uint32_t dst = smem_u32(s_ring) + panel * Geo::kPanel + box * box_rows * 128;
-      for (int si = 0; si < n_segments; ++si) {
-        const Segment s = ctl->seg[si];
-        const int n = s.chunk1 - s.chunk0;
-        const int32_t* table = a.b.table + s.seq * a.b.table_stride;
-        // A lane's row of the arrays for unit t, or -1
-        auto row_of = [&](int t) -> int64_t {
-          const long long pos = static_cast<long long>(s.chunk0 + t) * kTilePos + box * box_rows;
-          if (panel >= D / 64 || pos >= s.limit) return -1;
-          const int64_t r = find_slot(a.pool, table, a.b.table_stride, a.layer, pos);
-          if (r >= 0) return r + (static_cast<int64_t>(s.head) << shift);
-          raise(status, static_cast<int>(-r));
-          return -1;
-        };
-        int64_t row = row_of(0);
-        for (int t = 0; t < n; ++t) {
-          const int n_copies = __popc(__ballot_sync(0xffffffffu, row >= 0));
-#pragma unroll
-          for (int is_v = 0; is_v < 2; ++is_v) {
-            bool ok = true;
-            if (copies_before >= kSlots) ok = wait_for(bar_empty + 8 * ring.slot, ring.phase ^ 1, give_up, status);
-            ok = __all_sync(0xffffffffu, ok);
-            if (ok) {
-              if (lane == 0) mbar_expect(bar_full + 8 * ring.slot, static_cast<uint32_t>(n_copies) * box_rows * 128);
-              __syncwarp();
-              if (row >= 0) tma_load_2d(dst + ring.slot * Geo::kSlotBytes, is_v ? &v_map : &k_map, panel * 64, static_cast<int>(row), bar_full + 8 * ring.slot);
-            }
-            ring.step(1);
-            if (copies_before < kSlots) ++copies_before;
-          }
-          if (t + 1 < n) row = row_of(t + 1);
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    if (warp == 11) {
+      // ---- the plan ----
+      Cursor cursor(a, lane, blockIdx.x == 0);
+      Segment s;
+      s.rows = s.kind = 0;
+      for (uint32_t i = 0;; ++i) {
+        const bool more = cursor.next(&s);
+        if (i >= kSegments) wait_segment(bar_seg_empty + 8 * (i % kSegments), (i / kSegments - 1) & 1);
+        if (lane == 0) {
+          ctl->seg[i % kSegments] = s;
+          if (!more) ctl->seg[i % kSegments].n = 0;
+          mbar_arrive(bar_seg + 8 * (i % kSegments));
         }
-      }
-    } else if (warp >= 9) {
-      // ---- products: one warp per group, so that neither waits for the other's softmax ----
-      const uint32_t w = uniform(warp) - 9;
-      constexpr uint32_t kDescS = mma_f16_desc(kBf16, false, 128, kSub), kDescO = mma_f16_desc(kBf16, true, 128, D);
-      const uint32_t u_tmem = uniform(tmem), t_s = u_tmem + w * 2 * kSub, t_o = u_tmem + 256 + w * D;
-      const uint32_t ring_addr = uniform(smem_u32(s_ring)), q_addr = uniform(smem_u32(s_q));
-      const SmemOperand k_all = smem_operand(ring_addr, 16), v_all = smem_operand(ring_addr, Geo::kPanel);
-      for (int si = 0; si < n_segments; ++si) {
-        const bool halves = uniform(ctl->seg[si].rows) > 128;
-        const int n = uniform(ctl->seg[si].chunk1 - ctl->seg[si].chunk0), count = halves ? 2 * n : n;
-        const SmemOperand qq = smem_operand(q_addr + (halves ? w * Geo::kQBytes : 0), 16);
-        bool ok = wait_for(bar_q, n_q & 1, give_up, status);
-        ++n_q;
-        RingPlace<kSlots> pk = ring, pv = ring;      // of the unit whose keys, whose values are due
-        pv.step(1);
-        // Sub-tile j: half w of unit j, or half j % 2 of unit j / 2
-        auto scores = [&](int j) {                   // S = Q K^T
-          const uint32_t half = halves ? j & 1 : w;
-          if (!halves || half == 0) ok = wait_for(bar_full + 8 * pk.slot, pk.phase, give_up, status) && ok;
-          const bool last = !halves || half == 1;
-          tc_fence_after();
-          if (__all_sync(0xffffffffu, ok) && elect_one()) {
-            const uint32_t buffer = (n_sub + j) & 1;
-            const SmemOperand kk = k_all + (pk.slot * Geo::kSlotBytes + half * (kSub * 128));
-#pragma unroll
-            for (int i = 0; i < D / 16; ++i) mma_ss(t_s + buffer * kSub, qq + (i / 4 * Geo::kPanel + i % 4 * 32), kk + (i / 4 * Geo::kPanel + i % 4 * 32), kDescS, i > 0);
-            tc_commit(bar_s + 8 * (2 * w + buffer));
-            if (last) tc_commit(bar_empty + 8 * pk.slot);
-          }
-          __syncwarp();
-          if (last) pk.step(2);
-        };
-        auto outputs = [&](int j) {                  // O += P V
-          const uint32_t half = halves ? j & 1 : w;
-          if (!halves || half == 0) ok = wait_for(bar_full + 8 * pv.slot, pv.phase, give_up, status) && ok;
-          const bool last = !halves || half == 1;
-          const uint32_t buffer = (n_sub + j) & 1;
-          ok = wait_for(bar_p + 8 * (2 * w + buffer), (n_sub + j) >> 1 & 1, give_up, status) && ok;
-          tc_fence_after();
-          if (__all_sync(0xffffffffu, ok) && elect_one()) {
-            const SmemOperand vv = v_all + (pv.slot * Geo::kSlotBytes + half * (kSub * 128));
-#pragma unroll
-            for (int i = 0; i < kSub / 16; ++i) mma_ts(t_o, t_s + buffer * kSub + i * 8, vv + i * (16 * 128), kDescO, j > 0 || i > 0);
-            tc_commit(bar_pv + 8 * (2 * w + buffer));
-            if (last) tc_commit(bar_empty + 8 * pv.slot);
-          }
-          __syncwarp();
-          if (last) pv.step(2);
-        };
-        scores(0);
-        if (count > 1) scores(1);
-        for (int j = 0; j < count; ++j) {
-          outputs(j);
-          if (j + 2 < count) {
-            // P lies over S: the next scores of this buffer may not be written before the product has read it
-            ok = wait_for(bar_pv + 8 * (2 * w + ((n_sub + j) & 1)), (n_sub + j) >> 1 & 1, give_up, status) && ok;
-            scores(j + 2);
-          }
-        }
-        n_sub += count;
-        for (int k = 2 * n; k > 0; k -= kSlots) ring.step(min(k, kSlots));
-      }
-    } else {
-      // ---- softmax ----
-      const int w = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
-      const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
-      const uint32_t t_s = tmem + lanes + w * 2 * kSub, t_o = tmem + lanes + 256 + w * D;
-      const int group = a.shape.group;
-      for (int si = 0; si < n_segments; ++si) {
-        const Segment& s = ctl->seg[si];      // read again where it is needed
-        const bool halves = s.rows > 128;
-        const int n = s.chunk1 - s.chunk0;
-        auto view_of_segment = [&](bool bad_pages) {
-          return SegmentView{a.b, a.pool, s.first, s.nodes, s.ctx, s.limit, a.b.table + s.seq * a.b.table_stride, bad_pages};
-        };
-        // Row x of the tile: element 0 of its head in an array [n_tok][n_q_heads]
-        const int t0 = s.row0 / group, rem0 = s.row0 - t0 * group;
-        auto out_row = [&](int x) {
-          const int y = rem0 + x, t = small_div(y, a.group_inverse);
-          return static_cast<int64_t>(s.first + t0 + t) * a.n_q_heads + s.head * group + (y - t * group);
-        };
-        // Queries: this group's rows of the tile, or half of the only 128
-        constexpr int kPieces = D / 8;
-        const int q_first = 64 * w * (halves ? 2 : 1), q_rows = halves ? 128 : 64;      // rows q_first .. + q_rows of the tile
-        const T* q = static_cast<const T*>(a.q);
-        uint4 x[kPieces];
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-          const int idx = (tid & 127) + 128 * i, row = idx / kPieces, piece = idx % kPieces;
-          x[i] = make_uint4(0, 0, 0, 0);
-          if (row < q_rows && q_first + row < s.rows) x[i] = __ldg(reinterpret_cast<const uint4*>(q + out_row(q_first + row) * D) + piece);
-        }
-        uint32_t bad = 0;
-        {
-          const SegmentView view = view_of_segment(false);
-          const long long pos_end = min(static_cast<long long>(s.chunk1) * kTilePos, s.limit);
-          for (long long pg = (static_cast<long long>(s.chunk0) * kTilePos >> a.pool.page_shift) + tid; (pg << a.pool.page_shift) < pos_end; pg += kSoftmaxThreads)
-            bad |= !view.page_ok(pg << a.pool.page_shift);
-        }
-        // also: both groups are done with the previous segment
-        asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 q, %1, 0;\nbar.red.or.pred p, 1, %2, q;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(bad) : "r"(bad), "n"(kSoftmaxThreads) : "memory");
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-          const int idx = (tid & 127) + 128 * i, row = idx / kPieces, piece = idx % kPieces, in_acc = (q_first + row) & 127;
-          if (row < q_rows)
-            *reinterpret_cast<uint4*>(s_q + (halves && w ? Geo::kQBytes : 0) + piece / 8 * Geo::kPanel + in_acc * 128 + ((piece % 8) ^ (in_acc & 7)) * 16) = x[i];
-        }
-        fence_async_smem();
-        tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar_q);
-
-        const int in_tile = (halves ? w * 128 : 0) + r;            // this thread's row
-        const int my_rows = s.rows - (halves ? w * 128 : 0);
-        const bool live = quarter * 32 < my_rows;
-        const int node = in_tile < s.rows ? t0 + small_div(rem0 + in_tile, a.group_inverse) : 0;
-        const int count = halves ? 2 * n : n;
-        float m = -INFINITY;
-        float2 sum = make_float2(0.f, 0.f);
-        for (int j = 0; j < count; ++j, ++n_sub) {
-          const int t = halves ? j >> 1 : j, half = halves ? j & 1 : w;
-          const long long pos0 = static_cast<long long>(s.chunk0 + t) * kTilePos + half * kSub;
-          const bool edge = pos0 + kSub > s.ctx || bad;
-          const uint32_t buffer = n_sub & 1, phase = n_sub >> 1 & 1;
-          wait_for(bar_s + 8 * (2 * w + buffer), phase, give_up, status);
-          tc_fence_after();
-          if (live) {
-            uint32_t sc[2][32];
-#pragma unroll
-            for (int c = 0; c < 2; ++c) tmem_load(sc[c], t_s + buffer * kSub + 32 * c);
-            uint32_t seen[2] = {0xffffffffu, 0xffffffffu};
-            if (edge) {
-              const SegmentView view = view_of_segment(bad);
-              seen[0] = view.seen_by(node, pos0);
-              seen[1] = view.seen_by(node, pos0 + 32);
+        if (!more) break;
+      }
+      if (lane == 0) {
+        TailNote& note = a.notes[blockIdx.x];
+        note.rows = s.kind == 2 ? s.rows : 0;
+        if (s.kind == 2) {
+          note.row0 = s.row0;
+          note.first = s.first;
+          note.head = s.head;
+          note.last_cta = tree_cta_of(tree_shares(cursor.total, gridDim.x), cursor.last_unit);
+        }
+      }
+    } else if (warp == 8) {
+        // ---- copies ----
+        const int shift = a.pool.page_shift;
+        const int box_rows = min(1 << shift, kTilePos);
+        const int boxes = kTilePos / box_rows;           // per 64 columns of a unit
+        const int box = lane % boxes, panel = lane / boxes;
+        const uint32_t dst = smem_u32(s_ring) + panel * Geo::kPanel + box * box_rows * 128;
+        bool started = false;
+        uint32_t n_read = 0;      // units
+        const Segment* seg;
+        for (uint32_t si = 0; (seg = segment(si)); ++si) {
+          const Segment s = *seg;
+          done_with(si);
+          const int32_t* table = a.b.table + s.seq * a.b.table_stride;
+          for (int t = 0; t < s.n; ++t) {
+            const long long pos = static_cast<long long>(s.chunk0 + t) * kTilePos + box * box_rows;
+            int64_t row = -1;
+            bool bad = false;
+            if (panel < D / 64 && pos < s.limit) {
+              const int64_t r = find_slot(a.pool, table, a.b.table_stride, a.layer, pos);
+              bad = r < 0;
+              if (bad) raise(status, static_cast<int>(-r));
+              else row = r + (static_cast<int64_t>(s.head) << shift);
             }
-            tmem_wait_load();
+            const int n_copies = __popc(__ballot_sync(0xffffffffu, row >= 0));
+            const bool any_bad = __any_sync(0xffffffffu, bad);
 #pragma unroll
-            for (int c = 0; c < 2; ++c) tmem_use(sc[c]);
-            if (edge) {
-#pragma unroll
-              for (int c = 0; c < 2; ++c)
-#pragma unroll
-                for (int k = 0; k < 32; ++k)
-                  if (!(seen[c] >> k & 1)) sc[c][k] = 0xff800000u;
+            for (int is_v = 0; is_v < 2; ++is_v) {
+              bool ok = true;
+              if (copies_before >= kSlots) ok = wait_for(bar_empty + 8 * ring.slot, ring.phase ^ 1, give_up, status);
+              ok = __all_sync(0xffffffffu, ok);
+              if (ok) {
+                if (lane == 0) {
+                  if (!is_v) ctl->bad[n_read % 16] = any_bad;
+                  mbar_expect(bar_full + 8 * ring.slot, static_cast<uint32_t>(n_copies) * box_rows * 128);
+                }
+                __syncwarp();
+                if (row >= 0) tma_load_2d(dst + ring.slot * Geo::kSlotBytes, is_v ? &v_map : &k_map, panel * 64, static_cast<int>(row), bar_full + 8 * ring.slot);
+              }
+              // Queries before the rest of the first places: the first scores need them and one unit's keys, not what
+              // else fills the ring (measured: queries behind 160 KB of keys and values arrive 8 us late).
+              if (!started) wait_for(bar_q, 0, give_up, status);
+              started = true;
+              ring.step(1);
+              if (copies_before < kSlots) ++copies_before;
             }
-            const float top = fmaxf(max_of(sc[0]), max_of(sc[1])) * a.scale_log2;
-            if (j == 0) {
-              m = top;
-            } else if (__any_sync(0xffffffffu, top > m + kSlack)) {
-              const float m_new = top > m + kSlack ? top : m;
-              const float f = m == m_new ? 1.f : ex2(m - m_new);
-              m = m_new;
-              sum.x *= f;
-              sum.y *= f;
-              // the product of the sub-tile before, which may still be adding to O
-              wait_for(bar_pv + 8 * (2 * w + (buffer ^ 1)), (n_sub - 1) >> 1 & 1, give_up, status);
+            ++n_read;
+          }
+        }
+    } else {
+        // ---- products: one warp per group, so that neither waits for the other's softmax ----
+        const uint32_t w = uniform(warp) - 9;
+        constexpr uint32_t kDescS = mma_f16_desc(kBf16, false, 128, kTilePos), kDescO = mma_f16_desc(kBf16, true, 128, D);
+        const uint32_t u_tmem = uniform(tmem), t_s = u_tmem + w * kTilePos, t_o = u_tmem + 256 + w * D;
+        const uint32_t ring_addr = uniform(smem_u32(s_ring)), q_addr = uniform(smem_u32(s_q));
+        const SmemOperand k_all = smem_operand(ring_addr, 16), v_all = smem_operand(ring_addr, Geo::kPanel);
+        uint32_t n_units = 0;
+        const Segment* seg;
+        for (uint32_t si = 0; (seg = segment(si)); ++si) {
+          const bool halves = uniform(seg->rows) > 128;
+          const int n = uniform(seg->n), count = halves ? n : (n + 1 - w) / 2;
+          const SmemOperand qq = smem_operand(q_addr + ((halves ? w : si & 1) ? Geo::kQBytes : 0), 16);
+          done_with(si);
+          bool ok = wait_for(bar_q, si & 1, give_up, status);
+          RingPlace<kSlots> pk = ring, pv;      // of the unit whose keys, whose values are due
+          if (!halves && w) pk.step(2);
+          pv = pk;
+          pv.step(1);
+          auto scores = [&]() {                   // S = Q K^T
+            tc_fence_after();
+            if (__all_sync(0xffffffffu, ok) && elect_one()) {
+              const SmemOperand kk = k_all + pk.slot * Geo::kSlotBytes;
+#pragma unroll
+              for (int i = 0; i < D / 16; ++i) mma_ss(t_s, qq + (i / 4 * Geo::kPanel + i % 4 * 32), kk + (i / 4 * Geo::kPanel + i % 4 * 32), kDescS, i > 0);
+              tc_commit(bar_s + 8 * w);
+              tc_commit(bar_empty + 8 * pk.slot);
+              if (!halves) tc_commit(bar_empty + 8 * pk.slot);      // for the group that does not use it
+            }
+            __syncwarp();
+            pk.step(halves ? 2 : 4);
+          };
+          if (count > 0) {
+            ok = wait_for(bar_full + 8 * pk.slot, pk.phase, give_up, status) && ok;
+            scores();
+          }
+          for (int i = 0; i < count; ++i) {
+            // O += P V, in two halves of the positions: the first runs under the exponentials of the second.  The next
+            // keys are waited for before P is.
+            ok = wait_for(bar_full + 8 * pv.slot, pv.phase, give_up, status) && ok;
+            if (i + 1 < count) ok = wait_for(bar_full + 8 * pk.slot, pk.phase, give_up, status) && ok;
+            const SmemOperand vv = v_all + pv.slot * Geo::kSlotBytes;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              ok = wait_for(bar_p + 16 * w + 8 * h, n_units & 1, give_up, status) && ok;
               tc_fence_after();
-#pragma unroll 1
-              for (int k = 0; k < D / 16; ++k) {
-                uint32_t y[16];
-                tmem_load(y, t_o + 16 * k);
-                tmem_wait_load();
-                tmem_use(y);
+              if (__all_sync(0xffffffffu, ok) && elect_one()) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) y[i] = __float_as_uint(__uint_as_float(y[i]) * f);
-                tmem_store(t_o + 16 * k, y);
+                for (int k = 4 * h; k < 4 * h + 4; ++k) mma_ts(t_o, t_s + k * 8, vv + k * (16 * 128), kDescO, i > 0 || k > 0);
+                if (h) {
+                  tc_commit(bar_pv + 8 * w);
+                  tc_commit(bar_empty + 8 * pv.slot);
+                  if (!halves) tc_commit(bar_empty + 8 * pv.slot);
+                }
               }
+              __syncwarp();
             }
-            const float2 scale = make_float2(a.scale_log2, a.scale_log2), shift = m == -INFINITY ? make_float2(0.f, 0.f) : make_float2(-m, -m);
-            uint32_t packed[32];
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-              for (int k = 0; k < 16; ++k) {
-                float2 p = fma2(make_float2(__uint_as_float(sc[c][2 * k]), __uint_as_float(sc[c][2 * k + 1])), scale, shift);
-                p = make_float2(ex2(p.x), ex2(p.y));
-                sum = add2(sum, p);
-                packed[16 * c + k] = Half2Of<T>::pack(p.x, p.y);
-              }
-            tmem_store(t_s + buffer * kSub, packed);
-            tmem_wait_store();
+            pv.step(halves ? 2 : 4);
+            // P lies over S: the next scores are written behind the product that reads it (one warp's products run in order)
+            if (i + 1 < count) scores();
+            ++n_units;
           }
-          if (edge) {
-            // Values at positions that no row sees may be anything, and 0 x NaN is NaN: clear them.
-            const uint32_t seen = view_of_segment(bad).seen_by_any(pos0 + (r & 32), lane);
-            RingPlace<kSlots> pv = ring;
-            for (int k = 2 * t + 1; k > 0; k -= kSlots) pv.step(min(k, kSlots));
-            wait_for(bar_full + 8 * pv.slot, pv.phase, give_up, status);
-            if (!(seen >> lane & 1)) {
-              uint8_t* row = s_ring + pv.slot * Geo::kSlotBytes + (half * kSub + (r & 63)) * 128;
-              constexpr int kHalfRow = D / 16;      // 16-byte pieces
-#pragma unroll
-              for (int c = 0; c < kHalfRow; ++c) {
-                const int piece = (r >> 6) * kHalfRow + c;
-                *reinterpret_cast<uint4*>(row + piece / 8 * Geo::kPanel + piece % 8 * 16) = make_uint4(0, 0, 0, 0);
-              }
-            }
-            fence_async_smem();
-          }
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar_p + 8 * (2 * w + buffer));
+          ring.skip(2 * n);
         }
-        for (int k = 2 * n; k > 0; k -= kSlots) ring.step(min(k, kSlots));
-        wait_for(bar_pv + 8 * (2 * w + ((n_sub - 1) & 1)), (n_sub - 1) >> 1 & 1, give_up, status);
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+    // ---- softmax ----
+    const int w = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
+    const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
+    const uint32_t t_s = tmem + lanes + w * kTilePos, t_o = tmem + lanes + 256 + w * D;
+    const int group = a.shape.group;
+    uint32_t n_units = 0, unit_base = 0;    // taken by this group; of the segments before
+    bool loaded = false;                    // the queries of the segment are on their way already
+    bool joined = false;                    // group 0 reads group 1's output of the previous segment
+
+    // Row x of a segment's tile: its head's place in an array [n_tok][n_q_heads]
+    auto place_of = [&](const Segment& g, int t0, int rem0, int x) {
+      const int y = rem0 + x, t = small_div(y, a.group_inverse);
+      return static_cast<int64_t>(g.first + t0 + t) * a.n_q_heads + g.head * group + (y - t * group);
+    };
+    // Queries of a segment into its tile, in the background; both groups, all threads.
+    auto load_queries = [&](const Segment& g, uint32_t tile) {
+      constexpr int kPieces = D / 8;
+      const int t0 = g.row0 / group, rem0 = g.row0 - t0 * group;
+      const int rows = g.halves() ? kTileRows : 128;
+#pragma unroll 4
+      for (int idx = tid; idx < rows * kPieces; idx += kSoftmaxThreads) {
+        const int row = idx / kPieces, piece = idx % kPieces, in_acc = row & 127;
+        const bool there = row < g.rows;
+        copy16(smem_u32(s_q) + ((g.halves() ? row >> 7 : tile) ? Geo::kQBytes : 0) + piece / 8 * Geo::kPanel + in_acc * 128 + ((piece % 8) ^ (in_acc & 7)) * 16,
+               static_cast<const T*>(a.q) + place_of(g, t0, rem0, there ? row : 0) * D + piece * 8, there);
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    auto queries_ready = [&]() {
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      fence_async_smem();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_q);
+    };
+
+    const Segment* seg;
+    for (uint32_t si = 0; (seg = segment(si)); ++si) {
+      const Segment& s = *seg;      // read again where it is needed
+      if (!loaded) {
+        load_queries(s, si & 1);
+        queries_ready();
+      }
+      // A tile of at most 128 rows leaves room for the next one's queries.
+      bool next_loads = false;
+      if (!s.halves()) {
+        const Segment* next = segment(si + 1);
+        if (next && !next->halves()) {
+          load_queries(*next, (si + 1) & 1);
+          next_loads = true;
+        }
+      }
+      const int t0 = s.row0 / group, rem0 = s.row0 - t0 * group;
+      const int in_tile = (s.halves() ? w * 128 : 0) + r;            // this thread's row
+      const bool live = (s.halves() ? w * 128 : 0) + quarter * 32 < s.rows;
+      const int node = in_tile < s.rows ? t0 + small_div(rem0 + in_tile, a.group_inverse) : 0;
+      const int count = s.count(w), other = s.count(w ^ 1);
+      RingPlace<kSlots> pk = ring;            // of the unit's keys
+      if (!s.halves() && w) pk.step(2);
+      ring.skip(2 * s.n);
+      float m = -INFINITY;
+      float2 sum = make_float2(0.f, 0.f);
+      // Turns: of the two warps that share an exponential unit, one per group, one uses it at a time, at its full rate,
+      // while the other's products run.  Left alone the two fall into step and wait for the same things.
+      auto begin_turn = [&](int i) {
+        if (w == 1 || i > 0) asm volatile("bar.sync %0, 64;" ::"r"(3 + 2 * quarter + w) : "memory");
+      };
+      auto end_turn = [&](int i) {
+        if (i + w < other) asm volatile("bar.arrive %0, 64;" ::"r"(3 + 2 * quarter + (w ^ 1)) : "memory");
+      };
+      // Group 0 may still be reading group 1's output of an earlier segment.
+      auto output_free = [&]() {
+        if (joined && w == 1) asm volatile("bar.sync 14, %0;" ::"n"(kSoftmaxThreads) : "memory");
+        joined = false;
+      };
+      for (int i = 0; i < count; ++i, ++n_units) {
+        const long long pos0 = static_cast<long long>(s.chunk0 + s.unit(w, i)) * kTilePos;
+        wait_for(bar_s + 8 * w, n_units & 1, give_up, status);
         tc_fence_after();
-        // ---- the segment's result ----
-        const bool join = !halves;
-        float total = sum.x + sum.y, other_m = -INFINITY, other_sum = 0.f;
-        if (join) {      // group 1 hands its state to group 0 through tensor memory: the same lanes hold the same rows
-          if (w == 1 && live) {
-            const uint32_t ml[2] = {__float_as_uint(m), __float_as_uint(total)};
-            tmem_store(t_s, ml);
+        const bool bad = *static_cast<volatile int*>(&ctl->bad[(unit_base + s.unit(w, i)) % 16]) != 0;
+        const bool edge = pos0 + kTilePos > s.ctx || bad;
+        const SegmentView view{a.b, a.pool, s.first, s.nodes, s.ctx, s.limit, a.b.table + s.seq * a.b.table_stride, bad};
+        if (edge) {
+          // Values at positions that no row sees may be anything, and 0 x NaN is NaN: clear them.
+          const uint32_t seen = view.seen_by_any(pos0 + 32 * quarter, lane);
+          RingPlace<kSlots> pv = pk;
+          pv.step(1);
+          wait_for(bar_full + 8 * pv.slot, pv.phase, give_up, status);
+          if (!(seen >> lane & 1)) {
+            uint8_t* row = s_ring + pv.slot * Geo::kSlotBytes + r * 128;
+#pragma unroll
+            for (int c = 0; c < D / 8; ++c) *reinterpret_cast<uint4*>(row + c / 8 * Geo::kPanel + c % 8 * 16) = make_uint4(0, 0, 0, 0);
+          }
+          fence_async_smem();
+        }
+        pk.step(s.halves() ? 2 : 4);
+        if (live) {
+          if (edge) {
+            // -infinity where the row does not see, in tensor memory: one copy of this code
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+              uint32_t x[32];
+              tmem_load(x, t_s + 32 * c);
+              const uint32_t seen = view.seen_by(node, pos0 + 32 * c);
+              tmem_wait_load();
+              tmem_use(x);
+#pragma unroll
+              for (int j = 0; j < 32; ++j)
+                if (!(seen >> j & 1)) x[j] = 0xff800000u;
+              tmem_store(t_s + 32 * c, x);
+            }
             tmem_wait_store();
           }
-          tc_fence_before();
-          asm volatile("bar.sync 2, %0;" ::"n"(kSoftmaxThreads) : "memory");
-          tc_fence_after();
-          if (w == 0 && live) {
-            uint32_t ml[2];
-            tmem_load(ml, t_s + 2 * kSub);
-            tmem_wait_load();
-            tmem_use(ml);
-            other_m = __uint_as_float(ml[0]);
-            other_sum = __uint_as_float(ml[1]);
+          uint32_t sc[4][32];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) tmem_load(sc[c], t_s + 32 * c);
+          tmem_wait_load();
+#pragma unroll
+          for (int c = 0; c < 4; ++c) tmem_use(sc[c]);
+          float top = -INFINITY;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) top = max_of(sc[c], top);
+          top *= a.scale_log2;
+          if (i == 0) {
+            m = top;
+          } else if (__any_sync(0xffffffffu, top > m + kSlack)) {
+            const float m_new = top > m + kSlack ? top : m;
+            const float f = m == m_new ? 1.f : ex2(m - m_new);
+            m = m_new;
+            sum.x *= f;
+            sum.y *= f;
+            // the product before, which may still be adding to O
+            wait_for(bar_pv + 8 * w, (n_units - 1) & 1, give_up, status);
+            tc_fence_after();
+#pragma unroll 1
+            for (int k = 0; k < D / 16; ++k) {
+              uint32_t y[16];
+              tmem_load(y, t_o + 16 * k);
+              tmem_wait_load();
+              tmem_use(y);
+#pragma unroll
+              for (int j = 0; j < 16; ++j) y[j] = __float_as_uint(__uint_as_float(y[j]) * f);
+              tmem_store(t_o + 16 * k, y);
+            }
+          }
+          begin_turn(i);
+          const float2 scale = make_float2(a.scale_log2, a.scale_log2), shift = m == -INFINITY ? make_float2(0.f, 0.f) : make_float2(-m, -m);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            uint32_t packed[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              float2 p = fma2(make_float2(__uint_as_float(sc[c][2 * j]), __uint_as_float(sc[c][2 * j + 1])), scale, shift);
+              p = make_float2(ex2(p.x), ex2(p.y));
+              sum = add2(sum, p);
+              packed[j] = Half2Of<T>::pack(p.x, p.y);
+            }
+            if (c == 3) end_turn(i);
+            tmem_store(t_s + 16 * c, packed);
+            if (c & 1) tmem_wait_store();
+            if (c == 1 && i == 0) output_free();
+            if (c & 1) {
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(bar_p + 16 * w + 8 * (c >> 1));
+            }
+          }
+        } else {
+          begin_turn(i);
+          end_turn(i);
+          if (i == 0) output_free();
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(bar_p + 16 * w);
+            mbar_arrive(bar_p + 16 * w + 8);
           }
         }
-        if (live && (halves || w == 0)) {
-          const float m_all = fmaxf(m, other_m);
-          float f0 = m == -INFINITY ? 0.f : ex2(m - m_all), f1 = other_m == -INFINITY ? 0.f : ex2(other_m - m_all);
-          total = total * f0 + other_sum * f1;
-          if (s.kind == 0) {
-            const float inv = total > 0.f ? 1.f / total : 0.f;
-            f0 *= inv;
-            f1 *= inv;
-          }
-          const bool mine = in_tile < s.rows;
-          const int64_t at = mine ? out_row(in_tile) : 0;
-          const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) + (s.kind == 2);
+      }
+      // All products of the segment are done, the other group's too: its queries may be overwritten, S is free.
+      const bool join = !s.halves() && s.n > 1;      // the groups took every other unit each: group 0 adds group 1's state to its own
+      float total = sum.x + sum.y, other_m = -INFINITY, other_sum = 0.f;
+      if (count > 0) wait_for(bar_pv + 8 * w, (n_units - 1) & 1, give_up, status);
+      if (join && w == 1) ctl->ml[r] = make_float2(m, total);
+      tc_fence_before();
+      asm volatile("bar.sync 13, %0;" ::"n"(kSoftmaxThreads) : "memory");
+      tc_fence_after();
+      if (next_loads) queries_ready();
+      loaded = next_loads;
+      unit_base += s.n;
+      if (join && w == 0) {
+        const float2 ml = ctl->ml[r];
+        other_m = ml.x;
+        other_sum = ml.y;
+      }
+      if (live && (s.halves() || w == 0)) {
+        const float m_all = fmaxf(m, other_m);
+        float f0 = m == -INFINITY ? 0.f : ex2(m - m_all), f1 = other_m == -INFINITY ? 0.f : ex2(other_m - m_all);
+        total = total * f0 + other_sum * f1;
+        if (s.kind == 0) {
+          const float inv = total > 0.f ? 1.f / total : 0.f;
+          f0 *= inv;
+          f1 *= inv;
+        }
+        const bool mine = in_tile < s.rows;
+        const int64_t at = mine ? place_of(s, t0, rem0, in_tile) : 0;
+        const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) + (s.kind == 2);
 #pragma unroll 1
-          for (int c = 0; c < D / 32; ++c) {
-            uint32_t o[32];
-            float y[32];
-            tmem_load(o, t_o + 32 * c);
-            if (join) {
-              uint32_t o1[32];
-              tmem_load(o1, t_o + D + 32 * c);
-              tmem_wait_load();
-              tmem_use(o);
-              tmem_use(o1);
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t o[32], o1[32];
+          float y[32];
+          tmem_load(o, t_o + 32 * c);
+          if (join) tmem_load(o1, t_o + D + 32 * c);
+          tmem_wait_load();
+          tmem_use(o);
+          if (join) {
+            tmem_use(o1);
 #pragma unroll
-              for (int j = 0; j < 32; ++j) y[j] = __uint_as_float(o[j]) * f0 + __uint_as_float(o1[j]) * f1;
-            } else {
-              tmem_wait_load();
-              tmem_use(o);
+            for (int j = 0; j < 32; ++j) y[j] = __uint_as_float(o[j]) * f0 + __uint_as_float(o1[j]) * f1;
+          } else {
 #pragma unroll
-              for (int j = 0; j < 32; ++j) y[j] = __uint_as_float(o[j]) * f0;
-            }
-            if (mine) {
-              if (s.kind == 0) {
-                store_row(static_cast<Out*>(a.out) + at * D + 32 * c, y);
-              } else {
-                float4* dst = reinterpret_cast<float4*>(a.part_o) + (slot * (D / 4) + 8 * c) * kTileRows + in_tile;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) dst[j * kTileRows] = make_float4(y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]);
-              }
-            }
+            for (int j = 0; j < 32; ++j) y[j] = __uint_as_float(o[j]) * f0;
           }
           if (mine) {
-            if (s.kind != 0) a.part_ml[slot * kTileRows + in_tile] = make_float2(m_all, total);
-            else if (a.lse) a.lse[at] = total > 0.f ? (m_all + log2f(total)) * kLn2 : -INFINITY;
+            if (s.kind == 0) {
+              store_row(static_cast<Out*>(a.out) + at * D + 32 * c, y);
+            } else {
+              float4* dst = reinterpret_cast<float4*>(a.part_o) + (slot * (D / 4) + 8 * c) * kTileRows + in_tile;
+#pragma unroll
+              for (int j = 0; j < 8; ++j) dst[j * kTileRows] = make_float4(y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]);
+            }
           }
-          tc_fence_before();
+        }
+        if (mine) {
+          if (s.kind != 0) a.part_ml[slot * kTileRows + in_tile] = make_float2(m_all, total);
+          else if (a.lse) a.lse[at] = total > 0.f ? (m_all + log2f(total)) * kLn2 : -INFINITY;
         }
       }
+      tc_fence_before();
+      if (join && w == 0) asm volatile("bar.arrive 14, %0;" ::"n"(kSoftmaxThreads) : "memory");
+      joined |= join;
+      done_with(si);
     }
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
-  } while (u < u_end);
+    if (joined && w == 1) asm volatile("bar.sync 14, %0;" ::"n"(kSoftmaxThreads) : "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
 
   // A wait that gave up may have left products or copies under way: they end before the memory is given back.
   if (ctl->give_up) {
-    if (warp >= 9 && lane == 0) {
+    if ((warp == 9 || warp == 10) && lane == 0) {
       tc_commit(bar_drain + 8 * (warp - 9));
       for (int i = 0; i < (1 << 22) && !mbar_test(bar_drain + 8 * (warp - 9), 0); ++i) {}
     }
@@ -725,50 +773,59 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
 }
 
 // ---- joining the parts ----------------------------------------------------------------------------------------------
-// blockIdx.x = the CTA in which a cut segment begins, blockIdx.y = 32 of its rows; a thread owns one row and D / 8
-// columns, so that reads of the parts are contiguous across the warp.
+// blockIdx.x = the CTA in which a cut segment begins, blockIdx.y = 32 of its rows, blockIdx.z = 32 columns; a thread
+// owns one row and 4 columns, so that reads of the parts are contiguous across the warp.  The parts are taken eight at
+// a time, all their reads in flight: what this kernel costs is the latency of its reads.
 template <typename Out, int D>
 __global__ void __launch_bounds__(256) tree_merge_kernel(const __grid_constant__ TreeArgs a) {
   pdl_trigger();
   pdl_wait();
   const TailNote note = a.notes[blockIdx.x];
-  const int row = blockIdx.y * 32 + (threadIdx.x & 31), part = threadIdx.x >> 5;
+  const int row = blockIdx.y * 32 + (threadIdx.x & 31), quad = blockIdx.z * 8 + (threadIdx.x >> 5);
   if (row >= note.rows) return;
-  auto slot_of = [&](int c) { return c == static_cast<int>(blockIdx.x) ? 2 * static_cast<int64_t>(c) + 1 : 2 * static_cast<int64_t>(c); };
-  float m = -INFINITY;
-  for (int c = blockIdx.x; c <= note.last_cta; ++c)
-    m = fmaxf(m, __ldcg(&a.part_ml[slot_of(c) * kTileRows + row].x));
-  float total = 0.f;
-  constexpr int kQuads = D / 32;
-  float4 o[kQuads];
+  const int parts = note.last_cta - static_cast<int>(blockIdx.x) + 1;
+  float m = -INFINITY, total = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int c0 = 0; c0 < parts; c0 += 8) {
+    float2 ml[8];
+    float4 x[8];
 #pragma unroll
-  for (int i = 0; i < kQuads; ++i) o[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int c = blockIdx.x; c <= note.last_cta; ++c) {
-    const float2 ml = __ldcg(&a.part_ml[slot_of(c) * kTileRows + row]);
-    const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - m);
-    total += ml.y * f;
-    const float4* src = reinterpret_cast<const float4*>(a.part_o) + (slot_of(c) * (D / 4) + part * kQuads) * kTileRows + row;
+    for (int j = 0; j < 8; ++j) {
+      ml[j] = make_float2(-INFINITY, 0.f);
+      x[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (c0 + j < parts) {
+        const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x + c0 + j) + (c0 + j == 0);
+        ml[j] = __ldcg(&a.part_ml[slot * kTileRows + row]);
+        x[j] = __ldcg(reinterpret_cast<const float4*>(a.part_o) + (slot * (D / 4) + quad) * kTileRows + row);
+      }
+    }
+    float top = m;
 #pragma unroll
-    for (int i = 0; i < kQuads; ++i) {
-      const float4 x = __ldcg(src + i * kTileRows);
-      o[i].x += x.x * f;
-      o[i].y += x.y * f;
-      o[i].z += x.z * f;
-      o[i].w += x.w * f;
+    for (int j = 0; j < 8; ++j) top = fmaxf(top, ml[j].x);
+    const float f = m == -INFINITY ? 0.f : ex2(m - top);
+    m = top;
+    total *= f;
+    o.x *= f;
+    o.y *= f;
+    o.z *= f;
+    o.w *= f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float g = ml[j].x == -INFINITY ? 0.f : ex2(ml[j].x - m);
+      total += ml[j].y * g;
+      o.x += x[j].x * g;
+      o.y += x[j].y * g;
+      o.z += x[j].z * g;
+      o.w += x[j].w * g;
     }
   }
   const float inv = total > 0.f ? 1.f / total : 0.f;
   const int gr = note.row0 + row, group = a.shape.group;
   const int64_t out_row = static_cast<int64_t>(note.first + gr / group) * a.n_q_heads + note.head * group + gr % group;
-  Out* dst = static_cast<Out*>(a.out) + out_row * D + part * 4 * kQuads;
-#pragma unroll
-  for (int i = 0; i < kQuads; ++i) {
-    if constexpr (sizeof(Out) == 4)
-      *reinterpret_cast<float4*>(dst + 4 * i) = make_float4(o[i].x * inv, o[i].y * inv, o[i].z * inv, o[i].w * inv);
-    else
-      *reinterpret_cast<uint2*>(dst + 4 * i) = make_uint2(Half2Of<Out>::pack(o[i].x * inv, o[i].y * inv), Half2Of<Out>::pack(o[i].z * inv, o[i].w * inv));
-  }
-  if (a.lse && part == 0) a.lse[out_row] = total > 0.f ? (m + log2f(total)) * kLn2 : -INFINITY;
+  Out* dst = static_cast<Out*>(a.out) + out_row * D + 4 * quad;
+  if constexpr (sizeof(Out) == 4) *reinterpret_cast<float4*>(dst) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+  else *reinterpret_cast<uint2*>(dst) = make_uint2(Half2Of<Out>::pack(o.x * inv, o.y * inv), Half2Of<Out>::pack(o.z * inv, o.w * inv));
+  if (a.lse && quad == 0) a.lse[out_row] = total > 0.f ? (m + log2f(total)) * kLn2 : -INFINITY;
 }
 
 constexpr int64_t kAlign = 256;
@@ -781,7 +838,6 @@ cudaError_t launch_tree(const prima_paged& pool, TreeArgs a, cudaStream_t st) {
   using Geo = Geometry<D>;
   constexpr size_t kSmem = 1024 + 2 * Geo::kQBytes + Geo::kSlots * Geo::kSlotBytes + sizeof(Control);
   static_assert(kSmem <= 232448, "shared memory of a CTA");
-  static_assert(sizeof(long long) * (16 + kThreads + 1) + 3 * sizeof(int) * kThreads <= 2 * Geo::kQBytes, "planning fits where the queries go");
   static bool done[kMaxDevices] = {};
   int dev;
   auto kernel = tree_kernel<T, Out, D>;
@@ -793,7 +849,7 @@ cudaError_t launch_tree(const prima_paged& pool, TreeArgs a, cudaStream_t st) {
   const Maps* maps = static_cast<const Maps*>(pool.maps);
   cudaError_t e = launch_pdl(kernel, dim3(pool.sm_count), dim3(kThreads), kSmem, st, maps->k, maps->v, a);
   if (e != cudaSuccess) return e;
-  return launch_pdl(tree_merge_kernel<Out, D>, dim3(pool.sm_count, kTileRows / 32), dim3(256), 0, st, a);
+  return launch_pdl(tree_merge_kernel<Out, D>, dim3(pool.sm_count, kTileRows / 32, D / 32), dim3(256), 0, st, a);
 }
 
 }  // namespace
