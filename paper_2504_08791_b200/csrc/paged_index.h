@@ -33,38 +33,43 @@ PRIMA_HD int64_t find_slot(const PageShape& p, const int32_t* table_row, int64_t
 
 // ---- how the work of tree attention is dealt out -------------------------------------------------------------------
 // The rows of a sequence that read one KV head (node-major: row = node * group + query head in the group) are cut into
-// tiles of kTileRows, the positions that a tile may see into units of kTilePos.  The units of all sequences, KV heads
+// tiles of tile_rows, the positions that a tile may see into units of kTilePos.  The units of all sequences, KV heads
 // and row tiles, in this order, form one line that is cut into equal shares, one per CTA, so that long and short
-// sequences balance.  A stretch of units of one (sequence, KV head, row tile) inside a share is a segment.
-constexpr int kTileRows = 256;
+// sequences balance.  A stretch of units of one (sequence, KV head, row tile) inside a share is a segment.  Queries, the
+// first scores and the output cost a segment as much as some units, so each (sequence, KV head, row tile) has `overhead`
+// places at its head in the line that stand for no unit.
 constexpr int kTilePos = 128;
 
 struct TreeShape {
   int n_kv_heads, group;     // query heads that share a KV head
   int causal;                // no mask: row i of a sequence sees rows 0 .. i
   int64_t capacity;          // positions that a page table row can name
+  int overhead;              // what a segment costs besides its units, in units
+  int tile_rows;
 };
 
 PRIMA_HD int tree_row_tiles(const TreeShape& t, int nodes) {
-  return static_cast<int>((static_cast<int64_t>(nodes) * t.group + kTileRows - 1) / kTileRows);
+  return static_cast<int>((static_cast<int64_t>(nodes) * t.group + t.tile_rows - 1) / t.tile_rows);
 }
 // Positions 0 .. result-1 are all that the rows of tile rt may see.
 PRIMA_HD int64_t tree_kv_end(const TreeShape& t, int ctx, int nodes, int rt) {
   int64_t seen = nodes;
   if (t.causal) {
-    const int64_t last = (static_cast<int64_t>(rt + 1) * kTileRows + t.group - 1) / t.group;
+    const int64_t last = (static_cast<int64_t>(rt + 1) * t.tile_rows + t.group - 1) / t.group;
     if (last < seen) seen = last;
   }
   const int64_t end = ctx + seen;
   return end < t.capacity ? end : t.capacity;
 }
 PRIMA_HD int64_t tree_chunks(const TreeShape& t, int ctx, int nodes, int rt) { return (tree_kv_end(t, ctx, nodes, rt) + kTilePos - 1) / kTilePos; }
-PRIMA_HD int64_t tree_units(const TreeShape& t, int ctx, int nodes) {
-  int64_t n = 0;
+// Places in the line of one (sequence, KV head, row tile).
+PRIMA_HD int64_t tree_length(const TreeShape& t, int ctx, int nodes, int rt) { return t.overhead + tree_chunks(t, ctx, nodes, rt); }
+PRIMA_HD int64_t tree_units(const TreeShape& t, int ctx, int nodes) {      // of one KV head of a sequence
   const int tiles = tree_row_tiles(t, nodes);
-  if (!t.causal || tiles <= 1) return tiles ? t.n_kv_heads * tiles * tree_chunks(t, ctx, nodes, 0) : 0;
-  for (int rt = 0; rt < tiles; ++rt) n += tree_chunks(t, ctx, nodes, rt);
-  return n * t.n_kv_heads;
+  if (!t.causal || tiles <= 1) return tiles ? tiles * tree_length(t, ctx, nodes, 0) : 0;
+  int64_t n = 0;
+  for (int rt = 0; rt < tiles; ++rt) n += tree_length(t, ctx, nodes, rt);
+  return n;
 }
 // Division of non-negative numbers that are nearly always small: 64-bit division is a long subroutine on the GPU.
 PRIMA_HD int64_t div_small(int64_t a, int64_t b) {
@@ -86,39 +91,41 @@ PRIMA_HD int tree_cta_of(const TreeShares& s, int64_t u) {
   return static_cast<int>(u < long_ones ? div_small(u, s.base + 1) : s.more + div_small(u - long_ones, s.base));
 }
 
-// x / d for 0 <= x < kTileRows + 64, 1 <= d <= 64, by a multiplication with m = small_inverse(d).
+// x / d for 0 <= x < 256 + 64, 1 <= d <= 64, by a multiplication with m = small_inverse(d).
 PRIMA_HD uint32_t small_inverse(int d) { return 65536u / static_cast<uint32_t>(d) + 1u; }
 PRIMA_HD int small_div(int x, uint32_t m) { return static_cast<int>(static_cast<uint32_t>(x) * m >> 16); }
 
 struct TreeSegment {
-  int seq, head, row_tile;   // head: KV head
-  int chunk0, chunk1;        // units of this share
+  int head, row_tile;        // head: KV head
+  int chunk0, chunk1;        // units of this share; none where the share has only places at the head
   int chunks;                // units of the whole (sequence, KV head, row tile)
+  int64_t places;            // of this share, and to the end of the whole
+  int64_t to_end;
 };
-// The segment that starts at unit u (counted from the first unit of its sequence) and ends at or before unit u_end.
-PRIMA_HD TreeSegment tree_segment(const TreeShape& t, int seq, int ctx, int nodes, int64_t u, int64_t u_end) {
+// The segment at place u of a sequence whose KV heads have `per_head` places each; it ends at or before place u_end.
+PRIMA_HD TreeSegment tree_segment(const TreeShape& t, int ctx, int nodes, int64_t per_head, int64_t u, int64_t u_end) {
   TreeSegment s;
-  s.seq = seq;
   const int tiles = tree_row_tiles(t, nodes);
-  const int64_t per_head = div_small(tree_units(t, ctx, nodes), t.n_kv_heads);
   s.head = static_cast<int>(div_small(u, per_head));
   int64_t r = u - s.head * per_head;
-  int64_t chunks = tree_chunks(t, ctx, nodes, 0);
+  int64_t length = tree_length(t, ctx, nodes, 0);
   int rt = 0;
   if (!t.causal) {
-    rt = static_cast<int>(div_small(r, chunks));
-    r -= rt * chunks;
+    rt = static_cast<int>(div_small(r, length));
+    r -= rt * length;
   } else {
-    while (rt + 1 < tiles && r >= chunks) {
-      r -= chunks;
-      chunks = tree_chunks(t, ctx, nodes, ++rt);
+    while (rt + 1 < tiles && r >= length) {
+      r -= length;
+      length = tree_length(t, ctx, nodes, ++rt);
     }
   }
   s.row_tile = rt;
-  s.chunk0 = static_cast<int>(r);
-  s.chunks = static_cast<int>(chunks);
-  const int64_t end = r + (u_end - u);
-  s.chunk1 = static_cast<int>(end < chunks ? end : chunks);
+  s.chunks = static_cast<int>(length - t.overhead);
+  s.to_end = length - r;
+  s.places = s.to_end < u_end - u ? s.to_end : u_end - u;
+  const int64_t c0 = r - t.overhead, c1 = c0 + s.places;
+  s.chunk0 = static_cast<int>(c0 > 0 ? c0 : 0);
+  s.chunk1 = static_cast<int>(c1 > 0 ? c1 : 0);
   return s;
 }
 

@@ -29,6 +29,7 @@
 namespace prima {
 namespace {
 
+constexpr int kTileRows = 256;         // of the tensor-memory kernel
 constexpr int kSoftmaxThreads = 256;
 constexpr int kThreads = kSoftmaxThreads + 128;      // two warpgroups of softmax; one of copies, products (two warps) and an idle warp
 // Registers: 384 threads may have 168 each; the softmax threads hold a row of 128 scores and take what the others do
@@ -36,6 +37,7 @@ constexpr int kThreads = kSoftmaxThreads + 128;      // two warpgroups of softma
 constexpr int kSoftmaxRegs = 208, kOtherRegs = 80;
 static_assert(kSoftmaxThreads * kSoftmaxRegs + (kThreads - kSoftmaxThreads) * kOtherRegs <= kThreads * 168, "the split may not exceed the launch");
 constexpr int kSegments = 4;           // planned ahead
+constexpr int kSegmentCost = 3, kStreamSegmentCost = 1;      // of a segment besides its units, in units
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
 constexpr float kSlack = 8.f;          // binary exponent by which a score may exceed the reference
 
@@ -53,19 +55,19 @@ struct Segment {
   int kind;                            // 0: whole; 1: continues; 2: begins here and goes on
   long long limit;                     // positions that the tile may see
   __device__ __forceinline__ bool halves() const { return rows > 128; }
-  // Units of group w, and the i-th of them
-  __device__ __forceinline__ int count(int w) const { return halves() ? n : (n + 1 - w) >> 1; }
-  __device__ __forceinline__ int unit(int w, int i) const { return halves() ? i : 2 * i + w; }
+  // Units of the group that takes the first (rel = 0) and of the other, and the i-th of them
+  __device__ __forceinline__ int count(int rel) const { return halves() ? n : (n + 1 - rel) >> 1; }
+  __device__ __forceinline__ int unit(int rel, int i) const { return halves() ? i : 2 * i + rel; }
 };
 
 struct Control {
-  unsigned long long full[12], empty[12], s_ready[2], p_ready[4], pv_done[2], q_ready, drained[2];      // of each group; p_ready: of each half of its unit
+  unsigned long long full[12], empty[12], s_ready[2], p_ready[4], pv_done[2], q_ready, seg_done, drained[2];      // of each group; p_ready: of each half of its unit
   unsigned long long seg_full[kSegments], seg_empty[kSegments];
   Segment seg[kSegments];              // n = 0: no more
   uint32_t tmem;
   int give_up;
   int bad[16];                         // of the last units: some page is none (the ring holds at most six)
-  float2 ml[128];                      // reference and sum of group 1's rows
+  float2 ml[128];                      // reference and sum of the rows of the group that hands its state over
 };
 
 // What a CTA leaves about the segment that begins in it and goes on in later ones.
@@ -83,8 +85,8 @@ struct TreeArgs {
   const void* q;
   void* out;
   float* lse;
-  float* part_o;       // [2 n_cta][D / 4][256][4]
-  float2* part_ml;     // [2 n_cta][256]: reference (binary exponent), sum
+  float* part_o;       // [2 n_cta][D / 4][tile_rows][4]
+  float2* part_ml;     // [2 n_cta][tile_rows]: reference (binary exponent), sum
   TailNote* notes;     // [n_cta]
 };
 
@@ -121,7 +123,7 @@ struct Cursor {
     first = f;
     nodes = ok ? e - f : 0;
     ctx = c;
-    units = ok ? tree_units(a.shape, ctx, nodes) : 0;
+    units = ok ? tree_units(a.shape, ctx, nodes) * a.shape.n_kv_heads : 0;
     return ok;
   }
   __device__ void load(long long in_front) {
@@ -136,7 +138,8 @@ struct Cursor {
     before = in_front + x - units;
     window = in_front + __shfl_sync(0xffffffffu, x, 31);
   }
-  __device__ Cursor(const TreeArgs& args, int lane_, bool reports) : a(args), lane(lane_) {
+  __device__ Cursor(const TreeArgs& args, int lane_, bool reports, bool used = true) : a(args), lane(lane_) {
+    if (!used) return;
     for (int i = lane; i < a.b.n_seq; i += 32) {
       const bool ok = read(i);
       total += units;
@@ -153,29 +156,44 @@ struct Cursor {
     load(0);
   }
   __device__ bool next(Segment* s) {
-    if (u >= u_end) return false;
-    unsigned hit;
-    while (!(hit = __ballot_sync(0xffffffffu, u >= before && u < before + units))) {      // ends: u is below the total
-      w0 += 32;
-      load(window);
+    while (u < u_end) {
+      unsigned hit;
+      while (!(hit = __ballot_sync(0xffffffffu, u >= before && u < before + units))) {      // ends: u is below the total
+        w0 += 32;
+        load(window);
+      }
+      const int src = __ffs(hit) - 1;
+      const long long in_front = __shfl_sync(0xffffffffu, before, src);
+      s->first = __shfl_sync(0xffffffffu, first, src);
+      s->nodes = __shfl_sync(0xffffffffu, nodes, src);
+      s->ctx = __shfl_sync(0xffffffffu, ctx, src);
+      const long long per_head = div_small(__shfl_sync(0xffffffffu, units, src), a.shape.n_kv_heads);
+      const TreeSegment t = tree_segment(a.shape, s->ctx, s->nodes, per_head, u - in_front, u_end - in_front);
+      s->seq = w0 + src;
+      s->head = t.head;
+      s->row0 = t.row_tile * a.shape.tile_rows;
+      s->rows = static_cast<int>(min(static_cast<long long>(s->nodes) * a.shape.group - s->row0, static_cast<long long>(a.shape.tile_rows)));
+      s->chunk0 = t.chunk0;
+      s->n = t.chunk1 - t.chunk0;
+      s->kind = t.chunk0 ? 1 : t.chunk1 < t.chunks ? 2 : 0;
+      s->limit = tree_kv_end(a.shape, s->ctx, s->nodes, t.row_tile);
+      last_unit = u + t.to_end - 1;
+      u += t.places;
+      if (s->n) return true;
     }
-    const int src = __ffs(hit) - 1;
-    const long long in_front = __shfl_sync(0xffffffffu, before, src);
-    s->first = __shfl_sync(0xffffffffu, first, src);
-    s->nodes = __shfl_sync(0xffffffffu, nodes, src);
-    s->ctx = __shfl_sync(0xffffffffu, ctx, src);
-    const TreeSegment t = tree_segment(a.shape, w0 + src, s->ctx, s->nodes, u - in_front, u_end - in_front);
-    s->seq = t.seq;
-    s->head = t.head;
-    s->row0 = t.row_tile * kTileRows;
-    s->rows = static_cast<int>(min(static_cast<long long>(s->nodes) * a.shape.group - s->row0, static_cast<long long>(kTileRows)));
-    s->chunk0 = t.chunk0;
-    s->n = t.chunk1 - t.chunk0;
-    s->kind = t.chunk0 ? 1 : t.chunk1 < t.chunks ? 2 : 0;
-    s->limit = tree_kv_end(a.shape, s->ctx, s->nodes, t.row_tile);
-    last_unit = u + t.chunks - t.chunk0 - 1;
-    u += s->n;
-    return true;
+    return false;
+  }
+  // s: the last segment of the share, kind 0 if there was none
+  __device__ void write_note(const Segment& s) const {
+    TailNote& note = a.notes[blockIdx.x];
+    const bool cut = s.kind == 2 && s.n > 0;
+    note.rows = cut ? s.rows : 0;
+    if (cut) {
+      note.row0 = s.row0;
+      note.first = s.first;
+      note.head = s.head;
+      note.last_cta = tree_cta_of(tree_shares(total, gridDim.x), last_unit);
+    }
   }
   long long last_unit = 0;      // of the whole (sequence, KV head, row tile) of the segment that next() gave
 };
@@ -263,6 +281,13 @@ __device__ __forceinline__ float max_of(const uint32_t (&x)[32], float top) {
   return fmaxf(max3(t[0], t[1], t[2]), fmaxf(t[3], __uint_as_float(x[31])));
 }
 
+template <typename T>
+__device__ __forceinline__ void store4(T* dst, float4 x) {
+  *reinterpret_cast<uint2*>(dst) = make_uint2(Half2Of<T>::pack(x.x, x.y), Half2Of<T>::pack(x.z, x.w));
+}
+template <>
+__device__ __forceinline__ void store4<float>(float* dst, float4 x) { *reinterpret_cast<float4*>(dst) = x; }
+
 // 32 columns of a row of the result, scaled.
 template <typename T>
 __device__ __forceinline__ void store_row(T* dst, const float (&x)[32]) {
@@ -312,7 +337,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
   Control* ctl = reinterpret_cast<Control*>(s_ring + kSlots * Geo::kSlotBytes);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t bar_full = smem_u32(ctl->full), bar_empty = smem_u32(ctl->empty), bar_s = smem_u32(ctl->s_ready), bar_p = smem_u32(ctl->p_ready),
-                 bar_pv = smem_u32(ctl->pv_done), bar_seg = smem_u32(ctl->seg_full), bar_seg_empty = smem_u32(ctl->seg_empty), bar_q = smem_u32(&ctl->q_ready), bar_drain = smem_u32(ctl->drained);
+                 bar_pv = smem_u32(ctl->pv_done), bar_seg = smem_u32(ctl->seg_full), bar_seg_empty = smem_u32(ctl->seg_empty), bar_q = smem_u32(&ctl->q_ready), bar_done = smem_u32(&ctl->seg_done), bar_drain = smem_u32(ctl->drained);
   int* const give_up = &ctl->give_up;
   int* const status = a.pool.status;
 
@@ -333,6 +358,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
       mbar_init(bar_seg_empty + 8 * i, 11);
     }
     mbar_init(bar_q, 8);
+    mbar_init(bar_done, 8);
     mbar_init(bar_drain, 1);
     mbar_init(bar_drain + 8, 1);
     ctl->give_up = 0;
@@ -369,7 +395,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
       // ---- the plan ----
       Cursor cursor(a, lane, blockIdx.x == 0);
       Segment s;
-      s.rows = s.kind = 0;
+      s.kind = 0;
       for (uint32_t i = 0;; ++i) {
         const bool more = cursor.next(&s);
         if (i >= kSegments) wait_segment(bar_seg_empty + 8 * (i % kSegments), (i / kSegments - 1) & 1);
@@ -381,16 +407,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
         __syncwarp();
         if (!more) break;
       }
-      if (lane == 0) {
-        TailNote& note = a.notes[blockIdx.x];
-        note.rows = s.kind == 2 ? s.rows : 0;
-        if (s.kind == 2) {
-          note.row0 = s.row0;
-          note.first = s.first;
-          note.head = s.head;
-          note.last_cta = tree_cta_of(tree_shares(cursor.total, gridDim.x), cursor.last_unit);
-        }
-      }
+      if (lane == 0) cursor.write_note(s);
     } else if (warp == 8) {
         // ---- copies ----
         const int shift = a.pool.page_shift;
@@ -451,12 +468,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
         const Segment* seg;
         for (uint32_t si = 0; (seg = segment(si)); ++si) {
           const bool halves = uniform(seg->rows) > 128;
-          const int n = uniform(seg->n), count = halves ? n : (n + 1 - w) / 2;
+          const uint32_t rel = halves ? w : (w ^ si) & 1;      // tiles of few rows: the groups take turns in beginning
+          const int n = uniform(seg->n), count = halves ? n : (n + 1 - rel) / 2;
           const SmemOperand qq = smem_operand(q_addr + ((halves ? w : si & 1) ? Geo::kQBytes : 0), 16);
           done_with(si);
           bool ok = wait_for(bar_q, si & 1, give_up, status);
           RingPlace<kSlots> pk = ring, pv;      // of the unit whose keys, whose values are due
-          if (!halves && w) pk.step(2);
+          if (!halves && rel) pk.step(2);
           pv = pk;
           pv.step(1);
           auto scores = [&]() {                   // S = Q K^T
@@ -510,11 +528,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
     // ---- softmax ----
     const int w = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
-    const uint32_t t_s = tmem + lanes + w * kTilePos, t_o = tmem + lanes + 256 + w * D;
+    const uint32_t t_s = tmem + lanes + w * kTilePos, t_o = tmem + lanes + 256 + w * D, t_other = tmem + lanes + 256 + (w ^ 1) * D;
     const int group = a.shape.group;
     uint32_t n_units = 0, unit_base = 0;    // taken by this group; of the segments before
     bool loaded = false;                    // the queries of the segment are on their way already
-    bool joined = false;                    // group 0 reads group 1's output of the previous segment
+    bool handed = false;                    // the other group reads this group's output of an earlier segment
 
     // Row x of a segment's tile: its head's place in an array [n_tok][n_q_heads]
     auto place_of = [&](const Segment& g, int t0, int rem0, int x) {
@@ -546,86 +564,104 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
     const Segment* seg;
     for (uint32_t si = 0; (seg = segment(si)); ++si) {
       const Segment& s = *seg;      // read again where it is needed
+      // All warps are done with the segment before: awaited before its queries are overwritten, and by every warp before
+      // it reports this segment (a barrier counts arrivals of one phase at a time).
+      bool before_done = si == 0;
+      auto wait_before = [&]() {
+        if (!before_done) wait_for(bar_done, (si - 1) & 1, give_up, status);
+        before_done = true;
+      };
       if (!loaded) {
+        wait_before();
         load_queries(s, si & 1);
         queries_ready();
       }
-      // A tile of at most 128 rows leaves room for the next one's queries.
+      // A tile of at most 128 rows leaves room for the next one's queries, where the segment before had its own.
       bool next_loads = false;
-      if (!s.halves()) {
+      auto load_next = [&]() {
+        if (s.halves()) return;
         const Segment* next = segment(si + 1);
-        if (next && !next->halves()) {
-          load_queries(*next, (si + 1) & 1);
-          next_loads = true;
-        }
-      }
+        if (!next || next->halves()) return;
+        wait_before();
+        load_queries(*next, (si + 1) & 1);
+        next_loads = true;
+      };
       const int t0 = s.row0 / group, rem0 = s.row0 - t0 * group;
       const int in_tile = (s.halves() ? w * 128 : 0) + r;            // this thread's row
       const bool live = (s.halves() ? w * 128 : 0) + quarter * 32 < s.rows;
       const int node = in_tile < s.rows ? t0 + small_div(rem0 + in_tile, a.group_inverse) : 0;
-      const int count = s.count(w), other = s.count(w ^ 1);
+      const int rel = s.halves() ? w : (w ^ si) & 1;      // tiles of few rows: the groups take turns in beginning
+      const int count = s.count(rel), other = s.count(rel ^ 1);
       RingPlace<kSlots> pk = ring;            // of the unit's keys
-      if (!s.halves() && w) pk.step(2);
+      if (!s.halves() && rel) pk.step(2);
       ring.skip(2 * s.n);
       float m = -INFINITY;
       float2 sum = make_float2(0.f, 0.f);
       // Turns: of the two warps that share an exponential unit, one per group, one uses it at a time, at its full rate,
       // while the other's products run.  Left alone the two fall into step and wait for the same things.
       auto begin_turn = [&](int i) {
-        if (w == 1 || i > 0) asm volatile("bar.sync %0, 64;" ::"r"(3 + 2 * quarter + w) : "memory");
+        if (rel == 1 || i > 0) asm volatile("bar.sync %0, 64;" ::"r"(3 + 2 * quarter + w) : "memory");
       };
       auto end_turn = [&](int i) {
-        if (i + w < other) asm volatile("bar.arrive %0, 64;" ::"r"(3 + 2 * quarter + (w ^ 1)) : "memory");
+        if (i + rel < other) asm volatile("bar.arrive %0, 64;" ::"r"(3 + 2 * quarter + (w ^ 1)) : "memory");
       };
-      // Group 0 may still be reading group 1's output of an earlier segment.
+      // The other group may still be reading this group's output of an earlier segment.
       auto output_free = [&]() {
-        if (joined && w == 1) asm volatile("bar.sync 14, %0;" ::"n"(kSoftmaxThreads) : "memory");
-        joined = false;
+        if (handed) asm volatile("bar.sync %0, %1;" ::"r"(13 + w), "n"(kSoftmaxThreads) : "memory");
+        handed = false;
       };
+      if (count == 0) {      // this segment's queries are complete before the next one's are reported
+        wait_for(bar_q, si & 1, give_up, status);
+        load_next();
+      }
       for (int i = 0; i < count; ++i, ++n_units) {
-        const long long pos0 = static_cast<long long>(s.chunk0 + s.unit(w, i)) * kTilePos;
-        wait_for(bar_s + 8 * w, n_units & 1, give_up, status);
+        const long long pos0 = static_cast<long long>(s.chunk0 + s.unit(rel, i)) * kTilePos;
+        // At the edge: what this thread's row sees, and which of the warp's 32 positions any row sees.  Worked out
+        // before the scores are there; again in the rare case that the unit turns out to have a bad page.
+        bool edge = pos0 + kTilePos > s.ctx, waited = false, bad = false;
+        uint32_t seen[4], seen_any = 0xffffffffu;
+        for (;;) {
+          if (edge) {
+            const SegmentView view{a.b, a.pool, s.first, s.nodes, s.ctx, s.limit, a.b.table + s.seq * a.b.table_stride, bad};
+            seen_any = view.seen_by_any(pos0 + 32 * quarter, lane);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) seen[c] = live ? view.seen_by(node, pos0 + 32 * c) : 0u;
+          }
+          if (waited) break;
+          wait_for(bar_s + 8 * w, n_units & 1, give_up, status);
+          waited = true;
+          bad = *static_cast<volatile int*>(&ctl->bad[(unit_base + s.unit(rel, i)) % 16]) != 0;
+          if (!bad) break;
+          edge = true;
+        }
         tc_fence_after();
-        const bool bad = *static_cast<volatile int*>(&ctl->bad[(unit_base + s.unit(w, i)) % 16]) != 0;
-        const bool edge = pos0 + kTilePos > s.ctx || bad;
-        const SegmentView view{a.b, a.pool, s.first, s.nodes, s.ctx, s.limit, a.b.table + s.seq * a.b.table_stride, bad};
-        if (edge) {
-          // Values at positions that no row sees may be anything, and 0 x NaN is NaN: clear them.
-          const uint32_t seen = view.seen_by_any(pos0 + 32 * quarter, lane);
+        // Values at positions that no row sees may be anything, and 0 x NaN is NaN: they are cleared before P is given out.
+        auto clear_values = [&]() {
+          if (seen_any == 0xffffffffu) return;
           RingPlace<kSlots> pv = pk;
           pv.step(1);
           wait_for(bar_full + 8 * pv.slot, pv.phase, give_up, status);
-          if (!(seen >> lane & 1)) {
+          if (!(seen_any >> lane & 1)) {
             uint8_t* row = s_ring + pv.slot * Geo::kSlotBytes + r * 128;
 #pragma unroll
             for (int c = 0; c < D / 8; ++c) *reinterpret_cast<uint4*>(row + c / 8 * Geo::kPanel + c % 8 * 16) = make_uint4(0, 0, 0, 0);
           }
           fence_async_smem();
-        }
-        pk.step(s.halves() ? 2 : 4);
+        };
         if (live) {
-          if (edge) {
-            // -infinity where the row does not see, in tensor memory: one copy of this code
-#pragma unroll 1
-            for (int c = 0; c < 4; ++c) {
-              uint32_t x[32];
-              tmem_load(x, t_s + 32 * c);
-              const uint32_t seen = view.seen_by(node, pos0 + 32 * c);
-              tmem_wait_load();
-              tmem_use(x);
-#pragma unroll
-              for (int j = 0; j < 32; ++j)
-                if (!(seen >> j & 1)) x[j] = 0xff800000u;
-              tmem_store(t_s + 32 * c, x);
-            }
-            tmem_wait_store();
-          }
           uint32_t sc[4][32];
 #pragma unroll
           for (int c = 0; c < 4; ++c) tmem_load(sc[c], t_s + 32 * c);
           tmem_wait_load();
 #pragma unroll
           for (int c = 0; c < 4; ++c) tmem_use(sc[c]);
+          if (edge) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+              for (int j = 0; j < 32; ++j)
+                if (!(seen[c] >> j & 1)) sc[c][j] = 0xff800000u;
+          }
           float top = -INFINITY;
 #pragma unroll
           for (int c = 0; c < 4; ++c) top = max_of(sc[c], top);
@@ -667,7 +703,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
             if (c == 3) end_turn(i);
             tmem_store(t_s + 16 * c, packed);
             if (c & 1) tmem_wait_store();
-            if (c == 1 && i == 0) output_free();
+            if (c == 1) {
+              clear_values();
+              if (i == 0) output_free();
+            }
             if (c & 1) {
               tc_fence_before();
               __syncwarp();
@@ -677,6 +716,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
         } else {
           begin_turn(i);
           end_turn(i);
+          clear_values();
           if (i == 0) output_free();
           __syncwarp();
           if (lane == 0) {
@@ -684,24 +724,35 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
             mbar_arrive(bar_p + 16 * w + 8);
           }
         }
+        pk.step(s.halves() ? 2 : 4);
+        if (i == 0) load_next();
       }
-      // All products of the segment are done, the other group's too: its queries may be overwritten, S is free.
-      const bool join = !s.halves() && s.n > 1;      // the groups took every other unit each: group 0 adds group 1's state to its own
-      float total = sum.x + sum.y, other_m = -INFINITY, other_sum = 0.f;
-      if (count > 0) wait_for(bar_pv + 8 * w, (n_units - 1) & 1, give_up, status);
-      if (join && w == 1) ctl->ml[r] = make_float2(m, total);
-      tc_fence_before();
-      asm volatile("bar.sync 13, %0;" ::"n"(kSoftmaxThreads) : "memory");
-      tc_fence_after();
-      if (next_loads) queries_ready();
+      // ---- the segment's result ----
+      if (next_loads) queries_ready();      // the next scores may follow this group's last product
       loaded = next_loads;
       unit_base += s.n;
-      if (join && w == 0) {
-        const float2 ml = ctl->ml[r];
-        other_m = ml.x;
-        other_sum = ml.y;
+      const bool join = !s.halves() && s.n > 1;      // the groups took every other unit each: the first one adds the other's state to its own
+      float total = sum.x + sum.y, other_m = -INFINITY, other_sum = 0.f;
+      if (count > 0) wait_for(bar_pv + 8 * w, (n_units - 1) & 1, give_up, status);
+      tc_fence_after();
+      __syncwarp();
+      wait_before();
+      if (lane == 0) mbar_arrive(bar_done);
+      if (join) {
+        if (rel == 1) {
+          ctl->ml[r] = make_float2(m, total);
+          tc_fence_before();
+          asm volatile("bar.arrive %0, %1;" ::"r"(11 + w), "n"(kSoftmaxThreads) : "memory");
+          handed = true;
+        } else {
+          asm volatile("bar.sync %0, %1;" ::"r"(11 + (w ^ 1)), "n"(kSoftmaxThreads) : "memory");
+          tc_fence_after();
+          const float2 ml = ctl->ml[r];
+          other_m = ml.x;
+          other_sum = ml.y;
+        }
       }
-      if (live && (s.halves() || w == 0)) {
+      if (live && (s.halves() || rel == 0)) {
         const float m_all = fmaxf(m, other_m);
         float f0 = m == -INFINITY ? 0.f : ex2(m - m_all), f1 = other_m == -INFINITY ? 0.f : ex2(other_m - m_all);
         total = total * f0 + other_sum * f1;
@@ -718,7 +769,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
           uint32_t o[32], o1[32];
           float y[32];
           tmem_load(o, t_o + 32 * c);
-          if (join) tmem_load(o1, t_o + D + 32 * c);
+          if (join) tmem_load(o1, t_other + 32 * c);
           tmem_wait_load();
           tmem_use(o);
           if (join) {
@@ -745,11 +796,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
         }
       }
       tc_fence_before();
-      if (join && w == 0) asm volatile("bar.arrive 14, %0;" ::"n"(kSoftmaxThreads) : "memory");
-      joined |= join;
+      if (join && rel == 0) asm volatile("bar.arrive %0, %1;" ::"r"(13 + (w ^ 1)), "n"(kSoftmaxThreads) : "memory");
       done_with(si);
     }
-    if (joined && w == 1) asm volatile("bar.sync 14, %0;" ::"n"(kSoftmaxThreads) : "memory");
+    if (handed) asm volatile("bar.sync %0, %1;" ::"r"(13 + w), "n"(kSoftmaxThreads) : "memory");
   }
   tc_fence_before();
   __syncthreads();
@@ -772,16 +822,319 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
   if (warp == 9) tmem_free(tmem, 512);
 }
 
+// ---- few rows ---------------------------------------------------------------------------------------------------------
+// Where a KV head is read by at most 16 M rows of a sequence (single tokens, short drafts), 128-row products are mostly
+// padding and what counts is the path from one short sequence to the next.  Here a CTA of four warps takes a share;
+// each warp streams every fourth group of 16 positions through a ring of its own (16-byte asynchronous copies) and
+// applies it with m16n8k16 products, queries and output in registers; several CTAs per SM hide one another's starts and
+// ends.  The warps' states are joined through shared memory at the end of a segment.
+template <int D, int M> struct StreamGeometry {
+  static constexpr int kStages = 3;
+  static constexpr int kStep = 16;                             // positions
+  static constexpr int kRow = D * 2;                           // bytes
+  static constexpr int kStage = 2 * kStep * kRow;              // keys and values of a step
+  static constexpr int kWarpBytes = kStages * kStage;
+  static constexpr int kBytes = 4 * kWarpBytes + 16 * M * kRow;
+  static constexpr int kCtas = D == 128 ? 2 : M == 1 ? 4 : 3;  // per SM
+  static_assert(16 * M * D * 4 <= kWarpBytes, "a warp's output fits where its ring was");
+};
+
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+template <bool kBf16>
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if constexpr (kBf16)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+template <typename T, typename Out, int D, int M>
+__global__ void __launch_bounds__(128, StreamGeometry<D, M>::kCtas) tree_stream_kernel(const __grid_constant__ TreeArgs a) {
+  using Geo = StreamGeometry<D, M>;
+  constexpr bool kBf16 = !__is_same(T, __half);
+  constexpr int kPieces = D / 8, kRows = 16 * M;      // 16-byte pieces of a row
+  extern __shared__ __align__(128) uint8_t smem_raw[];
+  __shared__ Segment s_seg;
+  __shared__ float2 s_ml[4][kRows];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
+  uint8_t* const s_q = smem_raw + 4 * Geo::kWarpBytes;
+  uint8_t* const my_ring = smem_raw + warp * Geo::kWarpBytes;
+  const uint32_t q_addr = smem_u32(s_q), ring_addr = smem_u32(my_ring);
+  const int group = a.shape.group;
+  pdl_trigger();
+  pdl_wait();
+
+  Cursor cursor(a, lane, blockIdx.x == 0, warp == 0);
+  Segment plan;
+  plan.kind = 0;
+  for (;;) {
+    if (warp == 0) {
+      const bool more = cursor.next(&plan);
+      if (lane == 0) {
+        s_seg = plan;
+        if (!more) s_seg.n = 0;
+      }
+    }
+    __syncthreads();
+    const Segment s = s_seg;
+    if (s.n == 0) break;
+    const int t0 = s.row0 / group, rem0 = s.row0 - t0 * group;
+    auto place_of = [&](int x) {
+      const int y = rem0 + x, t = small_div(y, a.group_inverse);
+      return static_cast<int64_t>(s.first + t0 + t) * a.n_q_heads + s.head * group + (y - t * group);
+    };
+    for (int idx = tid; idx < kRows * kPieces; idx += 128) {
+      const int row = idx / kPieces, piece = idx % kPieces;
+      copy16(q_addr + row * Geo::kRow + (piece ^ (row & 7)) * 16, static_cast<const T*>(a.q) + place_of(row < s.rows ? row : 0) * D + piece * 8, row < s.rows);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+
+    const long long pos_first = static_cast<long long>(s.chunk0) * kTilePos;
+    const long long pos_end = min(static_cast<long long>(s.chunk0 + s.n) * kTilePos, s.limit);
+    const int steps = static_cast<int>((pos_end - pos_first + Geo::kStep - 1) / Geo::kStep);      // the warp's: warp, warp + 4, ...
+    const int32_t* table = a.b.table + s.seq * a.b.table_stride;
+    // Lane's rows of a step: lane / kPieces + 32 / kPieces * i, column piece lane % kPieces; pages hold at least 8
+    // positions, so a step's rows 0..7 and 8..15 lie in one page each.  The page ids are read a step ahead.
+    int page[2] = {-1, -1};
+    uint32_t bad_stages = 0;
+    auto read_pages = [&](int step) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const long long pos = pos_first + step * Geo::kStep + 8 * h;
+        page[h] = pos < pos_end ? __ldg(table + (pos >> a.pool.page_shift)) : -1;
+      }
+    };
+    auto load_step = [&](int step, int stage) {
+      if (step < steps) {
+        const long long pos0 = pos_first + step * Geo::kStep;
+        uint32_t seen = low_bits(pos_end - pos0);
+        bool bad = false;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          if (static_cast<unsigned>(page[h]) >= static_cast<unsigned>(a.pool.n_pages)) {
+            bad |= pos0 + 8 * h < pos_end;
+            seen &= h ? 0x00ffu : 0xff00u;
+          }
+        if (bad && lane == 0) raise(a.pool.status, kBadPage);
+        bad_stages = (bad_stages & ~(1u << stage)) | (bad ? 1u << stage : 0u);
+        if (pos0 + Geo::kStep > s.ctx) {      // rows of the step: those that no row sees are not read, whatever they hold
+          const SegmentView view{a.b, a.pool, s.first, s.nodes, s.ctx, s.limit, table, false};
+          seen &= view.seen_by_any(pos0, lane);
+        }
+        const uint32_t dst = ring_addr + stage * Geo::kStage;
+#pragma unroll
+        for (int i = 0; i < Geo::kStep * kPieces / 32; ++i) {
+          const int r = lane / kPieces + 32 / kPieces * i;
+          const int64_t row = (((static_cast<int64_t>(a.layer) * a.pool.n_pages + page[r >> 3]) * a.pool.n_kv_heads + s.head) << a.pool.page_shift) +
+                              ((pos0 + r) & ((1 << a.pool.page_shift) - 1));
+          const bool there = seen >> r & 1;
+          const int64_t off = there ? row * D + (lane % kPieces) * 8 : 0;
+          const uint32_t at = dst + r * Geo::kRow + ((lane % kPieces) ^ (r & 7)) * 16;
+          copy16(at, static_cast<const T*>(a.pool.k) + off, there);
+          copy16(at + Geo::kStep * Geo::kRow, static_cast<const T*>(a.pool.v) + off, there);
+        }
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    read_pages(warp);
+#pragma unroll
+    for (int i = 0; i < Geo::kStages - 1; ++i) {
+      load_step(warp + 4 * i, i);
+      read_pages(warp + 4 * (i + 1));
+    }
+    asm volatile("cp.async.wait_group %0;" ::"n"(Geo::kStages - 1) : "memory");      // the queries
+    __syncthreads();
+    uint32_t qf[M][D / 16][4];
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) {
+        const int row = 16 * m + (lane & 15);
+        ldsm4(qf[m][k], q_addr + row * Geo::kRow + ((2 * k + (lane >> 4)) ^ (row & 7)) * 16);
+      }
+    float o[M][D / 8][4];
+    float ref[M][2], sum[M][2];
+    int node[M][2];
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int x = 16 * m + 8 * h + g;
+        node[m][h] = x < s.rows ? t0 + small_div(rem0 + x, a.group_inverse) : -1;
+        ref[m][h] = -INFINITY;
+        sum[m][h] = 0.f;
+      }
+#pragma unroll
+      for (int n = 0; n < D / 8; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[m][n][e] = 0.f;
+    }
+    int stage = 0;
+#pragma unroll 1
+    for (int step = warp; step < steps; step += 4) {
+      {
+        const int ahead = stage + Geo::kStages - 1;
+        load_step(step + 4 * (Geo::kStages - 1), ahead >= Geo::kStages ? ahead - Geo::kStages : ahead);
+        read_pages(step + 4 * Geo::kStages);
+      }
+      asm volatile("cp.async.wait_group %0;" ::"n"(Geo::kStages - 1) : "memory");
+      __syncwarp();
+      const uint32_t kk = ring_addr + stage * Geo::kStage, vv = kk + Geo::kStep * Geo::kRow;
+      float sc[M][2][4];
+#pragma unroll
+      for (int m = 0; m < M; ++m)
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc[m][n][e] = 0.f;
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) {
+        uint32_t b[4];      // positions 0..7 and 8..15, two halves of 8 columns each
+        const int row = (lane >> 4) * 8 + (lane & 7);
+        ldsm4(b, kk + row * Geo::kRow + ((2 * k + (lane >> 3 & 1)) ^ (row & 7)) * 16);
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+          mma16816<kBf16>(sc[m][0], qf[m][k], b[0], b[1]);
+          mma16816<kBf16>(sc[m][1], qf[m][k], b[2], b[3]);
+        }
+      }
+      const long long pos0 = pos_first + step * Geo::kStep;
+      const bool bad = bad_stages >> stage & 1;
+      if (pos0 + Geo::kStep > s.ctx || bad) {      // positions that the row does not see, or on a bad page
+        const SegmentView view{a.b, a.pool, s.first, s.nodes, s.ctx, s.limit, table, bad};
+#pragma unroll
+        for (int m = 0; m < M; ++m)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t seen = node[m][h] >= 0 ? view.seen_by(node[m][h], pos0) : 0u;
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+              for (int e = 0; e < 2; ++e)
+                if (!(seen >> (8 * n + 2 * t4 + e) & 1)) sc[m][n][2 * h + e] = -INFINITY;
+          }
+      }
+#pragma unroll
+      for (int m = 0; m < M; ++m) {
+        float top[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) top[h] = fmaxf(fmaxf(sc[m][0][2 * h], sc[m][0][2 * h + 1]), fmaxf(sc[m][1][2 * h], sc[m][1][2 * h + 1])) * a.scale_log2;
+        if (__any_sync(0xffffffffu, top[0] > ref[m][0] + kSlack || top[1] > ref[m][1] + kSlack)) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            float x = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 1));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
+            const float r = x > ref[m][h] + kSlack ? x : ref[m][h];
+            const float f = r == ref[m][h] ? 1.f : ex2(ref[m][h] - r);
+            ref[m][h] = r;
+            sum[m][h] *= f;
+#pragma unroll
+            for (int n = 0; n < D / 8; ++n) {
+              o[m][n][2 * h] *= f;
+              o[m][n][2 * h + 1] *= f;
+            }
+          }
+        }
+        uint32_t p[4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float shift = ref[m][h] == -INFINITY ? 0.f : -ref[m][h];
+#pragma unroll
+          for (int n = 0; n < 2; ++n) {
+            const float x = ex2(fmaf(sc[m][n][2 * h], a.scale_log2, shift)), y = ex2(fmaf(sc[m][n][2 * h + 1], a.scale_log2, shift));
+            sum[m][h] += x + y;
+            p[2 * n + h] = Half2Of<T>::pack(x, y);
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc[m][e >> 1][e & 1] = __uint_as_float(p[e]);      // kept for the second product
+      }
+#pragma unroll
+      for (int n = 0; n < D / 16; ++n) {
+        uint32_t b[4];      // 16 positions, columns 16 n .. + 7 and + 8 .. + 15
+        const int row = (lane >> 3 & 1) * 8 + (lane & 7);
+        ldsm4_t(b, vv + row * Geo::kRow + ((2 * n + (lane >> 4)) ^ (row & 7)) * 16);
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+          const uint32_t p[4] = {__float_as_uint(sc[m][0][0]), __float_as_uint(sc[m][0][1]), __float_as_uint(sc[m][1][0]), __float_as_uint(sc[m][1][1])};
+          mma16816<kBf16>(o[m][2 * n], p, b[0], b[1]);
+          mma16816<kBf16>(o[m][2 * n + 1], p, b[2], b[3]);
+        }
+      }
+      stage = stage + 1 == Geo::kStages ? 0 : stage + 1;
+      __syncwarp();
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncwarp();
+    // ---- the segment's result: every warp's state to shared memory, in place of its ring ----
+    float* my_o = reinterpret_cast<float*>(my_ring);      // [kRows][D]
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int x = 16 * m + 8 * h + g;
+        float z = sum[m][h] + __shfl_xor_sync(0xffffffffu, sum[m][h], 1);
+        z += __shfl_xor_sync(0xffffffffu, z, 2);
+        if (t4 == 0) s_ml[warp][x] = make_float2(ref[m][h], z);
+#pragma unroll
+        for (int n = 0; n < D / 8; ++n) *reinterpret_cast<float2*>(my_o + x * D + 8 * n + 2 * t4) = make_float2(o[m][n][2 * h], o[m][n][2 * h + 1]);
+      }
+    __syncthreads();
+    const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) + (s.kind == 2);
+    for (int idx = tid; idx < s.rows * (D / 4); idx += 128) {
+      // whole rows side by side for the result; for the parts, rows innermost
+      const int x = s.kind == 0 ? idx / (D / 4) : idx % s.rows, quad = s.kind == 0 ? idx % (D / 4) : idx / s.rows;
+      float2 ml[4];
+      float top = -INFINITY, total = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        ml[w] = s_ml[w][x];
+        top = fmaxf(top, ml[w].x);
+      }
+      float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float f = ml[w].x == -INFINITY ? 0.f : ex2(ml[w].x - top);
+        total += ml[w].y * f;
+        const float4 v = *reinterpret_cast<const float4*>(smem_raw + w * Geo::kWarpBytes + (x * D + 4 * quad) * 4);
+        y.x += v.x * f;
+        y.y += v.y * f;
+        y.z += v.z * f;
+        y.w += v.w * f;
+      }
+      if (s.kind == 0) {
+        const float inv = total > 0.f ? 1.f / total : 0.f;
+        const int64_t at = place_of(x);
+        store4(static_cast<Out*>(a.out) + at * D + 4 * quad, make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv));
+        if (a.lse && quad == 0) a.lse[at] = total > 0.f ? (top + log2f(total)) * kLn2 : -INFINITY;
+      } else {
+        reinterpret_cast<float4*>(a.part_o)[(slot * (D / 4) + quad) * kRows + x] = y;
+        if (quad == 0) a.part_ml[slot * kRows + x] = make_float2(top, total);
+      }
+    }
+    __syncthreads();
+  }
+  if (tid == 0) cursor.write_note(plan);
+}
+
 // ---- joining the parts ----------------------------------------------------------------------------------------------
-// blockIdx.x = the CTA in which a cut segment begins, blockIdx.y = 32 of its rows, blockIdx.z = 32 columns; a thread
-// owns one row and 4 columns, so that reads of the parts are contiguous across the warp.  The parts are taken eight at
+// blockIdx.x = the CTA in which a cut segment begins, blockIdx.y = kRows of its rows, blockIdx.z = some of the columns;
+// a thread owns one row and 4 columns, so that reads of the parts are contiguous across the rows.  The parts are taken eight at
 // a time, all their reads in flight: what this kernel costs is the latency of its reads.
-template <typename Out, int D>
+template <typename Out, int D, int kRows>
 __global__ void __launch_bounds__(256) tree_merge_kernel(const __grid_constant__ TreeArgs a) {
   pdl_trigger();
   pdl_wait();
   const TailNote note = a.notes[blockIdx.x];
-  const int row = blockIdx.y * 32 + (threadIdx.x & 31), quad = blockIdx.z * 8 + (threadIdx.x >> 5);
+  const int tile_rows = a.shape.tile_rows;
+  const int row = blockIdx.y * kRows + threadIdx.x % kRows, quad = blockIdx.z * (256 / kRows) + threadIdx.x / kRows;
   if (row >= note.rows) return;
   const int parts = note.last_cta - static_cast<int>(blockIdx.x) + 1;
   float m = -INFINITY, total = 0.f;
@@ -795,8 +1148,8 @@ __global__ void __launch_bounds__(256) tree_merge_kernel(const __grid_constant__
       x[j] = make_float4(0.f, 0.f, 0.f, 0.f);
       if (c0 + j < parts) {
         const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x + c0 + j) + (c0 + j == 0);
-        ml[j] = __ldcg(&a.part_ml[slot * kTileRows + row]);
-        x[j] = __ldcg(reinterpret_cast<const float4*>(a.part_o) + (slot * (D / 4) + quad) * kTileRows + row);
+        ml[j] = __ldcg(&a.part_ml[slot * tile_rows + row]);
+        x[j] = __ldcg(reinterpret_cast<const float4*>(a.part_o) + (slot * (D / 4) + quad) * tile_rows + row);
       }
     }
     float top = m;
@@ -823,8 +1176,7 @@ __global__ void __launch_bounds__(256) tree_merge_kernel(const __grid_constant__
   const int gr = note.row0 + row, group = a.shape.group;
   const int64_t out_row = static_cast<int64_t>(note.first + gr / group) * a.n_q_heads + note.head * group + gr % group;
   Out* dst = static_cast<Out*>(a.out) + out_row * D + 4 * quad;
-  if constexpr (sizeof(Out) == 4) *reinterpret_cast<float4*>(dst) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-  else *reinterpret_cast<uint2*>(dst) = make_uint2(Half2Of<Out>::pack(o.x * inv, o.y * inv), Half2Of<Out>::pack(o.z * inv, o.w * inv));
+  store4(dst, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
   if (a.lse && quad == 0) a.lse[out_row] = total > 0.f ? (m + log2f(total)) * kLn2 : -INFINITY;
 }
 
@@ -833,23 +1185,55 @@ int64_t padded(int64_t n) { return (n + kAlign - 1) / kAlign * kAlign; }
 
 struct Maps { CUtensorMap k, v; };
 
+// Which kernel, by the rows that a KV head has of a sequence on average (the lengths themselves are on the device; each
+// kernel is right for any): up to 32 the streaming kernel, beyond it the tensor-memory kernel.
+int stream_tiles(const BatchView& b, int group) {
+  const int64_t rows = (static_cast<int64_t>(b.n_tok) + b.n_seq - 1) / b.n_seq * group;
+  return rows <= 16 ? 1 : rows <= 32 ? 2 : 0;
+}
+struct Workers {
+  int n, tile_rows;
+};
+Workers workers_of(const prima_paged& pool, const BatchView& b, int group) {
+  const int m = stream_tiles(b, group);
+  return m ? Workers{pool.sm_count * (pool.cfg.head_dim == 128 ? 2 : m == 1 ? 4 : 3), 16 * m} : Workers{pool.sm_count, kTileRows};
+}
+
+template <typename Kernel>
+cudaError_t allow_smem(Kernel kernel, size_t bytes, bool (&done)[kMaxDevices]) {
+  int dev;
+  if (!first_launch_on_device(done, &dev)) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+  if (e == cudaSuccess && dev >= 0) done[dev] = true;
+  return e;
+}
+
+template <typename T, typename Out, int D, int M>
+cudaError_t launch_stream(const TreeArgs& a, int n_cta, cudaStream_t st) {
+  using Geo = StreamGeometry<D, M>;
+  static bool done[kMaxDevices] = {};
+  auto kernel = tree_stream_kernel<T, Out, D, M>;
+  cudaError_t e = allow_smem(kernel, Geo::kBytes, done);
+  if (e == cudaSuccess) e = launch_pdl(kernel, dim3(n_cta), dim3(128), Geo::kBytes, st, a);
+  if (e != cudaSuccess) return e;
+  constexpr int kRows = 16 * M;
+  return launch_pdl(tree_merge_kernel<Out, D, kRows>, dim3(n_cta, 1, D / 4 * kRows / 256), dim3(256), 0, st, a);
+}
+
 template <typename T, typename Out, int D>
-cudaError_t launch_tree(const prima_paged& pool, TreeArgs a, cudaStream_t st) {
+cudaError_t launch_tree(const prima_paged& pool, TreeArgs a, int n_cta, cudaStream_t st) {
+  if (a.shape.tile_rows == 16) return launch_stream<T, Out, D, 1>(a, n_cta, st);
+  if (a.shape.tile_rows == 32) return launch_stream<T, Out, D, 2>(a, n_cta, st);
   using Geo = Geometry<D>;
   constexpr size_t kSmem = 1024 + 2 * Geo::kQBytes + Geo::kSlots * Geo::kSlotBytes + sizeof(Control);
   static_assert(kSmem <= 232448, "shared memory of a CTA");
   static bool done[kMaxDevices] = {};
-  int dev;
   auto kernel = tree_kernel<T, Out, D>;
-  if (first_launch_on_device(done, &dev)) {
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem));
-    if (e != cudaSuccess) return e;
-    if (dev >= 0) done[dev] = true;
-  }
+  cudaError_t e = allow_smem(kernel, kSmem, done);
   const Maps* maps = static_cast<const Maps*>(pool.maps);
-  cudaError_t e = launch_pdl(kernel, dim3(pool.sm_count), dim3(kThreads), kSmem, st, maps->k, maps->v, a);
+  if (e == cudaSuccess) e = launch_pdl(kernel, dim3(n_cta), dim3(kThreads), kSmem, st, maps->k, maps->v, a);
   if (e != cudaSuccess) return e;
-  return launch_pdl(tree_merge_kernel<Out, D>, dim3(pool.sm_count, kTileRows / 32, D / 32), dim3(256), 0, st, a);
+  return launch_pdl(tree_merge_kernel<Out, D, 32>, dim3(n_cta, kTileRows / 32, D / 32), dim3(256), 0, st, a);
 }
 
 }  // namespace
@@ -887,10 +1271,12 @@ using namespace prima;
 
 extern "C" {
 
+// Enough for either kernel: a worker's two parts, of which the tensor-memory kernel has the larger ones.
 int64_t prima_tree_attention_workspace(const prima_paged* p, int n_seq, int n_tok, int n_q_heads) {
   if (!p || n_seq < 1 || n_tok < 1 || n_q_heads < 1) return PRIMA_ERR_ARG;
   const int64_t n = p->sm_count;
-  return padded(n * static_cast<int64_t>(sizeof(TailNote))) + padded(2 * n * kTileRows * static_cast<int64_t>(sizeof(float2))) +
+  static_assert(4 * 32 <= kTileRows, "four workers of the streaming kernel need no more");
+  return padded(4 * n * static_cast<int64_t>(sizeof(TailNote))) + padded(2 * n * kTileRows * static_cast<int64_t>(sizeof(float2))) +
          padded(2 * n * kTileRows * p->cfg.head_dim * static_cast<int64_t>(sizeof(float)));
 }
 
@@ -910,11 +1296,13 @@ int prima_tree_attention(prima_paged* p, int layer, const prima_paged_batch* bat
     return call_fail(PRIMA_ERR_ARG, "prima_tree_attention: workspace too small or not 256-byte aligned");
   CallDevice dev(c.device);
   if (!dev.ok) return call_fail(PRIMA_ERR_CUDA, "cudaSetDevice failed");
-  const int64_t n = p->sm_count;
+  const BatchView view = view_of(*batch);
+  const Workers workers = workers_of(*p, view, n_q_heads / c.n_kv_heads);
+  const int64_t n = workers.n;
   TreeArgs a;
   a.pool = view_of(*p);
-  a.b = view_of(*batch);
-  a.shape = {c.n_kv_heads, n_q_heads / c.n_kv_heads, batch->mask == nullptr, batch->table_stride << p->page_shift};
+  a.b = view;
+  a.shape = {c.n_kv_heads, n_q_heads / c.n_kv_heads, batch->mask == nullptr, batch->table_stride << p->page_shift, workers.tile_rows == kTileRows ? kSegmentCost : kStreamSegmentCost, workers.tile_rows};
   a.layer = layer;
   a.n_q_heads = n_q_heads;
   a.scale_log2 = scale * kLog2e;
@@ -926,13 +1314,13 @@ int prima_tree_attention(prima_paged* p, int layer, const prima_paged_batch* bat
   a.notes = reinterpret_cast<TailNote*>(ws);
   ws += padded(n * static_cast<int64_t>(sizeof(TailNote)));
   a.part_ml = reinterpret_cast<float2*>(ws);
-  ws += padded(2 * n * kTileRows * static_cast<int64_t>(sizeof(float2)));
+  ws += padded(2 * n * workers.tile_rows * static_cast<int64_t>(sizeof(float2)));
   a.part_o = reinterpret_cast<float*>(ws);
-  using launcher = cudaError_t (*)(const prima_paged&, TreeArgs, cudaStream_t);
+  using launcher = cudaError_t (*)(const prima_paged&, TreeArgs, int, cudaStream_t);
   static const launcher table[2][2][2] = {{{launch_tree<__half, float, 64>, launch_tree<__half, float, 128>}, {launch_tree<__half, __half, 64>, launch_tree<__half, __half, 128>}},
                                           {{launch_tree<__nv_bfloat16, float, 64>, launch_tree<__nv_bfloat16, float, 128>},
                                            {launch_tree<__nv_bfloat16, __nv_bfloat16, 64>, launch_tree<__nv_bfloat16, __nv_bfloat16, 128>}}};
-  const cudaError_t e = table[c.dtype == PRIMA_DT_BF16][out_dtype != PRIMA_DT_F32][c.head_dim == 128](*p, a, static_cast<cudaStream_t>(stream));
+  const cudaError_t e = table[c.dtype == PRIMA_DT_BF16][out_dtype != PRIMA_DT_F32][c.head_dim == 128](*p, a, workers.n, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? PRIMA_OK : call_cuda_fail(e, "prima_tree_attention");
 }
 

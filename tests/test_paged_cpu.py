@@ -21,14 +21,15 @@ extern "C" int64_t find(int layers, int pages, int shift, int heads, const int32
   return prima::find_slot({layers, pages, shift, heads}, row, stride, layer, slot);
 }
 using namespace prima;
-extern "C" int64_t units(int heads, int group, int causal, int64_t capacity, int ctx, int nodes) { return tree_units({heads, group, causal, capacity}, ctx, nodes); }
-extern "C" int64_t kv_end(int heads, int group, int causal, int64_t capacity, int ctx, int nodes, int rt) { return tree_kv_end({heads, group, causal, capacity}, ctx, nodes, rt); }
+extern "C" int64_t units(int heads, int group, int causal, int64_t capacity, int overhead, int tile, int ctx, int nodes) { return tree_units({heads, group, causal, capacity, overhead, tile}, ctx, nodes); }
+extern "C" int64_t kv_end(int heads, int group, int causal, int64_t capacity, int tile, int ctx, int nodes, int rt) { return tree_kv_end({heads, group, causal, capacity, 0, tile}, ctx, nodes, rt); }
 extern "C" int64_t share(int64_t units, int n, int c) { return tree_share_begin(tree_shares(units, n), c); }
 extern "C" int cta_of(int64_t units, int n, int64_t u) { return tree_cta_of(tree_shares(units, n), u); }
 extern "C" int small(int x, int d) { return small_div(x, small_inverse(d)); }
-extern "C" void segment(int heads, int group, int causal, int64_t capacity, int seq, int ctx, int nodes, int64_t u, int64_t end, int* out) {
-  const TreeSegment s = tree_segment({heads, group, causal, capacity}, seq, ctx, nodes, u, end);
-  out[0] = s.seq; out[1] = s.head; out[2] = s.row_tile; out[3] = s.chunk0; out[4] = s.chunk1; out[5] = s.chunks;
+extern "C" void segment(int heads, int group, int causal, int64_t capacity, int overhead, int tile, int ctx, int nodes, int64_t u, int64_t end, int64_t* out) {
+  const TreeShape t{heads, group, causal, capacity, overhead, tile};
+  const TreeSegment s = tree_segment(t, ctx, nodes, tree_units(t, ctx, nodes), u, end);
+  out[0] = s.head; out[1] = s.row_tile; out[2] = s.chunk0; out[3] = s.chunk1; out[4] = s.chunks; out[5] = s.places; out[6] = s.to_end;
 }
 ''' % ROOT)
     lib = d / "index.so"
@@ -38,11 +39,11 @@ extern "C" void segment(int heads, int group, int causal, int64_t capacity, int 
     L.find.argtypes = [ctypes.c_int] * 4 + [ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_int64]
     i32, i64 = ctypes.c_int, ctypes.c_int64
     L.units.restype = L.kv_end.restype = L.share.restype = i64
-    L.units.argtypes = [i32, i32, i32, i64, i32, i32]
-    L.kv_end.argtypes = [i32, i32, i32, i64, i32, i32, i32]
+    L.units.argtypes = [i32, i32, i32, i64, i32, i32, i32, i32]
+    L.kv_end.argtypes = [i32, i32, i32, i64, i32, i32, i32, i32]
     L.share.argtypes = [i64, i32, i32]
     L.cta_of.argtypes = [i64, i32, i64]
-    L.segment.argtypes = [i32, i32, i32, i64, i32, i32, i32, i64, i64, ctypes.c_void_p]
+    L.segment.argtypes = [i32, i32, i32, i64, i32, i32, i32, i32, i64, i64, ctypes.c_void_p]
     return L
 
 
@@ -94,24 +95,26 @@ def test_shares_of_tree_attention_cover_every_position_once(index, seed):
     """The segments of all CTAs, put together, are every unit of every (sequence, KV head, row tile), once, in order."""
     rs = np.random.RandomState(seed)
     n_seq, heads, group, causal, n_cta = int(rs.randint(1, 30)), int(rs.choice([1, 2, 8])), int(rs.choice([1, 3, 5, 8, 64])), int(seed % 2), int(rs.choice([1, 3, 148]))
-    capacity = int(rs.choice([512, 1 << 20]))
+    capacity, overhead, tile = int(rs.choice([512, 1 << 20])), int(rs.choice([0, 2, 5])), int(rs.choice([16, 32, 256]))
     ctx, nodes = rs.randint(0, 3000, n_seq), rs.choice([0, 1, 2, 16, 33, 64, 300], n_seq)
-    want = []
+    want, places = [], 0
     for s in range(n_seq):
         for g in range(heads):
-            for rt in range(-(-int(nodes[s]) * group // 256)):
-                last_row = min(int(nodes[s]) * group, 256 * (rt + 1)) - 1
+            for rt in range(-(-int(nodes[s]) * group // tile)):
+                last_row = min(int(nodes[s]) * group, tile * (rt + 1)) - 1
                 end = min(capacity, int(ctx[s]) + (last_row // group + 1 if causal else int(nodes[s])))
-                got_end = index.kv_end(heads, group, causal, capacity, int(ctx[s]), int(nodes[s]), rt)
+                got_end = index.kv_end(heads, group, causal, capacity, tile, int(ctx[s]), int(nodes[s]), rt)
                 assert got_end == end
                 want += [(s, g, rt, c, -(-end // 128)) for c in range(-(-end // 128))]
-    per_seq = [index.units(heads, group, causal, capacity, int(c), int(n)) for c, n in zip(ctx, nodes)]
+                places += overhead + -(-end // 128)
+    per_seq = [heads * index.units(heads, group, causal, capacity, overhead, tile, int(c), int(n)) for c, n in zip(ctx, nodes)]
     total = sum(per_seq)
-    assert total == len(want)
+    assert total == places
     if not total:
         return
     got = []
-    out = (ctypes.c_int * 6)()
+    out = (ctypes.c_int64 * 7)()
+    parts = {}      # CTAs that hold units of a (sequence, KV head, row tile)
     for cta in range(n_cta):
         u, end = index.share(total, n_cta, cta), index.share(total, n_cta, cta + 1)
         assert end - u in (total // n_cta, total // n_cta + 1)
@@ -121,11 +124,20 @@ def test_shares_of_tree_attention_cover_every_position_once(index, seed):
             while u >= first + per_seq[s]:
                 first += per_seq[s]
                 s += 1
-            index.segment(heads, group, causal, capacity, s, int(ctx[s]), int(nodes[s]), u - first, end - first, out)
-            assert out[0] == s and out[4] > out[3]
-            got += [(s, out[1], out[2], c, out[5]) for c in range(out[3], out[4])]
-            u += out[4] - out[3]
+            index.segment(heads, group, causal, capacity, overhead, tile, int(ctx[s]), int(nodes[s]), u - first, end - first, out)
+            head, rt, c0, c1, chunks, n, to_end = out
+            assert n > 0 and c1 >= c0
+            got += [(s, head, rt, c, chunks) for c in range(c0, c1)]
+            if c1 > c0:
+                parts.setdefault((s, head, rt), []).append(cta)
+                assert index.cta_of(total, n_cta, u + to_end - 1) >= cta
+                parts[s, head, rt, "last"] = index.cta_of(total, n_cta, u + to_end - 1)
+            u += n
     assert got == want
+    # the parts of a whole lie in consecutive CTAs, up to the one that is named as the last
+    for k, v in list(parts.items()):
+        if len(k) == 3:
+            assert v == list(range(v[0], v[-1] + 1)) and parts[(*k, "last")] == v[-1]
 
 
 def test_refusals_need_no_gpu():
