@@ -312,25 +312,32 @@ class Context:
 DT_F32, DT_F16, DT_BF16 = 0, 1, 2
 
 
+_DTYPES: dict = {}      # torch type -> code, filled at the first use (torch is imported late)
+
+
 def _dtype_code(t) -> int:
-    import torch
-    code = {torch.float32: DT_F32, torch.float16: DT_F16, torch.bfloat16: DT_BF16}.get(t.dtype)
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.float32: DT_F32, torch.float16: DT_F16, torch.bfloat16: DT_BF16})
+    code = _DTYPES.get(t.dtype)
     if code is None:
         raise ValueError(f"expected float32, float16 or bfloat16, got {t.dtype}")
     return code
 
 
-def _need(t, name: str, dtype: str, shape, device):
+def _need(t, name: str, dtype, shape, device):
     """Checks a contiguous CUDA tensor of a plain argument; returns its address."""
-    if str(t.dtype) != "torch." + dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != device:
+    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
         raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
 def _stream_of(stream, device):
+    """The raw stream: torch's current one on the device unless one is given."""
+    if stream is not None:
+        return stream.cuda_stream
     import torch
-    s = stream if stream is not None else torch.cuda.current_stream(device)
-    return s.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(device.index)
 
 
 def _scratch(n_bytes: int, device, stream):
@@ -351,7 +358,8 @@ class PagedBatch:
     batch serves every layer of a step."""
 
     def __init__(self, table, row_begin, ctx_len, n_tok: int, pos=None, mask=None):
-        n_seq, dev = ctx_len.numel(), ctx_len.device
+        import torch
+        i32, n_seq, dev = torch.int32, ctx_len.numel(), ctx_len.device
         if table.dim() != 2 or not table.is_cuda:
             raise ValueError("table: expected a CUDA tensor [n_seq, pages]")
         self.device, self.n_seq, self.n_tok = dev, n_seq, int(n_tok)
@@ -361,10 +369,10 @@ class PagedBatch:
             if mask.dim() != 2:
                 raise ValueError("mask: expected [n_tok, words]")
             words = mask.shape[1]
-        self.desc = PagedBatchDesc(n_seq, self.n_tok, _need(row_begin, "row_begin", "int32", (n_seq + 1,), dev), _need(ctx_len, "ctx_len", "int32", (n_seq,), dev),
-                                   _need(table, "table", "int32", (n_seq, table.shape[1]), dev), table.shape[1],
-                                   _need(pos, "pos", "int32", (self.n_tok,), dev) if pos is not None else None,
-                                   _need(mask, "mask", "int64", (self.n_tok, words), dev) if mask is not None else None, words)
+        self.desc = PagedBatchDesc(n_seq, self.n_tok, _need(row_begin, "row_begin", i32, (n_seq + 1,), dev), _need(ctx_len, "ctx_len", i32, (n_seq,), dev),
+                                   _need(table, "table", i32, (n_seq, table.shape[1]), dev), table.shape[1],
+                                   _need(pos, "pos", i32, (self.n_tok,), dev) if pos is not None else None,
+                                   _need(mask, "mask", torch.int64, (self.n_tok, words), dev) if mask is not None else None, words)
         self._ref = C.byref(self.desc)
 
 
@@ -378,9 +386,13 @@ class PagedCache:
         self.n_layers, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k_pages.shape
         self.dtype, self.device = k_pages.dtype, k_pages.device
         self._keep = (k_pages, v_pages)
+        import torch
+        self._i32, self._f32 = torch.int32, torch.float32
+        self._code = _dtype_code(k_pages)
         self._h = C.c_void_p()
-        cfg = PagedConfig(*k_pages.shape[:2], self.page_size, self.n_kv_heads, self.head_dim, _dtype_code(k_pages), rope_theta, rope_mode, self.device.index)
-        _check(lib().prima_paged_create(C.byref(cfg), kp, vp, C.byref(self._h)))
+        cfg = PagedConfig(*k_pages.shape[:2], self.page_size, self.n_kv_heads, self.head_dim, self._code, rope_theta, rope_mode, self.device.index)
+        self._lib = lib()
+        _check(self._lib.prima_paged_create(C.byref(cfg), kp, vp, C.byref(self._h)))
 
     def close(self):
         if self._h:
@@ -393,12 +405,12 @@ class PagedCache:
         except Exception:
             pass
 
-    def _rows(self, t, name: str, batch: PagedBatch):
+    def _rows(self, t, name: str, n_tok: int, heads: int, dtype):
         """(address, elements from token to token) of [n_tok, heads, head_dim] with adjacent heads."""
-        if t.dim() != 3 or t.shape[0] != batch.n_tok or t.shape[2] != self.head_dim or t.device != self.device or \
-                t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != self.head_dim):
-            raise ValueError(f"{name}: expected [{batch.n_tok}, heads, {self.head_dim}] on {self.device} with adjacent heads, got {tuple(t.shape)} on {t.device}, strides {t.stride()}")
-        return t.data_ptr(), (t.stride(0) if batch.n_tok > 1 else t.shape[1] * self.head_dim)
+        stride = t.stride()
+        if t.shape != (n_tok, heads, self.head_dim) or t.dtype != dtype or t.device != self.device or stride[2] != 1 or (heads > 1 and stride[1] != self.head_dim):
+            raise ValueError(f"{name}: expected {dtype} [{n_tok}, {heads}, {self.head_dim}] on {self.device} with adjacent heads, got {t.dtype} {tuple(t.shape)} on {t.device}, strides {stride}")
+        return t.data_ptr(), (stride[0] if n_tok > 1 else heads * self.head_dim)
 
     def _batch(self, batch: PagedBatch):
         if batch.device != self.device:
@@ -407,19 +419,20 @@ class PagedCache:
 
     def append(self, layer: int, batch: PagedBatch, q, k, v, q_out=None, stream=None):
         """prima_paged_append: rotate q (or None) and k, write q_out, append k and v to ``layer``."""
-        if k.shape[1:2] != (self.n_kv_heads,) or v.shape[1:2] != (self.n_kv_heads,) or k.dtype != v.dtype or (q is not None and q.dtype != k.dtype):
-            raise ValueError(f"k and v: expected {self.n_kv_heads} heads; q, k and v of one type")
-        kp, ks = self._rows(k, "k", batch)
-        vp, vs = self._rows(v, "v", batch)
+        n, dt = batch.n_tok, k.dtype
+        kp, ks = self._rows(k, "k", n, self.n_kv_heads, dt)
+        vp, vs = self._rows(v, "v", n, self.n_kv_heads, dt)
         qp = qo = None
         qs = heads = 0
         if q is not None:
             heads = q.shape[1]
-            qp, qs = self._rows(q, "q", batch)
-            if q_out is None or q_out.dtype != self.dtype:
-                raise ValueError("q_out: expected a tensor of the cache's type")
-            qo = _need(q_out, "q_out", str(self.dtype)[6:], (batch.n_tok, heads, self.head_dim), self.device)
-        _check(lib().prima_paged_append(self._h, layer, self._batch(batch), qp, kp, vp, _dtype_code(k), heads, qs, ks, vs, qo, _stream_of(stream, self.device)))
+            qp, qs = self._rows(q, "q", n, heads, dt)
+            if q_out is None:
+                raise ValueError("q_out: expected a tensor")
+            qo = _need(q_out, "q_out", self.dtype, (n, heads, self.head_dim), self.device)
+        rc = self._lib.prima_paged_append(self._h, layer, self._batch(batch), qp, kp, vp, _dtype_code(k), heads, qs, ks, vs, qo, _stream_of(stream, self.device))
+        if rc:
+            _check(rc)
 
     def tree_attention_workspace(self, batch: PagedBatch, n_q_heads: int = 0, stream=None):
         """A workspace for ``tree_attention`` (for any number of query heads if none is named); calls that may overlap need one each."""
@@ -430,25 +443,25 @@ class PagedCache:
 
     def tree_attention(self, layer: int, batch: PagedBatch, q, out, scale=None, lse=None, workspace=None, stream=None):
         """prima_tree_attention; ``scale`` defaults to head_dim ** -0.5."""
-        if q.dim() != 3 or q.dtype != self.dtype:
-            raise ValueError("q: expected [n_tok, n_q_heads, head_dim] of the cache's type")
-        heads = q.shape[1]
+        heads = q.shape[1] if q.dim() == 3 else 0
         shape = (batch.n_tok, heads, self.head_dim)
-        qp = _need(q, "q", str(self.dtype)[6:], shape, self.device)
-        op = _need(out, "out", str(out.dtype)[6:], shape, self.device)
-        lp = _need(lse, "lse", "float32", shape[:2], self.device) if lse is not None else None
+        qp = _need(q, "q", self.dtype, shape, self.device)
+        op = _need(out, "out", out.dtype, shape, self.device)
+        lp = _need(lse, "lse", self._f32, shape[:2], self.device) if lse is not None else None
         if workspace is None:
             workspace = self.tree_attention_workspace(batch, heads, stream)
-        _check(lib().prima_tree_attention(self._h, layer, self._batch(batch), qp, heads, scale if scale is not None else self.head_dim ** -0.5, op, _dtype_code(out), lp,
-                                          workspace.data_ptr(), workspace.numel(), _stream_of(stream, self.device)))
+        rc = self._lib.prima_tree_attention(self._h, layer, self._batch(batch), qp, heads, self.head_dim ** -0.5 if scale is None else scale, op, _dtype_code(out), lp,
+                                            workspace.data_ptr(), workspace.numel(), _stream_of(stream, self.device))
+        if rc:
+            _check(rc)
 
     def accept(self, batch: PagedBatch, path, path_len, stream=None):
         """prima_paged_accept: ``path`` int32 [n_seq, longest], ``path_len`` int32 [n_seq]."""
         if path.dim() != 2:
             raise ValueError("path: expected [n_seq, longest path]")
-        pp = _need(path, "path", "int32", (batch.n_seq, path.shape[1]), self.device)
-        pl = _need(path_len, "path_len", "int32", (batch.n_seq,), self.device)
-        _check(lib().prima_paged_accept(self._h, self._batch(batch), pp, pl, path.shape[1], _stream_of(stream, self.device)))
+        pp = _need(path, "path", self._i32, (batch.n_seq, path.shape[1]), self.device)
+        pl = _need(path_len, "path_len", self._i32, (batch.n_seq,), self.device)
+        _check(self._lib.prima_paged_accept(self._h, self._batch(batch), pp, pl, path.shape[1], _stream_of(stream, self.device)))
 
     def reorder(self, table, length, parent, fresh, table_out, length_out, stream=None):
         """prima_paged_reorder: ``parent`` int32 [n_req, keep]; ``table`` int32 [n_req * n_beams, pages]; ``fresh`` int32 [n_req * keep]."""
@@ -456,11 +469,11 @@ class PagedCache:
         rows, pages = table.shape
         if rows % n_req:
             raise ValueError("table: expected a row for every beam of every request")
-        dev = self.device
-        _check(lib().prima_paged_reorder(self._h, n_req, rows // n_req, keep, _need(table, "table", "int32", (rows, pages), dev), pages,
-                                         _need(length, "length", "int32", (rows,), dev), _need(parent, "parent", "int32", (n_req, keep), dev),
-                                         _need(fresh, "fresh", "int32", (n_req * keep,), dev), _need(table_out, "table_out", "int32", (n_req * keep, pages), dev),
-                                         _need(length_out, "length_out", "int32", (n_req * keep,), dev), _stream_of(stream, dev)))
+        dev, i32, new = self.device, self._i32, n_req * keep
+        _check(self._lib.prima_paged_reorder(self._h, n_req, rows // n_req, keep, _need(table, "table", i32, (rows, pages), dev), pages,
+                                             _need(length, "length", i32, (rows,), dev), _need(parent, "parent", i32, (n_req, keep), dev),
+                                             _need(fresh, "fresh", i32, (new,), dev), _need(table_out, "table_out", i32, (new, pages), dev),
+                                             _need(length_out, "length_out", i32, (new,), dev), _stream_of(stream, dev)))
 
     def sync(self, stream=None):
         """Waits; raises if a kernel met a bad page, slot, row or path since the last call."""
@@ -478,16 +491,23 @@ def prima_beam_select_workspace(n_req: int, n_beams: int, vocab: int, keep: int,
 def prima_beam_select(logits, cum, score, parent, token, finished=None, end_token: int = -1, workspace=None, stream=None):
     """prima_beam_select: ``logits`` [n_req, n_beams, vocab] (rows may be padded), ``cum`` fp32 [n_req, n_beams],
     outputs ``score`` fp32, ``parent`` and ``token`` int32 [n_req, keep]."""
-    if logits.dim() != 3 or not logits.is_cuda or logits.stride(2) != 1 or (logits.shape[0] > 1 and logits.stride(0) != logits.shape[1] * logits.stride(1)):
+    import torch
+    shape, step = logits.shape, logits.stride()
+    if len(shape) != 3 or not logits.is_cuda or step[2] != 1 or (shape[0] > 1 and step[0] != shape[1] * step[1]):
         raise ValueError("logits: expected a CUDA tensor [n_req, n_beams, vocab] with evenly spaced rows")
-    n_req, n_beams, vocab = logits.shape
+    n_req, n_beams, vocab = shape
     dev, keep = logits.device, score.shape[-1]
+    beams, kept, f32, i32 = (n_req, n_beams), (n_req, keep), torch.float32, torch.int32
     if workspace is None:
         workspace = prima_beam_select_workspace(n_req, n_beams, vocab, keep, dev, stream)
-    stride = logits.stride(1) if n_beams > 1 else logits.stride(0) if n_req > 1 else vocab
-    import torch
-    with torch.cuda.device(dev):
-        _check(lib().prima_beam_select(logits.data_ptr(), _dtype_code(logits), n_req, n_beams, vocab, stride, _need(cum, "cum", "float32", (n_req, n_beams), dev),
-                                       _need(finished, "finished", "uint8", (n_req, n_beams), dev) if finished is not None else None, end_token, keep,
-                                       _need(score, "score", "float32", (n_req, keep), dev), _need(parent, "parent", "int32", (n_req, keep), dev),
-                                       _need(token, "token", "int32", (n_req, keep), dev), workspace.data_ptr(), workspace.numel(), _stream_of(stream, dev)))
+    stride = step[1] if n_beams > 1 else step[0] if n_req > 1 else vocab
+    args = (logits.data_ptr(), _dtype_code(logits), n_req, n_beams, vocab, stride, _need(cum, "cum", f32, beams, dev),
+            _need(finished, "finished", torch.uint8, beams, dev) if finished is not None else None, end_token, keep, _need(score, "score", f32, kept, dev),
+            _need(parent, "parent", i32, kept, dev), _need(token, "token", i32, kept, dev), workspace.data_ptr(), workspace.numel(), _stream_of(stream, dev))
+    if torch._C._cuda_getDevice() == dev.index:
+        rc = lib().prima_beam_select(*args)
+    else:
+        with torch.cuda.device(dev):
+            rc = lib().prima_beam_select(*args)
+    if rc:
+        _check(rc)
