@@ -20,19 +20,8 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMaxKeep = 64;
 
-struct Best { float x; int32_t w; };                   // a logit and its word
-struct SliceStat { double sum; float top; int32_t n; };
-
-// (value, index) as one integer that orders by value, then by the lower index.  0 is below everything that is stored.
-__device__ __forceinline__ unsigned long long key_of(float x, unsigned idx) {
-  const unsigned u = __float_as_uint(x);
-  const unsigned o = u & 0x80000000u ? ~u : u | 0x80000000u;
-  return static_cast<unsigned long long>(o) << 32 | (0xffffffffu - idx);
-}
-__device__ __forceinline__ unsigned long long key_of(double x) {
-  const unsigned long long u = __double_as_longlong(x);
-  return u >> 63 ? ~u : u | 0x8000000000000000ull;
-}
+struct Best { float x; int32_t w; };                   // a logit and its word; x = -infinity: none
+struct SliceStat { double sum; float top; int32_t unused; };
 
 template <typename T> __device__ __forceinline__ float as_float(T x);
 template <> __device__ __forceinline__ float as_float<float>(float x) { return x; }
@@ -41,39 +30,66 @@ template <> __device__ __forceinline__ float as_float<__nv_bfloat16>(__nv_bfloat
 
 // NaN and -infinity: no candidate; +infinity: the largest finite value.
 __device__ __forceinline__ float usable(float x) { return fminf(fmaxf(x, -INFINITY), FLT_MAX); }
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 
-// The kth largest (k = 1..) of the threads' keys: every thread sorts with its warp, then thread (w, l) counts how many
-// keys of the other warps are above its own by a binary search in their sorted lists.
-__device__ __forceinline__ unsigned long long kth_of_block(unsigned long long key, int k, unsigned long long* s_keys, unsigned long long* s_kth) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-#pragma unroll
-  for (int size = 2; size <= 32; size <<= 1)
-#pragma unroll
-    for (int step = size >> 1; step > 0; step >>= 1) {
-      const unsigned long long o = __shfl_xor_sync(0xffffffffu, key, step);
-      const bool keep_large = ((lane & step) == 0) == ((lane & size) == 0);      // descending overall
-      key = keep_large == (key > o) ? key : o;
-    }
-  s_keys[threadIdx.x] = key;
-  if (threadIdx.x == 0) *s_kth = 0;
+// A bound that at least `keep` of the threads' values reach (-infinity if fewer are above it): the keep-th largest of
+// the maxima of groups of threads.  The groups are the smallest number, 8 .. 64, that holds keep; of thousands of
+// values a few dozen reach the bound, at the cost of a few shuffles.  s_group: 64 values.
+template <typename V>
+__device__ __forceinline__ V block_bound(V mine, int keep, V* s_group, V* s_bound) {
+  const int n_groups = keep <= 8 ? 8 : keep <= 16 ? 16 : keep <= 32 ? 32 : 64, lanes = kThreads / n_groups;
+  const V lowest = static_cast<V>(-INFINITY);
+  for (int o = lanes >> 1; o > 0; o >>= 1) {
+    const V other = __shfl_xor_sync(0xffffffffu, mine, o);
+    mine = other > mine ? other : mine;
+  }
+  if (threadIdx.x % lanes == 0) s_group[threadIdx.x / lanes] = mine;
+  if (threadIdx.x == 0) *s_bound = lowest;
   __syncthreads();
-  if (key != 0) {
-    int rank = lane;
-#pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) {
-      if (w == warp) continue;
-      int above = 0;
-#pragma unroll
-      for (int step = 16; step > 0; step >>= 1)
-        if (s_keys[32 * w + above + step - 1] > key) above += step;
-      if (above == 31 && s_keys[32 * w + 31] > key) above = 32;
-      rank += above;
-    }
-    if (rank == k - 1) *s_kth = key;      // keys that are not 0 are all different
+  if (threadIdx.x < n_groups) {
+    const V v = s_group[threadIdx.x];
+    int rank = 0;
+    for (int j = 0; j < n_groups; ++j) rank += s_group[j] > v || (s_group[j] == v && j < static_cast<int>(threadIdx.x));
+    if (rank == keep - 1) *s_bound = v;
   }
   __syncthreads();
-  return *s_kth;                          // 0: fewer than k keys
+  return *s_bound;
 }
+
+// What is ahead: the higher value, of equal ones the lower index.
+template <typename V>
+__device__ __forceinline__ bool ahead(V x, int i, V y, int j) { return x > y || (x == y && i < j); }
+
+// The best of the CTA's (value, index) pairs, for every thread.
+template <typename V>
+__device__ __forceinline__ void block_best(V& x, int& i, V* s_x, int* s_i) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const V y = __shfl_xor_sync(0xffffffffu, x, o);
+    const int j = __shfl_xor_sync(0xffffffffu, i, o);
+    if (ahead(y, j, x, i)) {
+      x = y;
+      i = j;
+    }
+  }
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) {
+    s_x[threadIdx.x >> 5] = x;
+    s_i[threadIdx.x >> 5] = i;
+  }
+  __syncthreads();
+  for (int w = 0; w < kThreads / 32; ++w)
+    if (ahead(s_x[w], s_i[w], x, i)) {
+      x = s_x[w];
+      i = s_i[w];
+    }
+}
+
+constexpr int kSliceFound = 512;
 
 // E logits per thread: a slice of kThreads * E words of one row.
 template <typename T, int E>
@@ -81,11 +97,9 @@ __global__ void __launch_bounds__(kThreads) beam_slice_kernel(const T* __restric
                                                               const uint8_t* __restrict__ finished, int keep, int n_slices, bool wide,
                                                               SliceStat* __restrict__ stat, Best* __restrict__ best) {
   constexpr int kVec = 16 / sizeof(T);
-  __shared__ unsigned long long s_keys[kThreads], s_kth;
-  __shared__ float s_top[kThreads / 32];
+  __shared__ float s_group[64], s_bound, s_x[kSliceFound];
+  __shared__ int s_w[kSliceFound], s_n;
   __shared__ double s_sum[kThreads / 32];
-  __shared__ int s_n;
-  extern __shared__ unsigned long long s_found[];      // keep * E
   pdl_trigger();
   pdl_wait();
   const int row = blockIdx.y, slice = blockIdx.x;
@@ -96,102 +110,121 @@ __global__ void __launch_bounds__(kThreads) beam_slice_kernel(const T* __restric
   const int first = slice * kThreads * E;
   float x[E];
   // element i of a thread is word first + (i / kVec) * kThreads * kVec + tid * kVec + i % kVec
+  auto word = [&](int i) { return first + (i / kVec) * kThreads * kVec + tid * kVec + i % kVec; };
+  if (wide && first + kThreads * E <= vocab) {
 #pragma unroll
-  for (int i = 0; i < E; i += kVec) {
-    const int w = first + i * kThreads + tid * kVec;
-    if (wide && w + kVec <= vocab) {
-      const uint4 u = __ldcs(reinterpret_cast<const uint4*>(x0 + w));
+    for (int i = 0; i < E; i += kVec) {
+      const uint4 u = __ldcs(reinterpret_cast<const uint4*>(x0 + word(i)));
       const T* e = reinterpret_cast<const T*>(&u);
 #pragma unroll
-      for (int j = 0; j < kVec; ++j) x[i + j] = usable(as_float<T>(e[j]));
-    } else {
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) x[i + j] = w + j < vocab ? usable(as_float<T>(x0[w + j])) : -INFINITY;
+      for (int j = 0; j < kVec; ++j) x[i + j] = as_float<T>(e[j]);
     }
+  } else {
+#pragma unroll
+    for (int i = 0; i < E; ++i) x[i] = word(i) < vocab ? as_float<T>(x0[word(i)]) : -INFINITY;
   }
+#pragma unroll
+  for (int i = 0; i < E; ++i) x[i] = usable(x[i]);
   float top = x[0];
-  int at = 0;
 #pragma unroll
-  for (int i = 1; i < E; ++i)
-    if (x[i] > top) {
-      top = x[i];
-      at = i;
-    }
-  auto word = [&](int i) { return first + (i / kVec) * kThreads * kVec + tid * kVec + i % kVec; };
-  const unsigned long long mine = top > -INFINITY ? key_of(top, word(at)) : 0ull;
-  float m = top;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  if (lane == 0) s_top[warp] = m;
+  for (int i = 1; i < E; ++i) top = fmaxf(top, x[i]);
   if (tid == 0) s_n = 0;
-  const unsigned long long kth = kth_of_block(mine, keep, s_keys, &s_kth);
-  m = s_top[0];
-#pragma unroll
-  for (int w = 1; w < kThreads / 32; ++w) m = fmaxf(m, s_top[w]);
+  const float bound = block_bound(top, keep, s_group, &s_bound);
+  const int n_groups = keep <= 8 ? 8 : keep <= 16 ? 16 : keep <= 32 ? 32 : 64;
+  float m = s_group[0];
+  for (int w = 1; w < n_groups; ++w) m = fmaxf(m, s_group[w]);
   // Sum of exp(x - m): the difference first (exact for the large terms), then one ex2 (relative error 2^-22).
-  float part = 0.f;
+  const float from = m == -INFINITY ? 0.f : m;
+  float part[2] = {0.f, 0.f};
 #pragma unroll
-  for (int i = 0; i < E; ++i) {
-    const float d = x[i] - m;
-    part += d > -INFINITY ? exp2f(d * 1.4426950408889634f) : 0.f;
-  }
-  double sum = part;
+  for (int i = 0; i < E; ++i) part[i & 1] += ex2((x[i] - from) * 1.4426950408889634f);
+  double sum = static_cast<double>(part[0]) + part[1];
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   if (lane == 0) s_sum[warp] = sum;
-  // At most `keep` threads have a best key that reaches the kth, so at most keep * E elements do.
-  if (mine >= kth && mine != 0) {
+  if (top >= bound && top > -INFINITY) {
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-      const unsigned long long k = key_of(x[i], word(i));
-      if (x[i] > -INFINITY && k >= kth) s_found[atomicAdd(&s_n, 1)] = k;
-    }
+    for (int i = 0; i < E; ++i)
+      if (x[i] >= bound && x[i] > -INFINITY) {
+        const int at = atomicAdd(&s_n, 1);
+        if (at < kSliceFound) {
+          s_x[at] = x[i];
+          s_w[at] = word(i);
+        }
+      }
   }
   __syncthreads();
   const int n = s_n;
   const int64_t out = static_cast<int64_t>(row) * n_slices + slice;
-  for (int i = tid; i < n; i += kThreads) {
-    const unsigned long long k = s_found[i];
-    int rank = 0;
-    for (int j = 0; j < n; ++j) rank += s_found[j] > k;
-    if (rank < keep) {
-      const unsigned o = static_cast<unsigned>(k >> 32);
-      best[out * keep + rank] = {__uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o), static_cast<int32_t>(0xffffffffu - static_cast<unsigned>(k))};
-    }
-  }
+  Best* mine = best + out * keep;
   if (tid == 0) {
     double total = 0;
     for (int w = 0; w < kThreads / 32; ++w) total += s_sum[w];
-    stat[out] = {total, m, min(n, keep)};
+    stat[out] = {total, m, 0};
+  }
+  if (n <= kSliceFound) {
+    for (int i = tid; i < max(n, keep); i += kThreads) {
+      if (i >= n) {
+        mine[i] = {-INFINITY, 0};
+        continue;
+      }
+      int rank = 0;
+      for (int j = 0; j < n; ++j) rank += ahead(s_x[j], s_w[j], s_x[i], s_w[i]);
+      if (rank < keep) mine[rank] = {s_x[i], s_w[i]};
+    }
+    return;
+  }
+  // Hundreds of equal logits at the bound: one after the other.
+  float last = INFINITY;
+  int last_w = -1;
+  for (int place = 0; place < keep; ++place) {
+    float bx = -INFINITY;
+    int bw = 0x7fffffff;
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+      if (x[i] > -INFINITY && ahead(last, last_w, x[i], word(i)) && ahead(x[i], word(i), bx, bw)) {
+        bx = x[i];
+        bw = word(i);
+      }
+    block_best(bx, bw, s_x, s_w);
+    if (tid == 0) mine[place] = {bx, bw};
+    last = bx;
+    last_w = bw;
   }
 }
 
 // One CTA per request joins the slices of its beams.
-constexpr int kFound = 2048;
+constexpr int kFound = 1024;
 __global__ void __launch_bounds__(kThreads) beam_join_kernel(int n_beams, int vocab, const float* __restrict__ cum, const uint8_t* __restrict__ finished,
                                                              int end_token, int keep, int n_slices, const SliceStat* __restrict__ stat,
                                                              const Best* __restrict__ best, float* __restrict__ score, int32_t* __restrict__ parent,
                                                              int32_t* __restrict__ token) {
-  __shared__ double s_top[kMaxKeep], s_log[kMaxKeep];      // of every beam: maximum (+infinity: no row was read), log of the sum
-  __shared__ unsigned long long s_keys[kThreads], s_kth, s_best[kThreads / 32];
-  __shared__ double s_score[kFound];
-  __shared__ int s_at[kFound], s_n;
-  __shared__ int s_best_at[kThreads / 32];
+  // of every beam: what its logits are measured from, log of the sum; a beam without candidates: +infinity, 0;
+  // a finished one: NaN (its only candidate is the end token)
+  __shared__ double s_top[kMaxKeep], s_log[kMaxKeep], s_cum[kMaxKeep];
+  __shared__ double s_group[64], s_bound, s_score[kFound], s_bx[kThreads / 32];
+  __shared__ int s_at[kFound], s_n, s_bi[kThreads / 32];
   pdl_trigger();
   pdl_wait();
   const int req = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int row0 = req * n_beams;
+  const int row0 = req * n_beams, per_beam = n_slices * keep;
   for (int b = warp; b < n_beams; b += kThreads / 32) {
     const float c = __ldg(cum + row0 + b);
-    double top = INFINITY, sum = 0;
-    if (!(finished && finished[row0 + b]) && c > -INFINITY) {
+    const bool done = finished && finished[row0 + b];
+    double top = INFINITY, sum = 1;
+    if (done && c > -INFINITY) {
+      top = NAN;
+    } else if (c > -INFINITY) {
       const SliceStat* st = stat + static_cast<int64_t>(row0 + b) * n_slices;
       float m = -INFINITY;
-      for (int i = lane; i < n_slices; i += 32) m = fmaxf(m, st[i].top);
+      for (int i = lane; i < n_slices; i += 32) m = fmaxf(m, __ldcg(&st[i].top));
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-      for (int i = lane; i < n_slices; i += 32)
-        if (st[i].top > -INFINITY) sum += st[i].sum * exp(static_cast<double>(st[i].top) - static_cast<double>(m));
+      sum = 0;
+      for (int i = lane; i < n_slices; i += 32) {
+        const float t = __ldcg(&st[i].top);
+        if (t > -INFINITY) sum += __ldcg(&st[i].sum) * exp(static_cast<double>(t) - static_cast<double>(m));
+      }
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
       if (m > -INFINITY) top = m;
@@ -199,63 +232,42 @@ __global__ void __launch_bounds__(kThreads) beam_join_kernel(int n_beams, int vo
     if (lane == 0) {
       s_top[b] = top;
       s_log[b] = log(sum);
+      s_cum[b] = c;
     }
   }
   if (tid == 0) s_n = 0;
   __syncthreads();
 
-  const int per_beam = n_slices * keep;
-  const int n = n_beams * per_beam;
-  // Candidate i: place i % keep of slice i / keep % n_slices of beam i / per_beam; a finished beam has its end token as
-  // the candidate of place 0 of slice 0.  Returns whether there is one.
-  auto candidate = [&](int i, double* sc, int* at) {
-    const int b = i / per_beam, r = i - b * per_beam, sl = r / keep, place = r - sl * keep;
-    const float c = __ldg(cum + row0 + b);
-    if (!(c > -INFINITY)) return false;
-    if (finished && finished[row0 + b]) {
-      *sc = c;
-      *at = b * vocab + end_token;
-      return r == 0;
+  // Calls f(score, index) for the thread's candidates.  Candidates are dealt out one by one over all beams, so that the
+  // groups of threads whose maxima give the bound are alike.
+  const unsigned n_all = static_cast<unsigned>(n_beams) * per_beam;
+  const Best* list = best + static_cast<int64_t>(row0) * per_beam;
+  auto each = [&](auto f) {
+#pragma unroll 4
+    for (unsigned i = tid; i < n_all; i += kThreads) {
+      const unsigned b = i / per_beam;
+      const double top = s_top[b];
+      if (top < INFINITY) {
+        const float2 e = __ldcg(reinterpret_cast<const float2*>(list + i));
+        if (e.x > -INFINITY) f(s_cum[b] + ((static_cast<double>(e.x) - top) - s_log[b]), static_cast<int>(b) * vocab + __float_as_int(e.y));
+      } else if (top != top && i == b * per_beam) {
+        f(s_cum[b], static_cast<int>(b) * vocab + end_token);
+      }
     }
-    if (isinf(s_top[b])) return false;
-    const int64_t s = static_cast<int64_t>(row0 + b) * n_slices + sl;
-    if (place >= stat[s].n) return false;
-    const Best e = best[s * keep + place];
-    *sc = c + ((static_cast<double>(e.x) - s_top[b]) - s_log[b]);
-    *at = b * vocab + e.w;
-    return true;
   };
-  // ordered by (score, lower index)
-  auto ahead = [](double s, int a, double s2, int a2) { return s > s2 || (s == s2 && a < a2); };
-
   double my = -INFINITY;
-  int my_at = 0x7fffffff;
-  bool any = false;
-  for (int i = tid; i < n; i += kThreads) {
-    double sc;
-    int at;
-    if (candidate(i, &sc, &at) && (!any || ahead(sc, at, my, my_at))) {
-      my = sc;
-      my_at = at;
-      any = true;
-    }
-  }
-  // A bound that at least `keep` threads reach (the scores alone: ties may let a few more through).
-  const unsigned long long mine = any ? key_of(my) : 0ull;
-  const unsigned long long uniq = mine == 0 ? 0 : (mine & ~255ull) | (255 - tid);      // all different; 2^-44 coarser
-  const unsigned long long kth = kth_of_block(uniq, keep, s_keys, &s_kth) & ~255ull;
-  if (mine >= kth && any)
-    for (int i = tid; i < n; i += kThreads) {
-      double sc;
-      int at;
-      if (candidate(i, &sc, &at) && key_of(sc) >= kth) {
+  each([&](double sc, int) { my = sc > my ? sc : my; });
+  const double bound = block_bound(my, keep, s_group, &s_bound);
+  if (my >= bound)
+    each([&](double sc, int at) {
+      if (sc >= bound) {
         const int place = atomicAdd(&s_n, 1);
         if (place < kFound) {
           s_score[place] = sc;
           s_at[place] = at;
         }
       }
-    }
+    });
   __syncthreads();
   const int found = s_n;
   float* o_score = score + static_cast<int64_t>(req) * keep;
@@ -284,44 +296,21 @@ __global__ void __launch_bounds__(kThreads) beam_join_kernel(int n_beams, int vo
   for (int place = 0; place < keep; ++place) {
     double bs = -INFINITY;
     int ba = 0x7fffffff;
-    for (int i = tid; i < n; i += kThreads) {
-      double sc;
-      int at;
-      if (candidate(i, &sc, &at) && (place == 0 || ahead(last, last_at, sc, at)) && ahead(sc, at, bs, ba)) {
+    each([&](double sc, int at) {
+      if (ahead(last, last_at, sc, at) && ahead(sc, at, bs, ba)) {
         bs = sc;
         ba = at;
       }
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      const double s2 = __shfl_xor_sync(0xffffffffu, bs, o);
-      const int a2 = __shfl_xor_sync(0xffffffffu, ba, o);
-      if (ahead(s2, a2, bs, ba)) {
-        bs = s2;
-        ba = a2;
-      }
-    }
-    __syncthreads();
-    if (lane == 0) {
-      s_best[warp] = __double_as_longlong(bs);
-      s_best_at[warp] = ba;
-    }
-    __syncthreads();
-    for (int w = 0; w < kThreads / 32; ++w) {
-      const double s2 = __longlong_as_double(s_best[w]);
-      if (ahead(s2, s_best_at[w], bs, ba)) {
-        bs = s2;
-        ba = s_best_at[w];
-      }
-    }
+    });
+    block_best(bs, ba, s_bx, s_bi);
     if (tid == 0) put(place, bs, ba);
     last = bs;
     last_at = ba;
   }
 }
 
-// Words per thread: 32 where that still gives every SM a few CTAs, else 8, for the latency of small calls.
-int words_per_thread(int64_t rows, int vocab) { return rows * ((vocab + 32 * kThreads - 1) / (32 * kThreads)) >= 4 * 148 ? 32 : 8; }
+// Words per thread: 32 where that still gives every SM two CTAs, else 8, for the latency of small calls.
+int words_per_thread(int64_t rows, int vocab) { return rows * ((vocab + 32 * kThreads - 1) / (32 * kThreads)) >= 2 * 148 ? 32 : 8; }
 int slices_of(int64_t rows, int vocab) {
   const int w = words_per_thread(rows, vocab) * kThreads;
   return (vocab + w - 1) / w;
@@ -337,7 +326,7 @@ cudaError_t launch_select(const void* logits, int n_req, int n_beams, int vocab,
   const bool wide = (reinterpret_cast<uintptr_t>(logits) & 15) == 0 && row_stride % (16 / static_cast<int64_t>(sizeof(T))) == 0;
   const dim3 grid(static_cast<unsigned>(n_slices), static_cast<unsigned>(rows));
   auto kernel = e == 32 ? beam_slice_kernel<T, 32> : beam_slice_kernel<T, 8>;
-  cudaError_t err = launch_pdl(kernel, grid, dim3(kThreads), static_cast<size_t>(keep) * e * 8, st, static_cast<const T*>(logits), row_stride, vocab, cum, finished, keep,
+  cudaError_t err = launch_pdl(kernel, grid, dim3(kThreads), 0, st, static_cast<const T*>(logits), row_stride, vocab, cum, finished, keep,
                                n_slices, wide, stat, best);
   if (err != cudaSuccess) return err;
   return launch_pdl(beam_join_kernel, dim3(static_cast<unsigned>(n_req)), dim3(kThreads), 0, st, n_beams, vocab, cum, finished, end_token, keep, n_slices,

@@ -31,8 +31,7 @@ __global__ void __launch_bounds__(256) append_kernel(PoolView pool, BatchView b,
   const int per_tok = heads * kItems;
   const int n_items = min(kTok, b.n_tok - t0) * per_tok;
 
-  float x[2][8];
-  auto load = [&](int item) {
+  auto load = [&](int item, float (&x)[2][8]) {
     const int tk = item / per_tok, r = item - tk * per_tok;
     const int head = r / kItems, c = r % kItems;
     const int64_t t = t0 + tk;
@@ -47,8 +46,9 @@ __global__ void __launch_bounds__(256) append_kernel(PoolView pool, BatchView b,
       load8(src + 16 * c + 8, wide, x[1]);
     }
   };
+  float x[2][8];
   int item = threadIdx.x;
-  if (item < n_items) load(item);        // in flight while the places are looked up
+  if (item < n_items) load(item, x);      // in flight while the places are looked up
 
   for (int tk = warp; tk < kTok; tk += 8) {
     const int t = t0 + tk;
@@ -80,15 +80,12 @@ __global__ void __launch_bounds__(256) append_kernel(PoolView pool, BatchView b,
   }
   __syncthreads();
 
-  for (; item < n_items; item += 256) {
-    if (item != static_cast<int>(threadIdx.x)) load(item);
+  auto finish = [&](int item, const float (&x)[2][8]) {
     const int tk = item / per_tok, r = item - tk * per_tok;
     const int head = r / kItems, c = r % kItems;
     const int64_t row = s_row[tk];
-    if (row == -2) continue;
     const bool is_q = head < n_q_heads, is_v = head >= n_q_heads + G;
-    if (is_q && !q) continue;
-    if (!is_q && row < 0) continue;
+    if (row == -2 || (is_q ? !q : row < 0)) return;
     T* dst = is_q ? q_out + (static_cast<int64_t>(t0 + tk) * n_q_heads + head) * D
                   : static_cast<T*>(is_v ? pool.v : pool.k) + (row + (static_cast<int64_t>(head - n_q_heads - (is_v ? G : 0)) << pool.page_shift)) * D;
     if (is_v) {
@@ -116,65 +113,84 @@ __global__ void __launch_bounds__(256) append_kernel(PoolView pool, BatchView b,
       store8(dst + 16 * c, u[0]);
       store8(dst + 16 * c + 8, u[1]);
     }
+  };
+  while (item < n_items) {
+    finish(item, x);
+    item += 256;
+    if (item < n_items) load(item, x);
   }
 }
 
 // ---- accepted paths ---------------------------------------------------------------------------------------------
-// One warp per (sequence, layer, keys or values, KV head): rows path[0..n-1] of the step move to rows 0..n-1.  path
-// ascends, so path[j] >= j: a batch of up to 32 rows that is read whole before any of it is written never overwrites
-// a row that a later batch reads.
+// Rows path[0..n-1] of a sequence's step move to rows 0..n-1, in every layer.  blockIdx.x = the sequence; its CTAs look
+// the rows' places up once and share the columns: a column is 16 bytes of one head of keys or values of one layer, and
+// a thread moves it for all rows, in ascending order.  path ascends, so path[j] >= j: what is read for row j is
+// overwritten at the earliest for row path[j], and a batch that is read whole before any of it is written keeps that.
+constexpr int kPathBatch = 8, kPathBlock = 256;
 template <int D>
-__global__ void __launch_bounds__(128) accept_kernel(PoolView pool, BatchView b, const int32_t* __restrict__ path, const int32_t* __restrict__ path_len,
+__global__ void __launch_bounds__(256) accept_kernel(PoolView pool, BatchView b, const int32_t* __restrict__ path, const int32_t* __restrict__ path_len,
                                                      int path_stride) {
-  constexpr int kPieces = D * 2 / 16, kRows = 32 / kPieces;      // 16-byte pieces of a row, rows per warp instruction
-  const int lane = threadIdx.x & 31;
-  const int s = blockIdx.x;
-  const int G = pool.n_kv_heads;
-  const int64_t w = static_cast<int64_t>(blockIdx.y) * 4 + (threadIdx.x >> 5);
-  if (w >= static_cast<int64_t>(pool.n_layers) * 2 * G) return;
-  const int g = static_cast<int>(w % G), layer = static_cast<int>(w / G / 2);
-  uint4* const base = static_cast<uint4*>(w / G % 2 ? pool.v : pool.k);
-  const int first = __ldg(b.row_begin + s), end = __ldg(b.row_begin + s + 1), ctx = __ldg(b.ctx_len + s);
-  int n = __ldg(path_len + s);
+  constexpr int kPieces = D / 8;                  // 16-byte pieces of a row
+  __shared__ int2 s_move[kPathBlock];             // page and row in the page, packed: from, to; from < 0: stays
+  __shared__ int2 s_in[kPathBlock];
+  pdl_trigger();
+  pdl_wait();
+  const int s = blockIdx.x, G = pool.n_kv_heads;
+  const int first = __ldg(b.row_begin + s), end = __ldg(b.row_begin + s + 1), ctx = __ldg(b.ctx_len + s), n = __ldg(path_len + s);
   if (first < 0 || end < first || end > b.n_tok || ctx < 0 || n < 0 || n > path_stride) {
-    if (lane == 0) raise(pool.status, n < 0 || n > path_stride ? kBadPath : kBadRows);
+    if (threadIdx.x == 0) raise(pool.status, n < 0 || n > path_stride ? kBadPath : kBadRows);
     return;
   }
-  for (int j0 = 0; j0 < n; j0 += 32) {
-    int64_t from = -1, to = -1;
-    if (j0 + lane < n) {
-      const int a = __ldg(path + static_cast<int64_t>(s) * path_stride + j0 + lane);
+  const int32_t* table = b.table + s * b.table_stride;
+  const int in_page = (1 << pool.page_shift) - 1;
+  const int64_t columns = static_cast<int64_t>(pool.n_layers) * 2 * G * kPieces;
+  for (int j0 = 0; j0 < n; j0 += kPathBlock) {
+    const int m = min(n - j0, kPathBlock);
+    __syncthreads();
+    if (static_cast<int>(threadIdx.x) < m) {
+      const int j = j0 + threadIdx.x, a = __ldg(path + static_cast<int64_t>(s) * path_stride + j);
+      int2 pages = make_int2(-1, 0), rows = make_int2(0, 0);
       if (a < 0 || a >= end - first) {
         raise(pool.status, kBadPath);
-      } else if (a != j0 + lane) {
-        const int32_t* row = b.table + s * b.table_stride;
-        from = slot_row(pool, row, b.table_stride, layer, static_cast<int64_t>(ctx) + a);
-        to = slot_row(pool, row, b.table_stride, layer, static_cast<int64_t>(ctx) + j0 + lane);
+      } else if (a != j) {
+        const int64_t from = static_cast<int64_t>(ctx) + a, to = static_cast<int64_t>(ctx) + j;
+        if (slot_row(pool, table, b.table_stride, 0, from) >= 0 && slot_row(pool, table, b.table_stride, 0, to) >= 0) {
+          pages = make_int2(__ldg(table + (from >> pool.page_shift)), __ldg(table + (to >> pool.page_shift)));
+          rows = make_int2(static_cast<int>(from) & in_page, static_cast<int>(to) & in_page);
+        }
+      }
+      s_move[threadIdx.x] = pages;
+      s_in[threadIdx.x] = rows;
+    }
+    __syncthreads();
+    for (int64_t c = static_cast<int64_t>(blockIdx.y) * 256 + threadIdx.x; c < columns; c += static_cast<int64_t>(gridDim.y) * 256) {
+      const int piece = static_cast<int>(c % kPieces), w = static_cast<int>(c / kPieces), g = w % G, lv = w / G;      // lv: layer and keys or values
+      uint4* const base = static_cast<uint4*>(lv & 1 ? pool.v : pool.k) + piece;
+      const int64_t layer = static_cast<int64_t>(lv >> 1) * pool.n_pages;
+      auto at = [&](int page, int row) { return ((((layer + page) * G + g) << pool.page_shift) + row) * kPieces; };
+      for (int j = 0; j < m; j += kPathBatch) {
+        uint4 x[kPathBatch];
+#pragma unroll
+        for (int i = 0; i < kPathBatch; ++i)
+          if (j + i < m && s_move[j + i].x >= 0) x[i] = __ldcg(base + at(s_move[j + i].x, s_in[j + i].x));
+#pragma unroll
+        for (int i = 0; i < kPathBatch; ++i)
+          if (j + i < m && s_move[j + i].x >= 0) base[at(s_move[j + i].y, s_in[j + i].y)] = x[i];
       }
     }
-    const int64_t shift = static_cast<int64_t>(g) << pool.page_shift;
-    uint4 x[kPieces];
-#pragma unroll
-    for (int i = 0; i < kPieces; ++i) {
-      const int64_t f = __shfl_sync(0xffffffffu, from, i * kRows + lane / kPieces), o = __shfl_sync(0xffffffffu, to, i * kRows + lane / kPieces);
-      if (f >= 0 && o >= 0) x[i] = __ldcg(base + (f + shift) * kPieces + lane % kPieces);
-    }
-#pragma unroll
-    for (int i = 0; i < kPieces; ++i) {
-      const int64_t f = __shfl_sync(0xffffffffu, from, i * kRows + lane / kPieces), o = __shfl_sync(0xffffffffu, to, i * kRows + lane / kPieces);
-      if (f >= 0 && o >= 0) base[(o + shift) * kPieces + lane % kPieces] = x[i];
-    }
-    __syncwarp();
   }
 }
 
 // ---- reordering of beams ----------------------------------------------------------------------------------------
-// blockIdx.x = new row; the first CTA of a row writes its table and length, and one warp per (layer, keys or values,
-// KV head) copies the entries of the last page when an earlier row of the request has the same parent.  The entries
-// of one head are consecutive, (length % page_size) * head_dim * 2 bytes.
-__global__ void __launch_bounds__(128) reorder_kernel(PoolView pool, int D, int n_beams, int keep, const int32_t* __restrict__ table_in, int64_t stride,
+// blockIdx.x = new row; the first CTA of a row writes its table and length.  When an earlier row of the request has the
+// same parent, the row's CTAs copy the entries of the last page in all layers; those of one head are consecutive,
+// (length % page_size) * head_dim * 2 bytes.
+template <int D>
+__global__ void __launch_bounds__(256) reorder_kernel(PoolView pool, int n_beams, int keep, const int32_t* __restrict__ table_in, int64_t stride,
                                                       const int32_t* __restrict__ length_in, const int32_t* __restrict__ parent,
                                                       const int32_t* __restrict__ fresh, int32_t* __restrict__ table_out, int32_t* __restrict__ length_out) {
+  pdl_trigger();
+  pdl_wait();
   const int r = blockIdx.x, req = r / keep, j = r - req * keep;
   const int lane = threadIdx.x & 31;
   const int G = pool.n_kv_heads;
@@ -183,6 +199,7 @@ __global__ void __launch_bounds__(128) reorder_kernel(PoolView pool, int D, int 
   bool shared_parent = false;
   for (int i = lane; i < j; i += 32) shared_parent |= __ldg(parent + r - j + i) == p;
   shared_parent = __any_sync(0xffffffffu, shared_parent);
+  if (!shared_parent && blockIdx.y > 0) return;
   const bool bad = p < 0 || p >= n_beams;
   if (bad) p = 0;
   const int64_t src = static_cast<int64_t>(req) * n_beams + p;
@@ -204,24 +221,28 @@ __global__ void __launch_bounds__(128) reorder_kernel(PoolView pool, int D, int 
       table_out[r * stride + i] = bad_len || i >= pages ? -1 : copies && i == pages - 1 ? f : __ldg(table_in + src * stride + i);
   }
   if (!copies || bad_page) return;
-  const int64_t w = static_cast<int64_t>(blockIdx.y) * 4 + (threadIdx.x >> 5);
-  if (w >= static_cast<int64_t>(pool.n_layers) * 2 * G) return;
-  const int g = static_cast<int>(w % G);
-  const int64_t layer = w / G / 2;
-  const int pieces_row = D / 8;
-  uint4* const base = static_cast<uint4*>(w / G % 2 ? pool.v : pool.k);
-  const uint4* from = base + ((((layer * pool.n_pages + last) * G + g) << pool.page_shift)) * pieces_row;
-  uint4* to = base + ((((layer * pool.n_pages + f) * G + g) << pool.page_shift)) * pieces_row;
-  const int n = tail * pieces_row;
-  int i = lane;
-  for (; i + 96 < n; i += 128) {
-    const uint4 a = __ldcg(from + i), c = __ldcg(from + i + 32), d = __ldcg(from + i + 64), e = __ldcg(from + i + 96);
-    to[i] = a;
-    to[i + 32] = c;
-    to[i + 64] = d;
-    to[i + 96] = e;
+  const uint32_t n = static_cast<uint32_t>(tail) * (D / 8);      // 16-byte pieces of a head
+  const int64_t total = static_cast<int64_t>(pool.n_layers) * 2 * G * n;
+  const int64_t step = static_cast<int64_t>(gridDim.y) * 256;
+  for (int64_t c = static_cast<int64_t>(blockIdx.y) * 256 + threadIdx.x; c < total; c += 4 * step) {
+    uint4 x[4];
+    uint4* to[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t k = c + i * step;
+      if (k >= total) continue;
+      const int64_t w = div_small(k, n);
+      const uint32_t piece = static_cast<uint32_t>(k - w * n);
+      const int g = static_cast<int>(w % G), lv = static_cast<int>(w / G);
+      uint4* const base = static_cast<uint4*>(lv & 1 ? pool.v : pool.k) + piece;
+      const int64_t layer = static_cast<int64_t>(lv >> 1) * pool.n_pages;
+      x[i] = __ldcg(base + ((((layer + last) * G + g) << pool.page_shift)) * (D / 8));
+      to[i] = base + ((((layer + f) * G + g) << pool.page_shift)) * (D / 8);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (c + i * step < total) *to[i] = x[i];
   }
-  for (; i < n; i += 32) to[i] = __ldcg(from + i);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -365,12 +386,12 @@ int prima_paged_accept(prima_paged* p, const prima_paged_batch* batch, const int
   if (!path || !path_len || path_stride < 1) return call_fail(PRIMA_ERR_ARG, "prima_paged_accept: path, path_len and a positive path_stride are needed");
   CallDevice dev(p->cfg.device);
   if (!dev.ok) return call_fail(PRIMA_ERR_CUDA, "cudaSetDevice failed");
-  const int64_t warps = static_cast<int64_t>(p->cfg.n_layers) * 2 * p->cfg.n_kv_heads;
-  if ((warps + 3) / 4 > 65535) return call_fail(PRIMA_ERR_ARG, "prima_paged_accept: layers * KV heads above 131070");
-  const dim3 grid(static_cast<unsigned>(batch->n_seq), static_cast<unsigned>((warps + 3) / 4));
+  // CTAs of a sequence: as many as its columns fill, and as keep every SM busy with all sequences together
+  const int64_t columns = static_cast<int64_t>(p->cfg.n_layers) * 2 * p->cfg.n_kv_heads * (p->cfg.head_dim / 8);
+  const int64_t share = std::max<int64_t>(1, (8 * static_cast<int64_t>(p->sm_count) + batch->n_seq - 1) / batch->n_seq);
+  const dim3 grid(static_cast<unsigned>(batch->n_seq), static_cast<unsigned>(std::min<int64_t>({(columns + 255) / 256, share, 65535})));
   auto kernel = p->cfg.head_dim == 128 ? accept_kernel<128> : accept_kernel<64>;
-  kernel<<<grid, 128, 0, static_cast<cudaStream_t>(stream)>>>(view_of(*p), view_of(*batch), path, path_len, path_stride);
-  const cudaError_t e = cudaGetLastError();
+  const cudaError_t e = launch_pdl(kernel, grid, dim3(256), 0, static_cast<cudaStream_t>(stream), view_of(*p), view_of(*batch), path, path_len, path_stride);
   return e == cudaSuccess ? PRIMA_OK : call_cuda_fail(e, "prima_paged_accept");
 }
 
@@ -387,12 +408,13 @@ int prima_paged_reorder(prima_paged* p, int n_req, int n_beams, int keep, const 
     return call_fail(PRIMA_ERR_ARG, "prima_paged_reorder: the new tables overlap the old ones");
   CallDevice dev(p->cfg.device);
   if (!dev.ok) return call_fail(PRIMA_ERR_CUDA, "cudaSetDevice failed");
-  const int64_t warps = static_cast<int64_t>(p->cfg.n_layers) * 2 * p->cfg.n_kv_heads;
-  if ((warps + 3) / 4 > 65535) return call_fail(PRIMA_ERR_ARG, "prima_paged_reorder: layers * KV heads above 131070");
-  const dim3 grid(static_cast<unsigned>(rows_out), static_cast<unsigned>((warps + 3) / 4));
-  reorder_kernel<<<grid, 128, 0, static_cast<cudaStream_t>(stream)>>>(view_of(*p), p->cfg.head_dim, n_beams, keep, table_in, table_stride, length_in, parent,
-                                                                    fresh, table_out, length_out);
-  const cudaError_t e = cudaGetLastError();
+  // CTAs of a row: enough that a few rows which copy a whole page fill the GPU, as far as a page has pieces for them
+  const int64_t pieces = static_cast<int64_t>(p->cfg.n_layers) * 2 * p->cfg.n_kv_heads * p->cfg.page_size * (p->cfg.head_dim / 8);
+  const int64_t share = std::max<int64_t>(1, (16 * static_cast<int64_t>(p->sm_count) + rows_out - 1) / rows_out);
+  const dim3 grid(static_cast<unsigned>(rows_out), static_cast<unsigned>(std::min<int64_t>({(pieces + 1023) / 1024, share, 65535})));
+  auto kernel = p->cfg.head_dim == 128 ? reorder_kernel<128> : reorder_kernel<64>;
+  const cudaError_t e = launch_pdl(kernel, grid, dim3(256), 0, static_cast<cudaStream_t>(stream), view_of(*p), n_beams, keep, table_in, table_stride, length_in, parent,
+                                   fresh, table_out, length_out);
   return e == cudaSuccess ? PRIMA_OK : call_cuda_fail(e, "prima_paged_reorder");
 }
 
