@@ -2,8 +2,8 @@
 //
 //   score(b, w) = cum[b] + (x[b][w] - m_b - log sum_v exp(x[b][v] - m_b)),   m_b = max_v x[b][v]
 //
-// The logits are read once.  A CTA holds a slice of one row in registers and leaves the slice's maximum, its sum of
-// exponentials and its `keep` best logits; a second kernel joins the slices of a request.  Within a row the order of
+// The logits are read once.  A CTA holds slices of one row in registers, one after the other, and leaves each slice's
+// maximum and sum of exponentials and its `keep` best logits; a second kernel joins the slices of a request.  Within a row the order of
 // the scores is the order of the logits, so the slices can be cut down before the row's sum is known.
 // Which of two near candidates of DIFFERENT beams is ahead depends on the last bits of the two sums, so everything
 // behind a thread's own partial sum is in 64 bits.  Every sum has a fixed order that follows the index in the row, not
@@ -91,101 +91,121 @@ __device__ __forceinline__ void block_best(V& x, int& i, V* s_x, int* s_i) {
 
 constexpr int kSliceFound = 512;
 
-// E logits per thread: a slice of kThreads * E words of one row.
+// E logits per thread: a slice of kThreads * E words of one row.  A CTA takes `per_split` consecutive slices of a row,
+// the next one's logits in flight while it works on the current one, and leaves a maximum and a sum for each of them and
+// the `keep` best logits of them all.
 template <typename T, int E>
 __global__ void __launch_bounds__(kThreads) beam_slice_kernel(const T* __restrict__ logits, int64_t row_stride, int vocab, const float* __restrict__ cum,
-                                                              const uint8_t* __restrict__ finished, int keep, int n_slices, bool wide,
+                                                              const uint8_t* __restrict__ finished, int keep, int n_slices, int per_split, bool wide,
                                                               SliceStat* __restrict__ stat, Best* __restrict__ best) {
   constexpr int kVec = 16 / sizeof(T);
   __shared__ float s_group[64], s_bound, s_x[kSliceFound];
   __shared__ int s_w[kSliceFound], s_n;
   __shared__ double s_sum[kThreads / 32];
+  __shared__ Best s_keep[kMaxKeep];
   pdl_trigger();
   pdl_wait();
-  const int row = blockIdx.y, slice = blockIdx.x;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int row = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const float c = __ldg(cum + row);
   if ((finished && finished[row]) || !(c > -INFINITY)) return;
   const T* x0 = logits + row * row_stride;
-  const int first = slice * kThreads * E;
-  float x[E];
-  // element i of a thread is word first + (i / kVec) * kThreads * kVec + tid * kVec + i % kVec
-  auto word = [&](int i) { return first + (i / kVec) * kThreads * kVec + tid * kVec + i % kVec; };
-  if (wide && first + kThreads * E <= vocab) {
+  const int slice0 = blockIdx.x * per_split, slice1 = min(slice0 + per_split, n_slices);
+  // element i of a thread is word slice * kThreads * E + (i / kVec) * kThreads * kVec + tid * kVec + i % kVec
+  auto word = [&](int slice, int i) { return slice * kThreads * E + (i / kVec) * kThreads * kVec + tid * kVec + i % kVec; };
+  auto load = [&](int slice, uint4 (&u)[E / kVec]) {
+    if (wide && (slice + 1) * kThreads * E <= vocab) {
 #pragma unroll
-    for (int i = 0; i < E; i += kVec) {
-      const uint4 u = __ldcs(reinterpret_cast<const uint4*>(x0 + word(i)));
-      const T* e = reinterpret_cast<const T*>(&u);
+      for (int i = 0; i < E / kVec; ++i) u[i] = __ldcs(reinterpret_cast<const uint4*>(x0 + word(slice, i * kVec)));
+    } else {
+      const T none = static_cast<T>(-INFINITY);
 #pragma unroll
-      for (int j = 0; j < kVec; ++j) x[i + j] = as_float<T>(e[j]);
+      for (int i = 0; i < E; ++i) {
+        const int w = word(slice, i);
+        reinterpret_cast<T*>(u)[i] = w < vocab ? x0[w] : none;
+      }
     }
-  } else {
-#pragma unroll
-    for (int i = 0; i < E; ++i) x[i] = word(i) < vocab ? as_float<T>(x0[word(i)]) : -INFINITY;
-  }
-#pragma unroll
-  for (int i = 0; i < E; ++i) x[i] = usable(x[i]);
-  float top = x[0];
-#pragma unroll
-  for (int i = 1; i < E; ++i) top = fmaxf(top, x[i]);
+  };
+  uint4 next[E / kVec];
+  load(slice0, next);
   if (tid == 0) s_n = 0;
-  const float bound = block_bound(top, keep, s_group, &s_bound);
+  float bound = -INFINITY;
+  bool overflow = false;
   const int n_groups = keep <= 8 ? 8 : keep <= 16 ? 16 : keep <= 32 ? 32 : 64;
-  float m = s_group[0];
-  for (int w = 1; w < n_groups; ++w) m = fmaxf(m, s_group[w]);
-  // Sum of exp(x - m): the difference first (exact for the large terms), then one ex2 (relative error 2^-22).
-  const float from = m == -INFINITY ? 0.f : m;
-  float part[2] = {0.f, 0.f};
+  for (int slice = slice0; slice < slice1; ++slice) {
+    float x[E];
 #pragma unroll
-  for (int i = 0; i < E; ++i) part[i & 1] += ex2((x[i] - from) * 1.4426950408889634f);
-  double sum = static_cast<double>(part[0]) + part[1];
+    for (int i = 0; i < E; ++i) x[i] = usable(as_float<T>(reinterpret_cast<const T*>(next)[i]));
+    if (slice + 1 < slice1) load(slice + 1, next);
+    float top = x[0];
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  if (lane == 0) s_sum[warp] = sum;
-  if (top >= bound && top > -INFINITY) {
+    for (int i = 1; i < E; ++i) top = fmaxf(top, x[i]);
+    bound = fmaxf(bound, block_bound(top, keep, s_group, &s_bound));
+    float m = s_group[0];
+    for (int w = 1; w < n_groups; ++w) m = fmaxf(m, s_group[w]);
+    // Sum of exp(x - m): the difference first (exact for the large terms), then one ex2 (relative error 2^-22).
+    const float from = m == -INFINITY ? 0.f : m;
+    float part[2] = {0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < E; ++i)
-      if (x[i] >= bound && x[i] > -INFINITY) {
-        const int at = atomicAdd(&s_n, 1);
-        if (at < kSliceFound) {
-          s_x[at] = x[i];
-          s_w[at] = word(i);
+    for (int i = 0; i < E; ++i) part[i & 1] += ex2((x[i] - from) * 1.4426950408889634f);
+    double sum = static_cast<double>(part[0]) + part[1];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) s_sum[warp] = sum;
+    if (top >= bound && top > -INFINITY) {
+#pragma unroll
+      for (int i = 0; i < E; ++i)
+        if (x[i] >= bound && x[i] > -INFINITY) {
+          const int at = atomicAdd(&s_n, 1);
+          if (at < kSliceFound) {
+            s_x[at] = x[i];
+            s_w[at] = word(slice, i);
+          }
         }
-      }
-  }
-  __syncthreads();
-  const int n = s_n;
-  const int64_t out = static_cast<int64_t>(row) * n_slices + slice;
-  Best* mine = best + out * keep;
-  if (tid == 0) {
-    double total = 0;
-    for (int w = 0; w < kThreads / 32; ++w) total += s_sum[w];
-    stat[out] = {total, m, 0};
-  }
-  if (n <= kSliceFound) {
-    for (int i = tid; i < max(n, keep); i += kThreads) {
-      if (i >= n) {
-        mine[i] = {-INFINITY, 0};
-        continue;
-      }
-      int rank = 0;
-      for (int j = 0; j < n; ++j) rank += ahead(s_x[j], s_w[j], s_x[i], s_w[i]);
-      if (rank < keep) mine[rank] = {s_x[i], s_w[i]};
     }
+    __syncthreads();
+    if (tid == 0) {
+      double total = 0;
+      for (int w = 0; w < kThreads / 32; ++w) total += s_sum[w];
+      stat[static_cast<int64_t>(row) * n_slices + slice] = {total, m, 0};
+    }
+    int n = s_n;
+    overflow |= n > kSliceFound;
+    if (n > kSliceFound / 2 || slice + 1 == slice1) {      // cut the list down to the best
+      n = min(n, kSliceFound);
+      for (int i = tid; i < n; i += kThreads) {
+        int rank = 0;
+        for (int j = 0; j < n; ++j) rank += ahead(s_x[j], s_w[j], s_x[i], s_w[i]);
+        if (rank < keep) s_keep[rank] = {s_x[i], s_w[i]};
+      }
+      __syncthreads();
+      const int kept = min(n, keep);
+      if (tid < kept) {
+        s_x[tid] = s_keep[tid].x;
+        s_w[tid] = s_keep[tid].w;
+      }
+      if (tid == 0) s_n = kept;
+      if (kept == keep) bound = fmaxf(bound, s_keep[keep - 1].x);
+      __syncthreads();
+    }
+  }
+  Best* mine = best + (static_cast<int64_t>(row) * gridDim.x + blockIdx.x) * keep;
+  if (!overflow) {
+    for (int i = tid; i < keep; i += kThreads) mine[i] = i < s_n ? Best{s_x[i], s_w[i]} : Best{-INFINITY, 0};
     return;
   }
-  // Hundreds of equal logits at the bound: one after the other.
+  // Hundreds of equal logits at the bound: one after the other, from memory.
   float last = INFINITY;
   int last_w = -1;
   for (int place = 0; place < keep; ++place) {
     float bx = -INFINITY;
     int bw = 0x7fffffff;
-#pragma unroll
-    for (int i = 0; i < E; ++i)
-      if (x[i] > -INFINITY && ahead(last, last_w, x[i], word(i)) && ahead(x[i], word(i), bx, bw)) {
-        bx = x[i];
-        bw = word(i);
+    for (int w = slice0 * kThreads * E + tid; w < min(slice1 * kThreads * E, vocab); w += kThreads) {
+      const float y = usable(as_float<T>(x0[w]));
+      if (y > -INFINITY && ahead(last, last_w, y, w) && ahead(y, w, bx, bw)) {
+        bx = y;
+        bw = w;
       }
+    }
     block_best(bx, bw, s_x, s_w);
     if (tid == 0) mine[place] = {bx, bw};
     last = bx;
@@ -196,7 +216,7 @@ __global__ void __launch_bounds__(kThreads) beam_slice_kernel(const T* __restric
 // One CTA per request joins the slices of its beams.
 constexpr int kFound = 1024;
 __global__ void __launch_bounds__(kThreads) beam_join_kernel(int n_beams, int vocab, const float* __restrict__ cum, const uint8_t* __restrict__ finished,
-                                                             int end_token, int keep, int n_slices, const SliceStat* __restrict__ stat,
+                                                             int end_token, int keep, int n_slices, int n_splits, const SliceStat* __restrict__ stat,
                                                              const Best* __restrict__ best, float* __restrict__ score, int32_t* __restrict__ parent,
                                                              int32_t* __restrict__ token) {
   // of every beam: what its logits are measured from, log of the sum; a beam without candidates: +infinity, 0;
@@ -207,7 +227,7 @@ __global__ void __launch_bounds__(kThreads) beam_join_kernel(int n_beams, int vo
   pdl_trigger();
   pdl_wait();
   const int req = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int row0 = req * n_beams, per_beam = n_slices * keep;
+  const int row0 = req * n_beams, per_beam = n_splits * keep;
   for (int b = warp; b < n_beams; b += kThreads / 32) {
     const float c = __ldg(cum + row0 + b);
     const bool done = finished && finished[row0 + b];
@@ -309,27 +329,36 @@ __global__ void __launch_bounds__(kThreads) beam_join_kernel(int n_beams, int vo
   }
 }
 
-// Words per thread: 32 where that still gives every SM two CTAs, else 8, for the latency of small calls.
-int words_per_thread(int64_t rows, int vocab) { return rows * ((vocab + 32 * kThreads - 1) / (32 * kThreads)) >= 2 * 148 ? 32 : 8; }
-int slices_of(int64_t rows, int vocab) {
-  const int w = words_per_thread(rows, vocab) * kThreads;
-  return (vocab + w - 1) / w;
+// How a row is cut.  Words per thread: 32 where that still gives every SM two CTAs, else 8, for the latency of small
+// calls.  A row's slices are dealt to as many CTAs as give every SM about three.
+struct Cut {
+  int words, n_slices, n_splits, per_split;
+};
+Cut cut_of(int64_t rows, int vocab) {
+  constexpr int kSms = 148;
+  Cut c;
+  c.words = rows * ((vocab + 32 * kThreads - 1) / (32 * kThreads)) >= 2 * kSms ? 32 : 8;
+  c.n_slices = (vocab + c.words * kThreads - 1) / (c.words * kThreads);
+  const int64_t splits = std::min<int64_t>(c.n_slices, std::max<int64_t>(1, (3 * kSms + rows - 1) / rows));
+  c.per_split = static_cast<int>((c.n_slices + splits - 1) / splits);
+  c.n_splits = (c.n_slices + c.per_split - 1) / c.per_split;
+  return c;
 }
 
 template <typename T>
 cudaError_t launch_select(const void* logits, int n_req, int n_beams, int vocab, int64_t row_stride, const float* cum, const uint8_t* finished,
                           int end_token, int keep, float* score, int32_t* parent, int32_t* token, void* workspace, cudaStream_t st) {
   const int64_t rows = static_cast<int64_t>(n_req) * n_beams;
-  const int n_slices = slices_of(rows, vocab), e = words_per_thread(rows, vocab);
+  const Cut cut = cut_of(rows, vocab);
   SliceStat* stat = static_cast<SliceStat*>(workspace);
-  Best* best = reinterpret_cast<Best*>(stat + rows * n_slices);
+  Best* best = reinterpret_cast<Best*>(stat + rows * cut.n_slices);
   const bool wide = (reinterpret_cast<uintptr_t>(logits) & 15) == 0 && row_stride % (16 / static_cast<int64_t>(sizeof(T))) == 0;
-  const dim3 grid(static_cast<unsigned>(n_slices), static_cast<unsigned>(rows));
-  auto kernel = e == 32 ? beam_slice_kernel<T, 32> : beam_slice_kernel<T, 8>;
+  const dim3 grid(static_cast<unsigned>(cut.n_splits), static_cast<unsigned>(rows));
+  auto kernel = cut.words == 32 ? beam_slice_kernel<T, 32> : beam_slice_kernel<T, 8>;
   cudaError_t err = launch_pdl(kernel, grid, dim3(kThreads), 0, st, static_cast<const T*>(logits), row_stride, vocab, cum, finished, keep,
-                               n_slices, wide, stat, best);
+                               cut.n_slices, cut.per_split, wide, stat, best);
   if (err != cudaSuccess) return err;
-  return launch_pdl(beam_join_kernel, dim3(static_cast<unsigned>(n_req)), dim3(kThreads), 0, st, n_beams, vocab, cum, finished, end_token, keep, n_slices,
+  return launch_pdl(beam_join_kernel, dim3(static_cast<unsigned>(n_req)), dim3(kThreads), 0, st, n_beams, vocab, cum, finished, end_token, keep, cut.n_slices, cut.n_splits,
                     static_cast<const SliceStat*>(stat), static_cast<const Best*>(best), score, parent, token);
 }
 
@@ -351,8 +380,8 @@ extern "C" {
 int64_t prima_beam_select_workspace(int n_req, int n_beams, int vocab, int keep) {
   if (select_error(n_req, n_beams, vocab, keep)) return PRIMA_ERR_ARG;
   const int64_t rows = static_cast<int64_t>(n_req) * n_beams;
-  const int64_t n = rows * slices_of(rows, vocab);
-  return n * static_cast<int64_t>(sizeof(SliceStat)) + n * keep * static_cast<int64_t>(sizeof(Best));
+  const Cut cut = cut_of(rows, vocab);
+  return rows * (cut.n_slices * static_cast<int64_t>(sizeof(SliceStat)) + cut.n_splits * static_cast<int64_t>(keep) * static_cast<int64_t>(sizeof(Best)));
 }
 
 int prima_beam_select(const void* logits, int dtype, int n_req, int n_beams, int vocab, int64_t row_stride, const float* cum,

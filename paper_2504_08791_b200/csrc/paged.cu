@@ -15,109 +15,105 @@ namespace {
 // ---- rotation and append ----------------------------------------------------------------------------------------
 // Row t at position p: pair i of every query and key head is turned by 2 pi frac(p f_i), f_i = theta^(-2i/D) / (2 pi).
 // p f_i is formed in 64 bits (error p f_i 2^-53 turns, below 2^-24 up to p = 2^29), its whole turns are dropped and the
-// rest goes to sincospif in 32 bits.  A CTA takes kTok rows: the sines of a row are computed once, by head_dim / 2
-// threads, and serve all of its heads.  An item is 16 elements of a head: 8 pairs (two 16-byte pieces of the result).
-template <typename T, typename In, int D, int kTok>
+// rest goes to sincospif in 32 bits.
+// kWarps warps take one row, each looks its place up by itself.  A lane owns the same 8 pairs (16 elements) of every
+// head that it turns, so their sines stay in registers; a warp takes 32 / (D/16) heads at a time.  With the index
+// arithmetic of a division per item instead, the kernel was bound by instructions (prompts of 10,500 tokens: 65 us).
+template <typename T, typename In, int D, int kWarps>
 __global__ void __launch_bounds__(256) append_kernel(PoolView pool, BatchView b, int layer, const In* __restrict__ q, const In* __restrict__ k,
                                                      const In* __restrict__ v, int n_q_heads, int64_t q_stride, int64_t k_stride,
                                                      int64_t v_stride, bool wide, const double* __restrict__ freq, int mode,
                                                      T* __restrict__ q_out) {
-  constexpr int kPairs = D / 2, kItems = D / 16;
-  __shared__ float2 s_cs[kTok][kPairs];
-  __shared__ int64_t s_row[kTok];        // row of the arrays, -1: not to be written; -2: padding
-  const int t0 = blockIdx.x * kTok;
+  constexpr int kPairs = D / 2, kItems = D / 16, kHeads = 32 / kItems, kStep = kWarps * kHeads;
+  __shared__ __align__(16) float2 s_cs[8][kPairs];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int G = pool.n_kv_heads, heads = n_q_heads + 2 * G;
-  const int per_tok = heads * kItems;
-  const int n_items = min(kTok, b.n_tok - t0) * per_tok;
-
-  auto load = [&](int item, float (&x)[2][8]) {
-    const int tk = item / per_tok, r = item - tk * per_tok;
-    const int head = r / kItems, c = r % kItems;
-    const int64_t t = t0 + tk;
-    const In* src = head < n_q_heads ? (q ? q + t * q_stride + head * D : nullptr)
-                                     : head < n_q_heads + G ? k + t * k_stride + (head - n_q_heads) * D : v + t * v_stride + (head - n_q_heads - G) * D;
-    if (!src) return;
-    if (mode == 0 && head < n_q_heads + G) {
-      load8(src + 8 * c, wide, x[0]);
-      load8(src + kPairs + 8 * c, wide, x[1]);
-    } else {
-      load8(src + 16 * c, wide, x[0]);
-      load8(src + 16 * c + 8, wide, x[1]);
-    }
+  const int t = (static_cast<int>(blockIdx.x) * 8 + warp) / kWarps;
+  const int c = lane % kItems, G = pool.n_kv_heads, heads = n_q_heads + 2 * G;
+  if (t >= b.n_tok) return;
+  pdl_trigger();
+  pdl_wait();
+  const In* const q_row = q ? q + t * q_stride : nullptr;
+  const In* const k_row = k + t * k_stride;
+  const In* const v_row = v + t * v_stride;
+  struct Item { Raw8<In> lo, hi; };
+  // Turned heads: elements 8 c .. and D/2 + 8 c .. (mode 0); otherwise 16 c .. 16 c + 15
+  auto load = [&](int h, Item& x) {
+    if (h >= heads || (h < n_q_heads && !q)) return;
+    const In* src = h < n_q_heads ? q_row + h * D : h < n_q_heads + G ? k_row + (h - n_q_heads) * D : v_row + (h - n_q_heads - G) * D;
+    const bool halves = mode == 0 && h < n_q_heads + G;
+    load8(src + (halves ? 8 * c : 16 * c), wide, x.lo);
+    load8(src + (halves ? kPairs + 8 * c : 16 * c + 8), wide, x.hi);
   };
-  float x[2][8];
-  int item = threadIdx.x;
-  if (item < n_items) load(item, x);      // in flight while the places are looked up
+  int h = (warp % kWarps) * kHeads + lane / kItems;
+  Item x[2];
+  load(h, x[0]);                       // in flight while the place is looked up
+  load(h + kStep, x[1]);
 
-  for (int tk = warp; tk < kTok; tk += 8) {
-    const int t = t0 + tk;
-    int64_t row = -2;
-    int p = 0;
-    if (t < b.n_tok) {
-      if (b.pos) p = __ldg(b.pos + t);
-      const int s = seq_of_row(b, t, lane);
-      if (s < b.n_seq) {
-        const int first = __ldg(b.row_begin + s), ctx = __ldg(b.ctx_len + s);
-        if (t < first || first < 0 || ctx < 0) {
-          if (lane == 0) raise(pool.status, kBadRows);
-          row = -2;
-        } else {
-          const int64_t slot = static_cast<int64_t>(ctx) + (t - first);
-          if (lane == 0) row = slot_row(pool, b.table + s * b.table_stride, b.table_stride, layer, slot);
-          if (!b.pos) p = static_cast<int>(slot);
-        }
-      }
-    }
-    row = __shfl_sync(0xffffffffu, row, 0);
-    if (lane == 0) s_row[tk] = row;
-    for (int i = lane; i < kPairs; i += 32) {
-      const double turns = p * __ldg(freq + i);
-      float sn, cs;
-      sincospif(static_cast<float>(2.0 * (turns - rint(turns))), &sn, &cs);
-      s_cs[tk][i] = make_float2(cs, sn);
-    }
+  int p = b.pos ? __ldg(b.pos + t) : 0;
+  const int s = seq_of_row(b, t, lane);
+  if (s >= b.n_seq) return;            // padding
+  const int first = __ldg(b.row_begin + s), ctx = __ldg(b.ctx_len + s);
+  if (t < first || first < 0 || ctx < 0) {
+    if (lane == 0) raise(pool.status, kBadRows);
+    return;
   }
-  __syncthreads();
+  const int64_t slot = static_cast<int64_t>(ctx) + (t - first);
+  if (!b.pos) p = static_cast<int>(slot);
+  int64_t row = lane == 0 ? slot_row(pool, b.table + s * b.table_stride, b.table_stride, layer, slot) : 0;
+  for (int i = lane; i < kPairs; i += 32) {
+    const double turns = p * __ldg(freq + i);
+    float sn, cs;
+    sincospif(static_cast<float>(2.0 * (turns - rint(turns))), &sn, &cs);
+    s_cs[warp][i] = make_float2(cs, sn);
+  }
+  row = __shfl_sync(0xffffffffu, row, 0);      // -1: a bad page or slot, nothing is appended
+  __syncwarp();
+  float2 cs[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) cs[i] = s_cs[warp][8 * c + i];
 
-  auto finish = [&](int item, const float (&x)[2][8]) {
-    const int tk = item / per_tok, r = item - tk * per_tok;
-    const int head = r / kItems, c = r % kItems;
-    const int64_t row = s_row[tk];
-    const bool is_q = head < n_q_heads, is_v = head >= n_q_heads + G;
-    if (row == -2 || (is_q ? !q : row < 0)) return;
-    T* dst = is_q ? q_out + (static_cast<int64_t>(t0 + tk) * n_q_heads + head) * D
-                  : static_cast<T*>(is_v ? pool.v : pool.k) + (row + (static_cast<int64_t>(head - n_q_heads - (is_v ? G : 0)) << pool.page_shift)) * D;
+  T* const q_dst = q_out + static_cast<int64_t>(t) * n_q_heads * D;
+  T* const k_dst = static_cast<T*>(pool.k) + row * D;
+  T* const v_dst = static_cast<T*>(pool.v) + row * D;
+  auto finish = [&](int h, const Item& raw) {
+    const bool is_q = h < n_q_heads, is_v = h >= n_q_heads + G;
+    if (h >= heads || (is_q ? !q : row < 0)) return;
+    T* dst = is_q ? q_dst + h * D : is_v ? v_dst + (static_cast<int64_t>(h - n_q_heads - G) << pool.page_shift) * D
+                                         : k_dst + (static_cast<int64_t>(h - n_q_heads) << pool.page_shift) * D;
+    float lo[8], hi[8], u[8], w[8];
+    to_f(raw.lo, lo);
+    to_f(raw.hi, hi);
     if (is_v) {
-      store8(dst + 16 * c, x[0]);
-      store8(dst + 16 * c + 8, x[1]);
+      store8(dst + 16 * c, lo);
+      store8(dst + 16 * c + 8, hi);
     } else if (mode == 0) {
-      float u[8], w[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float2 cs = s_cs[tk][8 * c + i];
-        u[i] = x[0][i] * cs.x - x[1][i] * cs.y;
-        w[i] = x[0][i] * cs.y + x[1][i] * cs.x;
+        u[i] = lo[i] * cs[i].x - hi[i] * cs[i].y;
+        w[i] = lo[i] * cs[i].y + hi[i] * cs[i].x;
       }
       store8(dst + 8 * c, u);
       store8(dst + kPairs + 8 * c, w);
     } else {
-      float u[2][8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float2 cs = s_cs[tk][8 * c + i];
-        const float a = x[i / 4][2 * (i % 4)], d = x[i / 4][2 * (i % 4) + 1];
-        u[i / 4][2 * (i % 4)] = a * cs.x - d * cs.y;
-        u[i / 4][2 * (i % 4) + 1] = a * cs.y + d * cs.x;
+      for (int i = 0; i < 4; ++i) {
+        u[2 * i] = lo[2 * i] * cs[i].x - lo[2 * i + 1] * cs[i].y;
+        u[2 * i + 1] = lo[2 * i] * cs[i].y + lo[2 * i + 1] * cs[i].x;
+        w[2 * i] = hi[2 * i] * cs[4 + i].x - hi[2 * i + 1] * cs[4 + i].y;
+        w[2 * i + 1] = hi[2 * i] * cs[4 + i].y + hi[2 * i + 1] * cs[4 + i].x;
       }
-      store8(dst + 16 * c, u[0]);
-      store8(dst + 16 * c + 8, u[1]);
+      store8(dst + 16 * c, u);
+      store8(dst + 16 * c + 8, w);
     }
   };
-  while (item < n_items) {
-    finish(item, x);
-    item += 256;
-    if (item < n_items) load(item, x);
+  for (; h < heads; h += 2 * kStep) {
+    Item y[2];
+    load(h + 2 * kStep, y[0]);
+    load(h + 3 * kStep, y[1]);
+    finish(h, x[0]);
+    finish(h + kStep, x[1]);
+    x[0] = y[0];
+    x[1] = y[1];
   }
 }
 
@@ -223,25 +219,24 @@ __global__ void __launch_bounds__(256) reorder_kernel(PoolView pool, int n_beams
   if (!copies || bad_page) return;
   const uint32_t n = static_cast<uint32_t>(tail) * (D / 8);      // 16-byte pieces of a head
   const int64_t total = static_cast<int64_t>(pool.n_layers) * 2 * G * n;
-  const int64_t step = static_cast<int64_t>(gridDim.y) * 256;
-  for (int64_t c = static_cast<int64_t>(blockIdx.y) * 256 + threadIdx.x; c < total; c += 4 * step) {
-    uint4 x[4];
-    uint4* to[4];
+  const int64_t step = static_cast<int64_t>(gridDim.y) * 256, page_step = (static_cast<int64_t>(G) << pool.page_shift) * (D / 8);
+  constexpr int kFlight = 8;
+  for (int64_t c = static_cast<int64_t>(blockIdx.y) * 256 + threadIdx.x; c < total; c += kFlight * step) {
+    uint4 x[kFlight];
+    int64_t at[kFlight];      // in 16-byte pieces, from the layer's first page, and 1 for values in the last bit
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kFlight; ++i) {
       const int64_t k = c + i * step;
+      at[i] = -1;
       if (k >= total) continue;
-      const int64_t w = div_small(k, n);
-      const uint32_t piece = static_cast<uint32_t>(k - w * n);
-      const int g = static_cast<int>(w % G), lv = static_cast<int>(w / G);
-      uint4* const base = static_cast<uint4*>(lv & 1 ? pool.v : pool.k) + piece;
-      const int64_t layer = static_cast<int64_t>(lv >> 1) * pool.n_pages;
-      x[i] = __ldcg(base + ((((layer + last) * G + g) << pool.page_shift)) * (D / 8));
-      to[i] = base + ((((layer + f) * G + g) << pool.page_shift)) * (D / 8);
+      const uint32_t w = static_cast<uint32_t>(div_small(k, n)), lv = w / static_cast<uint32_t>(G), g = w - lv * G;      // lv: layer and keys or values
+      at[i] = (((static_cast<int64_t>(lv >> 1) * pool.n_pages * G + g) << pool.page_shift)) * (D / 8) + (k - static_cast<int64_t>(w) * n);
+      at[i] = at[i] << 1 | (lv & 1);
+      x[i] = __ldcg(static_cast<const uint4*>(lv & 1 ? pool.v : pool.k) + (at[i] >> 1) + page_step * last);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (c + i * step < total) *to[i] = x[i];
+    for (int i = 0; i < kFlight; ++i)
+      if (at[i] >= 0) static_cast<uint4*>(at[i] & 1 ? pool.v : pool.k)[(at[i] >> 1) + page_step * f] = x[i];
   }
 }
 
@@ -252,14 +247,11 @@ cudaError_t launch_append(const prima_paged& pool, const BatchView& b, int layer
                           int64_t qs, int64_t ks, int64_t vs, void* q_out, cudaStream_t st) {
   const int64_t per16 = 16 / static_cast<int64_t>(sizeof(In));
   const bool wide = (!q || (aligned16(q) && qs % per16 == 0)) && aligned16(k) && aligned16(v) && ks % per16 == 0 && vs % per16 == 0;
-  // Few rows: one per CTA, for the shortest path; many: four, which share the look-up's latency.
-  const bool few = b.n_tok <= 4 * pool.sm_count;
-  auto kernel = few ? append_kernel<T, In, D, 1> : append_kernel<T, In, D, 4>;
-  const int tok = few ? 1 : 4;
-  kernel<<<(b.n_tok + tok - 1) / tok, 256, 0, st>>>(view_of(pool), b, layer, static_cast<const In*>(q), static_cast<const In*>(k),
-                                                    static_cast<const In*>(v), n_q_heads, qs, ks, vs, wide, pool.freq, pool.cfg.rope_mode,
-                                                    static_cast<T*>(q_out));
-  return cudaGetLastError();
+  // Few rows: a CTA's eight warps share one, for the shortest path; many: a warp each, which looks up least.
+  const bool few = b.n_tok <= 16 * pool.sm_count;
+  auto kernel = few ? append_kernel<T, In, D, 8> : append_kernel<T, In, D, 1>;
+  return launch_pdl(kernel, dim3(few ? b.n_tok : (b.n_tok + 7) / 8), dim3(256), 0, st, view_of(pool), b, layer, static_cast<const In*>(q), static_cast<const In*>(k),
+                    static_cast<const In*>(v), n_q_heads, qs, ks, vs, wide, static_cast<const double*>(pool.freq), pool.cfg.rope_mode, static_cast<T*>(q_out));
 }
 
 }  // namespace
@@ -410,7 +402,7 @@ int prima_paged_reorder(prima_paged* p, int n_req, int n_beams, int keep, const 
   if (!dev.ok) return call_fail(PRIMA_ERR_CUDA, "cudaSetDevice failed");
   // CTAs of a row: enough that a few rows which copy a whole page fill the GPU, as far as a page has pieces for them
   const int64_t pieces = static_cast<int64_t>(p->cfg.n_layers) * 2 * p->cfg.n_kv_heads * p->cfg.page_size * (p->cfg.head_dim / 8);
-  const int64_t share = std::max<int64_t>(1, (16 * static_cast<int64_t>(p->sm_count) + rows_out - 1) / rows_out);
+  const int64_t share = std::max<int64_t>(1, (6 * static_cast<int64_t>(p->sm_count) + rows_out - 1) / rows_out);
   const dim3 grid(static_cast<unsigned>(rows_out), static_cast<unsigned>(std::min<int64_t>({(pieces + 1023) / 1024, share, 65535})));
   auto kernel = p->cfg.head_dim == 128 ? reorder_kernel<128> : reorder_kernel<64>;
   const cudaError_t e = launch_pdl(kernel, grid, dim3(256), 0, static_cast<cudaStream_t>(stream), view_of(*p), n_beams, keep, table_in, table_stride, length_in, parent,

@@ -97,32 +97,32 @@ template <> struct Half2Of<__nv_bfloat16> {
   __device__ static float2 unpack(uint32_t u) { return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u)); }
 };
 
-// Eight consecutive elements as fp32.  `wide`: the address is 16-byte aligned.
+// Eight consecutive elements as they lie in memory (half the registers of fp32 where they wait for something), and
+// as fp32.  `wide`: the address is 16-byte aligned.
+template <typename T> struct Raw8 { uint32_t w[8 * sizeof(T) / 4]; };
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, bool wide, float (&x)[8]) {
+__device__ __forceinline__ void load8(const T* p, bool wide, Raw8<T>& x) {
   if (wide) {
-    const uint4 u = __ldg(reinterpret_cast<const uint4*>(p));
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 f = Half2Of<T>::unpack(w[i]);
-      x[2 * i] = f.x;
-      x[2 * i + 1] = f.y;
-    }
+    for (int i = 0; i < static_cast<int>(sizeof(x.w) / 16); ++i) *(reinterpret_cast<uint4*>(x.w) + i) = __ldg(reinterpret_cast<const uint4*>(p) + i);
   } else {
+    T* e = reinterpret_cast<T*>(x.w);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = Half2Of<T>::to_f(p[i]);
+    for (int i = 0; i < 8; ++i) e[i] = p[i];
   }
 }
-template <>
-__device__ __forceinline__ void load8<float>(const float* p, bool wide, float (&x)[8]) {
-  if (wide) {
-    const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-  } else {
+template <typename T>
+__device__ __forceinline__ void to_f(const Raw8<T>& x, float (&y)[8]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = p[i];
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) {
+      y[2 * i] = __uint_as_float(x.w[2 * i]);
+      y[2 * i + 1] = __uint_as_float(x.w[2 * i + 1]);
+    } else {
+      const float2 f = Half2Of<T>::unpack(x.w[i]);
+      y[2 * i] = f.x;
+      y[2 * i + 1] = f.y;
+    }
   }
 }
 template <typename T>
