@@ -113,15 +113,15 @@ __global__ void __launch_bounds__(kThreads) beam_slice_kernel(const T* __restric
   // element i of a thread is word slice * kThreads * E + (i / kVec) * kThreads * kVec + tid * kVec + i % kVec
   auto word = [&](int slice, int i) { return slice * kThreads * E + (i / kVec) * kThreads * kVec + tid * kVec + i % kVec; };
   auto load = [&](int slice, uint4 (&u)[E / kVec]) {
-    if (wide && (slice + 1) * kThreads * E <= vocab) {
+    const T none = static_cast<T>(-INFINITY);
 #pragma unroll
-      for (int i = 0; i < E / kVec; ++i) u[i] = __ldcs(reinterpret_cast<const uint4*>(x0 + word(slice, i * kVec)));
-    } else {
-      const T none = static_cast<T>(-INFINITY);
+    for (int i = 0; i < E / kVec; ++i) {
+      const int w = word(slice, i * kVec);
+      if (wide && w + kVec <= vocab) {
+        u[i] = __ldcs(reinterpret_cast<const uint4*>(x0 + w));
+      } else {
 #pragma unroll
-      for (int i = 0; i < E; ++i) {
-        const int w = word(slice, i);
-        reinterpret_cast<T*>(u)[i] = w < vocab ? x0[w] : none;
+        for (int j = 0; j < kVec; ++j) reinterpret_cast<T*>(u + i)[j] = w + j < vocab ? x0[w + j] : none;
       }
     }
   };
@@ -136,18 +136,19 @@ __global__ void __launch_bounds__(kThreads) beam_slice_kernel(const T* __restric
 #pragma unroll
     for (int i = 0; i < E; ++i) x[i] = usable(as_float<T>(reinterpret_cast<const T*>(next)[i]));
     if (slice + 1 < slice1) load(slice + 1, next);
-    float top = x[0];
+    float tops[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
-    for (int i = 1; i < E; ++i) top = fmaxf(top, x[i]);
+    for (int i = 4; i < E; ++i) tops[i & 3] = fmaxf(tops[i & 3], x[i]);
+    const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
     bound = fmaxf(bound, block_bound(top, keep, s_group, &s_bound));
     float m = s_group[0];
     for (int w = 1; w < n_groups; ++w) m = fmaxf(m, s_group[w]);
     // Sum of exp(x - m): the difference first (exact for the large terms), then one ex2 (relative error 2^-22).
     const float from = m == -INFINITY ? 0.f : m;
-    float part[2] = {0.f, 0.f};
+    float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < E; ++i) part[i & 1] += ex2((x[i] - from) * 1.4426950408889634f);
-    double sum = static_cast<double>(part[0]) + part[1];
+    for (int i = 0; i < E; ++i) part[i & 3] += ex2((x[i] - from) * 1.4426950408889634f);
+    double sum = (static_cast<double>(part[0]) + part[1]) + (static_cast<double>(part[2]) + part[3]);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if (lane == 0) s_sum[warp] = sum;
@@ -170,7 +171,9 @@ __global__ void __launch_bounds__(kThreads) beam_slice_kernel(const T* __restric
     }
     int n = s_n;
     overflow |= n > kSliceFound;
-    if (n > kSliceFound / 2 || slice + 1 == slice1) {      // cut the list down to the best
+    // Cut the list down to the best: at the end, and early on, since the best of the first slice is the better bound for
+    // the next ones.
+    if (n > 2 * keep || slice + 1 == slice1) {
       n = min(n, kSliceFound);
       for (int i = tid; i < n; i += kThreads) {
         int rank = 0;

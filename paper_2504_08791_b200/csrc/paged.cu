@@ -217,26 +217,23 @@ __global__ void __launch_bounds__(256) reorder_kernel(PoolView pool, int n_beams
       table_out[r * stride + i] = bad_len || i >= pages ? -1 : copies && i == pages - 1 ? f : __ldg(table_in + src * stride + i);
   }
   if (!copies || bad_page) return;
-  const uint32_t n = static_cast<uint32_t>(tail) * (D / 8);      // 16-byte pieces of a head
-  const int64_t total = static_cast<int64_t>(pool.n_layers) * 2 * G * n;
-  const int64_t step = static_cast<int64_t>(gridDim.y) * 256, page_step = (static_cast<int64_t>(G) << pool.page_shift) * (D / 8);
-  constexpr int kFlight = 8;
-  for (int64_t c = static_cast<int64_t>(blockIdx.y) * 256 + threadIdx.x; c < total; c += kFlight * step) {
-    uint4 x[kFlight];
-    int64_t at[kFlight];      // in 16-byte pieces, from the layer's first page, and 1 for values in the last bit
+  // A warp takes one head of keys or values of one layer at a time (index arithmetic per 16 bytes would bound the kernel).
+  const int n = tail * (D / 8);      // 16-byte pieces
+  const int64_t page_step = (static_cast<int64_t>(G) << pool.page_shift) * (D / 8);
+  for (int w = blockIdx.y * 8 + (threadIdx.x >> 5); w < pool.n_layers * 2 * G; w += gridDim.y * 8) {
+    const int lv = w / G, g = w - lv * G;
+    uint4* const base = static_cast<uint4*>(lv & 1 ? pool.v : pool.k) + (lv >> 1) * page_step * pool.n_pages + ((static_cast<int64_t>(g) << pool.page_shift) * (D / 8));
+    const uint4* const from = base + page_step * last;
+    uint4* const to = base + page_step * f;
+    for (int i = lane; i < n; i += 128) {
+      uint4 x[4];
 #pragma unroll
-    for (int i = 0; i < kFlight; ++i) {
-      const int64_t k = c + i * step;
-      at[i] = -1;
-      if (k >= total) continue;
-      const uint32_t w = static_cast<uint32_t>(div_small(k, n)), lv = w / static_cast<uint32_t>(G), g = w - lv * G;      // lv: layer and keys or values
-      at[i] = (((static_cast<int64_t>(lv >> 1) * pool.n_pages * G + g) << pool.page_shift)) * (D / 8) + (k - static_cast<int64_t>(w) * n);
-      at[i] = at[i] << 1 | (lv & 1);
-      x[i] = __ldcg(static_cast<const uint4*>(lv & 1 ? pool.v : pool.k) + (at[i] >> 1) + page_step * last);
+      for (int j = 0; j < 4; ++j)
+        if (i + 32 * j < n) x[j] = __ldcg(from + i + 32 * j);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (i + 32 * j < n) to[i + 32 * j] = x[j];
     }
-#pragma unroll
-    for (int i = 0; i < kFlight; ++i)
-      if (at[i] >= 0) static_cast<uint4*>(at[i] & 1 ? pool.v : pool.k)[(at[i] >> 1) + page_step * f] = x[i];
   }
 }
 
@@ -400,10 +397,11 @@ int prima_paged_reorder(prima_paged* p, int n_req, int n_beams, int keep, const 
     return call_fail(PRIMA_ERR_ARG, "prima_paged_reorder: the new tables overlap the old ones");
   CallDevice dev(p->cfg.device);
   if (!dev.ok) return call_fail(PRIMA_ERR_CUDA, "cudaSetDevice failed");
-  // CTAs of a row: enough that a few rows which copy a whole page fill the GPU, as far as a page has pieces for them
-  const int64_t pieces = static_cast<int64_t>(p->cfg.n_layers) * 2 * p->cfg.n_kv_heads * p->cfg.page_size * (p->cfg.head_dim / 8);
-  const int64_t share = std::max<int64_t>(1, (6 * static_cast<int64_t>(p->sm_count) + rows_out - 1) / rows_out);
-  const dim3 grid(static_cast<unsigned>(rows_out), static_cast<unsigned>(std::min<int64_t>({(pieces + 1023) / 1024, share, 65535})));
+  // CTAs of a row: enough that a few rows which copy a page fill the GPU, as far as there are heads for their warps
+  const int64_t heads = static_cast<int64_t>(p->cfg.n_layers) * 2 * p->cfg.n_kv_heads;
+  if (heads > 2147483647) return call_fail(PRIMA_ERR_ARG, "prima_paged_reorder: layers * KV heads too large");
+  const int64_t share = std::max<int64_t>(1, (16 * static_cast<int64_t>(p->sm_count) + rows_out - 1) / rows_out);
+  const dim3 grid(static_cast<unsigned>(rows_out), static_cast<unsigned>(std::min<int64_t>({(heads + 7) / 8, share, 65535})));
   auto kernel = p->cfg.head_dim == 128 ? reorder_kernel<128> : reorder_kernel<64>;
   const cudaError_t e = launch_pdl(kernel, grid, dim3(256), 0, static_cast<cudaStream_t>(stream), view_of(*p), n_beams, keep, table_in, table_stride, length_in, parent,
                                    fresh, table_out, length_out);
