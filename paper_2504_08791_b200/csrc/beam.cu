@@ -2,8 +2,8 @@
 //
 //   score(b, w) = cum[b] + (x[b][w] - m_b - log sum_v exp(x[b][v] - m_b)),   m_b = max_v x[b][v]
 //
-// The logits are read once.  A CTA holds slices of one row in registers, one after the other, and leaves each slice's
-// maximum and sum of exponentials and its `keep` best logits; a second kernel joins the slices of a request.  Within a row the order of
+// The logits are read once.  A CTA holds slices of one row in registers, one after the other, and leaves their
+// maximum, their sum of exponentials and their `keep` best logits; a second kernel joins the slices of a request.  Within a row the order of
 // the scores is the order of the logits, so the slices can be cut down before the row's sum is known.
 // Which of two near candidates of DIFFERENT beams is ahead depends on the last bits of the two sums, so everything
 // behind a thread's own partial sum is in 64 bits.  Every sum has a fixed order that follows the index in the row, not
@@ -91,15 +91,29 @@ __device__ __forceinline__ void block_best(V& x, int& i, V* s_x, int* s_i) {
 
 constexpr int kSliceFound = 512;
 
-// E logits per thread: a slice of kThreads * E words of one row.  A CTA takes `per_split` consecutive slices of a row,
-// the next one's logits in flight while it works on the current one, and leaves a maximum and a sum for each of them and
-// the `keep` best logits of them all.
+// Two 32-bit operations in one instruction.
+__device__ __forceinline__ float2 add2(float2 x, float2 y) {
+  unsigned long long d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*reinterpret_cast<unsigned long long*>(&x)), "l"(*reinterpret_cast<unsigned long long*>(&y)));
+  return *reinterpret_cast<float2*>(&d);
+}
+__device__ __forceinline__ float2 mul2(float2 x, float2 y) {
+  unsigned long long d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*reinterpret_cast<unsigned long long*>(&x)), "l"(*reinterpret_cast<unsigned long long*>(&y)));
+  return *reinterpret_cast<float2*>(&d);
+}
+
+// E logits per thread: a slice of kThreads * E words of one row.  A CTA takes `per_split` consecutive slices of a row
+// and leaves a maximum, a sum and the `keep` best logits.  Every thread sums its own words against its own running
+// maximum.  After the first slice, whose best make the bound that later logits have to reach, the warps go on without
+// barriers, the next logits in flight.  Bound by instructions: about 200 per warp and 32 words each.
 template <typename T, int E>
-__global__ void __launch_bounds__(kThreads) beam_slice_kernel(const T* __restrict__ logits, int64_t row_stride, int vocab, const float* __restrict__ cum,
+__global__ void __launch_bounds__(kThreads, 3) beam_slice_kernel(const T* __restrict__ logits, int64_t row_stride, int vocab, const float* __restrict__ cum,
                                                               const uint8_t* __restrict__ finished, int keep, int n_slices, int per_split, bool wide,
                                                               SliceStat* __restrict__ stat, Best* __restrict__ best) {
   constexpr int kVec = 16 / sizeof(T);
-  __shared__ float s_group[64], s_bound, s_x[kSliceFound];
+  constexpr float kLog2e = 1.4426950408889634f;
+  __shared__ float s_group[64], s_bound, s_x[kSliceFound], s_top[kThreads / 32];
   __shared__ int s_w[kSliceFound], s_n;
   __shared__ double s_sum[kThreads / 32];
   __shared__ Best s_keep[kMaxKeep];
@@ -113,75 +127,91 @@ __global__ void __launch_bounds__(kThreads) beam_slice_kernel(const T* __restric
   // element i of a thread is word slice * kThreads * E + (i / kVec) * kThreads * kVec + tid * kVec + i % kVec
   auto word = [&](int slice, int i) { return slice * kThreads * E + (i / kVec) * kThreads * kVec + tid * kVec + i % kVec; };
   auto load = [&](int slice, uint4 (&u)[E / kVec]) {
+    const T* const p = x0 + word(slice, 0);
+    if (wide && (slice + 1) * kThreads * E <= vocab) {
+#pragma unroll
+      for (int i = 0; i < E / kVec; ++i) u[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i * kThreads);
+      return;
+    }
     const T none = static_cast<T>(-INFINITY);
 #pragma unroll
-    for (int i = 0; i < E / kVec; ++i) {
-      const int w = word(slice, i * kVec);
-      if (wide && w + kVec <= vocab) {
-        u[i] = __ldcs(reinterpret_cast<const uint4*>(x0 + w));
-      } else {
+    for (int i = 0; i < E / kVec; ++i)
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) reinterpret_cast<T*>(u + i)[j] = w + j < vocab ? x0[w + j] : none;
-      }
-    }
+      for (int j = 0; j < kVec; ++j) reinterpret_cast<T*>(u + i)[j] = word(slice, i * kVec + j) < vocab ? p[i * kThreads * kVec + j] : none;
   };
   uint4 next[E / kVec];
   load(slice0, next);
   if (tid == 0) s_n = 0;
+  const int period = max(1, kSliceFound / (4 * keep));      // slices between two cuts of the list
   float bound = -INFINITY;
+  float ref = -INFINITY;       // the sum is of exp(x - ref)
+  double sum = 0;
   bool overflow = false;
-  const int n_groups = keep <= 8 ? 8 : keep <= 16 ? 16 : keep <= 32 ? 32 : 64;
   for (int slice = slice0; slice < slice1; ++slice) {
     float x[E];
 #pragma unroll
-    for (int i = 0; i < E; ++i) x[i] = usable(as_float<T>(reinterpret_cast<const T*>(next)[i]));
+    for (int i = 0; i < E; ++i) x[i] = as_float<T>(reinterpret_cast<const T*>(next)[i]);
     if (slice + 1 < slice1) load(slice + 1, next);
-    float tops[4] = {x[0], x[1], x[2], x[3]};
+    constexpr int kChunk = E / 4;
+    float tops[4];             // of four stretches of the thread's words; a NaN loses every comparison
 #pragma unroll
-    for (int i = 4; i < E; ++i) tops[i & 3] = fmaxf(tops[i & 3], x[i]);
-    const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-    bound = fmaxf(bound, block_bound(top, keep, s_group, &s_bound));
-    float m = s_group[0];
-    for (int w = 1; w < n_groups; ++w) m = fmaxf(m, s_group[w]);
-    // Sum of exp(x - m): the difference first (exact for the large terms), then one ex2 (relative error 2^-22).
-    const float from = m == -INFINITY ? 0.f : m;
-    float part[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < 4; ++j) {
+      tops[j] = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < E; ++i) part[i & 3] += ex2((x[i] - from) * 1.4426950408889634f);
-    double sum = (static_cast<double>(part[0]) + part[1]) + (static_cast<double>(part[2]) + part[3]);
+      for (int i = 0; i < kChunk; ++i) tops[j] = fmaxf(tops[j], x[j * kChunk + i]);
+    }
+    const float top = fminf(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), FLT_MAX);
+    if (slice == slice0) bound = block_bound(top, keep, s_group, &s_bound);
+    if (top > -INFINITY) {
+      if (top > ref) {
+        sum *= ex2((ref - top) * kLog2e);
+        ref = top;
+      }
+      // The difference first (exact for the large terms), then one ex2 (relative error 2^-22).
+      float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (lane == 0) s_sum[warp] = sum;
-    if (top >= bound && top > -INFINITY) {
-#pragma unroll
-      for (int i = 0; i < E; ++i)
-        if (x[i] >= bound && x[i] > -INFINITY) {
-          const int at = atomicAdd(&s_n, 1);
-          if (at < kSliceFound) {
-            s_x[at] = x[i];
-            s_w[at] = word(slice, i);
-          }
+      for (int i = 0; i < E; i += 2) {
+        const float2 d = mul2(add2(make_float2(x[i], x[i + 1]), make_float2(-ref, -ref)), make_float2(kLog2e, kLog2e));
+        part[i >> 1 & 1] = add2(part[i >> 1 & 1], make_float2(ex2(d.x), ex2(d.y)));
+      }
+      float total = (part[0].x + part[0].y) + (part[1].x + part[1].y);
+      if (!(total <= FLT_MAX)) {      // a NaN or an infinity among them: once more, word by word
+        total = 0.f;
+#pragma unroll 1
+        for (int i = 0; i < E; ++i) {
+          const int w = word(slice, i);
+          if (w < vocab) total += ex2((usable(as_float<T>(x0[w])) - ref) * kLog2e);
         }
+      }
+      sum += total;
+      if (top >= bound) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (tops[j] >= bound) {
+#pragma unroll
+            for (int i = j * kChunk; i < (j + 1) * kChunk; ++i)
+              if (x[i] >= bound && x[i] > -INFINITY) {
+                const int at = atomicAdd(&s_n, 1);
+                if (at < kSliceFound) {
+                  s_x[at] = fminf(x[i], FLT_MAX);
+                  s_w[at] = word(slice, i);
+                }
+              }
+          }
+      }
     }
-    __syncthreads();
-    if (tid == 0) {
-      double total = 0;
-      for (int w = 0; w < kThreads / 32; ++w) total += s_sum[w];
-      stat[static_cast<int64_t>(row) * n_slices + slice] = {total, m, 0};
-    }
-    int n = s_n;
-    overflow |= n > kSliceFound;
-    // Cut the list down to the best: at the end, and early on, since the best of the first slice is the better bound for
-    // the next ones.
-    if (n > 2 * keep || slice + 1 == slice1) {
-      n = min(n, kSliceFound);
+    // Cut the list down to the best: after the first slice, at the end, and in between before it can run over (as it
+    // still may where the logits rise from slice to slice).
+    if ((slice - slice0) % period == 0 || slice + 1 == slice1) {
+      __syncthreads();
+      overflow |= s_n > kSliceFound;
+      const int n = min(s_n, kSliceFound), kept = min(n, keep);
       for (int i = tid; i < n; i += kThreads) {
         int rank = 0;
         for (int j = 0; j < n; ++j) rank += ahead(s_x[j], s_w[j], s_x[i], s_w[i]);
         if (rank < keep) s_keep[rank] = {s_x[i], s_w[i]};
       }
       __syncthreads();
-      const int kept = min(n, keep);
       if (tid < kept) {
         s_x[tid] = s_keep[tid].x;
         s_w[tid] = s_keep[tid].w;
@@ -191,7 +221,25 @@ __global__ void __launch_bounds__(kThreads) beam_slice_kernel(const T* __restric
       __syncthreads();
     }
   }
-  Best* mine = best + (static_cast<int64_t>(row) * gridDim.x + blockIdx.x) * keep;
+  // The CTA's maximum and sum
+  float top = ref;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  if (lane == 0) s_top[warp] = top;
+  __syncthreads();
+  for (int w = 0; w < kThreads / 32; ++w) top = fmaxf(top, s_top[w]);
+  sum *= ref == -INFINITY ? 0.f : ex2((ref - top) * kLog2e);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (lane == 0) s_sum[warp] = sum;
+  __syncthreads();
+  const int64_t out = static_cast<int64_t>(row) * gridDim.x + blockIdx.x;
+  if (tid == 0) {
+    double total = 0;
+    for (int w = 0; w < kThreads / 32; ++w) total += s_sum[w];
+    stat[out] = {total, top, 0};
+  }
+  Best* mine = best + out * keep;
   if (!overflow) {
     for (int i = tid; i < keep; i += kThreads) mine[i] = i < s_n ? Best{s_x[i], s_w[i]} : Best{-INFINITY, 0};
     return;
@@ -219,7 +267,7 @@ __global__ void __launch_bounds__(kThreads) beam_slice_kernel(const T* __restric
 // One CTA per request joins the slices of its beams.
 constexpr int kFound = 1024;
 __global__ void __launch_bounds__(kThreads) beam_join_kernel(int n_beams, int vocab, const float* __restrict__ cum, const uint8_t* __restrict__ finished,
-                                                             int end_token, int keep, int n_slices, int n_splits, const SliceStat* __restrict__ stat,
+                                                             int end_token, int keep, int n_splits, const SliceStat* __restrict__ stat,
                                                              const Best* __restrict__ best, float* __restrict__ score, int32_t* __restrict__ parent,
                                                              int32_t* __restrict__ token) {
   // of every beam: what its logits are measured from, log of the sum; a beam without candidates: +infinity, 0;
@@ -238,13 +286,13 @@ __global__ void __launch_bounds__(kThreads) beam_join_kernel(int n_beams, int vo
     if (done && c > -INFINITY) {
       top = NAN;
     } else if (c > -INFINITY) {
-      const SliceStat* st = stat + static_cast<int64_t>(row0 + b) * n_slices;
+      const SliceStat* st = stat + static_cast<int64_t>(row0 + b) * n_splits;
       float m = -INFINITY;
-      for (int i = lane; i < n_slices; i += 32) m = fmaxf(m, __ldcg(&st[i].top));
+      for (int i = lane; i < n_splits; i += 32) m = fmaxf(m, __ldcg(&st[i].top));
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
       sum = 0;
-      for (int i = lane; i < n_slices; i += 32) {
+      for (int i = lane; i < n_splits; i += 32) {
         const float t = __ldcg(&st[i].top);
         if (t > -INFINITY) sum += __ldcg(&st[i].sum) * exp(static_cast<double>(t) - static_cast<double>(m));
       }
@@ -333,7 +381,7 @@ __global__ void __launch_bounds__(kThreads) beam_join_kernel(int n_beams, int vo
 }
 
 // How a row is cut.  Words per thread: 32 where that still gives every SM two CTAs, else 8, for the latency of small
-// calls.  A row's slices are dealt to as many CTAs as give every SM about three.
+// calls.  A row's slices are dealt to as many CTAs as fit the GPU at a time.
 struct Cut {
   int words, n_slices, n_splits, per_split;
 };
@@ -342,7 +390,7 @@ Cut cut_of(int64_t rows, int vocab) {
   Cut c;
   c.words = rows * ((vocab + 32 * kThreads - 1) / (32 * kThreads)) >= 2 * kSms ? 32 : 8;
   c.n_slices = (vocab + c.words * kThreads - 1) / (c.words * kThreads);
-  const int64_t splits = std::min<int64_t>(c.n_slices, std::max<int64_t>(1, (3 * kSms + rows - 1) / rows));
+  const int64_t splits = std::min<int64_t>(c.n_slices, std::max<int64_t>(1, 3 * kSms / rows));
   c.per_split = static_cast<int>((c.n_slices + splits - 1) / splits);
   c.n_splits = (c.n_slices + c.per_split - 1) / c.per_split;
   return c;
@@ -354,14 +402,14 @@ cudaError_t launch_select(const void* logits, int n_req, int n_beams, int vocab,
   const int64_t rows = static_cast<int64_t>(n_req) * n_beams;
   const Cut cut = cut_of(rows, vocab);
   SliceStat* stat = static_cast<SliceStat*>(workspace);
-  Best* best = reinterpret_cast<Best*>(stat + rows * cut.n_slices);
+  Best* best = reinterpret_cast<Best*>(stat + rows * cut.n_splits);
   const bool wide = (reinterpret_cast<uintptr_t>(logits) & 15) == 0 && row_stride % (16 / static_cast<int64_t>(sizeof(T))) == 0;
   const dim3 grid(static_cast<unsigned>(cut.n_splits), static_cast<unsigned>(rows));
   auto kernel = cut.words == 32 ? beam_slice_kernel<T, 32> : beam_slice_kernel<T, 8>;
   cudaError_t err = launch_pdl(kernel, grid, dim3(kThreads), 0, st, static_cast<const T*>(logits), row_stride, vocab, cum, finished, keep,
                                cut.n_slices, cut.per_split, wide, stat, best);
   if (err != cudaSuccess) return err;
-  return launch_pdl(beam_join_kernel, dim3(static_cast<unsigned>(n_req)), dim3(kThreads), 0, st, n_beams, vocab, cum, finished, end_token, keep, cut.n_slices, cut.n_splits,
+  return launch_pdl(beam_join_kernel, dim3(static_cast<unsigned>(n_req)), dim3(kThreads), 0, st, n_beams, vocab, cum, finished, end_token, keep, cut.n_splits,
                     static_cast<const SliceStat*>(stat), static_cast<const Best*>(best), score, parent, token);
 }
 
@@ -384,7 +432,7 @@ int64_t prima_beam_select_workspace(int n_req, int n_beams, int vocab, int keep)
   if (select_error(n_req, n_beams, vocab, keep)) return PRIMA_ERR_ARG;
   const int64_t rows = static_cast<int64_t>(n_req) * n_beams;
   const Cut cut = cut_of(rows, vocab);
-  return rows * (cut.n_slices * static_cast<int64_t>(sizeof(SliceStat)) + cut.n_splits * static_cast<int64_t>(keep) * static_cast<int64_t>(sizeof(Best)));
+  return rows * cut.n_splits * (static_cast<int64_t>(sizeof(SliceStat)) + static_cast<int64_t>(keep) * static_cast<int64_t>(sizeof(Best)));
 }
 
 int prima_beam_select(const void* logits, int dtype, int n_req, int n_beams, int vocab, int64_t row_stride, const float* cum,
