@@ -419,6 +419,16 @@ int64_t prima_tree_attention_workspace(const prima_paged* pool, int n_seq, int n
 int prima_tree_attention(prima_paged* pool, int layer, const prima_paged_batch* batch, const void* q, int n_q_heads, float scale,
                          void* out, int out_dtype, float* lse, void* workspace, int64_t workspace_bytes, void* stream);
 
+/* One step of a context's layers [layer_begin, layer_end) over a paged cache: as prima_forward_window, for the
+ * batch->n_tok (1..max_n_tok) rows of hidden_in / hidden_out, each of its own sequence, at its own position, seeing what
+ * the batch says (a chain, a tree of drafted tokens, one token of each of several requests or beams).  The pool takes the
+ * place of the context's own caches; layer l of the model is layer l of the pool, whose KV heads, head size, rotation and
+ * device must be the model's.  The calls run on the context's stream, and the context keeps one workspace for them.  Rows
+ * behind the last sequence are computed with whatever their hidden rows hold and appended nowhere; they do not touch the
+ * others.  Errors as prima_forward_window. */
+int prima_forward_window_paged(prima_ctx* ctx, prima_paged* pool, int layer_begin, int layer_end, const float* hidden_in, float* hidden_out,
+                               const prima_paged_batch* batch);
+
 /* After a verification: the rows path[s][0 .. path_len[s]-1] of sequence s (indices into its rows of the step,
  * strictly ascending) were accepted; their keys and values move to the slots ctx_len[s], ctx_len[s] + 1, ... in all
  * layers.  path: dev int32 [n_seq][path_stride]; path_len: dev int32 [n_seq], 0..path_stride.  batch: row_begin,

@@ -36,7 +36,7 @@ EXPORTS = [
     "prima_forward_window_seqs", "prima_kv_load_seq", "prima_kv_read_seq", "prima_ctx_set_option", "prima_stream_stats",
     "prima_fmt_block_weights", "prima_fmt_block_bytes", "prima_dequant_fmt", "prima_gemv_fmt", "prima_fmt_last_error",
     "prima_paged_create", "prima_paged_destroy", "prima_paged_sync", "prima_paged_append", "prima_paged_accept", "prima_paged_reorder",
-    "prima_tree_attention", "prima_tree_attention_workspace", "prima_beam_select", "prima_beam_select_workspace",
+    "prima_tree_attention", "prima_tree_attention_workspace", "prima_beam_select", "prima_beam_select_workspace", "prima_forward_window_paged",
 ]
 
 
@@ -119,6 +119,7 @@ def lib():
         L.prima_tree_attention_workspace.argtypes = [vp, i32, i32, i32]
         L.prima_tree_attention_workspace.restype = i64
         L.prima_beam_select.argtypes = [vp, i32, i32, i32, i32, i64, vp, vp, i32, i32, vp, vp, vp, vp, i64, vp]
+        L.prima_forward_window_paged.argtypes = [vp, vp, i32, i32, vp, vp, vp]
         L.prima_beam_select_workspace.argtypes = [i32, i32, i32, i32]
         L.prima_beam_select_workspace.restype = i64
         for name in EXPORTS:
@@ -278,6 +279,13 @@ class Context:
             raise ValueError("one position per sequence")
         _check(lib().prima_forward_window_seqs(self._h, layer_begin, layer_end, _dev_ptr(hidden_in), _dev_ptr(hidden_out),
                                                _host_ptr(seqs), _host_ptr(positions), seqs.size), self._h)
+
+    def forward_window_paged(self, pool: "PagedCache", layer_begin: int, layer_end: int, hidden_in, hidden_out, batch: "PagedBatch"):
+        """prima_forward_window_paged: the rows of a batch of sequences over a paged cache."""
+        for name, t in (("hidden_in", hidden_in), ("hidden_out", hidden_out)):
+            if t.dim() != 2 or t.shape[0] < batch.n_tok or t.shape[1] != self.cfg["hidden"]:
+                raise ValueError(f"{name}: expected [{batch.n_tok}, {self.cfg['hidden']}], got {tuple(t.shape)}")
+        _check(lib().prima_forward_window_paged(self._h, pool._h, layer_begin, layer_end, _dev_ptr(hidden_in), _dev_ptr(hidden_out), pool._batch(batch)), self._h)
 
     def sync(self):
         _check(lib().prima_sync(self._h), self._h)

@@ -75,6 +75,12 @@ struct prima_ctx {
   float* h_a = nullptr;      // residual stream entering a layer / leaving its feed-forward block
   float* h_b = nullptr;      // residual stream after the attention block
   float* obuf = nullptr;
+  // steps over a paged cache, allocated at the first one: queries, keys and values of a layer, rotated queries, and the
+  // attention's workspace
+  float* paged_qkv = nullptr;
+  void* paged_q = nullptr;
+  void* paged_ws = nullptr;
+  int64_t paged_ws_bytes = 0;
   SumSq ssq_attn, ssq_ffn, ssq_out;
   float2* rope_tab = nullptr;
   AttnScratch attn{};
@@ -683,8 +689,13 @@ int prima_load_q4k_weights(prima_ctx* c, int layer, int tensor_id, const void* d
 // One step over layers [layer_begin, layer_end).  seq == nullptr: n_tok tokens of sequence 0 at positions
 // pos0 .. pos0 + n_tok - 1, causal among themselves.  Otherwise token t belongs to sequence seq[t] and sits at
 // position pos[t] of that sequence's own cache: the products run over all tokens together, attention per token.
+// Instead of the two: rows of sequences of a paged cache (batch).
+struct PagedStep {
+  prima_paged* pool;
+  const prima_paged_batch* batch;
+};
 static int forward_window_launch(prima_ctx* c, int layer_begin, int layer_end, const float* hidden_in, float* hidden_out, int pos0,
-                                 int n_tok, const int32_t* seq, const int32_t* pos);
+                                 int n_tok, const int32_t* seq, const int32_t* pos, const PagedStep* paged);
 
 // Attention reads little and leaves HBM idle, and so does the O product (its matrix is short: the kernel is bound by
 // its start-up, not by the stream).  In a step of one token their CTAs ask for the head of the gate/up matrix, the
@@ -712,7 +723,7 @@ static L2Ahead o_ahead(const prima_ctx* c, const Layer& L, int n_tok) {
 }
 
 static int forward_window_impl(prima_ctx* c, int layer_begin, int layer_end, const float* hidden_in, float* hidden_out, int pos0,
-                               int n_tok, const int32_t* seq, const int32_t* pos) {
+                               int n_tok, const int32_t* seq, const int32_t* pos, const PagedStep* paged = nullptr) {
   DeviceGuard guard(c->cfg.device);
   // Everything that can fail without a launch comes first: the caches of the window's (layer, sequence)
   // pairs are allocated here, so that an allocation failure means that nothing was queued.
@@ -724,16 +735,56 @@ static int forward_window_impl(prima_ctx* c, int layer_begin, int layer_end, con
         if (rc != PRIMA_OK) return rc;
       }
   }
+  if (paged) {
+    const int64_t n = c->cfg.max_n_tok, H = c->cfg.n_q_heads, G = c->cfg.n_kv_heads;
+    int rc = PRIMA_OK;
+    // zeroed: rows of a step that belong to no sequence are not written by the attention, but go through the products
+    if (!c->paged_qkv) rc = dev_alloc(c, &c->paged_qkv, static_cast<size_t>(n * (H + 2 * G) * kHeadDim), true);
+    if (rc == PRIMA_OK && !c->paged_q) {
+      uint16_t* q = nullptr;
+      rc = dev_alloc(c, &q, static_cast<size_t>(n * H * kHeadDim), true);
+      c->paged_q = q;
+    }
+    const int64_t need = prima_tree_attention_workspace(paged->pool, static_cast<int>(n), static_cast<int>(n), static_cast<int>(H));
+    if (rc == PRIMA_OK && c->paged_ws_bytes < need) {
+      uint8_t* ws = nullptr;
+      rc = dev_alloc(c, &ws, static_cast<size_t>(need));
+      c->paged_ws = ws;
+      if (rc == PRIMA_OK) c->paged_ws_bytes = need;
+      if (rc == PRIMA_OK) cudaMemsetAsync(c->obuf, 0, static_cast<size_t>(n * H * kHeadDim) * sizeof(float), c->stream);
+    }
+    if (rc != PRIMA_OK) return rc;
+  }
   const int64_t before = c->launches;
-  const int rc = forward_window_launch(c, layer_begin, layer_end, hidden_in, hidden_out, pos0, n_tok, seq, pos);
+  const int rc = forward_window_launch(c, layer_begin, layer_end, hidden_in, hidden_out, pos0, n_tok, seq, pos, paged);
   // A launch that failed after earlier kernels of the window were queued leaves accumulators that are
   // not zero: clear them behind the queued work, so that the next call starts from the usual state.
   if (rc != PRIMA_OK && c->launches != before) queue_reset(c);
   return rc;
 }
 
+// Attention of one layer over a paged cache: the QKV product is finished (deferred RMSNorm factor) into fp32 rows, which
+// the public append rotates and stores, and the public attention leaves its fp32 output where the O product reads it.
+static int paged_attention(prima_ctx* c, const Layer& L, int layer, int n_tok, const PagedStep& paged) {
+  const prima_model_config& g = c->cfg;
+  const int H = g.n_q_heads, G = g.n_kv_heads;
+  const int64_t width = static_cast<int64_t>(H + 2 * G) * kHeadDim;
+  LAUNCH(c, launch_finish_acc(c->acc_qkv, L.qkv.mpad(), width, n_tok, c->paged_qkv, c->ssq_attn, c->stream), "finish_acc(qkv)");
+  const float* k = c->paged_qkv + static_cast<int64_t>(H) * kHeadDim;
+  if (injected_failure(c)) return fail(c, PRIMA_ERR_CUDA, "paged append: injected launch failure");
+  int rc = prima_paged_append(paged.pool, layer, paged.batch, c->paged_qkv, k, k + static_cast<int64_t>(G) * kHeadDim, PRIMA_DT_F32, H, width, width, width, c->paged_q,
+                              c->stream);
+  if (rc != PRIMA_OK) return fail(c, rc, g_tls_error);
+  c->launches += 1;
+  if (injected_failure(c)) return fail(c, PRIMA_ERR_CUDA, "tree attention: injected launch failure");
+  rc = prima_tree_attention(paged.pool, layer, paged.batch, c->paged_q, H, 0.08838834764831845f, c->obuf, PRIMA_DT_F32, nullptr, c->paged_ws, c->paged_ws_bytes, c->stream);
+  if (rc != PRIMA_OK) return fail(c, rc, g_tls_error);
+  c->launches += 2;
+  return PRIMA_OK;
+}
+
 static int forward_window_launch(prima_ctx* c, int layer_begin, int layer_end, const float* hidden_in, float* hidden_out, int pos0,
-                                 int n_tok, const int32_t* seq, const int32_t* pos) {
+                                 int n_tok, const int32_t* seq, const int32_t* pos, const PagedStep* paged) {
   const prima_model_config& g = c->cfg;
   cudaStream_t st = c->stream;
   const int64_t e_ = g.hidden;
@@ -746,7 +797,9 @@ static int forward_window_launch(prima_ctx* c, int layer_begin, int layer_end, c
     }
     return PRIMA_OK;
   }
-  if (!seq) {
+  if (paged) {
+    // the rotation is part of the append
+  } else if (!seq) {
     LAUNCH(c, launch_rope_table(c->rope_tab, pos0, n_tok, g.rope_theta, st), "rope_table");
   } else {
     for (int t = 0; t < n_tok; ++t)
@@ -764,7 +817,7 @@ static int forward_window_launch(prima_ctx* c, int layer_begin, int layer_end, c
   if (seq)
     for (int t = 0; t < n_tok; ++t) first_pos = t == 0 ? pos[t] : std::min(first_pos, pos[t]);
   const int stable_below = std::min(first_pos, c->unsynced_min_pos);
-  c->unsynced_min_pos = stable_below;      // this call appends at first_pos and above
+  if (!paged) c->unsynced_min_pos = stable_below;      // this call appends at first_pos and above
   for (int l = layer_begin; l < layer_end; ++l) {
     Layer& L = c->layers[l];
     int slot = -1;
@@ -781,7 +834,10 @@ static int forward_window_launch(prima_ctx* c, int layer_begin, int layer_end, c
     c->ssq_attn = in.ssq_out;
     c->ssq_attn.eps = g.rms_eps;
     c->attn.ahead = attn_ahead(c, L, n_tok);
-    if (!seq) {
+    if (paged) {
+      const int rc = paged_attention(c, L, l, n_tok, *paged);
+      if (rc != PRIMA_OK) return rc;
+    } else if (!seq) {
       c->attn.stamp = next_stamp(c, PRIMA_PROF_ATTENTION, static_cast<int64_t>(2) * G * kHeadDim * 2 * (pos0 + n_tok), 2);
       LAUNCH_P(c, PRIMA_PROF_ATTENTION, static_cast<int64_t>(2) * G * kHeadDim * 2 * (pos0 + n_tok),
                launch_attention(c->acc_qkv, L.qkv.mpad(), c->ssq_attn, c->rope_tab, g.rope_mode, L.k, L.v, g.kv_capacity, H, G, pos0, stable_below,
@@ -870,6 +926,20 @@ int prima_forward_window_seqs(prima_ctx* c, int layer_begin, int layer_end, cons
       if (seq[u] == seq[t]) return fail(c, PRIMA_ERR_ARG, "a sequence may appear once per step");
   }
   return forward_window_impl(c, layer_begin, layer_end, hidden_in, hidden_out, 0, n_seq, seq, pos);
+}
+
+int prima_forward_window_paged(prima_ctx* c, prima_paged* pool, int layer_begin, int layer_end, const float* hidden_in, float* hidden_out,
+                               const prima_paged_batch* batch) {
+  if (!c) return fail(nullptr, PRIMA_ERR_ARG, "prima_forward_window_paged: null context");
+  if (check_batch(pool, batch, "prima_forward_window_paged") != PRIMA_OK) return fail(c, PRIMA_ERR_ARG, g_tls_error);
+  int rc = window_args_ok(c, "prima_forward_window_paged", layer_begin, layer_end, hidden_in, hidden_out, batch->n_tok);
+  if (rc != PRIMA_OK) return rc;
+  const prima_paged_config& p = pool->cfg;
+  if (p.n_kv_heads != c->cfg.n_kv_heads || p.head_dim != c->cfg.head_dim || p.n_layers < c->cfg.n_layers || p.device != c->cfg.device ||
+      p.rope_theta != c->cfg.rope_theta || p.rope_mode != c->cfg.rope_mode)
+    return fail(c, PRIMA_ERR_ARG, "prima_forward_window_paged: the pool's shape, rotation or device is not the model's");
+  const PagedStep step{pool, batch};
+  return forward_window_impl(c, layer_begin, layer_end, hidden_in, hidden_out, 0, batch->n_tok, nullptr, nullptr, &step);
 }
 
 int prima_logits(prima_ctx* c, const float* hidden, int n_tok, float* logits) {
