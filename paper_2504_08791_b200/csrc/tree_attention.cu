@@ -3,17 +3,18 @@
 //   out[t][h] = sum_j p_j v_j / sum_j p_j,   p_j = exp(scale q.k_j - m),   j over the context and the rows that t sees
 //
 // A step has few rows per sequence and a long cache, so the cache should be read once, at HBM speed: all query heads
-// that share a KV head and all rows of the sequence make one tile of up to 256 rows (two accumulators of 128), which
-// is what one pass over the cache can serve before the tensor core and the exponentials, about 2500 cycles per 128
-// positions, become slower than the SM's share of HBM, about 2850.
+// that share a KV head and all rows of the sequence make one tile of up to 256 rows (two accumulators of 128), which one
+// pass over the cache serves.
 //
 // One persistent CTA per SM takes an equal share of all units (paged_index.h): 128 positions of one KV head for one
 // tile of rows.  Warp 8 copies keys and values page by page into a ring in shared memory (one tiled copy per page and
 // 64 columns), warp 9 issues the products, S = Q K^T into tensor memory, O += P V with P read from tensor memory, and
-// two groups of four warps turn S into P, one thread per row: no shuffles.  The groups are the two halves of a tile of
-// more than 128 rows, or, where a tile has fewer rows, take every other unit each and join at the end; one group's
-// exponentials run under the other's products.  A row's reference maximum moves only when a score exceeds it by a
-// factor of 2^8, so that O is hardly ever rescaled.  Sums and maxima are in 32 bits, P has the cache's type.
+// eight warps turn S into P, one thread per row and half of the 128 positions: no shuffles.  There are two buffers of
+// scores, used in turn by the units (or by the two accumulators of a tile of more than 128 rows), so that the scores of
+// the next sub-unit are computed under the exponentials of this one; P takes the place of its scores.
+// The two threads of a row share its reference maximum, which moves only when a score exceeds it by a factor of 2^8:
+// that is one vote of two warps per sub-unit, and O is hardly ever rescaled.  Sums and maxima are in 32 bits, P has the
+// cache's type.
 // A segment that is not a whole (sequence, KV head, tile) leaves its maximum, sum and output in the workspace, and
 // tree_merge_kernel joins the parts in ascending order: the same lengths give the same bits.
 #include <cuda.h>
@@ -31,11 +32,7 @@ namespace {
 
 constexpr int kTileRows = 256;         // of the tensor-memory kernel
 constexpr int kSoftmaxThreads = 256;
-constexpr int kThreads = kSoftmaxThreads + 128;      // two warpgroups of softmax; one of copies, products (two warps) and an idle warp
-// Registers: 384 threads may have 168 each; the softmax threads hold a row of 128 scores and take what the others do
-// not need.
-constexpr int kSoftmaxRegs = 208, kOtherRegs = 80;
-static_assert(kSoftmaxThreads * kSoftmaxRegs + (kThreads - kSoftmaxThreads) * kOtherRegs <= kThreads * 168, "the split may not exceed the launch");
+constexpr int kThreads = kSoftmaxThreads + 96;       // eight warps of softmax; copies, products, the plan
 constexpr int kSegments = 4;           // planned ahead
 constexpr int kSegmentCost = 3, kStreamSegmentCost = 1;      // of a segment besides its units, in units
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
@@ -54,20 +51,17 @@ struct Segment {
   int chunk0, n;                       // first unit and their number
   int kind;                            // 0: whole; 1: continues; 2: begins here and goes on
   long long limit;                     // positions that the tile may see
-  __device__ __forceinline__ bool halves() const { return rows > 128; }
-  // Units of the group that takes the first (rel = 0) and of the other, and the i-th of them
-  __device__ __forceinline__ int count(int rel) const { return halves() ? n : (n + 1 - rel) >> 1; }
-  __device__ __forceinline__ int unit(int rel, int i) const { return halves() ? i : 2 * i + rel; }
+  __device__ __forceinline__ int halves() const { return rows > 128 ? 2 : 1; }      // accumulators of 128 rows
 };
 
 struct Control {
-  unsigned long long full[12], empty[12], s_ready[2], p_ready[4], pv_done[2], q_ready, seg_done, drained[2];      // of each group; p_ready: of each half of its unit
+  unsigned long long full[12], empty[12], s_ready[2], p_ready[4], pv_done[2], q_ready, seg_done, drained;      // of each buffer; p_ready: and half
   unsigned long long seg_full[kSegments], seg_empty[kSegments];
   Segment seg[kSegments];              // n = 0: no more
   uint32_t tmem;
   int give_up;
   int bad[16];                         // of the last units: some page is none (the ring holds at most six)
-  float2 ml[128];                      // reference and sum of the rows of the group that hands its state over
+  float top[2][2][128];                // [buffer][half of the positions][row]: what the other half has to know
 };
 
 // What a CTA leaves about the segment that begins in it and goes on in later ones.
@@ -330,14 +324,20 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
   using Geo = Geometry<D>;
   constexpr int kSlots = Geo::kSlots;
   constexpr bool kBf16 = !__is_same(T, __half);
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  // The swizzled tiles need 1024-byte alignment, which the shared memory of a kernel without static variables has; there
+  // is no room to round up.
+  extern __shared__ __align__(1024) uint8_t smem[];
+  if (smem_u32(smem) & 1023) {
+    if (threadIdx.x == 0) raise(a.pool.status, kGaveUp);
+    return;
+  }
   uint8_t* s_q = smem;
   uint8_t* s_ring = smem + 2 * Geo::kQBytes;
   Control* ctl = reinterpret_cast<Control*>(s_ring + kSlots * Geo::kSlotBytes);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t bar_full = smem_u32(ctl->full), bar_empty = smem_u32(ctl->empty), bar_s = smem_u32(ctl->s_ready), bar_p = smem_u32(ctl->p_ready),
-                 bar_pv = smem_u32(ctl->pv_done), bar_seg = smem_u32(ctl->seg_full), bar_seg_empty = smem_u32(ctl->seg_empty), bar_q = smem_u32(&ctl->q_ready), bar_done = smem_u32(&ctl->seg_done), bar_drain = smem_u32(ctl->drained);
+                 bar_pv = smem_u32(ctl->pv_done), bar_seg = smem_u32(ctl->seg_full), bar_seg_empty = smem_u32(ctl->seg_empty), bar_q = smem_u32(&ctl->q_ready),
+                 bar_done = smem_u32(&ctl->seg_done), bar_drain = smem_u32(&ctl->drained);
   int* const give_up = &ctl->give_up;
   int* const status = a.pool.status;
 
@@ -345,7 +345,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
   if (tid == 0) {
     for (int i = 0; i < kSlots; ++i) {
       mbar_init(bar_full + 8 * i, 1);
-      mbar_init(bar_empty + 8 * i, 2);
+      mbar_init(bar_empty + 8 * i, 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(bar_s + 8 * i, 1);
@@ -355,12 +355,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
     }
     for (int i = 0; i < kSegments; ++i) {
       mbar_init(bar_seg + 8 * i, 1);
-      mbar_init(bar_seg_empty + 8 * i, 11);
+      mbar_init(bar_seg_empty + 8 * i, 10);
     }
     mbar_init(bar_q, 8);
     mbar_init(bar_done, 8);
     mbar_init(bar_drain, 1);
-    mbar_init(bar_drain + 8, 1);
     ctl->give_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     tma_prefetch_map(&k_map);
@@ -370,7 +369,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = ctl->tmem;
+  const uint32_t tmem = ctl->tmem;      // scores of buffer 0 and 1: columns 0, 128; outputs of half tile 0 and 1: 256, 256 + D
   pdl_wait();
 
   // Segment i of this CTA, or nothing when there are no more; the caller's warp gives it back with done_with(i).
@@ -389,166 +388,163 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
   RingPlace<kSlots> ring;       // the place that the segment begins with
   uint32_t copies_before = 0;   // copies: places used so far, up to kSlots (the ring is empty at first)
 
-  if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-    if (warp == 11) {
-      // ---- the plan ----
-      Cursor cursor(a, lane, blockIdx.x == 0);
-      Segment s;
-      s.kind = 0;
-      for (uint32_t i = 0;; ++i) {
-        const bool more = cursor.next(&s);
-        if (i >= kSegments) wait_segment(bar_seg_empty + 8 * (i % kSegments), (i / kSegments - 1) & 1);
-        if (lane == 0) {
-          ctl->seg[i % kSegments] = s;
-          if (!more) ctl->seg[i % kSegments].n = 0;
-          mbar_arrive(bar_seg + 8 * (i % kSegments));
-        }
-        __syncwarp();
-        if (!more) break;
+  if (warp == 10) {
+    // ---- the plan ----
+    Cursor cursor(a, lane, blockIdx.x == 0);
+    Segment s;
+    s.kind = 0;
+    for (uint32_t i = 0;; ++i) {
+      const bool more = cursor.next(&s);
+      if (i >= kSegments) wait_segment(bar_seg_empty + 8 * (i % kSegments), (i / kSegments - 1) & 1);
+      if (lane == 0) {
+        ctl->seg[i % kSegments] = s;
+        if (!more) ctl->seg[i % kSegments].n = 0;
+        mbar_arrive(bar_seg + 8 * (i % kSegments));
       }
-      if (lane == 0) cursor.write_note(s);
-    } else if (warp == 8) {
-        // ---- copies ----
-        const int shift = a.pool.page_shift;
-        const int box_rows = min(1 << shift, kTilePos);
-        const int boxes = kTilePos / box_rows;           // per 64 columns of a unit
-        const int box = lane % boxes, panel = lane / boxes;
-        const uint32_t dst = smem_u32(s_ring) + panel * Geo::kPanel + box * box_rows * 128;
-        bool started = false;
-        uint32_t n_read = 0;      // units
-        const Segment* seg;
-        for (uint32_t si = 0; (seg = segment(si)); ++si) {
-          const Segment s = *seg;
-          done_with(si);
-          const int32_t* table = a.b.table + s.seq * a.b.table_stride;
-          for (int t = 0; t < s.n; ++t) {
-            const long long pos = static_cast<long long>(s.chunk0 + t) * kTilePos + box * box_rows;
-            int64_t row = -1;
-            bool bad = false;
-            if (panel < D / 64 && pos < s.limit) {
-              const int64_t r = find_slot(a.pool, table, a.b.table_stride, a.layer, pos);
-              bad = r < 0;
-              if (bad) raise(status, static_cast<int>(-r));
-              else row = r + (static_cast<int64_t>(s.head) << shift);
-            }
-            const int n_copies = __popc(__ballot_sync(0xffffffffu, row >= 0));
-            const bool any_bad = __any_sync(0xffffffffu, bad);
-#pragma unroll
-            for (int is_v = 0; is_v < 2; ++is_v) {
-              bool ok = true;
-              if (copies_before >= kSlots) ok = wait_for(bar_empty + 8 * ring.slot, ring.phase ^ 1, give_up, status);
-              ok = __all_sync(0xffffffffu, ok);
-              if (ok) {
-                if (lane == 0) {
-                  if (!is_v) ctl->bad[n_read % 16] = any_bad;
-                  mbar_expect(bar_full + 8 * ring.slot, static_cast<uint32_t>(n_copies) * box_rows * 128);
-                }
-                __syncwarp();
-                if (row >= 0) tma_load_2d(dst + ring.slot * Geo::kSlotBytes, is_v ? &v_map : &k_map, panel * 64, static_cast<int>(row), bar_full + 8 * ring.slot);
-              }
-              // Queries before the rest of the first places: the first scores need them and one unit's keys, not what
-              // else fills the ring (measured: queries behind 160 KB of keys and values arrive 8 us late).
-              if (!started) wait_for(bar_q, 0, give_up, status);
-              started = true;
-              ring.step(1);
-              if (copies_before < kSlots) ++copies_before;
-            }
-            ++n_read;
-          }
+      __syncwarp();
+      if (!more) break;
+    }
+    if (lane == 0) cursor.write_note(s);
+  } else if (warp == 8) {
+    // ---- copies ----
+    const int shift = a.pool.page_shift;
+    const int box_rows = min(1 << shift, kTilePos);
+    const int boxes = kTilePos / box_rows;           // per 64 columns of a unit
+    const int box = lane % boxes, panel = lane / boxes;
+    const uint32_t dst = smem_u32(s_ring) + panel * Geo::kPanel + box * box_rows * 128;
+    bool started = false;
+    uint32_t n_read = 0;      // units
+    const Segment* seg;
+    for (uint32_t si = 0; (seg = segment(si)); ++si) {
+      const Segment s = *seg;
+      done_with(si);
+      const int32_t* table = a.b.table + s.seq * a.b.table_stride;
+      for (int t = 0; t < s.n; ++t) {
+        const long long pos = static_cast<long long>(s.chunk0 + t) * kTilePos + box * box_rows;
+        int64_t row = -1;
+        bool bad = false;
+        if (panel < D / 64 && pos < s.limit) {
+          const int64_t r = find_slot(a.pool, table, a.b.table_stride, a.layer, pos);
+          bad = r < 0;
+          if (bad) raise(status, static_cast<int>(-r));
+          else row = r + (static_cast<int64_t>(s.head) << shift);
         }
-    } else {
-        // ---- products: one warp per group, so that neither waits for the other's softmax ----
-        const uint32_t w = uniform(warp) - 9;
-        constexpr uint32_t kDescS = mma_f16_desc(kBf16, false, 128, kTilePos), kDescO = mma_f16_desc(kBf16, true, 128, D);
-        const uint32_t u_tmem = uniform(tmem), t_s = u_tmem + w * kTilePos, t_o = u_tmem + 256 + w * D;
-        const uint32_t ring_addr = uniform(smem_u32(s_ring)), q_addr = uniform(smem_u32(s_q));
-        const SmemOperand k_all = smem_operand(ring_addr, 16), v_all = smem_operand(ring_addr, Geo::kPanel);
-        uint32_t n_units = 0;
-        const Segment* seg;
-        for (uint32_t si = 0; (seg = segment(si)); ++si) {
-          const bool halves = uniform(seg->rows) > 128;
-          const uint32_t rel = halves ? w : (w ^ si) & 1;      // tiles of few rows: the groups take turns in beginning
-          const int n = uniform(seg->n), count = halves ? n : (n + 1 - rel) / 2;
-          const SmemOperand qq = smem_operand(q_addr + ((halves ? w : si & 1) ? Geo::kQBytes : 0), 16);
-          done_with(si);
-          bool ok = wait_for(bar_q, si & 1, give_up, status);
-          RingPlace<kSlots> pk = ring, pv;      // of the unit whose keys, whose values are due
-          if (!halves && rel) pk.step(2);
-          pv = pk;
-          pv.step(1);
-          auto scores = [&]() {                   // S = Q K^T
-            tc_fence_after();
-            if (__all_sync(0xffffffffu, ok) && elect_one()) {
-              const SmemOperand kk = k_all + pk.slot * Geo::kSlotBytes;
+        const int n_copies = __popc(__ballot_sync(0xffffffffu, row >= 0));
+        const bool any_bad = __any_sync(0xffffffffu, bad);
 #pragma unroll
-              for (int i = 0; i < D / 16; ++i) mma_ss(t_s, qq + (i / 4 * Geo::kPanel + i % 4 * 32), kk + (i / 4 * Geo::kPanel + i % 4 * 32), kDescS, i > 0);
-              tc_commit(bar_s + 8 * w);
-              tc_commit(bar_empty + 8 * pk.slot);
-              if (!halves) tc_commit(bar_empty + 8 * pk.slot);      // for the group that does not use it
+        for (int is_v = 0; is_v < 2; ++is_v) {
+          bool ok = true;
+          if (copies_before >= kSlots) ok = wait_for(bar_empty + 8 * ring.slot, ring.phase ^ 1, give_up, status);
+          ok = __all_sync(0xffffffffu, ok);
+          if (ok) {
+            if (lane == 0) {
+              if (!is_v) ctl->bad[n_read % 16] = any_bad;
+              mbar_expect(bar_full + 8 * ring.slot, static_cast<uint32_t>(n_copies) * box_rows * 128);
             }
             __syncwarp();
-            pk.step(halves ? 2 : 4);
-          };
-          if (count > 0) {
-            ok = wait_for(bar_full + 8 * pk.slot, pk.phase, give_up, status) && ok;
-            scores();
+            if (row >= 0) tma_load_2d(dst + ring.slot * Geo::kSlotBytes, is_v ? &v_map : &k_map, panel * 64, static_cast<int>(row), bar_full + 8 * ring.slot);
           }
-          for (int i = 0; i < count; ++i) {
-            // O += P V, in two halves of the positions: the first runs under the exponentials of the second.  The next
-            // keys are waited for before P is.
-            ok = wait_for(bar_full + 8 * pv.slot, pv.phase, give_up, status) && ok;
-            if (i + 1 < count) ok = wait_for(bar_full + 8 * pk.slot, pk.phase, give_up, status) && ok;
-            const SmemOperand vv = v_all + pv.slot * Geo::kSlotBytes;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              ok = wait_for(bar_p + 16 * w + 8 * h, n_units & 1, give_up, status) && ok;
-              tc_fence_after();
-              if (__all_sync(0xffffffffu, ok) && elect_one()) {
-#pragma unroll
-                for (int k = 4 * h; k < 4 * h + 4; ++k) mma_ts(t_o, t_s + k * 8, vv + k * (16 * 128), kDescO, i > 0 || k > 0);
-                if (h) {
-                  tc_commit(bar_pv + 8 * w);
-                  tc_commit(bar_empty + 8 * pv.slot);
-                  if (!halves) tc_commit(bar_empty + 8 * pv.slot);
-                }
-              }
-              __syncwarp();
-            }
-            pv.step(halves ? 2 : 4);
-            // P lies over S: the next scores are written behind the product that reads it (one warp's products run in order)
-            if (i + 1 < count) scores();
-            ++n_units;
-          }
-          ring.skip(2 * n);
+          // Queries before the rest of the first places: the first scores need them and one unit's keys, not what
+          // else fills the ring (measured: queries behind 160 KB of keys and values arrive 8 us late).
+          if (!started) wait_for(bar_q, 0, give_up, status);
+          started = true;
+          ring.step(1);
+          if (copies_before < kSlots) ++copies_before;
         }
+        ++n_read;
+      }
+    }
+  } else if (warp == 9) {
+    // ---- products ----
+    constexpr uint32_t kDescS = mma_f16_desc(kBf16, false, 128, kTilePos), kDescO = mma_f16_desc(kBf16, true, 128, D);
+    const uint32_t u_tmem = uniform(tmem);
+    const uint32_t ring_addr = uniform(smem_u32(s_ring)), q_addr = uniform(smem_u32(s_q));
+    const SmemOperand k_all = smem_operand(ring_addr, 16), v_all = smem_operand(ring_addr, Geo::kPanel);
+    uint32_t n_sub = 0;      // sub-units before this segment; sub-unit i uses buffer i % 2
+    const Segment* seg;
+    for (uint32_t si = 0; (seg = segment(si)); ++si) {
+      const int halves = uniform(seg->rows) > 128 ? 2 : 1, count = uniform(seg->n) * halves;
+      done_with(si);
+      bool ok = wait_for(bar_q, si & 1, give_up, status);
+      RingPlace<kSlots> pk = ring, pv = ring;      // of the unit whose keys, whose values are due
+      pv.step(1);
+      // Sub-unit i: unit i, or half i % 2 of the rows of unit i / 2
+      auto wait_keys = [&](int i) {
+        if (halves == 1 || !(i & 1)) ok = wait_for(bar_full + 8 * pk.slot, pk.phase, give_up, status) && ok;
+      };
+      auto scores = [&](int i) {                   // S = Q K^T
+        const uint32_t h = halves == 2 ? i & 1 : 0, buffer = (n_sub + i) & 1;
+        const bool last = halves == 1 || h == 1;
+        tc_fence_after();
+        if (__all_sync(0xffffffffu, ok) && elect_one()) {
+          const SmemOperand qq = smem_operand(q_addr + (halves == 2 ? h : si & 1) * Geo::kQBytes, 16), kk = k_all + pk.slot * Geo::kSlotBytes;
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k) mma_ss(u_tmem + buffer * kTilePos, qq + (k / 4 * Geo::kPanel + k % 4 * 32), kk + (k / 4 * Geo::kPanel + k % 4 * 32), kDescS, k > 0);
+          tc_commit(bar_s + 8 * buffer);
+          if (last) tc_commit(bar_empty + 8 * pk.slot);
+        }
+        __syncwarp();
+        if (last) pk.step(2);
+      };
+      for (int i = 0; i < min(count, 2); ++i) {
+        wait_keys(i);
+        scores(i);
+      }
+      for (int i = 0; i < count; ++i) {
+        const uint32_t h = halves == 2 ? i & 1 : 0, buffer = (n_sub + i) & 1, phase = (n_sub + i) >> 1 & 1;
+        const bool first = i < halves, last = halves == 1 || h == 1;
+        if (halves == 1 || !h) ok = wait_for(bar_full + 8 * pv.slot, pv.phase, give_up, status) && ok;
+        if (i + 2 < count) wait_keys(i + 2);
+        // O += P V, each half of the positions when its P is there; the first product of a segment overwrites O, which
+        // all warps must have read (their P says so)
+        const SmemOperand vv = v_all + pv.slot * Geo::kSlotBytes;
+        if (first) ok = wait_for(bar_p + 16 * buffer + 8, phase, give_up, status) && ok;
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          if (w == 0 || !first) ok = wait_for(bar_p + 16 * buffer + 8 * w, phase, give_up, status) && ok;
+          tc_fence_after();
+          if (__all_sync(0xffffffffu, ok) && elect_one()) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              mma_ts(u_tmem + 256 + h * D, u_tmem + buffer * kTilePos + 64 * w + 8 * k, vv + (4 * w + k) * (16 * 128), kDescO, !first || w > 0 || k > 0);
+            if (w) {
+              tc_commit(bar_pv + 8 * buffer);
+              if (last) tc_commit(bar_empty + 8 * pv.slot);
+            }
+          }
+          __syncwarp();
+        }
+        if (last) pv.step(2);
+        // P lies over S: the next scores are written behind the product that reads it (one warp's products run in order)
+        if (i + 2 < count) scores(i + 2);
+      }
+      n_sub += count;
+      ring.skip(2 * (count / halves));
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
-    // ---- softmax ----
+    // ---- softmax: warps 0..3 take positions 0..63 of a unit, warps 4..7 the others; one thread per row and half ----
     const int w = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
-    const uint32_t t_s = tmem + lanes + w * kTilePos, t_o = tmem + lanes + 256 + w * D, t_other = tmem + lanes + 256 + (w ^ 1) * D;
+    const uint32_t t_s = tmem + lanes + 64 * w, t_o = tmem + lanes + 256;
     const int group = a.shape.group;
-    uint32_t n_units = 0, unit_base = 0;    // taken by this group; of the segments before
+    uint32_t n_sub = 0, unit_base = 0;      // sub-units, units of the segments before
     bool loaded = false;                    // the queries of the segment are on their way already
-    bool handed = false;                    // the other group reads this group's output of an earlier segment
 
     // Row x of a segment's tile: its head's place in an array [n_tok][n_q_heads]
     auto place_of = [&](const Segment& g, int t0, int rem0, int x) {
       const int y = rem0 + x, t = small_div(y, a.group_inverse);
       return static_cast<int64_t>(g.first + t0 + t) * a.n_q_heads + g.head * group + (y - t * group);
     };
-    // Queries of a segment into its tile, in the background; both groups, all threads.
+    // Queries of a segment into its tile, in the background; all threads.
     auto load_queries = [&](const Segment& g, uint32_t tile) {
       constexpr int kPieces = D / 8;
       const int t0 = g.row0 / group, rem0 = g.row0 - t0 * group;
-      const int rows = g.halves() ? kTileRows : 128;
+      const int rows = g.halves() * 128;
 #pragma unroll 4
       for (int idx = tid; idx < rows * kPieces; idx += kSoftmaxThreads) {
         const int row = idx / kPieces, piece = idx % kPieces, in_acc = row & 127;
         const bool there = row < g.rows;
-        copy16(smem_u32(s_q) + ((g.halves() ? row >> 7 : tile) ? Geo::kQBytes : 0) + piece / 8 * Geo::kPanel + in_acc * 128 + ((piece % 8) ^ (in_acc & 7)) * 16,
+        copy16(smem_u32(s_q) + ((rows > 128 ? row >> 7 : tile) ? Geo::kQBytes : 0) + piece / 8 * Geo::kPanel + in_acc * 128 + ((piece % 8) ^ (in_acc & 7)) * 16,
                static_cast<const T*>(a.q) + place_of(g, t0, rem0, there ? row : 0) * D + piece * 8, there);
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
@@ -556,10 +552,16 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
     auto queries_ready = [&]() {
       asm volatile("cp.async.wait_all;" ::: "memory");
       fence_async_smem();
-      tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar_q);
     };
+    // The two warps of the same rows
+    auto pair_any = [&](bool x) {
+      uint32_t y = x;
+      asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 q, %1, 0;\nbar.red.or.pred p, %2, 64, q;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(y) : "r"(y), "r"(1 + quarter) : "memory");
+      return y != 0;
+    };
+    auto pair_sync = [&]() { asm volatile("bar.sync %0, 64;" ::"r"(1 + quarter) : "memory"); };
 
     const Segment* seg;
     for (uint32_t si = 0; (seg = segment(si)); ++si) {
@@ -579,227 +581,186 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
       // A tile of at most 128 rows leaves room for the next one's queries, where the segment before had its own.
       bool next_loads = false;
       auto load_next = [&]() {
-        if (s.halves()) return;
+        if (s.halves() == 2) return;
         const Segment* next = segment(si + 1);
-        if (!next || next->halves()) return;
+        if (!next || next->halves() == 2) return;
         wait_before();
         load_queries(*next, (si + 1) & 1);
         next_loads = true;
       };
       const int t0 = s.row0 / group, rem0 = s.row0 - t0 * group;
-      const int in_tile = (s.halves() ? w * 128 : 0) + r;            // this thread's row
-      const bool live = (s.halves() ? w * 128 : 0) + quarter * 32 < s.rows;
-      const int node = in_tile < s.rows ? t0 + small_div(rem0 + in_tile, a.group_inverse) : 0;
-      const int rel = s.halves() ? w : (w ^ si) & 1;      // tiles of few rows: the groups take turns in beginning
-      const int count = s.count(rel), other = s.count(rel ^ 1);
+      const int halves = s.halves(), count = s.n * halves;
       RingPlace<kSlots> pk = ring;            // of the unit's keys
-      if (!s.halves() && rel) pk.step(2);
       ring.skip(2 * s.n);
-      float m = -INFINITY;
-      float2 sum = make_float2(0.f, 0.f);
-      // Turns: of the two warps that share an exponential unit, one per group, one uses it at a time, at its full rate,
-      // while the other's products run.  Left alone the two fall into step and wait for the same things.
-      auto begin_turn = [&](int i) {
-        if (rel == 1 || i > 0) asm volatile("bar.sync %0, 64;" ::"r"(3 + 2 * quarter + w) : "memory");
-      };
-      auto end_turn = [&](int i) {
-        if (i + rel < other) asm volatile("bar.arrive %0, 64;" ::"r"(3 + 2 * quarter + (w ^ 1)) : "memory");
-      };
-      // The other group may still be reading this group's output of an earlier segment.
-      auto output_free = [&]() {
-        if (handed) asm volatile("bar.sync %0, %1;" ::"r"(13 + w), "n"(kSoftmaxThreads) : "memory");
-        handed = false;
-      };
-      if (count == 0) {      // this segment's queries are complete before the next one's are reported
-        wait_for(bar_q, si & 1, give_up, status);
-        load_next();
-      }
-      for (int i = 0; i < count; ++i, ++n_units) {
-        const long long pos0 = static_cast<long long>(s.chunk0 + s.unit(rel, i)) * kTilePos;
+      // of the accumulator whose turn it is, and of the other one
+      float m = -INFINITY, m_other = -INFINITY;
+      float2 sum = make_float2(0.f, 0.f), sum_other = make_float2(0.f, 0.f);
+#pragma unroll 1
+      for (int i = 0; i < count; ++i, ++n_sub) {
+        const int h = halves == 2 ? i & 1 : 0, t = halves == 2 ? i >> 1 : i;
+        const int in_tile = h * 128 + r;
+        const bool live = h * 128 + quarter * 32 < s.rows;
+        const uint32_t buffer = n_sub & 1;
+        const long long pos0 = static_cast<long long>(s.chunk0 + t) * kTilePos + 64 * w;
         // At the edge: what this thread's row sees, and which of the warp's 32 positions any row sees.  Worked out
         // before the scores are there; again in the rare case that the unit turns out to have a bad page.
-        bool edge = pos0 + kTilePos > s.ctx, waited = false, bad = false;
-        uint32_t seen[4], seen_any = 0xffffffffu;
+        bool edge = pos0 + 64 > s.ctx, waited = false, bad = false;
+        uint32_t seen[2], seen_any = 0xffffffffu;
         for (;;) {
           if (edge) {
             const SegmentView view{a.b, a.pool, s.first, s.nodes, s.ctx, s.limit, a.b.table + s.seq * a.b.table_stride, bad};
-            seen_any = view.seen_by_any(pos0 + 32 * quarter, lane);
+            const int node = in_tile < s.rows ? t0 + small_div(rem0 + in_tile, a.group_inverse) : 0;
+            if (h == 0) seen_any = view.seen_by_any(pos0 + (r & 32), lane);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) seen[c] = live ? view.seen_by(node, pos0 + 32 * c) : 0u;
+            for (int c = 0; c < 2; ++c) seen[c] = live ? view.seen_by(node, pos0 + 32 * c) : 0u;
           }
           if (waited) break;
-          wait_for(bar_s + 8 * w, n_units & 1, give_up, status);
+          wait_for(bar_s + 8 * buffer, n_sub >> 1 & 1, give_up, status);
           waited = true;
-          bad = *static_cast<volatile int*>(&ctl->bad[(unit_base + s.unit(rel, i)) % 16]) != 0;
+          bad = *static_cast<volatile int*>(&ctl->bad[(unit_base + t) % 16]) != 0;
           if (!bad) break;
           edge = true;
         }
         tc_fence_after();
-        // Values at positions that no row sees may be anything, and 0 x NaN is NaN: they are cleared before P is given out.
-        auto clear_values = [&]() {
-          if (seen_any == 0xffffffffu) return;
-          RingPlace<kSlots> pv = pk;
-          pv.step(1);
-          wait_for(bar_full + 8 * pv.slot, pv.phase, give_up, status);
-          if (!(seen_any >> lane & 1)) {
-            uint8_t* row = s_ring + pv.slot * Geo::kSlotBytes + r * 128;
-#pragma unroll
-            for (int c = 0; c < D / 8; ++c) *reinterpret_cast<uint4*>(row + c / 8 * Geo::kPanel + c % 8 * 16) = make_uint4(0, 0, 0, 0);
-          }
-          fence_async_smem();
-        };
         if (live) {
-          uint32_t sc[4][32];
+          uint32_t sc[2][32];
 #pragma unroll
-          for (int c = 0; c < 4; ++c) tmem_load(sc[c], t_s + 32 * c);
+          for (int c = 0; c < 2; ++c) tmem_load(sc[c], t_s + buffer * kTilePos + 32 * c);
           tmem_wait_load();
 #pragma unroll
-          for (int c = 0; c < 4; ++c) tmem_use(sc[c]);
+          for (int c = 0; c < 2; ++c) tmem_use(sc[c]);
           if (edge) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
+            for (int c = 0; c < 2; ++c)
 #pragma unroll
               for (int j = 0; j < 32; ++j)
                 if (!(seen[c] >> j & 1)) sc[c][j] = 0xff800000u;
           }
-          float top = -INFINITY;
-#pragma unroll
-          for (int c = 0; c < 4; ++c) top = max_of(sc[c], top);
-          top *= a.scale_log2;
-          if (i == 0) {
-            m = top;
-          } else if (__any_sync(0xffffffffu, top > m + kSlack)) {
-            const float m_new = top > m + kSlack ? top : m;
+          // Both halves of the positions measure a row against the same reference.
+          const float top = max_of(sc[1], max_of(sc[0], -INFINITY)) * a.scale_log2;
+          if (i < halves) {
+            ctl->top[buffer][w][r] = top;
+            pair_sync();
+            m = fmaxf(top, ctl->top[buffer][w ^ 1][r]);
+          } else if (pair_any(top > m + kSlack)) {
+            ctl->top[buffer][w][r] = top;
+            pair_sync();
+            const float both = fmaxf(top, ctl->top[buffer][w ^ 1][r]);
+            const float m_new = both > m + kSlack ? both : m;
             const float f = m == m_new ? 1.f : ex2(m - m_new);
             m = m_new;
             sum.x *= f;
             sum.y *= f;
-            // the product before, which may still be adding to O
-            wait_for(bar_pv + 8 * w, (n_units - 1) & 1, give_up, status);
+            // behind the last product into this accumulator; each of the two warps takes half of its columns
+            if (halves == 1) wait_for(bar_pv + 8 * (buffer ^ 1), (n_sub - 1) >> 1 & 1, give_up, status);
             tc_fence_after();
 #pragma unroll 1
-            for (int k = 0; k < D / 16; ++k) {
+            for (int k = 0; k < D / 32; ++k) {
               uint32_t y[16];
-              tmem_load(y, t_o + 16 * k);
+              const uint32_t at = t_o + h * D + w * (D / 2) + 16 * k;
+              tmem_load(y, at);
               tmem_wait_load();
               tmem_use(y);
 #pragma unroll
               for (int j = 0; j < 16; ++j) y[j] = __float_as_uint(__uint_as_float(y[j]) * f);
-              tmem_store(t_o + 16 * k, y);
+              tmem_store(at, y);
             }
           }
-          begin_turn(i);
           const float2 scale = make_float2(a.scale_log2, a.scale_log2), shift = m == -INFINITY ? make_float2(0.f, 0.f) : make_float2(-m, -m);
+          uint32_t packed[32];
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            uint32_t packed[16];
+          for (int c = 0; c < 2; ++c)
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
               float2 p = fma2(make_float2(__uint_as_float(sc[c][2 * j]), __uint_as_float(sc[c][2 * j + 1])), scale, shift);
               p = make_float2(ex2(p.x), ex2(p.y));
               sum = add2(sum, p);
-              packed[j] = Half2Of<T>::pack(p.x, p.y);
+              packed[16 * c + j] = Half2Of<T>::pack(p.x, p.y);
             }
-            if (c == 3) end_turn(i);
-            tmem_store(t_s + 16 * c, packed);
-            if (c & 1) tmem_wait_store();
-            if (c == 1) {
-              clear_values();
-              if (i == 0) output_free();
-            }
-            if (c & 1) {
-              tc_fence_before();
-              __syncwarp();
-              if (lane == 0) mbar_arrive(bar_p + 16 * w + 8 * (c >> 1));
-            }
-          }
-        } else {
-          begin_turn(i);
-          end_turn(i);
-          clear_values();
-          if (i == 0) output_free();
-          __syncwarp();
-          if (lane == 0) {
-            mbar_arrive(bar_p + 16 * w);
-            mbar_arrive(bar_p + 16 * w + 8);
-          }
+          tmem_store(t_s + buffer * kTilePos, packed);
+          tmem_wait_store();
         }
-        pk.step(s.halves() ? 2 : 4);
+        if (seen_any != 0xffffffffu) {
+          // Values at positions that no row sees may be anything, and 0 x NaN is NaN: clear them.
+          RingPlace<kSlots> pv = pk;
+          pv.step(1);
+          wait_for(bar_full + 8 * pv.slot, pv.phase, give_up, status);
+          if (!(seen_any >> lane & 1)) {
+            uint8_t* row = s_ring + pv.slot * Geo::kSlotBytes + (64 * w + (r & 63)) * 128;
+            constexpr int kHalfRow = D / 16;      // 16-byte pieces
+#pragma unroll
+            for (int c = 0; c < kHalfRow; ++c) {
+              const int piece = (r >> 6) * kHalfRow + c;
+              *reinterpret_cast<uint4*>(row + piece / 8 * Geo::kPanel + piece % 8 * 16) = make_uint4(0, 0, 0, 0);
+            }
+          }
+          fence_async_smem();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_p + 16 * buffer + 8 * w);
+        if (h == halves - 1) pk.step(2);
+        if (halves == 2) {
+          const float x = m;
+          const float2 y = sum;
+          m = m_other;
+          sum = sum_other;
+          m_other = x;
+          sum_other = y;
+        }
         if (i == 0) load_next();
       }
-      // ---- the segment's result ----
-      if (next_loads) queries_ready();      // the next scores may follow this group's last product
+      // ---- the segment's result: each of the two warps takes half of the columns ----
+      if (next_loads) queries_ready();      // the next scores may follow the last product
       loaded = next_loads;
       unit_base += s.n;
-      const bool join = !s.halves() && s.n > 1;      // the groups took every other unit each: the first one adds the other's state to its own
-      float total = sum.x + sum.y, other_m = -INFINITY, other_sum = 0.f;
-      if (count > 0) wait_for(bar_pv + 8 * w, (n_units - 1) & 1, give_up, status);
+      wait_for(bar_pv + 8 * ((n_sub - 1) & 1), (n_sub - 1) >> 1 & 1, give_up, status);
       tc_fence_after();
       __syncwarp();
       wait_before();
       if (lane == 0) mbar_arrive(bar_done);
-      if (join) {
-        if (rel == 1) {
-          ctl->ml[r] = make_float2(m, total);
-          tc_fence_before();
-          asm volatile("bar.arrive %0, %1;" ::"r"(11 + w), "n"(kSoftmaxThreads) : "memory");
-          handed = true;
-        } else {
-          asm volatile("bar.sync %0, %1;" ::"r"(11 + (w ^ 1)), "n"(kSoftmaxThreads) : "memory");
-          tc_fence_after();
-          const float2 ml = ctl->ml[r];
-          other_m = ml.x;
-          other_sum = ml.y;
-        }
-      }
-      if (live && (s.halves() || rel == 0)) {
-        const float m_all = fmaxf(m, other_m);
-        float f0 = m == -INFINITY ? 0.f : ex2(m - m_all), f1 = other_m == -INFINITY ? 0.f : ex2(other_m - m_all);
-        total = total * f0 + other_sum * f1;
-        if (s.kind == 0) {
-          const float inv = total > 0.f ? 1.f / total : 0.f;
-          f0 *= inv;
-          f1 *= inv;
-        }
-        const bool mine = in_tile < s.rows;
-        const int64_t at = mine ? place_of(s, t0, rem0, in_tile) : 0;
-        const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) + (s.kind == 2);
 #pragma unroll 1
-        for (int c = 0; c < D / 32; ++c) {
-          uint32_t o[32], o1[32];
-          float y[32];
-          tmem_load(o, t_o + 32 * c);
-          if (join) tmem_load(o1, t_other + 32 * c);
-          tmem_wait_load();
-          tmem_use(o);
-          if (join) {
-            tmem_use(o1);
+      for (int h = 0; h < halves; ++h) {
+        const int in_tile = h * 128 + r;
+        if (h * 128 + quarter * 32 < s.rows) {
+          float total = sum.x + sum.y;
+          ctl->top[h][w][r] = total;
+          pair_sync();
+          total += ctl->top[h][w ^ 1][r];
+          const float f = s.kind == 0 ? (total > 0.f ? 1.f / total : 0.f) : 1.f;
+          const bool mine = in_tile < s.rows;
+          const int64_t at = mine ? place_of(s, t0, rem0, in_tile) : 0;
+          const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) + (s.kind == 2);
+#pragma unroll 1
+          for (int c = w * (D / 64); c < (w + 1) * (D / 64); ++c) {
+            uint32_t o[32];
+            float y[32];
+            tmem_load(o, t_o + h * D + 32 * c);
+            tmem_wait_load();
+            tmem_use(o);
 #pragma unroll
-            for (int j = 0; j < 32; ++j) y[j] = __uint_as_float(o[j]) * f0 + __uint_as_float(o1[j]) * f1;
-          } else {
+            for (int j = 0; j < 32; ++j) y[j] = __uint_as_float(o[j]) * f;
+            if (mine) {
+              if (s.kind == 0) {
+                store_row(static_cast<Out*>(a.out) + at * D + 32 * c, y);
+              } else {
+                float4* dst = reinterpret_cast<float4*>(a.part_o) + (slot * (D / 4) + 8 * c) * kTileRows + in_tile;
 #pragma unroll
-            for (int j = 0; j < 32; ++j) y[j] = __uint_as_float(o[j]) * f0;
-          }
-          if (mine) {
-            if (s.kind == 0) {
-              store_row(static_cast<Out*>(a.out) + at * D + 32 * c, y);
-            } else {
-              float4* dst = reinterpret_cast<float4*>(a.part_o) + (slot * (D / 4) + 8 * c) * kTileRows + in_tile;
-#pragma unroll
-              for (int j = 0; j < 8; ++j) dst[j * kTileRows] = make_float4(y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]);
+                for (int j = 0; j < 8; ++j) dst[j * kTileRows] = make_float4(y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]);
+              }
             }
           }
+          if (mine && w == 0) {
+            if (s.kind != 0) a.part_ml[slot * kTileRows + in_tile] = make_float2(m, total);
+            else if (a.lse) a.lse[at] = total > 0.f ? (m + log2f(total)) * kLn2 : -INFINITY;
+          }
         }
-        if (mine) {
-          if (s.kind != 0) a.part_ml[slot * kTileRows + in_tile] = make_float2(m_all, total);
-          else if (a.lse) a.lse[at] = total > 0.f ? (m_all + log2f(total)) * kLn2 : -INFINITY;
-        }
+        m = m_other;
+        sum = sum_other;
       }
       tc_fence_before();
-      if (join && rel == 0) asm volatile("bar.arrive %0, %1;" ::"r"(13 + (w ^ 1)), "n"(kSoftmaxThreads) : "memory");
       done_with(si);
     }
-    if (handed) asm volatile("bar.sync %0, %1;" ::"r"(13 + w), "n"(kSoftmaxThreads) : "memory");
   }
   tc_fence_before();
   __syncthreads();
@@ -807,9 +768,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
 
   // A wait that gave up may have left products or copies under way: they end before the memory is given back.
   if (ctl->give_up) {
-    if ((warp == 9 || warp == 10) && lane == 0) {
-      tc_commit(bar_drain + 8 * (warp - 9));
-      for (int i = 0; i < (1 << 22) && !mbar_test(bar_drain + 8 * (warp - 9), 0); ++i) {}
+    if (tid == 9 * 32) {
+      tc_commit(bar_drain);
+      for (int i = 0; i < (1 << 22) && !mbar_test(bar_drain, 0); ++i) {}
     }
     if (tid == 8 * 32)
       for (uint32_t p = 0; p < copies_before; ++p) {      // the last places
@@ -823,20 +784,20 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
 }
 
 // ---- few rows ---------------------------------------------------------------------------------------------------------
-// Where a KV head is read by at most 16 M rows of a sequence (single tokens, short drafts), 128-row products are mostly
+// Where a KV head is read by few rows of a sequence (single tokens, short drafts), 128-row products are mostly
 // padding and what counts is the path from one short sequence to the next.  Here a CTA of four warps takes a share;
 // each warp streams every fourth group of 16 positions through a ring of its own (16-byte asynchronous copies) and
 // applies it with m16n8k16 products, queries and output in registers; several CTAs per SM hide one another's starts and
 // ends.  The warps' states are joined through shared memory at the end of a segment.
-template <int D, int M> struct StreamGeometry {
+template <int D> struct StreamGeometry {
   static constexpr int kStages = 3;
   static constexpr int kStep = 16;                             // positions
   static constexpr int kRow = D * 2;                           // bytes
   static constexpr int kStage = 2 * kStep * kRow;              // keys and values of a step
   static constexpr int kWarpBytes = kStages * kStage;
-  static constexpr int kBytes = 4 * kWarpBytes + 16 * M * kRow;
-  static constexpr int kCtas = D == 128 ? 2 : M == 1 ? 4 : 3;  // per SM
-  static_assert(16 * M * D * 4 <= kWarpBytes, "a warp's output fits where its ring was");
+  static constexpr int kBytes = 4 * kWarpBytes + 16 * kRow;
+  static constexpr int kCtas = D == 128 ? 2 : 4;               // per SM
+  static_assert(16 * D * 4 <= kWarpBytes, "a warp's output fits where its ring was");
 };
 
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
@@ -855,9 +816,10 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-template <typename T, typename Out, int D, int M>
-__global__ void __launch_bounds__(128, StreamGeometry<D, M>::kCtas) tree_stream_kernel(const __grid_constant__ TreeArgs a) {
-  using Geo = StreamGeometry<D, M>;
+template <typename T, typename Out, int D>
+__global__ void __launch_bounds__(128, StreamGeometry<D>::kCtas) tree_stream_kernel(const __grid_constant__ TreeArgs a) {
+  using Geo = StreamGeometry<D>;
+  constexpr int M = 1;                                // tiles of 16 rows
   constexpr bool kBf16 = !__is_same(T, __half);
   constexpr int kPieces = D / 8, kRows = 16 * M;      // 16-byte pieces of a row
   extern __shared__ __align__(128) uint8_t smem_raw[];
@@ -1186,17 +1148,13 @@ int64_t padded(int64_t n) { return (n + kAlign - 1) / kAlign * kAlign; }
 struct Maps { CUtensorMap k, v; };
 
 // Which kernel, by the rows that a KV head has of a sequence on average (the lengths themselves are on the device; each
-// kernel is right for any): up to 32 the streaming kernel, beyond it the tensor-memory kernel.
-int stream_tiles(const BatchView& b, int group) {
-  const int64_t rows = (static_cast<int64_t>(b.n_tok) + b.n_seq - 1) / b.n_seq * group;
-  return rows <= 16 ? 1 : rows <= 32 ? 2 : 0;
-}
+// kernel is right for any): up to 32 the streaming kernel, which takes 16 at a time, beyond it the tensor-memory kernel.
+bool streams(const BatchView& b, int group) { return (static_cast<int64_t>(b.n_tok) + b.n_seq - 1) / b.n_seq * group <= 32; }
 struct Workers {
   int n, tile_rows;
 };
 Workers workers_of(const prima_paged& pool, const BatchView& b, int group) {
-  const int m = stream_tiles(b, group);
-  return m ? Workers{pool.sm_count * (pool.cfg.head_dim == 128 ? 2 : m == 1 ? 4 : 3), 16 * m} : Workers{pool.sm_count, kTileRows};
+  return streams(b, group) ? Workers{pool.sm_count * (pool.cfg.head_dim == 128 ? 2 : 4), 16} : Workers{pool.sm_count, kTileRows};
 }
 
 template <typename Kernel>
@@ -1208,24 +1166,23 @@ cudaError_t allow_smem(Kernel kernel, size_t bytes, bool (&done)[kMaxDevices]) {
   return e;
 }
 
-template <typename T, typename Out, int D, int M>
+template <typename T, typename Out, int D>
 cudaError_t launch_stream(const TreeArgs& a, int n_cta, cudaStream_t st) {
-  using Geo = StreamGeometry<D, M>;
+  using Geo = StreamGeometry<D>;
   static bool done[kMaxDevices] = {};
-  auto kernel = tree_stream_kernel<T, Out, D, M>;
+  auto kernel = tree_stream_kernel<T, Out, D>;
   cudaError_t e = allow_smem(kernel, Geo::kBytes, done);
   if (e == cudaSuccess) e = launch_pdl(kernel, dim3(n_cta), dim3(128), Geo::kBytes, st, a);
   if (e != cudaSuccess) return e;
-  constexpr int kRows = 16 * M;
+  constexpr int kRows = 16;
   return launch_pdl(tree_merge_kernel<Out, D, kRows>, dim3(n_cta, 1, D / 4 * kRows / 256), dim3(256), 0, st, a);
 }
 
 template <typename T, typename Out, int D>
 cudaError_t launch_tree(const prima_paged& pool, TreeArgs a, int n_cta, cudaStream_t st) {
-  if (a.shape.tile_rows == 16) return launch_stream<T, Out, D, 1>(a, n_cta, st);
-  if (a.shape.tile_rows == 32) return launch_stream<T, Out, D, 2>(a, n_cta, st);
+  if (a.shape.tile_rows == 16) return launch_stream<T, Out, D>(a, n_cta, st);
   using Geo = Geometry<D>;
-  constexpr size_t kSmem = 1024 + 2 * Geo::kQBytes + Geo::kSlots * Geo::kSlotBytes + sizeof(Control);
+  constexpr size_t kSmem = 2 * Geo::kQBytes + Geo::kSlots * Geo::kSlotBytes + sizeof(Control);
   static_assert(kSmem <= 232448, "shared memory of a CTA");
   static bool done[kMaxDevices] = {};
   auto kernel = tree_kernel<T, Out, D>;
@@ -1275,7 +1232,7 @@ extern "C" {
 int64_t prima_tree_attention_workspace(const prima_paged* p, int n_seq, int n_tok, int n_q_heads) {
   if (!p || n_seq < 1 || n_tok < 1 || n_q_heads < 1) return PRIMA_ERR_ARG;
   const int64_t n = p->sm_count;
-  static_assert(4 * 32 <= kTileRows, "four workers of the streaming kernel need no more");
+  static_assert(4 * 16 <= kTileRows, "four workers of the streaming kernel need no more");
   return padded(4 * n * static_cast<int64_t>(sizeof(TailNote))) + padded(2 * n * kTileRows * static_cast<int64_t>(sizeof(float2))) +
          padded(2 * n * kTileRows * p->cfg.head_dim * static_cast<int64_t>(sizeof(float)));
 }
