@@ -352,9 +352,10 @@ const char* prima_gemv_q4k_noalloc_error(void);
  * status word, which prima_paged_sync reports.
  *
  * All calls queue their kernels on `stream` and return; none allocates, waits or keeps anything of a call for the
- * next.  Calls on different streams are independent as far as their arrays and workspaces are.  Calls may be
- * captured.  The pool's device is made current for the duration of a call.  Errors: PRIMA_ERR_ARG with nothing
- * queued, the message in prima_last_error(NULL); PRIMA_ERR_CUDA. */
+ * next (prima_forward_window_paged: below).  Calls on different streams are independent as far as their arrays and
+ * workspaces are.  Calls may be captured.  The pool's device is made current for the duration of a call;
+ * prima_beam_select, which has no pool, runs on the current device.  Arrays are aligned to their elements at least.
+ * Errors: PRIMA_ERR_ARG with nothing queued, the message in prima_last_error(NULL); PRIMA_ERR_CUDA. */
 #define PRIMA_DT_F32 0
 #define PRIMA_DT_F16 1
 #define PRIMA_DT_BF16 2
@@ -379,7 +380,7 @@ typedef struct {
   const int32_t* row_begin;    /* dev [n_seq + 1]                                                     */
   const int32_t* ctx_len;      /* dev [n_seq]                                                         */
   const int32_t* table;        /* dev [n_seq][table_stride]: page ids                                 */
-  int64_t table_stride;        /* pages per row of the table, >= 1                                    */
+  int64_t table_stride;        /* pages per row of the table, 1 .. 2^31 - 1                           */
   const int32_t* pos;          /* dev [n_tok], or NULL: the slot.  Position that the rotation of a row uses (in a
                                   tree: context + depth of the node)                                  */
   const uint64_t* mask;        /* dev [n_tok][mask_words], or NULL.  Bit a (word a / 64, bit a % 64) of a row: the row
@@ -423,7 +424,8 @@ int prima_tree_attention(prima_paged* pool, int layer, const prima_paged_batch* 
  * batch->n_tok (1..max_n_tok) rows of hidden_in / hidden_out, each of its own sequence, at its own position, seeing what
  * the batch says (a chain, a tree of drafted tokens, one token of each of several requests or beams).  The pool takes the
  * place of the context's own caches; layer l of the model is layer l of the pool, whose KV heads, head size, rotation and
- * device must be the model's.  The calls run on the context's stream, and the context keeps one workspace for them.  Rows
+ * device must be the model's.  The calls run on the context's stream, and the context keeps one workspace for them, which
+ * the first call allocates (refused with PRIMA_ERR_STATE while the stream is being captured; later calls may be).  Rows
  * behind the last sequence are computed with whatever their hidden rows hold and appended nowhere; they do not touch the
  * others.  Errors as prima_forward_window. */
 int prima_forward_window_paged(prima_ctx* ctx, prima_paged* pool, int layer_begin, int layer_end, const float* hidden_in, float* hidden_out,

@@ -458,8 +458,10 @@ class PagedCache:
         lp = _need(lse, "lse", self._f32, shape[:2], self.device) if lse is not None else None
         if workspace is None:
             workspace = self.tree_attention_workspace(batch, heads, stream)
+        elif workspace.device != self.device or not workspace.is_contiguous():
+            raise ValueError(f"workspace: expected a contiguous tensor on {self.device}")
         rc = self._lib.prima_tree_attention(self._h, layer, self._batch(batch), qp, heads, self.head_dim ** -0.5 if scale is None else scale, op, _dtype_code(out), lp,
-                                            workspace.data_ptr(), workspace.numel(), _stream_of(stream, self.device))
+                                            workspace.data_ptr(), workspace.nbytes, _stream_of(stream, self.device))
         if rc:
             _check(rc)
 
@@ -501,17 +503,19 @@ def prima_beam_select(logits, cum, score, parent, token, finished=None, end_toke
     outputs ``score`` fp32, ``parent`` and ``token`` int32 [n_req, keep]."""
     import torch
     shape, step = logits.shape, logits.stride()
-    if len(shape) != 3 or not logits.is_cuda or step[2] != 1 or (shape[0] > 1 and step[0] != shape[1] * step[1]):
+    if len(shape) != 3 or not logits.is_cuda or step[2] != 1 or (shape[0] > 1 and shape[1] > 1 and step[0] != shape[1] * step[1]):
         raise ValueError("logits: expected a CUDA tensor [n_req, n_beams, vocab] with evenly spaced rows")
     n_req, n_beams, vocab = shape
     dev, keep = logits.device, score.shape[-1]
     beams, kept, f32, i32 = (n_req, n_beams), (n_req, keep), torch.float32, torch.int32
     if workspace is None:
         workspace = prima_beam_select_workspace(n_req, n_beams, vocab, keep, dev, stream)
+    elif workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace: expected a contiguous tensor on {dev}")
     stride = step[1] if n_beams > 1 else step[0] if n_req > 1 else vocab
     args = (logits.data_ptr(), _dtype_code(logits), n_req, n_beams, vocab, stride, _need(cum, "cum", f32, beams, dev),
             _need(finished, "finished", torch.uint8, beams, dev) if finished is not None else None, end_token, keep, _need(score, "score", f32, kept, dev),
-            _need(parent, "parent", i32, kept, dev), _need(token, "token", i32, kept, dev), workspace.data_ptr(), workspace.numel(), _stream_of(stream, dev))
+            _need(parent, "parent", i32, kept, dev), _need(token, "token", i32, kept, dev), workspace.data_ptr(), workspace.nbytes, _stream_of(stream, dev))
     if torch._C._cuda_getDevice() == dev.index:
         rc = lib().prima_beam_select(*args)
     else:

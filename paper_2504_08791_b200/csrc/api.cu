@@ -737,6 +737,13 @@ static int forward_window_impl(prima_ctx* c, int layer_begin, int layer_end, con
   }
   if (paged) {
     const int64_t n = c->cfg.max_n_tok, H = c->cfg.n_q_heads, G = c->cfg.n_kv_heads;
+    const int64_t need = prima_tree_attention_workspace(paged->pool, static_cast<int>(n), static_cast<int>(n), static_cast<int>(H));
+    if (c->paged_ws_bytes < need) {      // an allocation would end a capture
+      cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+      const cudaError_t e = cudaStreamIsCapturing(c->stream, &capture);
+      if (e != cudaSuccess) return cuda_fail(c, e, "prima_forward_window_paged");
+      if (capture != cudaStreamCaptureStatusNone) return fail(c, PRIMA_ERR_STATE, "prima_forward_window_paged: the first call allocates and cannot be captured");
+    }
     int rc = PRIMA_OK;
     // zeroed: rows of a step that belong to no sequence are not written by the attention, but go through the products
     if (!c->paged_qkv) rc = dev_alloc(c, &c->paged_qkv, static_cast<size_t>(n * (H + 2 * G) * kHeadDim), true);
@@ -745,7 +752,6 @@ static int forward_window_impl(prima_ctx* c, int layer_begin, int layer_end, con
       rc = dev_alloc(c, &q, static_cast<size_t>(n * H * kHeadDim), true);
       c->paged_q = q;
     }
-    const int64_t need = prima_tree_attention_workspace(paged->pool, static_cast<int>(n), static_cast<int>(n), static_cast<int>(H));
     if (rc == PRIMA_OK && c->paged_ws_bytes < need) {
       uint8_t* ws = nullptr;
       rc = dev_alloc(c, &ws, static_cast<size_t>(need));

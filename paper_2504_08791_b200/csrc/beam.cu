@@ -445,6 +445,8 @@ int prima_beam_select(const void* logits, int dtype, int n_req, int n_beams, int
   }
   if (!logits || !cum || !score || !parent || !token || !workspace) return call_fail(PRIMA_ERR_ARG, "prima_beam_select: null argument");
   if (dtype != PRIMA_DT_F32 && dtype != PRIMA_DT_F16 && dtype != PRIMA_DT_BF16) return call_fail(PRIMA_ERR_ARG, "prima_beam_select: unknown dtype");
+  if (!aligned_to(logits, dtype == PRIMA_DT_F32 ? 4 : 2) || !aligned_to(cum, 4) || !aligned_to(score, 4) || !aligned_to(parent, 4) || !aligned_to(token, 4))
+    return call_fail(PRIMA_ERR_ARG, "prima_beam_select: an array is not aligned to its elements");
   if (row_stride < vocab) return call_fail(PRIMA_ERR_ARG, "prima_beam_select: row_stride is shorter than a row");
   if (finished && (end_token < 0 || end_token >= vocab)) return call_fail(PRIMA_ERR_ARG, "prima_beam_select: end_token outside the vocabulary");
   if ((reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < prima_beam_select_workspace(n_req, n_beams, vocab, keep))

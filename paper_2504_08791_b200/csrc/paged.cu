@@ -237,7 +237,7 @@ __global__ void __launch_bounds__(256) reorder_kernel(PoolView pool, int n_beams
   }
 }
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+bool aligned16(const void* p) { return aligned_to(p, 16); }
 
 template <typename T, typename In, int D>
 cudaError_t launch_append(const prima_paged& pool, const BatchView& b, int layer, const void* q, const void* k, const void* v, int n_q_heads,
@@ -259,7 +259,10 @@ int check_batch(const prima_paged* pool, const prima_paged_batch* b, const char*
   if (!pool || !b) bad = "null pool or batch";
   else if (b->n_seq < 1 || b->n_tok < 1) bad = "n_seq and n_tok must be positive";
   else if (!b->row_begin || !b->ctx_len || !b->table || b->table_stride < 1) bad = "row_begin, ctx_len and table are needed";
+  else if (b->table_stride > 2147483647) bad = "table_stride reaches 2^31";
   else if (b->mask && (b->mask_words < 1 || b->mask_words > 16)) bad = "mask_words outside 1..16";
+  else if (!aligned_to(b->row_begin, 4) || !aligned_to(b->ctx_len, 4) || !aligned_to(b->table, 4) || !aligned_to(b->pos, 4) || !aligned_to(b->mask, 8))
+    bad = "an array is not aligned to its elements";
   if (!bad) return PRIMA_OK;
   snprintf(msg, sizeof msg, "%s: %s", who, bad);
   return call_fail(PRIMA_ERR_ARG, msg);
@@ -352,6 +355,8 @@ int prima_paged_append(prima_paged* p, int layer, const prima_paged_batch* batch
   if (!k || !v || (q != nullptr) != (q_out != nullptr)) return call_fail(PRIMA_ERR_ARG, "prima_paged_append: null k or v, or only one of q and q_out");
   if (in_dtype != PRIMA_DT_F32 && in_dtype != c.dtype) return call_fail(PRIMA_ERR_ARG, "prima_paged_append: in_dtype is neither fp32 nor the cache's type");
   if (q ? n_q_heads < 1 || n_q_heads > (1 << 16) : n_q_heads != 0) return call_fail(PRIMA_ERR_ARG, "prima_paged_append: n_q_heads");
+  const size_t size = in_dtype == PRIMA_DT_F32 ? 4 : 2;
+  if (!aligned_to(q, size) || !aligned_to(k, size) || !aligned_to(v, size)) return call_fail(PRIMA_ERR_ARG, "prima_paged_append: q, k or v is not aligned to its elements");
   if (!aligned16(q_out)) return call_fail(PRIMA_ERR_ARG, "prima_paged_append: q_out must be 16-byte aligned");
   const int64_t need_q = static_cast<int64_t>(n_q_heads) * c.head_dim, need_kv = static_cast<int64_t>(c.n_kv_heads) * c.head_dim;
   if ((q && q_stride < need_q) || k_stride < need_kv || v_stride < need_kv) return call_fail(PRIMA_ERR_ARG, "prima_paged_append: a stride is shorter than a row");
@@ -373,6 +378,7 @@ int prima_paged_accept(prima_paged* p, const prima_paged_batch* batch, const int
   const int rc = check_batch(p, batch, "prima_paged_accept");
   if (rc != PRIMA_OK) return rc;
   if (!path || !path_len || path_stride < 1) return call_fail(PRIMA_ERR_ARG, "prima_paged_accept: path, path_len and a positive path_stride are needed");
+  if (!aligned_to(path, 4) || !aligned_to(path_len, 4)) return call_fail(PRIMA_ERR_ARG, "prima_paged_accept: path or path_len is not 4-byte aligned");
   CallDevice dev(p->cfg.device);
   if (!dev.ok) return call_fail(PRIMA_ERR_CUDA, "cudaSetDevice failed");
   // CTAs of a sequence: as many as its columns fill, and as keep every SM busy with all sequences together
@@ -388,9 +394,11 @@ int prima_paged_reorder(prima_paged* p, int n_req, int n_beams, int keep, const 
                         const int32_t* parent, const int32_t* fresh, int32_t* table_out, int32_t* length_out, void* stream) {
   if (!p || !table_in || !length_in || !parent || !fresh || !table_out || !length_out)
     return call_fail(PRIMA_ERR_ARG, "prima_paged_reorder: null argument");
-  if (n_req < 1 || n_beams < 1 || keep < 1 || n_beams > 65536 || keep > 65536 || table_stride < 1 ||
+  if (n_req < 1 || n_beams < 1 || keep < 1 || n_beams > 65536 || keep > 65536 || table_stride < 1 || table_stride > 2147483647 ||
       static_cast<int64_t>(n_req) * std::max(n_beams, keep) > 2147483647)
     return call_fail(PRIMA_ERR_ARG, "prima_paged_reorder: bad size");
+  for (const int32_t* x : {table_in, length_in, parent, fresh, static_cast<const int32_t*>(table_out), static_cast<const int32_t*>(length_out)})
+    if (!aligned_to(x, 4)) return call_fail(PRIMA_ERR_ARG, "prima_paged_reorder: an array is not 4-byte aligned");
   const int64_t rows_in = static_cast<int64_t>(n_req) * n_beams, rows_out = static_cast<int64_t>(n_req) * keep;
   auto overlap = [](const int32_t* a, int64_t na, const int32_t* b, int64_t nb) { return a < b + nb && b < a + na; };
   if (overlap(table_in, rows_in * table_stride, table_out, rows_out * table_stride) || overlap(length_in, rows_in, length_out, rows_out))

@@ -37,6 +37,9 @@ struct CallDevice {              // makes a device current for the duration of a
   }
 };
 
+// Whether an address is a multiple of n, a power of two (device code faults on others).
+inline bool aligned_to(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
 // The checks of a batch that need no device memory; PRIMA_OK or an error that is already recorded.
 int check_batch(const prima_paged* pool, const prima_paged_batch* b, const char* who);
 

@@ -327,8 +327,12 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
   // The swizzled tiles need 1024-byte alignment, which the shared memory of a kernel without static variables has; there
   // is no room to round up.
   extern __shared__ __align__(1024) uint8_t smem[];
-  if (smem_u32(smem) & 1023) {
-    if (threadIdx.x == 0) raise(a.pool.status, kGaveUp);
+  if (smem_u32(smem) & 1023) {      // never seen; nothing is computed, and the joining kernel finds nothing to join
+    pdl_wait();
+    if (threadIdx.x == 0) {
+      a.notes[blockIdx.x].rows = 0;
+      raise(a.pool.status, kGaveUp);
+    }
     return;
   }
   uint8_t* s_q = smem;
@@ -1249,6 +1253,7 @@ int prima_tree_attention(prima_paged* p, int layer, const prima_paged_batch* bat
   if (!(scale > 0.f) || std::isinf(scale)) return call_fail(PRIMA_ERR_ARG, "prima_tree_attention: scale must be positive and finite");
   if (out_dtype != PRIMA_DT_F32 && out_dtype != c.dtype) return call_fail(PRIMA_ERR_ARG, "prima_tree_attention: out_dtype is neither fp32 nor the cache's type");
   if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & 15) return call_fail(PRIMA_ERR_ARG, "prima_tree_attention: q and out must be 16-byte aligned");
+  if (reinterpret_cast<uintptr_t>(lse) & 3) return call_fail(PRIMA_ERR_ARG, "prima_tree_attention: lse must be 4-byte aligned");
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < prima_tree_attention_workspace(p, batch->n_seq, batch->n_tok, n_q_heads))
     return call_fail(PRIMA_ERR_ARG, "prima_tree_attention: workspace too small or not 256-byte aligned");
   CallDevice dev(c.device);
