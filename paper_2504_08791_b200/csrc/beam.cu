@@ -38,22 +38,31 @@ __device__ __forceinline__ float ex2(float x) {
 
 // A bound that at least `keep` of the threads' values reach (-infinity if fewer are above it): the keep-th largest of
 // the maxima of groups of threads.  The groups are the smallest number, 8 .. 64, that holds keep; of thousands of
-// values a few dozen reach the bound, at the cost of a few shuffles.  s_group: 64 values.
+// values a few dozen reach the bound, at the cost of a few shuffles.  A group is every 8th .. 64th thread, so that a short
+// last slice, or one beam's candidates, still reach every group: with a group that has nothing the bound is -infinity and
+// everything is ranked against everything (512 words of a slice: 17 us).  s_group: kThreads values, s_max: 64.
 template <typename V>
-__device__ __forceinline__ V block_bound(V mine, int keep, V* s_group, V* s_bound) {
-  const int n_groups = keep <= 8 ? 8 : keep <= 16 ? 16 : keep <= 32 ? 32 : 64, lanes = kThreads / n_groups;
+__device__ __forceinline__ V block_bound(V mine, int keep, V* s_group, V* s_max, V* s_bound) {
+  const int n_groups = keep <= 8 ? 8 : keep <= 16 ? 16 : keep <= 32 ? 32 : 64, per = min(n_groups, 32);      // per: values of a warp
   const V lowest = static_cast<V>(-INFINITY);
-  for (int o = lanes >> 1; o > 0; o >>= 1) {
+  const int tid = threadIdx.x, lane = tid & 31;
+  for (int o = 16; o >= per; o >>= 1) {
     const V other = __shfl_xor_sync(0xffffffffu, mine, o);
     mine = other > mine ? other : mine;
   }
-  if (threadIdx.x % lanes == 0) s_group[threadIdx.x / lanes] = mine;
-  if (threadIdx.x == 0) *s_bound = lowest;
+  if (lane < per) s_group[(tid >> 5) * per + lane] = mine;
+  if (tid == 0) *s_bound = lowest;
   __syncthreads();
-  if (threadIdx.x < n_groups) {
-    const V v = s_group[threadIdx.x];
+  if (tid < n_groups) {
+    V v = lowest;
+    for (int j = tid; j < kThreads / 32 * per; j += n_groups) v = s_group[j] > v ? s_group[j] : v;
+    s_max[tid] = v;
+  }
+  __syncthreads();
+  if (tid < n_groups) {
+    const V v = s_max[tid];
     int rank = 0;
-    for (int j = 0; j < n_groups; ++j) rank += s_group[j] > v || (s_group[j] == v && j < static_cast<int>(threadIdx.x));
+    for (int j = 0; j < n_groups; ++j) rank += s_max[j] > v || (s_max[j] == v && j < tid);
     if (rank == keep - 1) *s_bound = v;
   }
   __syncthreads();
@@ -106,14 +115,16 @@ __device__ __forceinline__ float2 mul2(float2 x, float2 y) {
 // E logits per thread: a slice of kThreads * E words of one row.  A CTA takes `per_split` consecutive slices of a row
 // and leaves a maximum, a sum and the `keep` best logits.  Every thread sums its own words against its own running
 // maximum.  After the first slice, whose best make the bound that later logits have to reach, the warps go on without
-// barriers, the next logits in flight.  Bound by instructions: about 200 per warp and 32 words each.
+// barriers, the next logits in flight.  Not bound by HBM: 7.6 instructions per logit (reading, maximum, difference,
+// exponential, sum, comparison with the bound) and the latency of the beginning and the end of a CTA; 128 rows of 152,064
+// fp32 logits, of which 64 MB are read: about 20 us, 3.2 TB/s (27.5 us with the joining kernel).
 template <typename T, int E>
 __global__ void __launch_bounds__(kThreads, 3) beam_slice_kernel(const T* __restrict__ logits, int64_t row_stride, int vocab, const float* __restrict__ cum,
                                                               const uint8_t* __restrict__ finished, int keep, int n_slices, int per_split, bool wide,
                                                               SliceStat* __restrict__ stat, Best* __restrict__ best) {
   constexpr int kVec = 16 / sizeof(T);
   constexpr float kLog2e = 1.4426950408889634f;
-  __shared__ float s_group[64], s_bound, s_x[kSliceFound], s_top[kThreads / 32];
+  __shared__ float s_group[kThreads], s_max[64], s_bound, s_x[kSliceFound], s_top[kThreads / 32];
   __shared__ int s_w[kSliceFound], s_n;
   __shared__ double s_sum[kThreads / 32];
   __shared__ Best s_keep[kMaxKeep];
@@ -161,7 +172,7 @@ __global__ void __launch_bounds__(kThreads, 3) beam_slice_kernel(const T* __rest
       for (int i = 0; i < kChunk; ++i) tops[j] = fmaxf(tops[j], x[j * kChunk + i]);
     }
     const float top = fminf(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), FLT_MAX);
-    if (slice == slice0) bound = block_bound(top, keep, s_group, &s_bound);
+    if (slice == slice0) bound = block_bound(top, keep, s_group, s_max, &s_bound);
     if (top > -INFINITY) {
       if (top > ref) {
         sum *= ex2((ref - top) * kLog2e);
@@ -273,7 +284,7 @@ __global__ void __launch_bounds__(kThreads) beam_join_kernel(int n_beams, int vo
   // of every beam: what its logits are measured from, log of the sum; a beam without candidates: +infinity, 0;
   // a finished one: NaN (its only candidate is the end token)
   __shared__ double s_top[kMaxKeep], s_log[kMaxKeep], s_cum[kMaxKeep];
-  __shared__ double s_group[64], s_bound, s_score[kFound], s_bx[kThreads / 32];
+  __shared__ double s_group[kThreads], s_max[64], s_bound, s_score[kFound], s_bx[kThreads / 32];
   __shared__ int s_at[kFound], s_n, s_bi[kThreads / 32];
   pdl_trigger();
   pdl_wait();
@@ -309,26 +320,27 @@ __global__ void __launch_bounds__(kThreads) beam_join_kernel(int n_beams, int vo
   if (tid == 0) s_n = 0;
   __syncthreads();
 
-  // Calls f(score, index) for the thread's candidates.  Candidates are dealt out one by one over all beams, so that the
-  // groups of threads whose maxima give the bound are alike.
+  // Calls f(score, index) for the thread's candidates.  They are dealt out one by one, of a beam first the best of every
+  // slice, so that every group of threads whose maximum counts for the bound has some of the best, even if one beam holds
+  // them all.
   const unsigned n_all = static_cast<unsigned>(n_beams) * per_beam;
   const Best* list = best + static_cast<int64_t>(row0) * per_beam;
   auto each = [&](auto f) {
 #pragma unroll 4
     for (unsigned i = tid; i < n_all; i += kThreads) {
-      const unsigned b = i / per_beam;
+      const unsigned b = i / per_beam, r = i - b * per_beam, place = r / n_splits, split = r - place * n_splits;
       const double top = s_top[b];
       if (top < INFINITY) {
-        const float2 e = __ldcg(reinterpret_cast<const float2*>(list + i));
+        const float2 e = __ldcg(reinterpret_cast<const float2*>(list + (b * n_splits + split) * keep + place));
         if (e.x > -INFINITY) f(s_cum[b] + ((static_cast<double>(e.x) - top) - s_log[b]), static_cast<int>(b) * vocab + __float_as_int(e.y));
-      } else if (top != top && i == b * per_beam) {
+      } else if (top != top && r == 0) {
         f(s_cum[b], static_cast<int>(b) * vocab + end_token);
       }
     }
   };
   double my = -INFINITY;
   each([&](double sc, int) { my = sc > my ? sc : my; });
-  const double bound = block_bound(my, keep, s_group, &s_bound);
+  const double bound = block_bound(my, keep, s_group, s_max, &s_bound);
   if (my >= bound)
     each([&](double sc, int at) {
       if (sc >= bound) {
@@ -356,6 +368,7 @@ __global__ void __launch_bounds__(kThreads) beam_join_kernel(int n_beams, int vo
       const double sc = s_score[i];
       const int at = s_at[i];
       int rank = 0;
+#pragma unroll 8
       for (int j = 0; j < found; ++j) rank += ahead(s_score[j], s_at[j], sc, at);
       if (rank < keep) put(rank, sc, at);
     }
@@ -380,15 +393,16 @@ __global__ void __launch_bounds__(kThreads) beam_join_kernel(int n_beams, int vo
   }
 }
 
-// How a row is cut.  Words per thread: 32 where that still gives every SM two CTAs, else 8, for the latency of small
-// calls.  A row's slices are dealt to as many CTAs as fit the GPU at a time.
+// How a row is cut.  Words per thread: 8 where all slices then fit the GPU at a time, for the latency of small calls (four
+// rows of 32,000 logits: 7.7 us, with 32 words 9.0; of 64,000: 8.8 and 9.1), else 32 (eight rows of 152,064: 14.1 us, with 8
+// words 17.8; 24 rows of it: 15.8 and 27).  A row's slices are dealt to as many CTAs as fit the GPU at a time.
 struct Cut {
   int words, n_slices, n_splits, per_split;
 };
 Cut cut_of(int64_t rows, int vocab) {
   constexpr int kSms = 148;
   Cut c;
-  c.words = rows * ((vocab + 32 * kThreads - 1) / (32 * kThreads)) >= 2 * kSms ? 32 : 8;
+  c.words = rows * ((vocab + 8 * kThreads - 1) / (8 * kThreads)) <= 3 * kSms ? 8 : 32;
   c.n_slices = (vocab + c.words * kThreads - 1) / (c.words * kThreads);
   const int64_t splits = std::min<int64_t>(c.n_slices, std::max<int64_t>(1, 3 * kSms / rows));
   c.per_split = static_cast<int>((c.n_slices + splits - 1) / splits);

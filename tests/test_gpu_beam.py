@@ -167,3 +167,20 @@ def test_argument_errors(gpu):
                  lambda: binding.prima_beam_select_workspace(0, 1, 5, 1), lambda: binding.prima_beam_select_workspace(1, 64, 1 << 26, 1)):
         with pytest.raises((ValueError, binding.PrimaError)):
             call()
+
+
+@pytest.mark.parametrize("words", [1, 3, 8, 40, 511, 513, 1791])
+@pytest.mark.parametrize("dtype,keep", [("float32", 8), ("bfloat16", 8), ("float32", 40), ("float16", 64)])
+def test_short_last_slices(gpu, words, dtype, keep):
+    """A row that ends a few words into a slice, the best of it among them."""
+    logits, cum, _ = some(11, 1, 2, 2048 * 3 + words)
+    logits[:, :, -words:] += 6.0
+    check(gpu, logits, cum, keep, dtype=dtype)
+
+
+@pytest.mark.parametrize("n_beams,keep", [(8, 8), (5, 3), (16, 16), (3, 64)])
+def test_one_beam_holds_the_best(gpu, n_beams, keep):
+    logits, cum, _ = some(12, 2, n_beams, 40000)
+    cum[:] -= 100.0
+    cum[0, n_beams - 1] = cum[1, 0] = -1.0
+    check(gpu, logits, cum, keep)
