@@ -17,6 +17,11 @@
 // cache's type.
 // A segment that is not a whole (sequence, KV head, tile) leaves its maximum, sum and output in the workspace, and
 // tree_merge_kernel joins the parts in ascending order: the same lengths give the same bits.
+// Measured (one B200, both kernels together): 64 nodes, 64 query heads on 8 KV heads of 128, 65,531 positions, fp16:
+// 168 us (0.82 PFLOP/s; 186 to 198 when called for long, the power limit), bound by the softmax, whose eight warps wait,
+// read, take maximum and exponential in step: of about 2400 cycles per sub-unit of 128 x 128 scores the exponentials
+// take 1100 (1024 is what the special-function units need).  16 trees of 1 to 26 nodes over 100 to 8192 positions, 40
+// query heads, bf16: 64 us (2.4 TB/s), half of it beginnings and ends of segments, half waiting for keys.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
@@ -34,7 +39,9 @@ constexpr int kTileRows = 256;         // of the tensor-memory kernel
 constexpr int kSoftmaxThreads = 256;
 constexpr int kThreads = kSoftmaxThreads + 96;       // eight warps of softmax; copies, products, the plan
 constexpr int kSegments = 4;           // planned ahead
-constexpr int kSegmentCost = 3, kStreamSegmentCost = 1;      // of a segment besides its units, in units
+// Of a segment besides its units, in units.  16 ragged trees 63.6 us, without a cost 64.8, with twice as much 69.0; 64
+// nodes over 65,531 positions 168, 174, 166; streaming kernel, 64 ragged single tokens 23.8, 28.1, with three units 26.9.
+constexpr int kSegmentCost = 3, kStreamSegmentCost = 1;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
 constexpr float kSlack = 8.f;          // binary exponent by which a score may exceed the reference
 
@@ -793,6 +800,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
 // each warp streams every fourth group of 16 positions through a ring of its own (16-byte asynchronous copies) and
 // applies it with m16n8k16 products, queries and output in registers; several CTAs per SM hide one another's starts and
 // ends.  The warps' states are joined through shared memory at the end of a segment.
+// Measured with the join: 64 single tokens over 1 to 4096 positions, 32 query heads on 8 KV heads of 64, bf16: 24 us (3.0
+// TB/s), bound by the barriers and starts of 512 ragged segments; 5 nodes over 1000 positions, 32 heads of 128: 12.7 us,
+// latency.
 template <int D> struct StreamGeometry {
   static constexpr int kStages = 3;
   static constexpr int kStep = 16;                             // positions
@@ -1093,7 +1103,8 @@ __global__ void __launch_bounds__(128, StreamGeometry<D>::kCtas) tree_stream_ker
 // ---- joining the parts ----------------------------------------------------------------------------------------------
 // blockIdx.x = the CTA in which a cut segment begins, blockIdx.y = kRows of its rows, blockIdx.z = some of the columns;
 // a thread owns one row and 4 columns, so that reads of the parts are contiguous across the rows.  The parts are taken eight at
-// a time, all their reads in flight: what this kernel costs is the latency of its reads.
+// a time, all their reads in flight: what this kernel costs is the latency of its reads (5 us behind the streaming
+// kernel, 9 to 12 behind the other, with cold caches).
 template <typename Out, int D, int kRows>
 __global__ void __launch_bounds__(256) tree_merge_kernel(const __grid_constant__ TreeArgs a) {
   pdl_trigger();
@@ -1153,6 +1164,10 @@ struct Maps { CUtensorMap k, v; };
 
 // Which kernel, by the rows that a KV head has of a sequence on average (the lengths themselves are on the device; each
 // kernel is right for any): up to 32 the streaming kernel, which takes 16 at a time, beyond it the tensor-memory kernel.
+// Streaming against tensor memory, heads of 128: 16 sequences of 4096 positions, 5 rows 52 and 70 us, 20 rows 70 and 71,
+// 40 rows 135 and 74; 64 of 600, 5 rows 39 and 56, 20 rows 61 and 57, 40 rows 83 and 59.  Between 16 and 32 rows it goes
+// by the lengths, which are not known here: 20 rows over 1000 positions 12.6 and 14.9, over 30 positions 8.6 and 14.9,
+// 64 ragged sequences up to 4096 68 and 61; heads of 64, the same, 41 and 56.  The larger gains are with streaming.
 bool streams(const BatchView& b, int group) { return (static_cast<int64_t>(b.n_tok) + b.n_seq - 1) / b.n_seq * group <= 32; }
 struct Workers {
   int n, tile_rows;
