@@ -20,7 +20,7 @@ namespace {
 // head that it turns, so their sines stay in registers; a warp takes 32 / (D/16) heads at a time, two items in flight.
 // Four items in flight (fewer warps), or 8 and 16 rows per CTA, were slower or no faster; with the index arithmetic of a
 // division per item the kernel was bound by instructions (65 us where it is 61 now).
-// Prompts of 11,268 rows, 40 + 16 heads of 128, bf16, 323 MB: 61 us, 5.3 TB/s, HBM; one row 3.0 us, about 200 rows of
+// Prompts of 11,268 rows, 40 + 16 heads of 128, bf16, 323 MB: 61 us, 5.3 TB/s, HBM; one row 3.0 us, 278 rows of
 // trees 6 us, latency.
 template <typename T, typename In, int D, int kWarps>
 __global__ void __launch_bounds__(256) append_kernel(PoolView pool, BatchView b, int layer, const In* __restrict__ q, const In* __restrict__ k,

@@ -81,8 +81,14 @@ class PagedStepper:
         self.hid = torch.empty((self.max_n_tok, cfg["hidden"]), dtype=torch.float32, device=k_pages.device)
         self.logits = torch.empty((self.max_n_tok, cfg["vocab"]), dtype=torch.float32, device=k_pages.device)
 
+    def on_stream(self):
+        """torch's current stream becomes the context's own, if it has one: the small arrays of a step are then uploaded,
+        and their memory is used again, in the order of the steps that read them."""
+        return self.torch.cuda.stream(self.ctx._stream)
+
     def _gpu(self, a, dtype=np.int32):
-        return self.torch.from_numpy(np.ascontiguousarray(a, dtype=dtype)).to(self.hid.device)
+        with self.on_stream():
+            return self.torch.from_numpy(np.ascontiguousarray(a, dtype=dtype)).to(self.hid.device)
 
     def table_of(self, rows: Sequence[Sequence[int]]):
         width = max(1, max(len(r) for r in rows))
@@ -202,11 +208,20 @@ class BeamDecoder:
 
     def generate(self, prompt: Sequence[int], n_new: int) -> List[Tuple[float, List[int]]]:
         """(sum of log probabilities, tokens) of the beams after n_new steps (fewer where a beam has ended), best first."""
+        rows, fresh = [[]], []
+        try:
+            with self.model.on_stream():
+                return self._generate(prompt, n_new, rows, fresh)
+        finally:      # a full cache too leaves no page behind
+            for pages in (*rows, fresh):
+                for p in pages:
+                    self.model.pages.drop(p)
+
+    def _generate(self, prompt: Sequence[int], n_new: int, rows: List[List[int]], fresh: List[int]):
         m, torch, n = self.model, self.model.torch, self.n_beams
-        dev, stream = m.hid.device, m.ctx._stream
-        first: List[int] = []
-        length = m.prefill(prompt[:-1], first) if len(prompt) > 1 else 0
-        rows = [first] + [[m.pages.share(p) for p in first] for _ in range(n - 1)]
+        dev = m.hid.device
+        length = m.prefill(prompt[:-1], rows[0]) if len(prompt) > 1 else 0
+        rows += [[m.pages.share(p) for p in rows[0]] for _ in range(n - 1)]
         # all beams start as the prompt, but only the first one counts; their last pages become their own as they grow
         lengths, tokens = [length] * n, [[] for _ in range(n)]
         feed = [int(prompt[-1])] * n
@@ -226,13 +241,15 @@ class BeamDecoder:
                 lengths = [x + 1 for x in lengths]
             new_score = torch.empty_like(score)
             m.binding.prima_beam_select(logits.contiguous()[None], score, new_score, parent, token, finished=m._gpu([done], np.uint8) if done.any() else None,
-                                        end_token=self.end_token if done.any() else -1, stream=stream)
-            fresh = [m.pages.take() for _ in range(n)]
+                                        end_token=self.end_token if done.any() else -1)
+            while len(fresh) < n:
+                fresh.append(m.pages.take())
             table = m.table_of(rows)
             out = torch.empty_like(table), torch.empty(n, dtype=torch.int32, device=dev)
-            m.pool.reorder(table, m._gpu(lengths), parent, m._gpu(fresh), *out, stream=stream)
+            m.pool.reorder(table, m._gpu(lengths), parent, m._gpu(fresh), *out)
             parents, words = parent[0].tolist(), token[0].tolist()
-            rows = m.pages.reorder(rows, lengths, parents, fresh)
+            rows[:] = m.pages.reorder(rows, lengths, parents, fresh)
+            fresh.clear()
             lengths = [lengths[p] for p in parents]
             ended = [bool(done[p]) for p in parents]
             tokens = [tokens[p] + ([] if e else [w]) for p, w, e in zip(parents, words, ended)]
@@ -240,7 +257,4 @@ class BeamDecoder:
             feed, score = [max(0, w) for w in words], new_score
             if done.all():
                 break
-        for row in rows:
-            for p in row:
-                m.pages.drop(p)
         return list(zip(score[0].tolist(), tokens))

@@ -210,3 +210,45 @@ def test_first_beams_of_requests(gpu):
     for a, c in zip(*both):
         assert torch.equal(a, c)
     assert torch.equal(both[0][2], torch.topk(logits[:, 0], 5).indices.int())
+
+
+def test_steps_of_a_context_on_its_own_stream(gpu):
+    """A prompt of many steps, queued from torch's default stream while the context's own stream is still busy: the
+    small arrays of a step must not be overwritten by a later one's before it has read them."""
+    torch, binding = gpu
+    from paper_2504_08791_b200.paged import BeamDecoder, PagedStepper
+    cfg = synth.model_config("tiny", max_n_tok=4)
+    prompt = [int(x) for x in np.random.RandomState(5).randint(0, cfg["vocab"], 37)]
+    stream = torch.cuda.Stream()
+    seen = []
+    for own in (None, stream):
+        ctx = binding.Context(cfg, stream=own)
+        for layer, tid, rows, cols, data in synth.iter_model_tensors(48, cfg):
+            ctx.load(layer, tid, data, rows, cols)
+        shape = (cfg["n_layers"], 64, cfg["n_kv_heads"], 8, cfg["head_dim"])
+        k, v = (torch.zeros(shape, dtype=torch.float16, device="cuda") for _ in range(2))
+        torch.cuda.synchronize()
+        m = PagedStepper(ctx, k, v)
+        with torch.cuda.stream(own):
+            torch.cuda._sleep(50_000_000)      # some 25 ms
+        pages = []
+        m.prefill(prompt, pages)
+        torch.cuda.synchronize()
+        m.pool.sync()
+        seen.append([m.logits[:1].clone(), k[:, pages].clone(), v[:, pages].clone(), BeamDecoder(m, 3).generate(prompt, 4)])
+        assert len(m.pages.free) == 64 - len(pages)
+        ctx.close()
+    assert all(torch.equal(a, b) for a, b in zip(seen[0][:3], seen[1][:3])) and seen[0][3] == seen[1][3]
+
+
+def test_a_full_cache_leaves_no_page_behind(gpu):
+    torch, binding = gpu
+    from paper_2504_08791_b200.paged import BeamDecoder
+    cfg = synth.model_config("tiny", max_n_tok=4)
+    ctx = load(gpu, cfg, 49)
+    m = stepper(gpu, ctx, n_pages=9, page=8)
+    prompt = [int(x) for x in np.random.RandomState(6).randint(0, cfg["vocab"], 20)]
+    with pytest.raises(RuntimeError) as e:
+        BeamDecoder(m, 4).generate(prompt, 40)
+    assert "full" in str(e.value) and len(m.pages.free) == 9
+    ctx.close()
