@@ -9,6 +9,7 @@ from tests import _paged
 from tests._paged import Batch
 from tests.test_gpu_paged import batch_on_gpu, cache_on_gpu, gpu, on_gpu  # noqa: F401
 from tests.test_gpu_paged_decoding import load, stepper
+from tests.test_gpu_tree_attention import check as check_attention
 
 pytestmark = pytest.mark.gpu
 
@@ -252,3 +253,20 @@ def test_a_full_cache_leaves_no_page_behind(gpu):
         BeamDecoder(m, 4).generate(prompt, 40)
     assert "full" in str(e.value) and len(m.pages.free) == 9
     ctx.close()
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("page", [8, 1024, 32768])
+@pytest.mark.parametrize("nodes", [3, 45, 260], ids=["few rows", "one tile", "several tiles"])
+def test_attention_over_the_smallest_and_largest_pages(gpu, dim, page, nodes):
+    b = Batch(304, ctx=[0, 301, 127], nodes=[nodes, 2, nodes], page=page, q_heads=2, kv_heads=1, dim=dim, dtype="bfloat16", spare=1)
+    check_attention(gpu, b, b.trees(words=5)[0])
+    check_attention(gpu, b, None)
+
+
+@pytest.mark.parametrize("rows", [1, 40])
+def test_attention_of_thousands_of_sequences(gpu, rows):
+    n = 3000 if rows == 1 else 400
+    rs = np.random.RandomState(8)
+    b = Batch(305, ctx=rs.randint(0, 40, n), nodes=rs.randint(0, rows + 1, n) if rows == 1 else np.full(n, rows), page=8, q_heads=1, kv_heads=1, dim=64, pad=1)
+    check_attention(gpu, b, None)
