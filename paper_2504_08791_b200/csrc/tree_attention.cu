@@ -21,7 +21,7 @@
 // 168 us (0.82 PFLOP/s; 186 to 198 when called for long, the power limit), bound by the softmax, whose eight warps wait,
 // read, take maximum and exponential in step: of about 2400 cycles per sub-unit of 128 x 128 scores the exponentials
 // take 1100 (1024 is what the special-function units need).  16 trees of 1 to 26 nodes over 100 to 8192 positions, 40
-// query heads, bf16: 64 us (2.4 TB/s), half of it beginnings and ends of segments, half waiting for keys.
+// query heads, bf16: 62 us (2.5 TB/s), half of it beginnings and ends of segments, half waiting for keys.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
@@ -1102,59 +1102,64 @@ __global__ void __launch_bounds__(128, StreamGeometry<D>::kCtas) tree_stream_ker
 
 // ---- joining the parts ----------------------------------------------------------------------------------------------
 // blockIdx.x = the CTA in which a cut segment begins, blockIdx.y = kRows of its rows, blockIdx.z = some of the columns;
-// a thread owns one row and 4 columns, so that reads of the parts are contiguous across the rows.  The parts are taken eight at
+// a thread owns one row and 4 columns at a time, so that reads of the parts are contiguous across the rows.  The parts are taken eight at
 // a time, all their reads in flight: what this kernel costs is the latency of its reads (5 us behind the streaming
-// kernel, 9 to 12 behind the other, with cold caches).
-template <typename Out, int D, int kRows>
+// kernel, 9 to 12 behind the other, with cold caches).  A thread takes kTurns such places: many CTAs find nothing to do,
+// and fewer of them end sooner (heads of 128, 16 ragged trees: 63.6, 62.4 and 63.1 us in all with 1, 2 and 4 turns).
+template <typename Out, int D, int kRows, int kTurns>
 __global__ void __launch_bounds__(256) tree_merge_kernel(const __grid_constant__ TreeArgs a) {
   pdl_trigger();
   pdl_wait();
   const TailNote note = a.notes[blockIdx.x];
   const int tile_rows = a.shape.tile_rows;
-  const int row = blockIdx.y * kRows + threadIdx.x % kRows, quad = blockIdx.z * (256 / kRows) + threadIdx.x / kRows;
+  const int row = blockIdx.y * kRows + threadIdx.x % kRows;
   if (row >= note.rows) return;
   const int parts = note.last_cta - static_cast<int>(blockIdx.x) + 1;
-  float m = -INFINITY, total = 0.f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int c0 = 0; c0 < parts; c0 += 8) {
-    float2 ml[8];
-    float4 x[8];
+#pragma unroll 1
+  for (int turn = 0; turn < kTurns; ++turn) {
+    const int quad = (blockIdx.z * kTurns + turn) * (256 / kRows) + threadIdx.x / kRows;
+    float m = -INFINITY, total = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int c0 = 0; c0 < parts; c0 += 8) {
+      float2 ml[8];
+      float4 x[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      ml[j] = make_float2(-INFINITY, 0.f);
-      x[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (c0 + j < parts) {
-        const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x + c0 + j) + (c0 + j == 0);
-        ml[j] = __ldcg(&a.part_ml[slot * tile_rows + row]);
-        x[j] = __ldcg(reinterpret_cast<const float4*>(a.part_o) + (slot * (D / 4) + quad) * tile_rows + row);
+      for (int j = 0; j < 8; ++j) {
+        ml[j] = make_float2(-INFINITY, 0.f);
+        x[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (c0 + j < parts) {
+          const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x + c0 + j) + (c0 + j == 0);
+          ml[j] = __ldcg(&a.part_ml[slot * tile_rows + row]);
+          x[j] = __ldcg(reinterpret_cast<const float4*>(a.part_o) + (slot * (D / 4) + quad) * tile_rows + row);
+        }
+      }
+      float top = m;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) top = fmaxf(top, ml[j].x);
+      const float f = m == -INFINITY ? 0.f : ex2(m - top);
+      m = top;
+      total *= f;
+      o.x *= f;
+      o.y *= f;
+      o.z *= f;
+      o.w *= f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float g = ml[j].x == -INFINITY ? 0.f : ex2(ml[j].x - m);
+        total += ml[j].y * g;
+        o.x += x[j].x * g;
+        o.y += x[j].y * g;
+        o.z += x[j].z * g;
+        o.w += x[j].w * g;
       }
     }
-    float top = m;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) top = fmaxf(top, ml[j].x);
-    const float f = m == -INFINITY ? 0.f : ex2(m - top);
-    m = top;
-    total *= f;
-    o.x *= f;
-    o.y *= f;
-    o.z *= f;
-    o.w *= f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float g = ml[j].x == -INFINITY ? 0.f : ex2(ml[j].x - m);
-      total += ml[j].y * g;
-      o.x += x[j].x * g;
-      o.y += x[j].y * g;
-      o.z += x[j].z * g;
-      o.w += x[j].w * g;
-    }
+    const float inv = total > 0.f ? 1.f / total : 0.f;
+    const int gr = note.row0 + row, group = a.shape.group;
+    const int64_t out_row = static_cast<int64_t>(note.first + gr / group) * a.n_q_heads + note.head * group + gr % group;
+    Out* dst = static_cast<Out*>(a.out) + out_row * D + 4 * quad;
+    store4(dst, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+    if (a.lse && quad == 0) a.lse[out_row] = total > 0.f ? (m + log2f(total)) * kLn2 : -INFINITY;
   }
-  const float inv = total > 0.f ? 1.f / total : 0.f;
-  const int gr = note.row0 + row, group = a.shape.group;
-  const int64_t out_row = static_cast<int64_t>(note.first + gr / group) * a.n_q_heads + note.head * group + gr % group;
-  Out* dst = static_cast<Out*>(a.out) + out_row * D + 4 * quad;
-  store4(dst, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
-  if (a.lse && quad == 0) a.lse[out_row] = total > 0.f ? (m + log2f(total)) * kLn2 : -INFINITY;
 }
 
 constexpr int64_t kAlign = 256;
@@ -1194,7 +1199,7 @@ cudaError_t launch_stream(const TreeArgs& a, int n_cta, cudaStream_t st) {
   if (e == cudaSuccess) e = launch_pdl(kernel, dim3(n_cta), dim3(128), Geo::kBytes, st, a);
   if (e != cudaSuccess) return e;
   constexpr int kRows = 16;
-  return launch_pdl(tree_merge_kernel<Out, D, kRows>, dim3(n_cta, 1, D / 4 * kRows / 256), dim3(256), 0, st, a);
+  return launch_pdl(tree_merge_kernel<Out, D, kRows, 1>, dim3(n_cta, 1, D / 4 * kRows / 256), dim3(256), 0, st, a);
 }
 
 template <typename T, typename Out, int D>
@@ -1209,7 +1214,8 @@ cudaError_t launch_tree(const prima_paged& pool, TreeArgs a, int n_cta, cudaStre
   const Maps* maps = static_cast<const Maps*>(pool.maps);
   if (e == cudaSuccess) e = launch_pdl(kernel, dim3(n_cta), dim3(kThreads), kSmem, st, maps->k, maps->v, a);
   if (e != cudaSuccess) return e;
-  return launch_pdl(tree_merge_kernel<Out, D, 32>, dim3(n_cta, kTileRows / 32, D / 32), dim3(256), 0, st, a);
+  constexpr int kTurns = 2;
+  return launch_pdl(tree_merge_kernel<Out, D, 32, kTurns>, dim3(n_cta, kTileRows / 32, D / 32 / kTurns), dim3(256), 0, st, a);
 }
 
 }  // namespace
