@@ -506,8 +506,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
         const bool first = i < halves, last = halves == 1 || h == 1;
         if (halves == 1 || !h) ok = wait_for(bar_full + 8 * pv.slot, pv.phase, give_up, status) && ok;
         if (i + 2 < count) wait_keys(i + 2);
-        // O += P V, each half of the positions when its P is there; the first product of a segment overwrites O, which
-        // all warps must have read (their P says so)
+        // O += P V, each half of the positions when its P is there (warps that rescale O report no P before all of a row's
+        // columns are scaled); the first product of a segment overwrites O, which all warps must have read (their P says so)
         const SmemOperand vv = v_all + pv.slot * Geo::kSlotBytes;
         if (first) ok = wait_for(bar_p + 16 * buffer + 8, phase, give_up, status) && ok;
 #pragma unroll
@@ -676,6 +676,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
               for (int j = 0; j < 16; ++j) y[j] = __float_as_uint(__uint_as_float(y[j]) * f);
               tmem_store(at, y);
             }
+            // The next product adds to all columns and may be issued when one of the two warps has reported its P: neither
+            // reports before both have scaled their half.
+            tmem_wait_store();
+            tc_fence_before();
+            pair_sync();
           }
           const float2 scale = make_float2(a.scale_log2, a.scale_log2), shift = m == -INFINITY ? make_float2(0.f, 0.f) : make_float2(-m, -m);
           uint32_t packed[32];

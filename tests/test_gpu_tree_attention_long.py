@@ -1,0 +1,131 @@
+"""Tree attention where a CTA takes several consecutive units of a segment: references that move while the output is being
+summed, in both kernels and for tiles of one and of two accumulators, against softmax in 64 bits."""
+import numpy as np
+import pytest
+
+from tests import _paged
+from tests._paged import Batch
+from tests.test_gpu_paged import batch_on_gpu, cache_on_gpu, gpu, on_gpu  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+# nodes of a sequence (with 4 query heads per KV head) and positions: the streaming kernel; one accumulator; two; three
+# tiles of 256, 256 and 88 rows
+KINDS = {"stream": (3, 9000), "one": (12, 24000), "two": (45, 24000), "tiles": (150, 8000)}
+
+
+def units_of_a_cta(torch, b, mask):
+    """Of the tensor-memory kernel, on average: every (sequence, KV head, tile of 256 rows) has a cost of 3 besides."""
+    group, places, units = b.q_heads // b.kv_heads, 0, 0
+    for c, n in zip(b.ctx, b.nodes):
+        for rt in range(-(-int(n) * group // 256)):
+            end = int(c) + (int(n) if mask is not None else min(int(n), -(-(rt + 1) * 256 // group)))
+            units += b.kv_heads * -(-end // 128)
+            places += b.kv_heads * (-(-end // 128) + 3)
+    return units / torch.cuda.get_device_properties(0).multi_processor_count
+
+
+def attention(torch, b, q, mask, scale, seen=None):
+    """_paged.attention (the same bounds, all rows of a KV head at a time) on the GPU in 64 bits.  seen: [rows][slots] of every
+    sequence instead of what the batch says."""
+    group, u = b.q_heads // b.kv_heads, _paged.HALF_STEP[b.dtype]
+    out, bound = np.full((2, b.n_tok, b.q_heads, b.dim), np.nan)
+    lse, lse_bound = np.full((2, b.n_tok, b.q_heads), np.nan)
+    for s in range(len(b.ctx)):
+        r0, r1, n = int(b.row_begin[s]), int(b.row_begin[s + 1]), int(b.ctx[s] + b.nodes[s])
+        if r1 == r0:
+            continue
+        k, v = (on_gpu(torch, np.ascontiguousarray(b.entries(a, s, 0, n))).double() for a in (b.k, b.v))
+        see = on_gpu(torch, b.sees(s, mask) if seen is None else seen[s])
+        k, v = (torch.where(see.any(0)[:, None, None], a, 0.0) for a in (k, v))      # what no row sees may be anything
+        for g in range(b.kv_heads):
+            rows = on_gpu(torch, q[r0:r1, g * group:(g + 1) * group]).double()
+            for i0 in range(0, r1 - r0, 16):
+                part = rows[i0:i0 + 16].reshape(-1, b.dim)
+                look = see[i0:i0 + 16].repeat_interleave(group, 0)
+                x = torch.where(look, scale * (part @ k[:, g].T), -torch.inf)
+                top = x.amax(1, keepdim=True).clamp_min(-1e300)
+                p = torch.exp(x - top)
+                total = p.sum(1, keepdim=True)
+                share = p / torch.where(total > 0, total, 1.0)
+                count = look.sum(1, keepdim=True)
+                d_score = (b.dim + 4) * 2.0 ** -24 * scale * torch.where(look, part.abs() @ k[:, g].abs().T, 0.0).amax(1, keepdim=True) + \
+                    torch.where(look, x.abs(), 0.0).amax(1, keepdim=True) * 2.0 ** -22
+                rel = u + 2 * d_score + 2.0 ** -20 + count * 2.0 ** -24
+                o = share @ v[:, g]
+                z = torch.where(total > 0, top + torch.log(total), -torch.inf)
+                at = (slice(r0 + i0, min(r0 + i0 + 16, r1)), slice(g * group, (g + 1) * group))
+                shape = (at[0].stop - at[0].start, group)
+                out[at] = o.view(*shape, b.dim).cpu().numpy()
+                bound[at] = ((share @ v[:, g].abs()) * rel + o.abs() * rel).view(*shape, b.dim).cpu().numpy()
+                lse[at] = z.view(shape).cpu().numpy()
+                lse_bound[at] = (2 * d_score + 2.0 ** -20 + count * 2.0 ** -24 + z.abs() * 2.0 ** -22).view(shape).cpu().numpy()
+    return out, lse, bound, lse_bound
+
+
+def compare(b, got, want, final=None):
+    out, lse = got
+    ref, ref_lse, tol, lse_tol = want
+    n, final = b.live, _paged.HALF_STEP[b.dtype] if final is None else final
+    limit = tol[:n] * (1 + final) + np.abs(ref[:n]) * final + 2.0 ** -25
+    diff = np.abs(out[:n] - ref[:n])
+    assert np.all(diff <= limit), f"worst {np.nanmax(diff / limit):.2f} of the bound"
+    empty = np.isneginf(ref_lse[:n])
+    assert np.array_equal(np.isneginf(lse[:n]), empty) and np.all(out[:n][empty] == 0)
+    assert np.all(np.abs(lse[:n][~empty] - ref_lse[:n][~empty]) <= lse_tol[:n][~empty])
+    assert np.all(out[n:] == 7.0) and np.all(lse[n:] == 7.0)
+
+
+def run(gpu, b, mask, q, pool_kv=None, times=1):
+    """Output and log-sum-exp; of several runs, all with the same bits."""
+    torch, _ = gpu
+    k, v, pool = pool_kv or cache_on_gpu(gpu, b)
+    batch, dq = batch_on_gpu(gpu, b, mask=mask), on_gpu(torch, q).to(k.dtype)
+    first = None
+    for _ in range(times):
+        out = torch.full(q.shape, 7.0, dtype=k.dtype, device="cuda")
+        z = torch.full(q.shape[:2], 7.0, dtype=torch.float32, device="cuda")
+        pool.tree_attention(0, batch, dq, out, lse=z)
+        if first is None:
+            first = out, z
+        assert torch.equal(out, first[0]) and torch.equal(z, first[1])
+    pool.sync()
+    return first[0].float().cpu().numpy(), first[1].cpu().numpy()
+
+
+def peaks(b, slope):
+    """Keys and queries whose scores are tents over the positions: `slope` binary exponents per 128 positions up to a peak,
+    and down again behind it, at another place for every row.  Half of the rows of a warp rise while the others have their mass
+    already; every eighth sees all positions alike."""
+    dim, n = b.dim, int(b.ctx.max() + b.nodes.max())
+    width = 5 * 128
+    height = 5 * slope * np.log(2.0)
+    j = np.arange(n)
+    centre = (np.arange(dim) + 0.5) * n / dim
+    tent = np.maximum(0.0, 1 - np.abs(j[:, None] - centre) / width) * (height / (4 * dim ** -0.5))
+    for s in range(len(b.ctx)):
+        for i in range(int(b.ctx[s] + b.nodes[s])):
+            page, row = b.place(s, i)
+            b.k[:, page, :, row] = _paged.rounded((0.05 * b.k[:, page, :, row] + tent[i]).astype(np.float32), b.dtype)
+    q = 0.05 * b.rs.standard_normal((b.n_tok, b.q_heads, dim)).astype(np.float32)
+    for t in range(b.n_tok):
+        for h in range(b.q_heads):
+            x = t * b.q_heads + h
+            if x % 8:
+                q[t, h, x * 29 % dim] += 4
+    return _paged.rounded(q, b.dtype)
+
+
+@pytest.mark.parametrize("dim,dtype", [(128, "float16"), (64, "bfloat16")])
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("tree", [True, False])
+def test_references_that_move_in_every_unit(gpu, kind, dim, dtype, tree):
+    torch, _ = gpu
+    nodes, ctx = KINDS[kind]
+    b = Batch(200 + dim, ctx=[ctx], nodes=[nodes], page=64, q_heads=16, kv_heads=4, dim=dim, dtype=dtype, pad=1)
+    q = peaks(b, 12.0)
+    mask = b.trees(3)[0] if tree else None
+    if kind != "stream":
+        assert units_of_a_cta(torch, b, mask) >= 3
+    want = attention(torch, b, q, mask, dim ** -0.5)
+    compare(b, run(gpu, b, mask, q, times=30), want)
