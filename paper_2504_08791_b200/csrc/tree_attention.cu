@@ -743,6 +743,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
           ctl->top[h][w][r] = total;
           pair_sync();
           total += ctl->top[h][w ^ 1][r];
+          pair_sync();      // read before the next segment's maxima take its place
           const float f = s.kind == 0 ? (total > 0.f ? 1.f / total : 0.f) : 1.f;
           const bool mine = in_tile < s.rows;
           const int64_t at = mine ? place_of(s, t0, rem0, in_tile) : 0;

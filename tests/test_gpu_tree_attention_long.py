@@ -129,3 +129,17 @@ def test_references_that_move_in_every_unit(gpu, kind, dim, dtype, tree):
         assert units_of_a_cta(torch, b, mask) >= 3
     want = attention(torch, b, q, mask, dim ** -0.5)
     compare(b, run(gpu, b, mask, q, times=30), want)
+
+
+@pytest.mark.parametrize("nodes", [10, 33])
+def test_segments_that_follow_one_another(gpu, nodes):
+    """Many segments of one unit per CTA: what the two warps of a row exchange at the end of one segment and at the beginning
+    of the next lies in the same place.  Keys are large and sums small (one position has all of the weight), so that a maximum in
+    the place of a sum shows."""
+    torch, _ = gpu
+    n = 300
+    b = Batch(210, ctx=np.random.RandomState(1).randint(20, 128 - nodes, n), nodes=[nodes] * n, page=16, q_heads=16, kv_heads=4, dim=64)
+    q = _paged.rounded(b.rs.standard_normal((b.n_tok, 16, 64)).astype(np.float32) * 8, b.dtype)
+    mask, _ = b.trees()
+    assert units_of_a_cta(torch, b, mask) >= 8
+    compare(b, run(gpu, b, mask, q, times=30), attention(torch, b, q, mask, 0.125))
