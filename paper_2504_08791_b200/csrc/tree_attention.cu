@@ -62,7 +62,7 @@ struct Segment {
 };
 
 struct Control {
-  unsigned long long full[12], empty[12], s_ready[2], p_ready[4], pv_done[2], q_ready, seg_done, drained;      // of each buffer; p_ready: and half
+  unsigned long long full[12], empty[12], s_ready[2], p_ready[4], pv_done[2], q_ready, q_first, seg_done, drained;      // of each buffer; p_ready: and half; q_first: the first segment's queries
   unsigned long long seg_full[kSegments], seg_empty[kSegments];
   Segment seg[kSegments];              // n = 0: no more
   uint32_t tmem;
@@ -347,7 +347,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
   Control* ctl = reinterpret_cast<Control*>(s_ring + kSlots * Geo::kSlotBytes);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t bar_full = smem_u32(ctl->full), bar_empty = smem_u32(ctl->empty), bar_s = smem_u32(ctl->s_ready), bar_p = smem_u32(ctl->p_ready),
-                 bar_pv = smem_u32(ctl->pv_done), bar_seg = smem_u32(ctl->seg_full), bar_seg_empty = smem_u32(ctl->seg_empty), bar_q = smem_u32(&ctl->q_ready),
+                 bar_pv = smem_u32(ctl->pv_done), bar_seg = smem_u32(ctl->seg_full), bar_seg_empty = smem_u32(ctl->seg_empty), bar_q = smem_u32(&ctl->q_ready), bar_first = smem_u32(&ctl->q_first),
                  bar_done = smem_u32(&ctl->seg_done), bar_drain = smem_u32(&ctl->drained);
   int* const give_up = &ctl->give_up;
   int* const status = a.pool.status;
@@ -369,6 +369,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
       mbar_init(bar_seg_empty + 8 * i, 10);
     }
     mbar_init(bar_q, 8);
+    mbar_init(bar_first, 8);
     mbar_init(bar_done, 8);
     mbar_init(bar_drain, 1);
     ctl->give_up = 0;
@@ -456,8 +457,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
             if (row >= 0) tma_load_2d(dst + ring.slot * Geo::kSlotBytes, is_v ? &v_map : &k_map, panel * 64, static_cast<int>(row), bar_full + 8 * ring.slot);
           }
           // Queries before the rest of the first places: the first scores need them and one unit's keys, not what
-          // else fills the ring (measured: queries behind 160 KB of keys and values arrive 8 us late).
-          if (!started) wait_for(bar_q, 0, give_up, status);
+          // else fills the ring (measured: queries behind 160 KB of keys and values arrive 8 us late).  A barrier of their
+          // own: the next segment's queries may be ready before this warp looks, and bar_q a phase further.
+          if (!started) wait_for(bar_first, 0, give_up, status);
           started = true;
           ring.step(1);
           if (copies_before < kSlots) ++copies_before;
@@ -588,6 +590,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
         wait_before();
         load_queries(s, si & 1);
         queries_ready();
+        if (si == 0 && lane == 0) mbar_arrive(bar_first);
       }
       // A tile of at most 128 rows leaves room for the next one's queries, where the segment before had its own.
       bool next_loads = false;

@@ -143,3 +143,15 @@ def test_segments_that_follow_one_another(gpu, nodes):
     mask, _ = b.trees()
     assert units_of_a_cta(torch, b, mask) >= 8
     compare(b, run(gpu, b, mask, q, times=30), attention(torch, b, q, mask, 0.125))
+
+
+@pytest.mark.parametrize("nodes,dim", [(10, 64), (10, 128), (40, 128)])
+def test_first_segments_of_one_unit(gpu, nodes, dim):
+    """A CTA's first segment has one unit and the next one's queries are ready at once: the copies do not wait for a state
+    that has passed."""
+    torch, _ = gpu
+    n = 370
+    b = Batch(220, ctx=[100 - nodes] * n, nodes=[nodes] * n, page=128, q_heads=8, kv_heads=2, dim=dim, dtype="bfloat16")
+    q = _paged.rounded(b.rs.standard_normal((b.n_tok, 8, dim)).astype(np.float32), b.dtype)
+    mask, _ = b.trees()
+    compare(b, run(gpu, b, mask, q, times=50), attention(torch, b, q, mask, dim ** -0.5))
