@@ -59,6 +59,8 @@ struct Segment {
   int kind;                            // 0: whole; 1: continues; 2: begins here and goes on
   long long limit;                     // positions that the tile may see
   __device__ __forceinline__ int halves() const { return rows > 128 ? 2 : 1; }      // accumulators of 128 rows
+  // Positions that all rows see: the context, as far as the table names pages for it.
+  __device__ __forceinline__ long long all_see() const { return min(static_cast<long long>(ctx), limit); }
 };
 
 struct Control {
@@ -618,7 +620,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
         const long long pos0 = static_cast<long long>(s.chunk0 + t) * kTilePos + 64 * w;
         // At the edge: what this thread's row sees, and which of the warp's 32 positions any row sees.  Worked out
         // before the scores are there; again in the rare case that the unit turns out to have a bad page.
-        bool edge = pos0 + 64 > s.ctx, waited = false, bad = false;
+        bool edge = pos0 + 64 > s.all_see(), waited = false, bad = false;
         uint32_t seen[2], seen_any = 0xffffffffu;
         for (;;) {
           if (edge) {
@@ -992,7 +994,7 @@ __global__ void __launch_bounds__(128, StreamGeometry<D>::kCtas) tree_stream_ker
       }
       const long long pos0 = pos_first + step * Geo::kStep;
       const bool bad = bad_stages >> stage & 1;
-      if (pos0 + Geo::kStep > s.ctx || bad) {      // positions that the row does not see, or on a bad page
+      if (pos0 + Geo::kStep > s.all_see() || bad) {      // positions that the row does not see, or on a bad page
         const SegmentView view{a.b, a.pool, s.first, s.nodes, s.ctx, s.limit, table, bad};
 #pragma unroll
         for (int m = 0; m < M; ++m)

@@ -76,9 +76,9 @@ def compare(b, got, want, final=None):
     assert np.all(out[n:] == 7.0) and np.all(lse[n:] == 7.0)
 
 
-def run(gpu, b, mask, q, pool_kv=None, times=1):
-    """Output and log-sum-exp; of several runs, all with the same bits."""
-    torch, _ = gpu
+def run(gpu, b, mask, q, pool_kv=None, times=1, status=None):
+    """Output and log-sum-exp; of several runs, all with the same bits.  status: what the pool has to report."""
+    torch, binding = gpu
     k, v, pool = pool_kv or cache_on_gpu(gpu, b)
     batch, dq = batch_on_gpu(gpu, b, mask=mask), on_gpu(torch, q).to(k.dtype)
     first = None
@@ -88,8 +88,13 @@ def run(gpu, b, mask, q, pool_kv=None, times=1):
         pool.tree_attention(0, batch, dq, out, lse=z)
         if first is None:
             first = out, z
-        assert torch.equal(out, first[0]) and torch.equal(z, first[1])
-    pool.sync()
+        assert torch.equal(out.view(torch.int16), first[0].view(torch.int16)) and torch.equal(z.view(torch.int32), first[1].view(torch.int32))
+    if status:
+        with pytest.raises(binding.PrimaError) as e:
+            pool.sync()
+        assert e.value.code == binding.ERR_DEVICE and status in str(e.value)
+    else:
+        pool.sync()
     return first[0].float().cpu().numpy(), first[1].cpu().numpy()
 
 
@@ -155,3 +160,20 @@ def test_first_segments_of_one_unit(gpu, nodes, dim):
     q = _paged.rounded(b.rs.standard_normal((b.n_tok, 8, dim)).astype(np.float32), b.dtype)
     mask, _ = b.trees()
     compare(b, run(gpu, b, mask, q, times=50), attention(torch, b, q, mask, dim ** -0.5))
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("tree", [True, False])
+@pytest.mark.parametrize("nodes,page,pages,ctx", [(2, 8, 3, 25), (3, 8, 19, 1000), (12, 16, 10, 1000), (45, 16, 5, 100), (45, 16, 10, 150)])
+def test_positions_beyond_the_table_are_not_seen(gpu, nodes, page, pages, ctx, tree, dim):
+    """A sequence longer than its row of the table can name: its rows see what the table names, and the status says so."""
+    torch, binding = gpu
+    capacity = page * pages
+    b = Batch(230, ctx=[ctx, capacity - nodes], nodes=[nodes, nodes], page=page, q_heads=8, kv_heads=2, dim=dim)
+    mask = b.trees()[0] if tree else None
+    seen = [b.sees(s, mask) for s in range(2)]
+    seen[0][:, capacity:] = False
+    q = _paged.rounded(b.rs.standard_normal((b.n_tok, 8, dim)).astype(np.float32), b.dtype)
+    want = attention(torch, b, q, mask, dim ** -0.5, seen)
+    b.table = np.ascontiguousarray(b.table[:, :pages])
+    compare(b, run(gpu, b, mask, q, status="slot"), want)
