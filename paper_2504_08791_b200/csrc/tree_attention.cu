@@ -260,6 +260,10 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
+// A row that sees nothing has a sum of 0: its output is 0, its log-sum-exp -infinity.  A NaN stays one.
+__device__ __forceinline__ float inverse_of(float total) { return total == 0.f ? 0.f : 1.f / total; }
+__device__ __forceinline__ float log_sum(float reference, float total) { return total == 0.f ? -INFINITY : (reference + log2f(total)) * kLn2; }
+
 // Two 32-bit operations in one instruction.
 __device__ __forceinline__ float2 fma2(float2 x, float2 y, float2 z) {
   unsigned long long d;
@@ -749,7 +753,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
           pair_sync();
           total += ctl->top[h][w ^ 1][r];
           pair_sync();      // read before the next segment's maxima take its place
-          const float f = s.kind == 0 ? (total > 0.f ? 1.f / total : 0.f) : 1.f;
+          const float f = s.kind == 0 ? inverse_of(total) : 1.f;
           const bool mine = in_tile < s.rows;
           const int64_t at = mine ? place_of(s, t0, rem0, in_tile) : 0;
           const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) + (s.kind == 2);
@@ -774,7 +778,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
           }
           if (mine && w == 0) {
             if (s.kind != 0) a.part_ml[slot * kTileRows + in_tile] = make_float2(m, total);
-            else if (a.lse) a.lse[at] = total > 0.f ? (m + log2f(total)) * kLn2 : -INFINITY;
+            else if (a.lse) a.lse[at] = log_sum(m, total);
           }
         }
         m = m_other;
@@ -1097,10 +1101,10 @@ __global__ void __launch_bounds__(128, StreamGeometry<D>::kCtas) tree_stream_ker
         y.w += v.w * f;
       }
       if (s.kind == 0) {
-        const float inv = total > 0.f ? 1.f / total : 0.f;
+        const float inv = inverse_of(total);
         const int64_t at = place_of(x);
         store4(static_cast<Out*>(a.out) + at * D + 4 * quad, make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv));
-        if (a.lse && quad == 0) a.lse[at] = total > 0.f ? (top + log2f(total)) * kLn2 : -INFINITY;
+        if (a.lse && quad == 0) a.lse[at] = log_sum(top, total);
       } else {
         reinterpret_cast<float4*>(a.part_o)[(slot * (D / 4) + quad) * kRows + x] = y;
         if (quad == 0) a.part_ml[slot * kRows + x] = make_float2(top, total);
@@ -1164,12 +1168,12 @@ __global__ void __launch_bounds__(256) tree_merge_kernel(const __grid_constant__
         o.w += x[j].w * g;
       }
     }
-    const float inv = total > 0.f ? 1.f / total : 0.f;
+    const float inv = inverse_of(total);
     const int gr = note.row0 + row, group = a.shape.group;
     const int64_t out_row = static_cast<int64_t>(note.first + gr / group) * a.n_q_heads + note.head * group + gr % group;
     Out* dst = static_cast<Out*>(a.out) + out_row * D + 4 * quad;
     store4(dst, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
-    if (a.lse && quad == 0) a.lse[out_row] = total > 0.f ? (m + log2f(total)) * kLn2 : -INFINITY;
+    if (a.lse && quad == 0) a.lse[out_row] = log_sum(m, total);
   }
 }
 

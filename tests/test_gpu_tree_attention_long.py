@@ -177,3 +177,24 @@ def test_positions_beyond_the_table_are_not_seen(gpu, nodes, page, pages, ctx, t
     want = attention(torch, b, q, mask, dim ** -0.5, seen)
     b.table = np.ascontiguousarray(b.table[:, :pages])
     compare(b, run(gpu, b, mask, q, status="slot"), want)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_a_row_without_a_number_has_no_sum(gpu, kind):
+    """NaN in a query: output and log-sum-exp of that row are NaN, not those of a row that sees nothing; other rows do not
+    notice."""
+    torch, _ = gpu
+    nodes, ctx = KINDS[kind]
+    for c in (ctx, 70):
+        b = Batch(240, ctx=[c, 5], nodes=[nodes, nodes], page=64, q_heads=4, kv_heads=1, dim=64)
+        mask, _ = b.trees(3)
+        q = _paged.rounded(b.rs.standard_normal((b.n_tok, 4, 64)).astype(np.float32), b.dtype)
+        want = attention(torch, b, q, mask, 0.125)
+        bad = [(0, 1), (nodes - 1, 3), (nodes, 0)]
+        for t, h in bad:
+            q[t, h, 17] = np.nan
+        out, lse = run(gpu, b, mask, q)
+        for t, h in bad:
+            assert np.all(np.isnan(out[t, h])) and np.isnan(lse[t, h])
+            out[t, h], lse[t, h] = want[0][t, h], want[1][t, h]
+        compare(b, (out, lse), want)
