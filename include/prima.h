@@ -347,9 +347,9 @@ const char* prima_gemv_q4k_noalloc_error(void);
  * them.  row_begin must ascend from 0 to at most n_tok.
  *
  * What the kernels find in device memory cannot be checked when a call is made.  A page id outside 0..n_pages-1, a
- * slot beyond the table, a decreasing row_begin or a path entry outside the step never leads to an access outside the
- * arrays: the kernel skips the entry (attention: treats the position as not visible) and raises a bit of the pool's
- * status word, which prima_paged_sync reports.
+ * slot beyond the table, a decreasing row_begin, a path entry outside the step or not above the one before it never
+ * leads to an access outside the arrays: the kernel skips the entry (attention: treats the position as not visible)
+ * and raises a bit of the pool's status word, which prima_paged_sync reports.
  *
  * All calls queue their kernels on `stream` and return; none allocates, waits or keeps anything of a call for the
  * next (prima_forward_window_paged: below).  Calls on different streams are independent as far as their arrays and

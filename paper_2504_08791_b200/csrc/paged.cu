@@ -124,7 +124,8 @@ __global__ void __launch_bounds__(256) append_kernel(PoolView pool, BatchView b,
 // Rows path[0..n-1] of a sequence's step move to rows 0..n-1, in every layer.  blockIdx.x = the sequence; its CTAs look
 // the rows' places up once and share the columns: a column is 16 bytes of one head of keys or values of one layer, and
 // a thread moves it for all rows, in ascending order.  path ascends, so path[j] >= j: what is read for row j is
-// overwritten at the earliest for row path[j], and a batch that is read whole before any of it is written keeps that.
+// overwritten at the earliest for row path[j], and a batch that is read whole before any of it is written keeps that.  An
+// entry that is not above the one before it is reported and stays where it is.
 // Bound by scattered reads of 256 bytes in flight: 32 paths of 1 to 12 rows, 80 layers, 83 MB: 13.6 us (part of it from
 // L2; 17 when other data went through it); one path of 4 rows, 32 layers: 2.9 us.
 constexpr int kPathBatch = 8, kPathBlock = 256;
@@ -151,7 +152,7 @@ __global__ void __launch_bounds__(256) accept_kernel(PoolView pool, BatchView b,
     if (static_cast<int>(threadIdx.x) < m) {
       const int j = j0 + threadIdx.x, a = __ldg(path + static_cast<int64_t>(s) * path_stride + j);
       int2 pages = make_int2(-1, 0), rows = make_int2(0, 0);
-      if (a < 0 || a >= end - first) {
+      if (a < 0 || a >= end - first || (j > 0 && a <= __ldg(path + static_cast<int64_t>(s) * path_stride + j - 1))) {
         raise(pool.status, kBadPath);
       } else if (a != j) {
         const int64_t from = static_cast<int64_t>(ctx) + a, to = static_cast<int64_t>(ctx) + j;

@@ -270,3 +270,21 @@ def test_attention_of_thousands_of_sequences(gpu, rows):
     rs = np.random.RandomState(8)
     b = Batch(305, ctx=rs.randint(0, 40, n), nodes=rs.randint(0, rows + 1, n) if rows == 1 else np.full(n, rows), page=8, q_heads=1, kv_heads=1, dim=64, pad=1)
     check_attention(gpu, b, None)
+
+
+def test_accept_reports_paths_that_do_not_ascend(gpu):
+    torch, binding = gpu
+    b = Batch(13, ctx=[3, 3], nodes=[6, 6], page=8, dim=64)
+    for path, moved in (([2, 1, 4], {0: 2, 2: 4}), ([1, 1, 3], {0: 1, 2: 3}), ([0, 3, 2], {1: 3})):
+        k, v, pool = cache_on_gpu(gpu, b)
+        pool.accept(batch_on_gpu(gpu, b), on_gpu(torch, np.array([path, [1, 2, 5]], np.int32)), on_gpu(torch, np.array([3, 3], np.int32)))
+        with pytest.raises(binding.PrimaError) as e:
+            pool.sync()
+        assert "path" in str(e.value)
+        for got, old in ((k, b.k), (v, b.v)):
+            want = old.copy()
+            for s, moves in ((0, moved), (1, {0: 1, 1: 2, 2: 5})):
+                for j, a in moves.items():
+                    (pf, rf), (pt, rt) = b.place(s, 3 + a), b.place(s, 3 + j)
+                    want[:, pt, :, rt] = old[:, pf, :, rf]
+            assert np.array_equal(got.float().cpu().numpy(), want)
