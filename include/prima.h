@@ -456,8 +456,10 @@ int prima_beam_select(const void* logits, int dtype, int n_req, int n_beams, int
  * parent[request][j].  table_out[r] holds its pages up to its length_in positions and -1 behind them, length_out[r]
  * its length.  Full pages are shared.  Of the rows that continue the same old row, the first keeps the last, partly
  * filled page; every other one gets page fresh[r] (a page that no row uses, all different), into which the length %
- * page_size entries are copied in all layers.  table_in dev int32 [n_req * n_beams][table_stride]; table_out dev int32
- * [n_req * keep][table_stride], not overlapping table_in; length_in / length_out likewise. */
+ * page_size entries are copied in all layers.  A row whose parent is not 0..n_beams-1, or whose old row has more
+ * positions than table_stride pages hold, is empty: length 0, pages -1.  table_in dev int32
+ * [n_req * n_beams][table_stride]; table_out dev int32 [n_req * keep][table_stride], not overlapping table_in;
+ * length_in / length_out likewise. */
 int prima_paged_reorder(prima_paged* pool, int n_req, int n_beams, int keep, const int32_t* table_in, int64_t table_stride,
                         const int32_t* length_in, const int32_t* parent, const int32_t* fresh, int32_t* table_out, int32_t* length_out,
                         void* stream);

@@ -210,18 +210,19 @@ __global__ void __launch_bounds__(256) reorder_kernel(PoolView pool, int n_beams
   const int64_t pages = (static_cast<int64_t>(max(len, 0)) + (1 << pool.page_shift) - 1) >> pool.page_shift;
   const int tail = len & ((1 << pool.page_shift) - 1);
   const bool bad_len = len < 0 || pages > stride;
-  const int last = !bad_len && pages > 0 ? __ldg(table_in + src * stride + pages - 1) : 0;
-  const bool copies = shared_parent && tail != 0 && !bad_len;
+  const bool empty = bad || bad_len;      // continues nothing: it must not share another row's partly filled page
+  const int last = !empty && pages > 0 ? __ldg(table_in + src * stride + pages - 1) : 0;
+  const bool copies = shared_parent && tail != 0 && !empty;
   const bool bad_page = copies && (static_cast<unsigned>(last) >= static_cast<unsigned>(pool.n_pages) || static_cast<unsigned>(f) >= static_cast<unsigned>(pool.n_pages));
   if (blockIdx.y == 0) {
     if (threadIdx.x == 0) {
       if (bad) raise(pool.status, kBadPath);
-      if (bad_len) raise(pool.status, kBadRows);
+      if (!bad && bad_len) raise(pool.status, kBadRows);
       if (bad_page) raise(pool.status, kBadPage);
-      length_out[r] = bad_len ? 0 : len;
+      length_out[r] = empty ? 0 : len;
     }
     for (int64_t i = threadIdx.x; i < stride; i += blockDim.x)
-      table_out[r * stride + i] = bad_len || i >= pages ? -1 : copies && i == pages - 1 ? f : __ldg(table_in + src * stride + i);
+      table_out[r * stride + i] = empty || i >= pages ? -1 : copies && i == pages - 1 ? f : __ldg(table_in + src * stride + i);
   }
   if (!copies || bad_page) return;
   // A warp takes one head of keys or values of one layer at a time (index arithmetic per 16 bytes would bound the kernel).

@@ -288,3 +288,24 @@ def test_accept_reports_paths_that_do_not_ascend(gpu):
                     (pf, rf), (pt, rt) = b.place(s, 3 + a), b.place(s, 3 + j)
                     want[:, pt, :, rt] = old[:, pf, :, rf]
             assert np.array_equal(got.float().cpu().numpy(), want)
+
+
+def test_reorder_gives_rows_of_bad_parents_no_pages(gpu):
+    """Such a row would share the partly filled page of another one, and both would append to it."""
+    torch, binding = gpu
+    b = Batch(23, ctx=[13, 6], nodes=[0, 0], page=8, dim=64, spare=5)
+    used = set(b.table[b.table >= 0].tolist())
+    fresh = np.array([p for p in range(b.n_pages) if p not in used][:4], np.int32)
+    k, v, pool = cache_on_gpu(gpu, b)
+    for parent in ([0, -1, 1, 2], [-1, 0, 5, 1]):
+        out, n = torch.full((4, b.table.shape[1]), 99, dtype=torch.int32, device="cuda"), torch.full((4,), 99, dtype=torch.int32, device="cuda")
+        pool.reorder(on_gpu(torch, b.table), on_gpu(torch, b.ctx), on_gpu(torch, np.array([parent], np.int32)), on_gpu(torch, fresh), out, n)
+        with pytest.raises(binding.PrimaError) as e:
+            pool.sync()
+        assert "parent" in str(e.value)
+        for r, p in enumerate(parent):
+            good = p in (0, 1)
+            assert int(n[r]) == (b.ctx[p] if good else 0)
+            want = b.table[p].copy() if good else np.full(b.table.shape[1], -1, np.int32)
+            assert np.array_equal(out[r].cpu().numpy(), want)
+    assert np.array_equal(k.float().cpu().numpy(), b.k) and np.array_equal(v.float().cpu().numpy(), b.v)
