@@ -184,3 +184,30 @@ def test_one_beam_holds_the_best(gpu, n_beams, keep):
     cum[:] -= 100.0
     cum[0, n_beams - 1] = cum[1, 0] = -1.0
     check(gpu, logits, cum, keep)
+
+
+@pytest.mark.parametrize("n_req,n_beams,vocab,dtype", [(16, 8, 152064, "float32"), (1, 64, 152064, "bfloat16")])
+def test_the_longest_list_takes_no_search_word_by_word(gpu, n_req, n_beams, vocab, dtype):
+    """64 kept continuations of logits in no order: as many CTAs as these would meet a list that runs over in nearly every
+    call, and each would then go through its words 64 times (15 times the time of 63 kept ones)."""
+    torch, binding = gpu
+    torch.manual_seed(5)
+    x = (torch.randn((n_req, n_beams, vocab), device="cuda") * 2.2).to(getattr(torch, dtype))
+    cum = torch.randn((n_req, n_beams), device="cuda")
+    times = {}
+    for keep in (63, 64):
+        out = torch.zeros((n_req, keep), device="cuda"), torch.zeros((n_req, keep), dtype=torch.int32, device="cuda"), torch.zeros((n_req, keep), dtype=torch.int32, device="cuda")
+        events = [(torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)) for _ in range(9)]
+        for a, b in events:
+            a.record()
+            binding.prima_beam_select(x, cum, *out)
+            b.record()
+        torch.cuda.synchronize()
+        times[keep] = sorted(a.elapsed_time(b) for a, b in events)[4]
+        for r in range(n_req):      # two candidates that change places differ by their errors, 2^-20 each (see check)
+            score = cum[r].double()[:, None] + torch.log_softmax(x[r].double(), 1)
+            want = torch.topk(score.flatten(), keep).values
+            got = score[out[1][r].long(), out[2][r].long()]
+            assert torch.all((got - want).abs() <= 2.0 ** -19)
+            assert torch.unique(out[1][r].long() * vocab + out[2][r].long()).numel() == keep
+    assert times[64] < 4 * times[63], times
