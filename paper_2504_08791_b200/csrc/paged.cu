@@ -245,6 +245,9 @@ __global__ void __launch_bounds__(256) reorder_kernel(PoolView pool, int n_beams
   }
 }
 
+// Takes the reported bits out of the status word: a kernel on another stream may have raised others since it was read.
+__global__ void clear_bits_kernel(int* status, int bits) { atomicAnd(status, ~bits); }
+
 bool aligned16(const void* p) { return aligned_to(p, 16); }
 
 template <typename T, typename In, int D>
@@ -343,7 +346,8 @@ int prima_paged_sync(prima_paged* p, void* stream) {
   cudaError_t e = cudaMemcpyAsync(&status, p->status, sizeof(int), cudaMemcpyDeviceToHost, st);
   if (e == cudaSuccess) e = cudaStreamSynchronize(st);
   if (e == cudaSuccess && status) {
-    e = cudaMemsetAsync(p->status, 0, sizeof(int), st);
+    clear_bits_kernel<<<1, 1, 0, st>>>(p->status, status);
+    e = cudaGetLastError();
     if (e == cudaSuccess) e = cudaStreamSynchronize(st);
   }
   if (e != cudaSuccess) return call_cuda_fail(e, "prima_paged_sync");

@@ -309,3 +309,50 @@ def test_reorder_gives_rows_of_bad_parents_no_pages(gpu):
             want = b.table[p].copy() if good else np.full(b.table.shape[1], -1, np.int32)
             assert np.array_equal(out[r].cpu().numpy(), want)
     assert np.array_equal(k.float().cpu().numpy(), b.k) and np.array_equal(v.float().cpu().numpy(), b.v)
+
+
+def test_sync_of_one_stream_keeps_what_another_raises(gpu):
+    """One thread meets bad slots on its stream and reports them without end; what another thread meets on another stream is
+    reported by one of the calls that begin after it."""
+    import threading
+    import time
+    torch, binding = gpu
+    b = Batch(32, ctx=[4], nodes=[1], page=8, dim=64, q_heads=2, kv_heads=1)
+    k, v, pool = cache_on_gpu(gpu, b)
+    x = torch.zeros((1, 1, 64), device="cuda")
+    one = on_gpu(torch, b.row_begin)
+    slot = binding.PagedBatch(on_gpu(torch, b.table), one, on_gpu(torch, np.array([1000], np.int32)), 1)
+    page = binding.PagedBatch(torch.full_like(on_gpu(torch, b.table), -1), one, on_gpu(torch, b.ctx), 1)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    calls, told, stop, failed = [0], [], [], []
+
+    def report():
+        try:
+            while not stop:
+                pool.append(0, slot, None, x, x, stream=streams[0])
+                try:
+                    pool.sync(streams[0])
+                except binding.PrimaError as e:
+                    if "page" in str(e):
+                        told.append(1)
+                calls[0] += 1
+        except BaseException as e:
+            failed.append(e)
+    thread = threading.Thread(target=report)
+    thread.start()
+    try:
+        lost = 0
+        for i in range(2000):
+            told.clear()
+            pool.append(0, page, None, x, x, stream=streams[1])
+            streams[1].synchronize()
+            want, end = calls[0] + 2, time.monotonic() + 20
+            while calls[0] < want and not failed and time.monotonic() < end:
+                time.sleep(0)
+            assert calls[0] >= want
+            lost += not told
+    finally:
+        stop.append(1)
+        thread.join()
+    assert not failed and lost == 0
