@@ -445,8 +445,8 @@ int prima_paged_accept(prima_paged* pool, const prima_paged_batch* batch, const 
  * score fp32, parent int32 (b), token int32 (w), each [n_req][keep], best first.  A logit of -infinity or NaN is no
  * candidate and has no weight, +infinity counts as the largest finite fp32; a cum of -infinity or NaN leaves a beam
  * without candidates; places for which no candidate is left get score -infinity, parent 0, token -1.  finished: dev
- * uint8 [n_req][n_beams] or NULL (end_token is then ignored).  n_beams, keep: 1..64; n_beams * vocab < 2^31.
- * workspace as above. */
+ * uint8 [n_req][n_beams] or NULL (end_token is then ignored).  n_beams, keep: 1..64; n_beams * vocab < 2^31; vocab at
+ * most 2^31 - 8192.  workspace as above. */
 int64_t prima_beam_select_workspace(int n_req, int n_beams, int vocab, int keep);
 int prima_beam_select(const void* logits, int dtype, int n_req, int n_beams, int vocab, int64_t row_stride, const float* cum,
                       const uint8_t* finished, int end_token, int keep, float* score, int32_t* parent, int32_t* token, void* workspace,

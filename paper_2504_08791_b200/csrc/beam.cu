@@ -436,6 +436,7 @@ cudaError_t launch_select(const void* logits, int n_req, int n_beams, int vocab,
 const char* select_error(int n_req, int n_beams, int vocab, int keep) {
   if (n_req < 1 || vocab < 1) return "n_req and vocab must be positive";
   if (n_beams < 1 || n_beams > kMaxKeep || keep < 1 || keep > kMaxKeep) return "n_beams and keep are 1..64";
+  if (vocab > 2147483647 - 8191) return "vocab is above 2^31 - 8192";      // words are numbered in 32 bits to the end of the last slice
   if (static_cast<int64_t>(n_beams) * vocab > 2147483647) return "n_beams * vocab reaches 2^31";
   if (static_cast<int64_t>(n_req) * n_beams > 65535) return "more than 65535 beams";
   return nullptr;

@@ -176,3 +176,15 @@ def test_refusals_need_no_gpu():
     assert L.prima_beam_select(*args) == binding.ERR_ARG
     assert L.prima_beam_select_workspace(1, 64, 1 << 26, 4) == binding.ERR_ARG
     assert L.prima_beam_select_workspace(16, 8, 152064, 8) > 0
+
+
+def test_vocabularies_up_to_32_bits():
+    """Words are numbered in 32 bits up to the end of the last slice of 8192: longer rows are refused as arguments."""
+    build.build()
+    L = binding.lib()
+    longest = 2 ** 31 - 8192
+    assert L.prima_beam_select_workspace(1, 1, longest, 4) > 0
+    for vocab in (longest + 1, 2 ** 31 - 2048, 2 ** 31 - 1):
+        assert L.prima_beam_select_workspace(1, 1, vocab, 4) == binding.ERR_ARG, vocab
+        assert L.prima_beam_select(4096, binding.DT_F16, 1, 1, vocab, vocab, 4096, None, 0, 4, 4096, 4096, 4096, 4096, 1 << 40, None) == binding.ERR_ARG
+        assert b"vocab" in L.prima_last_error(None)
