@@ -374,7 +374,7 @@ class PagedBatch:
         self._keep = (table, row_begin, ctx_len, pos, mask)
         words = 0
         if mask is not None:
-            if mask.dim() != 2:
+            if mask.dim() != 2 or mask.shape[1] < 1:      # without words it has no address, which would read as no mask
                 raise ValueError("mask: expected [n_tok, words]")
             words = mask.shape[1]
         self.desc = PagedBatchDesc(n_seq, self.n_tok, _need(row_begin, "row_begin", i32, (n_seq + 1,), dev), _need(ctx_len, "ctx_len", i32, (n_seq,), dev),

@@ -188,3 +188,33 @@ def test_vocabularies_up_to_32_bits():
         assert L.prima_beam_select_workspace(1, 1, vocab, 4) == binding.ERR_ARG, vocab
         assert L.prima_beam_select(4096, binding.DT_F16, 1, 1, vocab, vocab, 4096, None, 0, 4, 4096, 4096, 4096, 4096, 1 << 40, None) == binding.ERR_ARG
         assert b"vocab" in L.prima_last_error(None)
+
+
+class Stand:
+    """What the binding looks at in a tensor."""
+
+    def __init__(self, dtype, *shape):
+        self.dtype, self.shape, self.device, self.is_cuda = dtype, shape, "cuda:0", True
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        return int(np.prod(self.shape))
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return 4096 if self.numel() else 0      # torch: no address without elements
+
+
+def test_a_mask_without_words_is_refused():
+    """It has no address, and a batch without a mask is a causal one."""
+    import torch
+    i32 = torch.int32
+    table, begin, ctx = Stand(i32, 2, 5), Stand(i32, 3), Stand(i32, 2)
+    assert binding.PagedBatch(table, begin, ctx, 4, mask=Stand(torch.int64, 4, 1)).desc.mask_words == 1
+    assert binding.PagedBatch(table, begin, ctx, 4).desc.mask is None
+    with pytest.raises(ValueError):
+        binding.PagedBatch(table, begin, ctx, 4, mask=Stand(torch.int64, 4, 0))
