@@ -221,7 +221,10 @@ class Context:
                          cfg["vocab"], cfg["kv_capacity"], cfg.get("max_n_tok", MAX_N_TOK), cfg["rms_eps"], cfg["rope_theta"],
                          cfg.get("rope_mode", 0), device)
         self._h = C.c_void_p()
-        self._stream = stream
+        if stream is None:
+            import torch
+            stream = torch.cuda.current_stream()
+        self._stream = stream      # what follows the context's steps has to run on it, whatever is current by then
         _check(lib().prima_ctx_create(C.byref(mc), _stream_ptr(stream), C.byref(self._h)))
 
     def close(self):

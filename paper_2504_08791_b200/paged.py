@@ -82,8 +82,8 @@ class PagedStepper:
         self.logits = torch.empty((self.max_n_tok, cfg["vocab"]), dtype=torch.float32, device=k_pages.device)
 
     def on_stream(self):
-        """torch's current stream becomes the context's own, if it has one: the small arrays of a step are then uploaded,
-        and their memory is used again, in the order of the steps that read them."""
+        """torch's current stream becomes the context's: the small arrays of a step are then uploaded, and their memory is
+        used again, in the order of the steps that read them."""
         return self.torch.cuda.stream(self.ctx._stream)
 
     def _gpu(self, a, dtype=np.int32):

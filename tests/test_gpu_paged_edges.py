@@ -356,3 +356,32 @@ def test_sync_of_one_stream_keeps_what_another_raises(gpu):
         stop.append(1)
         thread.join()
     assert not failed and lost == 0
+
+
+def test_a_context_made_on_a_side_stream_and_used_outside_of_it(gpu):
+    """Its steps run on the stream that was current when it was made; selection, reordering and accepted paths follow them,
+    though another stream is current."""
+    torch, binding = gpu
+    from paper_2504_08791_b200.paged import BeamDecoder, DraftTree, TreeSpeculativeDecoder
+    cfg = synth.model_config("tiny", max_n_tok=4)
+    prompt = [int(x) for x in np.random.RandomState(7).randint(0, cfg["vocab"], 9)]
+    side, seen = torch.cuda.Stream(), []
+
+    def propose(history, limit):
+        return DraftTree([history[-1], history[-2], 3, 4], [-1, 0, 0, 2])
+    for made_on in (None, side):
+        with torch.cuda.stream(made_on):
+            ctx = load(gpu, cfg, 50)
+            m = stepper(gpu, ctx, page=8)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(made_on):
+            torch.cuda._sleep(50_000_000)      # some 25 ms
+        beams = BeamDecoder(m, 3).generate(prompt, 5)
+        pages = []
+        m.prefill(prompt[:-1], pages)
+        out, _ = TreeSpeculativeDecoder(m, propose).generate(prompt, pages, len(prompt) - 1, 6)
+        torch.cuda.synchronize()
+        m.pool.sync()
+        seen.append((beams, out))
+        ctx.close()
+    assert seen[0] == seen[1]

@@ -153,3 +153,27 @@ def test_a_draft_that_does_not_fit_is_refused():
     for bad in (DraftTree([9], [-1]), DraftTree([2, 1, 1, 1, 1], [-1, 0, 1, 2, 3]), DraftTree([], [])):
         with pytest.raises(ValueError):
             TreeSpeculativeDecoder(toy, lambda h, n: bad).generate([1, 2], [], 1, 3)
+
+
+def test_a_context_knows_the_stream_it_was_made_on(monkeypatch):
+    """Selection and accepted paths have to follow its steps, whatever torch's current stream is by then."""
+    import torch
+    from paper_2504_08791_b200 import binding, synth
+
+    class Stream:
+        def __init__(self, raw):
+            self.cuda_stream = raw
+
+    class Lib:
+        def prima_ctx_create(self, cfg, stream, out):
+            self.got = stream.value
+            return 0
+
+        def prima_ctx_destroy(self, h):
+            return 0
+    fake = Lib()
+    monkeypatch.setattr(binding, "lib", lambda: fake)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: Stream(1234))
+    for given, raw in ((None, 1234), (Stream(99), 99)):
+        ctx = binding.Context(synth.model_config("tiny"), stream=given)
+        assert fake.got == raw and ctx._stream.cuda_stream == raw
