@@ -88,14 +88,10 @@ __device__ __forceinline__ int64_t slot_row(const PoolView& p, const int32_t* ta
 
 template <typename T> struct Half2Of;
 template <> struct Half2Of<__half> {
-  using type = __half2;
-  __device__ static float to_f(__half x) { return __half2float(x); }
   __device__ static uint32_t pack(float a, float b) { const __half2 h = __floats2half2_rn(a, b); return *reinterpret_cast<const uint32_t*>(&h); }
   __device__ static float2 unpack(uint32_t u) { return __half22float2(*reinterpret_cast<const __half2*>(&u)); }
 };
 template <> struct Half2Of<__nv_bfloat16> {
-  using type = __nv_bfloat162;
-  __device__ static float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
   __device__ static uint32_t pack(float a, float b) { const __nv_bfloat162 h = __floats2bfloat162_rn(a, b); return *reinterpret_cast<const uint32_t*>(&h); }
   __device__ static float2 unpack(uint32_t u) { return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u)); }
 };

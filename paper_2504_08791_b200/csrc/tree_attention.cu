@@ -848,9 +848,8 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
 template <typename T, typename Out, int D>
 __global__ void __launch_bounds__(128, StreamGeometry<D>::kCtas) tree_stream_kernel(const __grid_constant__ TreeArgs a) {
   using Geo = StreamGeometry<D>;
-  constexpr int M = 1;                                // tiles of 16 rows
   constexpr bool kBf16 = !__is_same(T, __half);
-  constexpr int kPieces = D / 8, kRows = 16 * M;      // 16-byte pieces of a row
+  constexpr int kPieces = D / 8, kRows = 16;          // 16-byte pieces of a row; rows of a tile
   extern __shared__ __align__(128) uint8_t smem_raw[];
   __shared__ Segment s_seg;
   __shared__ float2 s_ml[4][kRows];
@@ -942,31 +941,26 @@ __global__ void __launch_bounds__(128, StreamGeometry<D>::kCtas) tree_stream_ker
     }
     asm volatile("cp.async.wait_group %0;" ::"n"(Geo::kStages - 1) : "memory");      // the queries
     __syncthreads();
-    uint32_t qf[M][D / 16][4];
+    uint32_t qf[D / 16][4];
 #pragma unroll
-    for (int m = 0; m < M; ++m)
-#pragma unroll
-      for (int k = 0; k < D / 16; ++k) {
-        const int row = 16 * m + (lane & 15);
-        ldsm4(qf[m][k], q_addr + row * Geo::kRow + ((2 * k + (lane >> 4)) ^ (row & 7)) * 16);
-      }
-    float o[M][D / 8][4];
-    float ref[M][2], sum[M][2];
-    int node[M][2];
-#pragma unroll
-    for (int m = 0; m < M; ++m) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int x = 16 * m + 8 * h + g;
-        node[m][h] = x < s.rows ? t0 + small_div(rem0 + x, a.group_inverse) : -1;
-        ref[m][h] = -INFINITY;
-        sum[m][h] = 0.f;
-      }
-#pragma unroll
-      for (int n = 0; n < D / 8; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[m][n][e] = 0.f;
+    for (int k = 0; k < D / 16; ++k) {
+      const int row = lane & 15;
+      ldsm4(qf[k], q_addr + row * Geo::kRow + ((2 * k + (lane >> 4)) ^ (row & 7)) * 16);
     }
+    float o[D / 8][4];
+    float ref[2], sum[2];
+    int node[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int x = 8 * h + g;
+      node[h] = x < s.rows ? t0 + small_div(rem0 + x, a.group_inverse) : -1;
+      ref[h] = -INFINITY;
+      sum[h] = 0.f;
+    }
+#pragma unroll
+    for (int n = 0; n < D / 8; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
     int stage = 0;
 #pragma unroll 1
     for (int step = warp; step < steps; step += 4) {
@@ -978,86 +972,70 @@ __global__ void __launch_bounds__(128, StreamGeometry<D>::kCtas) tree_stream_ker
       asm volatile("cp.async.wait_group %0;" ::"n"(Geo::kStages - 1) : "memory");
       __syncwarp();
       const uint32_t kk = ring_addr + stage * Geo::kStage, vv = kk + Geo::kStep * Geo::kRow;
-      float sc[M][2][4];
+      float sc[2][4];
 #pragma unroll
-      for (int m = 0; m < M; ++m)
+      for (int n = 0; n < 2; ++n)
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) sc[m][n][e] = 0.f;
+        for (int e = 0; e < 4; ++e) sc[n][e] = 0.f;
 #pragma unroll
       for (int k = 0; k < D / 16; ++k) {
         uint32_t b[4];      // positions 0..7 and 8..15, two halves of 8 columns each
         const int row = (lane >> 4) * 8 + (lane & 7);
         ldsm4(b, kk + row * Geo::kRow + ((2 * k + (lane >> 3 & 1)) ^ (row & 7)) * 16);
-#pragma unroll
-        for (int m = 0; m < M; ++m) {
-          mma16816<kBf16>(sc[m][0], qf[m][k], b[0], b[1]);
-          mma16816<kBf16>(sc[m][1], qf[m][k], b[2], b[3]);
-        }
+        mma16816<kBf16>(sc[0], qf[k], b[0], b[1]);
+        mma16816<kBf16>(sc[1], qf[k], b[2], b[3]);
       }
       const long long pos0 = pos_first + step * Geo::kStep;
       const bool bad = bad_stages >> stage & 1;
       if (pos0 + Geo::kStep > s.all_see() || bad) {      // positions that the row does not see, or on a bad page
         const SegmentView view{a.b, a.pool, s.first, s.nodes, s.ctx, s.limit, table, bad};
 #pragma unroll
-        for (int m = 0; m < M; ++m)
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t seen = node[h] >= 0 ? view.seen_by(node[h], pos0) : 0u;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint32_t seen = node[m][h] >= 0 ? view.seen_by(node[m][h], pos0) : 0u;
+          for (int n = 0; n < 2; ++n)
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-              for (int e = 0; e < 2; ++e)
-                if (!(seen >> (8 * n + 2 * t4 + e) & 1)) sc[m][n][2 * h + e] = -INFINITY;
-          }
-      }
-#pragma unroll
-      for (int m = 0; m < M; ++m) {
-        float top[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) top[h] = fmaxf(fmaxf(sc[m][0][2 * h], sc[m][0][2 * h + 1]), fmaxf(sc[m][1][2 * h], sc[m][1][2 * h + 1])) * a.scale_log2;
-        if (__any_sync(0xffffffffu, top[0] > ref[m][0] + kSlack || top[1] > ref[m][1] + kSlack)) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            float x = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 1));
-            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
-            const float r = x > ref[m][h] + kSlack ? x : ref[m][h];
-            const float f = r == ref[m][h] ? 1.f : ex2(ref[m][h] - r);
-            ref[m][h] = r;
-            sum[m][h] *= f;
-#pragma unroll
-            for (int n = 0; n < D / 8; ++n) {
-              o[m][n][2 * h] *= f;
-              o[m][n][2 * h + 1] *= f;
-            }
-          }
+            for (int e = 0; e < 2; ++e)
+              if (!(seen >> (8 * n + 2 * t4 + e) & 1)) sc[n][2 * h + e] = -INFINITY;
         }
-        uint32_t p[4];
+      }
+      float top[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) top[h] = fmaxf(fmaxf(sc[0][2 * h], sc[0][2 * h + 1]), fmaxf(sc[1][2 * h], sc[1][2 * h + 1])) * a.scale_log2;
+      if (__any_sync(0xffffffffu, top[0] > ref[0] + kSlack || top[1] > ref[1] + kSlack)) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const float shift = ref[m][h] == -INFINITY ? 0.f : -ref[m][h];
+          float x = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 1));
+          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
+          const float r = x > ref[h] + kSlack ? x : ref[h];
+          const float f = r == ref[h] ? 1.f : ex2(ref[h] - r);
+          ref[h] = r;
+          sum[h] *= f;
 #pragma unroll
-          for (int n = 0; n < 2; ++n) {
-            const float x = ex2(fmaf(sc[m][n][2 * h], a.scale_log2, shift)), y = ex2(fmaf(sc[m][n][2 * h + 1], a.scale_log2, shift));
-            sum[m][h] += x + y;
-            p[2 * n + h] = Half2Of<T>::pack(x, y);
+          for (int n = 0; n < D / 8; ++n) {
+            o[n][2 * h] *= f;
+            o[n][2 * h + 1] *= f;
           }
         }
+      }
+      uint32_t p[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sc[m][e >> 1][e & 1] = __uint_as_float(p[e]);      // kept for the second product
+      for (int h = 0; h < 2; ++h) {
+        const float shift = ref[h] == -INFINITY ? 0.f : -ref[h];
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+          const float x = ex2(fmaf(sc[n][2 * h], a.scale_log2, shift)), y = ex2(fmaf(sc[n][2 * h + 1], a.scale_log2, shift));
+          sum[h] += x + y;
+          p[2 * n + h] = Half2Of<T>::pack(x, y);
+        }
       }
 #pragma unroll
       for (int n = 0; n < D / 16; ++n) {
         uint32_t b[4];      // 16 positions, columns 16 n .. + 7 and + 8 .. + 15
         const int row = (lane >> 3 & 1) * 8 + (lane & 7);
         ldsm4_t(b, vv + row * Geo::kRow + ((2 * n + (lane >> 4)) ^ (row & 7)) * 16);
-#pragma unroll
-        for (int m = 0; m < M; ++m) {
-          const uint32_t p[4] = {__float_as_uint(sc[m][0][0]), __float_as_uint(sc[m][0][1]), __float_as_uint(sc[m][1][0]), __float_as_uint(sc[m][1][1])};
-          mma16816<kBf16>(o[m][2 * n], p, b[0], b[1]);
-          mma16816<kBf16>(o[m][2 * n + 1], p, b[2], b[3]);
-        }
+        mma16816<kBf16>(o[2 * n], p, b[0], b[1]);
+        mma16816<kBf16>(o[2 * n + 1], p, b[2], b[3]);
       }
       stage = stage + 1 == Geo::kStages ? 0 : stage + 1;
       __syncwarp();
@@ -1067,16 +1045,14 @@ __global__ void __launch_bounds__(128, StreamGeometry<D>::kCtas) tree_stream_ker
     // ---- the segment's result: every warp's state to shared memory, in place of its ring ----
     float* my_o = reinterpret_cast<float*>(my_ring);      // [kRows][D]
 #pragma unroll
-    for (int m = 0; m < M; ++m)
+    for (int h = 0; h < 2; ++h) {
+      const int x = 8 * h + g;
+      float z = sum[h] + __shfl_xor_sync(0xffffffffu, sum[h], 1);
+      z += __shfl_xor_sync(0xffffffffu, z, 2);
+      if (t4 == 0) s_ml[warp][x] = make_float2(ref[h], z);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int x = 16 * m + 8 * h + g;
-        float z = sum[m][h] + __shfl_xor_sync(0xffffffffu, sum[m][h], 1);
-        z += __shfl_xor_sync(0xffffffffu, z, 2);
-        if (t4 == 0) s_ml[warp][x] = make_float2(ref[m][h], z);
-#pragma unroll
-        for (int n = 0; n < D / 8; ++n) *reinterpret_cast<float2*>(my_o + x * D + 8 * n + 2 * t4) = make_float2(o[m][n][2 * h], o[m][n][2 * h + 1]);
-      }
+      for (int n = 0; n < D / 8; ++n) *reinterpret_cast<float2*>(my_o + x * D + 8 * n + 2 * t4) = make_float2(o[n][2 * h], o[n][2 * h + 1]);
+    }
     __syncthreads();
     const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) + (s.kind == 2);
     for (int idx = tid; idx < s.rows * (D / 4); idx += 128) {
