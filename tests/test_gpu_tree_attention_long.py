@@ -198,3 +198,120 @@ def test_a_row_without_a_number_has_no_sum(gpu, kind):
             assert np.all(np.isnan(out[t, h])) and np.isnan(lse[t, h])
             out[t, h], lse[t, h] = want[0][t, h], want[1][t, h]
         compare(b, (out, lse), want)
+
+
+@pytest.mark.parametrize("gain", [1e-3, 12.0, 40.0])
+@pytest.mark.parametrize("kind", KINDS)
+def test_score_ranges_over_many_units(gpu, kind, gain):
+    """From an even softmax to one where a single position takes all."""
+    torch, _ = gpu
+    nodes, ctx = KINDS[kind]
+    b = Batch(250, ctx=[ctx], nodes=[nodes], page=32, q_heads=16, kv_heads=4, dim=64)
+    q = _paged.rounded(b.rs.standard_normal((b.n_tok, 16, 64)).astype(np.float32) * gain, b.dtype)
+    mask = b.trees(3)[0]
+    compare(b, run(gpu, b, mask, q, times=3), attention(torch, b, q, mask, 0.125))
+
+
+@pytest.mark.parametrize("dim,dtype", [(128, "float16"), (64, "bfloat16")])
+@pytest.mark.parametrize("junk", [np.inf, -np.inf, np.nan, 65504.0])
+@pytest.mark.parametrize("kind", KINDS)
+def test_stale_entries_do_no_harm_behind_many_units(gpu, kind, junk, dim, dtype):
+    """Whatever no row sees (behind a sequence's end, on pages of nobody, a node that is seen by no row) may hold anything, and
+    keys that a row does not see, too."""
+    torch, _ = gpu
+    nodes, ctx = KINDS[kind]
+    b = Batch(260 + dim, ctx=[ctx, 3, 250], nodes=[nodes, nodes, nodes], page=16, q_heads=16, kv_heads=4, dim=dim, dtype=dtype, pad=1)
+    mask, _ = b.trees(3)
+    mask[nodes - 1, (nodes - 1) // 64] &= ~np.int64(np.uint64(1 << (nodes - 1) % 64).view(np.int64))      # the last node of the first sequence
+    assert not b.sees(0, mask)[:, -1].any()
+    q = _paged.rounded(b.rs.standard_normal((b.n_tok, 16, dim)).astype(np.float32), b.dtype)
+    want = attention(torch, b, q, mask, dim ** -0.5)
+    keep = np.zeros((b.n_pages, b.page), bool)
+    for s in range(3):
+        for j in range(int(b.ctx[s] + nodes) - (s == 0)):
+            keep[b.place(s, j)] = True
+    for a in (b.k, b.v):
+        a[:] = np.where(keep[None, :, None, :, None], a, np.float32(junk))
+    compare(b, run(gpu, b, mask, q), want)
+    # a key that only its own row sees
+    t = int(b.row_begin[2]) + 1
+    mask[b.row_begin[2]:, 0] &= ~np.int64(2)
+    mask[t, 0] |= 2
+    want = attention(torch, b, q, mask, dim ** -0.5)
+    page, row = b.place(2, 251)
+    b.k[:, page, :, row] = junk
+    out, lse = run(gpu, b, mask, q)
+    out[t], lse[t] = want[0][t], want[1][t]
+    compare(b, (out, lse), want)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("page", [8, 64, 256])
+@pytest.mark.parametrize("kind", KINDS)
+def test_bad_pages_among_many_units(gpu, kind, page, dim):
+    """Positions on pages that the pool does not have are not seen: at the beginning, in runs, alone, and at the end, under the
+    rows of the step."""
+    torch, _ = gpu
+    nodes, ctx = KINDS[kind]
+    b = Batch(270, ctx=[ctx, 700], nodes=[nodes, nodes], page=page, q_heads=16, kv_heads=4, dim=dim, dtype="bfloat16")
+    mask, _ = b.trees(3)
+    q = _paged.rounded(b.rs.standard_normal((b.n_tok, 16, dim)).astype(np.float32), b.dtype)
+    used = -(-(ctx + nodes) // page)
+    lost = sorted({0, used // 3, used // 3 + 1, used // 3 + 2, used // 2, used - 1})
+    seen = [b.sees(s, mask) for s in range(2)]
+    for p in lost:
+        seen[0][:, p * page:(p + 1) * page] = False
+    want = attention(torch, b, q, mask, dim ** -0.5, seen)
+    b.table[0, lost] = np.array([-1, b.n_pages, -2 ** 31, 2 ** 31 - 1, -7, b.n_pages + 5], np.int64)[:len(lost)].astype(np.int32)
+    compare(b, run(gpu, b, mask, q, times=3, status="page id"), want)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_rows_that_see_nothing_beside_others(gpu, kind):
+    torch, _ = gpu
+    nodes, ctx = KINDS[kind]
+    b = Batch(280, ctx=[0, 0, ctx], nodes=[nodes, nodes, nodes], page=16, q_heads=16, kv_heads=4, dim=64, pad=2)
+    mask, _ = b.trees(3)
+    mask[:nodes] = 0                       # a whole sequence
+    mask[[nodes, nodes + 2]] = 0           # rows beside others in their tile
+    mask[b.row_begin[2] + 1] = 0           # sees its context only
+    q = _paged.rounded(b.rs.standard_normal((b.n_tok, 16, 64)).astype(np.float32), b.dtype)
+    want = attention(torch, b, q, mask, 0.125)
+    assert np.all(np.isneginf(want[1][:nodes])) and np.isfinite(want[1][b.row_begin[2]:b.live]).all()
+    compare(b, run(gpu, b, mask, q), want)
+
+
+@pytest.mark.parametrize("kind", ["one", "two"])
+def test_two_graphs_of_many_units_replayed_side_by_side(gpu, kind):
+    """Captured calls with a workspace each, replayed at once on two streams with new lengths: many units, one, none."""
+    torch, binding = gpu
+    nodes, ctx = KINDS[kind]
+    b = Batch(290, ctx=[ctx, 900], nodes=[nodes, nodes], page=64, q_heads=16, kv_heads=4, dim=64)
+    mask, _ = b.trees(1)
+    k, v, pool = cache_on_gpu(gpu, b)
+    dev = on_gpu(torch, b.ctx)
+    batch = binding.PagedBatch(on_gpu(torch, b.table), on_gpu(torch, b.row_begin), dev, b.n_tok, mask=on_gpu(torch, mask))
+    q = _paged.rounded(b.rs.standard_normal((b.n_tok, 16, 64)).astype(np.float32), b.dtype)
+    dq = on_gpu(torch, q).half()
+    outs, lses, graphs = [torch.zeros_like(dq) for _ in range(2)], [torch.zeros(dq.shape[:2], device="cuda") for _ in range(2)], []
+    torch.cuda.synchronize()
+    for i in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            pool.tree_attention(0, batch, dq, outs[i], lse=lses[i])
+        graphs.append(g)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for lens in ([ctx, 900], [40, 0], [5000, 127], [0, 0]):
+        dev.copy_(torch.tensor(lens, dtype=torch.int32))
+        b.ctx = np.array(lens, np.int32)
+        torch.cuda.synchronize()
+        for _ in range(5):
+            for g, s in zip(graphs, streams):
+                with torch.cuda.stream(s):
+                    g.replay()
+        torch.cuda.synchronize()
+        pool.sync()
+        want = attention(torch, b, q, mask, 0.125)
+        for o, z in zip(outs, lses):
+            compare(b, (o.float().cpu().numpy(), z.cpu().numpy()), want)
+    del graphs
