@@ -424,7 +424,8 @@ int prima_tree_attention(prima_paged* pool, int layer, const prima_paged_batch* 
  * batch->n_tok (1..max_n_tok) rows of hidden_in / hidden_out, each of its own sequence, at its own position, seeing what
  * the batch says (a chain, a tree of drafted tokens, one token of each of several requests or beams).  The pool takes the
  * place of the context's own caches; layer l of the model is layer l of the pool, whose KV heads, head size, rotation and
- * device must be the model's.  The calls run on the context's stream, and the context keeps one workspace for them, which
+ * device must be the model's.  Rotated queries are rounded to the pool's type, as keys and values are (a pool in bfloat16
+ * keeps fewer bits of them than the context's own binary16 caches).  The calls run on the context's stream, and the context keeps one workspace for them, which
  * the first call allocates (refused with PRIMA_ERR_STATE while the stream is being captured; later calls may be).  Rows
  * behind the last sequence are computed with whatever their hidden rows hold and appended nowhere; they do not touch the
  * others.  Errors as prima_forward_window. */
@@ -440,8 +441,11 @@ int prima_paged_accept(prima_paged* pool, const prima_paged_batch* batch, const 
 
 /* The `keep` best continuations of n_beams beams of each of n_req requests.  logits: dev [n_req][n_beams] rows of
  * `vocab` values of type dtype (fp32, fp16, bf16), row_stride elements apart.  Candidate (b, w) of a request has the
- * score cum[b] + log softmax(logits[b])[w], evaluated in 64 bits; a beam with finished[b] != 0 has one candidate,
- * (b, end_token) with score cum[b].  Candidates are ordered by score, equal ones by b * vocab + w; outputs: dev
+ * score cum[b] + log softmax(logits[b])[w]; a beam with finished[b] != 0 has one candidate, (b, end_token) with score
+ * cum[b].  The sum of a row has 32-bit exponentials, of which the 8 or 32 of a thread are added in 32 bits and those
+ * sums in 64: a relative error of some 2^-20, the same for equal rows.  Scores are formed and compared in 64 bits:
+ * candidates of one beam are in order, and those of different beams where they are further apart than that error.
+ * Candidates are ordered by score, equal ones by b * vocab + w; outputs: dev
  * score fp32, parent int32 (b), token int32 (w), each [n_req][keep], best first.  A logit of -infinity or NaN is no
  * candidate and has no weight, +infinity counts as the largest finite fp32; a cum of -infinity or NaN leaves a beam
  * without candidates; places for which no candidate is left get score -infinity, parent 0, token -1.  finished: dev

@@ -5,9 +5,11 @@
 // The logits are read once.  A CTA holds slices of one row in registers, one after the other, and leaves their
 // maximum, their sum of exponentials and their `keep` best logits; a second kernel joins the slices of a request.  Within a row the order of
 // the scores is the order of the logits, so the slices can be cut down before the row's sum is known.
-// Which of two near candidates of DIFFERENT beams is ahead depends on the last bits of the two sums, so everything
-// behind a thread's own partial sum is in 64 bits.  Every sum has a fixed order that follows the index in the row, not
-// the address: equal rows get equal bits, and their candidates tie exactly (the lower index wins).
+// Which of two near candidates of DIFFERENT beams is ahead depends on the last bits of the two sums, so all that is added
+// behind a thread's own 8 or 32 words is added in 64 bits.  The exponentials of a slice (of its words and of the
+// differences between its maxima) are 32-bit ones, 2^-22 each; in 64 bits they would cost about as much as all else (some
+// 40 operations a word, not measured).  Every sum has a fixed order that follows the index in the row, not the address:
+// equal rows get equal bits, and their candidates tie exactly (the lower index wins).
 // Rows that cannot contribute (finished beams, cum = -infinity) are not read.
 #include <cfloat>
 #include <cstdio>

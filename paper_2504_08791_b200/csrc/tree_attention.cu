@@ -13,8 +13,11 @@
 // scores, used in turn by the units (or by the two accumulators of a tile of more than 128 rows), so that the scores of
 // the next sub-unit are computed under the exponentials of this one; P takes the place of its scores.
 // The two threads of a row share its reference maximum, which moves only when a score exceeds it by a factor of 2^8:
-// that is one vote of two warps per sub-unit, and O is hardly ever rescaled.  Sums and maxima are in 32 bits, P has the
-// cache's type.
+// that is one vote of two warps per sub-unit, and O is hardly ever rescaled.  Sums and maxima are in 32 bits.  P is
+// rounded to the cache's type because the product takes both operands in one type; with values widened to 32 bits it would
+// run at half the rate and the values would take twice the ring, and P as a sum of two 16-bit numbers would double the
+// product.  It costs half a step of each probability (outputs in fp16 off by 2.9e-4 of their size from 64 bits where
+// unrounded probabilities give 2.1e-4, in bf16 2.1e-3 and 1.7e-3); the streaming kernel does the same.
 // A segment that is not a whole (sequence, KV head, tile) leaves its maximum, sum and output in the workspace, and
 // tree_merge_kernel joins the parts in ascending order: the same lengths give the same bits.
 // Measured (one B200, both kernels together): 64 nodes, 64 query heads on 8 KV heads of 128, 65,531 positions, fp16:
@@ -1164,6 +1167,10 @@ struct Maps { CUtensorMap k, v; };
 // 40 rows 135 and 74; 64 of 600, 5 rows 39 and 56, 20 rows 61 and 57, 40 rows 83 and 59.  Between 16 and 32 rows it goes
 // by the lengths, which are not known here: 20 rows over 1000 positions 12.6 and 14.9, over 30 positions 8.6 and 14.9,
 // 64 ragged sequences up to 4096 68 and 61; heads of 64, the same, 41 and 56.  The larger gains are with streaming.
+// The average hides mixed batches, and padding rows count in it: 63 single tokens and one tree of 64 nodes, 8 query heads
+// per KV head, go to the streaming kernel, which reads the tree's cache once per 16 of its 512 rows.  All over 30,000
+// positions that is still the faster one (1607 and 2078 us), but with the single tokens over 1000 it takes 454 and 189, 15
+// single tokens over 2000 and a tree over 8000, 4 heads per KV head, 89 and 75.
 bool streams(const BatchView& b, int group) { return (static_cast<int64_t>(b.n_tok) + b.n_seq - 1) / b.n_seq * group <= 32; }
 struct Workers {
   int n, tile_rows;
