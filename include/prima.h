@@ -412,8 +412,9 @@ int prima_paged_append(prima_paged* pool, int layer, const prima_paged_batch* ba
  * [n_tok][n_q_heads] or NULL: log(sum_j exp(scale * q . k_j)).  A row that sees nothing yields zeros and -infinity.
  * Positions that no row of the sequence sees are not used, whatever their bytes; keys may hold any bytes where a row
  * does not see them.  The value of a position that some row of the sequence sees must be finite.
- * scale > 0, finite.  n_q_heads: a multiple of n_kv_heads, at most 64 times it.  Scores, maxima and sums in 32 bits; the probabilities enter
- * the second product in the cache's type (rounding of half a step, relative 2^-11 resp. 2^-8 of each).
+ * scale > 0, finite.  n_q_heads: a multiple of n_kv_heads, at most 64 times it.  Scores, maxima and sums in 32 bits; the
+ * probabilities enter the second product in the cache's type: rounding of half a step, relative 2^-11 resp. 2^-8 of
+ * each; in binary16 2^-32 of the row's largest where that is more.
  * workspace: dev, 256-byte aligned, of at least the bytes that prima_tree_attention_workspace names for the same
  * (n_seq, n_tok, n_q_heads); its contents before and after mean nothing; calls that may overlap need one each. */
 int64_t prima_tree_attention_workspace(const prima_paged* pool, int n_seq, int n_tok, int n_q_heads);

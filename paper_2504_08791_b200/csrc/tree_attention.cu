@@ -12,8 +12,8 @@
 // eight warps turn S into P, one thread per row and half of the 128 positions: no shuffles.  There are two buffers of
 // scores, used in turn by the units (or by the two accumulators of a tile of more than 128 rows), so that the scores of
 // the next sub-unit are computed under the exponentials of this one; P takes the place of its scores.
-// The two threads of a row share its reference maximum, which moves only when a score exceeds it by a factor of 2^8:
-// that is one vote of two warps per sub-unit, and O is hardly ever rescaled.  Sums and maxima are in 32 bits.  P is
+// The two threads of a row share its reference, which moves only when a score exceeds the maximum that set it by a factor
+// of 2^8: that is one vote of two warps per sub-unit, and O is hardly ever rescaled.  Sums and maxima are in 32 bits.  P is
 // rounded to the cache's type because the product takes both operands in one type; with values widened to 32 bits it would
 // run at half the rate and the values would take twice the ring, and P as a sum of two 16-bit numbers would double the
 // product.  It costs half a step of each probability (outputs in fp16 off by 2.9e-4 of their size from 64 bits where
@@ -46,7 +46,11 @@ constexpr int kSegments = 4;           // planned ahead
 // nodes over 65,531 positions 168, 174, 166; streaming kernel, 64 ragged single tokens 23.8, 28.1, with three units 26.9.
 constexpr int kSegmentCost = 3, kStreamSegmentCost = 1;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
-constexpr float kSlack = 8.f;          // binary exponent by which a score may exceed the reference
+// Binary exponents: a reference is set kHeadroom below the row's maximum and stays until a score exceeds it by kSlack.  A
+// row's largest probability is held as 2^7 to 2^15 (binary16 ends at 65504), not as 1: what binary16 rounds below its normal
+// numbers, by up to 2^-25, is then 2^-32 of the largest, and thousands of positions that have 2^-25 of its weight
+// each are not rounded away one by one.
+constexpr float kHeadroom = 7.f, kSlack = 15.f;
 
 template <int D> struct Geometry {
   static constexpr int kQBytes = 128 * D * 2;                  // one tile of 128 rows of queries
@@ -265,7 +269,10 @@ __device__ __forceinline__ float ex2(float x) {
 
 // A row that sees nothing has a sum of 0: its output is 0, its log-sum-exp -infinity.  A NaN stays one.
 __device__ __forceinline__ float inverse_of(float total) { return total == 0.f ? 0.f : 1.f / total; }
-__device__ __forceinline__ float log_sum(float reference, float total) { return total == 0.f ? -INFINITY : (reference + log2f(total)) * kLn2; }
+__device__ __forceinline__ float log_sum(float reference, float total) {
+  constexpr float kDown = 1.f / 128.f;      // 2^-kHeadroom
+  return total == 0.f ? -INFINITY : (reference + kHeadroom + log2f(total * kDown)) * kLn2;
+}
 
 // Two 32-bit operations in one instruction.
 __device__ __forceinline__ float2 fma2(float2 x, float2 y, float2 z) {
@@ -664,12 +671,12 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
           if (i < halves) {
             ctl->top[buffer][w][r] = top;
             pair_sync();
-            m = fmaxf(top, ctl->top[buffer][w ^ 1][r]);
+            m = fmaxf(top, ctl->top[buffer][w ^ 1][r]) - kHeadroom;
           } else if (pair_any(top > m + kSlack)) {
             ctl->top[buffer][w][r] = top;
             pair_sync();
             const float both = fmaxf(top, ctl->top[buffer][w ^ 1][r]);
-            const float m_new = both > m + kSlack ? both : m;
+            const float m_new = both > m + kSlack ? both - kHeadroom : m;
             const float f = m == m_new ? 1.f : ex2(m - m_new);
             m = m_new;
             sum.x *= f;
@@ -1010,7 +1017,7 @@ __global__ void __launch_bounds__(128, StreamGeometry<D>::kCtas) tree_stream_ker
         for (int h = 0; h < 2; ++h) {
           float x = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 1));
           x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
-          const float r = x > ref[h] + kSlack ? x : ref[h];
+          const float r = x > ref[h] + kSlack ? x - kHeadroom : ref[h];
           const float f = r == ref[h] ? 1.f : ex2(ref[h] - r);
           ref[h] = r;
           sum[h] *= f;

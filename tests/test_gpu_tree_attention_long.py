@@ -25,6 +25,12 @@ def units_of_a_cta(torch, b, mask):
     return units / torch.cuda.get_device_properties(0).multi_processor_count
 
 
+def entries(b, a, s, n):
+    """Batch.entries of layer 0, a page at a time."""
+    pages = a[0, b.table[s, :-(-n // b.page)]]      # [pages][kv_heads][page][dim]
+    return np.ascontiguousarray(pages.transpose(0, 2, 1, 3)).reshape(-1, b.kv_heads, b.dim)[:n]
+
+
 def attention(torch, b, q, mask, scale, seen=None):
     """_paged.attention (the same bounds, all rows of a KV head at a time) on the GPU in 64 bits.  seen: [rows][slots] of every
     sequence instead of what the batch says."""
@@ -35,7 +41,7 @@ def attention(torch, b, q, mask, scale, seen=None):
         r0, r1, n = int(b.row_begin[s]), int(b.row_begin[s + 1]), int(b.ctx[s] + b.nodes[s])
         if r1 == r0:
             continue
-        k, v = (on_gpu(torch, np.ascontiguousarray(b.entries(a, s, 0, n))).double() for a in (b.k, b.v))
+        k, v = (on_gpu(torch, entries(b, a, s, n)).double() for a in (b.k, b.v))
         see = on_gpu(torch, b.sees(s, mask) if seen is None else seen[s])
         k, v = (torch.where(see.any(0)[:, None, None], a, 0.0) for a in (k, v))      # what no row sees may be anything
         for g in range(b.kv_heads):
@@ -315,3 +321,34 @@ def test_two_graphs_of_many_units_replayed_side_by_side(gpu, kind):
         for o, z in zip(outs, lses):
             compare(b, (o.float().cpu().numpy(), z.cpu().numpy()), want)
     del graphs
+
+
+@pytest.mark.parametrize("exponent,dtype", [(12.0, "float16"), (20.0, "float16"), (24.3, "float16"), (25.3, "float16"), (28.0, "float16"), (25.3, "bfloat16")])
+@pytest.mark.parametrize("kind", [*KINDS, "stream whole", "one whole", "two whole"])
+def test_a_long_even_context_under_one_position_that_has_most(gpu, kind, exponent, dtype):
+    """One position has a score so far above all others that each of them has a weight of 2^-exponent of its own; thousands of
+    them count all the same, and must not be rounded away one by one.  "whole": so many sequences that most are not cut."""
+    torch, _ = gpu
+    nodes, ctx = KINDS[kind.split()[0]]
+    n = 1
+    if "whole" in kind:
+        n, ctx = 80, 3000
+    b = Batch(300, ctx=[ctx] * n, nodes=[nodes] * n, page=64, q_heads=16, kv_heads=4, dim=64, dtype=dtype)
+    b.k[:] = 0
+    b.v[:] = _paged.rounded(1 + 0.1 * b.v, dtype)
+    for s in range(n):
+        for j, size in ((5, exponent), (ctx // 2, exponent - 3), (ctx - 70, exponent)):
+            page, row = b.place(s, j)
+            b.k[:, page, :, row, 0] = _paged.rounded(np.array([size], np.float32), dtype)
+            b.v[:, page, :, row] = 0
+    q = np.zeros((b.n_tok, 16, 64), np.float32)
+    q[:, :, 0] = _paged.rounded(np.array([8 * np.log(2.0)], np.float32), dtype)
+    want = list(attention(torch, b, q, None, 0.125))
+    # binary16: p is held as 2^7 and more times its share of the row's largest, so that half a step of its smallest numbers,
+    # 2^-25, is 2^-32 of the largest: 2^(28 - 32), a sixteenth, of the weights here at most
+    if dtype == "float16":
+        for s in range(n):
+            seen = np.abs(entries(b, b.v, s, ctx + nodes)).sum(0)      # [kv_heads][dim]
+            want[2][b.row_begin[s]:b.row_begin[s + 1]] += 2.0 ** -32 * np.repeat(seen, 4, 0)
+    assert np.nanmax(want[2] / want[0]) < 0.2
+    compare(b, run(gpu, b, None, q), want)
