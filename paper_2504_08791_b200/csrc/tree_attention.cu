@@ -21,7 +21,7 @@
 // A segment that is not a whole (sequence, KV head, tile) leaves its maximum, sum and output in the workspace, and
 // tree_merge_kernel joins the parts in ascending order: the same lengths give the same bits.
 // Measured (one B200, both kernels together): 64 nodes, 64 query heads on 8 KV heads of 128, 65,531 positions, fp16:
-// 168 us (0.82 PFLOP/s; 186 to 198 when called for long, the power limit), bound by the softmax, whose eight warps wait,
+// 168 us (0.82 PFLOP/s; 186 to 201 when called for long, the power limit), bound by the softmax, whose eight warps wait,
 // read, take maximum and exponential in step: of about 2400 cycles per sub-unit of 128 x 128 scores the exponentials
 // take 1100 (1024 is what the special-function units need).  16 trees of 1 to 26 nodes over 100 to 8192 positions, 40
 // query heads, bf16: 62 us (2.5 TB/s), half of it beginnings and ends of segments, half waiting for keys.
