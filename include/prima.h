@@ -422,14 +422,14 @@ int prima_tree_attention(prima_paged* pool, int layer, const prima_paged_batch* 
                          void* out, int out_dtype, float* lse, void* workspace, int64_t workspace_bytes, void* stream);
 
 /* One step of a context's layers [layer_begin, layer_end) over a paged cache: as prima_forward_window, for the
- * batch->n_tok (1..max_n_tok) rows of hidden_in / hidden_out, each of its own sequence, at its own position, seeing what
- * the batch says (a chain, a tree of drafted tokens, one token of each of several requests or beams).  The pool takes the
- * place of the context's own caches; layer l of the model is layer l of the pool, whose KV heads, head size, rotation and
- * device must be the model's.  Rotated queries are rounded to the pool's type, as keys and values are (a pool in bfloat16
- * keeps fewer bits of them than the context's own binary16 caches).  The calls run on the context's stream, and the context keeps one workspace for them, which
- * the first call allocates (refused with PRIMA_ERR_STATE while the stream is being captured; later calls may be).  Rows
- * behind the last sequence are computed with whatever their hidden rows hold and appended nowhere; they do not touch the
- * others.  Errors as prima_forward_window. */
+ * batch->n_tok (1..max_n_tok) rows of hidden_in / hidden_out, each of its own sequence, at its own position, seeing
+ * what the batch says (a chain, a tree of drafted tokens, one token of each of several requests or beams).  The pool
+ * takes the place of the context's own caches; layer l of the model is layer l of the pool, whose KV heads, head size,
+ * rotation and device must be the model's.  Rotated queries are rounded to the pool's type, as keys and values are (a
+ * pool in bfloat16 keeps fewer bits of them than the context's own binary16 caches).  The calls run on the context's
+ * stream, and the context keeps one workspace for them, which the first call allocates (refused with PRIMA_ERR_STATE
+ * while the stream is being captured; later calls may be).  Rows behind the last sequence are computed with whatever
+ * their hidden rows hold and appended nowhere; they do not touch the others.  Errors as prima_forward_window. */
 int prima_forward_window_paged(prima_ctx* ctx, prima_paged* pool, int layer_begin, int layer_end, const float* hidden_in, float* hidden_out,
                                const prima_paged_batch* batch);
 
