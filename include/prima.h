@@ -405,6 +405,29 @@ int prima_paged_sync(prima_paged* pool, void* stream);
 int prima_paged_append(prima_paged* pool, int layer, const prima_paged_batch* batch, const void* q, const void* k, const void* v,
                        int in_dtype, int n_q_heads, int64_t q_stride, int64_t k_stride, int64_t v_stride, void* q_out, void* stream);
 
+/* The same with an RMS norm of every query and key head in front of the rotation, and with rotation by positions on
+ * several axes (text: one; images and video: time, height, width).  Head h of row t becomes
+ *     y_d = gain_d * x_d / sqrt(sum_d x_d^2 / head_dim + eps)
+ * (unchanged without a gain), and pair i of it is turned by the angle positions[axis[i]][t] * theta^(-2 rank[i] / head_dim),
+ * or not at all where axis[i] is PRIMA_AXIS_NONE.  Values are not normed and not turned.  Sums and products in 32 bits,
+ * rounded once to the cache's type; a row's slot in the cache is ctx_len + index as ever, whatever its positions. */
+#define PRIMA_AXIS_NONE 255
+#define PRIMA_MAX_AXES 4
+typedef struct {
+  const float* q_gain;         /* dev [head_dim], or NULL: queries are not normed                     */
+  const float* k_gain;         /* dev [head_dim], or NULL: keys are not normed                        */
+  int64_t q_gain_stride;       /* elements from one head's gain to the next one's; 0: one gain for all */
+  int64_t k_gain_stride;
+  float eps;                   /* >= 0, finite                                                        */
+  int32_t n_axes;              /* 1..PRIMA_MAX_AXES                                                   */
+  const int32_t* positions;    /* dev [n_axes][n_tok], or NULL: batch->pos, or the slot, on every axis */
+  uint8_t axis[64];            /* of pair 0 .. head_dim/2 - 1: below n_axes, or PRIMA_AXIS_NONE        */
+  uint8_t rank[64];            /* below head_dim / 2; rank[i] = i is the usual rotation                */
+} prima_head_norm;
+int prima_paged_append_norm(prima_paged* pool, int layer, const prima_paged_batch* batch, const void* q, const void* k, const void* v,
+                            int in_dtype, int n_q_heads, int64_t q_stride, int64_t k_stride, int64_t v_stride, const prima_head_norm* norm,
+                            void* q_out, void* stream);
+
 /* Attention of every row over the positions 0 .. ctx_len-1 of its sequence and over the rows of its own sequence that
  * it sees (mask), all of which must be in the cache: out[t][h] = sum_j p_j v_j, p = softmax(scale * q . k_j), query
  * head h reading KV head h / (n_q_heads / n_kv_heads).  q, out: dev [n_tok][n_q_heads][head_dim], contiguous, 16-byte
@@ -420,6 +443,59 @@ int prima_paged_append(prima_paged* pool, int layer, const prima_paged_batch* ba
 int64_t prima_tree_attention_workspace(const prima_paged* pool, int n_seq, int n_tok, int n_q_heads);
 int prima_tree_attention(prima_paged* pool, int layer, const prima_paged_batch* batch, const void* q, int n_q_heads, float scale,
                          void* out, int out_dtype, float* lse, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Attention of a batch whose sequences share long prefixes (a system prompt, a document, the prompt of beams): as
+ * prima_tree_attention, with the positions of a prefix, all of which every row of its sequences sees, in front of the
+ * sequence's own.  A prefix lies once in the cache, on pages of its own table, and is read once for all rows that share it
+ * (once per 256 of a KV head's rows).  Slots and ctx_len of a sequence count its own positions alone; where the rotation is
+ * to go on behind the prefix, the append needs `pos`.  out, lse, q, scale, masks, types and refusals as there; n_q_heads at
+ * most 64 * n_kv_heads.  A prefix with a negative length or a bad range of sequences counts as none (and raises a status
+ * bit), positions behind its table are not seen.  The value of a position that is seen must be finite.
+ * workspace as there, for the same (n_seq, n_tok, n_q_heads). */
+typedef struct {
+  int32_t n_prefix;            /* >= 1                                                                */
+  const int32_t* seq_begin;    /* dev [n_prefix + 1], ascending in 0..n_seq: sequences seq_begin[p] .. seq_begin[p+1]-1 share
+                                  prefix p; those in front of the first and behind the last have none  */
+  const int32_t* len;          /* dev [n_prefix]: positions                                           */
+  const int32_t* table;        /* dev [n_prefix][table_stride]: page ids                              */
+  int64_t table_stride;        /* 1 .. 2^31 - 1                                                       */
+} prima_prefix;
+int64_t prima_prefix_attention_workspace(const prima_paged* pool, int n_seq, int n_tok, int n_q_heads);
+int prima_prefix_attention(prima_paged* pool, int layer, const prima_paged_batch* batch, const prima_prefix* prefix, const void* q, int n_q_heads,
+                           float scale, void* out, int out_dtype, float* lse, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* The attention weight that the positions of a cache receive in a step, the measure by which a bounded cache is evicted:
+ *     weight_out[s][g][j] = decay * weight_in[s][g][j] + sum over rows i of s and query heads h of KV head g that see slot j
+ *                           of exp(scale * q_ih . k_j - lse[i][h])
+ * for the slots j = 0 .. ctx_len-1 of every sequence that has rows, and the sum alone for those of the step's own rows, which
+ * enter the arrays here: born[s][g][j] = the row's position (batch->pos, or the slot).  lse: dev fp32 [n_tok][n_q_heads], as
+ * prima_tree_attention or prima_prefix_attention has left it (where a prefix took part, its positions have their share); a
+ * row whose lse is -infinity adds nothing.  weight_in (may be NULL: nothing so far; may be weight_out), weight_out: dev fp32
+ * [n_seq][n_kv_heads][stride], stride below 2^31; born: dev int32, the same shape, may be NULL.  Entries behind the rows, and
+ * those of sequences without rows, are left as they were.  A slot on a bad page receives nothing; slots from `stride` on are
+ * left out (and raise a status bit).  q, masks and positions as in prima_tree_attention; scores and sums in 32 bits, always
+ * added in the same order.  decay: 0..1.  For a model's cache the arrays are [n_layers][n_seq][n_kv_heads][stride], of which
+ * a call takes one layer's. */
+int prima_paged_weights(prima_paged* pool, int layer, const prima_paged_batch* batch, const void* q, int n_q_heads, float scale, const float* lse,
+                        const float* weight_in, float* weight_out, int32_t* born, int64_t stride, float decay, void* stream);
+
+/* Eviction: of the length[s] entries that each KV head of each layer holds of sequence s, m = min(keep[s], length[s]) stay,
+ * chosen by head: entries with born < first or born >= recent_from[s] before all others, whatever their weight; the
+ * others by weight (a NaN is less than any number); equal ones by slot, lower first.  The chosen ones in the slots 0 .. m-1 stay where they are; the others move
+ * into the slots that become free there, both in ascending order, so that as little as possible is moved.  Keys, values,
+ * weight and born move together; length_out[s] = m, and the pages behind are free.  Attention does not mind the order
+ * (keys carry their rotation); a later step's rows go to the slots from m on and need `pos`.  The pages of the slots must be
+ * the sequence's own (a shared prefix is kept apart: prima_prefix_attention).
+ * weight, weight_out: dev fp32 [n_layers][n_seq][n_kv_heads][stride]; born, born_out: dev int32, the same shape; keep,
+ * recent_from (NULL: none), length, length_out: dev int32 [n_seq].  weight_out may be weight (and then born_out must be born,
+ * and the other way round), otherwise the arrays must not overlap; entries from m on are left as they were.  length_out may
+ * be length.  A sequence with a negative length or keep, or more positions than stride or the table hold, is left as it is,
+ * length_out = length, and raises a status bit.  stride: at most 2^30.  workspace: dev, 256-byte aligned, as named for the
+ * same (n_seq, stride). */
+int64_t prima_paged_evict_workspace(const prima_paged* pool, int n_seq, int64_t stride);
+int prima_paged_evict(prima_paged* pool, int n_seq, const int32_t* table, int64_t table_stride, const int32_t* length, const float* weight,
+                      const int32_t* born, int64_t stride, const int32_t* keep, int first, const int32_t* recent_from, float* weight_out,
+                      int32_t* born_out, int32_t* length_out, void* workspace, int64_t workspace_bytes, void* stream);
 
 /* One step of a context's layers [layer_begin, layer_end) over a paged cache: as prima_forward_window, for the
  * batch->n_tok (1..max_n_tok) rows of hidden_in / hidden_out, each of its own sequence, at its own position, seeing

@@ -36,6 +36,8 @@ EXPORTS = [
     "prima_forward_window_seqs", "prima_kv_load_seq", "prima_kv_read_seq", "prima_ctx_set_option", "prima_stream_stats",
     "prima_fmt_block_weights", "prima_fmt_block_bytes", "prima_dequant_fmt", "prima_gemv_fmt", "prima_fmt_last_error",
     "prima_paged_create", "prima_paged_destroy", "prima_paged_sync", "prima_paged_append", "prima_paged_accept", "prima_paged_reorder",
+    "prima_paged_append_norm", "prima_paged_weights", "prima_paged_evict", "prima_paged_evict_workspace",
+    "prima_prefix_attention", "prima_prefix_attention_workspace",
     "prima_tree_attention", "prima_tree_attention_workspace", "prima_beam_select", "prima_beam_select_workspace", "prima_forward_window_paged",
 ]
 
@@ -54,6 +56,15 @@ class PagedConfig(C.Structure):
 class PagedBatchDesc(C.Structure):
     _fields_ = [("n_seq", C.c_int32), ("n_tok", C.c_int32), ("row_begin", C.c_void_p), ("ctx_len", C.c_void_p), ("table", C.c_void_p),
                 ("table_stride", C.c_int64), ("pos", C.c_void_p), ("mask", C.c_void_p), ("mask_words", C.c_int32)]
+
+
+class HeadNormDesc(C.Structure):
+    _fields_ = [("q_gain", C.c_void_p), ("k_gain", C.c_void_p), ("q_gain_stride", C.c_int64), ("k_gain_stride", C.c_int64), ("eps", C.c_float),
+                ("n_axes", C.c_int32), ("positions", C.c_void_p), ("axis", C.c_uint8 * 64), ("rank", C.c_uint8 * 64)]
+
+
+class PrefixDesc(C.Structure):
+    _fields_ = [("n_prefix", C.c_int32), ("seq_begin", C.c_void_p), ("len", C.c_void_p), ("table", C.c_void_p), ("table_stride", C.c_int64)]
 
 
 class PrimaError(RuntimeError):
@@ -118,13 +129,22 @@ def lib():
         L.prima_tree_attention.argtypes = [vp, i32, vp, vp, i32, C.c_float, vp, i32, vp, vp, i64, vp]
         L.prima_tree_attention_workspace.argtypes = [vp, i32, i32, i32]
         L.prima_tree_attention_workspace.restype = i64
+        L.prima_paged_append_norm.argtypes = [vp, i32, vp, vp, vp, vp, i32, i32, i64, i64, i64, vp, vp, vp]
+        L.prima_prefix_attention.argtypes = [vp, i32, vp, vp, vp, i32, C.c_float, vp, i32, vp, vp, i64, vp]
+        L.prima_prefix_attention_workspace.argtypes = [vp, i32, i32, i32]
+        L.prima_prefix_attention_workspace.restype = i64
+        L.prima_paged_weights.argtypes = [vp, i32, vp, vp, i32, C.c_float, vp, vp, vp, vp, i64, C.c_float, vp]
+        L.prima_paged_evict.argtypes = [vp, i32, vp, i64, vp, vp, vp, i64, vp, i32, vp, vp, vp, vp, vp, i64, vp]
+        L.prima_paged_evict_workspace.argtypes = [vp, i32, i64]
+        L.prima_paged_evict_workspace.restype = i64
         L.prima_beam_select.argtypes = [vp, i32, i32, i32, i32, i64, vp, vp, i32, i32, vp, vp, vp, vp, i64, vp]
         L.prima_forward_window_paged.argtypes = [vp, vp, i32, i32, vp, vp, vp]
         L.prima_beam_select_workspace.argtypes = [i32, i32, i32, i32]
         L.prima_beam_select_workspace.restype = i64
         for name in EXPORTS:
             if name not in ("prima_last_error", "prima_launch_count", "prima_gemv_q4k_noalloc_error", "prima_fmt_last_error",
-                            "prima_tree_attention_workspace", "prima_beam_select_workspace"):
+                            "prima_tree_attention_workspace", "prima_beam_select_workspace", "prima_prefix_attention_workspace",
+                            "prima_paged_evict_workspace"):
                 getattr(L, name).restype = C.c_int
         _lib = L
     return _lib
@@ -387,6 +407,39 @@ class PagedBatch:
         self._ref = C.byref(self.desc)
 
 
+AXIS_NONE, MAX_AXES = 255, 4
+
+
+class RopeAxes:
+    """Which axis of the positions turns every pair of a head (-1: none does), and the number of its frequency (by default
+    that of the pair)."""
+
+    def __init__(self, axis, rank=None):
+        axis = [int(a) for a in axis]
+        rank = list(range(len(axis))) if rank is None else [int(r) for r in rank]
+        if len(axis) not in (32, 64) or len(rank) != len(axis) or not all(-1 <= a < MAX_AXES for a in axis) or not all(0 <= r < len(axis) for r in rank):
+            raise ValueError(f"one axis (-1 .. {MAX_AXES - 1}) and one frequency for each of the 32 or 64 pairs of a head")
+        self.pairs, self.n_axes = len(axis), max(0, *axis) + 1
+        self.axis = (C.c_uint8 * 64)(*(AXIS_NONE if a < 0 else a for a in axis))
+        self.rank = (C.c_uint8 * 64)(*rank)
+
+
+class PrefixBatch:
+    """prima_prefix: prefixes that sequences of a batch share.  ``table`` int32 [n_prefix, pages], ``length`` int32
+    [n_prefix], ``seq_begin`` int32 [n_prefix + 1] (sequences seq_begin[p] .. seq_begin[p + 1] - 1 share prefix p): contiguous
+    CUDA tensors, read when the kernels run."""
+
+    def __init__(self, table, length, seq_begin):
+        import torch
+        i32, n, dev = torch.int32, length.numel(), length.device
+        if table.dim() != 2 or not table.is_cuda:
+            raise ValueError("table: expected a CUDA tensor [n_prefix, pages]")
+        self.device, self.n_prefix, self._keep = dev, n, (table, length, seq_begin)
+        self.desc = PrefixDesc(n, _need(seq_begin, "seq_begin", i32, (n + 1,), dev), _need(length, "length", i32, (n,), dev),
+                               _need(table, "table", i32, (n, table.shape[1]), dev), table.shape[1])
+        self._ref = C.byref(self.desc)
+
+
 class PagedCache:
     """prima_paged_*: a paged cache over two caller-owned tensors [n_layers, n_pages, n_kv_heads, page_size, head_dim]."""
 
@@ -398,7 +451,7 @@ class PagedCache:
         self.dtype, self.device = k_pages.dtype, k_pages.device
         self._keep = (k_pages, v_pages)
         import torch
-        self._i32, self._f32 = torch.int32, torch.float32
+        self._i32, self._f32, self._one_axis = torch.int32, torch.float32, None
         self._code = _dtype_code(k_pages)
         self._h = C.c_void_p()
         cfg = PagedConfig(*k_pages.shape[:2], self.page_size, self.n_kv_heads, self.head_dim, self._code, rope_theta, rope_mode, self.device.index)
@@ -442,6 +495,118 @@ class PagedCache:
                 raise ValueError("q_out: expected a tensor")
             qo = _need(q_out, "q_out", self.dtype, (n, heads, self.head_dim), self.device)
         rc = self._lib.prima_paged_append(self._h, layer, self._batch(batch), qp, kp, vp, _dtype_code(k), heads, qs, ks, vs, qo, _stream_of(stream, self.device))
+        if rc:
+            _check(rc)
+
+    def append_norm(self, layer: int, batch: PagedBatch, q, k, v, q_out=None, q_gain=None, k_gain=None, eps: float = 1e-6, positions=None,
+                    axes: RopeAxes = None, stream=None):
+        """prima_paged_append_norm: as ``append``, with an RMS norm of every head of q and k in front of the rotation (gains
+        fp32 [head_dim], or [heads, head_dim]; None: not normed) and rotation by ``positions`` int32 [axes, n_tok] (None: the
+        batch's, on every axis) as ``axes`` says (None: one axis for all pairs)."""
+        n, dt = batch.n_tok, k.dtype
+        kp, ks = self._rows(k, "k", n, self.n_kv_heads, dt)
+        vp, vs = self._rows(v, "v", n, self.n_kv_heads, dt)
+        qp = qo = None
+        qs = heads = 0
+        if q is not None:
+            heads = q.shape[1]
+            qp, qs = self._rows(q, "q", n, heads, dt)
+            if q_out is None:
+                raise ValueError("q_out: expected a tensor")
+            qo = _need(q_out, "q_out", self.dtype, (n, heads, self.head_dim), self.device)
+        d = HeadNormDesc(eps=eps)
+        if q_gain is not None:
+            d.q_gain = _need(q_gain, "q_gain", self._f32, (self.head_dim,) if q_gain.dim() == 1 else (heads, self.head_dim), self.device)
+            d.q_gain_stride = 0 if q_gain.dim() == 1 else self.head_dim
+        if k_gain is not None:
+            d.k_gain = _need(k_gain, "k_gain", self._f32, (self.head_dim,) if k_gain.dim() == 1 else (self.n_kv_heads, self.head_dim), self.device)
+            d.k_gain_stride = 0 if k_gain.dim() == 1 else self.head_dim
+        if axes is None:
+            axes = self._one_axis
+            if axes is None:
+                axes = self._one_axis = RopeAxes([0] * (self.head_dim // 2))
+        if axes.pairs != self.head_dim // 2:
+            raise ValueError("axes: expected as many pairs as a head has")
+        d.n_axes, d.axis, d.rank = axes.n_axes, axes.axis, axes.rank
+        if positions is not None:
+            if positions.dim() != 2 or not axes.n_axes <= positions.shape[0] <= MAX_AXES:
+                raise ValueError(f"positions: expected [axes, n_tok] with {axes.n_axes} .. {MAX_AXES} axes")
+            d.n_axes = positions.shape[0]
+            d.positions = _need(positions, "positions", self._i32, (d.n_axes, n), self.device)
+        rc = self._lib.prima_paged_append_norm(self._h, layer, self._batch(batch), qp, kp, vp, _dtype_code(k), heads, qs, ks, vs, C.byref(d), qo,
+                                               _stream_of(stream, self.device))
+        if rc:
+            _check(rc)
+
+    def prefix_attention_workspace(self, batch: PagedBatch, prefix: PrefixBatch, n_q_heads: int = 0, stream=None):
+        """A workspace for ``prefix_attention`` (for any number of query heads if none is named); calls that may overlap need one each."""
+        n = lib().prima_prefix_attention_workspace(self._h, batch.n_seq, batch.n_tok, n_q_heads or 64 * self.n_kv_heads)
+        if n < 0:
+            raise PrimaError(n, "prima_prefix_attention_workspace")
+        return _scratch(n, self.device, stream)
+
+    def prefix_attention(self, layer: int, batch: PagedBatch, prefix: PrefixBatch, q, out, scale=None, lse=None, workspace=None, stream=None):
+        """prima_prefix_attention; ``scale`` defaults to head_dim ** -0.5."""
+        heads = q.shape[1] if q.dim() == 3 else 0
+        shape = (batch.n_tok, heads, self.head_dim)
+        qp = _need(q, "q", self.dtype, shape, self.device)
+        op = _need(out, "out", out.dtype, shape, self.device)
+        lp = _need(lse, "lse", self._f32, shape[:2], self.device) if lse is not None else None
+        if prefix.device != self.device:
+            raise ValueError("the prefixes are on another device than the cache")
+        if workspace is None:
+            workspace = self.prefix_attention_workspace(batch, prefix, heads, stream)
+        elif workspace.device != self.device or not workspace.is_contiguous():
+            raise ValueError(f"workspace: expected a contiguous tensor on {self.device}")
+        rc = self._lib.prima_prefix_attention(self._h, layer, self._batch(batch), prefix._ref, qp, heads, self.head_dim ** -0.5 if scale is None else scale,
+                                              op, _dtype_code(out), lp, workspace.data_ptr(), workspace.nbytes, _stream_of(stream, self.device))
+        if rc:
+            _check(rc)
+
+    def attention_weights(self, layer: int, batch: PagedBatch, q, lse, weight, weight_in=None, decay: float = 1.0, born=None, scale=None, stream=None):
+        """prima_paged_weights: ``weight`` fp32 [n_seq, n_kv_heads, slots] becomes decay * ``weight_in`` (None: nothing so
+        far; may be ``weight``) plus what the slots receive; ``born`` int32 of the same shape, or None."""
+        heads = q.shape[1] if q.dim() == 3 else 0
+        qp = _need(q, "q", self.dtype, (batch.n_tok, heads, self.head_dim), self.device)
+        lp = _need(lse, "lse", self._f32, (batch.n_tok, heads), self.device)
+        if weight.dim() != 3:
+            raise ValueError("weight: expected [n_seq, n_kv_heads, slots]")
+        shape = (batch.n_seq, self.n_kv_heads, weight.shape[2])
+        wp = _need(weight, "weight", self._f32, shape, self.device)
+        ip = _need(weight_in, "weight_in", self._f32, shape, self.device) if weight_in is not None else None
+        bp = _need(born, "born", self._i32, shape, self.device) if born is not None else None
+        rc = self._lib.prima_paged_weights(self._h, layer, self._batch(batch), qp, heads, self.head_dim ** -0.5 if scale is None else scale, lp, ip, wp, bp,
+                                           shape[2], decay, _stream_of(stream, self.device))
+        if rc:
+            _check(rc)
+
+    def evict_workspace(self, n_seq: int, slots: int, stream=None):
+        """A workspace for ``evict``; calls that may overlap need one each."""
+        n = lib().prima_paged_evict_workspace(self._h, n_seq, slots)
+        if n < 0:
+            raise PrimaError(n, "prima_paged_evict_workspace: sizes out of range")
+        return _scratch(n, self.device, stream)
+
+    def evict(self, table, length, weight, born, keep, length_out, weight_out=None, born_out=None, first: int = 0, recent_from=None, workspace=None,
+              stream=None):
+        """prima_paged_evict: ``table`` int32 [n_seq, pages]; ``length``, ``keep``, ``length_out``, ``recent_from`` (or None) int32
+        [n_seq]; ``weight`` fp32 and ``born`` int32 [n_layers, n_seq, n_kv_heads, slots], changed in place unless
+        ``weight_out`` and ``born_out`` are given."""
+        if weight.dim() != 4 or table.dim() != 2:
+            raise ValueError("weight: expected [n_layers, n_seq, n_kv_heads, slots]; table: [n_seq, pages]")
+        dev, i32, n_seq = self.device, self._i32, table.shape[0]
+        shape = (self.n_layers, n_seq, self.n_kv_heads, weight.shape[3])
+        weight_out, born_out = weight if weight_out is None else weight_out, born if born_out is None else born_out
+        if workspace is None:
+            workspace = self.evict_workspace(n_seq, shape[3], stream)
+        elif workspace.device != dev or not workspace.is_contiguous():
+            raise ValueError(f"workspace: expected a contiguous tensor on {dev}")
+        rc = self._lib.prima_paged_evict(self._h, n_seq, _need(table, "table", i32, (n_seq, table.shape[1]), dev), table.shape[1], _need(length, "length", i32, (n_seq,), dev),
+                                         _need(weight, "weight", self._f32, shape, dev), _need(born, "born", i32, shape, dev), shape[3],
+                                         _need(keep, "keep", i32, (n_seq,), dev), first,
+                                         _need(recent_from, "recent_from", i32, (n_seq,), dev) if recent_from is not None else None,
+                                         _need(weight_out, "weight_out", self._f32, shape, dev), _need(born_out, "born_out", i32, shape, dev),
+                                         _need(length_out, "length_out", i32, (n_seq,), dev), workspace.data_ptr(), workspace.nbytes, _stream_of(stream, dev))
         if rc:
             _check(rc)
 

@@ -1,0 +1,146 @@
+// What the attention kernels over the paged cache share on the device: bounded waits, masks, the softmax's arithmetic,
+// copies and fragments.
+#pragma once
+
+#include "paged.cuh"
+#include "tcgen05.cuh"
+
+namespace prima {
+
+// ---- constants -------------------------------------------------------------------------------------------------------
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
+// Binary exponents: a reference is set kHeadroom below the row's maximum and stays until a score exceeds it by kSlack.  A
+// row's largest probability is held as 2^7 to 2^15 (binary16 ends at 65504), not as 1: what binary16 rounds below its normal
+// numbers, by up to 2^-25, is then 2^-32 of the largest, and thousands of positions that have 2^-25 of its weight
+// each are not rounded away one by one.
+constexpr float kHeadroom = 7.f, kSlack = 15.f;
+
+__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, int* give_up, int* status) {
+  for (int i = 0; i < (1 << 22); ++i) {
+    if (mbar_test(bar, parity)) return true;
+    if (*static_cast<volatile int*>(give_up)) return false;
+  }
+  *static_cast<volatile int*>(give_up) = 1;
+  raise(status, kGaveUp);
+  return false;
+}
+
+// ---- what a row sees ------------------------------------------------------------------------------------------------
+// Bits for 32 positions from `pos` on.  a = index of the position among the rows of the step, negative in the context.
+__device__ __forceinline__ uint32_t low_bits(long long n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << static_cast<int>(n)) - 1u; }
+__device__ __forceinline__ uint32_t mask_word(const uint32_t* words, int n_words, long long i) { return i < n_words ? __ldg(words + i) : 0u; }
+__device__ __forceinline__ uint32_t tree_bits(const uint32_t* words, int n_words, long long a) {
+  if (a <= -32) return 0xffffffffu;
+  if (a < 0) return mask_word(words, n_words, 0) << static_cast<int>(-a) | low_bits(-a);
+  return __funnelshift_r(mask_word(words, n_words, a >> 5), mask_word(words, n_words, (a >> 5) + 1), static_cast<uint32_t>(a) & 31u);
+}
+
+// ---- arithmetic ------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// A row that sees nothing has a sum of 0: its output is 0, its log-sum-exp -infinity.  A NaN stays one.
+__device__ __forceinline__ float inverse_of(float total) { return total == 0.f ? 0.f : 1.f / total; }
+__device__ __forceinline__ float log_sum(float reference, float total) {
+  constexpr float kDown = 1.f / 128.f;      // 2^-kHeadroom
+  return total == 0.f ? -INFINITY : (reference + kHeadroom + log2f(total * kDown)) * kLn2;
+}
+
+// Two 32-bit operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 x, float2 y, float2 z) {
+  unsigned long long d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(*reinterpret_cast<unsigned long long*>(&x)), "l"(*reinterpret_cast<unsigned long long*>(&y)),
+      "l"(*reinterpret_cast<unsigned long long*>(&z)));
+  return *reinterpret_cast<float2*>(&d);
+}
+__device__ __forceinline__ float2 add2(float2 x, float2 y) {
+  unsigned long long d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*reinterpret_cast<unsigned long long*>(&x)), "l"(*reinterpret_cast<unsigned long long*>(&y)));
+  return *reinterpret_cast<float2*>(&d);
+}
+__device__ __forceinline__ float max3(float x, float y, float z) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(x), "f"(y), "f"(z));
+  return d;
+}
+__device__ __forceinline__ float max_of(const uint32_t (&x)[32], float top) {
+  float t[4] = {top, __uint_as_float(x[0]), __uint_as_float(x[1]), __uint_as_float(x[2])};
+#pragma unroll
+  for (int j = 3; j + 1 < 32; j += 2) t[j / 2 & 3] = max3(t[j / 2 & 3], __uint_as_float(x[j]), __uint_as_float(x[j + 1]));
+  return fmaxf(max3(t[0], t[1], t[2]), fmaxf(t[3], __uint_as_float(x[31])));
+}
+
+template <typename T>
+__device__ __forceinline__ void store4(T* dst, float4 x) {
+  *reinterpret_cast<uint2*>(dst) = make_uint2(Half2Of<T>::pack(x.x, x.y), Half2Of<T>::pack(x.z, x.w));
+}
+template <>
+__device__ __forceinline__ void store4<float>(float* dst, float4 x) { *reinterpret_cast<float4*>(dst) = x; }
+
+// 32 columns of a row of the result, scaled.
+template <typename T>
+__device__ __forceinline__ void store_row(T* dst, const float (&x)[32]) {
+#pragma unroll
+  for (int i = 0; i < 32; i += 8) {
+    const float y[8] = {x[i], x[i + 1], x[i + 2], x[i + 3], x[i + 4], x[i + 5], x[i + 6], x[i + 7]};
+    store8(dst + i, y);
+  }
+}
+template <>
+__device__ __forceinline__ void store_row<float>(float* dst, const float (&x)[32]) {
+#pragma unroll
+  for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(dst + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+}
+
+// A place of the ring, stepped without divisions.
+template <int kSlots>
+struct RingPlace {
+  uint32_t slot = 0, phase = 0;
+  __device__ __forceinline__ void step(uint32_t n) {      // n <= kSlots
+    slot += n;
+    if (slot >= kSlots) {
+      slot -= kSlots;
+      phase ^= 1;
+    }
+  }
+  __device__ __forceinline__ void skip(int n) {
+    for (; n > 0; n -= kSlots) step(min(n, kSlots));
+  }
+};
+
+// 16 bytes to shared memory in the background; zeros where there is nothing to copy.
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+
+// ---- fragments of m16n8k16 -------------------------------------------------------------------------------------------
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+template <bool kBf16>
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if constexpr (kBf16)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------------
+template <typename Kernel>
+inline cudaError_t allow_smem(Kernel kernel, size_t bytes, bool (&done)[kMaxDevices]) {
+  int dev;
+  if (!first_launch_on_device(done, &dev)) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+  if (e == cudaSuccess && dev >= 0) done[dev] = true;
+  return e;
+}
+
+}  // namespace prima

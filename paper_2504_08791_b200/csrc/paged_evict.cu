@@ -1,0 +1,315 @@
+// Eviction from the paged cache: of a sequence's entries, those of largest weight stay and come together in front.
+//
+// Every (layer, sequence, KV head) chooses for itself, so a batch has hundreds of independent choices.  One kernel makes
+// them, a CTA each, and lists what moves; a second one moves keys, values, weights and positions with the whole GPU,
+// however few the choices are.  Moving only what lies behind slot m, into the free slots in front of it, costs
+// m (n - m) / n entries of n where a compaction in order would move nearly all m.
+#include <algorithm>
+#include <cstdio>
+
+#include "paged.cuh"
+
+namespace prima {
+namespace {
+
+constexpr int kThreads = 512, kWarps = kThreads / 32, kPer = 4, kTile = kThreads * kPer;
+constexpr int kBins = 2048, kDigits = 3;              // digits of 11, 11 and 10 bits
+// Keys that a CTA keeps in shared memory; those behind are made from the arrays again in every pass.  With 39 KB of keys
+// four CTAs share an SM, so that 592 choices run at once.
+constexpr int kCached = 10000;
+
+struct EvictArgs {
+  PoolView pool;
+  int n_seq;
+  const int32_t* table;
+  int64_t table_stride;
+  const int32_t* length;
+  const float* weight;
+  const int32_t* born;
+  int64_t stride;
+  const int32_t* keep;
+  int first;
+  const int32_t* recent_from;
+  float* weight_out;
+  int32_t* born_out;
+  int32_t* length_out;
+  int32_t* counts;      // [items]
+  int32_t* lists;       // [items][2][half]: free slots in front, chosen ones behind
+  int64_t half;
+  int cached;
+};
+
+// What the numbers of a sequence say; n < 0: they are bad.
+struct Sizes {
+  int n, m;
+};
+__device__ __forceinline__ Sizes sizes_of(const EvictArgs& a, int seq, int* length) {
+  const int n = __ldg(a.length + seq), keep = __ldg(a.keep + seq);
+  *length = n;
+  if (n < 0 || keep < 0 || n > a.stride || n > (a.table_stride << a.pool.page_shift)) return {-1, 0};
+  return {n, min(n, keep)};
+}
+
+// Larger is kept.  Whole numbers in the order of the weights: NaN below all, -0 equal to 0, protected entries above all.
+__device__ __forceinline__ uint32_t key_of(float w, bool is_protected) {
+  if (is_protected) return 0xffffffffu;
+  if (w != w) return 0u;
+  const uint32_t u = __float_as_uint(w + 0.f);
+  return u >> 31 ? ~u : u | 0x80000000u;
+}
+
+// Inclusive sums over the threads of the CTA; `total` is the sum of all.  Two barriers.
+__device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t* s_warp, uint32_t* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  __syncthreads();
+  if (lane == 31) s_warp[warp] = x;
+  __syncthreads();
+  uint32_t before = 0, all = 0;
+#pragma unroll
+  for (int i = 0; i < kWarps; ++i) {
+    const uint32_t y = s_warp[i];
+    before += i < warp ? y : 0u;
+    all += y;
+  }
+  *total = all;
+  return x + before;
+}
+
+// The m-th largest key by its digits, from the top: a histogram of the digit among the keys that agree with those found so
+// far, and the bin in which the count from above reaches what is still wanted.
+__global__ void __launch_bounds__(kThreads) evict_choose_kernel(const __grid_constant__ EvictArgs a) {
+  extern __shared__ uint32_t s_key[];
+  __shared__ uint32_t s_hist[kBins];
+  __shared__ uint32_t s_warp[kWarps];
+  __shared__ uint32_t s_found[2];      // bin, keys above it
+  const int item = blockIdx.x, head = item % a.pool.n_kv_heads, seq = item / a.pool.n_kv_heads % a.n_seq, tid = threadIdx.x;
+  pdl_trigger();
+  pdl_wait();
+  int length;
+  const Sizes z = sizes_of(a, seq, &length);
+  const int n = z.n, m = z.m;
+  if (n < 0 && tid == 0 && item / a.pool.n_kv_heads < a.n_seq && head == 0) raise(a.pool.status, length < 0 || __ldg(a.keep + seq) < 0 ? kBadRows : kBadSlot);
+  const int64_t at = static_cast<int64_t>(item) * a.stride;
+  const float* const weight = a.weight + at;
+  const int32_t* const born = a.born + at;
+  const bool apart = a.weight_out != a.weight;
+  if (n <= m || m == 0) {      // all stay, none, or bad numbers
+    if (tid == 0) a.counts[item] = 0;
+    if (apart)
+      for (int j = tid; j < m; j += kThreads) {
+        a.weight_out[at + j] = weight[j];
+        a.born_out[at + j] = born[j];
+      }
+    return;
+  }
+  const bool some_recent = a.recent_from != nullptr;
+  const int recent_from = some_recent ? __ldg(a.recent_from + seq) : 0;
+  auto make = [&](int j) {
+    const int b = born[j];
+    return key_of(weight[j], b < a.first || (some_recent && b >= recent_from));
+  };
+  for (int j = tid; j < min(n, a.cached); j += kThreads) s_key[j] = make(j);
+  auto key = [&](int j) { return j < a.cached ? s_key[j] : make(j); };
+
+  uint32_t prefix = 0, above = 0;      // digits found; keys that are larger
+  for (int d = 0; d < kDigits; ++d) {
+    const int shift = d == 0 ? 21 : d == 1 ? 10 : 0, bins = d == 2 ? 1024 : 2048;
+    for (int i = tid; i < bins; i += kThreads) s_hist[i] = 0;
+    __syncthreads();
+    for (int j = tid; j < n; j += kThreads) {
+      const uint32_t k = key(j);
+      if (d == 0 || k >> (d == 1 ? 21 : 10) == prefix) atomicAdd(&s_hist[(k >> shift) & (bins - 1)], 1u);
+    }
+    __syncthreads();
+    // thread t sums the bins below bins - t * per
+    const int per = bins / kThreads, top = bins - tid * per;
+    uint32_t mine = 0, total;
+    for (int i = 1; i <= per; ++i) mine += s_hist[top - i];
+    uint32_t upto = block_scan(mine, s_warp, &total);
+    const uint32_t wanted = m - above;
+    if (upto >= wanted && upto - mine < wanted) {      // one thread
+      uint32_t sum = upto - mine;
+      int i = 1;
+      while (sum + s_hist[top - i] < wanted) sum += s_hist[top - i++];
+      s_found[0] = top - i;
+      s_found[1] = sum;
+    }
+    __syncthreads();
+    prefix = d == 0 ? s_found[0] : prefix << (d == 1 ? 11 : 10) | s_found[0];
+    above += s_found[1];
+    __syncthreads();
+  }
+  const uint32_t border = prefix, wanted = m - above;      // of the keys equal to the border, the first `wanted` stay
+
+  int32_t* const holes = a.lists + 2 * a.half * item;
+  int32_t* const movers = holes + a.half;
+  uint32_t equal_before = 0, holes_before = 0, movers_before = 0, total;
+  for (int j0 = 0; j0 < n; j0 += kTile) {
+    const int j = j0 + tid * kPer;
+    uint32_t k[kPer], equal = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      k[i] = j + i < n ? key(j + i) : 0u;
+      equal += j + i < n && k[i] == border ? 1u : 0u;
+    }
+    uint32_t rank = equal_before + block_scan(equal, s_warp, &total) - equal;
+    equal_before += total;
+    uint32_t kept = 0, count = 0;      // holes in the lower half, movers in the upper one: 2048 at most each
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      if (j + i >= n) continue;
+      const bool stays = k[i] > border || (k[i] == border && rank < wanted);
+      rank += k[i] == border;
+      kept |= stays ? 1u << i : 0u;
+      count += j + i < m ? (stays ? 0u : 1u) : (stays ? 1u << 16 : 0u);
+    }
+    const uint32_t upto = block_scan(count, s_warp, &total) - count;
+    uint32_t hole = holes_before + (upto & 0xffffu), mover = movers_before + (upto >> 16);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      if (j + i >= n) continue;
+      const bool stays = kept >> i & 1;
+      if (j + i >= m) {
+        if (stays) movers[mover++] = j + i;
+      } else if (!stays) {
+        holes[hole++] = j + i;
+      } else if (apart) {
+        a.weight_out[at + j + i] = weight[j + i];
+        a.born_out[at + j + i] = born[j + i];
+      }
+    }
+    holes_before += total & 0xffffu;
+    movers_before += total >> 16;
+  }
+  if (tid == 0) a.counts[item] = static_cast<int>(holes_before);
+}
+
+// blockIdx.x = (layer, sequence, KV head); its warps share the moves.  A warp takes the key and the value of 32 / (D / 4)
+// entries at a time, 16 bytes a lane, kFlight times in flight.
+template <int D>
+__global__ void __launch_bounds__(256) evict_move_kernel(const __grid_constant__ EvictArgs a) {
+  constexpr int kPieces = D / 8, kEntries = 16 / kPieces, kFlight = 4;
+  const int item = blockIdx.x, head = item % a.pool.n_kv_heads, ls = item / a.pool.n_kv_heads, seq = ls % a.n_seq, layer = ls / a.n_seq;
+  const int lane = threadIdx.x & 31, warp = blockIdx.y * 8 + (threadIdx.x >> 5), n_warps = gridDim.y * 8;
+  pdl_trigger();
+  pdl_wait();
+  if (item < a.n_seq * a.pool.n_kv_heads && head == 0 && blockIdx.y == 0 && threadIdx.x == 0) {      // the choices have read `length`
+    int length;
+    const Sizes z = sizes_of(a, seq, &length);
+    a.length_out[seq] = z.n < 0 ? length : z.m;
+  }
+  const int count = __ldg(a.counts + item);
+  const int32_t* const holes = a.lists + 2 * a.half * item;
+  const int32_t* const movers = holes + a.half;
+  const int32_t* const table = a.table + seq * a.table_stride;
+  const int64_t at = static_cast<int64_t>(item) * a.stride;
+  const int entry = lane / (2 * kPieces), piece = lane % kPieces, is_v = lane / kPieces & 1;
+  uint4* const base = static_cast<uint4*>(is_v ? a.pool.v : a.pool.k) + piece;
+  for (int i0 = warp * kEntries * kFlight; i0 < count; i0 += n_warps * kEntries * kFlight) {
+    uint4 x[kFlight];
+    int64_t to[kFlight];
+    int hole[kFlight], mover[kFlight];
+#pragma unroll
+    for (int f = 0; f < kFlight; ++f) {
+      const int i = i0 + f * kEntries + entry;
+      hole[f] = i < count ? __ldg(holes + i) : -1;
+      mover[f] = i < count ? __ldg(movers + i) : -1;
+    }
+#pragma unroll
+    for (int f = 0; f < kFlight; ++f) {
+      to[f] = -1;
+      if (hole[f] < 0) continue;
+      const int64_t from = slot_row(a.pool, table, a.table_stride, layer, mover[f]);
+      to[f] = slot_row(a.pool, table, a.table_stride, layer, hole[f]);
+      if (from < 0) to[f] = -1;
+      if (to[f] >= 0) x[f] = __ldcg(base + (from + (static_cast<int64_t>(head) << a.pool.page_shift)) * kPieces);
+    }
+#pragma unroll
+    for (int f = 0; f < kFlight; ++f) {
+      if (to[f] >= 0) base[(to[f] + (static_cast<int64_t>(head) << a.pool.page_shift)) * kPieces] = x[f];
+      if (hole[f] >= 0 && lane % (2 * kPieces) == 0) a.weight_out[at + hole[f]] = a.weight[at + mover[f]];
+      if (hole[f] >= 0 && lane % (2 * kPieces) == 1) a.born_out[at + hole[f]] = a.born[at + mover[f]];
+    }
+  }
+}
+
+int64_t padded(int64_t n) { return (n + 255) / 256 * 256; }
+
+}  // namespace
+}  // namespace prima
+
+using namespace prima;
+
+extern "C" {
+
+int64_t prima_paged_evict_workspace(const prima_paged* p, int n_seq, int64_t stride) {
+  if (!p || n_seq < 1 || stride < 1 || stride > (1 << 30)) return PRIMA_ERR_ARG;
+  const int64_t items = static_cast<int64_t>(p->cfg.n_layers) * n_seq * p->cfg.n_kv_heads;
+  if (items > 2147483647) return PRIMA_ERR_ARG;
+  return padded(items * 4) + padded(items * 2 * ((stride + 1) / 2) * 4);
+}
+
+int prima_paged_evict(prima_paged* p, int n_seq, const int32_t* table, int64_t table_stride, const int32_t* length, const float* weight,
+                      const int32_t* born, int64_t stride, const int32_t* keep, int first, const int32_t* recent_from, float* weight_out,
+                      int32_t* born_out, int32_t* length_out, void* workspace, int64_t workspace_bytes, void* stream) {
+  auto refuse = [](const char* what) {
+    char msg[160];
+    snprintf(msg, sizeof msg, "prima_paged_evict: %s", what);
+    return call_fail(PRIMA_ERR_ARG, msg);
+  };
+  if (!p || !table || !length || !weight || !born || !keep || !weight_out || !born_out || !length_out) return refuse("null argument");
+  if (n_seq < 1 || table_stride < 1 || table_stride > 2147483647 || stride < 1 || stride > (1 << 30)) return refuse("bad size");
+  for (const void* x : {static_cast<const void*>(table), static_cast<const void*>(length), static_cast<const void*>(weight), static_cast<const void*>(born),
+                        static_cast<const void*>(keep), static_cast<const void*>(recent_from), static_cast<const void*>(weight_out),
+                        static_cast<const void*>(born_out), static_cast<const void*>(length_out)})
+    if (!aligned_to(x, 4)) return refuse("an array is not 4-byte aligned");
+  const int64_t items = static_cast<int64_t>(p->cfg.n_layers) * n_seq * p->cfg.n_kv_heads;
+  if (items > 2147483647) return refuse("layers * sequences * KV heads reach 2^31");
+  // Entries that move are read by one CTA and written by another: either the arrays are the same, entry for entry, or apart.
+  const bool same = weight == weight_out;
+  if (same != (born == born_out)) return refuse("weight_out is weight, but born_out is not born, or the other way round");
+  auto overlap = [&](const void* x, const void* y, int64_t n) {
+    const char *a = static_cast<const char*>(x), *b = static_cast<const char*>(y);
+    return a < b + 4 * n && b < a + 4 * n;
+  };
+  if (!same && (overlap(weight, weight_out, items * stride) || overlap(born, born_out, items * stride))) return refuse("the new arrays overlap the old ones");
+  if (length != length_out && overlap(length, length_out, n_seq)) return refuse("length_out overlaps length");
+  if (!workspace || !aligned_to(workspace, 256) || workspace_bytes < prima_paged_evict_workspace(p, n_seq, stride))
+    return refuse("workspace too small or not 256-byte aligned");
+  CallDevice dev(p->cfg.device);
+  if (!dev.ok) return call_fail(PRIMA_ERR_CUDA, "cudaSetDevice failed");
+  EvictArgs a;
+  a.pool = view_of(*p);
+  a.n_seq = n_seq;
+  a.table = table;
+  a.table_stride = table_stride;
+  a.length = length;
+  a.weight = weight;
+  a.born = born;
+  a.stride = stride;
+  a.keep = keep;
+  a.first = first;
+  a.recent_from = recent_from;
+  a.weight_out = weight_out;
+  a.born_out = born_out;
+  a.length_out = length_out;
+  a.counts = static_cast<int32_t*>(workspace);
+  a.lists = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + padded(items * 4));
+  a.half = (stride + 1) / 2;
+  a.cached = static_cast<int>(std::min<int64_t>(stride, kCached));
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cudaError_t e = launch_pdl(evict_choose_kernel, dim3(static_cast<unsigned>(items)), dim3(kThreads), a.cached * sizeof(uint32_t), st, a);
+  // CTAs of a choice's moves: enough that a few choices fill the GPU
+  const int64_t share = std::max<int64_t>(1, (16 * static_cast<int64_t>(p->sm_count) + items - 1) / items);
+  const int64_t most = (a.half + 31) / 32;
+  const dim3 grid(static_cast<unsigned>(items), static_cast<unsigned>(std::min<int64_t>({share, most, 65535})));
+  if (e == cudaSuccess) e = launch_pdl(p->cfg.head_dim == 128 ? evict_move_kernel<128> : evict_move_kernel<64>, grid, dim3(256), 0, st, a);
+  return e == cudaSuccess ? PRIMA_OK : call_cuda_fail(e, "prima_paged_evict");
+}
+
+}  // extern "C"
