@@ -129,4 +129,67 @@ PRIMA_HD TreeSegment tree_segment(const TreeShape& t, int ctx, int nodes, int64_
   return s;
 }
 
+// ---- how the work of attention over shared prefixes is dealt out ---------------------------------------------------
+// The rows of all sequences behind a prefix that read one KV head (in their order in the step) are cut into tiles of
+// kPrefixRows, the prefix into units of kTilePos positions, as above.  A tile has two accumulators of half its rows.  Where
+// it has more than half of them, each unit takes both accumulators in turn, two places of the line; a tile of at most
+// half the rows takes its units with one accumulator each, alternately, and a unit is one place.  A unit belongs to the
+// worker that has its first place.
+constexpr int kPrefixRows = 256;
+
+struct PrefixShape {
+  int n_kv_heads;
+  int64_t capacity;          // positions that a row of the prefixes' table can name
+  int overhead;              // what a segment costs besides its units, in places
+};
+
+PRIMA_HD int64_t prefix_units(const PrefixShape& t, int len) { return ((len < t.capacity ? len : t.capacity) + kTilePos - 1) / kTilePos; }
+PRIMA_HD int prefix_weight(int64_t rows, int64_t row_tile) { return rows - row_tile * kPrefixRows > kPrefixRows / 2 ? 2 : 1; }
+// Places in the line of one KV head of a prefix with this many rows.
+PRIMA_HD int64_t prefix_places(const PrefixShape& t, int64_t rows, int64_t units) {
+  if (rows <= 0 || units <= 0) return 0;
+  const int64_t last = (rows - 1) / kPrefixRows;
+  return last * (t.overhead + 2 * units) + t.overhead + prefix_weight(rows, last) * units;
+}
+
+struct PrefixSegment {
+  int head;
+  int64_t row_tile;
+  int unit0, unit1;          // none where the share has only places at the head, or the second one of a unit
+  int64_t places;            // of this share
+  int64_t first, last;       // place at which the first and the last unit of the whole (prefix, KV head, tile) begin
+};
+// The segment at place u of a prefix whose KV heads have `per_head` places each; it ends at or before place u_end.
+PRIMA_HD PrefixSegment prefix_segment(const PrefixShape& t, int64_t rows, int64_t units, int64_t per_head, int64_t u, int64_t u_end) {
+  PrefixSegment s;
+  s.head = static_cast<int>(div_small(u, per_head));
+  const int64_t r = u - s.head * per_head, last = (rows - 1) / kPrefixRows, full = t.overhead + 2 * units;
+  s.row_tile = div_small(r, full);
+  if (s.row_tile > last) s.row_tile = last;
+  const int weight = prefix_weight(rows, s.row_tile);
+  const int64_t in_tile = r - s.row_tile * full, to_end = t.overhead + weight * units - in_tile;
+  s.places = to_end < u_end - u ? to_end : u_end - u;
+  const int64_t p0 = in_tile - t.overhead, p1 = p0 + s.places;
+  s.unit0 = static_cast<int>(p0 > 0 ? (p0 + weight - 1) / weight : 0);
+  s.unit1 = static_cast<int>(p1 > 0 ? (p1 + weight - 1) / weight : 0);
+  s.first = u - p0;
+  s.last = s.first + weight * (units - 1);
+  return s;
+}
+
+// How many of n_cta workers take the prefixes' places, the others the sequences' own, of which one costs own_cost / 8 of
+// a prefix's.  Every worker of the prefixes has two places at least, so that it begins a unit in every tile that it
+// passes through.
+PRIMA_HD int prefix_workers(int64_t places, int64_t own, int own_cost, int n_cta) {
+  if (places <= 0) return 0;
+  int n = n_cta;
+  if (own > 0) {
+    const double p = 8.0 * static_cast<double>(places), o = static_cast<double>(own_cost) * static_cast<double>(own);
+    n = static_cast<int>(p / (p + o) * n_cta + 0.5);
+    if (n > n_cta - 1) n = n_cta - 1;
+  }
+  if (n > places / 2) n = static_cast<int>(places / 2);
+  return n < 1 ? 1 : n;
+}
+
 }  // namespace prima

@@ -54,3 +54,92 @@ def test_choices_of_an_eviction():
     assert _prefix.choose(w, born, 8, 2, 1, 6)[0].tolist() == [0, 6]        # protected entries are equal among themselves
     assert _prefix.choose(w, born, 8, 7, 0, None)[0].tolist() == [0, 1, 3, 4, 5, 6, 7]
     assert _prefix.choose(w, born, 2, 7, 0, None)[1].tolist() == [0, 1]
+
+
+@pytest.fixture(scope="module")
+def index(tmp_path_factory):
+    """The index arithmetic of the shared prefixes, compiled for the host."""
+    import os
+    import subprocess
+    at = tmp_path_factory.mktemp("prefix_index")
+    src, out = str(at / "x.cpp"), str(at / "x.so")
+    header = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2504_08791_b200", "csrc", "paged_index.h")
+    with open(src, "w") as f:
+        f.write(f'''#include "{header}"
+using namespace prima;
+extern "C" {{
+long long places(int heads, long long cap, int over, long long rows, int len) {{ PrefixShape t{{heads, cap, over}}; return prefix_places(t, rows, prefix_units(t, len)); }}
+long long units(int heads, long long cap, int over, int len) {{ PrefixShape t{{heads, cap, over}}; return prefix_units(t, len); }}
+int workers(long long p, long long o, int cost, int n) {{ return prefix_workers(p, o, cost, n); }}
+long long begin(long long total, int n, int c) {{ return tree_share_begin(tree_shares(total, n), c); }}
+int owner(long long total, int n, long long u) {{ return tree_cta_of(tree_shares(total, n), u); }}
+void segment(int heads, long long cap, int over, long long rows, int len, long long u, long long end, long long* out) {{
+  PrefixShape t{{heads, cap, over}};
+  const long long n = prefix_units(t, len);
+  const PrefixSegment s = prefix_segment(t, rows, n, prefix_places(t, rows, n), u, end);
+  out[0] = s.head; out[1] = s.row_tile; out[2] = s.unit0; out[3] = s.unit1; out[4] = s.places; out[5] = s.first; out[6] = s.last;
+}}
+}}''')
+    subprocess.run(["g++", "-O1", "-shared", "-fPIC", "-std=c++17", "-o", out, src], check=True)
+    L = ctypes.CDLL(out)
+    i64, i32 = ctypes.c_longlong, ctypes.c_int
+    L.places.argtypes, L.places.restype = [i32, i64, i32, i64, i32], i64
+    L.units.argtypes, L.units.restype = [i32, i64, i32, i32], i64
+    L.workers.argtypes = [i64, i64, i32, i32]
+    L.begin.argtypes, L.begin.restype = [i64, i32, i32], i64
+    L.owner.argtypes = [i64, i32, i64]
+    L.segment.argtypes = [i32, i64, i32, i64, i32, i64, i64, ctypes.POINTER(i64)]
+    return L
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_shares_of_the_prefixes_cover_every_unit_once(index, seed):
+    """Every unit of every (prefix, KV head, tile) belongs to one worker; the workers of a tile are consecutive and each has a
+    unit; the first and the last are those that the places name."""
+    rs = np.random.RandomState(seed)
+    heads, over, n_cta = int(rs.randint(1, 9)), 4, int(rs.choice([2, 3, 7, 148]))
+    n_prefix = int(rs.choice([1, 1, 2, 5]))
+    rows = rs.choice([0, 1, 16, 127, 128, 129, 255, 256, 257, 384, 385, 512, 1000], n_prefix)
+    length = rs.choice([0, 1, 127, 128, 129, 500, 3000, 40000], n_prefix)
+    cap = int(rs.choice([100, 1024, 1 << 20]))
+    per_head = [index.places(heads, cap, over, int(r), int(n)) for r, n in zip(rows, length)]
+    total = sum(per_head) * heads
+    own = int(rs.choice([0, 5, 1000]))
+    n = index.workers(total, own, 16, n_cta)
+    if total == 0:
+        assert n == 0
+        return
+    assert 1 <= n <= (n_cta if own == 0 else n_cta - 1) and (n == 1 or total // n >= 2)
+    front = np.concatenate([[0], np.cumsum([p * heads for p in per_head])])
+    seen, out = {}, (ctypes.c_longlong * 7)()
+    for c in range(n):
+        u, end = index.begin(total, n, c), index.begin(total, n, c + 1)
+        while u < end:
+            p = int(np.searchsorted(front, u, side="right")) - 1
+            while per_head[p] == 0:
+                p += 1
+            index.segment(heads, cap, over, int(rows[p]), int(length[p]), u - int(front[p]), end - int(front[p]), out)
+            head, tile, unit0, unit1, places, first, last = list(out)
+            assert 0 <= head < heads and 0 <= tile <= (rows[p] - 1) // 256 and places > 0 and 0 <= unit0 <= unit1
+            if unit1 > unit0:
+                seen.setdefault((p, head, tile), []).append((c, unit0, unit1))
+                if unit0 == 0:
+                    assert index.owner(total, n, first + int(front[p])) == c
+                last_owner = index.owner(total, n, last + int(front[p]))
+                assert last_owner >= c and (unit1 == index.units(heads, cap, over, int(length[p]))) == (last_owner == c)
+            u += places
+        assert u == end
+    for p in range(n_prefix):
+        units = index.units(heads, cap, over, int(length[p]))
+        for head in range(heads):
+            for tile in range(-(-int(rows[p]) // 256) if units else 0):
+                parts = seen.pop((p, head, tile))
+                assert [x[1] for x in parts] == [0] + [x[2] for x in parts[:-1]] and parts[-1][2] == units
+                assert [x[0] for x in parts] == list(range(parts[0][0], parts[0][0] + len(parts)))
+    assert not seen
+
+
+def test_workers_of_prefixes_and_own_positions(index):
+    assert index.workers(0, 100, 16, 148) == 0 and index.workers(100, 0, 16, 148) == 50 and index.workers(10 ** 6, 0, 16, 148) == 148
+    assert index.workers(1, 10 ** 9, 16, 148) == 1 and index.workers(10 ** 9, 1, 16, 148) == 147
+    assert index.workers(1000, 500, 16, 148) == 74 and index.workers(1 << 50, 1 << 50, 8, 148) == 74
