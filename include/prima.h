@@ -471,10 +471,10 @@ int prima_prefix_attention(prima_paged* pool, int layer, const prima_paged_batch
  * enter the arrays here: born[s][g][j] = the row's position (batch->pos, or the slot).  lse: dev fp32 [n_tok][n_q_heads], as
  * prima_tree_attention or prima_prefix_attention has left it (where a prefix took part, its positions have their share); a
  * row whose lse is -infinity adds nothing.  weight_in (may be NULL: nothing so far; may be weight_out), weight_out: dev fp32
- * [n_seq][n_kv_heads][stride], stride below 2^31; born: dev int32, the same shape, may be NULL.  Entries behind the rows, and
+ * [n_seq][n_kv_heads][stride], stride at most 2^31 - 256; born: dev int32, the same shape, may be NULL.  Entries behind the rows, and
  * those of sequences without rows, are left as they were.  A slot on a bad page receives nothing; slots from `stride` on are
  * left out (and raise a status bit).  q, masks and positions as in prima_tree_attention; scores and sums in 32 bits, always
- * added in the same order.  decay: 0..1.  For a model's cache the arrays are [n_layers][n_seq][n_kv_heads][stride], of which
+ * added in the same order.  decay: 0..1; n_tok * n_q_heads below 2^31.  For a model's cache the arrays are [n_layers][n_seq][n_kv_heads][stride], of which
  * a call takes one layer's. */
 int prima_paged_weights(prima_paged* pool, int layer, const prima_paged_batch* batch, const void* q, int n_q_heads, float scale, const float* lse,
                         const float* weight_in, float* weight_out, int32_t* born, int64_t stride, float decay, void* stream);

@@ -3,7 +3,7 @@
 #include <cmath>
 #include <cstdio>
 
-#include "paged_device.cuh"
+#include "tree_device.cuh"
 
 namespace prima {
 namespace {
@@ -26,8 +26,8 @@ struct WeightsArgs {
 // form one line, and every worker (a warp) takes an equal stretch of it.
 struct WeightsWork {
   int seq, first, nodes, ctx, head;
-  int64_t n;                 // positions that the sequence has an entry for
-  int64_t block0, block1;
+  int n;                     // positions that the sequence has an entry for
+  int block0, block1;
 };
 template <int kBlock>
 struct WeightsCursor {
@@ -92,26 +92,26 @@ struct WeightsCursor {
     s->first = __shfl_sync(0xffffffffu, first, src);
     s->nodes = __shfl_sync(0xffffffffu, nodes, src);
     s->ctx = __shfl_sync(0xffffffffu, ctx, src);
-    s->n = positions(s->ctx, s->nodes);
-    const int64_t at = u - __shfl_sync(0xffffffffu, before, src), per_head = (s->n + kBlock - 1) / kBlock;
+    s->n = static_cast<int>(positions(s->ctx, s->nodes));
+    const int64_t at = u - __shfl_sync(0xffffffffu, before, src), per_head = (static_cast<int64_t>(s->n) + kBlock - 1) / kBlock;
     s->head = static_cast<int>(div_small(at, per_head));
-    s->block0 = at - s->head * per_head;
-    s->block1 = min(per_head, s->block0 + (u_end - u));
+    s->block0 = static_cast<int>(at - s->head * per_head);
+    s->block1 = static_cast<int>(min(per_head, s->block0 + (u_end - u)));
     u += s->block1 - s->block0;
     return true;
   }
 };
 
 // Whether row `node` of a sequence sees its row `i` (the position behind the context).
-__device__ __forceinline__ bool sees(const WeightsArgs& a, int first, int node, int64_t i) {
+__device__ __forceinline__ bool sees(const WeightsArgs& a, int first, int node, int i) {
   if (!a.b.mask) return i <= node;
   const uint32_t* words = reinterpret_cast<const uint32_t*>(a.b.mask + static_cast<int64_t>(first + node) * a.b.mask_words);
   return mask_word(words, 2 * a.b.mask_words, i >> 5) >> (i & 31) & 1;
 }
 // -lse in binary exponents; -infinity (its probabilities are 0) for a row that is none or sees nothing.
-__device__ __forceinline__ float shift_of(const WeightsArgs& a, const WeightsWork& s, int64_t row) {
-  if (row >= static_cast<int64_t>(s.nodes) * a.group) return -INFINITY;
-  const int64_t node = row / a.group;
+__device__ __forceinline__ float shift_of(const WeightsArgs& a, const WeightsWork& s, int row) {
+  if (row >= s.nodes * a.group) return -INFINITY;
+  const int node = row / a.group;
   const float lse = __ldg(a.lse + (s.first + node) * a.n_q_heads + s.head * a.group + (row - node * a.group));
   return lse == -INFINITY ? -INFINITY : -lse * kLog2e;
 }
@@ -119,10 +119,10 @@ __device__ __forceinline__ float shift_of(const WeightsArgs& a, const WeightsWor
 __device__ __forceinline__ int64_t entry_of(const WeightsArgs& a, const WeightsWork& s, int64_t j) {
   return (static_cast<int64_t>(s.seq) * a.pool.n_kv_heads + s.head) * a.stride + j;
 }
-__device__ __forceinline__ void put(const WeightsArgs& a, const WeightsWork& s, int64_t j, float had, float sum) {
+__device__ __forceinline__ void put(const WeightsArgs& a, const WeightsWork& s, int j, float had, float sum) {
   const int64_t at = entry_of(a, s, j);
   a.weight_out[at] = j < s.ctx && a.weight_in ? fmaf(a.decay, had, sum) : sum;
-  if (a.born && j >= s.ctx) a.born[at] = a.b.pos ? __ldg(a.b.pos + s.first + (j - s.ctx)) : static_cast<int>(j);
+  if (a.born && j >= s.ctx) a.born[at] = a.b.pos ? __ldg(a.b.pos + s.first + (j - s.ctx)) : j;
 }
 
 // ---- few rows -----------------------------------------------------------------------------------------------------------
@@ -144,17 +144,17 @@ __global__ void __launch_bounds__(128, weights_ctas(D, kTiles)) weights_stream_k
   WeightsCursor<16> cursor(a, lane, (blockIdx.x * 128 + threadIdx.x) >> 5, gridDim.x * 4);
   WeightsWork s;
   while (cursor.next(&s)) {
-    const int64_t rows = static_cast<int64_t>(s.nodes) * a.group;
+    const int rows = s.nodes * a.group;      // n_tok * n_q_heads is below 2^31
     const int32_t* const table = a.b.table + s.seq * a.b.table_stride;
     const T* const keys = static_cast<const T*>(a.pool.k) + (static_cast<int64_t>(s.head) << a.pool.page_shift) * D;
     const float* const had_from = a.weight_in ? a.weight_in + entry_of(a, s, 0) : nullptr;
     uint4 q[kTiles][kChunks];
     float shift[kTiles][2];
-    auto load_queries = [&](int64_t row0) {
+    auto load_queries = [&](int row0) {
 #pragma unroll
       for (int n = 0; n < kTiles; ++n) {
-        const int64_t row = row0 + 8 * n + g, node = row / a.group;
-        const T* src = static_cast<const T*>(a.q) + ((s.first + node) * a.n_q_heads + s.head * a.group + (row - node * a.group)) * D;
+        const int row = row0 + 8 * n + g, node = row / a.group;
+        const T* src = static_cast<const T*>(a.q) + static_cast<int64_t>((s.first + node) * a.n_q_heads + s.head * a.group + (row - node * a.group)) * D;
 #pragma unroll
         for (int c = 0; c < kChunks; ++c) q[n][c] = row < rows ? __ldg(reinterpret_cast<const uint4*>(src) + t4 + 4 * c) : make_uint4(0, 0, 0, 0);
 #pragma unroll
@@ -167,37 +167,51 @@ __global__ void __launch_bounds__(128, weights_ctas(D, kTiles)) weights_stream_k
       int bad;             // bits: position has no key
     };
     // Positions 16 block + g and + 8: pages hold at least 8 positions, so each of the two lies in one page with its
-    // seven neighbours.
-    auto load = [&](int64_t block, Keys& x) {
+    // seven neighbours.  The ids of the pages are read a block ahead of the keys.
+    struct Pages {
+      int id[2];
+    };
+    const int blocks_end = s.block1;
+    auto pages_of = [&](int block, Pages& p) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int slot = (block * 16 + 8 * h) >> a.pool.page_shift;
+        p.id[h] = block < blocks_end && slot < a.b.table_stride ? __ldg(table + slot) : -1;
+      }
+    };
+    auto load = [&](int block, const Pages& p, Keys& x) {
       x.bad = 0;
       x.had = 0.f;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int64_t j = block * 16 + 8 * h + g;
-        int64_t row = -1;
-        if (block < s.block1 && j < s.n) {
-          row = find_slot(a.pool, table, a.b.table_stride, a.layer, j);
-          if (row < 0) raise(a.pool.status, static_cast<int>(-row));
-        }
-        x.bad |= row < 0 ? 1 << h : 0;
-        const uint4* src = reinterpret_cast<const uint4*>(keys + row * D);
+        const int j = block * 16 + 8 * h + g;
+        const bool wanted = block < blocks_end && j < s.n, good = static_cast<unsigned>(p.id[h]) < static_cast<unsigned>(a.pool.n_pages);
+        if (wanted && !good) raise(a.pool.status, j >> a.pool.page_shift < a.b.table_stride ? kBadPage : kBadSlot);
+        x.bad |= wanted && good ? 0 : 1 << h;
+        // below 2^31 rows (prima_paged_create)
+        const int row = ((a.layer * a.pool.n_pages + p.id[h]) * a.pool.n_kv_heads << a.pool.page_shift) + (j & ((1 << a.pool.page_shift) - 1));
+        const uint4* src = reinterpret_cast<const uint4*>(keys + static_cast<int64_t>(row) * D);
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c) x.k[h][c] = row >= 0 ? __ldg(src + t4 + 4 * c) : make_uint4(0, 0, 0, 0);
-        if (t4 == h && had_from && block < s.block1 && j < min(s.n, static_cast<int64_t>(s.ctx))) x.had = had_from[j];
+        for (int c = 0; c < kChunks; ++c) x.k[h][c] = wanted && good ? __ldg(src + t4 + 4 * c) : make_uint4(0, 0, 0, 0);
+        if (t4 == h && had_from && wanted && j < s.ctx) x.had = had_from[j];
       }
     };
     const bool again = rows > 8 * kTiles;
     Keys next;
-    load(s.block0, next);
+    Pages ahead;
+    pages_of(s.block0, ahead);
+    load(s.block0, ahead, next);
+    pages_of(s.block0 + 1, ahead);
     load_queries(0);
 #pragma unroll 1
-    for (int64_t block = s.block0; block < s.block1; ++block) {
+    for (int block = s.block0; block < blocks_end; ++block) {
       const Keys x = next;
-      load(block + 1, next);
+      load(block + 1, ahead, next);
+      pages_of(block + 2, ahead);
       float sum[2] = {0.f, 0.f};
       const bool edge = __any_sync(0xffffffffu, x.bad != 0) || block * 16 + 16 > s.ctx;
 #pragma unroll 1
-      for (int64_t row0 = 0; row0 < rows; row0 += 8 * kTiles) {
+      for (int row0 = 0; row0 < rows; row0 += 8 * kTiles) {
         if (again) load_queries(row0);
 #pragma unroll
         for (int n = 0; n < kTiles; ++n) {
@@ -212,8 +226,8 @@ __global__ void __launch_bounds__(128, weights_ctas(D, kTiles)) weights_stream_k
           for (int e = 0; e < 4; ++e) {
             float p = ex2(fmaf(c[e], a.scale_log2, shift[n][e & 1]));
             if (edge) {
-              const int64_t row = row0 + 8 * n + 2 * t4 + (e & 1), i = block * 16 + 8 * (e >> 1) + g - s.ctx;
-              if ((x.bad >> (e >> 1) & 1) || shift[n][e & 1] == -INFINITY || (i >= 0 && !sees(a, s.first, static_cast<int>(row / a.group), i))) p = 0.f;
+              const int row = row0 + 8 * n + 2 * t4 + (e & 1), i = block * 16 + 8 * (e >> 1) + g - s.ctx;
+              if ((x.bad >> (e >> 1) & 1) || shift[n][e & 1] == -INFINITY || (i >= 0 && !sees(a, s.first, row / a.group, i))) p = 0.f;
             }
             sum[e >> 1] += p;
           }
@@ -225,21 +239,368 @@ __global__ void __launch_bounds__(128, weights_ctas(D, kTiles)) weights_stream_k
         sum[h] += __shfl_xor_sync(0xffffffffu, sum[h], 2);
       }
       if (t4 < 2) {
-        const int64_t j = block * 16 + 8 * t4 + g;
+        const int j = block * 16 + 8 * t4 + g;
         if (j < s.n) put(a, s, j, x.had, t4 ? sum[1] : sum[0]);
       }
     }
   }
 }
 
+// ---- many rows ----------------------------------------------------------------------------------------------------------
+// The same product on the tensor core: 128 positions (the rows of an accumulator) by tiles of 128 query rows (its columns),
+// so that a thread has one position and adds over its columns, without any exchange; neither maximum nor second product is
+// needed.  One persistent CTA per SM: warp 8 copies keys page by page into a ring, warp 9 issues the products, warp 10 plans,
+// and two groups of four warps take the exponentials, each from two accumulators of its own in turns.  The tiles of a block
+// of positions alternate between the groups (a single tile: the blocks do); up to four tiles stay in shared memory for a
+// whole stretch, more are read again for every block, the next one under the exponentials of this one.
+constexpr int kBlockThreads = 384, kRowTile = 128;
+template <int D> struct BlockGeometry {
+  static constexpr int kTileBytes = kRowTile * D * 2;          // queries of a tile
+  static constexpr int kSlotBytes = kTilePos * D * 2;          // keys of a block
+  static constexpr int kPanel = kTilePos * 128;                // 64 columns of either
+  static constexpr int kSlots = D == 128 ? 3 : 6;
+  static constexpr int kBytes = 4 * kTileBytes + kSlots * kSlotBytes;
+};
+struct BlockControl {
+  unsigned long long full[6], empty[6], s_ready[4], s_free[4], q_ready[4], part_full, part_free, drained;
+  unsigned long long work_full[2], work_empty[2];
+  WeightsWork work[2];                 // block0 = block1: no more
+  uint32_t tmem;
+  int give_up;
+  int bad[16];                         // of the last blocks: some page is none (ring and accumulators hold at most ten)
+  alignas(16) float shift[4][kRowTile];      // [2 * group + slot]
+  float part[kTilePos];                // sums of the second group
+};
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kBlockThreads, 1) weights_block_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ WeightsArgs a) {
+  using Geo = BlockGeometry<D>;
+  constexpr bool kBf16 = !__is_same(T, __half);
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  int* const status = a.pool.status;
+  if (smem_u32(smem) & 1023) {      // never seen, as in tree attention
+    pdl_wait();
+    if (tid == 0) raise(status, kGaveUp);
+    return;
+  }
+  uint8_t* const s_ring = smem + 4 * Geo::kTileBytes;
+  BlockControl* const ctl = reinterpret_cast<BlockControl*>(smem + Geo::kBytes);
+  int* const give_up = &ctl->give_up;
+  const uint32_t bar_full = smem_u32(ctl->full), bar_empty = smem_u32(ctl->empty), bar_s = smem_u32(ctl->s_ready), bar_free = smem_u32(ctl->s_free), bar_q = smem_u32(ctl->q_ready),
+                 bar_part = smem_u32(&ctl->part_full), bar_part_free = smem_u32(&ctl->part_free), bar_work = smem_u32(ctl->work_full), bar_work_empty = smem_u32(ctl->work_empty);
+  pdl_trigger();
+  if (tid == 0) {
+    for (int i = 0; i < 6; ++i) {
+      mbar_init(bar_full + 8 * i, 1);
+      mbar_init(bar_empty + 8 * i, 1);
+    }
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(bar_s + 8 * i, 1);
+      mbar_init(bar_free + 8 * i, 4);
+      mbar_init(bar_q + 8 * i, 4);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(bar_work + 8 * i, 1);
+      mbar_init(bar_work_empty + 8 * i, 10);
+    }
+    mbar_init(bar_part, 4);
+    mbar_init(bar_part_free, 4);
+    mbar_init(smem_u32(&ctl->drained), 1);
+    ctl->give_up = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    tma_prefetch_map(&k_map);
+  }
+  if (warp == 9) tmem_alloc(smem_u32(&ctl->tmem), 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = ctl->tmem;      // accumulators: columns 128 * (2 * group + turn)
+  pdl_wait();
+
+  // Stretch i of this CTA, or nothing when there are no more; the caller's warp gives it back with done_with(i).
+  auto work = [&](uint32_t i) -> const WeightsWork* {
+    const WeightsWork* s = &ctl->work[i & 1];
+    if (!wait_segment(bar_work + 8 * (i & 1), i >> 1 & 1)) {
+      if (lane == 0) raise(status, kGaveUp);
+      return nullptr;
+    }
+    return s->block1 > s->block0 ? s : nullptr;
+  };
+  auto done_with = [&](uint32_t i) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar_work_empty + 8 * (i & 1));
+  };
+  auto tiles_of = [&](const WeightsWork& s) { return (s.nodes * a.group + kRowTile - 1) / kRowTile; };
+  RingPlace<Geo::kSlots> ring;
+  uint32_t copies_before = 0;      // copies: places used so far, up to kSlots (the ring is empty at first)
+
+  if (warp == 10) {
+    // ---- the plan ----
+    WeightsCursor<kTilePos> cursor(a, lane, blockIdx.x, gridDim.x);
+    WeightsWork s;
+    for (uint32_t i = 0;; ++i) {
+      const bool more = cursor.next(&s);
+      if (i >= 2) wait_segment(bar_work_empty + 8 * (i & 1), (i / 2 - 1) & 1);
+      if (lane == 0) {
+        ctl->work[i & 1] = s;
+        if (!more) ctl->work[i & 1].block0 = ctl->work[i & 1].block1 = 0;
+        mbar_arrive(bar_work + 8 * (i & 1));
+      }
+      __syncwarp();
+      if (!more) break;
+    }
+  } else if (warp == 8) {
+    // ---- copies ----
+    const int shift = a.pool.page_shift, box_rows = min(1 << shift, kTilePos), boxes = kTilePos / box_rows;
+    const int box = lane % boxes, panel = lane / boxes;
+    const uint32_t dst = smem_u32(s_ring) + panel * Geo::kPanel + box * box_rows * 128;
+    uint32_t n_read = 0;
+    const WeightsWork* w;
+    for (uint32_t i = 0; (w = work(i)); ++i) {
+      const WeightsWork s = *w;
+      done_with(i);
+      const int32_t* table = a.b.table + s.seq * a.b.table_stride;
+      for (int block = s.block0; block < s.block1; ++block) {
+        const int pos = block * kTilePos + box * box_rows;
+        int64_t row = -1;
+        bool bad = false;
+        if (panel < D / 64 && pos < s.n) {
+          const int64_t x = find_slot(a.pool, table, a.b.table_stride, a.layer, pos);
+          bad = x < 0;
+          if (bad) raise(status, static_cast<int>(-x));
+          else row = x + (static_cast<int64_t>(s.head) << shift);
+        }
+        const int n_copies = __popc(__ballot_sync(0xffffffffu, row >= 0));
+        const bool any_bad = __any_sync(0xffffffffu, bad);
+        bool ok = true;
+        if (copies_before >= Geo::kSlots) ok = wait_for(bar_empty + 8 * ring.slot, ring.phase ^ 1, give_up, status);
+        if (__all_sync(0xffffffffu, ok)) {
+          if (lane == 0) {
+            ctl->bad[n_read % 16] = any_bad;
+            mbar_expect(bar_full + 8 * ring.slot, static_cast<uint32_t>(n_copies) * box_rows * 128);
+          }
+          __syncwarp();
+          if (row >= 0) tma_load_2d(dst + ring.slot * Geo::kSlotBytes, &k_map, panel * 64, static_cast<int>(row), bar_full + 8 * ring.slot);
+        }
+        ring.step(1);
+        if (copies_before < Geo::kSlots) ++copies_before;
+        ++n_read;
+      }
+    }
+  } else if (warp == 9) {
+    // ---- products ----
+    constexpr uint32_t kDesc = mma_f16_desc(kBf16, false, kTilePos, kRowTile);
+    const uint32_t u_tmem = uniform(tmem), ring_addr = uniform(smem_u32(s_ring)), q_addr = uniform(smem_u32(smem));
+    const SmemOperand k_all = smem_operand(ring_addr, 16);
+    uint32_t turn[2] = {0, 0}, loads[4] = {0, 0, 0, 0};      // of the groups; of the tiles' places
+    const WeightsWork* w;
+    for (uint32_t i = 0; (w = work(i)); ++i) {
+      const int tiles = uniform(tiles_of(*w)), blocks = uniform(w->block1 - w->block0);
+      done_with(i);
+      const bool again = tiles > 4;
+      uint32_t in_stretch[2] = {0, 0};      // tiles of the groups
+      bool ok = true;
+      for (int block = 0; block < blocks; ++block) {
+        ok = wait_for(bar_full + 8 * ring.slot, ring.phase, give_up, status) && ok;
+        for (int t = 0; t < tiles; ++t) {
+          const uint32_t h = tiles == 1 ? block & 1 : t & 1, n = h ? turn[1]++ : turn[0]++, nth = h ? in_stretch[1]++ : in_stretch[0]++;
+          const uint32_t q = 2 * h + (again ? nth & 1 : tiles == 1 ? 0 : t >> 1);      // place of the tile
+          if (again || block < (tiles == 1 ? 2 : 1)) {
+            uint32_t phase = 0;      // no indexed registers
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j)
+              if (j == q) phase = loads[j]++ & 1;
+            ok = wait_for(bar_q + 8 * q, phase, give_up, status) && ok;
+          }
+          const uint32_t d = 2 * h + (n & 1);
+          if (n >= 2) ok = wait_for(bar_free + 8 * d, (n / 2 - 1) & 1, give_up, status) && ok;
+          tc_fence_after();
+          if (__all_sync(0xffffffffu, ok) && elect_one()) {
+            const SmemOperand qq = smem_operand(q_addr + q * Geo::kTileBytes, 16), kk = k_all + ring.slot * Geo::kSlotBytes;
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) mma_ss(u_tmem + kRowTile * d, kk + (k / 4 * Geo::kPanel + k % 4 * 32), qq + (k / 4 * Geo::kPanel + k % 4 * 32), kDesc, k > 0);
+            tc_commit(bar_s + 8 * d);
+            if (t == tiles - 1) tc_commit(bar_empty + 8 * ring.slot);
+          }
+          __syncwarp();
+        }
+        ring.step(1);
+      }
+    }
+  } else if (warp < 8) {
+    // ---- exponentials and sums ----
+    const int h = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
+    const uint32_t t_s = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + 2 * h * kRowTile;
+    uint32_t turn = 0, n_part = 0, unit_base = 0;
+    // Tile t of a stretch into place p of this group, in the background, and its rows' shifts.
+    auto load_tile = [&](const WeightsWork& s, int t, int p) {
+      constexpr int kPieces = D / 8;
+      const int rows = s.nodes * a.group;
+      uint8_t* const dst = smem + (2 * h + p) * Geo::kTileBytes;
+#pragma unroll 4
+      for (int idx = r; idx < kRowTile * kPieces; idx += 128) {
+        const int in_tile = idx / kPieces, piece = idx % kPieces, row = t * kRowTile + in_tile;
+        const bool there = row < rows;
+        const int node = there ? row / a.group : 0, in_group = there ? row - node * a.group : 0;
+        copy16(smem_u32(dst) + piece / 8 * Geo::kPanel + in_tile * 128 + ((piece % 8) ^ (in_tile & 7)) * 16,
+               static_cast<const T*>(a.q) + (static_cast<int64_t>(s.first + node) * a.n_q_heads + s.head * a.group + in_group) * D + piece * 8, there);
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      ctl->shift[2 * h + p][r] = shift_of(a, s, t * kRowTile + r);
+    };
+    auto group_sync = [&]() { asm volatile("bar.sync %0, 128;" ::"r"(1 + h) : "memory"); };
+    auto tile_ready = [&](int p) {
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      fence_async_smem();
+      group_sync();      // the group reads all shifts
+      if (lane == 0) mbar_arrive(bar_q + 8 * (2 * h + p));
+    };
+    const float2 scale = make_float2(a.scale_log2, a.scale_log2);
+    const WeightsWork* w;
+    for (uint32_t i = 0; (w = work(i)); ++i) {
+      const WeightsWork& s = *w;
+      const int tiles = tiles_of(s), blocks = s.block1 - s.block0;
+      const bool single = tiles == 1, again = tiles > 4;
+      const int mine = single ? 1 : (tiles - h + 1) >> 1;      // tiles of this group
+      const int32_t* const table = a.b.table + s.seq * a.b.table_stride;
+      // The places are free: all of this group have seen the last scores of the stretch before and read its shifts.
+      group_sync();
+      if (!single || h < blocks) {
+        for (int p = 0; p < min(mine, 2); ++p) load_tile(s, single ? 0 : 2 * p + h, p);
+        for (int p = 0; p < min(mine, 2); ++p) tile_ready(p);
+      }
+      uint32_t nth = 0;      // tile of this group
+#pragma unroll 1
+      for (int block = single ? h : 0; block < blocks; block += single ? 2 : 1) {
+        const int pos0 = (s.block0 + block) * kTilePos, j = pos0 + r;
+        float had = 0.f;
+        if ((single || h == 0) && a.weight_in && j < min(s.n, s.ctx)) had = __ldg(a.weight_in + entry_of(a, s, j));
+        float2 sum = make_float2(0.f, 0.f);
+        bool hidden = false;
+#pragma unroll 1
+        for (int m = 0; m < mine; ++m, ++turn, ++nth) {
+          const int t = single ? 0 : 2 * m + h, p = again ? nth & 1 : m;
+          const uint32_t d = turn & 1;
+          wait_for(bar_s + 8 * (2 * h + d), turn >> 1 & 1, give_up, status);
+          tc_fence_after();
+          if (m == 0) hidden = *static_cast<volatile int*>(&ctl->bad[(unit_base + block) % 16]) != 0 && (j >= s.n || find_slot(a.pool, table, a.b.table_stride, a.layer, j) < 0);
+          const bool edge = pos0 + kTilePos > s.ctx;
+          const int behind = j - s.ctx;      // index of the position among the rows of the step
+          const float* const shift = ctl->shift[2 * h + p];
+          uint32_t x[2][32];
+          tmem_load(x[0], t_s + kRowTile * d);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            tmem_wait_load();
+            tmem_use(x[c & 1]);
+            if (c < 3) {
+              tmem_load(x[(c + 1) & 1], t_s + kRowTile * d + 32 * (c + 1));
+            } else {      // all are read: the next product may have the accumulator
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(bar_free + 8 * (2 * h + d));
+            }
+            uint32_t seen = 0xffffffffu;
+            if (edge && behind >= 0) {
+              const int row = t * kRowTile + 32 * c;
+              if (!a.b.mask) {      // rows from the position's own node on
+                const long long skip = static_cast<long long>(behind) * a.group - row;
+                seen = skip >= 32 ? 0u : skip <= 0 ? 0xffffffffu : 0xffffffffu << static_cast<int>(skip);
+              } else {
+                seen = 0;
+#pragma unroll 1
+                for (int e = 0; e < 32; ++e) {
+                  const int node = (row + e) / a.group;
+                  if (node < s.nodes && sees(a, s.first, node, behind)) seen |= 1u << e;
+                }
+              }
+            }
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+              const float4 z = *reinterpret_cast<const float4*>(shift + 32 * c + e);
+              float2 u = fma2(make_float2(__uint_as_float(x[c & 1][e]), __uint_as_float(x[c & 1][e + 1])), scale, make_float2(z.x, z.y));
+              float2 v = fma2(make_float2(__uint_as_float(x[c & 1][e + 2]), __uint_as_float(x[c & 1][e + 3])), scale, make_float2(z.z, z.w));
+              u = make_float2(ex2(u.x), ex2(u.y));
+              v = make_float2(ex2(v.x), ex2(v.y));
+              if (edge) {
+                u.x = seen >> e & 1 ? u.x : 0.f;
+                u.y = seen >> (e + 1) & 1 ? u.y : 0.f;
+                v.x = seen >> (e + 2) & 1 ? v.x : 0.f;
+                v.y = seen >> (e + 3) & 1 ? v.y : 0.f;
+              }
+              sum = add2(sum, add2(u, v));
+            }
+          }
+          // Many tiles: the one after the next into this place, whose scores are there (for the next block, from the first on).
+          if (again && !(block == blocks - 1 && m + 2 >= mine)) {
+            group_sync();      // all have read the shifts
+            load_tile(s, 2 * (m + 2 < mine ? m + 2 : m + 2 - mine) + h, p);
+            tile_ready(p);
+          }
+        }
+        float total = sum.x + sum.y;
+        if (!single) {
+          const uint32_t phase = n_part++ & 1;
+          if (h == 1) {
+            if (n_part > 1) wait_for(bar_part_free, phase ^ 1, give_up, status);
+            ctl->part[r] = total;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_part);
+          } else {
+            wait_for(bar_part, phase, give_up, status);
+            total += ctl->part[r];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_part_free);
+          }
+        }
+        if ((single || h == 0) && j < s.n) put(a, s, j, had, hidden ? 0.f : total);
+      }
+      unit_base += blocks;
+      done_with(i);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  // A wait that gave up may have left products or copies under way: they end before the memory is given back.
+  if (ctl->give_up) {
+    if (tid == 9 * 32) {
+      tc_commit(smem_u32(&ctl->drained));
+      for (int i = 0; i < (1 << 22) && !mbar_test(smem_u32(&ctl->drained), 0); ++i) {}
+    }
+    if (tid == 8 * 32)
+      for (uint32_t p = 0; p < copies_before; ++p) {      // the last places
+        ring.phase ^= ring.slot == 0;
+        ring.slot = ring.slot == 0 ? Geo::kSlots - 1 : ring.slot - 1;
+        for (int i = 0; i < (1 << 16) && !mbar_test(bar_full + 8 * ring.slot, ring.phase); ++i) {}
+      }
+    __syncthreads();
+  }
+  if (warp == 9) tmem_free(tmem, 512);
+}
+
+constexpr int64_t kLongest = 2147483647 - 255;      // positions that the arrays may have entries for: numbers of blocks' ends fit 32 bits
+
 template <typename T, int D, int kTiles>
 cudaError_t launch_stream(const prima_paged& pool, const WeightsArgs& a, cudaStream_t st) {
   return launch_pdl(weights_stream_kernel<T, D, kTiles>, dim3(pool.sm_count * weights_ctas(D, kTiles)), dim3(128), 0, st, a);
 }
 template <typename T, int D>
+cudaError_t launch_block(const prima_paged& pool, const WeightsArgs& a, cudaStream_t st) {
+  constexpr size_t kSmem = BlockGeometry<D>::kBytes + sizeof(BlockControl);
+  static_assert(kSmem <= 232448, "shared memory of a CTA");
+  static bool done[kMaxDevices] = {};
+  auto kernel = weights_block_kernel<T, D>;
+  const cudaError_t e = allow_smem(kernel, kSmem, done);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(kernel, dim3(pool.sm_count), dim3(kBlockThreads), kSmem, st, static_cast<const Maps*>(pool.maps)->k, a);
+}
+template <typename T, int D>
 cudaError_t launch_weights(const prima_paged& pool, const WeightsArgs& a, cudaStream_t st) {
   // Rows that a KV head has of a sequence on average; each variant is right for any.
   const int64_t rows = (static_cast<int64_t>(a.b.n_tok) + a.b.n_seq - 1) / a.b.n_seq * a.group;
+  if (rows > 32) return launch_block<T, D>(pool, a, st);
   return (rows <= 8 ? launch_stream<T, D, 1> : rows <= 16 ? launch_stream<T, D, 2> : launch_stream<T, D, 4>)(pool, a, st);
 }
 
@@ -265,9 +626,10 @@ int prima_paged_weights(prima_paged* p, int layer, const prima_paged_batch* batc
   if (n_q_heads < 1 || n_q_heads % c.n_kv_heads || n_q_heads / c.n_kv_heads > 64) return refuse("n_q_heads must be a multiple of n_kv_heads, at most 64 times it");
   if (!(scale > 0.f) || std::isinf(scale)) return refuse("scale must be positive and finite");
   if (!(decay >= 0.f && decay <= 1.f)) return refuse("decay outside 0..1");
-  if (stride < 1 || stride > 2147483647) return refuse("stride outside 1..2^31 - 1");
+  if (stride < 1 || stride > kLongest) return refuse("stride outside 1..2^31 - 256");
   if (!aligned_to(q, 16)) return refuse("q must be 16-byte aligned");
   if (!aligned_to(lse, 4) || !aligned_to(weight_in, 4) || !aligned_to(weight_out, 4) || !aligned_to(born, 4)) return refuse("an array is not 4-byte aligned");
+  if (static_cast<int64_t>(batch->n_tok) * n_q_heads > 2147483647) return refuse("n_tok * n_q_heads reaches 2^31");
   const int64_t bytes = 4 * static_cast<int64_t>(batch->n_seq) * c.n_kv_heads * stride;
   const char *in = reinterpret_cast<const char*>(weight_in), *to = reinterpret_cast<const char*>(weight_out);
   if (in && in != to && in < to + bytes && to < in + bytes) return refuse("weight_in overlaps weight_out without being it");
