@@ -2,6 +2,8 @@
 // copies and fragments.
 #pragma once
 
+#include <cuda.h>
+
 #include "paged.cuh"
 #include "tcgen05.cuh"
 
@@ -25,6 +27,13 @@ __device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, int* giv
   return false;
 }
 
+// The hand-over of segments, which goes on after a wait has given up elsewhere (nothing else may be left waiting).
+__device__ __forceinline__ bool wait_segment(uint32_t bar, uint32_t parity) {
+  for (int i = 0; i < (1 << 24); ++i)
+    if (mbar_test(bar, parity)) return true;
+  return false;
+}
+
 // ---- what a row sees ------------------------------------------------------------------------------------------------
 // Bits for 32 positions from `pos` on.  a = index of the position among the rows of the step, negative in the context.
 __device__ __forceinline__ uint32_t low_bits(long long n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << static_cast<int>(n)) - 1u; }
@@ -34,6 +43,49 @@ __device__ __forceinline__ uint32_t tree_bits(const uint32_t* words, int n_words
   if (a < 0) return mask_word(words, n_words, 0) << static_cast<int>(-a) | low_bits(-a);
   return __funnelshift_r(mask_word(words, n_words, a >> 5), mask_word(words, n_words, (a >> 5) + 1), static_cast<uint32_t>(a) & 31u);
 }
+
+struct SegmentView {
+  const BatchView& b;
+  const PoolView& pool;
+  int first, nodes, ctx;
+  long long limit;
+  const int32_t* table;
+  bool bad_pages;
+
+  __device__ __forceinline__ bool page_ok(long long pos) const {
+    return static_cast<unsigned>(__ldg(table + (pos >> pool.page_shift))) < static_cast<unsigned>(pool.n_pages);
+  }
+  __device__ uint32_t good_pages(long long pos) const {      // pos < limit: a page id is read only where it is needed
+    uint32_t w = 0;
+#pragma unroll 1
+    for (int i = 0; i < 32; ++i)
+      if (pos + i < limit && page_ok(pos + i)) w |= 1u << i;
+    return w;
+  }
+  // node: index of the row in its sequence
+  __device__ uint32_t seen_by(int node, long long pos) const {
+    const long long a = pos - ctx;
+    uint32_t w = b.mask ? tree_bits(reinterpret_cast<const uint32_t*>(b.mask + static_cast<long long>(first + node) * b.mask_words), 2 * b.mask_words, a)
+                        : low_bits(static_cast<long long>(node) + 1 - a);
+    w &= low_bits(limit - pos);
+    if (bad_pages) w &= good_pages(pos);
+    return w;
+  }
+  // Positions that any row of the sequence sees; the whole warp calls it.
+  __device__ uint32_t seen_by_any(long long pos, int lane) const {
+    const long long a = pos - ctx;
+    uint32_t w = 0xffffffffu;
+    if (b.mask && a > -32) {
+      w = 0;
+      for (int i = lane; i < nodes; i += 32)
+        w |= tree_bits(reinterpret_cast<const uint32_t*>(b.mask + static_cast<long long>(first + i) * b.mask_words), 2 * b.mask_words, a);
+      w = __reduce_or_sync(0xffffffffu, w);
+    }
+    w &= low_bits(limit - pos);
+    if (bad_pages) w &= good_pages(pos);
+    return w;
+  }
+};
 
 // ---- arithmetic ------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ float ex2(float x) {
@@ -133,7 +185,29 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+template <int D> struct Geometry {
+  static constexpr int kQBytes = 128 * D * 2;                  // one tile of 128 rows of queries
+  static constexpr int kSlotBytes = kTilePos * D * 2;          // keys or values of a unit
+  static constexpr int kPanel = kTilePos * 128;                // 64 columns of a unit
+  static constexpr int kSlots = D == 128 ? 5 : 12;
+};
+
 // ---- host ------------------------------------------------------------------------------------------------------------
+struct Maps {      // of a pool's two arrays: pages, or their rows 16 at a time
+  CUtensorMap k, v, k_few, v_few;
+};
+
+// Which kernel, by the rows that a KV head has of a sequence on average (the lengths themselves are on the device; each
+// kernel is right for any): up to 32 the streaming kernel, which takes 16 at a time, beyond it the tensor-memory kernel.
+// Streaming against tensor memory, heads of 128: 16 sequences of 4096 positions, 5 rows 52 and 70 us, 20 rows 70 and 71,
+// 40 rows 135 and 74; 64 of 600, 5 rows 39 and 56, 20 rows 61 and 57, 40 rows 83 and 59.  Between 16 and 32 rows it goes
+// by the lengths, which are not known here: 20 rows over 1000 positions 12.6 and 14.9, over 30 positions 8.6 and 14.9,
+// 64 ragged sequences up to 4096 68 and 61; heads of 64, the same, 41 and 56.  The larger gains are with streaming.
+// The average hides mixed batches, and padding rows count in it: 63 single tokens and one tree of 64 nodes, 8 query heads
+// per KV head, go to the streaming kernel, which reads the tree's cache once per 16 of its 512 rows.  All over 30,000
+// positions that is still the faster one (1607 and 2078 us), but with the single tokens over 1000 it takes 454 and 189, 15
+// single tokens over 2000 and a tree over 8000, 4 heads per KV head, 89 and 75.
+inline bool streams(const BatchView& b, int group) { return (static_cast<int64_t>(b.n_tok) + b.n_seq - 1) / b.n_seq * group <= 32; }
 template <typename Kernel>
 inline cudaError_t allow_smem(Kernel kernel, size_t bytes, bool (&done)[kMaxDevices]) {
   int dev;

@@ -177,14 +177,44 @@ PRIMA_HD PrefixSegment prefix_segment(const PrefixShape& t, int64_t rows, int64_
   return s;
 }
 
-// How many of n_cta workers take the prefixes' places, the others the sequences' own, of which one costs own_cost / 8 of
+// The sequences' own positions: steps of kFewPos of one KV head for a tile of kFewRows rows, kOwnOverhead places in front of
+// each (sequence, KV head, tile).
+constexpr int kFewPos = 16, kFewRows = 16, kOwnOverhead = 2;
+
+PRIMA_HD int64_t own_steps(int64_t limit) { return (limit + kFewPos - 1) / kFewPos; }
+PRIMA_HD int own_tiles(int rows) { return (rows + kFewRows - 1) / kFewRows; }
+PRIMA_HD int64_t own_places(int rows, int64_t limit) { return rows > 0 && limit > 0 ? own_tiles(rows) * (kOwnOverhead + own_steps(limit)) : 0; }      // of one KV head
+
+struct OwnSegment {
+  int head, tile;
+  int step0, step1;          // none where the share has only places at the head
+  int64_t places;            // of this share
+  int64_t last;              // place of the last step of the whole (sequence, KV head, tile)
+};
+// The segment at place u of a sequence whose KV heads have `per_head` places each; it ends at or before place u_end.
+PRIMA_HD OwnSegment own_segment(int64_t limit, int64_t per_head, int64_t u, int64_t u_end) {
+  OwnSegment s;
+  const int64_t length = kOwnOverhead + own_steps(limit);
+  s.head = static_cast<int>(div_small(u, per_head));
+  const int64_t r = u - s.head * per_head;
+  s.tile = static_cast<int>(div_small(r, length));
+  const int64_t in_tile = r - s.tile * length;
+  s.places = length - in_tile < u_end - u ? length - in_tile : u_end - u;
+  const int64_t p0 = in_tile - kOwnOverhead, p1 = p0 + s.places;
+  s.step0 = static_cast<int>(p0 > 0 ? p0 : 0);
+  s.step1 = static_cast<int>(p1 > 0 ? p1 : 0);
+  s.last = u + length - in_tile - 1;
+  return s;
+}
+
+// How many of n_cta workers take the prefixes' places, the others the sequences' own, of which one costs own_cost / 64 of
 // a prefix's.  Every worker of the prefixes has two places at least, so that it begins a unit in every tile that it
 // passes through.
 PRIMA_HD int prefix_workers(int64_t places, int64_t own, int own_cost, int n_cta) {
   if (places <= 0) return 0;
   int n = n_cta;
   if (own > 0) {
-    const double p = 8.0 * static_cast<double>(places), o = static_cast<double>(own_cost) * static_cast<double>(own);
+    const double p = 64.0 * static_cast<double>(places), o = static_cast<double>(own_cost) * static_cast<double>(own);
     n = static_cast<int>(p / (p + o) * n_cta + 0.5);
     if (n > n_cta - 1) n = n_cta - 1;
   }

@@ -3,7 +3,7 @@
 #include <cmath>
 #include <cstdio>
 
-#include "tree_device.cuh"
+#include "paged_device.cuh"
 
 namespace prima {
 namespace {

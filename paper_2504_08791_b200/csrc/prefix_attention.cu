@@ -6,7 +6,7 @@
 // prefix contributes is one large product for all rows that share it: with 256 rows of a KV head in a tile the cache of the
 // prefix is read once per tile, and the tensor core, not the cache, bounds the work.  What the sequences' own positions
 // contribute is a few rows over a short stretch each, bound by the cache.  One launch does both at once: some CTAs take the
-// prefixes (tensor memory), the others the own positions (streaming, tree_device.cuh), in shares that cost about the same,
+// prefixes (tensor memory), the others the own positions (a stream for every warp), in shares that cost about the same,
 // so that the memory system works for the ones while the tensor cores work for the others.  prefix_join_kernel joins the
 // parts in ascending order: the same lengths give the same bits.
 //
@@ -23,7 +23,7 @@
 #include <cmath>
 #include <cstdio>
 
-#include "tree_device.cuh"
+#include "paged_device.cuh"
 
 namespace prima {
 namespace {
@@ -35,8 +35,8 @@ constexpr int kPrefixSegmentCost = 4;  // in places
 // sum is what the block is launched with: 384 x 168 = 256 x 208 + 128 x 88.
 constexpr int kManyRegisters = 208, kFewRegisters = 88;
 
-// What a unit of 128 own positions costs, in eighths of a prefix's place.
-constexpr int kOwnCost128 = 16, kOwnCost64 = 8;
+// What a step of 16 own positions costs, in 64ths of a prefix's place.
+constexpr int kOwnCost128 = 8, kOwnCost64 = 6;
 
 struct PrefixView {
   int n;
@@ -50,17 +50,28 @@ struct PrefixView {
 // What a worker has whole lies at [head][D/4][rows][4]; what it has of something that is cut, at
 // [2 * worker + (it begins here)][D/4][tile rows][4].
 struct PrefixArgs {
-  TreeArgs own;              // part_o, part_ml: of the streaming workers
+  PoolView pool;
+  BatchView b;
   PrefixView prefix;
   PrefixShape shape;
-  int own_cost;
+  int64_t capacity;          // positions that a row of the sequences' table can name
+  int layer, n_q_heads, group;
+  uint32_t group_inverse;    // small_inverse(group)
+  float scale_log2;
+  const void* q;
+  void* out;
+  float* lse;
+  int own_cost;              // 0: the own positions' attention is done in front
   int64_t rows;              // n_tok * group
-  int n_cta;                 // workers there are at most: of the prefixes; twice as many stream
+  int n_cta;                 // workers there are at most: of the prefixes; eight times as many stream
   float* whole_o[2];
   float2* whole_ml[2];       // [head][rows]: reference, sum
   int2* note[2];             // [head][rows]: first worker, number of parts
+  int4* place;               // [n_tok], see write_places
   float* part_o;             // of the prefixes' workers
   float2* part_ml;
+  float* own_part_o;         // of the streaming ones
+  float2* own_part_ml;
 };
 
 struct PrefixWork {
@@ -82,13 +93,7 @@ struct PrefixControl {
   int give_up;
   int edge[16];                        // of the last units: not all positions are seen (the ring holds at most six)
   uint32_t seen[16][4];
-  union {
-    float2 ml[2][128];                 // a group's reference and sum, for the other one
-    struct {                           // of the streaming groups, in the CTAs that have these
-      Segment seg[2];
-      float2 ml[2][4][16];
-    } own;
-  };
+  float2 ml[2][128];                   // a group's reference and sum, for the other one
 };
 
 // The range of a prefix: rows of the step that share it, or none.  Reads device memory; false: the numbers are bad.
@@ -96,7 +101,7 @@ struct PrefixRange {
   int first = 0, rows = 0, len = 0;    // rows: of the step
 };
 __device__ __forceinline__ bool prefix_range(const PrefixArgs& a, int p, PrefixRange* out) {
-  const BatchView& b = a.own.b;
+  const BatchView& b = a.b;
   const int s0 = __ldg(a.prefix.seq_begin + p), s1 = __ldg(a.prefix.seq_begin + p + 1), len = __ldg(a.prefix.len + p);
   *out = PrefixRange();
   if (s0 < 0 || s1 < s0 || s1 > b.n_seq || len < 0) return false;
@@ -124,7 +129,7 @@ struct PrefixCursor {
     range = PrefixRange();
     if (p0 + lane < a.prefix.n) {
       prefix_range(a, p0 + lane, &range);
-      per_head = prefix_places(a.shape, static_cast<long long>(range.rows) * a.own.shape.group, prefix_units(a.shape, range.len));
+      per_head = prefix_places(a.shape, static_cast<long long>(range.rows) * a.group, prefix_units(a.shape, range.len));
     }
     places = per_head * a.shape.n_kv_heads;
     long long x = places;
@@ -153,13 +158,13 @@ struct PrefixCursor {
       const int src = __ffs(hit) - 1;
       const long long in_front = __shfl_sync(0xffffffffu, before, src), mine = __shfl_sync(0xffffffffu, per_head, src);
       const int first = __shfl_sync(0xffffffffu, range.first, src), n_rows = __shfl_sync(0xffffffffu, range.rows, src), len = __shfl_sync(0xffffffffu, range.len, src);
-      const long long rows = static_cast<long long>(n_rows) * a.own.shape.group, units = prefix_units(a.shape, len);
+      const long long rows = static_cast<long long>(n_rows) * a.group, units = prefix_units(a.shape, len);
       const PrefixSegment t = prefix_segment(a.shape, rows, units, mine, u - in_front, u_end - in_front);
       s->prefix = p0 + src;
       s->head = t.head;
       s->row0 = static_cast<int>(t.row_tile * kPrefixRows);
       s->rows = static_cast<int>(min(rows - s->row0, static_cast<long long>(kPrefixRows)));
-      s->first = static_cast<long long>(first) * a.own.shape.group;
+      s->first = static_cast<long long>(first) * a.group;
       s->unit0 = t.unit0;
       s->n = t.unit1 - t.unit0;
       s->kind = t.unit0 ? 1 : t.unit1 < units ? 2 : 0;
@@ -172,33 +177,364 @@ struct PrefixCursor {
   }
 };
 
-// The results of the streaming groups.
-struct OwnEnv {
-  static constexpr bool kFinal = false;
-  const PrefixArgs& a;
-  int tid, worker, n_workers;
-  bool reports;
-  uint8_t* smem;
-  Segment* seg;
-  float2 (*ml)[16];
-  int barrier, dim;
-  __device__ __forceinline__ void sync() const { asm volatile("bar.sync %0, 128;" ::"r"(barrier) : "memory"); }
-  // Row x of the segment as row R of its KV head
-  __device__ __forceinline__ int64_t row_of(const Segment& s, int x) const {
-    return static_cast<int64_t>(s.head) * a.rows + static_cast<int64_t>(s.first) * a.own.shape.group + s.row0 + x;
+// ---- the sequences' own positions ------------------------------------------------------------------------------------
+// A worker is a warp: it copies 16 positions at a time through a ring of its own, a few steps ahead and on into its next
+// segments, and applies them with m16n8k16 products, queries and output in registers; nothing waits for another warp.
+template <int D> struct OwnGeometry {
+  static constexpr int kWarps = 8, kStages = D == 128 ? 3 : 6;
+  static constexpr int kHalf = kFewPos * D * 2;                // keys or values of a step
+  static constexpr int kStage = 2 * kHalf;
+  static constexpr int kPanel = kFewPos * 128;                 // 64 columns of either
+  static constexpr int kWarpBytes = kStages * kStage;
+};
+struct OwnWork {
+  int seq, first, nodes, ctx, head, row0, rows, step0, n;      // rows row0 .. of the (sequence, KV head)
+  int kind, last_worker;               // as PrefixWork
+  long long limit;                     // positions there are
+};
+constexpr int kWindows = 1024;         // of the sequences, for which their places are added up
+struct OwnControl {                    // behind the warps' rings
+  long long before[kWindows];          // places in front of a window
+  unsigned long long full[8][6];
+  OwnWork fifo[8][8];                  // segments between a warp's copies (at most five steps ahead) and its products
+};
+// Sequences of a window: 32, or a multiple where there are too many.
+__device__ __forceinline__ int window_of(int n_seq) { return 32 * ((n_seq + 32 * kWindows - 1) / (32 * kWindows)); }
+
+// A sequence as the own positions' line counts it.
+struct OwnSeq {
+  int first = 0, nodes = 0, ctx = 0;
+  long long limit = 0, per_head = 0;
+};
+__device__ __forceinline__ bool own_seq(const PrefixArgs& a, int i, OwnSeq* s) {
+  const int f = __ldg(a.b.row_begin + i), e = __ldg(a.b.row_begin + i + 1), c = __ldg(a.b.ctx_len + i);
+  *s = OwnSeq();
+  if (f < 0 || e < f || e > a.b.n_tok || c < 0) return false;
+  s->first = f;
+  s->nodes = e - f;
+  s->ctx = c;
+  s->limit = min(static_cast<long long>(c) + s->nodes, static_cast<long long>(a.capacity));
+  s->per_head = own_places(s->nodes * a.group, s->limit);
+  return true;
+}
+// Places of each window of sequences, by all warps; their sums by the first one.  Two barriers.
+__device__ void add_up_own(const PrefixArgs& a, OwnControl* own, long long* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, size = window_of(a.b.n_seq), n = (a.b.n_seq + size - 1) / size;
+  for (int w = warp; w < n; w += kPrefixThreads / 32) {
+    long long sum = 0;
+    for (int i = w * size + lane; i < min((w + 1) * size, a.b.n_seq); i += 32) {
+      OwnSeq s;
+      const bool ok = own_seq(a, i, &s);
+      sum += s.per_head * a.pool.n_kv_heads;
+      if (blockIdx.x == 0) {
+        if (!ok) raise(a.pool.status, kBadRows);
+        else if (s.nodes && static_cast<long long>(s.ctx) + s.nodes > a.capacity) raise(a.pool.status, kBadSlot);
+      }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) own->before[w] = sum;
   }
-  __device__ __forceinline__ void whole(const Segment& s, int x, int64_t, int quad, float4 y, float top, float total) const {
-    const int64_t row = row_of(s, x), head = s.head;
-    reinterpret_cast<float4*>(a.whole_o[1])[(head * (dim / 4) + quad) * a.rows + (row - head * a.rows)] = y;
-    if (quad == 0) {
-      a.whole_ml[1][row] = make_float2(top, total);
-      a.note[1][row] = make_int2(worker, 1);
+  __syncthreads();
+  if (warp == 0) {
+    long long front = 0;
+    for (int w0 = 0; w0 < n; w0 += 32) {
+      const long long mine = w0 + lane < n ? own->before[w0 + lane] : 0;
+      long long x = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+      }
+      if (w0 + lane < n) own->before[w0 + lane] = front + x - mine;
+      front += __shfl_sync(0xffffffffu, x, 31);
+    }
+    if (lane == 0) *total = front;
+  }
+  __syncthreads();
+}
+
+// Walks a worker's share of the own positions, 32 sequences at a time, one per lane.
+struct OwnCursor {
+  const PrefixArgs& a;
+  const int lane, worker;
+  const TreeShares shares;
+  long long u, u_end, window = 0, front = 0;      // front: places in front of the lane's sequence
+  int w0 = 0;
+  OwnSeq mine;
+
+  __device__ __forceinline__ void load(long long in_front) {
+    mine = OwnSeq();
+    if (w0 + lane < a.b.n_seq) own_seq(a, w0 + lane, &mine);
+    long long x = mine.per_head * a.pool.n_kv_heads;
+    const long long places = x;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    front = in_front + x - places;
+    window = in_front + __shfl_sync(0xffffffffu, x, 31);
+  }
+  __device__ OwnCursor(const PrefixArgs& args, const OwnControl* own, int lane_, int worker_, int n_workers, long long total)
+      : a(args), lane(lane_), worker(worker_), shares(tree_shares(total, n_workers)) {
+    u = tree_share_begin(shares, worker);
+    u_end = tree_share_begin(shares, worker + 1);
+    if (u >= u_end) return;
+    const int size = window_of(a.b.n_seq);
+    int lo = 0, hi = (a.b.n_seq + size - 1) / size;
+    while (hi - lo > 1) {      // the last window with at most u places in front
+      const int at = (lo + hi) / 2;
+      if (own->before[at] <= u) lo = at;
+      else hi = at;
+    }
+    w0 = lo * size;
+    load(own->before[lo]);
+  }
+  __device__ __forceinline__ bool next(OwnWork* s) {
+    while (u < u_end) {
+      unsigned hit;
+      while (!(hit = __ballot_sync(0xffffffffu, u >= front && u < front + mine.per_head * a.pool.n_kv_heads))) {      // ends: u is below the total
+        w0 += 32;
+        load(window);
+      }
+      const int src = __ffs(hit) - 1;
+      const long long in_front = __shfl_sync(0xffffffffu, front, src), per_head = __shfl_sync(0xffffffffu, mine.per_head, src);
+      s->first = __shfl_sync(0xffffffffu, mine.first, src);
+      s->nodes = __shfl_sync(0xffffffffu, mine.nodes, src);
+      s->ctx = __shfl_sync(0xffffffffu, mine.ctx, src);
+      s->limit = __shfl_sync(0xffffffffu, mine.limit, src);
+      const OwnSegment t = own_segment(s->limit, per_head, u - in_front, u_end - in_front);
+      s->seq = w0 + src;
+      s->head = t.head;
+      s->row0 = t.tile * kFewRows;
+      s->rows = min(s->nodes * a.group - s->row0, kFewRows);
+      s->step0 = t.step0;
+      s->n = t.step1 - t.step0;
+      s->kind = t.step0 ? 1 : t.step1 < own_steps(s->limit) ? 2 : 0;
+      s->last_worker = s->kind == 2 ? tree_cta_of(shares, in_front + t.last) : worker;
+      u += t.places;
+      if (s->n) return true;
+    }
+    return false;
+  }
+};
+
+template <typename T, int D>
+__device__ __forceinline__ void own_share(const CUtensorMap* k_map, const CUtensorMap* v_map, const PrefixArgs& a, uint8_t* smem, OwnControl* own, int* give_up, int worker,
+                                          int n_workers, long long total) {
+  using Geo = OwnGeometry<D>;
+  constexpr bool kBf16 = !__is_same(T, __half);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
+  int* const status = a.pool.status;
+  const uint32_t ring_addr = smem_u32(smem + warp * Geo::kWarpBytes), bar_full = smem_u32(own->full[warp]);
+  const int shift = a.pool.page_shift;
+  // Copies of a step: lane i < boxes takes 64 columns of box_rows positions of keys or values.
+  const int box_rows = min(1 << shift, kFewPos), halves = kFewPos / box_rows, boxes = 2 * (D / 64) * halves;
+  const int is_v = lane / (boxes / 2), panel = lane % (boxes / 2) / halves, half = lane % halves;
+  const CUtensorMap* const map = is_v ? v_map : k_map;
+  const uint32_t box_at = ring_addr + is_v * Geo::kHalf + panel * Geo::kPanel + half * box_rows * 128;
+
+  OwnCursor cursor(a, own, lane, worker, n_workers, total);
+  RingPlace<Geo::kStages> put, get;
+  uint32_t bad_stages = 0, planned = 0, begun = 0;
+  // The segment that is copied, its next step, the page that this lane's box of that step lies on
+  OwnWork from{};
+  int step = 0, page = -1;
+  bool more = false;
+  auto read_page = [&]() {
+    const long long pos = static_cast<long long>(from.step0 + step) * kFewPos + half * box_rows;
+    page = more && lane < boxes && pos < from.limit ? __ldg(a.b.table + from.seq * a.b.table_stride + (pos >> shift)) : -1;
+  };
+  auto plan = [&]() {
+    more = cursor.next(&from);
+    step = 0;
+    if (more) {
+      __syncwarp();
+      if (lane == 0) own->fifo[warp][planned & 7] = from;
+      __syncwarp();
+      ++planned;
+    }
+  };
+  auto copy = [&]() {
+    if (!more) return;
+    const long long pos = static_cast<long long>(from.step0 + step) * kFewPos + half * box_rows;
+    const bool wanted = lane < boxes && pos < from.limit, good = static_cast<unsigned>(page) < static_cast<unsigned>(a.pool.n_pages);
+    if (wanted && !good) raise(status, kBadPage);
+    const uint32_t copies = __ballot_sync(0xffffffffu, wanted && good);
+    const bool bad = __any_sync(0xffffffffu, wanted && !good);
+    bad_stages = (bad_stages & ~(1u << put.slot)) | (bad ? 1u << put.slot : 0u);
+    if (lane == 0) mbar_expect(bar_full + 8 * put.slot, static_cast<uint32_t>(__popc(copies)) * box_rows * 128);
+    __syncwarp();
+    // below 2^31 rows (prima_paged_create)
+    const int row = (((a.layer * a.pool.n_pages + page) * a.pool.n_kv_heads + from.head) << shift) + (static_cast<int>(pos) & ((1 << shift) - 1));
+    if (wanted && good) tma_load_2d(box_at + put.slot * Geo::kStage, map, panel * 64, row, bar_full + 8 * put.slot);
+    put.step(1);
+    if (++step == from.n) plan();
+    read_page();
+  };
+  plan();
+  read_page();
+#pragma unroll 1
+  for (int i = 0; i < Geo::kStages - 1; ++i) copy();
+
+  while (begun < planned) {
+    const OwnWork s = own->fifo[warp][begun & 7];
+    ++begun;
+    const int t0 = s.row0 / a.group, rem0 = s.row0 - t0 * a.group;
+    // Fragments of the queries: rows g and g + 8, columns 2 t4, + 1, + 8, + 9 of every 16
+    uint32_t qf[D / 16][4];
+    int node[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int x = 8 * h + g, y = rem0 + x, n = small_div(y, a.group_inverse);
+      node[h] = x < s.rows ? t0 + n : -1;
+      const uint32_t* src = reinterpret_cast<const uint32_t*>(static_cast<const T*>(a.q) + (static_cast<int64_t>(s.first + t0 + n) * a.n_q_heads + s.head * a.group + (y - n * a.group)) * D) + t4;
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) {
+        qf[k][h] = x < s.rows ? __ldg(src + 8 * k) : 0u;
+        qf[k][2 + h] = x < s.rows ? __ldg(src + 8 * k + 4) : 0u;
+      }
+    }
+    float o[D / 8][4], ref[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int n = 0; n < D / 8; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
+#pragma unroll 1
+    for (int i = 0; i < s.n; ++i) {
+      __syncwarp();      // all have read the step whose place is filled again
+      copy();
+      wait_for(bar_full + 8 * get.slot, get.phase, give_up, status);
+      const uint32_t kk = ring_addr + get.slot * Geo::kStage, vv = kk + Geo::kHalf;
+      const long long pos0 = static_cast<long long>(s.step0 + i) * kFewPos;
+      const bool bad = bad_stages >> get.slot & 1, edge = bad || pos0 + kFewPos > min(static_cast<long long>(s.ctx), s.limit);
+      const SegmentView view{a.b, a.pool, s.first, s.nodes, s.ctx, s.limit, a.b.table + s.seq * a.b.table_stride, bad};
+      if (edge) {
+        // Values at positions that no row sees may be anything, and 0 x NaN is NaN: clear them.
+        const uint32_t seen = view.seen_by_any(pos0, lane);
+        if (lane < kFewPos && !(seen >> lane & 1)) {
+#pragma unroll
+          for (int c = 0; c < D / 8; ++c)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(vv + c / 8 * Geo::kPanel + lane * 128 + c % 8 * 16), "r"(0) : "memory");
+        }
+        fence_async_smem();
+        __syncwarp();
+      }
+      float sc[2][4];
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc[n][e] = 0.f;
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) {
+        uint32_t b[4];      // positions 0..7 and 8..15, two halves of 8 columns each
+        const int row = (lane >> 4) * 8 + (lane & 7), chunk = 2 * k + (lane >> 3 & 1);
+        ldsm4(b, kk + chunk / 8 * Geo::kPanel + row * 128 + (chunk % 8 ^ (row & 7)) * 16);
+        mma16816<kBf16>(sc[0], qf[k], b[0], b[1]);
+        mma16816<kBf16>(sc[1], qf[k], b[2], b[3]);
+      }
+      if (edge) {      // positions that the row does not see, or on a bad page
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t seen = node[h] >= 0 ? view.seen_by(node[h], pos0) : 0u;
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+              if (!(seen >> (8 * n + 2 * t4 + e) & 1)) sc[n][2 * h + e] = -INFINITY;
+        }
+      }
+      float top[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) top[h] = fmaxf(fmaxf(sc[0][2 * h], sc[0][2 * h + 1]), fmaxf(sc[1][2 * h], sc[1][2 * h + 1])) * a.scale_log2;
+      if (__any_sync(0xffffffffu, top[0] > ref[0] + kSlack || top[1] > ref[1] + kSlack)) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float x = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], 1));
+          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
+          const float r = x > ref[h] + kSlack ? x - kHeadroom : ref[h];
+          const float f = r == ref[h] ? 1.f : ex2(ref[h] - r);
+          ref[h] = r;
+          sum[h] *= f;
+#pragma unroll
+          for (int n = 0; n < D / 8; ++n) {
+            o[n][2 * h] *= f;
+            o[n][2 * h + 1] *= f;
+          }
+        }
+      }
+      uint32_t p[4];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float down = ref[h] == -INFINITY ? 0.f : -ref[h];
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+          const float x = ex2(fmaf(sc[n][2 * h], a.scale_log2, down)), y = ex2(fmaf(sc[n][2 * h + 1], a.scale_log2, down));
+          sum[h] += x + y;
+          p[2 * n + h] = Half2Of<T>::pack(x, y);
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < D / 16; ++n) {
+        uint32_t b[4];      // 16 positions, columns 16 n .. + 7 and + 8 .. + 15
+        const int row = (lane >> 3 & 1) * 8 + (lane & 7), chunk = 2 * n + (lane >> 4);
+        ldsm4_t(b, vv + chunk / 8 * Geo::kPanel + row * 128 + (chunk % 8 ^ (row & 7)) * 16);
+        mma16816<kBf16>(o[2 * n], p, b[0], b[1]);
+        mma16816<kBf16>(o[2 * n + 1], p, b[2], b[3]);
+      }
+      get.step(1);
+    }
+    // ---- the segment's part ----
+    const int64_t slot = 2 * static_cast<int64_t>(worker) + (s.kind == 2), at = static_cast<int64_t>(s.first) * a.group + s.row0;
+    float* const dst = s.kind == 0 ? a.whole_o[1] + (static_cast<int64_t>(s.head) * (D / 4) * a.rows + at) * 4 : a.own_part_o + slot * (D / 4) * kFewRows * 4;
+    const int64_t stride = 4 * (s.kind == 0 ? a.rows : kFewRows);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int x = 8 * h + g;
+      float z = sum[h] + __shfl_xor_sync(0xffffffffu, sum[h], 1);
+      z += __shfl_xor_sync(0xffffffffu, z, 2);
+      if (x >= s.rows) continue;
+#pragma unroll
+      for (int n = 0; n < D / 8; ++n) *reinterpret_cast<float2*>(dst + (2 * n + (t4 >> 1)) * stride + 4 * x + 2 * (t4 & 1)) = make_float2(o[n][2 * h], o[n][2 * h + 1]);
+      if (t4 == 0) {
+        const int64_t row = static_cast<int64_t>(s.head) * a.rows + at + x;
+        if (s.kind == 0) a.whole_ml[1][row] = make_float2(ref[h], z);
+        else a.own_part_ml[slot * kFewRows + x] = make_float2(ref[h], z);
+        if (s.kind != 1) a.note[1][row] = make_int2(worker, s.last_worker - worker + 1);
+      }
     }
   }
-  __device__ __forceinline__ void begins(const Segment& s, int x) const { a.note[1][row_of(s, x)] = make_int2(worker, s.last_worker - worker + 1); }
-  __device__ __forceinline__ void ends(const Cursor&, const Segment&) const {}
-};
-template <int D> struct OwnStream { static constexpr int kStages = D == 128 ? 3 : 6; };
+  // A wait that gave up may have left copies under way: they end before the memory is given back.
+  if (*static_cast<volatile int*>(give_up))
+    for (uint32_t i = 0; i < Geo::kStages; ++i)
+      for (int j = 0; j < (1 << 16) && !mbar_test(bar_full + 8 * i, i < put.slot ? put.phase : put.phase ^ 1); ++j) {}
+}
+
+// Where the joining kernel finds what belongs to a token, written here for all tokens (nothing of what it reads depends on
+// the attention): whether it is any sequence's, that sequence's first row of the step, and the first row of those that share
+// its prefix, -1 without one.
+__device__ __forceinline__ void write_places(const PrefixArgs& a, int warp, int n_warps) {
+  const int lane = threadIdx.x & 31;
+  for (int t0 = 32 * warp; t0 < a.b.n_tok; t0 += 32 * n_warps) {
+    const int t = t0 + lane;
+    // the warp looks the first token's sequence and prefix up, the others are not far behind
+    int s = seq_of_row(a.b, t0, lane), p = 0;
+    for (int i = lane; i < a.prefix.n; i += 32) p += __ldg(a.prefix.seq_begin + i + 1) <= s ? 1 : 0;
+    p = __reduce_add_sync(0xffffffffu, p);
+    if (t >= a.b.n_tok) continue;
+    while (s < a.b.n_seq && __ldg(a.b.row_begin + s + 1) <= t) ++s;
+    OwnSeq seq;
+    int4 x = make_int4(0, 0, -1, 0);
+    if (s < a.b.n_seq && own_seq(a, s, &seq) && t >= seq.first) {
+      while (p < a.prefix.n && __ldg(a.prefix.seq_begin + p + 1) <= s) ++p;
+      PrefixRange range;
+      const bool shares = p < a.prefix.n && __ldg(a.prefix.seq_begin + p) <= s && prefix_range(a, p, &range) && prefix_units(a.shape, range.len) > 0;
+      x = make_int4(1, seq.first, shares ? range.first : -1, 0);
+    }
+    a.place[t] = x;
+  }
+}
 
 // What the warps of a prefixes' CTA share.
 template <int D>
@@ -210,7 +546,7 @@ struct PrefixCta {
   int n_workers;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   int* const give_up = &ctl->give_up;
-  int* const status = a.own.pool.status;
+  int* const status = a.pool.status;
   uint8_t* const s_q = smem;
   uint8_t* const s_ring = smem + 2 * Geometry<D>::kQBytes;
   const uint32_t bar_full = smem_u32(ctl->full), bar_empty = smem_u32(ctl->empty), bar_s = smem_u32(ctl->s_ready), bar_p = smem_u32(ctl->p_ready),
@@ -233,7 +569,7 @@ struct PrefixCta {
     __syncwarp();
     if (lane == 0) mbar_arrive(bar_seg_empty + 8 * (i % kPlanned));
   }
-  template <typename T> __device__ __forceinline__ void feed(const CUtensorMap* k_map, const CUtensorMap* v_map);
+  template <typename T> __device__ __forceinline__ void feed(const Maps& maps);
   template <typename T> __device__ __forceinline__ void softmax();
   __device__ __forceinline__ void drain();
 };
@@ -241,10 +577,10 @@ struct PrefixCta {
 // Warps 8 to 10.
 template <int D>
 template <typename T>
-__device__ __forceinline__ void PrefixCta<D>::feed(const CUtensorMap* k_map, const CUtensorMap* v_map) {
+__device__ __forceinline__ void PrefixCta<D>::feed(const Maps& maps) {
   using Geo = Geometry<D>;
   constexpr bool kBf16 = !__is_same(T, __half);
-  const PoolView& pool = a.own.pool;
+  const PoolView& pool = a.pool;
   if (warp == 10) {
     // ---- the plan ----
     PrefixCursor cursor(a, lane, blockIdx.x, n_workers, ctl->places);
@@ -279,7 +615,7 @@ __device__ __forceinline__ void PrefixCta<D>::feed(const CUtensorMap* k_map, con
         int64_t row = -1;
         bool bad = false;
         if (panel < D / 64 && pos < s.limit) {
-          const int64_t r = find_slot(pool, table, a.prefix.table_stride, a.own.layer, pos);
+          const int64_t r = find_slot(pool, table, a.prefix.table_stride, a.layer, pos);
           bad = r < 0;
           if (bad) raise(status, static_cast<int>(-r));
           else row = r + (static_cast<int64_t>(s.head) << shift);
@@ -291,7 +627,7 @@ __device__ __forceinline__ void PrefixCta<D>::feed(const CUtensorMap* k_map, con
 #pragma unroll 1
           for (int i = 0; i < 4; ++i) {
             const long long at = unit + 32 * i + lane;
-            const uint32_t word = __ballot_sync(0xffffffffu, at < s.limit && find_slot(pool, table, a.prefix.table_stride, a.own.layer, at) >= 0);
+            const uint32_t word = __ballot_sync(0xffffffffu, at < s.limit && find_slot(pool, table, a.prefix.table_stride, a.layer, at) >= 0);
             if (lane == i) seen = word;
           }
         }
@@ -306,7 +642,7 @@ __device__ __forceinline__ void PrefixCta<D>::feed(const CUtensorMap* k_map, con
             __syncwarp();
             if (lane == 0) mbar_expect(bar_full + 8 * ring.slot, static_cast<uint32_t>(n_copies) * box_rows * 128);
             __syncwarp();
-            if (row >= 0) tma_load_2d(dst + ring.slot * Geo::kSlotBytes, is_v ? v_map : k_map, panel * 64, static_cast<int>(row), bar_full + 8 * ring.slot);
+            if (row >= 0) tma_load_2d(dst + ring.slot * Geo::kSlotBytes, is_v ? &maps.v : &maps.k, panel * 64, static_cast<int>(row), bar_full + 8 * ring.slot);
           }
           // Queries before the rest of the first places, as in tree attention.
           if (!started) wait_for(bar_first, 0, give_up, status);
@@ -389,7 +725,7 @@ __device__ __forceinline__ void PrefixCta<D>::softmax() {
   const int w = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
   const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
   const uint32_t t_s = tmem + lanes + kTilePos * w, t_o = tmem + lanes + 256;
-  const int group = a.own.shape.group, n_q_heads = a.own.n_q_heads;
+  const int group = a.group, n_q_heads = a.n_q_heads;
   uint32_t n_sub = 0, n_seg = 0, unit_base = 0;      // sub-units of this accumulator, segments that had some, units before
   bool loaded = false;                               // the queries of the segment are on their way already
 
@@ -405,9 +741,9 @@ __device__ __forceinline__ void PrefixCta<D>::softmax() {
     for (int idx = r; idx < 128 * kPieces; idx += 128) {
       const int row = idx / kPieces, piece = idx % kPieces;
       const bool there = from + row < g.rows;
-      const int y = there ? rem0 + row : rem0, t = small_div(y, a.own.group_inverse);
+      const int y = there ? rem0 + row : rem0, t = small_div(y, a.group_inverse);
       copy16(smem_u32(s_q) + w * Geo::kQBytes + piece / 8 * Geo::kPanel + row * 128 + ((piece % 8) ^ (row & 7)) * 16,
-             static_cast<const T*>(a.own.q) + ((t0 + t) * n_q_heads + g.head * group + (y - t * group)) * D + piece * 8, there);
+             static_cast<const T*>(a.q) + ((t0 + t) * n_q_heads + g.head * group + (y - t * group)) * D + piece * 8, there);
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
@@ -478,7 +814,7 @@ __device__ __forceinline__ void PrefixCta<D>::softmax() {
               if (!(word >> j & 1)) sc[c][j] = 0xff800000u;
           }
         }
-        const float top = fmaxf(max_of(sc[1], max_of(sc[0], -INFINITY)), max_of(sc[3], max_of(sc[2], -INFINITY))) * a.own.scale_log2;
+        const float top = fmaxf(max_of(sc[1], max_of(sc[0], -INFINITY)), max_of(sc[3], max_of(sc[2], -INFINITY))) * a.scale_log2;
         if (__any_sync(0xffffffffu, top > m + kSlack)) {
           const float m_new = top > m + kSlack ? top - kHeadroom : m;
           const float f = m == m_new ? 1.f : ex2(m - m_new);
@@ -500,7 +836,7 @@ __device__ __forceinline__ void PrefixCta<D>::softmax() {
             tmem_wait_store();
           }
         }
-        scale = make_float2(a.own.scale_log2, a.own.scale_log2);
+        scale = make_float2(a.scale_log2, a.scale_log2);
         shift = m == -INFINITY ? make_float2(0.f, 0.f) : make_float2(-m, -m);
       }
 #pragma unroll
@@ -603,19 +939,19 @@ __device__ __forceinline__ void PrefixCta<D>::drain() {
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
-                                                                   const __grid_constant__ PrefixArgs a) {
+__global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_constant__ Maps maps, const __grid_constant__ PrefixArgs a) {
   using Geo = Geometry<D>;
-  using Stream = StreamGeometry<D, OwnStream<D>::kStages>;
+  using Own = OwnGeometry<D>;
   constexpr int kRingBytes = 2 * Geo::kQBytes + Geo::kSlots * Geo::kSlotBytes;
-  static_assert(2 * Stream::kBytes <= kRingBytes, "two streaming groups fit where the ring is");
+  static_assert(Own::kWarps * Own::kWarpBytes + sizeof(OwnControl) <= kRingBytes, "the streaming warps' memory fits where the ring is");
   extern __shared__ __align__(1024) uint8_t smem[];
   if (smem_u32(smem) & 1023) {      // never seen, as in tree attention; the joining kernel does without what is not there
     pdl_wait();
-    if (threadIdx.x == 0) raise(a.own.pool.status, kGaveUp);
+    if (threadIdx.x == 0) raise(a.pool.status, kGaveUp);
     return;
   }
-  PrefixControl* ctl = reinterpret_cast<PrefixControl*>(smem + kRingBytes);
+  PrefixControl* const ctl = reinterpret_cast<PrefixControl*>(smem + kRingBytes);
+  OwnControl* const own = reinterpret_cast<OwnControl*>(smem + Own::kWarps * Own::kWarpBytes);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   pdl_trigger();
   if (tid == 0) {
@@ -637,10 +973,13 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
     mbar_init(smem_u32(&ctl->q_first), 8);
     mbar_init(smem_u32(&ctl->drained), 1);
     ctl->give_up = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    tma_prefetch_map(&k_map);
-    tma_prefetch_map(&v_map);
+    ctl->own_places = 0;
+    tma_prefetch_map(&maps.k);
+    tma_prefetch_map(&maps.v);
+  } else if (tid < 1 + 8 * 6) {
+    mbar_init(smem_u32(&own->full[0][0] + (tid - 1)), 1);
   }
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   if (warp == 9) tmem_alloc(smem_u32(&ctl->tmem), 512);
   pdl_wait();
   if (warp == 10) {      // places of all prefixes
@@ -648,19 +987,18 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
     for (int p = lane; p < a.prefix.n; p += 32) {
       PrefixRange range;
       const bool ok = prefix_range(a, p, &range);
-      n += prefix_places(a.shape, static_cast<long long>(range.rows) * a.own.shape.group, prefix_units(a.shape, range.len)) * a.own.shape.n_kv_heads;
+      n += prefix_places(a.shape, static_cast<long long>(range.rows) * a.group, prefix_units(a.shape, range.len)) * a.pool.n_kv_heads;
       if (blockIdx.x == 0) {
-        if (!ok) raise(a.own.pool.status, kBadRows);
-        else if (range.rows && range.len > a.shape.capacity) raise(a.own.pool.status, kBadSlot);
+        if (!ok) raise(a.pool.status, kBadRows);
+        else if (range.rows && range.len > a.shape.capacity) raise(a.pool.status, kBadSlot);
       }
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
     if (lane == 0) ctl->places = n;
-  } else if (warp == 11) {      // and of the own positions
-    const long long n = a.own_cost ? Cursor(a.own, lane, 0, 1, blockIdx.x == 0).total : 0;
-    if (lane == 0) ctl->own_places = n;
   }
+  if (a.own_cost) add_up_own(a, own, &ctl->own_places);
+  fence_async_smem();      // the ring's copies follow where the sums were
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -670,16 +1008,13 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
   PrefixCta<D> cta{a, smem, ctl, n_prefix};
   if (warp < 8) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegisters));
-    if (is_prefix) {
-      cta.template softmax<T>();
-    } else if (own_places > 0) {
-      const int g = warp >> 2, worker = 2 * (static_cast<int>(blockIdx.x) - n_prefix) + g;
-      stream_share<T, D, OwnStream<D>::kStages>(a.own, OwnEnv{a, tid & 127, worker, 2 * (static_cast<int>(gridDim.x) - n_prefix), false, smem + g * Stream::kBytes,
-                                                              &ctl->own.seg[g], ctl->own.ml[g], 1 + g, D});
-    }
+    if (is_prefix) cta.template softmax<T>();
+    else if (own_places > 0)
+      own_share<T, D>(&maps.k_few, &maps.v_few, a, smem, own, &ctl->give_up, 8 * (static_cast<int>(blockIdx.x) - n_prefix) + warp, 8 * (static_cast<int>(gridDim.x) - n_prefix), own_places);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegisters));
-    if (is_prefix) cta.template feed<T>(&k_map, &v_map);
+    if (is_prefix) cta.template feed<T>(maps);
+    if (warp == 11) write_places(a, blockIdx.x, gridDim.x);
   }
   tc_fence_before();
   __syncthreads();
@@ -697,41 +1032,26 @@ template <typename Out, int D, bool kOwnRows>
 __global__ void __launch_bounds__(256) prefix_join_kernel(const __grid_constant__ PrefixArgs a) {
   pdl_trigger();
   pdl_wait();
-  const BatchView& b = a.own.b;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, group = a.own.shape.group, head = blockIdx.y;
-  const int64_t first_row = static_cast<int64_t>(blockIdx.x) * 32, row = first_row + lane;
-  const int t0 = static_cast<int>(first_row / group);
-  const int t = t0 + static_cast<int>(first_row - static_cast<int64_t>(t0) * group + lane) / group;
-  // The sequence of the row and its prefix: the warp looks the first row's up, the others are not far behind.
-  int s = seq_of_row(b, min(t0, b.n_tok - 1), lane), p = 0;
-  while (s < b.n_seq && __ldg(b.row_begin + s + 1) <= t) ++s;
-  const int s_first = __shfl_sync(0xffffffffu, s, 0);
-  for (int i = lane; i < a.prefix.n; i += 32) p += __ldg(a.prefix.seq_begin + i + 1) <= s_first ? 1 : 0;
-  p = __reduce_add_sync(0xffffffffu, p);
-  if (t >= b.n_tok || s >= b.n_seq) return;
-  const int first = __ldg(b.row_begin + s);
-  if (first < 0 || t < first || __ldg(b.row_begin + s + 1) > b.n_tok || __ldg(b.ctx_len + s) < 0) return;
-  while (p < a.prefix.n && __ldg(a.prefix.seq_begin + p + 1) <= s) ++p;
-
-  // Parts 0 .. n0 - 1 of the prefix, then n1 of the own positions: addresses of their first columns and statistics
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, group = a.group, head = blockIdx.y;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * 32 + lane;
+  if (row >= a.rows) return;
+  const int t = static_cast<int>(row / group);
   const int64_t at = static_cast<int64_t>(head) * a.rows + row;
-  int n0 = 0, n1 = 1, w0 = 0, w1 = 0, x0 = 0, x1 = 0;
-  PrefixRange range;
-  if (p < a.prefix.n && __ldg(a.prefix.seq_begin + p) <= s && prefix_range(a, p, &range) && prefix_units(a.shape, range.len) > 0) {
-    const int2 note = __ldcg(a.note[0] + at);
-    if (note.x >= 0 && note.y > 0 && note.y <= a.n_cta - note.x) {
-      w0 = note.x;
-      n0 = note.y;
-    }
-    x0 = static_cast<int>((row - static_cast<int64_t>(range.first) * group) % kPrefixRows);
+  const int4 place = __ldcg(a.place + t);
+  const int2 far = __ldcg(a.note[0] + at), near = kOwnRows ? make_int2(0, 1) : __ldcg(a.note[1] + at);
+  if (!place.x) return;
+  // Parts 0 .. n0 - 1 of the prefix, then n1 of the own positions
+  int n0 = 0, n1 = near.y, x0 = 0, x1 = 0;
+  const int w0 = far.x, w1 = near.x;
+  if (place.z >= 0 && far.x >= 0 && far.y > 0 && far.y <= a.n_cta - far.x) {
+    n0 = far.y;
+    x0 = static_cast<int>((row - static_cast<int64_t>(place.z) * group) % kPrefixRows);
   }
   if (!kOwnRows) {
-    const int2 note = __ldcg(a.note[1] + at);
-    w1 = note.x;
-    n1 = note.x >= 0 && note.y > 0 && note.y <= 2 * a.n_cta - note.x ? note.y : 0;
-    x1 = static_cast<int>((row - static_cast<int64_t>(first) * group) % 16);
+    if (near.x < 0 || near.y < 0 || near.y > 8 * a.n_cta - near.x) n1 = 0;
+    x1 = static_cast<int>((row - static_cast<int64_t>(place.y) * group) % kFewRows);
   }
-  const int64_t out_row = static_cast<int64_t>(t) * a.own.n_q_heads + head * group + (row - static_cast<int64_t>(t) * group);
+  const int64_t out_row = static_cast<int64_t>(t) * a.n_q_heads + head * group + (row - static_cast<int64_t>(t) * group);
   auto stats = [&](int i) {
     if (i < n0) return n0 == 1 ? __ldcg(a.whole_ml[0] + at) : __ldcg(a.part_ml + (2 * static_cast<int64_t>(w0 + i) + (i == 0)) * kPrefixRows + x0);
     i -= n0;
@@ -739,7 +1059,7 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(const __grid_constant_
       const float lse = __ldcg(reinterpret_cast<const float*>(a.whole_ml[1]) + out_row);
       return make_float2(lse * kLog2e, lse == -INFINITY ? 0.f : 1.f);
     }
-    return n1 == 1 ? __ldcg(a.whole_ml[1] + at) : __ldcg(a.own.part_ml + (2 * static_cast<int64_t>(w1 + i) + (i == 0)) * 16 + x1);
+    return n1 == 1 ? __ldcg(a.whole_ml[1] + at) : __ldcg(a.own_part_ml + (2 * static_cast<int64_t>(w1 + i) + (i == 0)) * kFewRows + x1);
   };
   auto columns = [&](int i, int quad) {
     if (i < n0) {
@@ -749,7 +1069,7 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(const __grid_constant_
     i -= n0;
     if (kOwnRows) return __ldcg(reinterpret_cast<const float4*>(a.whole_o[1]) + out_row * (D / 4) + quad);
     return n1 == 1 ? __ldcg(reinterpret_cast<const float4*>(a.whole_o[1]) + (static_cast<int64_t>(head) * (D / 4) + quad) * a.rows + row)
-                   : __ldcg(reinterpret_cast<const float4*>(a.own.part_o) + ((2 * static_cast<int64_t>(w1 + i) + (i == 0)) * (D / 4) + quad) * 16 + x1);
+                   : __ldcg(reinterpret_cast<const float4*>(a.own_part_o) + ((2 * static_cast<int64_t>(w1 + i) + (i == 0)) * (D / 4) + quad) * kFewRows + x1);
   };
   const int n = n0 + n1;
   constexpr int kQuads = D / 32;      // of a warp
@@ -798,11 +1118,11 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(const __grid_constant_
     }
   }
   const float inv = inverse_of(total);
-  Out* const dst = static_cast<Out*>(a.own.out) + out_row * D;
+  Out* const dst = static_cast<Out*>(a.out) + out_row * D;
 #pragma unroll
   for (int k = 0; k < kQuads; ++k)
     store4(dst + 4 * (warp * kQuads + k), make_float4(o[k].x * inv, o[k].y * inv, o[k].z * inv, o[k].w * inv));
-  if (a.own.lse && warp == 0) a.own.lse[out_row] = log_sum(m, total);
+  if (a.lse && warp == 0) a.lse[out_row] = log_sum(m, total);
 }
 
 constexpr int64_t kAlign = 256;
@@ -817,7 +1137,7 @@ cudaError_t launch_prefix(const prima_paged& pool, const PrefixArgs& a, cudaStre
   auto kernel = prefix_kernel<T, D>;
   cudaError_t e = allow_smem(kernel, kSmem, done);
   const Maps* maps = static_cast<const Maps*>(pool.maps);
-  if (e == cudaSuccess) e = launch_pdl(kernel, dim3(pool.sm_count), dim3(kPrefixThreads), kSmem, st, maps->k, maps->v, a);
+  if (e == cudaSuccess) e = launch_pdl(kernel, dim3(pool.sm_count), dim3(kPrefixThreads), kSmem, st, *maps, a);
   if (e != cudaSuccess) return e;
   const dim3 grid(static_cast<unsigned>((a.rows + 31) / 32), static_cast<unsigned>(pool.cfg.n_kv_heads));
   return launch_pdl(a.own_cost ? prefix_join_kernel<Out, D, false> : prefix_join_kernel<Out, D, true>, grid, dim3(256), 0, st, a);
@@ -834,8 +1154,8 @@ int64_t prima_prefix_attention_workspace(const prima_paged* p, int n_seq, int n_
   if (!p || n_seq < 1 || n_tok < 1 || n_q_heads < 1) return PRIMA_ERR_ARG;
   const int64_t rows = static_cast<int64_t>(n_tok) * n_q_heads, dim = p->cfg.head_dim, sm = p->sm_count;
   const int64_t whole = 2 * (padded(rows * dim * 4) + padded(rows * 8) + padded(rows * 8));
-  const int64_t parts = padded(2 * sm * kPrefixRows * dim * 4) + padded(2 * sm * kPrefixRows * 8) + padded(4 * sm * 16 * dim * 4) + padded(4 * sm * 16 * 8);
-  return whole + std::max(parts, parts - padded(4 * sm * 16 * dim * 4) - padded(4 * sm * 16 * 8) + prima_tree_attention_workspace(p, n_seq, n_tok, n_q_heads));
+  const int64_t parts = padded(2 * sm * kPrefixRows * dim * 4) + padded(2 * sm * kPrefixRows * 8), own = padded(16 * sm * kFewRows * dim * 4) + padded(16 * sm * kFewRows * 8);
+  return padded(static_cast<int64_t>(n_tok) * 16) + whole + parts + std::max(own, prima_tree_attention_workspace(p, n_seq, n_tok, n_q_heads));
 }
 
 int prima_prefix_attention(prima_paged* p, int layer, const prima_paged_batch* batch, const prima_prefix* prefix, const void* q, int n_q_heads,
@@ -863,19 +1183,18 @@ int prima_prefix_attention(prima_paged* p, int layer, const prima_paged_batch* b
   CallDevice dev(c.device);
   if (!dev.ok) return call_fail(PRIMA_ERR_CUDA, "cudaSetDevice failed");
   PrefixArgs a;
-  TreeArgs& own = a.own;
-  own.pool = view_of(*p);
-  own.b = view_of(*batch);
+  a.pool = view_of(*p);
+  a.b = view_of(*batch);
   const int group = n_q_heads / c.n_kv_heads;
-  own.shape = {c.n_kv_heads, group, batch->mask == nullptr, batch->table_stride << p->page_shift, kStreamSegmentCost, 16};
-  own.layer = layer;
-  own.n_q_heads = n_q_heads;
-  own.scale_log2 = scale * kLog2e;
-  own.group_inverse = small_inverse(group);
-  own.q = q;
-  own.out = out;
-  own.lse = lse;
-  own.notes = nullptr;
+  a.capacity = batch->table_stride << p->page_shift;
+  a.layer = layer;
+  a.n_q_heads = n_q_heads;
+  a.group = group;
+  a.group_inverse = small_inverse(group);
+  a.scale_log2 = scale * kLog2e;
+  a.q = q;
+  a.out = out;
+  a.lse = lse;
   a.prefix = {prefix->n_prefix, prefix->seq_begin, prefix->len, prefix->table, prefix->table_stride};
   a.shape = {c.n_kv_heads, prefix->table_stride << p->page_shift, kPrefixSegmentCost};
   a.rows = static_cast<int64_t>(batch->n_tok) * group;
@@ -887,6 +1206,7 @@ int prima_prefix_attention(prima_paged* p, int layer, const prima_paged_batch* b
     ws += padded(bytes);
     return at;
   };
+  a.place = reinterpret_cast<int4*>(take(batch->n_tok * static_cast<int64_t>(16)));
   for (int i = 0; i < 2; ++i) {
     a.whole_o[i] = reinterpret_cast<float*>(take(rows * dim * 4));
     a.whole_ml[i] = reinterpret_cast<float2*>(take(rows * 8));
@@ -896,13 +1216,13 @@ int prima_prefix_attention(prima_paged* p, int layer, const prima_paged_batch* b
   a.part_ml = reinterpret_cast<float2*>(take(2 * sm * kPrefixRows * 8));
   // Few rows of a sequence: its own positions are streamed beside the prefixes.  Many: tree attention's tensor-memory kernel
   // is the better one for them (its rule), and runs in front.
-  a.own_cost = streams(own.b, group) ? (dim == 128 ? kOwnCost128 : kOwnCost64) : 0;
+  a.own_cost = streams(a.b, group) ? (dim == 128 ? kOwnCost128 : kOwnCost64) : 0;
   if (a.own_cost) {
-    own.part_o = reinterpret_cast<float*>(take(4 * sm * 16 * dim * 4));
-    own.part_ml = reinterpret_cast<float2*>(take(4 * sm * 16 * 8));
+    a.own_part_o = reinterpret_cast<float*>(take(16 * sm * kFewRows * dim * 4));
+    a.own_part_ml = reinterpret_cast<float2*>(take(16 * sm * kFewRows * 8));
   } else {
-    own.part_o = nullptr;
-    own.part_ml = nullptr;
+    a.own_part_o = nullptr;
+    a.own_part_ml = nullptr;
     const int tree = prima_tree_attention(p, layer, batch, q, n_q_heads, scale, a.whole_o[1], PRIMA_DT_F32, reinterpret_cast<float*>(a.whole_ml[1]), ws,
                                           static_cast<char*>(workspace) + workspace_bytes - ws, stream);
     if (tree != PRIMA_OK) return tree;

@@ -70,6 +70,11 @@ using namespace prima;
 extern "C" {{
 long long places(int heads, long long cap, int over, long long rows, int len) {{ PrefixShape t{{heads, cap, over}}; return prefix_places(t, rows, prefix_units(t, len)); }}
 long long units(int heads, long long cap, int over, int len) {{ PrefixShape t{{heads, cap, over}}; return prefix_units(t, len); }}
+long long own_places_(int rows, long long limit) {{ return own_places(rows, limit); }}
+void own(long long limit, long long per_head, long long u, long long end, long long* out) {{
+  const OwnSegment s = own_segment(limit, per_head, u, end);
+  out[0] = s.head; out[1] = s.tile; out[2] = s.step0; out[3] = s.step1; out[4] = s.places; out[5] = s.last;
+}}
 int workers(long long p, long long o, int cost, int n) {{ return prefix_workers(p, o, cost, n); }}
 long long begin(long long total, int n, int c) {{ return tree_share_begin(tree_shares(total, n), c); }}
 int owner(long long total, int n, long long u) {{ return tree_cta_of(tree_shares(total, n), u); }}
@@ -85,6 +90,9 @@ void segment(int heads, long long cap, int over, long long rows, int len, long l
     i64, i32 = ctypes.c_longlong, ctypes.c_int
     L.places.argtypes, L.places.restype = [i32, i64, i32, i64, i32], i64
     L.units.argtypes, L.units.restype = [i32, i64, i32, i32], i64
+    L.own_places = L.own_places_
+    L.own_places.argtypes, L.own_places.restype = [i32, i64], i64
+    L.own.argtypes = [i64, i64, i64, i64, ctypes.POINTER(i64)]
     L.workers.argtypes = [i64, i64, i32, i32]
     L.begin.argtypes, L.begin.restype = [i64, i32, i32], i64
     L.owner.argtypes = [i64, i32, i64]
@@ -105,7 +113,7 @@ def test_shares_of_the_prefixes_cover_every_unit_once(index, seed):
     per_head = [index.places(heads, cap, over, int(r), int(n)) for r, n in zip(rows, length)]
     total = sum(per_head) * heads
     own = int(rs.choice([0, 5, 1000]))
-    n = index.workers(total, own, 16, n_cta)
+    n = index.workers(total, own, 128, n_cta)
     if total == 0:
         assert n == 0
         return
@@ -140,6 +148,40 @@ def test_shares_of_the_prefixes_cover_every_unit_once(index, seed):
 
 
 def test_workers_of_prefixes_and_own_positions(index):
-    assert index.workers(0, 100, 16, 148) == 0 and index.workers(100, 0, 16, 148) == 50 and index.workers(10 ** 6, 0, 16, 148) == 148
-    assert index.workers(1, 10 ** 9, 16, 148) == 1 and index.workers(10 ** 9, 1, 16, 148) == 147
-    assert index.workers(1000, 500, 16, 148) == 74 and index.workers(1 << 50, 1 << 50, 8, 148) == 74
+    assert index.workers(0, 100, 128, 148) == 0 and index.workers(100, 0, 128, 148) == 50 and index.workers(10 ** 6, 0, 128, 148) == 148
+    assert index.workers(1, 10 ** 9, 128, 148) == 1 and index.workers(10 ** 9, 1, 128, 148) == 147
+    assert index.workers(1000, 500, 128, 148) == 74 and index.workers(1 << 50, 1 << 50, 64, 148) == 74
+
+
+@pytest.mark.parametrize("seed", range(25))
+def test_shares_of_the_own_positions_cover_every_step_once(index, seed):
+    rs = np.random.RandomState(seed)
+    heads, n = int(rs.randint(1, 9)), int(rs.choice([1, 8, 9, 800]))
+    rows = rs.choice([0, 1, 5, 8, 16, 17, 33, 64], 12)
+    limit = rs.choice([1, 15, 16, 17, 128, 700, 3000], 12)
+    per_head = [index.own_places(int(r), int(m)) for r, m in zip(rows, limit)]
+    total = sum(per_head) * heads
+    if total == 0:
+        return
+    front = np.concatenate([[0], np.cumsum([p * heads for p in per_head])])
+    seen, out = {}, (ctypes.c_longlong * 6)()
+    for c in range(n):
+        u, end = index.begin(total, n, c), index.begin(total, n, c + 1)
+        while u < end:
+            s = int(np.searchsorted(front, u, side="right")) - 1
+            index.own(int(limit[s]), per_head[s], u - int(front[s]), end - int(front[s]), out)
+            head, tile, step0, step1, places, last = list(out)
+            assert 0 <= head < heads and 0 <= tile < -(-int(rows[s]) // 16) and places > 0 and 0 <= step0 <= step1
+            if step1 > step0:
+                seen.setdefault((s, head, tile), []).append((c, step0, step1))
+                owner = index.owner(total, n, last + int(front[s]))
+                assert owner >= c and (step1 == -(-int(limit[s]) // 16)) == (owner == c)
+            u += places
+        assert u == end
+    for s in range(12):
+        for head in range(heads):
+            for tile in range(-(-int(rows[s]) // 16)):
+                parts = seen.pop((s, head, tile))
+                assert [x[1] for x in parts] == [0] + [x[2] for x in parts[:-1]] and parts[-1][2] == -(-int(limit[s]) // 16)
+                assert [x[0] for x in parts] == list(range(parts[0][0], parts[0][0] + len(parts)))
+    assert not seen
