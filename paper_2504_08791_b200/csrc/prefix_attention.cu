@@ -36,7 +36,7 @@ constexpr int kPrefixSegmentCost = 4;  // in places
 constexpr int kManyRegisters = 208, kFewRegisters = 88;
 
 // What a step of 16 own positions costs, in 64ths of a prefix's place.
-constexpr int kOwnCost128 = 8, kOwnCost64 = 6;
+constexpr int kOwnCost128 = 10, kOwnCost64 = 6;
 
 struct PrefixView {
   int n;
@@ -1025,14 +1025,14 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
 }
 
 // ---- joining the parts ----------------------------------------------------------------------------------------------
-// blockIdx.y = KV head, blockIdx.x = 32 of its rows, one per lane; the eight warps share the columns, four at a time, so
-// that reads of the parts are contiguous across the rows.  kOwnRows: the own positions' attention is done, its outputs lie
-// as rows and its log-sum-exps behind one another.
+// blockIdx.y = KV head, blockIdx.x = 32 of its rows, one per lane; a warp has 4 columns, blockIdx.z 32 of them: reads of the
+// parts are contiguous across the rows, eight parts of a thread in flight.  kOwnRows: the own positions' attention is done, its
+// outputs lie as rows and its log-sum-exps behind one another.
 template <typename Out, int D, bool kOwnRows>
 __global__ void __launch_bounds__(256) prefix_join_kernel(const __grid_constant__ PrefixArgs a) {
   pdl_trigger();
   pdl_wait();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, group = a.group, head = blockIdx.y;
+  const int lane = threadIdx.x & 31, quad = blockIdx.z * 8 + (threadIdx.x >> 5), group = a.group, head = blockIdx.y;
   const int64_t row = static_cast<int64_t>(blockIdx.x) * 32 + lane;
   if (row >= a.rows) return;
   const int t = static_cast<int>(row / group);
@@ -1061,7 +1061,7 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(const __grid_constant_
     }
     return n1 == 1 ? __ldcg(a.whole_ml[1] + at) : __ldcg(a.own_part_ml + (2 * static_cast<int64_t>(w1 + i) + (i == 0)) * kFewRows + x1);
   };
-  auto columns = [&](int i, int quad) {
+  auto columns = [&](int i) {
     if (i < n0) {
       return n0 == 1 ? __ldcg(reinterpret_cast<const float4*>(a.whole_o[0]) + (static_cast<int64_t>(head) * (D / 4) + quad) * a.rows + row)
                      : __ldcg(reinterpret_cast<const float4*>(a.part_o) + ((2 * static_cast<int64_t>(w0 + i) + (i == 0)) * (D / 4) + quad) * kPrefixRows + x0);
@@ -1072,22 +1072,18 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(const __grid_constant_
                    : __ldcg(reinterpret_cast<const float4*>(a.own_part_o) + ((2 * static_cast<int64_t>(w1 + i) + (i == 0)) * (D / 4) + quad) * kFewRows + x1);
   };
   const int n = n0 + n1;
-  constexpr int kQuads = D / 32;      // of a warp
   float m = -INFINITY, total = 0.f;
-  float4 o[kQuads];
-#pragma unroll
-  for (int k = 0; k < kQuads; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-  constexpr int kFlight = 4;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  constexpr int kFlight = 8;
   for (int i0 = 0; i0 < n; i0 += kFlight) {
     float2 ml[kFlight];
-    float4 x[kFlight][kQuads];
+    float4 x[kFlight];
 #pragma unroll
     for (int j = 0; j < kFlight; ++j) {
       ml[j] = make_float2(-INFINITY, 0.f);
       if (i0 + j < n) {
         ml[j] = stats(i0 + j);
-#pragma unroll
-        for (int k = 0; k < kQuads; ++k) x[j][k] = columns(i0 + j, warp * kQuads + k);
+        x[j] = columns(i0 + j);
       }
     }
     float top = m;
@@ -1096,33 +1092,24 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(const __grid_constant_
     const float f = m == -INFINITY ? 0.f : ex2(m - top);
     m = top;
     total *= f;
-#pragma unroll
-    for (int k = 0; k < kQuads; ++k) {
-      o[k].x *= f;
-      o[k].y *= f;
-      o[k].z *= f;
-      o[k].w *= f;
-    }
+    o.x *= f;
+    o.y *= f;
+    o.z *= f;
+    o.w *= f;
 #pragma unroll
     for (int j = 0; j < kFlight; ++j) {
       if (ml[j].x == -INFINITY) continue;      // nothing was seen: its columns may be anything
       const float g = ex2(ml[j].x - m);
       total += ml[j].y * g;
-#pragma unroll
-      for (int k = 0; k < kQuads; ++k) {
-        o[k].x += x[j][k].x * g;
-        o[k].y += x[j][k].y * g;
-        o[k].z += x[j][k].z * g;
-        o[k].w += x[j][k].w * g;
-      }
+      o.x += x[j].x * g;
+      o.y += x[j].y * g;
+      o.z += x[j].z * g;
+      o.w += x[j].w * g;
     }
   }
   const float inv = inverse_of(total);
-  Out* const dst = static_cast<Out*>(a.out) + out_row * D;
-#pragma unroll
-  for (int k = 0; k < kQuads; ++k)
-    store4(dst + 4 * (warp * kQuads + k), make_float4(o[k].x * inv, o[k].y * inv, o[k].z * inv, o[k].w * inv));
-  if (a.lse && warp == 0) a.lse[out_row] = log_sum(m, total);
+  store4(static_cast<Out*>(a.out) + out_row * D + 4 * quad, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+  if (a.lse && quad == 0) a.lse[out_row] = log_sum(m, total);
 }
 
 constexpr int64_t kAlign = 256;
@@ -1139,7 +1126,7 @@ cudaError_t launch_prefix(const prima_paged& pool, const PrefixArgs& a, cudaStre
   const Maps* maps = static_cast<const Maps*>(pool.maps);
   if (e == cudaSuccess) e = launch_pdl(kernel, dim3(pool.sm_count), dim3(kPrefixThreads), kSmem, st, *maps, a);
   if (e != cudaSuccess) return e;
-  const dim3 grid(static_cast<unsigned>((a.rows + 31) / 32), static_cast<unsigned>(pool.cfg.n_kv_heads));
+  const dim3 grid(static_cast<unsigned>((a.rows + 31) / 32), static_cast<unsigned>(pool.cfg.n_kv_heads), D / 32);
   return launch_pdl(a.own_cost ? prefix_join_kernel<Out, D, false> : prefix_join_kernel<Out, D, true>, grid, dim3(256), 0, st, a);
 }
 
