@@ -1,22 +1,22 @@
 // Eviction from the paged cache: of a sequence's entries, those of largest weight stay and come together in front.
 //
 // Every (layer, sequence, KV head) chooses for itself, so a batch has hundreds of independent choices.  One kernel makes
-// them, a CTA each, and lists what moves; a second one moves keys, values, weights and positions with the whole GPU,
-// however few the choices are.  Moving only what lies behind slot m, into the free slots in front of it, costs
-// m (n - m) / n entries of n where a compaction in order would move nearly all m.
+// them, a CTA each, moves weights and positions and lists the rows of the cache that move; a second one moves keys and values
+// with the whole GPU, however few the choices are.  Moving only what lies behind slot m, into the free slots in front of it,
+// costs m (n - m) / n entries of n where a compaction in order would move nearly all m.
 #include <algorithm>
 #include <cstdio>
 
-#include "paged.cuh"
+#include "paged_device.cuh"
 
 namespace prima {
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32, kPer = 4, kTile = kThreads * kPer;
+constexpr int kThreads = 512, kWarps = kThreads / 32, kPer = 8, kTile = kThreads * kPer;
 constexpr int kBins = 2048, kDigits = 3;              // digits of 11, 11 and 10 bits
-// Keys that a CTA keeps in shared memory; those behind are made from the arrays again in every pass.  With 39 KB of keys
-// four CTAs share an SM, so that 592 choices run at once.
-constexpr int kCached = 10000;
+constexpr int kFlight = 8;                            // loads of a thread in flight
+// Keys that a CTA keeps in shared memory; those behind are made from the arrays again in every pass.
+constexpr int kCached = 24576;
 
 struct EvictArgs {
   PoolView pool;
@@ -34,7 +34,7 @@ struct EvictArgs {
   int32_t* born_out;
   int32_t* length_out;
   int32_t* counts;      // [items]
-  int32_t* lists;       // [items][2][half]: free slots in front, chosen ones behind
+  int32_t* lists;       // [items][2][half]: free slots in front, chosen ones behind; then their rows in the cache
   int64_t half;
   int cached;
 };
@@ -82,18 +82,19 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t* s_warp, uin
 
 // The m-th largest key by its digits, from the top: a histogram of the digit among the keys that agree with those found so
 // far, and the bin in which the count from above reaches what is still wanted.
+// Bound by latency: the passes over the keys of a CTA and their barriers.
 __global__ void __launch_bounds__(kThreads) evict_choose_kernel(const __grid_constant__ EvictArgs a) {
-  extern __shared__ uint32_t s_key[];
+  extern __shared__ __align__(16) uint32_t s_key[];
   __shared__ uint32_t s_hist[kBins];
   __shared__ uint32_t s_warp[kWarps];
-  __shared__ uint32_t s_found[2];      // bin, keys above it
-  const int item = blockIdx.x, head = item % a.pool.n_kv_heads, seq = item / a.pool.n_kv_heads % a.n_seq, tid = threadIdx.x;
+  __shared__ uint32_t s_found[3];      // bin, keys above it, keys in it
+  const int item = blockIdx.x, head = item % a.pool.n_kv_heads, ls = item / a.pool.n_kv_heads, seq = ls % a.n_seq, layer = ls / a.n_seq, tid = threadIdx.x;
   pdl_trigger();
   pdl_wait();
   int length;
   const Sizes z = sizes_of(a, seq, &length);
   const int n = z.n, m = z.m;
-  if (n < 0 && tid == 0 && item / a.pool.n_kv_heads < a.n_seq && head == 0) raise(a.pool.status, length < 0 || __ldg(a.keep + seq) < 0 ? kBadRows : kBadSlot);
+  if (n < 0 && tid == 0 && layer == 0 && head == 0) raise(a.pool.status, length < 0 || __ldg(a.keep + seq) < 0 ? kBadRows : kBadSlot);
   const int64_t at = static_cast<int64_t>(item) * a.stride;
   const float* const weight = a.weight + at;
   const int32_t* const born = a.born + at;
@@ -109,23 +110,46 @@ __global__ void __launch_bounds__(kThreads) evict_choose_kernel(const __grid_con
   }
   const bool some_recent = a.recent_from != nullptr;
   const int recent_from = some_recent ? __ldg(a.recent_from + seq) : 0;
-  auto make = [&](int j) {
-    const int b = born[j];
-    return key_of(weight[j], b < a.first || (some_recent && b >= recent_from));
-  };
-  for (int j = tid; j < min(n, a.cached); j += kThreads) s_key[j] = make(j);
-  auto key = [&](int j) { return j < a.cached ? s_key[j] : make(j); };
+  auto make = [&](float w, int b) { return key_of(w, b < a.first || (some_recent && b >= recent_from)); };
+  const int cached = min(n, a.cached);
+  for (int i = tid; i < kBins; i += kThreads) s_hist[i] = 0;
+  __syncthreads();
+  // Keys, and the histogram of their first digit
+  for (int j0 = tid; j0 < n; j0 += kThreads * kFlight) {
+    float w[kFlight];
+    int b[kFlight];
+#pragma unroll
+    for (int i = 0; i < kFlight; ++i) {
+      const int j = min(j0 + i * kThreads, n - 1);
+      w[i] = weight[j];
+      b[i] = born[j];
+    }
+#pragma unroll
+    for (int i = 0; i < kFlight; ++i) {
+      const int j = j0 + i * kThreads;
+      if (j >= n) continue;
+      const uint32_t k = make(w[i], b[i]);
+      if (j < cached) s_key[j] = k;
+      atomicAdd(&s_hist[k >> 21], 1u);
+    }
+  }
+  __syncthreads();
+  auto key = [&](int j) { return j < cached ? s_key[j] : make(weight[j], born[j]); };
 
   uint32_t prefix = 0, above = 0;      // digits found; keys that are larger
   for (int d = 0; d < kDigits; ++d) {
-    const int shift = d == 0 ? 21 : d == 1 ? 10 : 0, bins = d == 2 ? 1024 : 2048;
-    for (int i = tid; i < bins; i += kThreads) s_hist[i] = 0;
-    __syncthreads();
-    for (int j = tid; j < n; j += kThreads) {
-      const uint32_t k = key(j);
-      if (d == 0 || k >> (d == 1 ? 21 : 10) == prefix) atomicAdd(&s_hist[(k >> shift) & (bins - 1)], 1u);
+    const int bins = d == 2 ? 1024 : 2048;
+    if (d > 0) {
+      for (int i = tid; i < bins; i += kThreads) s_hist[i] = 0;
+      __syncthreads();
+      const int shift = d == 1 ? 10 : 0, done = d == 1 ? 21 : 10;
+#pragma unroll 4
+      for (int j = tid; j < n; j += kThreads) {
+        const uint32_t k = key(j);
+        if (k >> done == prefix) atomicAdd(&s_hist[(k >> shift) & (bins - 1)], 1u);
+      }
+      __syncthreads();
     }
-    __syncthreads();
     // thread t sums the bins below bins - t * per
     const int per = bins / kThreads, top = bins - tid * per;
     uint32_t mine = 0, total;
@@ -138,32 +162,41 @@ __global__ void __launch_bounds__(kThreads) evict_choose_kernel(const __grid_con
       while (sum + s_hist[top - i] < wanted) sum += s_hist[top - i++];
       s_found[0] = top - i;
       s_found[1] = sum;
+      s_found[2] = s_hist[top - i];
     }
     __syncthreads();
     prefix = d == 0 ? s_found[0] : prefix << (d == 1 ? 11 : 10) | s_found[0];
     above += s_found[1];
-    __syncthreads();
   }
-  const uint32_t border = prefix, wanted = m - above;      // of the keys equal to the border, the first `wanted` stay
+  // Of the keys equal to the border, the first `wanted` stay; nearly always those are all.
+  const uint32_t border = prefix, wanted = m - above;
+  const bool some_equal = s_found[2] != wanted;
 
   int32_t* const holes = a.lists + 2 * a.half * item;
   int32_t* const movers = holes + a.half;
   uint32_t equal_before = 0, holes_before = 0, movers_before = 0, total;
   for (int j0 = 0; j0 < n; j0 += kTile) {
     const int j = j0 + tid * kPer;
-    uint32_t k[kPer], equal = 0;
+    uint32_t k[kPer], rank = 0;
+    if (j + kPer <= cached) {
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      k[i] = j + i < n ? key(j + i) : 0u;
-      equal += j + i < n && k[i] == border ? 1u : 0u;
+      for (int i = 0; i < kPer; i += 4) *reinterpret_cast<uint4*>(k + i) = *reinterpret_cast<const uint4*>(s_key + j + i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) k[i] = j + i < n ? key(j + i) : 0u;
     }
-    uint32_t rank = equal_before + block_scan(equal, s_warp, &total) - equal;
-    equal_before += total;
-    uint32_t kept = 0, count = 0;      // holes in the lower half, movers in the upper one: 2048 at most each
+    if (some_equal) {
+      uint32_t equal = 0;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) equal += j + i < n && k[i] == border ? 1u : 0u;
+      rank = equal_before + block_scan(equal, s_warp, &total) - equal;
+      equal_before += total;
+    }
+    uint32_t kept = 0, count = 0;      // holes in the lower half, movers in the upper one: 4096 at most each
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       if (j + i >= n) continue;
-      const bool stays = k[i] > border || (k[i] == border && rank < wanted);
+      const bool stays = k[i] > border || (k[i] == border && (!some_equal || rank < wanted));
       rank += k[i] == border;
       kept |= stays ? 1u << i : 0u;
       count += j + i < m ? (stays ? 0u : 1u) : (stays ? 1u << 16 : 0u);
@@ -186,15 +219,29 @@ __global__ void __launch_bounds__(kThreads) evict_choose_kernel(const __grid_con
     holes_before += total & 0xffffu;
     movers_before += total >> 16;
   }
-  if (tid == 0) a.counts[item] = static_cast<int>(holes_before);
+  __syncthreads();
+  // Weights and positions move here (all that read the free slots' are done), and the lists become rows of the cache.
+  const int moves = static_cast<int>(holes_before);
+  const int32_t* const table = a.table + seq * a.table_stride;
+  if (tid == 0) a.counts[item] = moves;
+#pragma unroll 4
+  for (int i = tid; i < moves; i += kThreads) {
+    const int hole = holes[i], mover = movers[i];
+    a.weight_out[at + hole] = weight[mover];
+    a.born_out[at + hole] = born[mover];
+    const int64_t to = slot_row(a.pool, table, a.table_stride, layer, hole), from = slot_row(a.pool, table, a.table_stride, layer, mover);
+    const bool good = to >= 0 && from >= 0;      // a row is below 2^31 (prima_paged_create)
+    holes[i] = good ? static_cast<int>(to) + (head << a.pool.page_shift) : -1;
+    movers[i] = good ? static_cast<int>(from) + (head << a.pool.page_shift) : -1;
+  }
 }
 
 // blockIdx.x = (layer, sequence, KV head); its warps share the moves.  A warp takes the key and the value of 32 / (D / 4)
-// entries at a time, 16 bytes a lane, kFlight times in flight.
+// entries at a time, 16 bytes a lane, kFlight times in flight, while the rows of the next ones are read.
 template <int D>
 __global__ void __launch_bounds__(256) evict_move_kernel(const __grid_constant__ EvictArgs a) {
-  constexpr int kPieces = D / 8, kEntries = 16 / kPieces, kFlight = 4;
-  const int item = blockIdx.x, head = item % a.pool.n_kv_heads, ls = item / a.pool.n_kv_heads, seq = ls % a.n_seq, layer = ls / a.n_seq;
+  constexpr int kPieces = D / 8, kEntries = 16 / kPieces;
+  const int item = blockIdx.x, head = item % a.pool.n_kv_heads, seq = item / a.pool.n_kv_heads % a.n_seq;
   const int lane = threadIdx.x & 31, warp = blockIdx.y * 8 + (threadIdx.x >> 5), n_warps = gridDim.y * 8;
   pdl_trigger();
   pdl_wait();
@@ -204,37 +251,33 @@ __global__ void __launch_bounds__(256) evict_move_kernel(const __grid_constant__
     a.length_out[seq] = z.n < 0 ? length : z.m;
   }
   const int count = __ldg(a.counts + item);
-  const int32_t* const holes = a.lists + 2 * a.half * item;
-  const int32_t* const movers = holes + a.half;
-  const int32_t* const table = a.table + seq * a.table_stride;
-  const int64_t at = static_cast<int64_t>(item) * a.stride;
+  const int32_t* const to = a.lists + 2 * a.half * item;
+  const int32_t* const from = to + a.half;
   const int entry = lane / (2 * kPieces), piece = lane % kPieces, is_v = lane / kPieces & 1;
   uint4* const base = static_cast<uint4*>(is_v ? a.pool.v : a.pool.k) + piece;
-  for (int i0 = warp * kEntries * kFlight; i0 < count; i0 += n_warps * kEntries * kFlight) {
-    uint4 x[kFlight];
-    int64_t to[kFlight];
-    int hole[kFlight], mover[kFlight];
+  int row_to[kFlight], row_from[kFlight];
+  auto rows = [&](int i0) {
 #pragma unroll
     for (int f = 0; f < kFlight; ++f) {
       const int i = i0 + f * kEntries + entry;
-      hole[f] = i < count ? __ldg(holes + i) : -1;
-      mover[f] = i < count ? __ldg(movers + i) : -1;
+      row_to[f] = i < count ? __ldg(to + i) : -1;
+      row_from[f] = i < count ? __ldg(from + i) : -1;
     }
+  };
+  int i0 = warp * kEntries * kFlight;
+  rows(i0);
+  for (; i0 < count; i0 += n_warps * kEntries * kFlight) {
+    uint4 x[kFlight];
+    int dst[kFlight];
 #pragma unroll
     for (int f = 0; f < kFlight; ++f) {
-      to[f] = -1;
-      if (hole[f] < 0) continue;
-      const int64_t from = slot_row(a.pool, table, a.table_stride, layer, mover[f]);
-      to[f] = slot_row(a.pool, table, a.table_stride, layer, hole[f]);
-      if (from < 0) to[f] = -1;
-      if (to[f] >= 0) x[f] = __ldcg(base + (from + (static_cast<int64_t>(head) << a.pool.page_shift)) * kPieces);
+      dst[f] = row_to[f];
+      if (dst[f] >= 0) x[f] = __ldcs(base + static_cast<int64_t>(row_from[f]) * kPieces);
     }
+    rows(i0 + n_warps * kEntries * kFlight);
 #pragma unroll
-    for (int f = 0; f < kFlight; ++f) {
-      if (to[f] >= 0) base[(to[f] + (static_cast<int64_t>(head) << a.pool.page_shift)) * kPieces] = x[f];
-      if (hole[f] >= 0 && lane % (2 * kPieces) == 0) a.weight_out[at + hole[f]] = a.weight[at + mover[f]];
-      if (hole[f] >= 0 && lane % (2 * kPieces) == 1) a.born_out[at + hole[f]] = a.born[at + mover[f]];
-    }
+    for (int f = 0; f < kFlight; ++f)
+      if (dst[f] >= 0) base[static_cast<int64_t>(dst[f]) * kPieces] = x[f];
   }
 }
 
@@ -303,10 +346,12 @@ int prima_paged_evict(prima_paged* p, int n_seq, const int32_t* table, int64_t t
   a.half = (stride + 1) / 2;
   a.cached = static_cast<int>(std::min<int64_t>(stride, kCached));
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  cudaError_t e = launch_pdl(evict_choose_kernel, dim3(static_cast<unsigned>(items)), dim3(kThreads), a.cached * sizeof(uint32_t), st, a);
+  static bool done[kMaxDevices] = {};
+  cudaError_t e = allow_smem(evict_choose_kernel, kCached * sizeof(uint32_t), done);
+  if (e == cudaSuccess) e = launch_pdl(evict_choose_kernel, dim3(static_cast<unsigned>(items)), dim3(kThreads), a.cached * sizeof(uint32_t), st, a);
   // CTAs of a choice's moves: enough that a few choices fill the GPU
   const int64_t share = std::max<int64_t>(1, (16 * static_cast<int64_t>(p->sm_count) + items - 1) / items);
-  const int64_t most = (a.half + 31) / 32;
+  const int64_t most = (a.half + 63) / 64;
   const dim3 grid(static_cast<unsigned>(items), static_cast<unsigned>(std::min<int64_t>({share, most, 65535})));
   if (e == cudaSuccess) e = launch_pdl(p->cfg.head_dim == 128 ? evict_move_kernel<128> : evict_move_kernel<64>, grid, dim3(256), 0, st, a);
   return e == cudaSuccess ? PRIMA_OK : call_cuda_fail(e, "prima_paged_evict");

@@ -655,64 +655,91 @@ __device__ __forceinline__ void PrefixCta<D>::feed(const Maps& maps) {
     }
   } else if (warp == 9) {
     // ---- products ----
+    // Whichever group's operands are there goes next: scores of its next unit behind the product with the probabilities of
+    // the one before (they lie in the same columns, and one warp's products run in order).
     constexpr uint32_t kDescS = mma_f16_desc(kBf16, false, 128, kTilePos), kDescO = mma_f16_desc(kBf16, true, 128, D);
     const uint32_t u_tmem = uniform(tmem);
     const uint32_t ring_addr = uniform(smem_u32(s_ring)), q_addr = uniform(smem_u32(s_q));
     const SmemOperand k_all = smem_operand(ring_addr, 16), v_all = smem_operand(ring_addr, Geo::kPanel);
     uint32_t turns[2] = {0, 0};      // probabilities of an accumulator so far
+    bool ok = true;
     const PrefixWork* seg;
     for (uint32_t si = 0; (seg = segment(si)); ++si) {
-      const uint32_t both = uniform(seg->rows) > kPrefixRows / 2 ? 1 : 0;
-      const int count = uniform(seg->n) << both;
+      const bool both = uniform(seg->rows) > kPrefixRows / 2;
+      const int n = uniform(seg->n);
       done_with(si);
-      bool ok = wait_for(bar_q, si & 1, give_up, status);
+      ok = wait_for(bar_q, si & 1, give_up, status) && ok;
       ok = wait_for(bar_q + 8, si & 1, give_up, status) && ok;
-      RingPlace<kSlots> pk = ring, pv = ring;      // of the unit whose keys, whose values are due
-      pv.step(1);
-      // Sub-unit i: accumulator i % 2 and unit i, or unit i / 2 where a unit takes both
-      auto scores = [&](int i) {                   // S = Q K^T
-        const uint32_t h = i & 1;
-        const bool last = !both || h == 1;
-        if (!both || h == 0) ok = wait_for(bar_full + 8 * pk.slot, pk.phase, give_up, status) && ok;
-        tc_fence_after();
-        if (__all_sync(0xffffffffu, ok) && elect_one()) {
-          const SmemOperand qq = smem_operand(q_addr + h * Geo::kQBytes, 16), kk = k_all + pk.slot * Geo::kSlotBytes;
+      ok = __all_sync(0xffffffffu, ok);
+      // Of a group: units, scores and outputs issued, halves of the probabilities taken; the place of its next unit's keys, and
+      // of the unit's values whose probabilities come next.  Where only one group takes a unit it gives its places back twice.
+      int count[2], scored[2] = {0, 0}, summed[2] = {0, 0}, idle = 0;
+      uint32_t half[2] = {0, 0};
+      RingPlace<kSlots> pk[2] = {ring, ring}, pv[2];
 #pragma unroll
-          for (int k = 0; k < D / 16; ++k) mma_ss(u_tmem + h * kTilePos, qq + (k / 4 * Geo::kPanel + k % 4 * 32), kk + (k / 4 * Geo::kPanel + k % 4 * 32), kDescS, k > 0);
-          tc_commit(bar_s + 8 * h);
-          if (last) tc_commit(bar_empty + 8 * pk.slot);
-        }
-        __syncwarp();
-        if (last) pk.step(2);
+      for (int h = 0; h < 2; ++h) {
+        count[h] = both ? n : (n + 1 - h) >> 1;
+        if (!both && h) pk[h].step(2);
+        pv[h] = pk[h];
+        pv[h].step(1);
+      }
+      auto give_back = [&](uint32_t slot) {
+        tc_commit(bar_empty + 8 * slot);
+        if (!both) tc_commit(bar_empty + 8 * slot);
       };
-      for (int i = 0; i < min(count, 2); ++i) scores(i);
-      for (int i = 0; i < count; ++i) {
-        const uint32_t h = i & 1, phase = (h ? turns[1]++ : turns[0]++) & 1;
-        const bool first = i < 2, last = !both || h == 1;
-        if (!both || h == 0) ok = wait_for(bar_full + 8 * pv.slot, pv.phase, give_up, status) && ok;
-        // O += P V, each half of the positions when its P is there; the first product of a segment overwrites O, which its
-        // group has read by then (its P says so)
-        const SmemOperand vv = v_all + pv.slot * Geo::kSlotBytes;
+      while (ok && (summed[0] < count[0] || summed[1] < count[1])) {
+        bool any = false;
 #pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          ok = wait_for(bar_p + 16 * h + 8 * w, phase, give_up, status) && ok;
-          tc_fence_after();
-          if (__all_sync(0xffffffffu, ok) && elect_one()) {
+        for (int h = 0; h < 2; ++h) {
+          if (scored[h] > summed[h]) {      // O += P V, a half of the positions
+            const bool ready = mbar_peek(bar_p + 16 * h + 8 * half[h], turns[h] & 1) && (half[h] || mbar_peek(bar_full + 8 * pv[h].slot, pv[h].phase));
+            if (__all_sync(0xffffffffu, ready)) {
+              any = true;
+              tc_fence_after();
+              const SmemOperand vv = v_all + pv[h].slot * Geo::kSlotBytes;
+              const bool last = half[h];
+              if (elect_one()) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-              mma_ts(u_tmem + 256 + h * D, u_tmem + h * kTilePos + 32 * w + 8 * k, vv + (4 * w + k) * (16 * 128), kDescO, !first || w > 0 || k > 0);
-            if (w) {
-              if (i + 2 >= count) tc_commit(bar_pv + 8 * h);
-              if (last) tc_commit(bar_empty + 8 * pv.slot);
+                for (int k = 0; k < 4; ++k)
+                  mma_ts(u_tmem + 256 + h * D, u_tmem + h * kTilePos + 32 * half[h] + 8 * k, vv + (4 * half[h] + k) * (16 * 128), kDescO, summed[h] > 0 || last || k > 0);
+                if (last) {
+                  if (summed[h] + 1 == count[h]) tc_commit(bar_pv + 8 * h);
+                  give_back(pv[h].slot);
+                }
+              }
+              __syncwarp();
+              half[h] ^= 1;
+              if (last) {
+                ++turns[h];
+                ++summed[h];
+                pv[h].step(both ? 2 : 4);
+              }
             }
           }
-          __syncwarp();
+          if (scored[h] == summed[h] && scored[h] < count[h] && __all_sync(0xffffffffu, mbar_peek(bar_full + 8 * pk[h].slot, pk[h].phase))) {      // S = Q K^T
+            any = true;
+            tc_fence_after();
+            if (elect_one()) {
+              const SmemOperand qq = smem_operand(q_addr + h * Geo::kQBytes, 16), kk = k_all + pk[h].slot * Geo::kSlotBytes;
+#pragma unroll
+              for (int k = 0; k < D / 16; ++k) mma_ss(u_tmem + h * kTilePos, qq + (k / 4 * Geo::kPanel + k % 4 * 32), kk + (k / 4 * Geo::kPanel + k % 4 * 32), kDescS, k > 0);
+              tc_commit(bar_s + 8 * h);
+              give_back(pk[h].slot);
+            }
+            __syncwarp();
+            ++scored[h];
+            pk[h].step(both ? 2 : 4);
+          }
         }
-        if (last) pv.step(2);
-        // P lies over S: the next scores are written behind the product that reads it (one warp's products run in order)
-        if (i + 2 < count) scores(i + 2);
+        idle = any ? 0 : idle + 1;
+        if (idle == 1 << 22 || (idle % 1024 == 1023 && *static_cast<volatile int*>(give_up))) {
+          *static_cast<volatile int*>(give_up) = 1;
+          raise(status, kGaveUp);
+          ok = false;
+        }
       }
-      ring.skip(2 * (count >> both));
+      ok = __all_sync(0xffffffffu, ok);
+      ring.skip(2 * n);
     }
   }
 }
@@ -785,8 +812,9 @@ __device__ __forceinline__ void PrefixCta<D>::softmax() {
       if (i == count - 1) load_next();
       const bool edge = *static_cast<volatile int*>(&ctl->edge[(unit_base + t) % 16]) != 0;
       const volatile uint32_t* seen = ctl->seen[(unit_base + t) % 16];
-      if (edge && (!both || w == 0)) {
-        // Values at positions that are not seen may be anything, and 0 x NaN is NaN: clear them.
+      if (edge) {
+        // Values at positions that are not seen may be anything, and 0 x NaN is NaN: clear them (each group for its own
+        // product, which may come first).
         RingPlace<kSlots> pv = ring;
         pv.skip(2 * t + 1);
         wait_for(bar_full + 8 * pv.slot, pv.phase, give_up, status);
@@ -957,7 +985,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
   if (tid == 0) {
     for (int i = 0; i < 12; ++i) {
       mbar_init(smem_u32(&ctl->full[i]), 1);
-      mbar_init(smem_u32(&ctl->empty[i]), 1);
+      mbar_init(smem_u32(&ctl->empty[i]), 2);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&ctl->s_ready[i]), 1);
