@@ -12,8 +12,9 @@
 namespace prima {
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32, kPer = 8, kTile = kThreads * kPer;
-constexpr int kBins = 2048, kDigits = 3;              // digits of 11, 11 and 10 bits
+constexpr int kThreads = 512, kWarps = kThreads / 32, kPer = 4, kTile = kThreads * kPer;
+constexpr int kBins = 2048;                           // of a digit: 11, 11 and 10 bits
+constexpr int kListed = 2048;                         // keys with the border's first digit that are set apart
 constexpr int kFlight = 8;                            // loads of a thread in flight
 // Keys that a CTA keeps in shared memory; those behind are made from the arrays again in every pass.
 constexpr int kCached = 24576;
@@ -34,7 +35,7 @@ struct EvictArgs {
   int32_t* born_out;
   int32_t* length_out;
   int32_t* counts;      // [items]
-  int32_t* lists;       // [items][2][half]: free slots in front, chosen ones behind; then their rows in the cache
+  int32_t* lists;       // [items][2 * half]: free slots in front, chosen ones behind; then their rows in the cache
   int64_t half;
   int cached;
 };
@@ -58,21 +59,22 @@ __device__ __forceinline__ uint32_t key_of(float w, bool is_protected) {
   return u >> 31 ? ~u : u | 0x80000000u;
 }
 
-// Inclusive sums over the threads of the CTA; `total` is the sum of all.  Two barriers.
-__device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t* s_warp, uint32_t* total) {
+// Inclusive sums over the threads of the CTA; `total` is the sum of all.  One barrier: two scans that follow one another use
+// the two halves of s_warp in turns.
+__device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t (*s_warp)[kWarps], uint32_t& turn, uint32_t* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
     if (lane >= o) x += y;
   }
-  __syncthreads();
-  if (lane == 31) s_warp[warp] = x;
+  uint32_t* const sums = s_warp[turn++ & 1];
+  if (lane == 31) sums[warp] = x;
   __syncthreads();
   uint32_t before = 0, all = 0;
 #pragma unroll
   for (int i = 0; i < kWarps; ++i) {
-    const uint32_t y = s_warp[i];
+    const uint32_t y = sums[i];
     before += i < warp ? y : 0u;
     all += y;
   }
@@ -80,15 +82,40 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t* s_warp, uin
   return x + before;
 }
 
+// The same for kPer counts of every warp, those of place i behind all of place i - 1; `front`: what is in front of this warp's.
+__device__ __forceinline__ void tile_scan(const uint32_t (&count)[kPer], uint32_t (&front)[kPer], uint32_t (*s_tile)[kPer * kWarps], uint32_t& turn, uint32_t* total) {
+  static_assert(kPer * kWarps == 64, "two counts a lane");
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint32_t* const counts = s_tile[turn++ & 1];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i)
+    if (lane == i) counts[i * kWarps + warp] = count[i];
+  __syncthreads();
+  const uint2 mine = *reinterpret_cast<const uint2*>(counts + 2 * lane);
+  uint32_t x = mine.x + mine.y;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  *total = __shfl_sync(0xffffffffu, x, 31);
+  const uint32_t second = x - mine.y, first = second - mine.x;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) front[i] = __shfl_sync(0xffffffffu, warp & 1 ? second : first, (i * kWarps + warp) >> 1);
+}
+
 // The m-th largest key by its digits, from the top: a histogram of the digit among the keys that agree with those found so
 // far, and the bin in which the count from above reaches what is still wanted.
 // Bound by latency: the passes over the keys of a CTA and their barriers.
 __global__ void __launch_bounds__(kThreads) evict_choose_kernel(const __grid_constant__ EvictArgs a) {
   extern __shared__ __align__(16) uint32_t s_key[];
-  __shared__ uint32_t s_hist[kBins];
-  __shared__ uint32_t s_warp[kWarps];
-  __shared__ uint32_t s_found[3];      // bin, keys above it, keys in it
-  const int item = blockIdx.x, head = item % a.pool.n_kv_heads, ls = item / a.pool.n_kv_heads, seq = ls % a.n_seq, layer = ls / a.n_seq, tid = threadIdx.x;
+  __shared__ uint32_t s_hist[2][kBins];
+  __shared__ uint32_t s_list[kListed];
+  __shared__ uint32_t s_warp[2][kWarps];
+  __shared__ __align__(8) uint32_t s_tile[2][kPer * kWarps];
+  __shared__ uint32_t s_found[3], s_listed;      // bin, keys above it, keys in it
+  uint32_t turn = 0;
+  const int item = blockIdx.x, head = item % a.pool.n_kv_heads, ls = item / a.pool.n_kv_heads, seq = ls % a.n_seq, layer = ls / a.n_seq, tid = threadIdx.x, lane = tid & 31;
   pdl_trigger();
   pdl_wait();
   int length;
@@ -112,7 +139,8 @@ __global__ void __launch_bounds__(kThreads) evict_choose_kernel(const __grid_con
   const int recent_from = some_recent ? __ldg(a.recent_from + seq) : 0;
   auto make = [&](float w, int b) { return key_of(w, b < a.first || (some_recent && b >= recent_from)); };
   const int cached = min(n, a.cached);
-  for (int i = tid; i < kBins; i += kThreads) s_hist[i] = 0;
+  for (int i = tid; i < kBins; i += kThreads) s_hist[0][i] = s_hist[1][i] = 0;
+  if (tid == 0) s_listed = 0;
   __syncthreads();
   // Keys, and the histogram of their first digit
   for (int j0 = tid; j0 < n; j0 += kThreads * kFlight) {
@@ -120,9 +148,9 @@ __global__ void __launch_bounds__(kThreads) evict_choose_kernel(const __grid_con
     int b[kFlight];
 #pragma unroll
     for (int i = 0; i < kFlight; ++i) {
-      const int j = min(j0 + i * kThreads, n - 1);
-      w[i] = weight[j];
-      b[i] = born[j];
+      const int j = j0 + i * kThreads;
+      w[i] = j < n ? weight[j] : 0.f;
+      b[i] = j < n ? born[j] : 0;
     }
 #pragma unroll
     for (int i = 0; i < kFlight; ++i) {
@@ -130,109 +158,131 @@ __global__ void __launch_bounds__(kThreads) evict_choose_kernel(const __grid_con
       if (j >= n) continue;
       const uint32_t k = make(w[i], b[i]);
       if (j < cached) s_key[j] = k;
-      atomicAdd(&s_hist[k >> 21], 1u);
+      if (apart && j < m) {      // as if all of them stayed; what moves there overwrites them
+        a.weight_out[at + j] = w[i];
+        a.born_out[at + j] = b[i];
+      }
+      atomicAdd(&s_hist[0][k >> 21], 1u);
     }
   }
   __syncthreads();
   auto key = [&](int j) { return j < cached ? s_key[j] : make(weight[j], born[j]); };
 
   uint32_t prefix = 0, above = 0;      // digits found; keys that are larger
-  for (int d = 0; d < kDigits; ++d) {
-    const int bins = d == 2 ? 1024 : 2048;
-    if (d > 0) {
-      for (int i = tid; i < bins; i += kThreads) s_hist[i] = 0;
-      __syncthreads();
-      const int shift = d == 1 ? 10 : 0, done = d == 1 ? 21 : 10;
-#pragma unroll 4
-      for (int j = tid; j < n; j += kThreads) {
-        const uint32_t k = key(j);
-        if (k >> done == prefix) atomicAdd(&s_hist[(k >> shift) & (bins - 1)], 1u);
-      }
-      __syncthreads();
+  auto find = [&](const uint32_t* hist, int bits) {
+    // thread t has the `per` bins below bins - t * per
+    constexpr int kMost = kBins / kThreads;
+    const int per = (1 << bits) / kThreads, low = (1 << bits) - (tid + 1) * per;
+    uint32_t v[kMost], mine = 0, total;
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+      v[i] = i < per ? hist[low + i] : 0;
+      mine += v[i];
     }
-    // thread t sums the bins below bins - t * per
-    const int per = bins / kThreads, top = bins - tid * per;
-    uint32_t mine = 0, total;
-    for (int i = 1; i <= per; ++i) mine += s_hist[top - i];
-    uint32_t upto = block_scan(mine, s_warp, &total);
-    const uint32_t wanted = m - above;
+    const uint32_t upto = block_scan(mine, s_warp, turn, &total), wanted = m - above;
     if (upto >= wanted && upto - mine < wanted) {      // one thread
       uint32_t sum = upto - mine;
-      int i = 1;
-      while (sum + s_hist[top - i] < wanted) sum += s_hist[top - i++];
-      s_found[0] = top - i;
-      s_found[1] = sum;
-      s_found[2] = s_hist[top - i];
+      bool found = false;
+#pragma unroll
+      for (int i = kMost - 1; i >= 0; --i) {
+        if (i >= per || found) continue;
+        if (sum + v[i] >= wanted) {
+          s_found[0] = low + i;
+          s_found[1] = sum;
+          s_found[2] = v[i];
+          found = true;
+        }
+        sum += v[i];
+      }
     }
     __syncthreads();
-    prefix = d == 0 ? s_found[0] : prefix << (d == 1 ? 11 : 10) | s_found[0];
+    prefix = prefix << bits | s_found[0];
     above += s_found[1];
+  };
+  find(s_hist[0], 11);
+  // The keys with this first digit, few as a rule, are set apart in any order: only their numbers count.
+  const bool listed = s_found[2] <= kListed;
+  const int n_listed = listed ? static_cast<int>(s_found[2]) : n;
+  if (listed) {
+    for (int j = 4 * tid; j < n; j += 4 * kThreads) {
+      uint32_t k[4];
+      if (j + 4 <= cached) {
+        *reinterpret_cast<uint4*>(k) = *reinterpret_cast<const uint4*>(s_key + j);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) k[i] = j + i < n ? key(j + i) : ~prefix << 21;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (k[i] >> 21 == prefix) s_list[atomicAdd(&s_listed, 1u)] = k[i];
+    }
+  }
+  for (int i = tid; i < kBins; i += kThreads) s_hist[0][i] = 0;      // all have found the first digit; for the third
+  __syncthreads();
+#pragma unroll
+  for (int d = 1; d < 3; ++d) {
+    const int shift = d == 1 ? 10 : 0, done = d == 1 ? 21 : 10;
+    uint32_t* const hist = s_hist[d & 1];
+    for (int j = tid; j < n_listed; j += kThreads) {
+      const uint32_t k = listed ? s_list[j] : key(j);
+      if (k >> done == prefix) atomicAdd(&hist[(k >> shift) & (d == 1 ? 2047 : 1023)], 1u);
+    }
+    __syncthreads();
+    find(hist, d == 1 ? 11 : 10);
   }
   // Of the keys equal to the border, the first `wanted` stay; nearly always those are all.
   const uint32_t border = prefix, wanted = m - above;
   const bool some_equal = s_found[2] != wanted;
 
-  int32_t* const holes = a.lists + 2 * a.half * item;
-  int32_t* const movers = holes + a.half;
-  uint32_t equal_before = 0, holes_before = 0, movers_before = 0, total;
+  // What is out of place, in the order of the slots: the free slots in front, then as many chosen ones behind.
+  int32_t* const list = a.lists + 2 * a.half * item;
+  uint32_t equal_before = 0, listed_before = 0;
+  const uint32_t below = (1u << lane) - 1u;
   for (int j0 = 0; j0 < n; j0 += kTile) {
-    const int j = j0 + tid * kPer;
-    uint32_t k[kPer], rank = 0;
-    if (j + kPer <= cached) {
+    // Slot j0 + i * kThreads + tid: a warp's slots are consecutive, so that ranks are counts of bits and the list is written
+    // side by side.
+    uint32_t k[kPer], moves[kPer], count[kPer], front[kPer], total;
 #pragma unroll
-      for (int i = 0; i < kPer; i += 4) *reinterpret_cast<uint4*>(k + i) = *reinterpret_cast<const uint4*>(s_key + j + i);
-    } else {
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) k[i] = j + i < n ? key(j + i) : 0u;
+    for (int i = 0; i < kPer; ++i) {
+      const int j = j0 + i * kThreads + tid;
+      k[i] = j < n ? key(j) : 0u;
+      moves[i] = __ballot_sync(0xffffffffu, j < n && (k[i] > border || (k[i] == border && !some_equal)) != (j < m));
     }
     if (some_equal) {
-      uint32_t equal = 0;
+      uint32_t equal[kPer];
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) equal += j + i < n && k[i] == border ? 1u : 0u;
-      rank = equal_before + block_scan(equal, s_warp, &total) - equal;
+      for (int i = 0; i < kPer; ++i) {
+        equal[i] = __ballot_sync(0xffffffffu, j0 + i * kThreads + tid < n && k[i] == border);
+        count[i] = __popc(equal[i]);
+      }
+      tile_scan(count, front, s_tile, turn, &total);
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)      // one that stays after all
+        moves[i] ^= __ballot_sync(0xffffffffu, (equal[i] >> lane & 1) && equal_before + front[i] + __popc(equal[i] & below) < wanted);
       equal_before += total;
     }
-    uint32_t kept = 0, count = 0;      // holes in the lower half, movers in the upper one: 4096 at most each
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      if (j + i >= n) continue;
-      const bool stays = k[i] > border || (k[i] == border && (!some_equal || rank < wanted));
-      rank += k[i] == border;
-      kept |= stays ? 1u << i : 0u;
-      count += j + i < m ? (stays ? 0u : 1u) : (stays ? 1u << 16 : 0u);
-    }
-    const uint32_t upto = block_scan(count, s_warp, &total) - count;
-    uint32_t hole = holes_before + (upto & 0xffffu), mover = movers_before + (upto >> 16);
+    for (int i = 0; i < kPer; ++i) count[i] = __popc(moves[i]);
+    tile_scan(count, front, s_tile, turn, &total);
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      if (j + i >= n) continue;
-      const bool stays = kept >> i & 1;
-      if (j + i >= m) {
-        if (stays) movers[mover++] = j + i;
-      } else if (!stays) {
-        holes[hole++] = j + i;
-      } else if (apart) {
-        a.weight_out[at + j + i] = weight[j + i];
-        a.born_out[at + j + i] = born[j + i];
-      }
-    }
-    holes_before += total & 0xffffu;
-    movers_before += total >> 16;
+    for (int i = 0; i < kPer; ++i)
+      if (moves[i] >> lane & 1) list[listed_before + front[i] + __popc(moves[i] & below)] = j0 + i * kThreads + tid;
+    listed_before += total;
   }
   __syncthreads();
-  // Weights and positions move here (all that read the free slots' are done), and the lists become rows of the cache.
-  const int moves = static_cast<int>(holes_before);
+  // Weights and positions move here (all that read the free slots' are done), and the list becomes rows of the cache.
+  const int n_moves = static_cast<int>(listed_before / 2);
   const int32_t* const table = a.table + seq * a.table_stride;
-  if (tid == 0) a.counts[item] = moves;
+  if (tid == 0) a.counts[item] = n_moves;
 #pragma unroll 4
-  for (int i = tid; i < moves; i += kThreads) {
-    const int hole = holes[i], mover = movers[i];
+  for (int i = tid; i < n_moves; i += kThreads) {
+    const int hole = list[i], mover = list[n_moves + i];
     a.weight_out[at + hole] = weight[mover];
     a.born_out[at + hole] = born[mover];
     const int64_t to = slot_row(a.pool, table, a.table_stride, layer, hole), from = slot_row(a.pool, table, a.table_stride, layer, mover);
     const bool good = to >= 0 && from >= 0;      // a row is below 2^31 (prima_paged_create)
-    holes[i] = good ? static_cast<int>(to) + (head << a.pool.page_shift) : -1;
-    movers[i] = good ? static_cast<int>(from) + (head << a.pool.page_shift) : -1;
+    list[i] = good ? static_cast<int>(to) + (head << a.pool.page_shift) : -1;
+    list[n_moves + i] = good ? static_cast<int>(from) + (head << a.pool.page_shift) : -1;
   }
 }
 
@@ -252,7 +302,7 @@ __global__ void __launch_bounds__(256) evict_move_kernel(const __grid_constant__
   }
   const int count = __ldg(a.counts + item);
   const int32_t* const to = a.lists + 2 * a.half * item;
-  const int32_t* const from = to + a.half;
+  const int32_t* const from = to + count;
   const int entry = lane / (2 * kPieces), piece = lane % kPieces, is_v = lane / kPieces & 1;
   uint4* const base = static_cast<uint4*>(is_v ? a.pool.v : a.pool.k) + piece;
   int row_to[kFlight], row_from[kFlight];
