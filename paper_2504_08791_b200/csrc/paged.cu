@@ -3,7 +3,6 @@
 // All three kernels move bytes and compute next to nothing; what bounds them is HBM for large steps and, for the small
 // ones that decoding makes, the chain of dependent reads (row_begin -> ctx_len -> table -> entry), so each keeps that
 // chain short and has everything else in flight beside it.
-#include <algorithm>
 #include <cmath>
 #include <cstdio>
 #include <new>
@@ -23,26 +22,11 @@ namespace {
 // division per item the kernel was bound by instructions (65 us where it is 61 now).
 // Prompts of 11,268 rows, 40 + 16 heads of 128, bf16, 323 MB: 61 us, 5.3 TB/s, HBM; one row 3.0 us, 278 rows of
 // trees 6 us, latency.
-//
-// With a norm (HeadNorm) a head is multiplied by gain / sqrt(mean x^2 + eps) first: its lanes hold it whole, so the sum of
-// squares is one butterfly over D / 16 lanes.  The gain of the lane's 16 elements stays in registers from head to head
-// and is read again only where it changes.
-struct NoNorm {};
-struct HeadNorm {
-  const float* q_gain;
-  const float* k_gain;
-  int64_t q_gain_stride, k_gain_stride;
-  float eps;
-  bool wide;                   // gains may be read 16 bytes at a time
-  const int32_t* positions;
-  uint8_t axis[64], rank[64];
-};
-template <typename T, typename In, int D, int kWarps, typename Norm>
+template <typename T, typename In, int D, int kWarps>
 __global__ void __launch_bounds__(256) append_kernel(PoolView pool, BatchView b, int layer, const In* __restrict__ q, const In* __restrict__ k,
                                                      const In* __restrict__ v, int n_q_heads, int64_t q_stride, int64_t k_stride,
                                                      int64_t v_stride, bool wide, const double* __restrict__ freq, int mode,
-                                                     T* __restrict__ q_out, const __grid_constant__ Norm norm) {
-  constexpr bool kNorm = __is_same(Norm, HeadNorm);
+                                                     T* __restrict__ q_out) {
   constexpr int kPairs = D / 2, kItems = D / 16, kHeads = 32 / kItems, kStep = kWarps * kHeads;
   __shared__ __align__(16) float2 s_cs[8][kPairs];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -80,15 +64,7 @@ __global__ void __launch_bounds__(256) append_kernel(PoolView pool, BatchView b,
   if (!b.pos) p = static_cast<int>(slot);
   int64_t row = lane == 0 ? slot_row(pool, b.table + s * b.table_stride, b.table_stride, layer, slot) : 0;
   for (int i = lane; i < kPairs; i += 32) {
-    int rank = i;
-    if constexpr (kNorm) {
-      const int axis = norm.axis[i];
-      rank = norm.rank[i];
-      if (axis == PRIMA_AXIS_NONE) p = 0;      // not turned: by an angle of 0
-      else if (norm.positions) p = __ldg(norm.positions + static_cast<int64_t>(axis) * b.n_tok + t);
-      else p = b.pos ? __ldg(b.pos + t) : static_cast<int>(slot);
-    }
-    const double turns = p * __ldg(freq + rank);
+    const double turns = p * __ldg(freq + i);
     float sn, cs;
     sincospif(static_cast<float>(2.0 * (turns - rint(turns))), &sn, &cs);
     s_cs[warp][i] = make_float2(cs, sn);
@@ -102,8 +78,6 @@ __global__ void __launch_bounds__(256) append_kernel(PoolView pool, BatchView b,
   T* const q_dst = q_out + static_cast<int64_t>(t) * n_q_heads * D;
   T* const k_dst = static_cast<T*>(pool.k) + row * D;
   T* const v_dst = static_cast<T*>(pool.v) + row * D;
-  const float* gain_of = nullptr;
-  Raw8<float> gain[2];
   auto finish = [&](int h, const Item& raw) {
     const bool is_q = h < n_q_heads, is_v = h >= n_q_heads + G;
     if (h >= heads || (is_q ? !q : row < 0)) return;
@@ -112,28 +86,6 @@ __global__ void __launch_bounds__(256) append_kernel(PoolView pool, BatchView b,
     float lo[8], hi[8], u[8], w[8];
     to_f(raw.lo, lo);
     to_f(raw.hi, hi);
-    if constexpr (kNorm) {
-      const float* const from = is_q ? norm.q_gain : is_v ? nullptr : norm.k_gain;
-      if (from) {
-        const float* const mine = is_q ? from + h * norm.q_gain_stride : from + (h - n_q_heads) * norm.k_gain_stride;
-        if (mine != gain_of) {
-          load8(mine + (mode == 0 ? 8 * c : 16 * c), norm.wide, gain[0]);
-          load8(mine + (mode == 0 ? kPairs + 8 * c : 16 * c + 8), norm.wide, gain[1]);
-          gain_of = mine;
-        }
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum = fmaf(lo[i], lo[i], fmaf(hi[i], hi[i], sum));
-#pragma unroll
-        for (int o = 1; o < kItems; o <<= 1) sum += __shfl_xor_sync(((1u << kItems) - 1u) << (lane / kItems * kItems), sum, o);
-        const float f = rsqrtf(fmaf(sum, 1.f / D, norm.eps));
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          lo[i] *= f * __uint_as_float(gain[0].w[i]);
-          hi[i] *= f * __uint_as_float(gain[1].w[i]);
-        }
-      }
-    }
     if (is_v) {
       store8(dst + 16 * c, lo);
       store8(dst + 16 * c + 8, hi);
@@ -300,51 +252,15 @@ bool aligned16(const void* p) { return aligned_to(p, 16); }
 
 template <typename T, typename In, int D>
 cudaError_t launch_append(const prima_paged& pool, const BatchView& b, int layer, const void* q, const void* k, const void* v, int n_q_heads,
-                          int64_t qs, int64_t ks, int64_t vs, void* q_out, const HeadNorm* norm, cudaStream_t st) {
+                          int64_t qs, int64_t ks, int64_t vs, void* q_out, cudaStream_t st) {
   const int64_t per16 = 16 / static_cast<int64_t>(sizeof(In));
   const bool wide = (!q || (aligned16(q) && qs % per16 == 0)) && aligned16(k) && aligned16(v) && ks % per16 == 0 && vs % per16 == 0;
   // Few rows: a CTA's eight warps share one, for the shortest path; many: a warp each, which looks up least.  40 + 16
   // heads of 128, 64 rows 3.3 and 7.8 us, 1200 rows 9.5 and 10.2, 2400 rows 16.9 and 16.5, 9600 rows 66 and 56.
   const bool few = b.n_tok <= 16 * pool.sm_count;
-  const dim3 grid(few ? b.n_tok : (b.n_tok + 7) / 8);
-  auto launch = [&](auto kernel, const auto& n) {
-    return launch_pdl(kernel, grid, dim3(256), 0, st, view_of(pool), b, layer, static_cast<const In*>(q), static_cast<const In*>(k), static_cast<const In*>(v),
-                      n_q_heads, qs, ks, vs, wide, static_cast<const double*>(pool.freq), pool.cfg.rope_mode, static_cast<T*>(q_out), n);
-  };
-  if (norm) return launch(few ? append_kernel<T, In, D, 8, HeadNorm> : append_kernel<T, In, D, 1, HeadNorm>, *norm);
-  return launch(few ? append_kernel<T, In, D, 8, NoNorm> : append_kernel<T, In, D, 1, NoNorm>, NoNorm{});
-}
-
-// Both calls: the checks of the arguments that they share, and the launch.
-int append_rows(prima_paged* p, int layer, const prima_paged_batch* batch, const void* q, const void* k, const void* v, int in_dtype, int n_q_heads,
-                int64_t q_stride, int64_t k_stride, int64_t v_stride, const HeadNorm* norm, void* q_out, void* stream, const char* who) {
-  const prima_paged_config& c = p->cfg;
-  const char* bad = nullptr;
-  const size_t size = in_dtype == PRIMA_DT_F32 ? 4 : 2;
-  const int64_t need_q = static_cast<int64_t>(n_q_heads) * c.head_dim, need_kv = static_cast<int64_t>(c.n_kv_heads) * c.head_dim;
-  if (layer < 0 || layer >= c.n_layers) bad = "layer out of range";
-  else if (!k || !v || (q != nullptr) != (q_out != nullptr)) bad = "null k or v, or only one of q and q_out";
-  else if (in_dtype != PRIMA_DT_F32 && in_dtype != c.dtype) bad = "in_dtype is neither fp32 nor the cache's type";
-  else if (q ? n_q_heads < 1 || n_q_heads > (1 << 16) : n_q_heads != 0) bad = "n_q_heads";
-  else if (!aligned_to(q, size) || !aligned_to(k, size) || !aligned_to(v, size)) bad = "q, k or v is not aligned to its elements";
-  else if (!aligned16(q_out)) bad = "q_out must be 16-byte aligned";
-  else if ((q && q_stride < need_q) || k_stride < need_kv || v_stride < need_kv) bad = "a stride is shorter than a row";
-  if (bad) {
-    char msg[160];
-    snprintf(msg, sizeof msg, "%s: %s", who, bad);
-    return call_fail(PRIMA_ERR_ARG, msg);
-  }
-  CallDevice dev(c.device);
-  if (!dev.ok) return call_fail(PRIMA_ERR_CUDA, "cudaSetDevice failed");
-  using launcher = cudaError_t (*)(const prima_paged&, const BatchView&, int, const void*, const void*, const void*, int, int64_t, int64_t, int64_t, void*, const HeadNorm*,
-                                   cudaStream_t);
-  static const launcher table[2][2][2] = {
-      {{launch_append<__half, float, 64>, launch_append<__half, float, 128>}, {launch_append<__half, __half, 64>, launch_append<__half, __half, 128>}},
-      {{launch_append<__nv_bfloat16, float, 64>, launch_append<__nv_bfloat16, float, 128>},
-       {launch_append<__nv_bfloat16, __nv_bfloat16, 64>, launch_append<__nv_bfloat16, __nv_bfloat16, 128>}}};
-  const cudaError_t e = table[c.dtype == PRIMA_DT_BF16][in_dtype != PRIMA_DT_F32][c.head_dim == 128](*p, view_of(*batch), layer, q, k, v, n_q_heads, q_stride, k_stride,
-                                                                                                  v_stride, q_out, norm, static_cast<cudaStream_t>(stream));
-  return e == cudaSuccess ? PRIMA_OK : call_cuda_fail(e, who);
+  auto kernel = few ? append_kernel<T, In, D, 8> : append_kernel<T, In, D, 1>;
+  return launch_pdl(kernel, dim3(few ? b.n_tok : (b.n_tok + 7) / 8), dim3(256), 0, st, view_of(pool), b, layer, static_cast<const In*>(q), static_cast<const In*>(k),
+                    static_cast<const In*>(v), n_q_heads, qs, ks, vs, wide, static_cast<const double*>(pool.freq), pool.cfg.rope_mode, static_cast<T*>(q_out));
 }
 
 }  // namespace
@@ -359,6 +275,25 @@ int check_batch(const prima_paged* pool, const prima_paged_batch* b, const char*
   else if (b->mask && (b->mask_words < 1 || b->mask_words > 16)) bad = "mask_words outside 1..16";
   else if (!aligned_to(b->row_begin, 4) || !aligned_to(b->ctx_len, 4) || !aligned_to(b->table, 4) || !aligned_to(b->pos, 4) || !aligned_to(b->mask, 8))
     bad = "an array is not aligned to its elements";
+  if (!bad) return PRIMA_OK;
+  snprintf(msg, sizeof msg, "%s: %s", who, bad);
+  return call_fail(PRIMA_ERR_ARG, msg);
+}
+
+int check_append(const prima_paged* pool, int layer, const void* q, const void* k, const void* v, int in_dtype, int n_q_heads, int64_t q_stride, int64_t k_stride,
+                 int64_t v_stride, const void* q_out, const char* who) {
+  const prima_paged_config& c = pool->cfg;
+  const size_t size = in_dtype == PRIMA_DT_F32 ? 4 : 2;
+  const int64_t need_q = static_cast<int64_t>(n_q_heads) * c.head_dim, need_kv = static_cast<int64_t>(c.n_kv_heads) * c.head_dim;
+  char msg[160];
+  const char* bad = nullptr;
+  if (layer < 0 || layer >= c.n_layers) bad = "layer out of range";
+  else if (!k || !v || (q != nullptr) != (q_out != nullptr)) bad = "null k or v, or only one of q and q_out";
+  else if (in_dtype != PRIMA_DT_F32 && in_dtype != c.dtype) bad = "in_dtype is neither fp32 nor the cache's type";
+  else if (q ? n_q_heads < 1 || n_q_heads > (1 << 16) : n_q_heads != 0) bad = "n_q_heads";
+  else if (!aligned_to(q, size) || !aligned_to(k, size) || !aligned_to(v, size)) bad = "q, k or v is not aligned to its elements";
+  else if (!aligned_to(q_out, 16)) bad = "q_out must be 16-byte aligned";
+  else if ((q && q_stride < need_q) || k_stride < need_kv || v_stride < need_kv) bad = "a stride is shorter than a row";
   if (!bad) return PRIMA_OK;
   snprintf(msg, sizeof msg, "%s: %s", who, bad);
   return call_fail(PRIMA_ERR_ARG, msg);
@@ -447,35 +382,21 @@ int prima_paged_append(prima_paged* p, int layer, const prima_paged_batch* batch
                        int n_q_heads, int64_t q_stride, int64_t k_stride, int64_t v_stride, void* q_out, void* stream) {
   const int rc = check_batch(p, batch, "prima_paged_append");
   if (rc != PRIMA_OK) return rc;
-  return append_rows(p, layer, batch, q, k, v, in_dtype, n_q_heads, q_stride, k_stride, v_stride, nullptr, q_out, stream, "prima_paged_append");
-}
-
-int prima_paged_append_norm(prima_paged* p, int layer, const prima_paged_batch* batch, const void* q, const void* k, const void* v, int in_dtype,
-                            int n_q_heads, int64_t q_stride, int64_t k_stride, int64_t v_stride, const prima_head_norm* norm, void* q_out, void* stream) {
-  const int rc = check_batch(p, batch, "prima_paged_append_norm");
-  if (rc != PRIMA_OK) return rc;
-  if (!norm) return call_fail(PRIMA_ERR_ARG, "prima_paged_append_norm: null norm");
-  const int dim = p->cfg.head_dim;
-  if (!(norm->eps >= 0.f) || std::isinf(norm->eps)) return call_fail(PRIMA_ERR_ARG, "prima_paged_append_norm: eps must be finite and not negative");
-  if (norm->n_axes < 1 || norm->n_axes > PRIMA_MAX_AXES) return call_fail(PRIMA_ERR_ARG, "prima_paged_append_norm: n_axes outside 1..4");
-  for (int i = 0; i < dim / 2; ++i)
-    if ((norm->axis[i] >= norm->n_axes && norm->axis[i] != PRIMA_AXIS_NONE) || norm->rank[i] >= dim / 2)
-      return call_fail(PRIMA_ERR_ARG, "prima_paged_append_norm: an axis or rank out of range");
-  if ((norm->q_gain_stride != 0 && norm->q_gain_stride < dim) || (norm->k_gain_stride != 0 && norm->k_gain_stride < dim))
-    return call_fail(PRIMA_ERR_ARG, "prima_paged_append_norm: a gain's stride is neither 0 nor at least head_dim");
-  if (!aligned_to(norm->q_gain, 4) || !aligned_to(norm->k_gain, 4) || !aligned_to(norm->positions, 4))
-    return call_fail(PRIMA_ERR_ARG, "prima_paged_append_norm: an array is not 4-byte aligned");
-  HeadNorm n;
-  n.q_gain = norm->q_gain;
-  n.k_gain = norm->k_gain;
-  n.q_gain_stride = norm->q_gain_stride;
-  n.k_gain_stride = norm->k_gain_stride;
-  n.eps = norm->eps;
-  n.wide = aligned16(n.q_gain) && aligned16(n.k_gain) && n.q_gain_stride % 4 == 0 && n.k_gain_stride % 4 == 0;
-  n.positions = norm->positions;
-  std::copy(norm->axis, norm->axis + 64, n.axis);
-  std::copy(norm->rank, norm->rank + 64, n.rank);
-  return append_rows(p, layer, batch, q, k, v, in_dtype, n_q_heads, q_stride, k_stride, v_stride, &n, q_out, stream, "prima_paged_append_norm");
+  const int bad = check_append(p, layer, q, k, v, in_dtype, n_q_heads, q_stride, k_stride, v_stride, q_out, "prima_paged_append");
+  if (bad != PRIMA_OK) return bad;
+  const prima_paged_config& c = p->cfg;
+  CallDevice dev(c.device);
+  if (!dev.ok) return call_fail(PRIMA_ERR_CUDA, "cudaSetDevice failed");
+  const BatchView b = view_of(*batch);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  using launcher = cudaError_t (*)(const prima_paged&, const BatchView&, int, const void*, const void*, const void*, int, int64_t, int64_t, int64_t, void*, cudaStream_t);
+  static const launcher table[2][2][2] = {
+      {{launch_append<__half, float, 64>, launch_append<__half, float, 128>}, {launch_append<__half, __half, 64>, launch_append<__half, __half, 128>}},
+      {{launch_append<__nv_bfloat16, float, 64>, launch_append<__nv_bfloat16, float, 128>},
+       {launch_append<__nv_bfloat16, __nv_bfloat16, 64>, launch_append<__nv_bfloat16, __nv_bfloat16, 128>}}};
+  const cudaError_t e = table[c.dtype == PRIMA_DT_BF16][in_dtype != PRIMA_DT_F32][c.head_dim == 128](*p, b, layer, q, k, v, n_q_heads, q_stride, k_stride,
+                                                                                                  v_stride, q_out, st);
+  return e == cudaSuccess ? PRIMA_OK : call_cuda_fail(e, "prima_paged_append");
 }
 
 int prima_paged_accept(prima_paged* p, const prima_paged_batch* batch, const int32_t* path, const int32_t* path_len, int path_stride, void* stream) {

@@ -43,6 +43,10 @@ inline bool aligned_to(const void* p, size_t n) { return (reinterpret_cast<uintp
 // The checks of a batch that need no device memory; PRIMA_OK or an error that is already recorded.
 int check_batch(const prima_paged* pool, const prima_paged_batch* b, const char* who);
 
+// The same of an append's other arguments.
+int check_append(const prima_paged* pool, int layer, const void* q, const void* k, const void* v, int in_dtype, int n_q_heads, int64_t q_stride, int64_t k_stride,
+                 int64_t v_stride, const void* q_out, const char* who);
+
 // The tensor maps that the attention kernel's copies use (tree_attention.cu).
 cudaError_t make_tree_maps(prima_paged* pool);
 void free_tree_maps(prima_paged* pool);
@@ -84,6 +88,24 @@ __device__ __forceinline__ int64_t slot_row(const PoolView& p, const int32_t* ta
   if (row >= 0) return row;
   raise(p.status, static_cast<int>(-row));
   return -1;
+}
+
+// Two 32-bit operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 x, float2 y, float2 z) {
+  unsigned long long d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(*reinterpret_cast<unsigned long long*>(&x)), "l"(*reinterpret_cast<unsigned long long*>(&y)),
+      "l"(*reinterpret_cast<unsigned long long*>(&z)));
+  return *reinterpret_cast<float2*>(&d);
+}
+__device__ __forceinline__ float2 add2(float2 x, float2 y) {
+  unsigned long long d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*reinterpret_cast<unsigned long long*>(&x)), "l"(*reinterpret_cast<unsigned long long*>(&y)));
+  return *reinterpret_cast<float2*>(&d);
+}
+__device__ __forceinline__ float2 mul2(float2 x, float2 y) {
+  unsigned long long d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*reinterpret_cast<unsigned long long*>(&x)), "l"(*reinterpret_cast<unsigned long long*>(&y)));
+  return *reinterpret_cast<float2*>(&d);
 }
 
 template <typename T> struct Half2Of;

@@ -101,40 +101,6 @@ __device__ __forceinline__ float log_sum(float reference, float total) {
   return total == 0.f ? -INFINITY : (reference + kHeadroom + log2f(total * kDown)) * kLn2;
 }
 
-// Two 32-bit operations in one instruction.
-__device__ __forceinline__ float2 fma2(float2 x, float2 y, float2 z) {
-  unsigned long long d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(*reinterpret_cast<unsigned long long*>(&x)), "l"(*reinterpret_cast<unsigned long long*>(&y)),
-      "l"(*reinterpret_cast<unsigned long long*>(&z)));
-  return *reinterpret_cast<float2*>(&d);
-}
-__device__ __forceinline__ float2 add2(float2 x, float2 y) {
-  unsigned long long d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*reinterpret_cast<unsigned long long*>(&x)), "l"(*reinterpret_cast<unsigned long long*>(&y)));
-  return *reinterpret_cast<float2*>(&d);
-}
-__device__ __forceinline__ float2 mul2(float2 x, float2 y) {
-  unsigned long long d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*reinterpret_cast<unsigned long long*>(&x)), "l"(*reinterpret_cast<unsigned long long*>(&y)));
-  return *reinterpret_cast<float2*>(&d);
-}
-// 2^x of two numbers x < 128 by multiplications and additions, for kernels whose exponentials fill the special-function
-// units (4 a clock of each scheduler's, 8 cycles a warp): x is split into a whole number n and r in [-1/2, 1/2] by adding and
-// taking away 1.5 * 2^23, 2^r is the polynomial of degree 5 with the least largest relative error there (Remez exchange;
-// 7.5e-8, evaluated in 32 bits 2.1e-7, as much as ex2's bound of two units), 2^n is made from n's bits.  Below 2^-126.5 the
-// result is 0; NaN stays NaN.
-__device__ __forceinline__ float2 ex2_poly(float2 x) {
-  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-127.f));
-  asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-127.f));
-  constexpr float kRound = 12582912.f;
-  const float2 t = add2(x, make_float2(kRound, kRound)), r = fma2(add2(t, make_float2(-kRound, -kRound)), make_float2(-1.f, -1.f), x);
-  float2 p = fma2(r, make_float2(0.0013276472454890609f, 0.0013276472454890609f), make_float2(0.009675540961325169f, 0.009675540961325169f));
-  p = fma2(p, r, make_float2(0.05550713092088699f, 0.05550713092088699f));
-  p = fma2(p, r, make_float2(0.24022120237350464f, 0.24022120237350464f));
-  p = fma2(p, r, make_float2(0.6931469440460205f, 0.6931469440460205f));
-  p = fma2(p, r, make_float2(1.0000001192092896f, 1.0000001192092896f));
-  return mul2(p, make_float2(__uint_as_float((__float_as_uint(t.x) << 23) + 0x3f800000u), __uint_as_float((__float_as_uint(t.y) << 23) + 0x3f800000u)));
-}
 __device__ __forceinline__ float max3(float x, float y, float z) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(x), "f"(y), "f"(z));
