@@ -101,7 +101,17 @@ __global__ void __launch_bounds__(256) norm_kernel(PoolView pool, BatchView b, i
       else x[i] = Half2Of<In>::unpack(raw.w[i]);
     }
   };
-  auto finish = [&](int h, const Item& raw) {
+  // The sum of the lane's squares, where the head is normed.
+  auto squares_of = [&](int h, const Item& raw) {
+    if (h >= turned || !(h < n_q_heads ? norm.q_gain : norm.k_gain)) return 0.f;
+    float2 lo[4], hi[4], sum = make_float2(0.f, 0.f);
+    unpack(raw.lo, lo);
+    unpack(raw.hi, hi);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum = fma2(lo[i], lo[i], fma2(hi[i], hi[i], sum));
+    return sum.x + sum.y;
+  };
+  auto finish = [&](int h, const Item& raw, float sum) {
     const bool is_q = h < n_q_heads;
     if (h >= heads || (is_q ? !q : row < 0)) return;
     if (h >= turned) {
@@ -130,12 +140,6 @@ __global__ void __launch_bounds__(256) norm_kernel(PoolView pool, BatchView b, i
         load8(mine + kWide * c + kGap, norm.wide, gain[1]);
         gain_of = mine;
       }
-      float2 squares = make_float2(0.f, 0.f);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) squares = fma2(lo[i], lo[i], fma2(hi[i], hi[i], squares));
-      float sum = squares.x + squares.y;
-#pragma unroll
-      for (int o = 1; o < kItems; o <<= 1) sum += __shfl_xor_sync(((1u << kItems) - 1u) << (lane / kItems * kItems), sum, o);
       const float f = rsqrtf(fmaf(sum, 1.f / D, norm.eps));
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -162,12 +166,18 @@ __global__ void __launch_bounds__(256) norm_kernel(PoolView pool, BatchView b, i
     *reinterpret_cast<uint4*>(dst) = pack(u);
     *reinterpret_cast<uint4*>(dst + kGap) = pack(w);
   };
-  for (; h < heads; h += 2 * kStep) {
+  for (int h0 = warp % kWarps * kHeads; h0 < heads; h0 += 2 * kStep, h += 2 * kStep) {
     Item y[2];
     load(h + 2 * kStep, y[0]);
     load(h + 3 * kStep, y[1]);
-    finish(h, x[0]);
-    finish(h + kStep, x[1]);
+    float sum[2] = {squares_of(h, x[0]), squares_of(h + kStep, x[1])};
+#pragma unroll
+    for (int o = 1; o < kItems; o <<= 1) {
+      sum[0] += __shfl_xor_sync(0xffffffffu, sum[0], o);
+      sum[1] += __shfl_xor_sync(0xffffffffu, sum[1], o);
+    }
+    finish(h, x[0], sum[0]);
+    finish(h + kStep, x[1], sum[1]);
     x[0] = y[0];
     x[1] = y[1];
   }
