@@ -23,13 +23,15 @@ struct WeightsArgs {
 
 // ---- the work ---------------------------------------------------------------------------------------------------------
 // Positions are independent of one another, so nothing is joined: the blocks of kBlock positions of all (sequence, KV head)
-// form one line, and every worker (a warp) takes an equal stretch of it.
+// form one line, and every worker takes an equal stretch of it.  What the first block of a (sequence, KV head) costs besides
+// counts as kOverhead places in front of it.
+constexpr int kStreamOverhead = 2, kBlockOverhead = 1;
 struct WeightsWork {
   int seq, first, nodes, ctx, head;
   int n;                     // positions that the sequence has an entry for
   int block0, block1;
 };
-template <int kBlock>
+template <int kBlock, int kOverhead>
 struct WeightsCursor {
   const WeightsArgs& a;
   const int lane;
@@ -37,13 +39,14 @@ struct WeightsCursor {
   int w0 = 0, first = 0, nodes = 0, ctx = 0;
 
   __device__ __forceinline__ int64_t positions(int64_t ctx_, int64_t nodes_) const { return min(ctx_ + nodes_, a.slots); }
+  __device__ __forceinline__ int64_t per_head(int64_t n) const { return kOverhead + (n + kBlock - 1) / kBlock; }
   __device__ __forceinline__ bool read(int i) {
     const int f = __ldg(a.b.row_begin + i), e = __ldg(a.b.row_begin + i + 1), c = __ldg(a.b.ctx_len + i);
     const bool ok = f >= 0 && e >= f && e <= a.b.n_tok && c >= 0;
     first = f;
     nodes = ok ? e - f : 0;
     ctx = c;
-    blocks = nodes ? (positions(c, nodes) + kBlock - 1) / kBlock * a.pool.n_kv_heads : 0;
+    blocks = nodes ? per_head(positions(c, nodes)) * a.pool.n_kv_heads : 0;
     return ok;
   }
   __device__ void load(int64_t in_front) {
@@ -81,24 +84,27 @@ struct WeightsCursor {
     if (u < u_end) load(0);
   }
   __device__ bool next(WeightsWork* s) {
-    if (u >= u_end) return false;
-    unsigned hit;
-    while (!(hit = __ballot_sync(0xffffffffu, u >= before && u < before + blocks))) {      // ends: u is below the total
-      w0 += 32;
-      load(window);
+    while (u < u_end) {
+      unsigned hit;
+      while (!(hit = __ballot_sync(0xffffffffu, u >= before && u < before + blocks))) {      // ends: u is below the total
+        w0 += 32;
+        load(window);
+      }
+      const int src = __ffs(hit) - 1;
+      s->seq = w0 + src;
+      s->first = __shfl_sync(0xffffffffu, first, src);
+      s->nodes = __shfl_sync(0xffffffffu, nodes, src);
+      s->ctx = __shfl_sync(0xffffffffu, ctx, src);
+      s->n = static_cast<int>(positions(s->ctx, s->nodes));
+      const int64_t at = u - __shfl_sync(0xffffffffu, before, src), length = per_head(s->n);
+      s->head = static_cast<int>(div_small(at, length));
+      const int64_t r = at - s->head * length, places = min(length - r, u_end - u);
+      s->block0 = static_cast<int>(max(r - kOverhead, static_cast<int64_t>(0)));
+      s->block1 = static_cast<int>(max(r - kOverhead + places, static_cast<int64_t>(0)));
+      u += places;
+      if (s->block1 > s->block0) return true;
     }
-    const int src = __ffs(hit) - 1;
-    s->seq = w0 + src;
-    s->first = __shfl_sync(0xffffffffu, first, src);
-    s->nodes = __shfl_sync(0xffffffffu, nodes, src);
-    s->ctx = __shfl_sync(0xffffffffu, ctx, src);
-    s->n = static_cast<int>(positions(s->ctx, s->nodes));
-    const int64_t at = u - __shfl_sync(0xffffffffu, before, src), per_head = (static_cast<int64_t>(s->n) + kBlock - 1) / kBlock;
-    s->head = static_cast<int>(div_small(at, per_head));
-    s->block0 = static_cast<int>(at - s->head * per_head);
-    s->block1 = static_cast<int>(min(per_head, s->block0 + (u_end - u)));
-    u += s->block1 - s->block0;
-    return true;
+    return false;
   }
 };
 
@@ -119,7 +125,7 @@ __device__ __forceinline__ float shift_of(const WeightsArgs& a, const WeightsWor
 __device__ __forceinline__ int64_t entry_of(const WeightsArgs& a, const WeightsWork& s, int64_t j) {
   return (static_cast<int64_t>(s.seq) * a.pool.n_kv_heads + s.head) * a.stride + j;
 }
-__device__ __forceinline__ void put(const WeightsArgs& a, const WeightsWork& s, int j, float had, float sum) {
+__device__ __forceinline__ void put_entry(const WeightsArgs& a, const WeightsWork& s, int j, float had, float sum) {
   const int64_t at = entry_of(a, s, j);
   a.weight_out[at] = j < s.ctx && a.weight_in ? fmaf(a.decay, had, sum) : sum;
   if (a.born && j >= s.ctx) a.born[at] = a.b.pos ? __ldg(a.b.pos + s.first + (j - s.ctx)) : j;
@@ -127,111 +133,161 @@ __device__ __forceinline__ void put(const WeightsArgs& a, const WeightsWork& s, 
 
 // ---- few rows -----------------------------------------------------------------------------------------------------------
 // Scores with the positions as rows of m16n8k16 products and the query rows as columns, S^T = K Q^T: a lane then holds
-// scores of two positions, and the sum over the rows is one over its own columns and the quad.  Products do not mind in
-// which order the D axis runs, as long as both operands agree: a lane takes 16 consecutive bytes of a key (and of a query)
-// as its part of two products, so that keys go from memory into operands with wide loads and without shared memory.
-// A warp keeps kTiles * 8 rows of queries and takes 16 positions at a time, the next 16 on their way; where a sequence has
-// more rows, it reads its queries again for every 16 positions (all sums of a position before what it had is added, which
-// may be larger than all of them).
-constexpr int weights_ctas(int dim, int tiles) { return dim == 128 ? (tiles == 1 ? 4 : 2) : (tiles == 4 ? 3 : 4); }      // per SM: what the registers allow
+// scores of two positions, and the sum over the rows is one over its own columns and the quad.  A worker is a warp: it copies
+// 16 positions at a time through a ring of its own, some steps ahead and on into its next stretches, and keeps kTiles * 8
+// rows of queries in registers; where a sequence has more, it reads its queries again for every 16 positions (all sums of a
+// position before what it had is added, which may be larger than all of them).
+template <int D> struct StreamGeometry {
+  static constexpr int kWarps = 8, kStages = D == 128 ? 3 : 6;
+  static constexpr int kPanel = kFewPos * 128;                 // 64 columns of the keys of a step
+  static constexpr int kStage = kFewPos * D * 2;
+  static constexpr int kWarpBytes = kStages * kStage;
+};
+struct StreamControl {
+  unsigned long long full[8][6];
+  WeightsWork fifo[8][8];              // stretches between a warp's copies (at most five steps ahead) and its products
+  int give_up;
+};
+constexpr int stream_ctas(int dim, int tiles) { return dim == 128 && tiles == 4 ? 1 : 2; }      // per SM: what the registers allow
 template <typename T, int D, int kTiles>
-__global__ void __launch_bounds__(128, weights_ctas(D, kTiles)) weights_stream_kernel(const __grid_constant__ WeightsArgs a) {
+__global__ void __launch_bounds__(256, stream_ctas(D, kTiles)) weights_stream_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ WeightsArgs a) {
+  using Geo = StreamGeometry<D>;
   constexpr bool kBf16 = !__is_same(T, __half);
-  constexpr int kChunks = D / 32;      // 16-byte pieces of a row that a lane takes
-  const int lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  __shared__ StreamControl ctl;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t4 = lane & 3;
+  int* const status = a.pool.status;
+  uint8_t* const base = smem + (1024 - (smem_u32(smem) & 1023)) % 1024;
+  const uint32_t ring_addr = smem_u32(base) + warp * Geo::kWarpBytes, bar_full = smem_u32(ctl.full[warp]);
   pdl_trigger();
+  if (tid == 0) {
+    ctl.give_up = 0;
+    tma_prefetch_map(&k_map);
+  }
+  if (lane < 6) mbar_init(bar_full + 8 * lane, 1);
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  __syncthreads();
   pdl_wait();
-  WeightsCursor<16> cursor(a, lane, (blockIdx.x * 128 + threadIdx.x) >> 5, gridDim.x * 4);
-  WeightsWork s;
-  while (cursor.next(&s)) {
+  const int shift = a.pool.page_shift;
+  // Copies of a step: lane i < boxes takes 64 columns of box_rows positions.
+  const int box_rows = min(1 << shift, kFewPos), halves = kFewPos / box_rows, boxes = D / 64 * halves;
+  const int panel = lane / halves, half = lane % halves;
+  const uint32_t box_at = ring_addr + panel * Geo::kPanel + half * box_rows * 128;
+
+  WeightsCursor<kFewPos, kStreamOverhead> cursor(a, lane, blockIdx.x * Geo::kWarps + warp, gridDim.x * Geo::kWarps);
+  RingPlace<Geo::kStages> put, get;
+  uint32_t bad_stages[2] = {0, 0}, planned = 0, begun = 0;      // stages whose positions 0..7, 8..15 have no keys
+  // The stretch that is copied, its next block, the page that this lane's box of that block lies on
+  WeightsWork from{};
+  int next = 0, page = -1;
+  bool more = false;
+  auto read_page = [&]() {
+    const int pos = next * kFewPos + half * box_rows, slot = pos >> shift;
+    page = more && lane < boxes && pos < from.n && slot < a.b.table_stride ? __ldg(a.b.table + from.seq * a.b.table_stride + slot) : -1;
+  };
+  auto plan = [&]() {
+    more = cursor.next(&from);
+    next = from.block0;
+    if (more) {
+      __syncwarp();
+      if (lane == 0) ctl.fifo[warp][planned & 7] = from;
+      __syncwarp();
+      ++planned;
+    }
+  };
+  auto copy = [&]() {
+    if (!more) return;
+    const int pos = next * kFewPos + half * box_rows;
+    const bool wanted = lane < boxes && pos < from.n, good = static_cast<unsigned>(page) < static_cast<unsigned>(a.pool.n_pages);
+    if (wanted && !good) raise(status, pos >> shift < a.b.table_stride ? kBadPage : kBadSlot);
+    const uint32_t copies = __ballot_sync(0xffffffffu, wanted && good);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const bool bad = __any_sync(0xffffffffu, wanted && !good && (halves == 1 || half == h));
+      bad_stages[h] = (bad_stages[h] & ~(1u << put.slot)) | (bad ? 1u << put.slot : 0u);
+    }
+    if (lane == 0) mbar_expect(bar_full + 8 * put.slot, static_cast<uint32_t>(__popc(copies)) * box_rows * 128);
+    __syncwarp();
+    // below 2^31 rows (prima_paged_create)
+    const int row = (((a.layer * a.pool.n_pages + page) * a.pool.n_kv_heads + from.head) << shift) + (pos & ((1 << shift) - 1));
+    if (wanted && good) tma_load_2d(box_at + put.slot * Geo::kStage, &k_map, panel * 64, row, bar_full + 8 * put.slot);
+    put.step(1);
+    if (++next == from.block1) plan();
+    read_page();
+  };
+  plan();
+  read_page();
+#pragma unroll 1
+  for (int i = 0; i < Geo::kStages - 1; ++i) copy();
+
+  while (begun < planned) {
+    const WeightsWork s = ctl.fifo[warp][begun & 7];
+    ++begun;
     const int rows = s.nodes * a.group;      // n_tok * n_q_heads is below 2^31
-    const int32_t* const table = a.b.table + s.seq * a.b.table_stride;
-    const T* const keys = static_cast<const T*>(a.pool.k) + (static_cast<int64_t>(s.head) << a.pool.page_shift) * D;
     const float* const had_from = a.weight_in ? a.weight_in + entry_of(a, s, 0) : nullptr;
-    uint4 q[kTiles][kChunks];
-    float shift[kTiles][2];
+    // Fragments of the queries: column g of tile n, elements 2 t4, + 1 and + 8, + 9 of every 16
+    uint32_t q[kTiles][D / 16][2];
+    float down[kTiles][2];
     auto load_queries = [&](int row0) {
 #pragma unroll
       for (int n = 0; n < kTiles; ++n) {
         const int row = row0 + 8 * n + g, node = row / a.group;
-        const T* src = static_cast<const T*>(a.q) + static_cast<int64_t>((s.first + node) * a.n_q_heads + s.head * a.group + (row - node * a.group)) * D;
+        const uint32_t* src = reinterpret_cast<const uint32_t*>(static_cast<const T*>(a.q) + static_cast<int64_t>((s.first + node) * a.n_q_heads + s.head * a.group + (row - node * a.group)) * D) + t4;
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c) q[n][c] = row < rows ? __ldg(reinterpret_cast<const uint4*>(src) + t4 + 4 * c) : make_uint4(0, 0, 0, 0);
+        for (int k = 0; k < D / 16; ++k) {
+          q[n][k][0] = row < rows ? __ldg(src + 8 * k) : 0u;
+          q[n][k][1] = row < rows ? __ldg(src + 8 * k + 4) : 0u;
+        }
 #pragma unroll
-        for (int e = 0; e < 2; ++e) shift[n][e] = shift_of(a, s, row0 + 8 * n + 2 * t4 + e);
+        for (int e = 0; e < 2; ++e) down[n][e] = shift_of(a, s, row0 + 8 * n + 2 * t4 + e);
       }
     };
-    struct Keys {
-      uint4 k[2][kChunks];
-      float had;
-      int bad;             // bits: position has no key
-    };
-    // Positions 16 block + g and + 8: pages hold at least 8 positions, so each of the two lies in one page with its
-    // seven neighbours.  The ids of the pages are read a block ahead of the keys.
-    struct Pages {
-      int id[2];
-    };
-    const int blocks_end = s.block1;
-    auto pages_of = [&](int block, Pages& p) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int slot = (block * 16 + 8 * h) >> a.pool.page_shift;
-        p.id[h] = block < blocks_end && slot < a.b.table_stride ? __ldg(table + slot) : -1;
-      }
-    };
-    auto load = [&](int block, const Pages& p, Keys& x) {
-      x.bad = 0;
-      x.had = 0.f;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int j = block * 16 + 8 * h + g;
-        const bool wanted = block < blocks_end && j < s.n, good = static_cast<unsigned>(p.id[h]) < static_cast<unsigned>(a.pool.n_pages);
-        if (wanted && !good) raise(a.pool.status, j >> a.pool.page_shift < a.b.table_stride ? kBadPage : kBadSlot);
-        x.bad |= wanted && good ? 0 : 1 << h;
-        // below 2^31 rows (prima_paged_create)
-        const int row = ((a.layer * a.pool.n_pages + p.id[h]) * a.pool.n_kv_heads << a.pool.page_shift) + (j & ((1 << a.pool.page_shift) - 1));
-        const uint4* src = reinterpret_cast<const uint4*>(keys + static_cast<int64_t>(row) * D);
-#pragma unroll
-        for (int c = 0; c < kChunks; ++c) x.k[h][c] = wanted && good ? __ldg(src + t4 + 4 * c) : make_uint4(0, 0, 0, 0);
-        if (t4 == h && had_from && wanted && j < s.ctx) x.had = had_from[j];
-      }
+    // What position g (lanes with t4 = 0) or g + 8 (t4 = 1) of a block has had, read a block ahead
+    auto had_of = [&](int block) {
+      const int j = block * kFewPos + 8 * t4 + g;
+      return t4 < 2 && had_from && block < s.block1 && j < min(s.n, s.ctx) ? __ldcg(had_from + j) : 0.f;
     };
     const bool again = rows > 8 * kTiles;
-    Keys next;
-    Pages ahead;
-    pages_of(s.block0, ahead);
-    load(s.block0, ahead, next);
-    pages_of(s.block0 + 1, ahead);
+    float had_next = had_of(s.block0);
     load_queries(0);
 #pragma unroll 1
-    for (int block = s.block0; block < blocks_end; ++block) {
-      const Keys x = next;
-      load(block + 1, ahead, next);
-      pages_of(block + 2, ahead);
+    for (int block = s.block0; block < s.block1; ++block) {
+      __syncwarp();      // all have read the step whose place is filled again
+      copy();
+      const float had = had_next;
+      had_next = had_of(block + 1);
+      wait_for(bar_full + 8 * get.slot, get.phase, &ctl.give_up, status);
+      const uint32_t kk = ring_addr + get.slot * Geo::kStage;
+      const bool bad[2] = {(bad_stages[0] >> get.slot & 1) != 0, (bad_stages[1] >> get.slot & 1) != 0};
+      const bool edge = bad[0] || bad[1] || block * kFewPos + kFewPos > s.ctx;
       float sum[2] = {0.f, 0.f};
-      const bool edge = __any_sync(0xffffffffu, x.bad != 0) || block * 16 + 16 > s.ctx;
 #pragma unroll 1
       for (int row0 = 0; row0 < rows; row0 += 8 * kTiles) {
         if (again) load_queries(row0);
+        float c[kTiles][4];
 #pragma unroll
-        for (int n = 0; n < kTiles; ++n) {
-          float c[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int n = 0; n < kTiles; ++n)
 #pragma unroll
-          for (int k = 0; k < kChunks; ++k) {
-            const uint32_t lo[4] = {x.k[0][k].x, x.k[1][k].x, x.k[0][k].y, x.k[1][k].y}, hi[4] = {x.k[0][k].z, x.k[1][k].z, x.k[0][k].w, x.k[1][k].w};
-            mma16816<kBf16>(c, lo, q[n][k].x, q[n][k].y);
-            mma16816<kBf16>(c, hi, q[n][k].z, q[n][k].w);
-          }
+          for (int e = 0; e < 4; ++e) c[n][e] = 0.f;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          uint32_t x[4];
+          const int row = lane & 15, chunk = 2 * k + (lane >> 4);
+          ldsm4(x, kk + chunk / 8 * Geo::kPanel + row * 128 + (chunk % 8 ^ (row & 7)) * 16);
+#pragma unroll
+          for (int n = 0; n < kTiles; ++n) mma16816<kBf16>(c[n], x, q[n][k][0], q[n][k][1]);
+        }
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            float p = ex2(fmaf(c[e], a.scale_log2, shift[n][e & 1]));
+            float p = ex2(fmaf(c[n][e], a.scale_log2, down[n][e & 1]));
             if (edge) {
-              const int row = row0 + 8 * n + 2 * t4 + (e & 1), i = block * 16 + 8 * (e >> 1) + g - s.ctx;
-              if ((x.bad >> (e >> 1) & 1) || shift[n][e & 1] == -INFINITY || (i >= 0 && !sees(a, s.first, row / a.group, i))) p = 0.f;
+              const int row = row0 + 8 * n + 2 * t4 + (e & 1), i = block * kFewPos + 8 * (e >> 1) + g - s.ctx;
+              if (bad[e >> 1] || down[n][e & 1] == -INFINITY || (i >= 0 && !sees(a, s.first, row / a.group, i))) p = 0.f;
             }
             sum[e >> 1] += p;
           }
-        }
       }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -239,11 +295,16 @@ __global__ void __launch_bounds__(128, weights_ctas(D, kTiles)) weights_stream_k
         sum[h] += __shfl_xor_sync(0xffffffffu, sum[h], 2);
       }
       if (t4 < 2) {
-        const int j = block * 16 + 8 * t4 + g;
-        if (j < s.n) put(a, s, j, x.had, t4 ? sum[1] : sum[0]);
+        const int j = block * kFewPos + 8 * t4 + g;
+        if (j < s.n) put_entry(a, s, j, had, t4 ? sum[1] : sum[0]);
       }
+      get.step(1);
     }
   }
+  // A wait that gave up may have left copies under way: they end before the memory is given back.
+  if (*static_cast<volatile int*>(&ctl.give_up))
+    for (uint32_t i = 0; i < Geo::kStages; ++i)
+      for (int j = 0; j < (1 << 16) && !mbar_test(bar_full + 8 * i, i < put.slot ? put.phase : put.phase ^ 1); ++j) {}
 }
 
 // ---- many rows ----------------------------------------------------------------------------------------------------------
@@ -337,7 +398,7 @@ __global__ void __launch_bounds__(kBlockThreads, 1) weights_block_kernel(const _
 
   if (warp == 10) {
     // ---- the plan ----
-    WeightsCursor<kTilePos> cursor(a, lane, blockIdx.x, gridDim.x);
+    WeightsCursor<kTilePos, kBlockOverhead> cursor(a, lane, blockIdx.x, gridDim.x);
     WeightsWork s;
     for (uint32_t i = 0;; ++i) {
       const bool more = cursor.next(&s);
@@ -554,7 +615,7 @@ __global__ void __launch_bounds__(kBlockThreads, 1) weights_block_kernel(const _
             if (lane == 0) mbar_arrive(bar_part_free);
           }
         }
-        if ((single || h == 0) && j < s.n) put(a, s, j, had, hidden ? 0.f : total);
+        if ((single || h == 0) && j < s.n) put_entry(a, s, j, had, hidden ? 0.f : total);
       }
       unit_base += blocks;
       done_with(i);
@@ -584,7 +645,12 @@ constexpr int64_t kLongest = 2147483647 - 255;      // positions that the arrays
 
 template <typename T, int D, int kTiles>
 cudaError_t launch_stream(const prima_paged& pool, const WeightsArgs& a, cudaStream_t st) {
-  return launch_pdl(weights_stream_kernel<T, D, kTiles>, dim3(pool.sm_count * weights_ctas(D, kTiles)), dim3(128), 0, st, a);
+  constexpr size_t kSmem = 1024 + StreamGeometry<D>::kWarps * StreamGeometry<D>::kWarpBytes;
+  static bool done[kMaxDevices] = {};
+  auto kernel = weights_stream_kernel<T, D, kTiles>;
+  const cudaError_t e = allow_smem(kernel, kSmem, done);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(kernel, dim3(stream_ctas(D, kTiles) * pool.sm_count), dim3(256), kSmem, st, static_cast<const Maps*>(pool.maps)->k_few, a);
 }
 template <typename T, int D>
 cudaError_t launch_block(const prima_paged& pool, const WeightsArgs& a, cudaStream_t st) {
