@@ -156,6 +156,30 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
 
+// A tile of up to 128 rows of queries into shared memory in the background, by 128 threads (r: this one): rows of 128 bytes
+// in the 128-byte swizzle, 64 columns a panel; rows behind the last one are zeros.  Row x is query head (in0 + x) % group of a KV
+// head, (in0 + x) / group tokens behind the one that `from` (that token's first query head of the KV head) belongs to.  A
+// thread takes one 16-byte piece of every 128 / (D / 8)-th row and steps its place without divisions.
+template <typename T, int D>
+__device__ __forceinline__ void load_query_tile(uint32_t tile, int panel_bytes, const T* from, int in0, int group, int64_t token_stride, int rows, int r) {
+  constexpr int kPieces = D / 8, kStep = 128 / kPieces;
+  const int piece = r % kPieces, row0 = r / kPieces, tokens = kStep / group, heads = kStep - tokens * group;
+  int token = (in0 + row0) / group, in_group = in0 + row0 - token * group;
+  const uint32_t dst = tile + piece / 8 * panel_bytes;
+#pragma unroll 4
+  for (int row = row0; row < 128; row += kStep) {
+    const bool there = row < rows;
+    copy16(dst + row * 128 + ((piece % 8) ^ (row & 7)) * 16, from + (there ? token * token_stride + in_group * D : 0) + piece * 8, there);
+    token += tokens;
+    in_group += heads;
+    if (in_group >= group) {
+      in_group -= group;
+      ++token;
+    }
+  }
+  asm volatile("cp.async.commit_group;" ::: "memory");
+}
+
 // ---- fragments of m16n8k16 -------------------------------------------------------------------------------------------
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");

@@ -496,18 +496,10 @@ __global__ void __launch_bounds__(kBlockThreads, 1) weights_block_kernel(const _
     uint32_t turn = 0, n_part = 0, unit_base = 0;
     // Tile t of a stretch into place p of this group, in the background, and its rows' shifts.
     auto load_tile = [&](const WeightsWork& s, int t, int p) {
-      constexpr int kPieces = D / 8;
-      const int rows = s.nodes * a.group;
-      uint8_t* const dst = smem + (2 * h + p) * Geo::kTileBytes;
-#pragma unroll 4
-      for (int idx = r; idx < kRowTile * kPieces; idx += 128) {
-        const int in_tile = idx / kPieces, piece = idx % kPieces, row = t * kRowTile + in_tile;
-        const bool there = row < rows;
-        const int node = there ? row / a.group : 0, in_group = there ? row - node * a.group : 0;
-        copy16(smem_u32(dst) + piece / 8 * Geo::kPanel + in_tile * 128 + ((piece % 8) ^ (in_tile & 7)) * 16,
-               static_cast<const T*>(a.q) + (static_cast<int64_t>(s.first + node) * a.n_q_heads + s.head * a.group + in_group) * D + piece * 8, there);
-      }
-      asm volatile("cp.async.commit_group;" ::: "memory");
+      const int row0 = t * kRowTile, token0 = row0 / a.group;
+      load_query_tile<T, D>(smem_u32(smem) + (2 * h + p) * Geo::kTileBytes, Geo::kPanel,
+                            static_cast<const T*>(a.q) + (static_cast<int64_t>(s.first + token0) * a.n_q_heads + s.head * a.group) * D, row0 - token0 * a.group, a.group,
+                            static_cast<int64_t>(a.n_q_heads) * D, s.nodes * a.group - row0, r);
       ctl->shift[2 * h + p][r] = shift_of(a, s, t * kRowTile + r);
     };
     auto group_sync = [&]() { asm volatile("bar.sync %0, 128;" ::"r"(1 + h) : "memory"); };

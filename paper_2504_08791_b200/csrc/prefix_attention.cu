@@ -114,24 +114,27 @@ __device__ __forceinline__ bool prefix_range(const PrefixArgs& a, int p, PrefixR
   return true;
 }
 
-// Walks the share of a prefixes' worker, 32 prefixes at a time, one per lane.
+// The prefixes' line, 32 prefixes at a time, one per lane of a warp: its length, then a worker's share of it.
 struct PrefixCursor {
   const PrefixArgs& a;
-  const int lane, worker, n_workers;
-  const long long total;
-  long long u, u_end;
-  int p0 = 0;                          // first prefix of the window
-  long long window = 0, before = 0, per_head = 0, places = 0;
+  const int lane;
+  int worker = 0, p0 = 0;              // p0: first prefix of the window
+  long long total = 0, u = 0, u_end = 0, window = 0, before = 0, per_head = 0, places = 0;
+  TreeShares shares{};
   PrefixRange range;
 
-  __device__ void load(long long in_front) {
-    per_head = 0;
-    range = PrefixRange();
-    if (p0 + lane < a.prefix.n) {
-      prefix_range(a, p0 + lane, &range);
-      per_head = prefix_places(a.shape, static_cast<long long>(range.rows) * a.group, prefix_units(a.shape, range.len));
+  __device__ __forceinline__ bool read(int p) {
+    const bool ok = prefix_range(a, p, &range);
+    per_head = prefix_places(a.shape, static_cast<long long>(range.rows) * a.group, prefix_units(a.shape, range.len));
+    places = per_head * a.pool.n_kv_heads;
+    return ok;
+  }
+  __device__ void load(long long in_front, bool has_read = false) {
+    if (!has_read) {
+      per_head = places = 0;
+      range = PrefixRange();
+      if (p0 + lane < a.prefix.n) read(p0 + lane);
     }
-    places = per_head * a.shape.n_kv_heads;
     long long x = places;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -141,12 +144,25 @@ struct PrefixCursor {
     before = in_front + x - places;
     window = in_front + __shfl_sync(0xffffffffu, x, 31);
   }
-  __device__ PrefixCursor(const PrefixArgs& args, int lane_, int worker_, int n_workers_, long long total_)
-      : a(args), lane(lane_), worker(worker_), n_workers(n_workers_), total(total_) {
-    const TreeShares shares = tree_shares(total, n_workers);
+  __device__ __forceinline__ PrefixCursor(const PrefixArgs& args, int lane_) : a(args), lane(lane_) {}
+  __device__ __forceinline__ void add_up(bool reports) {
+    for (int p = lane; p < a.prefix.n; p += 32) {
+      const bool ok = read(p);
+      total += places;
+      if (reports) {
+        if (!ok) raise(a.pool.status, kBadRows);
+        else if (range.rows && range.len > a.shape.capacity) raise(a.pool.status, kBadSlot);
+      }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+  }
+  __device__ __forceinline__ void begin(int worker_, int n_workers) {
+    worker = worker_;
+    shares = tree_shares(total, n_workers);
     u = tree_share_begin(shares, worker);
     u_end = tree_share_begin(shares, worker + 1);
-    load(0);
+    load(0, a.prefix.n <= 32);      // what add_up has read last
   }
   __device__ bool next(PrefixWork* s) {
     while (u < u_end) {
@@ -168,7 +184,7 @@ struct PrefixCursor {
       s->unit0 = t.unit0;
       s->n = t.unit1 - t.unit0;
       s->kind = t.unit0 ? 1 : t.unit1 < units ? 2 : 0;
-      s->last_worker = s->kind == 2 ? tree_cta_of(tree_shares(total, n_workers), in_front + t.last) : worker;
+      s->last_worker = s->kind == 2 ? tree_cta_of(shares, in_front + t.last) : worker;
       s->limit = min(static_cast<long long>(len), static_cast<long long>(a.shape.capacity));
       u += t.places;
       if (s->n) return true;
@@ -569,7 +585,7 @@ struct PrefixCta {
     __syncwarp();
     if (lane == 0) mbar_arrive(bar_seg_empty + 8 * (i % kPlanned));
   }
-  template <typename T> __device__ __forceinline__ void feed(const Maps& maps);
+  template <typename T> __device__ __forceinline__ void feed(const Maps& maps, PrefixCursor& cursor);
   template <typename T> __device__ __forceinline__ void softmax();
   __device__ __forceinline__ void drain();
 };
@@ -577,13 +593,13 @@ struct PrefixCta {
 // Warps 8 to 10.
 template <int D>
 template <typename T>
-__device__ __forceinline__ void PrefixCta<D>::feed(const Maps& maps) {
+__device__ __forceinline__ void PrefixCta<D>::feed(const Maps& maps, PrefixCursor& cursor) {
   using Geo = Geometry<D>;
   constexpr bool kBf16 = !__is_same(T, __half);
   const PoolView& pool = a.pool;
   if (warp == 10) {
     // ---- the plan ----
-    PrefixCursor cursor(a, lane, blockIdx.x, n_workers, ctl->places);
+    cursor.begin(blockIdx.x, n_workers);
     PrefixWork s;
     for (uint32_t i = 0;; ++i) {
       const bool more = cursor.next(&s);
@@ -759,20 +775,10 @@ __device__ __forceinline__ void PrefixCta<D>::softmax() {
   // Queries of a segment into this group's tile, in the background.  Its products have read what was there before: the
   // caller has seen the last scores.
   auto load_queries = [&](const PrefixWork& g) {
-    constexpr int kPieces = D / 8;
     const int from = g.both() ? w * 128 : 0;
-    const long long r0 = g.first + g.row0 + from;
-    const long long t0 = r0 / group;
-    const int rem0 = static_cast<int>(r0 - t0 * group);
-#pragma unroll 4
-    for (int idx = r; idx < 128 * kPieces; idx += 128) {
-      const int row = idx / kPieces, piece = idx % kPieces;
-      const bool there = from + row < g.rows;
-      const int y = there ? rem0 + row : rem0, t = small_div(y, a.group_inverse);
-      copy16(smem_u32(s_q) + w * Geo::kQBytes + piece / 8 * Geo::kPanel + row * 128 + ((piece % 8) ^ (row & 7)) * 16,
-             static_cast<const T*>(a.q) + ((t0 + t) * n_q_heads + g.head * group + (y - t * group)) * D + piece * 8, there);
-    }
-    asm volatile("cp.async.commit_group;" ::: "memory");
+    const long long r0 = g.first + g.row0 + from, t0 = div_small(r0, group);
+    load_query_tile<T, D>(smem_u32(s_q) + w * Geo::kQBytes, Geo::kPanel, static_cast<const T*>(a.q) + (t0 * n_q_heads + g.head * group) * D, static_cast<int>(r0 - t0 * group),
+                          group, static_cast<int64_t>(n_q_heads) * D, g.rows - from, r);
   };
   auto queries_ready = [&]() {
     asm volatile("cp.async.wait_all;" ::: "memory");
@@ -1010,20 +1016,10 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   if (warp == 9) tmem_alloc(smem_u32(&ctl->tmem), 512);
   pdl_wait();
-  if (warp == 10) {      // places of all prefixes
-    long long n = 0;
-    for (int p = lane; p < a.prefix.n; p += 32) {
-      PrefixRange range;
-      const bool ok = prefix_range(a, p, &range);
-      n += prefix_places(a.shape, static_cast<long long>(range.rows) * a.group, prefix_units(a.shape, range.len)) * a.pool.n_kv_heads;
-      if (blockIdx.x == 0) {
-        if (!ok) raise(a.pool.status, kBadRows);
-        else if (range.rows && range.len > a.shape.capacity) raise(a.pool.status, kBadSlot);
-      }
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
-    if (lane == 0) ctl->places = n;
+  PrefixCursor cursor(a, lane);
+  if (warp == 10) {
+    cursor.add_up(blockIdx.x == 0);
+    if (lane == 0) ctl->places = cursor.total;
   }
   if (a.own_cost) add_up_own(a, own, &ctl->own_places);
   fence_async_smem();      // the ring's copies follow where the sums were
@@ -1041,7 +1037,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
       own_share<T, D>(&maps.k_few, &maps.v_few, a, smem, own, &ctl->give_up, 8 * (static_cast<int>(blockIdx.x) - n_prefix) + warp, 8 * (static_cast<int>(gridDim.x) - n_prefix), own_places);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegisters));
-    if (is_prefix) cta.template feed<T>(maps);
+    if (is_prefix) cta.template feed<T>(maps, cursor);
     if (warp == 11) write_places(a, blockIdx.x, gridDim.x);
   }
   tc_fence_before();
