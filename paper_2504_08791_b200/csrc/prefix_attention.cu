@@ -29,6 +29,7 @@ namespace prima {
 namespace {
 
 constexpr int kGroupThreads = 128, kPrefixThreads = 3 * kGroupThreads;
+constexpr int kBlock = 64;              // positions whose scores are one product
 constexpr int kPlanned = 4;            // segments ahead
 constexpr int kPrefixSegmentCost = 4;  // in places
 // Registers of a thread: the two groups that hold scores (or the fragments of the streaming body), and the third one.  Their
@@ -85,7 +86,7 @@ struct PrefixWork {
 };
 
 struct PrefixControl {
-  unsigned long long full[12], empty[12], s_ready[2], p_ready[4], pv_done[2], q_ready[2], q_first, drained;
+  unsigned long long full[12], empty[12], s_ready[4], p_ready[4], pv_done[4], q_ready[2], q_first, drained;
   unsigned long long seg_full[kPlanned], seg_empty[kPlanned];
   PrefixWork seg[kPlanned];
   long long places, own_places;
@@ -590,7 +591,7 @@ struct PrefixCta {
   __device__ __forceinline__ void drain();
 };
 
-// Warps 8 to 10.
+// Warps 8 to 11.
 template <int D>
 template <typename T>
 __device__ __forceinline__ void PrefixCta<D>::feed(const Maps& maps, PrefixCursor& cursor) {
@@ -669,94 +670,81 @@ __device__ __forceinline__ void PrefixCta<D>::feed(const Maps& maps, PrefixCurso
         ++n_read;
       }
     }
-  } else if (warp == 9) {
-    // ---- products ----
-    // Whichever group's operands are there goes next: scores of its next unit behind the product with the probabilities of
-    // the one before (they lie in the same columns, and one warp's products run in order).
-    constexpr uint32_t kDescS = mma_f16_desc(kBf16, false, 128, kTilePos), kDescO = mma_f16_desc(kBf16, true, 128, D);
-    const uint32_t u_tmem = uniform(tmem);
-    const uint32_t ring_addr = uniform(smem_u32(s_ring)), q_addr = uniform(smem_u32(s_q));
-    const SmemOperand k_all = smem_operand(ring_addr, 16), v_all = smem_operand(ring_addr, Geo::kPanel);
-    uint32_t turns[2] = {0, 0};      // probabilities of an accumulator so far
-    bool ok = true;
-    const PrefixWork* seg;
-    for (uint32_t si = 0; (seg = segment(si)); ++si) {
-      const bool both = uniform(seg->rows) > kPrefixRows / 2;
-      const int n = uniform(seg->n);
-      done_with(si);
-      ok = wait_for(bar_q, si & 1, give_up, status) && ok;
-      ok = wait_for(bar_q + 8, si & 1, give_up, status) && ok;
-      ok = __all_sync(0xffffffffu, ok);
-      // Of a group: units, scores and outputs issued, halves of the probabilities taken; the place of its next unit's keys, and
-      // of the unit's values whose probabilities come next.  Where only one group takes a unit it gives its places back twice.
-      int count[2], scored[2] = {0, 0}, summed[2] = {0, 0}, idle = 0;
-      uint32_t half[2] = {0, 0};
-      RingPlace<kSlots> pk[2] = {ring, ring}, pv[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        count[h] = both ? n : (n + 1 - h) >> 1;
-        if (!both && h) pk[h].step(2);
-        pv[h] = pk[h];
-        pv[h].step(1);
-      }
-      auto give_back = [&](uint32_t slot) {
-        tc_commit(bar_empty + 8 * slot);
-        if (!both) tc_commit(bar_empty + 8 * slot);
-      };
-      while (ok && (summed[0] < count[0] || summed[1] < count[1])) {
-        bool any = false;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (scored[h] > summed[h]) {      // O += P V, a half of the positions
-            const bool ready = mbar_peek(bar_p + 16 * h + 8 * half[h], turns[h] & 1) && (half[h] || mbar_peek(bar_full + 8 * pv[h].slot, pv[h].phase));
-            if (__all_sync(0xffffffffu, ready)) {
-              any = true;
-              tc_fence_after();
-              const SmemOperand vv = v_all + pv[h].slot * Geo::kSlotBytes;
-              const bool last = half[h];
-              if (elect_one()) {
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                  mma_ts(u_tmem + 256 + h * D, u_tmem + h * kTilePos + 32 * half[h] + 8 * k, vv + (4 * half[h] + k) * (16 * 128), kDescO, summed[h] > 0 || last || k > 0);
-                if (last) {
-                  if (summed[h] + 1 == count[h]) tc_commit(bar_pv + 8 * h);
-                  give_back(pv[h].slot);
-                }
-              }
-              __syncwarp();
-              half[h] ^= 1;
-              if (last) {
-                ++turns[h];
-                ++summed[h];
-                pv[h].step(both ? 2 : 4);
-              }
-            }
-          }
-          if (scored[h] == summed[h] && scored[h] < count[h] && __all_sync(0xffffffffu, mbar_peek(bar_full + 8 * pk[h].slot, pk[h].phase))) {      // S = Q K^T
-            any = true;
-            tc_fence_after();
-            if (elect_one()) {
-              const SmemOperand qq = smem_operand(q_addr + h * Geo::kQBytes, 16), kk = k_all + pk[h].slot * Geo::kSlotBytes;
-#pragma unroll
-              for (int k = 0; k < D / 16; ++k) mma_ss(u_tmem + h * kTilePos, qq + (k / 4 * Geo::kPanel + k % 4 * 32), kk + (k / 4 * Geo::kPanel + k % 4 * 32), kDescS, k > 0);
-              tc_commit(bar_s + 8 * h);
-              give_back(pk[h].slot);
-            }
-            __syncwarp();
-            ++scored[h];
-            pk[h].step(both ? 2 : 4);
-          }
-        }
-        idle = any ? 0 : idle + 1;
-        if (idle == 1 << 22 || (idle % 1024 == 1023 && *static_cast<volatile int*>(give_up))) {
-          *static_cast<volatile int*>(give_up) = 1;
+  } else if (warp == 9 || warp == 11) {
+    // ---- products of a group ----
+    // Blocks of 64 positions, two per unit, with a buffer of scores each: the scores of the group's next block are computed
+    // while it has the exponentials of this one.  They follow the product with the probabilities of the block before last,
+    // which lay in the same columns (one thread's products run in order).  A thread for each group: waiting for barriers,
+    // issuing and committing takes it longer than the tensor core takes for its products (830 and 640 cycles a block).
+    constexpr uint32_t kDescS = mma_f16_desc(kBf16, false, 128, kBlock), kDescO = mma_f16_desc(kBf16, true, 128, D);
+    const uint32_t h = warp == 11, ring_addr = uniform(smem_u32(s_ring));
+    const uint32_t t_s = uniform(tmem + h * kTilePos), t_o = uniform(tmem + 256 + h * D);
+    const SmemOperand qq = smem_operand(uniform(smem_u32(s_q) + h * Geo::kQBytes), 16), k_all = smem_operand(ring_addr, 16), v_all = smem_operand(ring_addr, Geo::kPanel);
+    const uint32_t my_s = bar_s + 16 * h, my_p = bar_p + 16 * h, my_pv = bar_pv + 16 * h;
+    if (elect_one()) {
+      uint32_t turn = 0;      // blocks so far
+      bool ok = true;
+      auto wait = [&](uint32_t bar, uint32_t parity) { ok = wait_for(bar, parity, give_up, status) && ok; };
+      for (uint32_t si = 0;; ++si) {
+        const uint32_t at = si % kPlanned;
+        if (!wait_segment(bar_seg + 8 * at, si / kPlanned & 1)) {
           raise(status, kGaveUp);
-          ok = false;
+          break;
         }
+        const bool both = ctl->seg[at].both();
+        const int n = ctl->seg[at].n, count = 2 * (both ? n : (n + 1 - static_cast<int>(h)) >> 1);
+        if (n == 0) break;
+        mbar_arrive(bar_seg_empty + 8 * at);
+        wait(bar_q + 8 * h, si & 1);
+        // The places of the next scores' keys and of the next product's values.  Where only one group takes a unit it gives its
+        // places back twice.
+        RingPlace<kSlots> pk = ring, pv;
+        if (!both && h) pk.step(2);
+        pv = pk;
+        pv.step(1);
+        auto give_back = [&](uint32_t slot) {
+          tc_commit(bar_empty + 8 * slot);
+          if (!both) tc_commit(bar_empty + 8 * slot);
+        };
+        auto scores = [&](uint32_t half) {      // S = Q K^T
+          if (!half) wait(bar_full + 8 * pk.slot, pk.phase);
+          if (ok) {
+            tc_fence_after();
+            const SmemOperand kk = k_all + (pk.slot * Geo::kSlotBytes + half * (kBlock * 128));
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) mma_ss(t_s + kBlock * half, qq + (k / 4 * Geo::kPanel + k % 4 * 32), kk + (k / 4 * Geo::kPanel + k % 4 * 32), kDescS, k > 0);
+            tc_commit(my_s + 8 * half);
+            if (half) give_back(pk.slot);
+          }
+          if (half) pk.step(both ? 2 : 4);
+        };
+        auto outputs = [&](uint32_t half, bool add) {      // O += P V
+          if (!half) wait(bar_full + 8 * pv.slot, pv.phase);
+          wait(my_p + 8 * half, turn++ >> 1 & 1);
+          if (ok) {
+            tc_fence_after();
+            const SmemOperand vv = v_all + (pv.slot * Geo::kSlotBytes + half * (kBlock * 128));
+#pragma unroll
+            for (int k = 0; k < kBlock / 16; ++k) mma_ts(t_o, t_s + kBlock * half + 8 * k, vv + k * (16 * 128), kDescO, add || k > 0);
+            tc_commit(my_pv + 8 * half);
+            if (half) give_back(pv.slot);
+          }
+          if (half) pv.step(both ? 2 : 4);
+        };
+        if (count) {
+          scores(0);
+          scores(1);
+        }
+        for (int j = 0; j < count; j += 2) {
+          outputs(0, j > 0);
+          if (j + 2 < count) scores(0);
+          outputs(1, true);
+          if (j + 2 < count) scores(1);
+        }
+        ring.skip(2 * n);
       }
-      ok = __all_sync(0xffffffffu, ok);
-      ring.skip(2 * n);
     }
+    __syncwarp();
   }
 }
 
@@ -769,7 +757,7 @@ __device__ __forceinline__ void PrefixCta<D>::softmax() {
   const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
   const uint32_t t_s = tmem + lanes + kTilePos * w, t_o = tmem + lanes + 256;
   const int group = a.group, n_q_heads = a.n_q_heads;
-  uint32_t n_sub = 0, n_seg = 0, unit_base = 0;      // sub-units of this accumulator, segments that had some, units before
+  uint32_t n_block = 0, unit_base = 0;      // blocks of this accumulator, units before
   bool loaded = false;                               // the queries of the segment are on their way already
 
   // Queries of a segment into this group's tile, in the background.  Its products have read what was there before: the
@@ -811,44 +799,47 @@ __device__ __forceinline__ void PrefixCta<D>::softmax() {
     // (without a unit the next queries wait for the other group's end: the barrier of the queries may be one phase ahead of
     // the warp that issues the products, not two)
 #pragma unroll 1
-    for (int i = 0; i < count; ++i, ++n_sub) {
-      const int t = both ? i : 2 * i + w;
-      wait_for(bar_s + 8 * w, n_sub & 1, give_up, status);
+    for (int i = 0; i < 2 * count; ++i, ++n_block) {
+      const int t = both ? i >> 1 : (i & ~1) + w, half = i & 1;
+      wait_for(bar_s + 16 * w + 8 * half, n_block >> 1 & 1, give_up, status);
       tc_fence_after();
-      if (i == count - 1) load_next();
+      if (i == 2 * count - 1) load_next();
       const bool edge = *static_cast<volatile int*>(&ctl->edge[(unit_base + t) % 16]) != 0;
-      const volatile uint32_t* seen = ctl->seen[(unit_base + t) % 16];
+      const volatile uint32_t* seen = ctl->seen[(unit_base + t) % 16] + 2 * half;
       if (edge) {
         // Values at positions that are not seen may be anything, and 0 x NaN is NaN: clear them (each group for its own
         // product, which may come first).
         RingPlace<kSlots> pv = ring;
         pv.skip(2 * t + 1);
         wait_for(bar_full + 8 * pv.slot, pv.phase, give_up, status);
-        if (!(seen[quarter] >> lane & 1)) {
-          uint8_t* row = s_ring + pv.slot * Geo::kSlotBytes + r * 128;
+        if (!(seen[quarter & 1] >> lane & 1)) {
+          uint8_t* row = s_ring + pv.slot * Geo::kSlotBytes + (kBlock * half + (r & 63)) * 128;
+          constexpr int kHalfRow = D / 16;      // 16-byte pieces
 #pragma unroll
-          for (int c = 0; c < D / 8; ++c) *reinterpret_cast<uint4*>(row + c / 8 * Geo::kPanel + c % 8 * 16) = make_uint4(0, 0, 0, 0);
+          for (int c = 0; c < kHalfRow; ++c) {
+            const int piece = (r >> 6) * kHalfRow + c;
+            *reinterpret_cast<uint4*>(row + piece / 8 * Geo::kPanel + piece % 8 * 16) = make_uint4(0, 0, 0, 0);
+          }
         }
         fence_async_smem();
       }
-      uint32_t sc[4][32];
-      float2 scale, shift;
       if (live) {
+        uint32_t sc[2][32];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) tmem_load(sc[c], t_s + 32 * c);
+        for (int c = 0; c < 2; ++c) tmem_load(sc[c], t_s + kBlock * half + 32 * c);
         tmem_wait_load();
 #pragma unroll
-        for (int c = 0; c < 4; ++c) tmem_use(sc[c]);
+        for (int c = 0; c < 2; ++c) tmem_use(sc[c]);
         if (edge) {
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
+          for (int c = 0; c < 2; ++c) {
             const uint32_t word = seen[c];
 #pragma unroll
             for (int j = 0; j < 32; ++j)
               if (!(word >> j & 1)) sc[c][j] = 0xff800000u;
           }
         }
-        const float top = fmaxf(max_of(sc[1], max_of(sc[0], -INFINITY)), max_of(sc[3], max_of(sc[2], -INFINITY))) * a.scale_log2;
+        const float top = max_of(sc[1], max_of(sc[0], -INFINITY)) * a.scale_log2;
         if (__any_sync(0xffffffffu, top > m + kSlack)) {
           const float m_new = top > m + kSlack ? top - kHeadroom : m;
           const float f = m == m_new ? 1.f : ex2(m - m_new);
@@ -856,6 +847,9 @@ __device__ __forceinline__ void PrefixCta<D>::softmax() {
           sum.x *= f;
           sum.y *= f;
           if (i > 0) {
+            // behind the last product into this accumulator (the one before it is done: these scores came behind it)
+            wait_for(bar_pv + 16 * w + 8 * (half ^ 1), (n_block - 1) >> 1 & 1, give_up, status);
+            tc_fence_after();
 #pragma unroll 1
             for (int k = 0; k < D / 16; ++k) {
               uint32_t y[16];
@@ -870,39 +864,30 @@ __device__ __forceinline__ void PrefixCta<D>::softmax() {
             tmem_wait_store();
           }
         }
-        scale = make_float2(a.scale_log2, a.scale_log2);
-        shift = m == -INFINITY ? make_float2(0.f, 0.f) : make_float2(-m, -m);
+        const float2 scale = make_float2(a.scale_log2, a.scale_log2), shift = m == -INFINITY ? make_float2(0.f, 0.f) : make_float2(-m, -m);
+        uint32_t packed[32];
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            float2 p = fma2(make_float2(__uint_as_float(sc[c][2 * j]), __uint_as_float(sc[c][2 * j + 1])), scale, shift);
+            p = make_float2(ex2(p.x), ex2(p.y));
+            sum = add2(sum, p);
+            packed[16 * c + j] = Half2Of<T>::pack(p.x, p.y);
+          }
+        tmem_store(t_s + kBlock * half, packed);
+        tmem_wait_store();
       }
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        if (live) {
-          uint32_t packed[32];
-#pragma unroll
-          for (int c = 0; c < 2; ++c)
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              float2 p = fma2(make_float2(__uint_as_float(sc[2 * half + c][2 * j]), __uint_as_float(sc[2 * half + c][2 * j + 1])), scale, shift);
-              p = make_float2(ex2(p.x), ex2(p.y));
-              sum = add2(sum, p);
-              packed[16 * c + j] = Half2Of<T>::pack(p.x, p.y);
-            }
-          tmem_store(t_s + 32 * half, packed);
-          tmem_wait_store();
-        }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar_p + 16 * w + 8 * half);
-      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_p + 16 * w + 8 * half);
     }
     // ---- the segment's part ----
     if (next_loads) queries_ready();
     loaded = next_loads;
     unit_base += s.n;
     ring.skip(2 * s.n);
-    if (count > 0) {
-      wait_for(bar_pv + 8 * w, n_seg & 1, give_up, status);
-      ++n_seg;
-    }
+    if (count > 0) wait_for(bar_pv + 16 * w + 8, (n_block / 2 - 1) & 1, give_up, status);      // the last product
     tc_fence_after();
     const int64_t head = s.head, at = s.first + s.row0 + in_tile;
     const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) + (s.kind == 2);
@@ -960,7 +945,7 @@ __device__ __forceinline__ void PrefixCta<D>::softmax() {
 template <int D>
 __device__ __forceinline__ void PrefixCta<D>::drain() {
   if (!ctl->give_up) return;
-  if (tid == 9 * 32) {
+  if ((warp == 9 || warp == 11) && elect_one()) {
     tc_commit(smem_u32(&ctl->drained));
     for (int i = 0; i < (1 << 22) && !mbar_test(smem_u32(&ctl->drained), 0); ++i) {}
   }
@@ -994,18 +979,20 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
       mbar_init(smem_u32(&ctl->empty[i]), 2);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(smem_u32(&ctl->s_ready[i]), 1);
+      mbar_init(smem_u32(&ctl->s_ready[2 * i]), 1);
+      mbar_init(smem_u32(&ctl->s_ready[2 * i + 1]), 1);
       mbar_init(smem_u32(&ctl->p_ready[2 * i]), 4);
       mbar_init(smem_u32(&ctl->p_ready[2 * i + 1]), 4);
-      mbar_init(smem_u32(&ctl->pv_done[i]), 1);
+      mbar_init(smem_u32(&ctl->pv_done[2 * i]), 1);
+      mbar_init(smem_u32(&ctl->pv_done[2 * i + 1]), 1);
       mbar_init(smem_u32(&ctl->q_ready[i]), 4);
     }
     for (int i = 0; i < kPlanned; ++i) {
       mbar_init(smem_u32(&ctl->seg_full[i]), 1);
-      mbar_init(smem_u32(&ctl->seg_empty[i]), 10);
+      mbar_init(smem_u32(&ctl->seg_empty[i]), 11);
     }
     mbar_init(smem_u32(&ctl->q_first), 8);
-    mbar_init(smem_u32(&ctl->drained), 1);
+    mbar_init(smem_u32(&ctl->drained), 2);
     ctl->give_up = 0;
     ctl->own_places = 0;
     tma_prefetch_map(&maps.k);
@@ -1038,7 +1025,7 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegisters));
     if (is_prefix) cta.template feed<T>(maps, cursor);
-    if (warp == 11) write_places(a, blockIdx.x, gridDim.x);
+    if (warp == 10) write_places(a, blockIdx.x, gridDim.x);
   }
   tc_fence_before();
   __syncthreads();
