@@ -420,8 +420,8 @@ class RopeAxes:
         if len(axis) not in (32, 64) or len(rank) != len(axis) or not all(-1 <= a < MAX_AXES for a in axis) or not all(0 <= r < len(axis) for r in rank):
             raise ValueError(f"one axis (-1 .. {MAX_AXES - 1}) and one frequency for each of the 32 or 64 pairs of a head")
         self.pairs, self.n_axes = len(axis), max(0, *axis) + 1
-        self.axis = (C.c_uint8 * 64)(*(AXIS_NONE if a < 0 else a for a in axis))
-        self.rank = (C.c_uint8 * 64)(*rank)
+        # what a call copies and completes
+        self.desc = HeadNormDesc(n_axes=self.n_axes, axis=(C.c_uint8 * 64)(*(AXIS_NONE if a < 0 else a for a in axis)), rank=(C.c_uint8 * 64)(*rank))
 
 
 class PrefixBatch:
@@ -514,20 +514,24 @@ class PagedCache:
             if q_out is None:
                 raise ValueError("q_out: expected a tensor")
             qo = _need(q_out, "q_out", self.dtype, (n, heads, self.head_dim), self.device)
-        d = HeadNormDesc(eps=eps)
-        if q_gain is not None:
-            d.q_gain = _need(q_gain, "q_gain", self._f32, (self.head_dim,) if q_gain.dim() == 1 else (heads, self.head_dim), self.device)
-            d.q_gain_stride = 0 if q_gain.dim() == 1 else self.head_dim
-        if k_gain is not None:
-            d.k_gain = _need(k_gain, "k_gain", self._f32, (self.head_dim,) if k_gain.dim() == 1 else (self.n_kv_heads, self.head_dim), self.device)
-            d.k_gain_stride = 0 if k_gain.dim() == 1 else self.head_dim
         if axes is None:
             axes = self._one_axis
             if axes is None:
                 axes = self._one_axis = RopeAxes([0] * (self.head_dim // 2))
         if axes.pairs != self.head_dim // 2:
             raise ValueError("axes: expected as many pairs as a head has")
-        d.n_axes, d.axis, d.rank = axes.n_axes, axes.axis, axes.rank
+        d = HeadNormDesc.from_buffer_copy(axes.desc)
+        d.eps = eps
+        if q_gain is not None:
+            each = q_gain.dim() != 1
+            d.q_gain = _need(q_gain, "q_gain", self._f32, (heads, self.head_dim) if each else (self.head_dim,), self.device)
+            if each:
+                d.q_gain_stride = self.head_dim
+        if k_gain is not None:
+            each = k_gain.dim() != 1
+            d.k_gain = _need(k_gain, "k_gain", self._f32, (self.n_kv_heads, self.head_dim) if each else (self.head_dim,), self.device)
+            if each:
+                d.k_gain_stride = self.head_dim
         if positions is not None:
             if positions.dim() != 2 or not axes.n_axes <= positions.shape[0] <= MAX_AXES:
                 raise ValueError(f"positions: expected [axes, n_tok] with {axes.n_axes} .. {MAX_AXES} axes")

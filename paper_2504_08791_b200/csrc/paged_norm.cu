@@ -151,8 +151,9 @@ __global__ void __launch_bounds__(256) norm_kernel(PoolView pool, BatchView b, i
     if constexpr (kMode == 0) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        u[i] = fma2(hi[i], make_float2(-sn[i].x, -sn[i].y), mul2(lo[i], cs[i]));
-        w[i] = fma2(hi[i], cs[i], mul2(lo[i], sn[i]));
+        // in the order of append_kernel: without gains the bits are the same
+        u[i] = fma2(lo[i], cs[i], mul2(hi[i], make_float2(-sn[i].x, -sn[i].y)));
+        w[i] = fma2(lo[i], sn[i], mul2(hi[i], cs[i]));
       }
     } else {
 #pragma unroll

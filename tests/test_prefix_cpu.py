@@ -33,7 +33,7 @@ def test_axes_and_prefixes_are_checked():
     import torch
     i32 = torch.int32
     axes = binding.RopeAxes([0] * 8 + [2] * 8 + [-1] * 16)
-    assert axes.n_axes == 3 and axes.pairs == 32 and axes.axis[16] == binding.AXIS_NONE and axes.rank[31] == 31
+    assert axes.n_axes == 3 and axes.pairs == 32 and axes.desc.axis[16] == binding.AXIS_NONE and axes.desc.rank[31] == 31
     assert binding.RopeAxes([-1] * 64).n_axes == 1
     for axis, rank in (([0] * 33, None), ([0] * 32, [0] * 31), ([0] * 32, [0] * 31 + [32]), ([4] * 32, None), ([-2] * 32, None)):
         with pytest.raises(ValueError):
