@@ -448,10 +448,11 @@ int prima_tree_attention(prima_paged* pool, int layer, const prima_paged_batch* 
  * prima_tree_attention, with the positions of a prefix, all of which every row of its sequences sees, in front of the
  * sequence's own.  A prefix lies once in the cache, on pages of its own table, and is read once for all rows that share it
  * (once per 256 of a KV head's rows).  Slots and ctx_len of a sequence count its own positions alone; where the rotation is
- * to go on behind the prefix, the append needs `pos`.  out, lse, q, scale, masks, types and refusals as there; n_q_heads at
- * most 64 * n_kv_heads.  A prefix with a negative length or a bad range of sequences counts as none (and raises a status
- * bit), positions behind its table are not seen.  The value of a position that is seen must be finite.
- * workspace as there, for the same (n_seq, n_tok, n_q_heads). */
+ * to go on behind the prefix, the append needs `pos`.  out, lse, q, scale, masks, types and refusals as there; n_tok *
+ * n_q_heads below 2^31.  A prefix with a negative length or a bad range of sequences or rows counts as none (and raises a
+ * status bit), positions behind its table are not seen.  The value of a position that is seen must be finite.
+ * workspace as there, of the bytes that prima_prefix_attention_workspace names (room for the prefix's and the own part of
+ * every row's output in 32 bits, among others). */
 typedef struct {
   int32_t n_prefix;            /* >= 1                                                                */
   const int32_t* seq_begin;    /* dev [n_prefix + 1], ascending in 0..n_seq: sequences seq_begin[p] .. seq_begin[p+1]-1 share

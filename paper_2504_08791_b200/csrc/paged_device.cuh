@@ -156,13 +156,13 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
 
-// A tile of up to 128 rows of queries into shared memory in the background, by kThreads threads (r: this one): rows of 128 bytes
-// in the 128-byte swizzle, 64 columns a panel; rows behind the last one are zeros.  Row x is query head (in0 + x) % group of a KV
+// A tile of up to 128 rows of queries into shared memory in the background, by 128 threads (r: this one): rows of 128 bytes in
+// the 128-byte swizzle, 64 columns a panel; rows behind the last one are zeros.  Row x is query head (in0 + x) % group of a KV
 // head, (in0 + x) / group tokens behind the one that `from` (that token's first query head of the KV head) belongs to.  A
-// thread takes one 16-byte piece of every kThreads / (D / 8)-th row and steps its place without divisions.
-template <typename T, int D, int kThreads = 128>
+// thread takes one 16-byte piece of every 128 / (D / 8)-th row and steps its place without divisions.
+template <typename T, int D>
 __device__ __forceinline__ void load_query_tile(uint32_t tile, int panel_bytes, const T* from, int in0, int group, int64_t token_stride, int rows, int r) {
-  constexpr int kPieces = D / 8, kStep = kThreads / kPieces;
+  constexpr int kPieces = D / 8, kStep = 128 / kPieces;
   const int piece = r % kPieces, row0 = r / kPieces, tokens = kStep / group, heads = kStep - tokens * group;
   int token = (in0 + row0) / group, in_group = in0 + row0 - token * group;
   const uint32_t dst = tile + piece / 8 * panel_bytes;

@@ -16,8 +16,8 @@ constexpr int kThreads = 512, kWarps = kThreads / 32, kPer = 4, kTile = kThreads
 constexpr int kBins = 2048;                           // of a digit: 11, 11 and 10 bits
 constexpr int kListed = 2048;                         // keys with the border's first digit that are set apart
 constexpr int kFlight = 8;                            // loads of a thread in flight
-// Keys that a CTA keeps in shared memory; those behind are made from the arrays again in every pass.
-constexpr int kCached = 24576;
+// Keys that a CTA keeps in shared memory; those behind are made from the arrays again in every pass.  Two CTAs share an SM.
+constexpr int kCached = 16384;
 
 struct EvictArgs {
   PoolView pool;

@@ -190,10 +190,9 @@ cudaError_t launch_norm(const prima_paged& pool, const BatchView& b, int layer, 
   const int64_t per16 = 16 / static_cast<int64_t>(sizeof(In));
   const bool wide = (!q || (aligned_to(q, 16) && qs % per16 == 0)) && aligned_to(k, 16) && aligned_to(v, 16) && ks % per16 == 0 && vs % per16 == 0;
   // Few rows: a CTA's eight warps share one, for the shortest path; many: a warp each, which looks up least.
-  constexpr int kMany = 1;
   const bool few = b.n_tok <= 16 * pool.sm_count;
-  auto kernel = pool.cfg.rope_mode == 0 ? (few ? norm_kernel<T, In, D, 8, 0> : norm_kernel<T, In, D, kMany, 0>) : (few ? norm_kernel<T, In, D, 8, 1> : norm_kernel<T, In, D, kMany, 1>);
-  return launch_pdl(kernel, dim3(few ? b.n_tok : static_cast<unsigned>((static_cast<int64_t>(b.n_tok) * kMany + 7) / 8)), dim3(256), 0, st, view_of(pool), b, layer, static_cast<const In*>(q), static_cast<const In*>(k),
+  auto kernel = pool.cfg.rope_mode == 0 ? (few ? norm_kernel<T, In, D, 8, 0> : norm_kernel<T, In, D, 1, 0>) : (few ? norm_kernel<T, In, D, 8, 1> : norm_kernel<T, In, D, 1, 1>);
+  return launch_pdl(kernel, dim3(few ? b.n_tok : static_cast<unsigned>((static_cast<int64_t>(b.n_tok) + 7) / 8)), dim3(256), 0, st, view_of(pool), b, layer, static_cast<const In*>(q), static_cast<const In*>(k),
                     static_cast<const In*>(v), n_q_heads, qs, ks, vs, wide, static_cast<const double*>(pool.freq), static_cast<T*>(q_out), norm);
 }
 

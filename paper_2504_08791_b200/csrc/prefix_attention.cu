@@ -28,7 +28,7 @@
 namespace prima {
 namespace {
 
-constexpr int kGroupThreads = 128, kPrefixThreads = 3 * kGroupThreads;
+constexpr int kPrefixThreads = 384;
 constexpr int kBlock = 64;              // positions whose scores are one product
 constexpr int kPlanned = 4;            // segments ahead
 constexpr int kPrefixSegmentCost = 4;  // in places
@@ -1151,6 +1151,7 @@ extern "C" {
 int64_t prima_prefix_attention_workspace(const prima_paged* p, int n_seq, int n_tok, int n_q_heads) {
   if (!p || n_seq < 1 || n_tok < 1 || n_q_heads < 1) return PRIMA_ERR_ARG;
   const int64_t rows = static_cast<int64_t>(n_tok) * n_q_heads, dim = p->cfg.head_dim, sm = p->sm_count;
+  if (rows > 2147483647) return PRIMA_ERR_ARG;
   const int64_t whole = 2 * (padded(rows * dim * 4) + padded(rows * 8) + padded(rows * 8));
   const int64_t parts = padded(2 * sm * kPrefixRows * dim * 4) + padded(2 * sm * kPrefixRows * 8), own = padded(16 * sm * kFewRows * dim * 4) + padded(16 * sm * kFewRows * 8);
   return padded(static_cast<int64_t>(n_tok) * 16) + whole + parts + std::max(own, prima_tree_attention_workspace(p, n_seq, n_tok, n_q_heads));
@@ -1172,6 +1173,7 @@ int prima_prefix_attention(prima_paged* p, int layer, const prima_paged_batch* b
   if (!aligned_to(prefix->seq_begin, 4) || !aligned_to(prefix->len, 4) || !aligned_to(prefix->table, 4)) return refuse("an array of the prefix is not 4-byte aligned");
   if (!q || !out) return refuse("null q or out");
   if (n_q_heads < 1 || n_q_heads % c.n_kv_heads || n_q_heads / c.n_kv_heads > 64) return refuse("n_q_heads must be a multiple of n_kv_heads, at most 64 times it");
+  if (static_cast<int64_t>(batch->n_tok) * n_q_heads > 2147483647) return refuse("n_tok * n_q_heads reaches 2^31");
   if (!(scale > 0.f) || std::isinf(scale)) return refuse("scale must be positive and finite");
   if (out_dtype != PRIMA_DT_F32 && out_dtype != c.dtype) return refuse("out_dtype is neither fp32 nor the cache's type");
   if (!aligned_to(q, 16) || !aligned_to(out, 16)) return refuse("q and out must be 16-byte aligned");

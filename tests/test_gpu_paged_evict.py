@@ -60,14 +60,16 @@ def test_how_many_stay(gpu, keep):
     check(gpu, Batch(801, ctx=[300], nodes=[0], page=16, kv_heads=2, dim=64), keep)
 
 
-@pytest.mark.parametrize("n", [511, 512, 513, 2047, 2048, 2049, 10000, 10001, 13000])
+@pytest.mark.parametrize("n", [511, 512, 513, 2047, 2048, 2049, 10000, 10001, 13000, 16384, 16385, 20000])
 def test_lengths_around_the_tiles(gpu, n):
-    """Up to 10,000 keys stay in shared memory; the others are made again."""
+    """Up to 16,384 keys stay in shared memory; the others are made again."""
     check(gpu, Batch(802, ctx=[n], nodes=[0], page=32, kv_heads=1, dim=64), n // 3, recent_from=n - 50)
 
 
-def test_equal_weights_stay_by_slot(gpu):
-    b = Batch(803, ctx=[5000, 90], nodes=[0, 0], page=16, kv_heads=2, dim=64)
+@pytest.mark.parametrize("n", [5000, 17000])
+def test_equal_weights_stay_by_slot(gpu, n):
+    """Among them more keys with the border's first digit than are set apart (2048)."""
+    b = Batch(803, ctx=[n, 90], nodes=[0, 0], page=16, kv_heads=2, dim=64)
     w, born = arrays(b)
     for values in ([1.0], [0.0, -0.0], [3.0, 2.0, 2.0, 2.0, 1.0]):
         w[:] = np.random.RandomState(3).choice(np.array(values, np.float32), w.shape)
