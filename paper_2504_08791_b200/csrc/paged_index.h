@@ -178,7 +178,7 @@ PRIMA_HD PrefixSegment prefix_segment(const PrefixShape& t, int64_t rows, int64_
 }
 
 // The sequences' own positions: steps of kFewPos of one KV head for a tile of kFewRows rows, kOwnOverhead places in front of
-// each (sequence, KV head, tile).
+// each (sequence, KV head, tile); 64 rows over 8192 positions: 67 us without them, 56 with two.
 constexpr int kFewPos = 16, kFewRows = 16, kOwnOverhead = 2;
 
 PRIMA_HD int64_t own_steps(int64_t limit) { return (limit + kFewPos - 1) / kFewPos; }

@@ -1,4 +1,12 @@
 // The attention weight that cached positions receive in a step.
+//
+//   w[s][g][j] = decay * w_in[s][g][j] + sum over rows t of s and query heads h of g that see j of exp(scale q_th . k_jg - lse_th)
+//
+// With the log-sum-exp of the attention the probabilities need no pass of their own: one product, one exponential a pair, one
+// sum.  Few rows are bound by the keys (48 single tokens over up to 8192 positions, heads of 128: 26.5 us, floor 18.2 at the
+// copy bandwidth), many by the exponentials, which the special-function units take at 16 a cycle and SM (64 rows of 32 heads
+// over 32,704 positions: 60 us, 31 of them exponentials at the least, 20.5 products).  Polynomials on the ordinary units for a
+// part of the exponentials gave 63 for 65 at that point and are not used.
 #include <algorithm>
 #include <cmath>
 #include <cstdio>
@@ -24,7 +32,7 @@ struct WeightsArgs {
 // ---- the work ---------------------------------------------------------------------------------------------------------
 // Positions are independent of one another, so nothing is joined: the blocks of kBlock positions of all (sequence, KV head)
 // form one line, and every worker takes an equal stretch of it.  What the first block of a (sequence, KV head) costs besides
-// counts as kOverhead places in front of it.
+// counts as kOverhead places in front of it (48 single tokens over up to 8192 positions: 37 us without, 26.5 with 2).
 constexpr int kStreamOverhead = 2, kBlockOverhead = 1;
 struct WeightsWork {
   int seq, first, nodes, ctx, head;
@@ -148,9 +156,9 @@ struct StreamControl {
   WeightsWork fifo[8][8];              // stretches between a warp's copies (at most five steps ahead) and its products
   int give_up;
 };
-constexpr int stream_ctas(int dim, int tiles) { return dim == 128 && tiles == 4 ? 1 : 2; }      // per SM: what the registers allow
+constexpr int kStreamCtas = 2;         // per SM: what the registers allow
 template <typename T, int D, int kTiles>
-__global__ void __launch_bounds__(256, stream_ctas(D, kTiles)) weights_stream_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ WeightsArgs a) {
+__global__ void __launch_bounds__(256, kStreamCtas) weights_stream_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ WeightsArgs a) {
   using Geo = StreamGeometry<D>;
   constexpr bool kBf16 = !__is_same(T, __half);
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -642,7 +650,7 @@ cudaError_t launch_stream(const prima_paged& pool, const WeightsArgs& a, cudaStr
   auto kernel = weights_stream_kernel<T, D, kTiles>;
   const cudaError_t e = allow_smem(kernel, kSmem, done);
   if (e != cudaSuccess) return e;
-  return launch_pdl(kernel, dim3(stream_ctas(D, kTiles) * pool.sm_count), dim3(256), kSmem, st, static_cast<const Maps*>(pool.maps)->k_few, a);
+  return launch_pdl(kernel, dim3(kStreamCtas * pool.sm_count), dim3(256), kSmem, st, static_cast<const Maps*>(pool.maps)->k_few, a);
 }
 template <typename T, int D>
 cudaError_t launch_block(const prima_paged& pool, const WeightsArgs& a, cudaStream_t st) {
@@ -656,10 +664,16 @@ cudaError_t launch_block(const prima_paged& pool, const WeightsArgs& a, cudaStre
 }
 template <typename T, int D>
 cudaError_t launch_weights(const prima_paged& pool, const WeightsArgs& a, cudaStream_t st) {
-  // Rows that a KV head has of a sequence on average; each variant is right for any.
+  // Rows that a KV head has of a sequence on average; each variant is right for any.  Streaming against tensor memory, 8 KV
+  // heads, B200: of 128, 16 sequences of 4096 positions, 8 rows 27 and 41 us, 16 rows 29 and 41, 24 rows 52 and 41; 64 of 600,
+  // 16 rows 19 and 33, 24 rows 34 and 34; one of 8192, 16 rows 9.3 and 10.2, 24 rows 12.9 and 10.2 (32 rows of 128 elements
+  // leave registers for one CTA per SM).  Of 64, 16 sequences of 4096, 32 rows 31 and 35, 40 rows 96 and 35; 64 of 600, 22 and
+  // 31, then 66 and 31.
   const int64_t rows = (static_cast<int64_t>(a.b.n_tok) + a.b.n_seq - 1) / a.b.n_seq * a.group;
-  if (rows > 32) return launch_block<T, D>(pool, a, st);
-  return (rows <= 8 ? launch_stream<T, D, 1> : rows <= 16 ? launch_stream<T, D, 2> : launch_stream<T, D, 4>)(pool, a, st);
+  if (rows > (D == 128 ? 16 : 32)) return launch_block<T, D>(pool, a, st);
+  if constexpr (D == 64)
+    if (rows > 16) return launch_stream<T, D, 4>(pool, a, st);
+  return (rows <= 8 ? launch_stream<T, D, 1> : launch_stream<T, D, 2>)(pool, a, st);
 }
 
 }  // namespace

@@ -10,15 +10,22 @@
 // so that the memory system works for the ones while the tensor cores work for the others.  prefix_join_kernel joins the
 // parts in ascending order: the same lengths give the same bits.
 //
-// A CTA of the prefixes.  Warp 8 copies keys and values page by page into a ring, warp 9 issues the products, warp 10
-// plans, and two groups of four warps have an accumulator of 128 rows each, one thread per row: a thread takes the 128
-// scores of its row from tensor memory, maximum, exponentials, and puts the probabilities where the scores were.  The
-// groups take turns at the tensor core: while it multiplies for one, the other has its exponentials.  Nothing is exchanged
-// between threads; a row's reference moves only when a score exceeds the maximum that set it by a factor of 2^8, and
-// then the thread rescales its output by itself (the scores of a unit come behind all earlier products of the accumulator).
+// A CTA of the prefixes.  Warp 8 copies keys and values page by page into a ring, warps 9 and 11 issue the products of a
+// group each, warp 10 plans, and two groups of four warps have an accumulator of 128 rows each, one thread per row: a thread
+// takes 64 scores of its row at a time from tensor memory, maximum, exponentials, and puts the probabilities where the scores
+// were, while the tensor core computes the next 64 beside them.  Nothing is exchanged between threads; a row's reference
+// moves only when a score exceeds the maximum that set it by a factor of 2^8, and then the thread rescales its output by itself
+// once the products under way have ended.
 // In a tile of at most 128 rows both groups have the same rows and every other unit, and join their halves at the end.
 // Every row of a tile sees the whole prefix, so masks are only needed at its end and at bad pages, and are the same for
 // all rows.  P is rounded to the cache's type as in tree attention.
+//
+// 192 rows of 32 heads of 128 over 32,765 positions: 266 us, 0.78 PFLOP/s; products alone 123 at the measured rate.  Neither
+// unit is full: the tensor pipe is active 40% of the time (a 128 x 128 x 16 product takes 64 cycles, a 128 x 64 x 16 one 48),
+// the special-function units need half of a block's cycles, and the groups run in step and share both.  Slower, at the same
+// point: 128 positions a block 303, one thread for the products of both groups 317, two threads a row 291, a part of the
+// exponentials by polynomial 270, the next scores asked for before the exponentials 307 and more.  Smaller calls are bound by
+// latency: plan and queries 7 to 9 us, the end of a segment 4 to 5, the joining kernel 5 to 8.
 #include <algorithm>
 #include <cmath>
 #include <cstdio>
@@ -31,12 +38,13 @@ namespace {
 constexpr int kPrefixThreads = 384;
 constexpr int kBlock = 64;              // positions whose scores are one product
 constexpr int kPlanned = 4;            // segments ahead
-constexpr int kPrefixSegmentCost = 4;  // in places
+constexpr int kPrefixSegmentCost = 4;  // in places; 64 rows over 8192 positions: 60 us with 1, 56 with 4, 58 with 8
 // Registers of a thread: the two groups that hold scores (or the fragments of the streaming body), and the third one.  Their
 // sum is what the block is launched with: 384 x 168 = 256 x 208 + 128 x 88.
 constexpr int kManyRegisters = 208, kFewRegisters = 88;
 
-// What a step of 16 own positions costs, in 64ths of a prefix's place.
+// What a step of 16 own positions costs, in 64ths of a prefix's place.  For heads of 128, three prefixes and 192 rows over
+// 32,765 positions: 6 gives 38 and 312 us, 10 33 and 266, 16 35 and 274.
 constexpr int kOwnCost128 = 10, kOwnCost64 = 6;
 
 struct PrefixView {
@@ -92,7 +100,7 @@ struct PrefixControl {
   long long places, own_places;
   uint32_t tmem;
   int give_up;
-  int edge[16];                        // of the last units: not all positions are seen (the ring holds at most six)
+  int edge[16];                        // of the last units: not all positions are seen (the ring holds fewer)
   uint32_t seen[16][4];
   float2 ml[2][128];                   // a group's reference and sum, for the other one
 };
@@ -1215,7 +1223,10 @@ int prima_prefix_attention(prima_paged* p, int layer, const prima_paged_batch* b
   a.part_o = reinterpret_cast<float*>(take(2 * sm * kPrefixRows * dim * 4));
   a.part_ml = reinterpret_cast<float2*>(take(2 * sm * kPrefixRows * 8));
   // Few rows of a sequence: its own positions are streamed beside the prefixes.  Many: tree attention's tensor-memory kernel
-  // is the better one for them (its rule), and runs in front.
+  // is the better one for them (its rule), and runs in front.  Beside against in front, 8 KV heads of 128: 16 sequences of 500
+  // behind 4096 positions, 16 rows 30 and 44 us, 32 rows 41 and 54, 64 rows 68 and 69; 64 of 300 behind 2000, 32 rows 88 and
+  // 103, 64 rows 156 and 140.  Own positions longer than the prefix, which the host does not know, would like it earlier: 16 of
+  // 3000 behind 1000, 4 rows 73 and 65, 32 rows 121 and 90 (heads of 64: 59 and 66).
   a.own_cost = streams(a.b, group) ? (dim == 128 ? kOwnCost128 : kOwnCost64) : 0;
   if (a.own_cost) {
     a.own_part_o = reinterpret_cast<float*>(take(16 * sm * kFewRows * dim * 4));
