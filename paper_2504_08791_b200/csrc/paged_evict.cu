@@ -5,8 +5,8 @@
 // with the whole GPU, however few the choices are.  Moving only what lies behind slot m, into the free slots in front of it,
 // costs m (n - m) / n entries of n where a compaction in order would move nearly all m.
 //
-// The choice is bound by latency (six prompts of up to 12,000 entries in ten layers: 29 us of 101, the longest sequence
-// decides), the moves by the copy (56 us at 5.3 TB/s; floor of both 58).  One request: 24 us, floor 10.
+// The choice is bound by latency (six prompts of up to 16,001 entries in ten layers: 45 us of 101, the longest sequence
+// decides), the moves by the copy (55 us at 5.3 TB/s; floor of both 58).  One request: 24 us, floor 10.
 #include <algorithm>
 #include <cstdio>
 

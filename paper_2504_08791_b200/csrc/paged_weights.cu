@@ -3,8 +3,8 @@
 //   w[s][g][j] = decay * w_in[s][g][j] + sum over rows t of s and query heads h of g that see j of exp(scale q_th . k_jg - lse_th)
 //
 // With the log-sum-exp of the attention the probabilities need no pass of their own: one product, one exponential a pair, one
-// sum.  Few rows are bound by the keys (48 single tokens over up to 8192 positions, heads of 128: 26.5 us, floor 18.2 at the
-// copy bandwidth), many by the exponentials, which the special-function units take at 16 a cycle and SM (64 rows of 32 heads
+// sum.  Few rows are bound by the keys (48 single tokens over up to 8192 positions, 40 and 8 heads of 128: 26.5 us, floor 18.2 at the
+// copy bandwidth), many by the exponentials, which the special-function units take at 16 a cycle and SM (64 rows of 64 heads
 // over 32,704 positions: 60 us, 31 of them exponentials at the least, 20.5 products).  Polynomials on the ordinary units for a
 // part of the exponentials gave 63 for 65 at that point and are not used.
 #include <algorithm>

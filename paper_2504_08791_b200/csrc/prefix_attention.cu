@@ -20,7 +20,7 @@
 // Every row of a tile sees the whole prefix, so masks are only needed at its end and at bad pages, and are the same for
 // all rows.  P is rounded to the cache's type as in tree attention.
 //
-// 192 rows of 32 heads of 128 over 32,765 positions: 266 us, 0.78 PFLOP/s; products alone 123 at the measured rate.  Neither
+// 192 rows of 64 and 8 heads of 128 over 32,765 positions: 266 us, 0.78 PFLOP/s; products alone 123 at the measured rate.  Neither
 // unit is full: the tensor pipe is active 40% of the time (a 128 x 128 x 16 product takes 64 cycles, a 128 x 64 x 16 one 48),
 // the special-function units need half of a block's cycles, and the groups run in step and share both.  Slower, at the same
 // point: 128 positions a block 303, one thread for the products of both groups 317, two threads a row 291, a part of the
