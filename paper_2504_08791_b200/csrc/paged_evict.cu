@@ -303,7 +303,8 @@ __global__ void __launch_bounds__(256) evict_move_kernel(const __grid_constant__
     const Sizes z = sizes_of(a, seq, &length);
     a.length_out[seq] = z.n < 0 ? length : z.m;
   }
-  const int count = __ldg(a.counts + item);
+  // From L2: the choices wrote counts and lists while this grid may have been resident, and lists share lines.
+  const int count = __ldcg(a.counts + item);
   const int32_t* const to = a.lists + 2 * a.half * item;
   const int32_t* const from = to + count;
   const int entry = lane / (2 * kPieces), piece = lane % kPieces, is_v = lane / kPieces & 1;
@@ -313,8 +314,8 @@ __global__ void __launch_bounds__(256) evict_move_kernel(const __grid_constant__
 #pragma unroll
     for (int f = 0; f < kFlight; ++f) {
       const int i = i0 + f * kEntries + entry;
-      row_to[f] = i < count ? __ldg(to + i) : -1;
-      row_from[f] = i < count ? __ldg(from + i) : -1;
+      row_to[f] = i < count ? __ldcg(to + i) : -1;
+      row_from[f] = i < count ? __ldcg(from + i) : -1;
     }
   };
   int i0 = warp * kEntries * kFlight;
