@@ -472,18 +472,18 @@ int prima_prefix_attention(prima_paged* pool, int layer, const prima_paged_batch
  * enter the arrays here: born[s][g][j] = the row's position (batch->pos, or the slot).  lse: dev fp32 [n_tok][n_q_heads], as
  * prima_tree_attention or prima_prefix_attention has left it (where a prefix took part, its positions have their share); a
  * row whose lse is -infinity adds nothing.  weight_in (may be NULL: nothing so far; may be weight_out), weight_out: dev fp32
- * [n_seq][n_kv_heads][stride], stride at most 2^31 - 256; born: dev int32, the same shape, may be NULL.  Entries behind the rows, and
- * those of sequences without rows, are left as they were.  A slot on a bad page receives nothing; slots from `stride` on are
- * left out (and raise a status bit).  q, masks and positions as in prima_tree_attention; scores and sums in 32 bits, always
- * added in the same order.  decay: 0..1; n_tok * n_q_heads below 2^31.  For a model's cache the arrays are [n_layers][n_seq][n_kv_heads][stride], of which
- * a call takes one layer's. */
+ * [n_seq][n_kv_heads][stride], stride at most 2^31 - 256; born: dev int32, the same shape, may be NULL.  Entries behind
+ * the rows, and those of sequences without rows, are left as they were.  The keys of slots that are seen must be finite.  A
+ * slot on a bad page receives nothing; slots from `stride` on are left out (and raise a status bit).  q, masks and positions as in prima_tree_attention; scores and sums in 32 bits, always
+ * added in the same order.  decay: 0..1; n_tok * n_q_heads below 2^31.  For a model's cache the arrays are
+ * [n_layers][n_seq][n_kv_heads][stride], of which a call takes one layer's. */
 int prima_paged_weights(prima_paged* pool, int layer, const prima_paged_batch* batch, const void* q, int n_q_heads, float scale, const float* lse,
                         const float* weight_in, float* weight_out, int32_t* born, int64_t stride, float decay, void* stream);
 
 /* Eviction: of the length[s] entries that each KV head of each layer holds of sequence s, m = min(keep[s], length[s]) stay,
  * chosen by head: entries with born < first or born >= recent_from[s] before all others, whatever their weight; the
- * others by weight (a NaN is less than any number); equal ones by slot, lower first.  The chosen ones in the slots 0 .. m-1 stay where they are; the others move
- * into the slots that become free there, both in ascending order, so that as little as possible is moved.  Keys, values,
+ * others by weight (a NaN is less than any number); equal ones by slot, lower first.  The chosen ones in the slots
+ * 0 .. m-1 stay where they are; the others move into the slots that become free there, both in ascending order, so that as little as possible is moved.  Keys, values,
  * weight and born move together; length_out[s] = m, and the pages behind are free.  Attention does not mind the order
  * (keys carry their rotation); a later step's rows go to the slots from m on and need `pos`.  The pages of the slots must be
  * the sequence's own (a shared prefix is kept apart: prima_prefix_attention).

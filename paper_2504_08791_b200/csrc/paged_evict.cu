@@ -5,8 +5,8 @@
 // with the whole GPU, however few the choices are.  Moving only what lies behind slot m, into the free slots in front of it,
 // costs m (n - m) / n entries of n where a compaction in order would move nearly all m.
 //
-// The choice is bound by latency (six prompts of up to 16,001 entries in ten layers: 45 us of 101, the longest sequence
-// decides), the moves by the copy (55 us at 5.3 TB/s; floor of both 58).  One request: 24 us, floor 10.
+// The choice is bound by latency (six prompts of up to 16,001 entries in ten layers: 34 us of 90, the longest sequence
+// decides), the moves by the copy (55 us at 5.3 TB/s; floor of both 58).  One request: 23 us, floor 10.
 #include <algorithm>
 #include <cstdio>
 
@@ -19,6 +19,7 @@ constexpr int kThreads = 512, kWarps = kThreads / 32, kPer = 4, kTile = kThreads
 constexpr int kBins = 2048;                           // of a digit: 11, 11 and 10 bits
 constexpr int kListed = 2048;                         // keys with the border's first digit that are set apart
 constexpr int kFlight = 8;                            // loads of a thread in flight
+constexpr int kRanked = 64;                           // sequences that are taken by length
 // Keys that a CTA keeps in shared memory; those behind are made from the arrays again in every pass.  Two CTAs share an SM.
 constexpr int kCached = 16384;
 
@@ -118,14 +119,33 @@ __global__ void __launch_bounds__(kThreads) evict_choose_kernel(const __grid_con
   __shared__ __align__(8) uint32_t s_tile[2][kPer * kWarps];
   __shared__ uint32_t s_found[3], s_listed;      // bin, keys above it, keys in it
   uint32_t turn = 0;
-  const int item = blockIdx.x, head = item % a.pool.n_kv_heads, ls = item / a.pool.n_kv_heads, seq = ls % a.n_seq, layer = ls / a.n_seq, tid = threadIdx.x, lane = tid & 31;
+  __shared__ int s_seq;
+  const int per_seq = gridDim.x / a.n_seq, layer = blockIdx.x % per_seq / a.pool.n_kv_heads, head = blockIdx.x % a.pool.n_kv_heads, tid = threadIdx.x, lane = tid & 31;
+  int seq = blockIdx.x / per_seq;
   pdl_trigger();
   pdl_wait();
+  // All choices of the longest sequence first, and so on: the GPU ends with short ones.  A thread ranks one sequence, in every
+  // choice, which many sequences do not pay back: six of up to 16,001 entries in ten layers 90 us, 101 by layers, two in 16
+  // layers 20 and 24, 64 in four 192 and 194, 500 in one 367 and 191.
+  if (a.n_seq > 1 && a.n_seq <= kRanked) {
+    int* const lengths = reinterpret_cast<int*>(s_hist[0]);
+    const int mine = tid < a.n_seq ? __ldg(a.length + tid) : 0;
+    if (tid < a.n_seq) lengths[tid] = mine;
+    __syncthreads();
+    if (tid < a.n_seq) {
+      int rank = 0;
+      for (int i = 0; i < a.n_seq; ++i) rank += lengths[i] > mine || (lengths[i] == mine && i < tid);
+      if (rank == seq) s_seq = tid;
+    }
+    __syncthreads();
+    seq = s_seq;
+  }
+  const int64_t item = (static_cast<int64_t>(layer) * a.n_seq + seq) * a.pool.n_kv_heads + head;
   int length;
   const Sizes z = sizes_of(a, seq, &length);
   const int n = z.n, m = z.m;
   if (n < 0 && tid == 0 && layer == 0 && head == 0) raise(a.pool.status, length < 0 || __ldg(a.keep + seq) < 0 ? kBadRows : kBadSlot);
-  const int64_t at = static_cast<int64_t>(item) * a.stride;
+  const int64_t at = item * a.stride;
   const float* const weight = a.weight + at;
   const int32_t* const born = a.born + at;
   const bool apart = a.weight_out != a.weight;
@@ -303,8 +323,8 @@ __global__ void __launch_bounds__(256) evict_move_kernel(const __grid_constant__
     const Sizes z = sizes_of(a, seq, &length);
     a.length_out[seq] = z.n < 0 ? length : z.m;
   }
-  // From L2: the choices wrote counts and lists while this grid may have been resident, and lists share lines.
-  const int count = __ldcg(a.counts + item);
+  // Ordinary loads: the choices wrote counts and lists while this grid may have been resident, and lists share lines.
+  const int count = a.counts[item];
   const int32_t* const to = a.lists + 2 * a.half * item;
   const int32_t* const from = to + count;
   const int entry = lane / (2 * kPieces), piece = lane % kPieces, is_v = lane / kPieces & 1;
@@ -314,8 +334,8 @@ __global__ void __launch_bounds__(256) evict_move_kernel(const __grid_constant__
 #pragma unroll
     for (int f = 0; f < kFlight; ++f) {
       const int i = i0 + f * kEntries + entry;
-      row_to[f] = i < count ? __ldcg(to + i) : -1;
-      row_from[f] = i < count ? __ldcg(from + i) : -1;
+      row_to[f] = i < count ? to[i] : -1;
+      row_from[f] = i < count ? from[i] : -1;
     }
   };
   int i0 = warp * kEntries * kFlight;

@@ -536,7 +536,7 @@ __global__ void __launch_bounds__(kBlockThreads, 1) weights_block_kernel(const _
       for (int block = single ? h : 0; block < blocks; block += single ? 2 : 1) {
         const int pos0 = (s.block0 + block) * kTilePos, j = pos0 + r;
         float had = 0.f;
-        if ((single || h == 0) && a.weight_in && j < min(s.n, s.ctx)) had = __ldg(a.weight_in + entry_of(a, s, j));
+        if ((single || h == 0) && a.weight_in && j < min(s.n, s.ctx)) had = a.weight_in[entry_of(a, s, j)];      // may be weight_out
         float2 sum = make_float2(0.f, 0.f);
         bool hidden = false;
 #pragma unroll 1

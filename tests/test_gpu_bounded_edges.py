@@ -187,3 +187,13 @@ def test_more_rows_than_32_bits_count_are_refused(gpu):
     rc = lib.prima_prefix_attention(pool._h, 0, C.byref(desc), C.byref(prefix.desc), q.data_ptr(), 64, 0.125, q.data_ptr(), 1, None, scratch.data_ptr(), 1 << 62, None)
     assert rc == binding.ERR_ARG and b"2^31" in lib.prima_last_error(None)
     pool.sync()
+
+
+@pytest.mark.parametrize("n_seq", [2, 63, 64, 65, 600])
+def test_evictions_of_many_sequences_in_any_order_of_lengths(gpu, n_seq):
+    """Sequences are taken by length up to 64, beyond it as they come; equal lengths, zeros and bad ones among them."""
+    from tests.test_gpu_paged_evict import check
+    rs = np.random.RandomState(n_seq)
+    ctx = rs.randint(0, 60, n_seq)
+    ctx[: n_seq // 2] = 37
+    check(gpu, Batch(913, ctx=ctx, nodes=[0] * n_seq, page=8, kv_heads=2, dim=64, layers=2), 20)
