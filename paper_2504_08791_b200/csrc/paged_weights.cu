@@ -430,16 +430,19 @@ __global__ void __launch_bounds__(kBlockThreads, 1) weights_block_kernel(const _
       const WeightsWork s = *w;
       done_with(i);
       const int32_t* table = a.b.table + s.seq * a.b.table_stride;
+      // The page that this lane's box of a block lies on, read a block ahead
+      auto page_of = [&](int block) {
+        const int pos = block * kTilePos + box * box_rows, slot = pos >> shift;
+        return panel < D / 64 && block < s.block1 && pos < s.n && slot < a.b.table_stride ? __ldg(table + slot) : -1;
+      };
+      int next_page = page_of(s.block0);
       for (int block = s.block0; block < s.block1; ++block) {
-        const int pos = block * kTilePos + box * box_rows;
-        int64_t row = -1;
-        bool bad = false;
-        if (panel < D / 64 && pos < s.n) {
-          const int64_t x = find_slot(a.pool, table, a.b.table_stride, a.layer, pos);
-          bad = x < 0;
-          if (bad) raise(status, static_cast<int>(-x));
-          else row = x + (static_cast<int64_t>(s.head) << shift);
-        }
+        const int pos = block * kTilePos + box * box_rows, page = next_page;
+        next_page = page_of(block + 1);
+        const bool wanted = panel < D / 64 && pos < s.n, bad = wanted && static_cast<unsigned>(page) >= static_cast<unsigned>(a.pool.n_pages);
+        int row = -1;      // below 2^31 (prima_paged_create)
+        if (bad) raise(status, pos >> shift < a.b.table_stride ? kBadPage : kBadSlot);
+        else if (wanted) row = (((a.layer * a.pool.n_pages + page) * a.pool.n_kv_heads + s.head) << shift) + (pos & ((1 << shift) - 1));
         const int n_copies = __popc(__ballot_sync(0xffffffffu, row >= 0));
         const bool any_bad = __any_sync(0xffffffffu, bad);
         bool ok = true;
@@ -450,7 +453,7 @@ __global__ void __launch_bounds__(kBlockThreads, 1) weights_block_kernel(const _
             mbar_expect(bar_full + 8 * ring.slot, static_cast<uint32_t>(n_copies) * box_rows * 128);
           }
           __syncwarp();
-          if (row >= 0) tma_load_2d(dst + ring.slot * Geo::kSlotBytes, &k_map, panel * 64, static_cast<int>(row), bar_full + 8 * ring.slot);
+          if (row >= 0) tma_load_2d(dst + ring.slot * Geo::kSlotBytes, &k_map, panel * 64, row, bar_full + 8 * ring.slot);
         }
         ring.step(1);
         if (copies_before < Geo::kSlots) ++copies_before;
