@@ -5,11 +5,12 @@
 // With the log-sum-exp of the attention the probabilities need no pass of their own: one product, one exponential a pair, one
 // sum.  Few rows are bound by the keys (48 single tokens over up to 8192 positions, 40 and 8 heads of 128: 26.5 us, floor 18.2 at the
 // copy bandwidth), many by the exponentials, which the special-function units take at 16 a cycle and SM (64 rows of 64 heads
-// over 32,704 positions: 60 us, 31 of them exponentials at the least, 20.5 products).  Polynomials on the ordinary units for a
+// over 32,704 positions: 61 us, 31 of them exponentials at the least, 20.5 products).  Polynomials on the ordinary units for a
 // part of the exponentials gave 63 for 65 at that point and are not used.
 #include <algorithm>
 #include <cmath>
 #include <cstdio>
+#include <type_traits>
 
 #include "paged_device.cuh"
 
@@ -552,50 +553,59 @@ __global__ void __launch_bounds__(kBlockThreads, 1) weights_block_kernel(const _
           const bool edge = pos0 + kTilePos > s.ctx;
           const int behind = j - s.ctx;      // index of the position among the rows of the step
           const float* const shift = ctl->shift[2 * h + p];
-          uint32_t x[2][32];
-          tmem_load(x[0], t_s + kRowTile * d);
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            tmem_wait_load();
-            tmem_use(x[c & 1]);
-            if (c < 3) {
-              tmem_load(x[(c + 1) & 1], t_s + kRowTile * d + 32 * (c + 1));
-            } else {      // all are read: the next product may have the accumulator
-              tc_fence_before();
-              __syncwarp();
-              if (lane == 0) mbar_arrive(bar_free + 8 * (2 * h + d));
-            }
-            uint32_t seen = 0xffffffffu;
-            if (edge && behind >= 0) {
-              const int row = t * kRowTile + 32 * c;
-              if (!a.b.mask) {      // rows from the position's own node on
-                const long long skip = static_cast<long long>(behind) * a.group - row;
-                seen = skip >= 32 ? 0u : skip <= 0 ? 0xffffffffu : 0xffffffffu << static_cast<int>(skip);
-              } else {
-                seen = 0;
-#pragma unroll 1
-                for (int e = 0; e < 32; ++e) {
-                  const int node = (row + e) / a.group;
-                  if (node < s.nodes && sees(a, s.first, node, behind)) seen |= 1u << e;
+          const int chunks = min(kRowTile / 32, (s.nodes * a.group - t * kRowTile + 31) >> 5);      // 32 columns each that hold rows
+          // Full tiles, whose columns are known when this is compiled, and others.  64 rows of 64 heads over 32,704 positions 61 us,
+          // with one body for both 64, with full tiles alone 60; but then 16 sequences of 4096 with 24 rows 36 us, so 32.
+          auto take = [&](auto full) {
+            constexpr bool kFull = decltype(full)::value;
+            uint32_t x[2][32];
+            tmem_load(x[0], t_s + kRowTile * d);
+  #pragma unroll
+            for (int c = 0; c < kRowTile / 32; ++c) {
+              if (!kFull && c == chunks) break;
+              tmem_wait_load();
+              tmem_use(x[c & 1]);
+              if (kFull ? c + 1 < kRowTile / 32 : c + 1 < chunks) {
+                tmem_load(x[(c + 1) & 1], t_s + kRowTile * d + 32 * (c + 1));
+              } else {      // all are read: the next product may have the accumulator
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar_free + 8 * (2 * h + d));
+              }
+              uint32_t seen = 0xffffffffu;
+              if (edge && behind >= 0) {
+                const int row = t * kRowTile + 32 * c;
+                if (!a.b.mask) {      // rows from the position's own node on
+                  const long long skip = static_cast<long long>(behind) * a.group - row;
+                  seen = skip >= 32 ? 0u : skip <= 0 ? 0xffffffffu : 0xffffffffu << static_cast<int>(skip);
+                } else {
+                  seen = 0;
+  #pragma unroll 1
+                  for (int e = 0; e < 32; ++e) {
+                    const int node = (row + e) / a.group;
+                    if (node < s.nodes && sees(a, s.first, node, behind)) seen |= 1u << e;
+                  }
                 }
               }
-            }
-#pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-              const float4 z = *reinterpret_cast<const float4*>(shift + 32 * c + e);
-              float2 u = fma2(make_float2(__uint_as_float(x[c & 1][e]), __uint_as_float(x[c & 1][e + 1])), scale, make_float2(z.x, z.y));
-              float2 v = fma2(make_float2(__uint_as_float(x[c & 1][e + 2]), __uint_as_float(x[c & 1][e + 3])), scale, make_float2(z.z, z.w));
-              u = make_float2(ex2(u.x), ex2(u.y));
-              v = make_float2(ex2(v.x), ex2(v.y));
-              if (edge) {
-                u.x = seen >> e & 1 ? u.x : 0.f;
-                u.y = seen >> (e + 1) & 1 ? u.y : 0.f;
-                v.x = seen >> (e + 2) & 1 ? v.x : 0.f;
-                v.y = seen >> (e + 3) & 1 ? v.y : 0.f;
+  #pragma unroll
+              for (int e = 0; e < 32; e += 4) {
+                const float4 z = *reinterpret_cast<const float4*>(shift + 32 * c + e);
+                float2 u = fma2(make_float2(__uint_as_float(x[c & 1][e]), __uint_as_float(x[c & 1][e + 1])), scale, make_float2(z.x, z.y));
+                float2 v = fma2(make_float2(__uint_as_float(x[c & 1][e + 2]), __uint_as_float(x[c & 1][e + 3])), scale, make_float2(z.z, z.w));
+                u = make_float2(ex2(u.x), ex2(u.y));
+                v = make_float2(ex2(v.x), ex2(v.y));
+                if (edge) {
+                  u.x = seen >> e & 1 ? u.x : 0.f;
+                  u.y = seen >> (e + 1) & 1 ? u.y : 0.f;
+                  v.x = seen >> (e + 2) & 1 ? v.x : 0.f;
+                  v.y = seen >> (e + 3) & 1 ? v.y : 0.f;
+                }
+                sum = add2(sum, add2(u, v));
               }
-              sum = add2(sum, add2(u, v));
             }
-          }
+          };
+          if (chunks == kRowTile / 32) take(std::true_type());
+          else take(std::false_type());
           // Many tiles: the one after the next into this place, whose scores are there (for the next block, from the first on).
           if (again && !(block == blocks - 1 && m + 2 >= mine)) {
             group_sync();      // all have read the shifts
@@ -668,14 +678,11 @@ cudaError_t launch_block(const prima_paged& pool, const WeightsArgs& a, cudaStre
 template <typename T, int D>
 cudaError_t launch_weights(const prima_paged& pool, const WeightsArgs& a, cudaStream_t st) {
   // Rows that a KV head has of a sequence on average; each variant is right for any.  Streaming against tensor memory, 8 KV
-  // heads, B200: of 128, 16 sequences of 4096 positions, 8 rows 27 and 41 us, 16 rows 29 and 41, 24 rows 52 and 41; 64 of 600,
-  // 16 rows 19 and 33, 24 rows 34 and 34; one of 8192, 16 rows 9.3 and 10.2, 24 rows 12.9 and 10.2 (32 rows of 128 elements
-  // leave registers for one CTA per SM).  Of 64, 16 sequences of 4096, 32 rows 31 and 35, 40 rows 96 and 35; 64 of 600, 22 and
-  // 31, then 66 and 31.
+  // heads, B200: of 128, 16 sequences of 4096 positions, 4 rows 27 and 33 us, 16 rows 29 and 33; 64 of 600, 15 and 26, 19 and 26;
+  // one of 8192, 6.7 and 8.8, 9.3 and 8.8.  Of 64, 17 and 24, 23 and 24; 13 and 22, 16 and 22; 6.1 and 7.7, 8.0 and 7.7.  32 rows
+  // in registers: heads of 128 53 and 33, 35 and 26, 14 and 8.7; of 64 31 and 24, 22 and 21, 12 and 7.7.
   const int64_t rows = (static_cast<int64_t>(a.b.n_tok) + a.b.n_seq - 1) / a.b.n_seq * a.group;
-  if (rows > (D == 128 ? 16 : 32)) return launch_block<T, D>(pool, a, st);
-  if constexpr (D == 64)
-    if (rows > 16) return launch_stream<T, D, 4>(pool, a, st);
+  if (rows > 16) return launch_block<T, D>(pool, a, st);
   return (rows <= 8 ? launch_stream<T, D, 1> : launch_stream<T, D, 2>)(pool, a, st);
 }
 
