@@ -145,6 +145,9 @@ struct PrefixShape {
 
 PRIMA_HD int64_t prefix_units(const PrefixShape& t, int len) { return ((len < t.capacity ? len : t.capacity) + kTilePos - 1) / kTilePos; }
 PRIMA_HD int prefix_weight(int64_t rows, int64_t row_tile) { return rows - row_tile * kPrefixRows > kPrefixRows / 2 ? 2 : 1; }
+// Units that accumulator `group` (0 or 1) has of a stretch of n: all of them in a tile of more than half the rows, otherwise
+// every other one, which may be none.  The first accumulator has the first unit.
+PRIMA_HD int prefix_group_units(bool both, int n, int group) { return both ? n : (n + 1 - group) >> 1; }
 // Places in the line of one KV head of a prefix with this many rows.
 PRIMA_HD int64_t prefix_places(const PrefixShape& t, int64_t rows, int64_t units) {
   if (rows <= 0 || units <= 0) return 0;

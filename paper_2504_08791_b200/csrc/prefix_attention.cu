@@ -91,6 +91,7 @@ struct PrefixWork {
   int last_worker;
   long long limit;                     // positions that are seen
   __device__ __forceinline__ bool both() const { return rows > kPrefixRows / 2; }      // accumulators per unit
+  __device__ __forceinline__ int units_of(int group_of_warps) const { return prefix_group_units(both(), n, group_of_warps); }
 };
 
 struct PrefixControl {
@@ -690,7 +691,7 @@ __device__ __forceinline__ void PrefixCta<D>::feed(const Maps& maps, PrefixCurso
     const SmemOperand qq = smem_operand(uniform(smem_u32(s_q) + h * Geo::kQBytes), 16), k_all = smem_operand(ring_addr, 16), v_all = smem_operand(ring_addr, Geo::kPanel);
     const uint32_t my_s = bar_s + 16 * h, my_p = bar_p + 16 * h, my_pv = bar_pv + 16 * h;
     if (elect_one()) {
-      uint32_t turn = 0;      // blocks so far
+      uint32_t turn = 0, tiles = 0;      // blocks so far; tiles of queries
       bool ok = true;
       auto wait = [&](uint32_t bar, uint32_t parity) { ok = wait_for(bar, parity, give_up, status) && ok; };
       for (uint32_t si = 0;; ++si) {
@@ -700,10 +701,10 @@ __device__ __forceinline__ void PrefixCta<D>::feed(const Maps& maps, PrefixCurso
           break;
         }
         const bool both = ctl->seg[at].both();
-        const int n = ctl->seg[at].n, count = 2 * (both ? n : (n + 1 - static_cast<int>(h)) >> 1);
+        const int n = ctl->seg[at].n, count = 2 * ctl->seg[at].units_of(h);
         if (n == 0) break;
         mbar_arrive(bar_seg_empty + 8 * at);
-        wait(bar_q + 8 * h, si & 1);
+        if (count) wait(bar_q + 8 * h, tiles++ & 1);      // without a unit the group loads none
         // The places of the next scores' keys and of the next product's values.  Where only one group takes a unit it gives its
         // places back twice.
         RingPlace<kSlots> pk = ring, pv;
@@ -786,26 +787,26 @@ __device__ __forceinline__ void PrefixCta<D>::softmax() {
   const PrefixWork* seg;
   for (uint32_t si = 0; (seg = segment(si)); ++si) {
     const PrefixWork& s = *seg;
-    if (!loaded) {
+    const bool both = s.both();
+    const int count = s.units_of(w);
+    // A group loads the queries of the segments that it has units of, and of no other: what orders a phase of the barrier
+    // behind the wait for the one before it is that the group has seen the scores between the two.
+    if (!loaded && count) {
       load_queries(s);
       queries_ready();
-      if (si == 0 && lane == 0) mbar_arrive(bar_first);
     }
+    if (si == 0 && lane == 0) mbar_arrive(bar_first);
     bool next_loads = false;
     auto load_next = [&]() {
       const PrefixWork* next = segment(si + 1);
-      if (!next) return;
+      if (!next || !next->units_of(w)) return;
       load_queries(*next);
       next_loads = true;
     };
-    const bool both = s.both();
-    const int count = both ? s.n : (s.n + 1 - w) >> 1;
     const int in_tile = (both ? w * 128 : 0) + r;
     const bool live = in_tile - lane < s.rows, mine = in_tile < s.rows;
     float m = -INFINITY;
     float2 sum = make_float2(0.f, 0.f);
-    // (without a unit the next queries wait for the other group's end: the barrier of the queries may be one phase ahead of
-    // the warp that issues the products, not two)
 #pragma unroll 1
     for (int i = 0; i < 2 * count; ++i, ++n_block) {
       const int t = both ? i >> 1 : (i & ~1) + w, half = i & 1;
