@@ -361,6 +361,10 @@ __device__ __forceinline__ void own_share(const CUtensorMap* k_map, const CUtens
   const CUtensorMap* const map = is_v ? v_map : k_map;
   const uint32_t box_at = ring_addr + is_v * Geo::kHalf + panel * Geo::kPanel + half * box_rows * 128;
 
+  // Only here, where it is known that this CTA streams: in the others copies write over this memory.
+  if (lane < Geo::kStages) mbar_init(bar_full + 8 * lane, 1);
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  __syncwarp();
   OwnCursor cursor(a, own, lane, worker, n_workers, total);
   RingPlace<Geo::kStages> put, get;
   uint32_t bad_stages = 0, planned = 0, begun = 0;
@@ -1006,8 +1010,6 @@ __global__ void __launch_bounds__(kPrefixThreads, 1) prefix_kernel(const __grid_
     ctl->own_places = 0;
     tma_prefetch_map(&maps.k);
     tma_prefetch_map(&maps.v);
-  } else if (tid < 1 + 8 * 6) {
-    mbar_init(smem_u32(&own->full[0][0] + (tid - 1)), 1);
   }
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   if (warp == 9) tmem_alloc(smem_u32(&ctl->tmem), 512);
