@@ -450,7 +450,8 @@ int prima_tree_attention(prima_paged* pool, int layer, const prima_paged_batch* 
  * (once per 256 of a KV head's rows).  Slots and ctx_len of a sequence count its own positions alone; where the rotation is
  * to go on behind the prefix, the append needs `pos`.  out, lse, q, scale, masks, types and refusals as there; n_tok *
  * n_q_heads below 2^31.  A prefix with a negative length or a bad range of sequences or rows counts as none (and raises a
- * status bit), positions behind its table are not seen.  The value of a position that is seen must be finite.
+ * status bit), positions behind its table are not seen.  The value of a position that is seen must be finite.  A row with a
+ * NaN among its scores is NaN, and its log-sum-exp too.
  * workspace as there, of the bytes that prima_prefix_attention_workspace names (room for the prefix's and the own part of
  * every row's output in 32 bits, among others). */
 typedef struct {

@@ -1120,7 +1120,7 @@ __global__ void __launch_bounds__(256) prefix_join_kernel(const __grid_constant_
     o.w *= f;
 #pragma unroll
     for (int j = 0; j < kFlight; ++j) {
-      if (ml[j].x == -INFINITY) continue;      // nothing was seen: its columns may be anything
+      if (ml[j].y == 0.f) continue;      // nothing was seen: its columns may be anything.  (All scores NaN: reference -infinity, sum NaN.)
       const float g = ex2(ml[j].x - m);
       total += ml[j].y * g;
       o.x += x[j].x * g;
