@@ -484,16 +484,17 @@ int prima_paged_weights(prima_paged* pool, int layer, const prima_paged_batch* b
 /* Eviction: of the length[s] entries that each KV head of each layer holds of sequence s, m = min(keep[s], length[s]) stay,
  * chosen by head: entries with born < first or born >= recent_from[s] before all others, whatever their weight; the
  * others by weight (a NaN is less than any number); equal ones by slot, lower first.  The chosen ones in the slots
- * 0 .. m-1 stay where they are; the others move into the slots that become free there, both in ascending order, so that as little as possible is moved.  Keys, values,
- * weight and born move together; length_out[s] = m, and the pages behind are free.  Attention does not mind the order
+ * 0 .. m-1 stay where they are; the others move into the slots that become free there, both in ascending order, so that as
+ * little as possible is moved.  Keys, values, weight and born move together; length_out[s] = m, and the pages behind are free.  Attention does not mind the order
  * (keys carry their rotation); a later step's rows go to the slots from m on and need `pos`.  The pages of the slots must be
  * the sequence's own (a shared prefix is kept apart: prima_prefix_attention).
  * weight, weight_out: dev fp32 [n_layers][n_seq][n_kv_heads][stride]; born, born_out: dev int32, the same shape; keep,
  * recent_from (NULL: none), length, length_out: dev int32 [n_seq].  weight_out may be weight (and then born_out must be born,
  * and the other way round), otherwise the arrays must not overlap; entries from m on are left as they were.  length_out may
  * be length.  A sequence with a negative length or keep, or more positions than stride or the table hold, is left as it is,
- * length_out = length, and raises a status bit.  stride: at most 2^30.  workspace: dev, 256-byte aligned, as named for the
- * same (n_seq, stride). */
+ * length_out = length, and raises a status bit.  An entry from or to a slot on a bad page does not move, its weight and born
+ * neither: that slot keeps what it had (weight_out and born_out: the slot's own), and a status bit is raised.  stride: at
+ * most 2^30.  workspace: dev, 256-byte aligned, as named for the same (n_seq, stride). */
 int64_t prima_paged_evict_workspace(const prima_paged* pool, int n_seq, int64_t stride);
 int prima_paged_evict(prima_paged* pool, int n_seq, const int32_t* table, int64_t table_stride, const int32_t* length, const float* weight,
                       const int32_t* born, int64_t stride, const int32_t* keep, int first, const int32_t* recent_from, float* weight_out,

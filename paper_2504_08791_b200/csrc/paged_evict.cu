@@ -300,10 +300,14 @@ __global__ void __launch_bounds__(kThreads) evict_choose_kernel(const __grid_con
 #pragma unroll 4
   for (int i = tid; i < n_moves; i += kThreads) {
     const int hole = list[i], mover = list[n_moves + i];
-    a.weight_out[at + hole] = weight[mover];
-    a.born_out[at + hole] = born[mover];
+    const float w = weight[mover];
+    const int b = born[mover];
     const int64_t to = slot_row(a.pool, table, a.table_stride, layer, hole), from = slot_row(a.pool, table, a.table_stride, layer, mover);
-    const bool good = to >= 0 && from >= 0;      // a row is below 2^31 (prima_paged_create)
+    const bool good = to >= 0 && from >= 0;      // a row is below 2^31 (prima_paged_create); otherwise nothing of the entry moves
+    if (good) {
+      a.weight_out[at + hole] = w;
+      a.born_out[at + hole] = b;
+    }
     list[i] = good ? static_cast<int>(to) + (head << a.pool.page_shift) : -1;
     list[n_moves + i] = good ? static_cast<int>(from) + (head << a.pool.page_shift) : -1;
   }
