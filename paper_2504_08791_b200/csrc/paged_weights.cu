@@ -249,6 +249,11 @@ __global__ void __launch_bounds__(256, kStreamCtas) weights_stream_kernel(const 
         }
 #pragma unroll
         for (int e = 0; e < 2; ++e) down[n][e] = shift_of(a, s, row0 + 8 * n + 2 * t4 + e);
+        // A row that adds nothing: its scores are 0, whatever its query holds (its shift makes them 0 as probabilities).
+        const float even = __shfl_sync(0xffffffffu, down[n][0], g >> 1), odd = __shfl_sync(0xffffffffu, down[n][1], g >> 1);
+        if ((g & 1 ? odd : even) == -INFINITY)
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k) q[n][k][0] = q[n][k][1] = 0u;
       }
     };
     // What position g (lanes with t4 = 0) or g + 8 (t4 = 1) of a block has had, read a block ahead
@@ -519,6 +524,12 @@ __global__ void __launch_bounds__(kBlockThreads, 1) weights_block_kernel(const _
       asm volatile("cp.async.wait_all;" ::: "memory");
       fence_async_smem();
       group_sync();      // the group reads all shifts
+      if (ctl->shift[2 * h + p][r] == -INFINITY) {      // adds nothing: scores of 0, whatever its query holds
+#pragma unroll
+        for (int c = 0; c < D / 8; ++c) *reinterpret_cast<uint4*>(smem + (2 * h + p) * Geo::kTileBytes + c / 8 * Geo::kPanel + r * 128 + c % 8 * 16) = make_uint4(0, 0, 0, 0);
+        fence_async_smem();
+      }
+      __syncwarp();
       if (lane == 0) mbar_arrive(bar_q + 8 * (2 * h + p));
     };
     const float2 scale = make_float2(a.scale_log2, a.scale_log2);
