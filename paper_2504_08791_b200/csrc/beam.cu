@@ -125,8 +125,8 @@ __device__ __forceinline__ float2 mul2(float2 x, float2 y) {
 // exponential, sum, comparison with the bound) and the latency of the beginning and the end of a CTA; 128 rows of 152,064
 // fp32 logits, of which 64 MB are read: about 20 us, 3.2 TB/s (27.5 us with the joining kernel).
 template <typename T, int E>
-__global__ void __launch_bounds__(kThreads, 3) beam_slice_kernel(const T* __restrict__ logits, int64_t row_stride, int vocab, const float* __restrict__ cum,
-                                                              const uint8_t* __restrict__ finished, int keep, int n_slices, int per_split, bool wide,
+__global__ void __launch_bounds__(kThreads, 3) beam_slice_kernel(const T* logits, int64_t row_stride, int vocab, const float* cum,
+                                                              const uint8_t* finished, int keep, int n_slices, int per_split, bool wide,
                                                               SliceStat* __restrict__ stat, Best* __restrict__ best) {
   constexpr int kVec = 16 / sizeof(T);
   constexpr float kLog2e = 1.4426950408889634f;
@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(kThreads, 3) beam_slice_kernel(const T* __rest
   pdl_trigger();
   pdl_wait();
   const int row = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const float c = __ldg(cum + row);
+  const float c = cum[row];
   if ((finished && finished[row]) || !(c > -INFINITY)) return;
   const T* x0 = logits + row * row_stride;
   const int slice0 = blockIdx.x * per_split, slice1 = min(slice0 + per_split, n_slices);
@@ -285,7 +285,7 @@ __global__ void __launch_bounds__(kThreads, 3) beam_slice_kernel(const T* __rest
 // One CTA per request joins the slices of its beams: 5 to 9 us, latency of its reads, of the sums in 64 bits and of the
 // barriers.
 constexpr int kFound = 1024;
-__global__ void __launch_bounds__(kThreads) beam_join_kernel(int n_beams, int vocab, const float* __restrict__ cum, const uint8_t* __restrict__ finished,
+__global__ void __launch_bounds__(kThreads) beam_join_kernel(int n_beams, int vocab, const float* cum, const uint8_t* finished,
                                                              int end_token, int keep, int n_splits, const SliceStat* __restrict__ stat,
                                                              const Best* __restrict__ best, float* __restrict__ score, int32_t* __restrict__ parent,
                                                              int32_t* __restrict__ token) {
@@ -299,7 +299,7 @@ __global__ void __launch_bounds__(kThreads) beam_join_kernel(int n_beams, int vo
   const int req = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int row0 = req * n_beams, per_beam = n_splits * keep;
   for (int b = warp; b < n_beams; b += kThreads / 32) {
-    const float c = __ldg(cum + row0 + b);
+    const float c = cum[row0 + b];
     const bool done = finished && finished[row0 + b];
     double top = INFINITY, sum = 1;
     if (done && c > -INFINITY) {

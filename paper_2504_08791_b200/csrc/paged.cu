@@ -23,8 +23,8 @@ namespace {
 // Prompts of 11,268 rows, 40 + 16 heads of 128, bf16, 323 MB: 61 us, 5.3 TB/s, HBM; one row 3.0 us, 278 rows of
 // trees 6 us, latency.
 template <typename T, typename In, int D, int kWarps>
-__global__ void __launch_bounds__(256) append_kernel(PoolView pool, BatchView b, int layer, const In* __restrict__ q, const In* __restrict__ k,
-                                                     const In* __restrict__ v, int n_q_heads, int64_t q_stride, int64_t k_stride,
+__global__ void __launch_bounds__(256) append_kernel(PoolView pool, BatchView b, int layer, const In* q, const In* k,
+                                                     const In* v, int n_q_heads, int64_t q_stride, int64_t k_stride,
                                                      int64_t v_stride, bool wide, const double* __restrict__ freq, int mode,
                                                      T* __restrict__ q_out) {
   constexpr int kPairs = D / 2, kItems = D / 16, kHeads = 32 / kItems, kStep = kWarps * kHeads;
@@ -52,10 +52,10 @@ __global__ void __launch_bounds__(256) append_kernel(PoolView pool, BatchView b,
   load(h, x[0]);                       // in flight while the place is looked up
   load(h + kStep, x[1]);
 
-  int p = b.pos ? __ldg(b.pos + t) : 0;
+  int p = b.pos ? b.pos[t] : 0;
   const int s = seq_of_row(b, t, lane);
   if (s >= b.n_seq) return;            // padding
-  const int first = __ldg(b.row_begin + s), ctx = __ldg(b.ctx_len + s);
+  const int first = b.row_begin[s], ctx = b.ctx_len[s];
   if (t < first || first < 0 || ctx < 0) {
     if (lane == 0) raise(pool.status, kBadRows);
     return;
@@ -130,7 +130,7 @@ __global__ void __launch_bounds__(256) append_kernel(PoolView pool, BatchView b,
 // L2; 17 when other data went through it); one path of 4 rows, 32 layers: 2.9 us.
 constexpr int kPathBatch = 8, kPathBlock = 256;
 template <int D>
-__global__ void __launch_bounds__(256) accept_kernel(PoolView pool, BatchView b, const int32_t* __restrict__ path, const int32_t* __restrict__ path_len,
+__global__ void __launch_bounds__(256) accept_kernel(PoolView pool, BatchView b, const int32_t* path, const int32_t* path_len,
                                                      int path_stride) {
   constexpr int kPieces = D / 8;                  // 16-byte pieces of a row
   __shared__ int2 s_move[kPathBlock];             // page and row in the page, packed: from, to; from < 0: stays
@@ -138,7 +138,7 @@ __global__ void __launch_bounds__(256) accept_kernel(PoolView pool, BatchView b,
   pdl_trigger();
   pdl_wait();
   const int s = blockIdx.x, G = pool.n_kv_heads;
-  const int first = __ldg(b.row_begin + s), end = __ldg(b.row_begin + s + 1), ctx = __ldg(b.ctx_len + s), n = __ldg(path_len + s);
+  const int first = b.row_begin[s], end = b.row_begin[s + 1], ctx = b.ctx_len[s], n = path_len[s];
   if (first < 0 || end < first || end > b.n_tok || ctx < 0 || n < 0 || n > path_stride) {
     if (threadIdx.x == 0) raise(pool.status, n < 0 || n > path_stride ? kBadPath : kBadRows);
     return;
@@ -150,14 +150,14 @@ __global__ void __launch_bounds__(256) accept_kernel(PoolView pool, BatchView b,
     const int m = min(n - j0, kPathBlock);
     __syncthreads();
     if (static_cast<int>(threadIdx.x) < m) {
-      const int j = j0 + threadIdx.x, a = __ldg(path + static_cast<int64_t>(s) * path_stride + j);
+      const int j = j0 + threadIdx.x, a = path[static_cast<int64_t>(s) * path_stride + j];
       int2 pages = make_int2(-1, 0), rows = make_int2(0, 0);
-      if (a < 0 || a >= end - first || (j > 0 && a <= __ldg(path + static_cast<int64_t>(s) * path_stride + j - 1))) {
+      if (a < 0 || a >= end - first || (j > 0 && a <= path[static_cast<int64_t>(s) * path_stride + j - 1])) {
         raise(pool.status, kBadPath);
       } else if (a != j) {
         const int64_t from = static_cast<int64_t>(ctx) + a, to = static_cast<int64_t>(ctx) + j;
         if (slot_row(pool, table, b.table_stride, 0, from) >= 0 && slot_row(pool, table, b.table_stride, 0, to) >= 0) {
-          pages = make_int2(__ldg(table + (from >> pool.page_shift)), __ldg(table + (to >> pool.page_shift)));
+          pages = make_int2(table[from >> pool.page_shift], table[to >> pool.page_shift]);
           rows = make_int2(static_cast<int>(from) & in_page, static_cast<int>(to) & in_page);
         }
       }
@@ -189,29 +189,29 @@ __global__ void __launch_bounds__(256) accept_kernel(PoolView pool, BatchView b,
 // (length % page_size) * head_dim * 2 bytes.  128 rows, 16 layers, 8 KV heads: 9.7 us, bound by the reads that a warp has
 // in flight; with index arithmetic per 16 bytes it took 20.
 template <int D>
-__global__ void __launch_bounds__(256) reorder_kernel(PoolView pool, int n_beams, int keep, const int32_t* __restrict__ table_in, int64_t stride,
-                                                      const int32_t* __restrict__ length_in, const int32_t* __restrict__ parent,
-                                                      const int32_t* __restrict__ fresh, int32_t* __restrict__ table_out, int32_t* __restrict__ length_out) {
+__global__ void __launch_bounds__(256) reorder_kernel(PoolView pool, int n_beams, int keep, const int32_t* table_in, int64_t stride,
+                                                      const int32_t* length_in, const int32_t* parent,
+                                                      const int32_t* fresh, int32_t* __restrict__ table_out, int32_t* __restrict__ length_out) {
   pdl_trigger();
   pdl_wait();
   const int r = blockIdx.x, req = r / keep, j = r - req * keep;
   const int lane = threadIdx.x & 31;
   const int G = pool.n_kv_heads;
-  int p = __ldg(parent + r);
-  const int f = __ldg(fresh + r);
+  int p = parent[r];
+  const int f = fresh[r];
   bool shared_parent = false;
-  for (int i = lane; i < j; i += 32) shared_parent |= __ldg(parent + r - j + i) == p;
+  for (int i = lane; i < j; i += 32) shared_parent |= parent[r - j + i] == p;
   shared_parent = __any_sync(0xffffffffu, shared_parent);
   if (!shared_parent && blockIdx.y > 0) return;
   const bool bad = p < 0 || p >= n_beams;
   if (bad) p = 0;
   const int64_t src = static_cast<int64_t>(req) * n_beams + p;
-  const int len = __ldg(length_in + src);
+  const int len = length_in[src];
   const int64_t pages = (static_cast<int64_t>(max(len, 0)) + (1 << pool.page_shift) - 1) >> pool.page_shift;
   const int tail = len & ((1 << pool.page_shift) - 1);
   const bool bad_len = len < 0 || pages > stride;
   const bool empty = bad || bad_len;      // continues nothing: it must not share another row's partly filled page
-  const int last = !empty && pages > 0 ? __ldg(table_in + src * stride + pages - 1) : 0;
+  const int last = !empty && pages > 0 ? table_in[src * stride + pages - 1] : 0;
   const bool copies = shared_parent && tail != 0 && !empty;
   const bool bad_page = copies && (static_cast<unsigned>(last) >= static_cast<unsigned>(pool.n_pages) || static_cast<unsigned>(f) >= static_cast<unsigned>(pool.n_pages));
   if (blockIdx.y == 0) {
@@ -222,7 +222,7 @@ __global__ void __launch_bounds__(256) reorder_kernel(PoolView pool, int n_beams
       length_out[r] = empty ? 0 : len;
     }
     for (int64_t i = threadIdx.x; i < stride; i += blockDim.x)
-      table_out[r * stride + i] = empty || i >= pages ? -1 : copies && i == pages - 1 ? f : __ldg(table_in + src * stride + i);
+      table_out[r * stride + i] = empty || i >= pages ? -1 : copies && i == pages - 1 ? f : table_in[src * stride + i];
   }
   if (!copies || bad_page) return;
   // A warp takes one head of keys or values of one layer at a time (index arithmetic per 16 bytes would bound the kernel).

@@ -51,6 +51,8 @@ int check_append(const prima_paged* pool, int layer, const void* q, const void* 
 cudaError_t make_tree_maps(prima_paged* pool);
 void free_tree_maps(prima_paged* pool);
 
+// What a kernel in front may have written (a batch's arrays, queries, keys, values, log-sum-exps) is read by ordinary loads: grids
+// overlap their predecessors, and the read-only path asks for data that nobody writes while the grid is there.
 struct BatchView {
   int n_seq, n_tok;
   const int32_t* row_begin;
@@ -78,7 +80,7 @@ __device__ __forceinline__ void raise(int* status, int bit) { atomicOr(status, b
 // side by side (a binary search would be a chain of dependent reads, 0.5 us each).
 __device__ __forceinline__ int seq_of_row(const BatchView& b, int t, int lane) {
   int n = 0;
-  for (int i = lane; i < b.n_seq; i += 32) n += __ldg(b.row_begin + i + 1) <= t ? 1 : 0;
+  for (int i = lane; i < b.n_seq; i += 32) n += b.row_begin[i + 1] <= t ? 1 : 0;
   return __reduce_add_sync(0xffffffffu, n);
 }
 
@@ -120,12 +122,17 @@ template <> struct Half2Of<__nv_bfloat16> {
 
 // Eight consecutive elements as they lie in memory (half the registers of fp32 where they wait for something), and
 // as fp32.  `wide`: the address is 16-byte aligned.
+// The path: ordinary, past L1 (also of what a kernel in front has written), or the read-only one (of weights).
+enum class Path { kOrdinary, kL2, kReadOnly };
 template <typename T> struct Raw8 { uint32_t w[8 * sizeof(T) / 4]; };
-template <typename T>
+template <Path kPath = Path::kOrdinary, typename T>
 __device__ __forceinline__ void load8(const T* p, bool wide, Raw8<T>& x) {
   if (wide) {
 #pragma unroll
-    for (int i = 0; i < static_cast<int>(sizeof(x.w) / 16); ++i) *(reinterpret_cast<uint4*>(x.w) + i) = __ldg(reinterpret_cast<const uint4*>(p) + i);
+    for (int i = 0; i < static_cast<int>(sizeof(x.w) / 16); ++i) {
+      const uint4* const from = reinterpret_cast<const uint4*>(p) + i;
+      *(reinterpret_cast<uint4*>(x.w) + i) = kPath == Path::kL2 ? __ldcg(from) : kPath == Path::kReadOnly ? __ldg(from) : *from;
+    }
   } else {
     T* e = reinterpret_cast<T*>(x.w);
 #pragma unroll

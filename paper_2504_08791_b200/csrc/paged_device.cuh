@@ -37,7 +37,7 @@ __device__ __forceinline__ bool wait_segment(uint32_t bar, uint32_t parity) {
 // ---- what a row sees ------------------------------------------------------------------------------------------------
 // Bits for 32 positions from `pos` on.  a = index of the position among the rows of the step, negative in the context.
 __device__ __forceinline__ uint32_t low_bits(long long n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << static_cast<int>(n)) - 1u; }
-__device__ __forceinline__ uint32_t mask_word(const uint32_t* words, int n_words, long long i) { return i < n_words ? __ldg(words + i) : 0u; }
+__device__ __forceinline__ uint32_t mask_word(const uint32_t* words, int n_words, long long i) { return i < n_words ? words[i] : 0u; }
 __device__ __forceinline__ uint32_t tree_bits(const uint32_t* words, int n_words, long long a) {
   if (a <= -32) return 0xffffffffu;
   if (a < 0) return mask_word(words, n_words, 0) << static_cast<int>(-a) | low_bits(-a);
@@ -53,7 +53,7 @@ struct SegmentView {
   bool bad_pages;
 
   __device__ __forceinline__ bool page_ok(long long pos) const {
-    return static_cast<unsigned>(__ldg(table + (pos >> pool.page_shift))) < static_cast<unsigned>(pool.n_pages);
+    return static_cast<unsigned>(table[pos >> pool.page_shift]) < static_cast<unsigned>(pool.n_pages);
   }
   __device__ uint32_t good_pages(long long pos) const {      // pos < limit: a page id is read only where it is needed
     uint32_t w = 0;

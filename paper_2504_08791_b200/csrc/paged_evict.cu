@@ -49,7 +49,7 @@ struct Sizes {
   int n, m;
 };
 __device__ __forceinline__ Sizes sizes_of(const EvictArgs& a, int seq, int* length) {
-  const int n = __ldg(a.length + seq), keep = __ldg(a.keep + seq);
+  const int n = a.length[seq], keep = a.keep[seq];
   *length = n;
   if (n < 0 || keep < 0 || n > a.stride || n > (a.table_stride << a.pool.page_shift)) return {-1, 0};
   return {n, min(n, keep)};
@@ -129,7 +129,7 @@ __global__ void __launch_bounds__(kThreads) evict_choose_kernel(const __grid_con
   // layers 20 and 24, 64 in four 192 and 194, 500 in one 367 and 191.
   if (a.n_seq > 1 && a.n_seq <= kRanked) {
     int* const lengths = reinterpret_cast<int*>(s_hist[0]);
-    const int mine = tid < a.n_seq ? __ldg(a.length + tid) : 0;
+    const int mine = tid < a.n_seq ? a.length[tid] : 0;
     if (tid < a.n_seq) lengths[tid] = mine;
     __syncthreads();
     if (tid < a.n_seq) {
@@ -144,7 +144,7 @@ __global__ void __launch_bounds__(kThreads) evict_choose_kernel(const __grid_con
   int length;
   const Sizes z = sizes_of(a, seq, &length);
   const int n = z.n, m = z.m;
-  if (n < 0 && tid == 0 && layer == 0 && head == 0) raise(a.pool.status, length < 0 || __ldg(a.keep + seq) < 0 ? kBadRows : kBadSlot);
+  if (n < 0 && tid == 0 && layer == 0 && head == 0) raise(a.pool.status, length < 0 || a.keep[seq] < 0 ? kBadRows : kBadSlot);
   const int64_t at = item * a.stride;
   const float* const weight = a.weight + at;
   const int32_t* const born = a.born + at;
@@ -159,7 +159,7 @@ __global__ void __launch_bounds__(kThreads) evict_choose_kernel(const __grid_con
     return;
   }
   const bool some_recent = a.recent_from != nullptr;
-  const int recent_from = some_recent ? __ldg(a.recent_from + seq) : 0;
+  const int recent_from = some_recent ? a.recent_from[seq] : 0;
   auto make = [&](float w, int b) { return key_of(w, b < a.first || (some_recent && b >= recent_from)); };
   const int cached = min(n, a.cached);
   for (int i = tid; i < kBins; i += kThreads) s_hist[0][i] = s_hist[1][i] = 0;

@@ -29,7 +29,7 @@ struct HeadNorm {
 // gain / sqrt(mean x^2 + eps) and then turned; its lanes hold it whole, so the sum of squares is one butterfly over D / 16
 // lanes.  Pair i is turned by the position on its own axis, as a fraction of a turn in 64 bits.
 template <typename T, typename In, int D, int kWarps, int kMode>
-__global__ void __launch_bounds__(256) norm_kernel(PoolView pool, BatchView b, int layer, const In* __restrict__ q, const In* __restrict__ k, const In* __restrict__ v, int n_q_heads,
+__global__ void __launch_bounds__(256) norm_kernel(PoolView pool, BatchView b, int layer, const In* q, const In* k, const In* v, int n_q_heads,
                                                    int64_t q_stride, int64_t k_stride, int64_t v_stride, bool wide, const double* __restrict__ freq, T* __restrict__ q_out,
                                                    const __grid_constant__ HeadNorm norm) {
   constexpr int kPairs = D / 2, kItems = D / 16, kHeads = 32 / kItems, kStep = kWarps * kHeads;
@@ -46,16 +46,17 @@ __global__ void __launch_bounds__(256) norm_kernel(PoolView pool, BatchView b, i
   const In* const k_row = k + t * k_stride;
   const In* const v_row = v + t * v_stride;
   struct Item { Raw8<In> lo, hi; };
+  // 11,500 rows of prompts: past L1 71.6 us, through it 73.7
   auto load = [&](int h, Item& x) {
     if (h >= heads || (h < n_q_heads && !q)) return;
     if (h < turned) {
       const In* src = (h < n_q_heads ? q_row + h * D : k_row + (h - n_q_heads) * D) + kWide * c;
-      load8(src, wide, x.lo);
-      load8(src + kGap, wide, x.hi);
+      load8<Path::kL2>(src, wide, x.lo);
+      load8<Path::kL2>(src + kGap, wide, x.hi);
     } else {
       const In* src = v_row + (h - turned) * D + 16 * c;
-      load8(src, wide, x.lo);
-      load8(src + 8, wide, x.hi);
+      load8<Path::kL2>(src, wide, x.lo);
+      load8<Path::kL2>(src + 8, wide, x.hi);
     }
   };
   int h = (warp % kWarps) * kHeads + lane / kItems;
@@ -65,7 +66,7 @@ __global__ void __launch_bounds__(256) norm_kernel(PoolView pool, BatchView b, i
 
   const int s = seq_of_row(b, t, lane);
   if (s >= b.n_seq) return;            // padding
-  const int first = __ldg(b.row_begin + s), ctx = __ldg(b.ctx_len + s);
+  const int first = b.row_begin[s], ctx = b.ctx_len[s];
   if (t < first || first < 0 || ctx < 0) {
     if (lane == 0) raise(pool.status, kBadRows);
     return;
@@ -75,7 +76,7 @@ __global__ void __launch_bounds__(256) norm_kernel(PoolView pool, BatchView b, i
   for (int i = lane; i < kPairs; i += 32) {
     const int axis = norm.axis[i];
     int p = 0;                         // not turned: by an angle of 0
-    if (axis != PRIMA_AXIS_NONE) p = norm.positions ? __ldg(norm.positions + static_cast<int64_t>(axis) * b.n_tok + t) : b.pos ? __ldg(b.pos + t) : static_cast<int>(slot);
+    if (axis != PRIMA_AXIS_NONE) p = norm.positions ? norm.positions[static_cast<int64_t>(axis) * b.n_tok + t] : b.pos ? b.pos[t] : static_cast<int>(slot);
     const double turns = p * __ldg(freq + norm.rank[i]);
     float sn, cs;
     sincospif(static_cast<float>(2.0 * (turns - rint(turns))), &sn, &cs);
@@ -142,8 +143,8 @@ __global__ void __launch_bounds__(256) norm_kernel(PoolView pool, BatchView b, i
     if (from) {
       const float* const mine = is_q ? from + h * norm.q_gain_stride : from + (h - n_q_heads) * norm.k_gain_stride;
       if (mine != gain_of) {           // the same for every head, as a rule
-        load8(mine + kWide * c, norm.wide, gain[0]);
-        load8(mine + kWide * c + kGap, norm.wide, gain[1]);
+        load8<Path::kReadOnly>(mine + kWide * c, norm.wide, gain[0]);
+        load8<Path::kReadOnly>(mine + kWide * c + kGap, norm.wide, gain[1]);
         gain_of = mine;
       }
       const float f = rsqrtf(fmaf(sum, 1.f / D, norm.eps));

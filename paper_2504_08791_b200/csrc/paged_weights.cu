@@ -50,7 +50,7 @@ struct WeightsCursor {
   __device__ __forceinline__ int64_t positions(int64_t ctx_, int64_t nodes_) const { return min(ctx_ + nodes_, a.slots); }
   __device__ __forceinline__ int64_t per_head(int64_t n) const { return kOverhead + (n + kBlock - 1) / kBlock; }
   __device__ __forceinline__ bool read(int i) {
-    const int f = __ldg(a.b.row_begin + i), e = __ldg(a.b.row_begin + i + 1), c = __ldg(a.b.ctx_len + i);
+    const int f = a.b.row_begin[i], e = a.b.row_begin[i + 1], c = a.b.ctx_len[i];
     const bool ok = f >= 0 && e >= f && e <= a.b.n_tok && c >= 0;
     first = f;
     nodes = ok ? e - f : 0;
@@ -127,7 +127,7 @@ __device__ __forceinline__ bool sees(const WeightsArgs& a, int first, int node, 
 __device__ __forceinline__ float shift_of(const WeightsArgs& a, const WeightsWork& s, int row) {
   if (row >= s.nodes * a.group) return -INFINITY;
   const int node = row / a.group;
-  const float lse = __ldg(a.lse + (s.first + node) * a.n_q_heads + s.head * a.group + (row - node * a.group));
+  const float lse = a.lse[(s.first + node) * a.n_q_heads + s.head * a.group + (row - node * a.group)];
   return lse == -INFINITY ? -INFINITY : -lse * kLog2e;
 }
 // What position j of the sequence has had, and where it is to be.
@@ -137,7 +137,7 @@ __device__ __forceinline__ int64_t entry_of(const WeightsArgs& a, const WeightsW
 __device__ __forceinline__ void put_entry(const WeightsArgs& a, const WeightsWork& s, int j, float had, float sum) {
   const int64_t at = entry_of(a, s, j);
   a.weight_out[at] = j < s.ctx && a.weight_in ? fmaf(a.decay, had, sum) : sum;
-  if (a.born && j >= s.ctx) a.born[at] = a.b.pos ? __ldg(a.b.pos + s.first + (j - s.ctx)) : j;
+  if (a.born && j >= s.ctx) a.born[at] = a.b.pos ? a.b.pos[s.first + (j - s.ctx)] : j;
 }
 
 // ---- few rows -----------------------------------------------------------------------------------------------------------
@@ -192,7 +192,7 @@ __global__ void __launch_bounds__(256, kStreamCtas) weights_stream_kernel(const 
   bool more = false;
   auto read_page = [&]() {
     const int pos = next * kFewPos + half * box_rows, slot = pos >> shift;
-    page = more && lane < boxes && pos < from.n && slot < a.b.table_stride ? __ldg(a.b.table + from.seq * a.b.table_stride + slot) : -1;
+    page = more && lane < boxes && pos < from.n && slot < a.b.table_stride ? a.b.table[from.seq * a.b.table_stride + slot] : -1;
   };
   auto plan = [&]() {
     more = cursor.next(&from);
@@ -244,8 +244,8 @@ __global__ void __launch_bounds__(256, kStreamCtas) weights_stream_kernel(const 
         const uint32_t* src = reinterpret_cast<const uint32_t*>(static_cast<const T*>(a.q) + static_cast<int64_t>((s.first + node) * a.n_q_heads + s.head * a.group + (row - node * a.group)) * D) + t4;
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
-          q[n][k][0] = row < rows ? __ldg(src + 8 * k) : 0u;
-          q[n][k][1] = row < rows ? __ldg(src + 8 * k + 4) : 0u;
+          q[n][k][0] = row < rows ? src[8 * k] : 0u;
+          q[n][k][1] = row < rows ? src[8 * k + 4] : 0u;
         }
 #pragma unroll
         for (int e = 0; e < 2; ++e) down[n][e] = shift_of(a, s, row0 + 8 * n + 2 * t4 + e);
@@ -439,7 +439,7 @@ __global__ void __launch_bounds__(kBlockThreads, 1) weights_block_kernel(const _
       // The page that this lane's box of a block lies on, read a block ahead
       auto page_of = [&](int block) {
         const int pos = block * kTilePos + box * box_rows, slot = pos >> shift;
-        return panel < D / 64 && block < s.block1 && pos < s.n && slot < a.b.table_stride ? __ldg(table + slot) : -1;
+        return panel < D / 64 && block < s.block1 && pos < s.n && slot < a.b.table_stride ? table[slot] : -1;
       };
       int next_page = page_of(s.block0);
       for (int block = s.block0; block < s.block1; ++block) {

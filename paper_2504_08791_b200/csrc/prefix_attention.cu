@@ -112,11 +112,11 @@ struct PrefixRange {
 };
 __device__ __forceinline__ bool prefix_range(const PrefixArgs& a, int p, PrefixRange* out) {
   const BatchView& b = a.b;
-  const int s0 = __ldg(a.prefix.seq_begin + p), s1 = __ldg(a.prefix.seq_begin + p + 1), len = __ldg(a.prefix.len + p);
+  const int s0 = a.prefix.seq_begin[p], s1 = a.prefix.seq_begin[p + 1], len = a.prefix.len[p];
   *out = PrefixRange();
   if (s0 < 0 || s1 < s0 || s1 > b.n_seq || len < 0) return false;
   if (s1 == s0) return true;
-  const int first = __ldg(b.row_begin + s0), end = __ldg(b.row_begin + s1);
+  const int first = b.row_begin[s0], end = b.row_begin[s1];
   if (first < 0 || end < first || end > b.n_tok) return false;
   out->first = first;
   out->rows = end - first;
@@ -233,7 +233,7 @@ struct OwnSeq {
   long long limit = 0, per_head = 0;
 };
 __device__ __forceinline__ bool own_seq(const PrefixArgs& a, int i, OwnSeq* s) {
-  const int f = __ldg(a.b.row_begin + i), e = __ldg(a.b.row_begin + i + 1), c = __ldg(a.b.ctx_len + i);
+  const int f = a.b.row_begin[i], e = a.b.row_begin[i + 1], c = a.b.ctx_len[i];
   *s = OwnSeq();
   if (f < 0 || e < f || e > a.b.n_tok || c < 0) return false;
   s->first = f;
@@ -374,7 +374,7 @@ __device__ __forceinline__ void own_share(const CUtensorMap* k_map, const CUtens
   bool more = false;
   auto read_page = [&]() {
     const long long pos = static_cast<long long>(from.step0 + step) * kFewPos + half * box_rows;
-    page = more && lane < boxes && pos < from.limit ? __ldg(a.b.table + from.seq * a.b.table_stride + (pos >> shift)) : -1;
+    page = more && lane < boxes && pos < from.limit ? a.b.table[from.seq * a.b.table_stride + (pos >> shift)] : -1;
   };
   auto plan = [&]() {
     more = cursor.next(&from);
@@ -422,8 +422,8 @@ __device__ __forceinline__ void own_share(const CUtensorMap* k_map, const CUtens
       const uint32_t* src = reinterpret_cast<const uint32_t*>(static_cast<const T*>(a.q) + (static_cast<int64_t>(s.first + t0 + n) * a.n_q_heads + s.head * a.group + (y - n * a.group)) * D) + t4;
 #pragma unroll
       for (int k = 0; k < D / 16; ++k) {
-        qf[k][h] = x < s.rows ? __ldg(src + 8 * k) : 0u;
-        qf[k][2 + h] = x < s.rows ? __ldg(src + 8 * k + 4) : 0u;
+        qf[k][h] = x < s.rows ? src[8 * k] : 0u;
+        qf[k][2 + h] = x < s.rows ? src[8 * k + 4] : 0u;
       }
     }
     float o[D / 8][4], ref[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
@@ -550,16 +550,16 @@ __device__ __forceinline__ void write_places(const PrefixArgs& a, int warp, int 
     const int t = t0 + lane;
     // the warp looks the first token's sequence and prefix up, the others are not far behind
     int s = seq_of_row(a.b, t0, lane), p = 0;
-    for (int i = lane; i < a.prefix.n; i += 32) p += __ldg(a.prefix.seq_begin + i + 1) <= s ? 1 : 0;
+    for (int i = lane; i < a.prefix.n; i += 32) p += a.prefix.seq_begin[i + 1] <= s ? 1 : 0;
     p = __reduce_add_sync(0xffffffffu, p);
     if (t >= a.b.n_tok) continue;
-    while (s < a.b.n_seq && __ldg(a.b.row_begin + s + 1) <= t) ++s;
+    while (s < a.b.n_seq && a.b.row_begin[s + 1] <= t) ++s;
     OwnSeq seq;
     int4 x = make_int4(0, 0, -1, 0);
     if (s < a.b.n_seq && own_seq(a, s, &seq) && t >= seq.first) {
-      while (p < a.prefix.n && __ldg(a.prefix.seq_begin + p + 1) <= s) ++p;
+      while (p < a.prefix.n && a.prefix.seq_begin[p + 1] <= s) ++p;
       PrefixRange range;
-      const bool shares = p < a.prefix.n && __ldg(a.prefix.seq_begin + p) <= s && prefix_range(a, p, &range) && prefix_units(a.shape, range.len) > 0;
+      const bool shares = p < a.prefix.n && a.prefix.seq_begin[p] <= s && prefix_range(a, p, &range) && prefix_units(a.shape, range.len) > 0;
       x = make_int4(1, seq.first, shares ? range.first : -1, 0);
     }
     a.place[t] = x;

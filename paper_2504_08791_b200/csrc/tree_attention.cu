@@ -95,7 +95,7 @@ struct Cursor {
   int first = 0, nodes = 0, ctx = 0;
 
   __device__ __forceinline__ bool read(int i) {
-    const int f = __ldg(a.b.row_begin + i), e = __ldg(a.b.row_begin + i + 1), c = __ldg(a.b.ctx_len + i);
+    const int f = a.b.row_begin[i], e = a.b.row_begin[i + 1], c = a.b.ctx_len[i];
     const bool ok = f >= 0 && e >= f && e <= a.b.n_tok && c >= 0;
     first = f;
     nodes = ok ? e - f : 0;
@@ -726,7 +726,7 @@ __global__ void __launch_bounds__(128, StreamGeometry<D>::kCtas) tree_stream_ker
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const long long pos = pos_first + step * Geo::kStep + 8 * h;
-        page[h] = pos < pos_end ? __ldg(table + (pos >> a.pool.page_shift)) : -1;
+        page[h] = pos < pos_end ? table[pos >> a.pool.page_shift] : -1;
       }
     };
     auto load_step = [&](int step, int stage) {
