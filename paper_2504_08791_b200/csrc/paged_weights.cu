@@ -416,7 +416,10 @@ __global__ void __launch_bounds__(kBlockThreads, 1) weights_block_kernel(const _
     WeightsWork s;
     for (uint32_t i = 0;; ++i) {
       const bool more = cursor.next(&s);
-      if (i >= 2) wait_segment(bar_work_empty + 8 * (i & 1), (i / 2 - 1) & 1);
+      if (i >= 2 && !__all_sync(0xffffffffu, wait_segment(bar_work_empty + 8 * (i & 1), (i / 2 - 1) & 1))) {      // never seen; what others may still read stays
+        if (lane == 0) raise(status, kGaveUp);
+        break;
+      }
       if (lane == 0) {
         ctl->work[i & 1] = s;
         if (!more) ctl->work[i & 1].block0 = ctl->work[i & 1].block1 = 0;

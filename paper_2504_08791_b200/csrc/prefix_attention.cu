@@ -617,7 +617,10 @@ __device__ __forceinline__ void PrefixCta<D>::feed(const Maps& maps, PrefixCurso
     PrefixWork s;
     for (uint32_t i = 0;; ++i) {
       const bool more = cursor.next(&s);
-      if (i >= kPlanned) wait_segment(bar_seg_empty + 8 * (i % kPlanned), (i / kPlanned - 1) & 1);
+      if (i >= kPlanned && !__all_sync(0xffffffffu, wait_segment(bar_seg_empty + 8 * (i % kPlanned), (i / kPlanned - 1) & 1))) {      // never seen; what others may still read stays
+        if (lane == 0) raise(status, kGaveUp);
+        break;
+      }
       if (lane == 0) {
         ctl->seg[i % kPlanned] = s;
         if (!more) ctl->seg[i % kPlanned].n = 0;

@@ -257,7 +257,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_kernel(const __grid_constant
     s.kind = 0;
     for (uint32_t i = 0;; ++i) {
       const bool more = cursor.next(&s);
-      if (i >= kSegments) wait_segment(bar_seg_empty + 8 * (i % kSegments), (i / kSegments - 1) & 1);
+      if (i >= kSegments && !__all_sync(0xffffffffu, wait_segment(bar_seg_empty + 8 * (i % kSegments), (i / kSegments - 1) & 1))) {      // never seen; what others may still read stays
+        if (lane == 0) raise(status, kGaveUp);
+        break;
+      }
       if (lane == 0) {
         ctl->seg[i % kSegments] = s;
         if (!more) ctl->seg[i % kSegments].n = 0;
