@@ -2,7 +2,7 @@
 //
 //   y = gain * x / sqrt(mean x^2 + eps);  (y_a, y_b) of pair i turned by the angle p[axis i] * frequency[rank i]
 //
-// Rows are read and written once: bound by the copy (11,500 rows of prompts, 40 query and 8 KV heads of 128: 71 us, floor 50),
+// Rows are read and written once: bound by the copy (11,500 rows of prompts, 40 query and 8 KV heads of 128: 72 us, floor 50),
 // a few rows by the latency of looking their place up (one row 4.6 us).  Tried for many rows and slower: 24 resident warps
 // per SM by fewer registers 77 us, sines in shared memory 80, two or four warps a row 86 and 113.
 #include <algorithm>

@@ -3,9 +3,9 @@
 //   w[s][g][j] = decay * w_in[s][g][j] + sum over rows t of s and query heads h of g that see j of exp(scale q_th . k_jg - lse_th)
 //
 // With the log-sum-exp of the attention the probabilities need no pass of their own: one product, one exponential a pair, one
-// sum.  Few rows are bound by the keys (48 single tokens over up to 8192 positions, 40 and 8 heads of 128: 26.5 us, floor 18.2 at the
+// sum.  Few rows are bound by the keys (48 single tokens over up to 8192 positions, 40 and 8 heads of 128: 26.4 us, floor 18.2 at the
 // copy bandwidth), many by the exponentials, which the special-function units take at 16 a cycle and SM (64 rows of 64 heads
-// over 32,704 positions: 61 us, 31 of them exponentials at the least, 20.5 products).  Polynomials on the ordinary units for a
+// over 32,704 positions: 62 us, 31 of them exponentials at the least, 20.5 products).  Polynomials on the ordinary units for a
 // part of the exponentials gave 63 for 65 at that point and are not used.
 #include <algorithm>
 #include <cmath>
@@ -514,20 +514,25 @@ __global__ void __launch_bounds__(kBlockThreads, 1) weights_block_kernel(const _
     const int h = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
     const uint32_t t_s = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + 2 * h * kRowTile;
     uint32_t turn = 0, n_part = 0, unit_base = 0;
-    // Tile t of a stretch into place p of this group, in the background, and its rows' shifts.
+    // Tile t of a stretch into place p of this group, in the background, and its rows' shifts.  `empty`, a bit for each place: this
+    // thread's row adds nothing.
+    uint32_t empty = 0;
     auto load_tile = [&](const WeightsWork& s, int t, int p) {
       const int row0 = t * kRowTile, token0 = row0 / a.group;
       load_query_tile<T, D>(smem_u32(smem) + (2 * h + p) * Geo::kTileBytes, Geo::kPanel,
                             static_cast<const T*>(a.q) + (static_cast<int64_t>(s.first + token0) * a.n_q_heads + s.head * a.group) * D, row0 - token0 * a.group, a.group,
                             static_cast<int64_t>(a.n_q_heads) * D, s.nodes * a.group - row0, r);
-      ctl->shift[2 * h + p][r] = shift_of(a, s, t * kRowTile + r);
+      const float shift = shift_of(a, s, t * kRowTile + r);
+      ctl->shift[2 * h + p][r] = shift;
+      const bool none = shift == -INFINITY && t * kRowTile + r < s.nodes * a.group;      // rows behind the last one are zeros already
+      empty = (empty & ~(1u << p)) | (none ? 1u << p : 0u);
     };
     auto group_sync = [&]() { asm volatile("bar.sync %0, 128;" ::"r"(1 + h) : "memory"); };
     auto tile_ready = [&](int p) {
       asm volatile("cp.async.wait_all;" ::: "memory");
       fence_async_smem();
       group_sync();      // the group reads all shifts
-      if (ctl->shift[2 * h + p][r] == -INFINITY) {      // adds nothing: scores of 0, whatever its query holds
+      if (empty >> p & 1) {      // scores of 0, whatever the query holds
 #pragma unroll
         for (int c = 0; c < D / 8; ++c) *reinterpret_cast<uint4*>(smem + (2 * h + p) * Geo::kTileBytes + c / 8 * Geo::kPanel + r * 128 + c % 8 * 16) = make_uint4(0, 0, 0, 0);
         fence_async_smem();

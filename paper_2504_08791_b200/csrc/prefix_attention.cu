@@ -20,8 +20,8 @@
 // Every row of a tile sees the whole prefix, so masks are only needed at its end and at bad pages, and are the same for
 // all rows.  P is rounded to the cache's type as in tree attention.
 //
-// 192 rows of 64 and 8 heads of 128 over 32,765 positions: 266 us, 0.78 PFLOP/s; products alone 123 at the measured rate.  Neither
-// unit is full: the tensor pipe is active 40% of the time (a 128 x 128 x 16 product takes 64 cycles, a 128 x 64 x 16 one 48),
+// 192 rows of 64 and 8 heads of 128 over 32,765 positions: 264 to 272 us in a burst, 315 in a long run under the power limit (0.66
+// PFLOP/s); products alone 123 and 145 at the measured rates.  Neither unit is full: the tensor pipe is active 40% of the time (a 128 x 128 x 16 product takes 64 cycles, a 128 x 64 x 16 one 48),
 // the special-function units need half of a block's cycles, and the groups run in step and share both.  Slower, at the same
 // point: 128 positions a block 303, one thread for the products of both groups 317, two threads a row 291, a part of the
 // exponentials by polynomial 270, the next scores asked for before the exponentials 307 and more.  Smaller calls are bound by
@@ -38,13 +38,17 @@ namespace {
 constexpr int kPrefixThreads = 384;
 constexpr int kBlock = 64;              // positions whose scores are one product
 constexpr int kPlanned = 4;            // segments ahead
-constexpr int kPrefixSegmentCost = 4;  // in places; 64 rows over 8192 positions: 60 us with 1, 56 with 4, 58 with 8
+// In places.  With 1, 4, 8: 64 rows over 8192 positions 61, 58, 59 us, three prefixes 36, 35, 35 (heads of 64), 56, 48, 46 (of 128), 192
+// rows over 32,765 positions 268, 264, 264, of heads of 64 229, 228, 250.
+constexpr int kPrefixSegmentCost = 4;
 // Registers of a thread: the two groups that hold scores (or the fragments of the streaming body), and the third one.  Their
-// sum is what the block is launched with: 384 x 168 = 256 x 208 + 128 x 88.
+// sum is what the block is launched with: 384 x 168 = 256 x 208 + 128 x 88.  18 to 20 registers are
+// spilled (half of the joining kernel's forms spill one or two).
 constexpr int kManyRegisters = 208, kFewRegisters = 88;
 
-// What a step of 16 own positions costs, in 64ths of a prefix's place.  For heads of 128, three prefixes and 192 rows over
-// 32,765 positions: 6 gives 38 and 312 us, 10 33 and 266, 16 35 and 274.
+// What a step of 16 own positions costs, in 64ths of a prefix's place.  Heads of 128, 6, 10 and 16: three prefixes 50, 48, 52 us, 64
+// rows over 8192 positions 59, 58, 66, 192 rows over 32,765 positions 309, 264, 272; 32 requests of 900 to 1900 positions behind 2000,
+// which are mostly own ones, 58, 67, 84.  Heads of 64, 3, 6 and 10, the same: 44, 35, 35; 51, 40, 43; 420, 228, 225; 43, 42, 51.
 constexpr int kOwnCost128 = 10, kOwnCost64 = 6;
 
 struct PrefixView {
