@@ -409,8 +409,9 @@ int prima_paged_append(prima_paged* pool, int layer, const prima_paged_batch* ba
  * several axes (text: one; images and video: time, height, width).  Head h of row t becomes
  *     y_d = gain_d * x_d / sqrt(sum_d x_d^2 / head_dim + eps)
  * (unchanged without a gain), and pair i of it is turned by the angle positions[axis[i]][t] * theta^(-2 rank[i] / head_dim),
- * or not at all where axis[i] is PRIMA_AXIS_NONE.  Values are not normed and not turned.  Sums and products in 32 bits,
- * rounded once to the cache's type; a row's slot in the cache is ctx_len + index as ever, whatever its positions. */
+ * or not at all where axis[i] is PRIMA_AXIS_NONE (by an angle of 0: both members of the pair must be finite).  Values are not
+ * normed and not turned.  Sums and products in 32 bits, rounded once to the cache's type; a row's slot in the cache is
+ * ctx_len + index as ever, whatever its positions. */
 #define PRIMA_AXIS_NONE 255
 #define PRIMA_MAX_AXES 4
 typedef struct {
@@ -450,8 +451,9 @@ int prima_tree_attention(prima_paged* pool, int layer, const prima_paged_batch* 
  * (once per 256 of a KV head's rows).  Slots and ctx_len of a sequence count its own positions alone; where the rotation is
  * to go on behind the prefix, the append needs `pos`.  out, lse, q, scale, masks, types and refusals as there; n_tok *
  * n_q_heads below 2^31.  A prefix with a negative length or a bad range of sequences or rows counts as none (and raises a
- * status bit), positions behind its table are not seen.  The value of a position that is seen must be finite.  A row with a
- * NaN among its scores is NaN, and its log-sum-exp too.
+ * status bit; where seq_begin does not ascend, the rows behind the others may hold anything), positions behind its table are
+ * not seen.  The value of a position that is seen must be finite.  A row with a NaN among its scores is NaN, and its
+ * log-sum-exp too.
  * workspace as there, of the bytes that prima_prefix_attention_workspace names (room for the prefix's and the own part of
  * every row's output in 32 bits, among others). */
 typedef struct {

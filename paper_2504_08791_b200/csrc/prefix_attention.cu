@@ -1234,9 +1234,9 @@ int prima_prefix_attention(prima_paged* p, int layer, const prima_paged_batch* b
   a.part_ml = reinterpret_cast<float2*>(take(2 * sm * kPrefixRows * 8));
   // Few rows of a sequence: its own positions are streamed beside the prefixes.  Many: tree attention's tensor-memory kernel
   // is the better one for them (its rule), and runs in front.  Beside against in front, 8 KV heads of 128: 16 sequences of 500
-  // behind 4096 positions, 16 rows 30 and 44 us, 32 rows 41 and 54, 64 rows 68 and 69; 64 of 300 behind 2000, 32 rows 88 and
-  // 103, 64 rows 156 and 140.  Own positions longer than the prefix, which the host does not know, would like it earlier: 16 of
-  // 3000 behind 1000, 4 rows 73 and 65, 32 rows 121 and 90 (heads of 64: 59 and 66).
+  // behind 4096 positions, 16 rows 31 and 45 us, 32 rows 42 and 54, 64 rows 69 and 70; 64 of 300 behind 2000, 32 rows 90 and
+  // 103, 64 rows 160 and 140.  Own positions longer than the prefix, which the host does not know, would like it earlier: 16 of
+  // 3000 behind 1000, 4 rows 73 and 65, 32 rows 122 and 91 (heads of 64: 59 and 66).
   a.own_cost = streams(a.b, group) ? (dim == 128 ? kOwnCost128 : kOwnCost64) : 0;
   if (a.own_cost) {
     a.own_part_o = reinterpret_cast<float*>(take(16 * sm * kFewRows * dim * 4));
